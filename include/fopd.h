@@ -119,6 +119,9 @@ typedef enum {
 #define FOPD_DEV_BAD_LENGTH 8   /* seq_len <= 0 or aligned count > seq_len      */
 #define FOPD_DEV_TIMEOUT 16     /* a bounded in-kernel wait ran out; results of
                                    that call are not to be trusted               */
+#define FOPD_DEV_BAD_LOGITS 32  /* a row to draw from holds NaN or +inf, or no finite logit */
+#define FOPD_DEV_BAD_UNIFORM 64 /* a given random number outside [0, 1)         */
+#define FOPD_DEV_NONFINITE 128  /* the gradients' norm is infinite or NaN       */
 
 /* alpha, beta >= 0 scale the two drift diagnostics (Eq. 11); xi is the gate
  * threshold (Eq. 13); lambda weights the rollout anchor (Eq. 16).  The paper
@@ -446,6 +449,112 @@ int fopd_shard_merge(const float *partials, int32_t n_parts, const fopd_chunk *r
 int fopd_shard_loss_fwd_bwd(const fopd_chunk *shard, int64_t vocab_offset, int64_t vocab_total,
                             int32_t B, const float *coef, const float *row_ws, fopd_params p,
                             void *dlogits, double *loss_acc, void *stream);
+
+/*
+ * Rollout: where a chunk's tokens and behaviour log-probs come from (the data y_{i,h} ~ pi^{r(i)}
+ * of Sec. 3.1 and their log pi^{r(i)}; Sec. 4.1 needs both).
+ *
+ * Both entry points below take the random numbers as input (fp64, in [0, 1)) and work on
+ * p = softmax(logits / temperature), 2^-10 <= temperature <= 2^10, or, with temperature = 0, on the
+ * distribution that has everything on the lowest index of the largest logit.  Logits may be -infinity
+ * (banned tokens: probability 0); the columns behind `vocab` in a row are not read.  Tokens are those of
+ * exact arithmetic: the sweeps run in fp32 with a bound on their error, and whatever the bound does not
+ * decide is decided again in fp64 (error ~1e-13 of a row's sum).  A row that is needed and holds NaN or
+ * +infinity, or nothing but -infinity, sets FOPD_DEV_BAD_LOGITS, a number outside [0, 1) that is needed
+ * FOPD_DEV_BAD_UNIFORM; that row's (sequence's) token is then -1 with log-prob 0 and mask 0.
+ */
+
+/*
+ * Draws one token from each row: tokens[n] = min { i : sum_{k <= i} p_k > uniform[n] }, the inverse of
+ * the distribution function, and logprob[n] = log p_{tokens[n]}.
+ *
+ *   logits    [n_rows, vocab] at a pitch of row_stride elements, layout rules of fopd_chunk
+ *   uniform   [n_rows] fp64
+ *   tokens    [n_rows] int32;  logprob [n_rows] fp32 or NULL
+ *   status    device int32 status word, or NULL
+ */
+int fopd_draw_tokens(const void *logits, const double *uniform, int64_t n_rows, int64_t vocab,
+                     int64_t row_stride, int32_t dtype, float temperature, int32_t *tokens,
+                     float *logprob, int32_t *status, void *stream);
+
+/* Drafts of B sequences, up to K each, with the logits rows they are checked against. */
+typedef struct {
+  const void *target;     /* [B, K + 1, vocab]: row j of a sequence belongs to its draft j, the row behind the
+                             last draft to the token that follows when all drafts are accepted         */
+  const void *draft;      /* [B, K, vocab] rows the drafts were drawn from, or NULL: every draft was certain
+                             (looked up, or drawn greedily: q = 1 on the drafted token, 0 elsewhere)    */
+  const int32_t *tokens;  /* [B, K] drafted tokens x_j                                                  */
+  const int32_t *n_draft; /* [B] drafts of each sequence, 0 <= n_draft <= K, or NULL: K for all         */
+  const double *uniform;  /* [B, K + 1]: u_j decides on draft j, the last column draws the new token    */
+  int64_t vocab;
+  int64_t target_seq_stride, target_row_stride; /* in elements; row strides >= vocab                    */
+  int64_t draft_seq_stride, draft_row_stride;
+  int32_t B, K;           /* B >= 0, 0 <= K < 2^20                                                      */
+  int32_t dtype;          /* fopd_dtype of both                                                         */
+  float temperature;      /* of the target's distribution p                                             */
+  float draft_temperature; /* of the draft's distribution q                                             */
+} fopd_draft;
+
+/*
+ * Verifies drafted tokens so that what comes out is distributed as draws from the target alone:
+ * draft j is accepted while  u_j q_j(x_j) < p_j(x_j);  the first one that is not is replaced by a
+ * draw from  max(p_j - q_j, 0)  normalised (from p_j where that is zero everywhere), and behind n_draft
+ * accepted drafts comes a draw from p_{n_draft}.  Use: a rollout whose drafts come from a cheaper model,
+ * or a stale response checked against the policy that has moved on since (what a refresh of the buffer
+ * asks for).  The outputs are rows of a fopd_chunk: tokens, behaviour log-probs and mask of the B (K + 1)
+ * target rows.
+ *
+ *   tokens      [B, K + 1] int32: accepted drafts, the new token, then -1
+ *   logprob     [B, K + 1] fp32: log p_j of each of these tokens, 0 behind them, or NULL
+ *   mask        [B, K + 1] uint8: 1 where there is a token, or NULL
+ *   n_accepted  [B] int32: accepted drafts, or NULL
+ *
+ * A drafted token outside [0, vocab) sets FOPD_DEV_BAD_TOKEN and is rejected; n_draft outside [0, K] sets
+ * FOPD_DEV_BAD_LENGTH and is taken as the nearer bound.  Only what is reached counts: rows behind the
+ * first rejection may hold anything.  Long drafts (a whole response) cost the rows that are reached and
+ * those in flight when the rejection is found.  With K = 0 draft, tokens and n_draft are not used.
+ */
+int fopd_verify_draft(const fopd_draft *d /* HOST */, int32_t *tokens, float *logprob, uint8_t *mask,
+                      int32_t *n_accepted, int32_t *status, void *stream);
+
+/*
+ * Norm and clipping of a set of gradients (the chunks' dlogits, or the parameters' gradients behind them:
+ * the step between Algorithm 1's gradient and its update).  With g all elements of all tensors:
+ *
+ *   norm = sqrt(sum g^2),   coef = min(1, max_norm / norm),   out = coef g  (rounded once to the type).
+ *
+ * Nothing is added to the norm before the division: a set above max_norm comes out with norm max_norm.
+ * Squares are formed and summed in fp64 in a fixed order: no overflow, reproducible bit for bit.
+ */
+typedef struct {
+  const void *data;   /* [rows, cols] at a pitch of row_stride elements; aligned to its element          */
+  void *out;          /* same layout: where the scaled gradient goes; NULL or data: in place             */
+  int64_t rows, cols, row_stride; /* row_stride >= cols where rows > 1; rows or cols may be 0             */
+  int32_t dtype;      /* fopd_dtype, tensor by tensor                                                     */
+  int32_t reserved;   /* 0                                                                                */
+} fopd_tensor;
+
+/* Doubles of the workspace ws (DEVICE, 16-byte aligned), zeroed by the caller before the first use of a
+ * set.  ws[0] is the sum of squares so far; the rest belongs to the library.  Calls that share a workspace
+ * are ordered by the caller (one stream). */
+#define FOPD_GRAD_WS 2048
+#define FOPD_GRAD_WS_SUM 0
+
+/* ws[0] += sum of squares of the set; norm[0] (fp32, or NULL) = sqrt(ws[0]).  A set may come in several calls
+ * (chunk by chunk), and ws[0] may be all-reduced before the next call.  `out` is not used. */
+int fopd_grad_norm(const fopd_tensor *tensors /* HOST */, int32_t n_tensors, double *ws, float *norm,
+                   int32_t *status, void *stream);
+
+/* out = coef data with coef from ws[0] and max_norm (finite, > 0); coef[0], norm[0] fp32 or NULL.  With coef = 1
+ * in place nothing is read or written.  If the norm is infinite or NaN, FOPD_DEV_NONFINITE is set, coef is 1 and
+ * the values are left (or copied) as they are.  Elements of two tensors of the set must not overlap, nor those of
+ * an `out` and another tensor's data (FOPD_ERR_ALIAS where address ranges show it). */
+int fopd_grad_scale(const fopd_tensor *tensors /* HOST */, int32_t n_tensors, double *ws, float max_norm,
+                    float *norm, float *coef, int32_t *status, void *stream);
+
+/* Both in one call for a set that is all there: ws[0] is set (not added to), then the set is scaled. */
+int fopd_grad_clip(const fopd_tensor *tensors /* HOST */, int32_t n_tensors, double *ws, float max_norm,
+                   float *norm, float *coef, int32_t *status, void *stream);
 
 /*
  * Gives back what the library holds on the current device between calls: trims

@@ -23,8 +23,10 @@ EXPORTS = (
     "fopd_token_stats_static", "fopd_loss_fwd_bwd_plan", "fopd_row_divergence", "fopd_supervision_drift",
     "fopd_refresh_decision", "fopd_shard_stats", "fopd_shard_merge", "fopd_shard_loss_fwd_bwd",
     "fopd_loss_fwd_bwd_set_plan", "fopd_release_device_memory", "fopd_selftest_bounded_wait",
-    "fopd_token_stats_student",
+    "fopd_token_stats_student", "fopd_draw_tokens", "fopd_verify_draft", "fopd_grad_norm", "fopd_grad_scale",
+    "fopd_grad_clip",
 )
+GRAD_WS = 2048  # doubles of the workspace of fopd_grad_norm, fopd_grad_scale and fopd_grad_clip
 
 
 class FopdError(RuntimeError):
@@ -51,6 +53,20 @@ class fopd_host_outputs(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in
                 ("f", "w", "d_roll", "l_distill", "m_align", "per_sample_loss", "buffer_means", "loss",
                  "status_bits", "copied_bytes")]
+
+
+class fopd_draft(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("target", "draft", "tokens", "n_draft", "uniform")] + \
+        [(n, ctypes.c_int64) for n in ("vocab", "target_seq_stride", "target_row_stride", "draft_seq_stride",
+                                       "draft_row_stride")] + \
+        [("B", ctypes.c_int32), ("K", ctypes.c_int32), ("dtype", ctypes.c_int32), ("temperature", ctypes.c_float),
+         ("draft_temperature", ctypes.c_float)]
+
+
+class fopd_tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -93,6 +109,11 @@ def lib() -> ctypes.CDLL:
         L.fopd_step_host.argtypes = [ctypes.POINTER(fopd_chunk), i32, i32, vp, vp, vp, fopd_params,
                                      ctypes.POINTER(ctypes.c_void_p), ctypes.POINTER(fopd_host_outputs), vp,
                                      ctypes.c_uint64, vp]
+        L.fopd_draw_tokens.argtypes = [vp, vp, i64, i64, i64, i32, f32, vp, vp, vp, vp]
+        L.fopd_verify_draft.argtypes = [ctypes.POINTER(fopd_draft), vp, vp, vp, vp, vp, vp]
+        L.fopd_grad_norm.argtypes = [vp, i32, vp, vp, vp, vp]
+        L.fopd_grad_scale.argtypes = [vp, i32, vp, f32, vp, vp, vp, vp]
+        L.fopd_grad_clip.argtypes = [vp, i32, vp, f32, vp, vp, vp, vp]
         for name in EXPORTS:
             getattr(L, name)
         _lib = L
@@ -292,6 +313,152 @@ def fopd_shard_loss_fwd_bwd(shard: Chunk, vocab_offset: int, vocab_total: int, B
     _check(lib().fopd_shard_loss_fwd_bwd(ctypes.byref(c), int(vocab_offset), int(vocab_total), B, _ptr(coef),
                                          _ptr(row_ws), p, _ptr(dlogits), _ptr(loss_acc), _stream(stream)),
            "fopd_shard_loss_fwd_bwd")
+
+
+def _dtype(t: torch.Tensor) -> int:
+    if t.dtype == torch.bfloat16:
+        return FOPD_BF16
+    assert t.dtype == torch.float32, t.dtype
+    return FOPD_F32
+
+
+def _check_out(t, dtype, shape, device):
+    """An output (or None): the entry points write whole contiguous arrays on the current device."""
+    assert t is None or (t.dtype == dtype and t.shape == shape and t.is_contiguous() and t.device == device)
+
+
+def _check_status_word(status, device):
+    assert status is None or (status.dtype == torch.int32 and status.numel() >= 1 and status.device == device)
+
+
+def _on_current_device(t):
+    """The library launches on the current device."""
+    assert t.is_cuda and t.device.index == torch.cuda.current_device(), t.device
+
+
+def fopd_draw_tokens(logits, uniform, tokens, *, logprob=None, temperature=1.0, vocab=None, status=None, stream=None):
+    """One token from each row of ``logits`` [n, V] by the given fp64 numbers ``uniform`` [n]: the
+    inverse of the distribution function of softmax(logits / temperature) (temperature 0: the best
+    token).  ``tokens`` int32 [n], ``logprob`` fp32 [n] or None."""
+    assert logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] <= 1)
+    n, cols = logits.shape
+    dev = logits.device
+    _on_current_device(logits)
+    assert uniform.dtype == torch.float64 and uniform.shape == (n,) and uniform.is_contiguous() and uniform.device == dev
+    _check_out(tokens, torch.int32, (n,), dev)
+    _check_out(logprob, torch.float32, (n,), dev)
+    _check_status_word(status, dev)
+    assert vocab is None or 0 < vocab <= cols
+    per = 16 // logits.element_size()
+    pitch = logits.stride(0) if n > 1 else -(-cols // per) * per
+    _check(lib().fopd_draw_tokens(logits.data_ptr(), uniform.data_ptr(), n, vocab or cols, pitch, _dtype(logits),
+                                  temperature, tokens.data_ptr(), _ptr(logprob), _ptr(status), _stream(stream)),
+           "fopd_draw_tokens")
+
+
+def fopd_verify_draft(target, draft, draft_tokens, uniform, tokens, *, n_draft=None, logprob=None, mask=None,
+                      n_accepted=None, temperature=1.0, draft_temperature=1.0, vocab=None, status=None, stream=None):
+    """Verification of drafted tokens (see ``fopd_verify_draft`` in fopd.h): ``target`` [B, K + 1, V],
+    ``draft`` [B, K, V] or None (certain drafts), ``draft_tokens`` int32 [B, K], ``uniform`` fp64
+    [B, K + 1], ``n_draft`` int32 [B] or None.  Outputs ``tokens`` int32, ``logprob`` fp32 and ``mask``
+    uint8 [B, K + 1], ``n_accepted`` int32 [B]; all but the first may be None."""
+    assert target.dim() == 3 and (target.stride(2) == 1 or target.shape[2] <= 1)
+    B, W, cols = target.shape
+    K, dev = W - 1, target.device
+    _on_current_device(target)
+    assert draft_tokens.dtype == torch.int32 and draft_tokens.shape == (B, K) and draft_tokens.is_contiguous()
+    assert uniform.dtype == torch.float64 and uniform.shape == (B, W) and uniform.is_contiguous()
+    assert draft_tokens.device == dev and uniform.device == dev
+    if draft is not None:
+        assert draft.shape == (B, K, cols) and draft.dtype == target.dtype and draft.device == dev
+        assert draft.stride(2) == 1 or cols <= 1
+    if n_draft is not None:
+        assert n_draft.dtype == torch.int32 and n_draft.shape == (B,) and n_draft.is_contiguous() and n_draft.device == dev
+    _check_out(tokens, torch.int32, (B, W), dev)
+    _check_out(logprob, torch.float32, (B, W), dev)
+    _check_out(mask, torch.uint8, (B, W), dev)
+    _check_out(n_accepted, torch.int32, (B,), dev)
+    _check_status_word(status, dev)
+    assert vocab is None or 0 < vocab <= cols
+    d = fopd_draft(target.data_ptr(), None if draft is None else draft.data_ptr(), draft_tokens.data_ptr(),
+                   None if n_draft is None else n_draft.data_ptr(), uniform.data_ptr(), vocab or cols,
+                   target.stride(0), target.stride(1), 0 if draft is None else draft.stride(0),
+                   0 if draft is None else draft.stride(1), B, K, _dtype(target), temperature, draft_temperature)
+    _check(lib().fopd_verify_draft(ctypes.byref(d), tokens.data_ptr(), _ptr(logprob), _ptr(mask), _ptr(n_accepted),
+                                   _ptr(status), _stream(stream)), "fopd_verify_draft")
+
+
+def _as_rows(t: torch.Tensor):
+    """(rows, cols, pitch) under which the elements of ``t`` lie in memory, in any order; None if they do not."""
+    dims = sorted((st, n) for n, st in zip(t.shape, t.stride()) if n != 1)
+    if t.numel() == 0:
+        return 0, 0, 0
+    cols = 1
+    while dims and dims[0][0] == cols:
+        cols *= dims.pop(0)[1]
+    if not dims:
+        return 1, cols, cols
+    pitch, rows = dims[0][0], 1
+    while dims and dims[0][0] == pitch * rows:
+        rows *= dims.pop(0)[1]
+    return (rows, cols, pitch) if not dims and pitch >= cols else None
+
+
+class GradientList:
+    """The tensors of one fopd_grad_* call, marshalled once: keep it as long as the tensors keep their
+    memory (it holds them).  bf16 and fp32, mixed; dense in any order of dimensions, or rows at a pitch.
+    ``outs``: where the scaled values go (same shapes, types and strides); None: in place."""
+
+    def __init__(self, tensors, outs=None):
+        self.tensors, self.outs = list(tensors), None if outs is None else list(outs)
+        assert self.outs is None or len(self.outs) == len(self.tensors)
+        self.n = len(self.tensors)
+        self.array = (fopd_tensor * max(1, self.n))()
+        self.device = self.tensors[0].device if self.n else None
+        for i, t in enumerate(self.tensors):
+            _on_current_device(t)
+            layout = _as_rows(t)
+            assert layout is not None, f"tensor {i}: strides {t.stride()} of shape {tuple(t.shape)}"
+            o = None if self.outs is None else self.outs[i]
+            assert o is None or (o.shape == t.shape and o.dtype == t.dtype and o.device == t.device and
+                                 (o.stride() == t.stride() or (o.is_contiguous() and t.is_contiguous())))
+            assert self.device == t.device
+            self.array[i] = fopd_tensor(t.data_ptr(), None if o is None else o.data_ptr(), *layout, _dtype(t), 0)
+
+
+def grad_workspace(device) -> torch.Tensor:
+    """The fopd_grad_* workspace of one set: fp64, zeroed."""
+    return torch.zeros(GRAD_WS, dtype=torch.float64, device=device)
+
+
+def _grad_args(grads, ws, status, scalars):
+    assert ws.dtype == torch.float64 and ws.numel() >= GRAD_WS and ws.is_contiguous()
+    _on_current_device(ws)
+    assert grads.device is None or grads.device == ws.device
+    _check_status_word(status, ws.device)
+    for t in scalars:
+        assert t is None or (t.dtype == torch.float32 and t.numel() >= 1 and t.device == ws.device)
+
+
+def fopd_grad_norm(grads: GradientList, ws, *, norm=None, status=None, stream=None):
+    """ws[0] += sum of squares; ``norm`` fp32 [1] = sqrt(ws[0])."""
+    _grad_args(grads, ws, status, (norm,))
+    _check(lib().fopd_grad_norm(grads.array, grads.n, ws.data_ptr(), _ptr(norm), _ptr(status), _stream(stream)),
+           "fopd_grad_norm")
+
+
+def fopd_grad_scale(grads: GradientList, ws, max_norm, *, norm=None, coef=None, status=None, stream=None):
+    """Every element times min(1, max_norm / sqrt(ws[0])), into ``outs`` or in place."""
+    _grad_args(grads, ws, status, (norm, coef))
+    _check(lib().fopd_grad_scale(grads.array, grads.n, ws.data_ptr(), float(max_norm), _ptr(norm), _ptr(coef),
+                                 _ptr(status), _stream(stream)), "fopd_grad_scale")
+
+
+def fopd_grad_clip(grads: GradientList, max_norm, ws, *, norm=None, coef=None, status=None, stream=None):
+    """Norm of the whole set and scaling in one call."""
+    _grad_args(grads, ws, status, (norm, coef))
+    _check(lib().fopd_grad_clip(grads.array, grads.n, ws.data_ptr(), float(max_norm), _ptr(norm), _ptr(coef),
+                                _ptr(status), _stream(stream)), "fopd_grad_clip")
 
 
 def fopd_check_status(status, stream=None) -> int:

@@ -1,0 +1,180 @@
+// Norm and clipping of a set of tensors: sum of squares over all of them, then every element
+// times min(1, max_norm / norm).  Both are streams over memory; the set's table travels in the
+// kernel parameters, so a call needs no device-side table, no copy and no allocation.
+#pragma once
+
+#include "common.cuh"
+
+namespace fopd {
+
+constexpr int kClipThreads = 256;
+constexpr int kClipTileBytes = 32768;  // a CTA's piece of a row of a tensor
+constexpr int kClipMaxGrid = 1480;     // partial sums of a launch fit the workspace
+constexpr int kClipTicket = 1;         // ws[1]: counter of finished CTAs (left at zero by every launch)
+constexpr int kClipPartials = 8;       // ws[8 ..]: partial sums, one per CTA
+static_assert(kClipPartials + kClipMaxGrid <= FOPD_GRAD_WS, "the workspace holds the partial sums");
+
+struct ClipEntry {
+  const char *data;
+  char *out;
+  int64_t cols, row_stride;  // elements
+  int64_t tile0;             // first tile of this tensor in the launch
+  int32_t tiles_per_row, dtype;
+};
+
+template <int N>
+struct ClipTable {
+  int64_t n_tiles;
+  int32_t n;
+  ClipEntry e[N];
+};
+
+// The tensor a tile belongs to (the last one whose first tile is not behind it).
+template <int N>
+__device__ __forceinline__ int find_entry(const ClipTable<N> &t, int64_t tile) {
+  int lo = 0, hi = t.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (t.e[mid].tile0 <= tile) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+// A tile as a range of elements: [off, off + n) behind the tensor's base.
+struct ClipTile {
+  int64_t off;
+  int n;
+};
+__device__ __forceinline__ ClipTile tile_range(const ClipEntry &e, int64_t tile) {
+  const int64_t local = tile - e.tile0;
+  const int64_t row = local / e.tiles_per_row, piece = local % e.tiles_per_row;
+  const int per = kClipTileBytes / (e.dtype == FOPD_BF16 ? 2 : 4);
+  const int64_t left = e.cols - piece * per;
+  return {row * e.row_stride + piece * per, (int)(left < per ? left : per)};
+}
+
+// Sum of squares of n elements at p, per thread, in fp64 (|g| up to 3e38: its square is out of fp32's range).
+template <int DT>
+__device__ __forceinline__ double tile_squares(const char *p, int n) {
+  using E = Elem<DT>;
+  constexpr int P = E::kPerVec;
+  // elements before the first 16-byte boundary, whole vectors, the rest
+  int head = (int)(((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / E::kBytes);
+  if (head > n) head = n;
+  const int nvec = (n - head) / P;
+  const uint4 *v = reinterpret_cast<const uint4 *>(p + (size_t)head * E::kBytes);
+  double s = 0.0;
+  for (int i = threadIdx.x; i < nvec; i += kClipThreads) {
+    float x[P];
+    E::unpack(ld_stream(v + i), x);
+#pragma unroll
+    for (int k = 0; k < P; ++k) s = fma((double)x[k], (double)x[k], s);
+  }
+  const int tail0 = head + nvec * P;
+  const int k = (int)threadIdx.x < head ? (int)threadIdx.x : tail0 + ((int)threadIdx.x - head);
+  if (k < n) {
+    const double x = (double)E::load1(p, k);
+    s = fma(x, x, s);
+  }
+  return s;
+}
+
+// grid <= kClipMaxGrid.  The CTAs' partial sums go to the workspace; the last CTA to finish adds them in the order
+// of the CTAs.  set != 0: ws[0] = the sum, else ws[0] += it.
+template <int N>
+__global__ void __launch_bounds__(kClipThreads)
+    grad_norm_kernel(const __grid_constant__ ClipTable<N> t, double *ws, int set, float *norm, int32_t *status) {
+  __shared__ double sh[kClipThreads];
+  __shared__ int last;
+  double s = 0.0;
+  for (int64_t tile = blockIdx.x; tile < t.n_tiles; tile += gridDim.x) {
+    const ClipEntry &e = t.e[find_entry(t, tile)];
+    const ClipTile r = tile_range(e, tile);
+    s += e.dtype == FOPD_BF16 ? tile_squares<FOPD_BF16>(e.data + r.off * 2, r.n)
+                              : tile_squares<FOPD_F32>(e.data + r.off * 4, r.n);
+  }
+  sh[threadIdx.x] = s;
+  __syncthreads();
+  for (int off = kClipThreads / 2; off > 0; off >>= 1) {
+    if ((int)threadIdx.x < off) sh[threadIdx.x] += sh[threadIdx.x + off];
+    __syncthreads();
+  }
+  unsigned long long *ticket = reinterpret_cast<unsigned long long *>(ws + kClipTicket);
+  if (threadIdx.x == 0) {
+    ws[kClipPartials + blockIdx.x] = sh[0];
+    __threadfence();
+    last = atomicAdd(ticket, 1ull) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  double v = 0.0;
+  for (int i = threadIdx.x; i < (int)gridDim.x; i += kClipThreads) v += __ldcg(ws + kClipPartials + i);
+  sh[threadIdx.x] = v;
+  __syncthreads();
+  for (int off = kClipThreads / 2; off > 0; off >>= 1) {
+    if ((int)threadIdx.x < off) sh[threadIdx.x] += sh[threadIdx.x + off];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    const double total = set ? sh[0] : ws[FOPD_GRAD_WS_SUM] + sh[0];
+    ws[FOPD_GRAD_WS_SUM] = total;
+    *ticket = 0;
+    if (norm) norm[0] = (float)sqrt(total);
+    if (status && !(total <= 1.7976931348623157e308)) atomicOr(status, FOPD_DEV_NONFINITE);
+  }
+}
+
+// coef of a sum of squares (see fopd_grad_scale); 1 where the norm is not finite.
+__device__ __forceinline__ float clip_coef(double sum, float max_norm) {
+  const double norm = sqrt(sum);
+  return norm > (double)max_norm && norm <= 1.7976931348623157e308 ? (float)((double)max_norm / norm) : 1.f;
+}
+
+template <int DT>
+__device__ __forceinline__ void tile_scale(const char *p, char *o, int n, float c) {
+  using E = Elem<DT>;
+  constexpr int P = E::kPerVec;
+  if (((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(o)) & 15) != 0) {  // no common vector boundary
+    for (int i = threadIdx.x; i < n; i += kClipThreads) E::store1(o, i, E::load1(p, i) * c);
+    return;
+  }
+  int head = (int)(((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / E::kBytes);
+  if (head > n) head = n;
+  const int nvec = (n - head) / P;
+  const uint4 *v = reinterpret_cast<const uint4 *>(p + (size_t)head * E::kBytes);
+  uint4 *w = reinterpret_cast<uint4 *>(o + (size_t)head * E::kBytes);
+  for (int i = threadIdx.x; i < nvec; i += kClipThreads) {
+    float x[P];
+    E::unpack(ld_stream(v + i), x);
+#pragma unroll
+    for (int k = 0; k < P; ++k) x[k] *= c;
+    st_stream(w + i, E::pack(x));
+  }
+  const int tail0 = head + nvec * P;
+  const int k = (int)threadIdx.x < head ? (int)threadIdx.x : tail0 + ((int)threadIdx.x - head);
+  if (k < n) E::store1(o, k, E::load1(p, k) * c);
+}
+
+template <int N>
+__global__ void __launch_bounds__(kClipThreads)
+    grad_scale_kernel(const __grid_constant__ ClipTable<N> t, const double *ws, float max_norm, float *norm,
+                      float *coef, int32_t *status) {
+  const double sum = ws[FOPD_GRAD_WS_SUM];
+  const float c = clip_coef(sum, max_norm);
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (norm) norm[0] = (float)sqrt(sum);
+    if (coef) coef[0] = c;
+    if (status && !(sum <= 1.7976931348623157e308)) atomicOr(status, FOPD_DEV_NONFINITE);
+  }
+  for (int64_t tile = blockIdx.x; tile < t.n_tiles; tile += gridDim.x) {
+    const ClipEntry &e = t.e[find_entry(t, tile)];
+    if (c == 1.f && e.out == e.data) continue;
+    const ClipTile r = tile_range(e, tile);
+    if (e.dtype == FOPD_BF16) tile_scale<FOPD_BF16>(e.data + r.off * 2, e.out + r.off * 2, r.n, c);
+    else tile_scale<FOPD_F32>(e.data + r.off * 4, e.out + r.off * 4, r.n, c);
+  }
+}
+
+}  // namespace fopd

@@ -1,0 +1,184 @@
+// Gradient norm and clipping: argument checks, the set's table, launches.
+#include <algorithm>
+#include <vector>
+
+#include "clip_kernels.cuh"
+#include "host_common.cuh"
+
+using namespace fopd;
+
+namespace {
+
+// Tensors of one launch: the table is a kernel parameter (at most 32,764 bytes).  Small sets take the small table,
+// whose parameters are quicker to hand over.
+constexpr int kSmallTable = 64, kLargeTable = 580;
+
+int check_tensors(const fopd_tensor *t, int32_t n, const double *ws) {
+  if (n < 0) return FOPD_ERR_SIZE;
+  if (!ws || (n > 0 && !t)) return FOPD_ERR_NULL;
+  if (!aligned16(ws)) return FOPD_ERR_ALIGN;
+  for (int32_t i = 0; i < n; ++i) {
+    if (t[i].dtype != FOPD_BF16 && t[i].dtype != FOPD_F32) return FOPD_ERR_DTYPE;
+    const int64_t most = (int64_t)1 << 42, esz = t[i].dtype == FOPD_BF16 ? 2 : 4;
+    if (t[i].rows < 0 || t[i].cols < 0 || t[i].rows > most || t[i].cols > most) return FOPD_ERR_SIZE;
+    if (t[i].rows == 0 || t[i].cols == 0) continue;
+    if (t[i].rows > 1 && (t[i].row_stride < t[i].cols || t[i].row_stride > most / t[i].rows)) return FOPD_ERR_SIZE;
+    if (!t[i].data) return FOPD_ERR_NULL;
+    if ((uintptr_t)t[i].data % esz != 0 || (uintptr_t)t[i].out % esz != 0) return FOPD_ERR_ALIGN;
+  }
+  return FOPD_OK;
+}
+
+struct Range {
+  uintptr_t lo, hi, row;  // row: pitch in bytes (0: one row)
+  uintptr_t width;        // bytes of a row
+  int32_t tensor;
+  bool written;
+};
+
+Range range_of(const fopd_tensor &t, const void *p, int32_t i, bool written) {
+  const uintptr_t esz = t.dtype == FOPD_BF16 ? 2 : 4, a = (uintptr_t)p, width = (uintptr_t)t.cols * esz;
+  const uintptr_t pitch = t.rows > 1 ? (uintptr_t)t.row_stride * esz : 0;
+  return {a, a + (uintptr_t)(t.rows - 1) * pitch + width, pitch, width, i, written};
+}
+
+// Column blocks of one wider matrix overlap as ranges but not as elements.
+bool disjoint_columns(const Range &a, const Range &b) {
+  if (a.row == 0 || a.row != b.row || a.lo > b.lo) return false;
+  const uintptr_t shift = (b.lo - a.lo) % a.row;
+  return shift >= a.width && shift + b.width <= a.row;
+}
+
+// Whether a written range meets another one (its own tensor's data exactly in place excepted).
+int check_overlap(const fopd_tensor *t, int32_t n) {
+  std::vector<Range> r;
+  r.reserve(2 * n);
+  bool sorted = true;
+  for (int32_t i = 0; i < n; ++i) {
+    if (t[i].rows == 0 || t[i].cols == 0) continue;
+    const bool in_place = !t[i].out || t[i].out == t[i].data;
+    r.push_back(range_of(t[i], t[i].data, i, in_place));
+    if (!in_place) r.push_back(range_of(t[i], t[i].out, i, true));
+  }
+  for (size_t i = 1; i < r.size() && sorted; ++i) sorted = r[i - 1].lo <= r[i].lo;
+  if (!sorted) std::sort(r.begin(), r.end(), [](const Range &a, const Range &b) { return a.lo < b.lo; });
+  // open: ranges that reach beyond the start of the next one
+  std::vector<Range> open;
+  for (const Range &b : r) {
+    size_t k = 0;
+    for (const Range &a : open) {
+      if (a.hi <= b.lo) continue;
+      if ((a.written || b.written) && !disjoint_columns(a, b)) return FOPD_ERR_ALIAS;
+      open[k++] = a;
+    }
+    open.resize(k);
+    open.push_back(b);
+  }
+  return FOPD_OK;
+}
+
+// Fills a launch's table from tensors [*next, n); empty ones are left out.
+template <int N>
+void fill_table(const fopd_tensor *t, int32_t n, int32_t *next, ClipTable<N> *tab) {
+  tab->n = 0;
+  tab->n_tiles = 0;
+  for (; *next < n && tab->n < N; ++*next) {
+    const fopd_tensor &x = t[*next];
+    if (x.rows == 0 || x.cols == 0) continue;
+    ClipEntry &e = tab->e[tab->n++];
+    const bool one_row = x.rows == 1 || x.row_stride == x.cols;
+    const int64_t rows = one_row ? 1 : x.rows;
+    e.data = static_cast<const char *>(x.data);
+    e.out = static_cast<char *>(x.out ? x.out : const_cast<void *>(x.data));
+    e.cols = one_row ? x.rows * x.cols : x.cols;
+    e.row_stride = one_row ? e.cols : x.row_stride;
+    e.tile0 = tab->n_tiles;
+    e.dtype = x.dtype;
+    const int64_t per = kClipTileBytes / (x.dtype == FOPD_BF16 ? 2 : 4);
+    e.tiles_per_row = (int32_t)((e.cols + per - 1) / per);
+    tab->n_tiles += rows * e.tiles_per_row;
+  }
+}
+
+unsigned clip_grid(int64_t n_tiles) {
+  return (unsigned)(n_tiles < 1 ? 1 : n_tiles < kClipMaxGrid ? n_tiles : kClipMaxGrid);
+}
+
+template <int N>
+int launch_norm(const fopd_tensor *t, int32_t n, double *ws, int set, float *norm, int32_t *status, cudaStream_t st) {
+  ClipTable<N> tab;
+  int32_t next = 0;
+  do {
+    fill_table<N>(t, n, &next, &tab);
+    grad_norm_kernel<N><<<clip_grid(tab.n_tiles), kClipThreads, 0, st>>>(tab, ws, set, norm, status);
+    const int rc = launch_ok();
+    if (rc != FOPD_OK) return rc;
+    set = 0;
+  } while (next < n);
+  return FOPD_OK;
+}
+
+template <int N>
+int launch_scale(const fopd_tensor *t, int32_t n, const double *ws, float max_norm, float *norm, float *coef,
+                 int32_t *status, cudaStream_t st) {
+  ClipTable<N> tab;
+  int32_t next = 0;
+  do {
+    fill_table<N>(t, n, &next, &tab);
+    grad_scale_kernel<N><<<clip_grid(tab.n_tiles), kClipThreads, 0, st>>>(tab, ws, max_norm, norm, coef, status);
+    const int rc = launch_ok();
+    if (rc != FOPD_OK) return rc;
+  } while (next < n);
+  return FOPD_OK;
+}
+
+int norm_any(const fopd_tensor *t, int32_t n, double *ws, int set, float *norm, int32_t *status, cudaStream_t st) {
+  return n <= kSmallTable ? launch_norm<kSmallTable>(t, n, ws, set, norm, status, st)
+                          : launch_norm<kLargeTable>(t, n, ws, set, norm, status, st);
+}
+int scale_any(const fopd_tensor *t, int32_t n, const double *ws, float max_norm, float *norm, float *coef,
+              int32_t *status, cudaStream_t st) {
+  return n <= kSmallTable ? launch_scale<kSmallTable>(t, n, ws, max_norm, norm, coef, status, st)
+                          : launch_scale<kLargeTable>(t, n, ws, max_norm, norm, coef, status, st);
+}
+
+int check_scale(const fopd_tensor *t, int32_t n, const double *ws, float max_norm) {
+  const int rc = check_tensors(t, n, ws);
+  if (rc != FOPD_OK) return rc;
+  if (!std::isfinite(max_norm) || !(max_norm > 0.f)) return FOPD_ERR_PARAM;
+  try {
+    return check_overlap(t, n);
+  } catch (...) {  // host memory for the ranges
+    return FOPD_ERR_CUDA;
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int fopd_grad_norm(const fopd_tensor *tensors, int32_t n_tensors, double *ws, float *norm, int32_t *status,
+                   void *stream) {
+  const int rc = check_tensors(tensors, n_tensors, ws);
+  if (rc != FOPD_OK) return rc;
+  return norm_any(tensors, n_tensors, ws, 0, norm, status, static_cast<cudaStream_t>(stream));
+}
+
+int fopd_grad_scale(const fopd_tensor *tensors, int32_t n_tensors, double *ws, float max_norm, float *norm,
+                    float *coef, int32_t *status, void *stream) {
+  const int rc = check_scale(tensors, n_tensors, ws, max_norm);
+  if (rc != FOPD_OK) return rc;
+  return scale_any(tensors, n_tensors, ws, max_norm, norm, coef, status, static_cast<cudaStream_t>(stream));
+}
+
+int fopd_grad_clip(const fopd_tensor *tensors, int32_t n_tensors, double *ws, float max_norm, float *norm,
+                   float *coef, int32_t *status, void *stream) {
+  int rc = check_scale(tensors, n_tensors, ws, max_norm);
+  if (rc != FOPD_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  rc = norm_any(tensors, n_tensors, ws, 1, nullptr, nullptr, st);
+  if (rc != FOPD_OK) return rc;
+  return scale_any(tensors, n_tensors, ws, max_norm, norm, coef, status, st);
+}
+
+}  // extern "C"

@@ -100,15 +100,35 @@ def optimise(chunks, dlogits, buf: BatchBuffers, p, rows=None, *, use_row_ws=Tru
                           per_sample_loss=buf.per_sample_loss, stream=stream)
 
 
-def step(chunks, dlogits, buf: BatchBuffers, tau, H, d_sup, p, rows=None, *, use_row_ws=True, stream=None):
-    """One pass of the whole hot path over one batch."""
+class GradientClip:
+    """Norm and clipping of one set of gradients (a batch's dlogits, or the parameters' gradients
+    behind them), in place unless ``outs`` is given.  Keep it as long as the tensors keep their memory."""
+
+    def __init__(self, tensors, max_norm: float, outs=None):
+        self.grads = fb.GradientList(tensors, outs)
+        self.max_norm = float(max_norm)
+        dev = self.grads.device
+        self.ws = fb.grad_workspace(dev)
+        self.norm, self.coef = (torch.zeros(1, dtype=torch.float32, device=dev) for _ in range(2))
+
+    def __call__(self, *, status=None, stream=None):
+        fb.fopd_grad_clip(self.grads, self.max_norm, self.ws, norm=self.norm, coef=self.coef, status=status,
+                          stream=stream)
+        return self.norm
+
+
+def step(chunks, dlogits, buf: BatchBuffers, tau, H, d_sup, p, rows=None, *, use_row_ws=True, clip=None, stream=None):
+    """One pass of the whole hot path over one batch.  ``clip``: a GradientClip over the batch's
+    dlogits (their columns in use), applied when all of them are written."""
     buf.reset()
     measure(chunks, buf, rows, keep_row_ws=use_row_ws, stream=stream)
     freshness(buf, tau, H, d_sup, p, stream=stream)
     optimise(chunks, dlogits, buf, p, rows, use_row_ws=use_row_ws, stream=stream)
+    if clip is not None:
+        clip(status=buf.status, stream=stream)
 
 
-def step_student_stats(chunks, dlogits, buf: BatchBuffers, tau, H, d_sup, p, rows=None, *, stream=None):
+def step_student_stats(chunks, dlogits, buf: BatchBuffers, tau, H, d_sup, p, rows=None, *, clip=None, stream=None):
     """The whole hot path with the fewest bytes: the student's statistics (V e per token), the
     freshness, then the loss forward + backward without cached statistics (3 V e per
     differentiated token)."""
@@ -116,6 +136,47 @@ def step_student_stats(chunks, dlogits, buf: BatchBuffers, tau, H, d_sup, p, row
     measure_student(chunks, buf, rows, stream=stream)
     freshness(buf, tau, H, d_sup, p, stream=stream)
     optimise(chunks, dlogits, buf, p, None, use_row_ws=False, stream=stream)
+    if clip is not None:
+        clip(status=buf.status, stream=stream)
+
+
+# ---- rollout: where a chunk's tokens and behaviour log-probs come from ----
+
+@dataclass
+class Rollout:
+    """Tokens of B sequences with the log-probabilities they were drawn at; [B, K + 1] unless said."""
+    tokens: torch.Tensor
+    logprob: torch.Tensor
+    mask: torch.Tensor
+    n_accepted: torch.Tensor  # [B]
+    status: torch.Tensor  # [1]
+
+    @staticmethod
+    def alloc(B: int, K: int, device) -> "Rollout":
+        z = lambda shape, d: torch.zeros(shape, dtype=d, device=device)
+        return Rollout(z((B, K + 1), torch.int32), z((B, K + 1), torch.float32), z((B, K + 1), torch.uint8),
+                       z((B,), torch.int32), z((1,), torch.int32))
+
+
+def verify_rollout(target, draft, draft_tokens, uniform, out: Rollout, *, n_draft=None, temperature=1.0,
+                   draft_temperature=1.0, vocab=None, stream=None) -> Rollout:
+    """Drafted (or stale) tokens against the policy that has the logits ``target`` [B, K + 1, V]."""
+    fb.fopd_verify_draft(target, draft, draft_tokens, uniform, out.tokens, n_draft=n_draft, logprob=out.logprob,
+                         mask=out.mask, n_accepted=out.n_accepted, temperature=temperature,
+                         draft_temperature=draft_temperature, vocab=vocab, status=out.status, stream=stream)
+    return out
+
+
+def rollout_chunk(target, teacher, out: Rollout, sample_id, vocab=None, loss_kind: int = fb.LOSS_FULL_KL) -> fb.Chunk:
+    """The B (K + 1) target rows of a rollout as a chunk of the loss, without a copy: the policy's own
+    logits, the teacher's on the same positions, and the tokens, log-probs and mask that came out.
+    ``target`` and ``teacher`` have their rows at one pitch; ``sample_id`` [B] int32, non-decreasing."""
+    B, W, V = target.shape
+    assert target.stride(0) == W * target.stride(1), "rows at one pitch"
+    rows = lambda t: t.as_strided((B * W, V), (t.stride(1), 1))
+    assert teacher is None or teacher.stride() == target.stride()
+    return fb.Chunk(rows(target), None if teacher is None else rows(teacher), out.logprob.view(-1), out.tokens.view(-1),
+                    out.mask.view(-1), sample_id.repeat_interleave(W), vocab, loss_kind)
 
 
 def to_chunk(d: dict, vocab=None, loss_kind: int = fb.LOSS_FULL_KL) -> fb.Chunk:

@@ -1,0 +1,447 @@
+"""GPU tests of fopd_draw_tokens and fopd_verify_draft against the fp64 definitions in
+oracle/rollout_oracle.py.  Tokens, masks and counts are compared exactly.
+
+Log-probabilities: log p = (x - max) / T - log Z with the first term in fp64 and Z from the fp32 sweep, whose
+relative error is at most 7.5e-6 (three roundings in an exponent above -24, ex2, 69 additions: 3.1e-6 + 0.3e-6 + 4.1e-6);
+the result is rounded to fp32 once, 2^-24 |log p|."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import rollout_oracle as ro
+from paper_2605_17862_b200 import binding as fb
+from paper_2605_17862_b200 import pipeline as pl
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+TOP = 1 - 2.0 ** -53
+
+
+def lp_tol(lp):
+    return 7.5e-6 + 2.0 ** -24 * np.abs(lp)
+
+
+def rows_of(shape, V, dtype, seed, pad=None, scale=3.0):
+    """N(0, scale^2) logits at a pitch of whole vectors; what lies behind V is NaN."""
+    per = 8 if dtype == BF16 else 4
+    pitch = -(-(V + (pad or 0)) // per) * per
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.full((*shape, pitch), math.nan, device=DEV, dtype=dtype)
+    x[..., :V] = torch.randn((*shape, V), generator=g, device=DEV) * scale
+    return x[..., :V]
+
+
+def uniforms(shape, seed):
+    return torch.rand(shape, generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV, dtype=torch.float64)
+
+
+def run_draw(x, u, T, vocab=None):
+    n = x.shape[0]
+    tokens = torch.full((n,), 77, dtype=torch.int32, device=DEV)
+    lp = torch.full((n,), 77.0, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    fb.fopd_draw_tokens(x, u, tokens, logprob=lp, temperature=T, vocab=vocab, status=status)
+    return tokens, lp, int(status.cpu()[0])
+
+
+def check_draw(x, u, T, bits=0):
+    tokens, lp, got_bits = run_draw(x, u, T)
+    want = [ro.draw(r, float(v), T) for r, v in zip(x.cpu(), u.cpu())]
+    assert got_bits == bits
+    assert tokens.cpu().tolist() == [w[0] for w in want]
+    wl = np.array([w[1] for w in want])
+    assert np.all(np.abs(lp.cpu().numpy() - wl) <= lp_tol(wl))
+    return tokens
+
+
+def run_verify(target, draft, drafted, u, *, n_draft=None, T=1.0, Td=1.0):
+    B, W = target.shape[:2]
+    out = dict(tokens=torch.full((B, W), 77, dtype=torch.int32, device=DEV), logprob=torch.full((B, W), 77.0, device=DEV),
+               mask=torch.full((B, W), 77, dtype=torch.uint8, device=DEV),
+               n_accepted=torch.full((B,), 77, dtype=torch.int32, device=DEV))
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    tokens = out["tokens"]
+    fb.fopd_verify_draft(target, draft, drafted, u, tokens, n_draft=n_draft, logprob=out["logprob"], mask=out["mask"],
+                         n_accepted=out["n_accepted"], temperature=T, draft_temperature=Td, status=status)
+    return {k: v.cpu().numpy() for k, v in out.items()}, int(status.cpu()[0])
+
+
+def check_verify(target, draft, drafted, u, *, n_draft=None, T=1.0, Td=1.0):
+    got, bits = run_verify(target, draft, drafted, u, n_draft=n_draft, T=T, Td=Td)
+    B, W = target.shape[:2]
+    K = W - 1
+    t, d = target.cpu(), None if draft is None else draft.cpu()
+    xs, us = drafted.cpu().numpy(), u.cpu().numpy()
+    want_bits = 0
+    for b in range(B):
+        n = K if n_draft is None else int(n_draft[b])
+        if not 0 <= n <= K:
+            n = min(max(n, 0), K)
+            want_bits |= 8
+        tokens, lps, acc, why, bad_token = ro.verify(t[b], None if d is None else d[b], xs[b], n, us[b], T, Td)
+        want_bits |= {"": 0, "logits": 32, "uniform": 64}[why] | (1 if bad_token else 0)
+        m = len(tokens)
+        assert got["n_accepted"][b] == acc, b
+        assert got["tokens"][b].tolist() == tokens + [-1] * (W - m), b
+        assert got["mask"][b].tolist() == [1] * m + [0] * (W - m), b
+        assert np.all(np.abs(got["logprob"][b, :m] - np.array(lps)) <= lp_tol(np.array(lps))), b
+        assert np.all(got["logprob"][b, m:] == 0)
+    assert bits == want_bits
+    return got
+
+
+def drafts_from(draft, Td, seed):
+    """Tokens drawn from the draft's rows (its distribution decides how many are accepted)."""
+    B, K, V = draft.shape
+    z = draft.float()
+    if Td:
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        z = z / Td - torch.empty(z.shape, device=DEV).exponential_(generator=g).log()
+    return z.argmax(-1).int()
+
+
+# ---- draws ----
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("V", [1, 2, 7, 8, 9, 33, 257, 1023, 1025, 2047, 2049, 4099, 20001])
+def test_draw_odd_vocabularies(V, dtype):
+    for T in (1.0, 0.3, 0.0):
+        check_draw(rows_of((19,), V, dtype, V, pad=V % 11), uniforms(19, V + 1), T)
+
+
+@pytest.mark.parametrize("V,dtype,n", [(151936, BF16, 40), (128256, F32, 12), (70001, BF16, 1)])
+def test_draw_large_vocabularies(V, dtype, n):
+    x = rows_of((n,), V, dtype, 5)
+    x[:, ::101] += 8
+    for T in (0.7, 1.0, 1.6):
+        check_draw(x, uniforms(n, 9), T)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_draw_flat_rows_where_no_probability_exceeds_the_sum_error(dtype):
+    """All probabilities near 1/V: the fp32 running sums do not decide any of these."""
+    V = 151936
+    x = rows_of((24,), V, dtype, 3, scale=0.02)
+    check_draw(x, uniforms(24, 4), 1.0)
+    # exactly even weights: a running sum that equals v times the total is not passed yet
+    even = torch.full((5, 4096), 1.5, device=DEV, dtype=dtype)
+    u = torch.tensor([0.0, 0.25, 0.25 - 2.0 ** -40, 4095 / 4096, TOP], device=DEV, dtype=torch.float64)
+    assert check_draw(even, u, 1.0).tolist() == [0, 1024, 1023, 4095, 4095]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_draw_at_the_ends_of_the_unit_interval_and_at_boundaries(dtype):
+    V = 5003
+    x = rows_of((6,), V, dtype, 11)
+    u = torch.tensor([0.0, 1e-300, 1e-12, 0.5, 1 - 1e-12, TOP], device=DEV, dtype=torch.float64)
+    check_draw(x, u, 1.0)
+    # just below and just above a boundary of the fp64 distribution function (by 1e-11, a thousand times its error)
+    row = x[:1].expand(8, V).contiguous()
+    per = -(-V // 8) * 8
+    wide = torch.zeros(8, per, device=DEV, dtype=dtype)
+    wide[:, :V] = row
+    c = np.cumsum(ro.probabilities(row[0].cpu(), 1.0))
+    ids = [10, 999, 2500, 4444]
+    u = torch.tensor([c[i] + s for i in ids for s in (-1e-11, 1e-11)], device=DEV, dtype=torch.float64)
+    check_draw(wide[:, :V], u, 1.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_draw_masked_logits(dtype):
+    low = torch.finfo(dtype).min
+    V, n = 3001, 10
+    x = rows_of((n,), V, dtype, 21)
+    x[0, :] = -math.inf
+    x[0, 2999] = 3.0            # one token left
+    x[1, :2998] = -math.inf     # everything but the end
+    x[2, 5:] = -math.inf        # everything but the beginning
+    x[3, ::2] = -math.inf
+    x[4, :] = low               # the lowest value everywhere is an even row
+    x[5, 1:] = low              # ... and no weight beside a real one
+    x[6, ::3] = low
+    x[7, :] = -300.0
+    x[8, :] += 5000.0
+    x[9, 7] = 90.0              # all the weight on one token
+    for T in (1.0, 0.5, 0.0):
+        check_draw(x, uniforms(n, 22), T)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T", [1.0, 0.0])
+def test_draw_rows_without_a_distribution(dtype, T):
+    x = rows_of((6,), 2500, dtype, 31)
+    x[0, 2400] = math.nan
+    x[1, 3] = math.inf
+    x[2, :] = -math.inf
+    x[4, :] = -math.inf
+    x[4, 70] = math.nan
+    check_draw(x, uniforms(6, 32), T, bits=32)
+    y = rows_of((4,), 100, dtype, 33)
+    u = torch.tensor([-1e-9, 1.0, math.nan, 0.5], device=DEV, dtype=torch.float64)
+    check_draw(y, u, T, bits=64 if T else 0)
+
+
+def test_draw_vocab_argument_no_rows_and_optional_outputs():
+    x = rows_of((3,), 64, F32, 41)
+    tokens, lp, bits = run_draw(x, uniforms(3, 42), 1.0, vocab=10)
+    assert bits == 0 and [ro.draw(r[:10], float(v), 1.0)[0] for r, v in zip(x.cpu(), uniforms(3, 42).cpu())] == tokens.tolist()
+    none = torch.empty(0, dtype=torch.int32, device=DEV)
+    fb.fopd_draw_tokens(x[:0], uniforms(0, 1), none)
+    fb.fopd_draw_tokens(x, uniforms(3, 42), tokens)
+
+
+def test_draw_rows_behind_the_32_bit_offsets():
+    """16,400 rows of 151,936: the last ones start beyond 2^31 elements."""
+    n, V = 16400, 151936
+    x = torch.zeros((n, V), device=DEV, dtype=BF16)
+    tail = rows_of((8,), V, BF16, 51)
+    x[-8:] = tail
+    u = uniforms(n, 52)
+    tokens, lp, bits = run_draw(x, u, 1.0)
+    assert bits == 0
+    want = [ro.draw(r, float(v), 1.0)[0] for r, v in zip(tail.cpu(), u[-8:].cpu())]
+    assert tokens[-8:].tolist() == want
+    # even rows: token = floor(v V)
+    assert torch.equal(tokens[:-8].long(), (u[:-8] * V).floor().long())
+
+
+# ---- verification ----
+
+@pytest.mark.parametrize("dtype,V", [(BF16, 9), (F32, 9), (BF16, 2050), (F32, 1030), (BF16, 32000)])
+@pytest.mark.parametrize("form", ["rows", "certain", "best"])
+@pytest.mark.parametrize("K", [1, 3, 8])
+def test_verify_forms(dtype, V, form, K):
+    B, T = 12, 0.8
+    target = rows_of((B, K + 1), V, dtype, V + K, pad=5)
+    draft = rows_of((B, K), V, dtype, 1, pad=13)
+    draft += target[:, :K] - 0.6 * draft  # near the target's
+    Td = 0.0 if form == "best" else 1.2
+    drafted = drafts_from(draft, Td, 7)
+    if form == "certain":
+        drafted[:, ::2] = target[:, :K].argmax(-1).int()[:, ::2]
+    n_draft = torch.randint(0, K + 1, (B,), device=DEV, dtype=torch.int32)
+    n_draft[0], n_draft[1] = 0, K
+    d = None if form == "certain" else draft
+    got = check_verify(target, d, drafted, uniforms((B, K + 1), 8), n_draft=n_draft, T=T, Td=Td)
+    check_verify(target, d, drafted, uniforms((B, K + 1), 9), T=T, Td=Td)
+    assert got["n_accepted"].max() <= K
+
+
+def test_verify_large_vocabulary():
+    B, K, V = 6, 5, 151936
+    target = rows_of((B, K + 1), V, BF16, 61)
+    target[:, :, ::97] += 8
+    draft = (target[:, :K].float() + 0.4 * rows_of((B, K), V, F32, 62, scale=1.0)).to(BF16)
+    got = check_verify(target, draft, drafts_from(draft, 1.0, 63), uniforms((B, K + 1), 64))
+    assert 0 < got["n_accepted"].sum() < B * K
+
+
+def test_verify_temperature_zero_takes_the_best_tokens():
+    B, K, V = 9, 4, 700
+    target = rows_of((B, K + 1), V, BF16, 71)
+    best = target[:, :K].argmax(-1).int()
+    for k in range(K):
+        best[k, k] = (best[k, k] + 1) % V
+    u = torch.full((B, K + 1), math.nan, device=DEV, dtype=torch.float64)  # not needed
+    got = check_verify(target, None, best, u, T=0.0)
+    assert got["n_accepted"].tolist() == [0, 1, 2, 3] + [4] * (B - 4)
+    nan = torch.full((B, K, V + 4), math.nan, device=DEV, dtype=BF16)[:, :, :V]  # neither are the draft's rows
+    assert np.array_equal(check_verify(target, nan, best, u, T=0.0, Td=0.0)["tokens"], got["tokens"])
+
+
+def test_verify_ties_and_equal_rows():
+    """u q = p exactly is a rejection; a draft equal to the target is always accepted; a drafted token that neither
+    can give leaves no residual and the token comes from p."""
+    V = 4096
+    even = torch.zeros((5, 2, V), device=DEV, dtype=F32)
+    draft = torch.zeros((5, 1, V), device=DEV, dtype=F32)
+    draft[:4, :, V // 2:] = -math.inf  # q = 2 / V on the lower half: accepted below u = 1/2
+    draft[4] = even[4, :1]
+    drafted = torch.tensor([[5], [5], [5], [V - 1], [17]], device=DEV, dtype=torch.int32)
+    u = torch.tensor([[0.5, 0.0], [0.5 - 2.0 ** -40, 0.5], [0.5, TOP], [TOP, 0.3], [TOP, 0.9]], device=DEV, dtype=torch.float64)
+    got = check_verify(even, draft, drafted, u)
+    assert got["n_accepted"].tolist() == [0, 1, 0, 1, 1]
+    assert got["tokens"][0, 0] == V // 2 and got["tokens"][2, 0] == V - 1
+    target = rows_of((3, 2), 999, BF16, 81)
+    target[:, 0, 300:] = -math.inf
+    d = target[:, :1].contiguous()
+    wide = torch.zeros((3, 1, 1000), device=DEV, dtype=BF16)
+    wide[:, :, :999] = d
+    got = check_verify(target, wide[:, :, :999], torch.full((3, 1), 500, dtype=torch.int32, device=DEV), uniforms((3, 2), 82))
+    assert got["n_accepted"].tolist() == [0, 0, 0] and got["tokens"][:, 0].max() < 300
+
+
+def test_verify_rows_that_are_not_reached_may_hold_anything():
+    B, K, V = 4, 6, 1500
+    target, draft = rows_of((B, K + 1), V, F32, 91), rows_of((B, K), V, F32, 92)
+    drafted = drafts_from(draft, 1.0, 93)
+    u = uniforms((B, K + 1), 94)
+    first = check_verify(target, draft, drafted, u)
+    assert first["n_accepted"].max() < K - 1  # unrelated drafts are soon rejected
+    for b in range(B):
+        a = int(first["n_accepted"][b])
+        target[b, a + 1:] = math.nan
+        draft[b, a + 1:] = math.inf
+        drafted[b, a + 1:] = -5
+        u[b, a + 1:K] = math.nan
+    again, bits = run_verify(target, draft, drafted, u)
+    assert bits == 0 and all(np.array_equal(first[k], again[k]) for k in first)
+
+
+def test_verify_bad_rows_numbers_tokens_and_lengths():
+    B, K, V = 12, 3, 777
+    target, draft = rows_of((B, K + 1), V, F32, 101), rows_of((B, K), V, F32, 102)
+    draft[:] = target[:, :K]  # everything is accepted where nothing is wrong
+    drafted = drafts_from(draft, 1.0, 103)
+    u = uniforms((B, K + 1), 104)
+    n_draft = torch.full((B,), K, dtype=torch.int32, device=DEV)
+    target[0, 1, 5] = math.nan
+    target[1, 3, 700] = math.inf
+    draft[2, 2, 9] = math.nan
+    draft[3, 0, :] = -math.inf
+    u[4, 1] = 1.0
+    u[5, K] = -0.5
+    drafted[6, 1] = V
+    drafted[7, 0] = -1
+    n_draft[8], n_draft[9] = -2, K + 4
+    got = check_verify(target, draft, drafted, u, n_draft=n_draft)
+    assert got["n_accepted"].tolist() == [1, 3, 2, 0, 1, 3, 1, 0, 0, 3, 3, 3]
+    check_verify(target, None, drafted, u, n_draft=n_draft)
+    check_verify(target, draft, drafted, u, n_draft=n_draft, Td=0.0)
+    check_verify(target, draft, drafted, u, n_draft=n_draft, T=0.0)
+
+
+def test_verify_without_drafts_is_a_draw():
+    x, u = rows_of((7, 1), 3333, BF16, 111), uniforms((7, 1), 112)
+    got = check_verify(x, None, torch.empty((7, 0), dtype=torch.int32, device=DEV), u)
+    assert got["tokens"][:, 0].tolist() == run_draw(x[:, 0], u[:, 0].contiguous(), 1.0)[0].tolist()
+
+
+@pytest.mark.parametrize("B,K,V,close", [(3, 300, 520, 0.05), (2, 1000, 130, 0.005), (40, 64, 2100, 0.1)])
+def test_verify_long_drafts(B, K, V, close):
+    target = rows_of((B, K + 1), V, BF16, K)
+    draft = (target[:, :K].float() + close * torch.randn((B, K, V), device=DEV)).to(BF16)
+    per = -(-V // 8) * 8
+    wide = torch.zeros((B, K, per), device=DEV, dtype=BF16)
+    wide[:, :, :V] = draft
+    got = check_verify(target, wide[:, :, :V], drafts_from(draft, 1.0, 3), uniforms((B, K + 1), 4))
+    assert got["n_accepted"].max() > 3
+
+
+def test_verify_strides():
+    """Sequences interleaved with each other, rows within a wider buffer, one draft row for all sequences."""
+    B, K, V = 5, 4, 300
+    big = rows_of((K + 1, 2 * B, 3), V, F32, 121)
+    target = big[:, ::2, 1].transpose(0, 1)
+    assert target.shape == (B, K + 1, V) and not target.is_contiguous()
+    draft = rows_of((1, K), V, F32, 122).expand(B, K, V)
+    drafted = drafts_from(draft, 1.0, 123)
+    check_verify(target, draft, drafted, uniforms((B, K + 1), 124), T=2.0, Td=1.5)
+
+
+def test_rollout_calls_on_a_side_stream_in_a_graph_and_at_the_same_time():
+    B, K, V = 6, 4, 30001
+    target, draft = rows_of((B, K + 1), V, BF16, 131), rows_of((B, K), V, BF16, 132)
+    draft += target[:, :K] * 0.9 - draft * 0.6
+    drafted, u = drafts_from(draft, 1.0, 133), uniforms((B, K + 1), 134)
+    want, _ = run_verify(target, draft, drafted, u)
+    rows = rows_of((300,), V, BF16, 135)
+    ur = uniforms(300, 136)
+    want_rows = run_draw(rows, ur, 1.0)[0]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    outs = []
+    for k in range(12):
+        s = streams[k % 3]
+        with torch.cuda.stream(s):
+            t = torch.empty((B, K + 1), dtype=torch.int32, device=DEV)
+            r = torch.empty(300, dtype=torch.int32, device=DEV)
+            fb.fopd_verify_draft(target, draft, drafted, u, t, stream=s)
+            fb.fopd_draw_tokens(rows, ur, r, stream=s)
+            outs.append((t, r))
+    torch.cuda.synchronize()
+    for t, r in outs:
+        assert np.array_equal(t.cpu().numpy(), want["tokens"]) and torch.equal(r, want_rows)
+    # captured once, replayed on new inputs; two graphs whose temporaries must not be each other's
+    t1, t2 = (torch.empty((B, K + 1), dtype=torch.int32, device=DEV) for _ in range(2))
+    r1 = torch.empty(300, dtype=torch.int32, device=DEV)
+    g1, g2 = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g1):
+        fb.fopd_verify_draft(target, draft, drafted, u, t1)
+    with torch.cuda.graph(g2):
+        fb.fopd_draw_tokens(rows, ur, r1)
+        fb.fopd_verify_draft(target, draft, drafted, u, t2)
+    u.copy_(uniforms((B, K + 1), 137))
+    want2, _ = run_verify(target, draft, drafted, u)
+    with torch.cuda.stream(streams[0]):
+        g1.replay()
+    with torch.cuda.stream(streams[1]):
+        g2.replay()
+    torch.cuda.synchronize()
+    for t in (t1, t2):
+        assert np.array_equal(t.cpu().numpy(), want2["tokens"])
+    assert torch.equal(r1, want_rows)
+
+
+# ---- together, as a training program uses them ----
+
+@pytest.mark.parametrize("dtype,T", [(F32, 1.0), (BF16, 1.0)])
+def test_draw_verify_loss_and_clip_in_one_run(dtype, T):
+    """Drafts are drawn from one policy, verified against the one that has moved on, graded by a teacher; the rows
+    that came out are a chunk of the loss, whose gradient is clipped by its norm.  Each stage against its fp64
+    definition."""
+    import _parity as par
+    from oracle import fopd_oracle as orc
+
+    B, K, V = 6, 9, 1201
+    W = K + 1
+    target, teacher, draft = (rows_of(s, V, dtype, k, pad=3) for k, s in ((201, (B, W)), (202, (B, W)), (203, (B, K))))
+    draft[:] = target[:, :K] + 0.3 * draft
+    teacher += target - 0.7 * teacher
+    flat = draft.as_strided((B * K, V), (draft.stride(1), 1))
+    drafted = torch.empty(B * K, dtype=torch.int32, device=DEV)
+    fb.fopd_draw_tokens(flat, uniforms(B * K, 204), drafted, temperature=T)
+    assert drafted.tolist() == [ro.draw(r, float(v), T)[0] for r, v in zip(flat.cpu(), uniforms(B * K, 204).cpu())]
+    drafted = drafted.view(B, K)
+    u = uniforms((B, W), 205)
+    out = pl.verify_rollout(target, draft, drafted, u, pl.Rollout.alloc(B, K, DEV), temperature=T, draft_temperature=T)
+    want = check_verify(target, draft, drafted, u, T=T, Td=T)
+    assert np.array_equal(out.tokens.cpu().numpy(), want["tokens"])
+
+    sid = torch.arange(B, dtype=torch.int32, device=DEV)
+    chunk = pl.rollout_chunk(target, teacher, out, sid)
+    n = B * W
+    dl_buf = torch.zeros((n, target.stride(1)), dtype=dtype, device=DEV)
+    dlogits = dl_buf[:, :V]
+    tau = torch.tensor([0, 1, 0, 2, 0, 1], dtype=torch.int32, device=DEV)
+    H = torch.full((B,), W, dtype=torch.int32, device=DEV)
+    p = fb.params(**par.PARAMS)
+
+    def run(clip):
+        buf, rows = pl.BatchBuffers(B, DEV), [pl.RowOutputs.alloc(n, DEV)]
+        pl.step([chunk], [dlogits], buf, tau, H, None, p, rows, clip=clip)
+        assert fb.fopd_check_status(buf.status) == 0
+        return buf, dlogits.clone()
+
+    buf, plain = run(None)
+    # the behaviour policy is the current one: ratio 1, no rollout drift, freshness 1 / (tau + 1)
+    assert np.allclose(buf.f.cpu().numpy(), 1.0 / (tau.cpu().numpy() + 1), rtol=1e-4)
+    assert buf.acc[:, 0].cpu().tolist() == (out.n_accepted + 1).cpu().tolist()
+    wide = lambda t: t.as_strided((n, t.stride(1)), (t.stride(1), 1))  # the loss on these rows against its own oracle
+    ch = dict(student=wide(target), teacher=wide(teacher), tokens=chunk.tokens, behav_logprob=chunk.behav_logprob,
+              mask=chunk.mask, sample_id=chunk.sample_id)
+    par.compare([ch], B, tau.cpu().numpy(), H.cpu().numpy(), vocab=V)
+    assert torch.equal(plain[chunk.mask == 0], torch.zeros_like(plain[chunk.mask == 0]))
+    norm, coef, scaled = ro.clip([plain], 0.01)
+    assert coef < 1
+    clip = pl.GradientClip([dlogits], 0.01)
+    _, clipped = run(clip)
+    assert abs(float(clip.norm) - norm) <= 2.0 ** -23 * norm and abs(float(clip.coef) - coef) <= 2.0 ** -23 * coef
+    got = clipped.cpu().double().numpy()
+    step = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+    assert np.all(np.abs(got - scaled[0]) <= np.abs(scaled[0]) * (step * 1.001 + 2.0 ** -22) + 1e-38)
+    _, again = run(None)
+    assert torch.equal(again, plain)  # without clipping a step is what it was
