@@ -8,28 +8,83 @@ namespace {
 
 bool temperature_ok(float t) { return t == 0.f || (t >= 1.f / 1024 && t <= 1024.f); }
 
-template <int DT>
-int launch_rollout(RolloutDev d, int32_t *tokens, float *logprob, uint8_t *mask, int32_t *n_accepted, int32_t *status,
-                   cudaStream_t st) {
-  d.n_tiles = (d.vocab + TileShape<DT>::kElems - 1) / TileShape<DT>::kElems;
-  const bool draft_rows = d.kind == kDraftRows || d.kind == kDraftBest;
-  const int64_t positions = (int64_t)d.B * (d.K + 1);
-  const int64_t rows = positions + (draft_rows ? (int64_t)d.B * d.K : 0);
-  const size_t part_bytes = ((size_t)rows * d.n_tiles * sizeof(float2) + 255) & ~size_t(255);
-  const size_t tsum_bytes = ((size_t)d.B * d.n_tiles * sizeof(double) + 255) & ~size_t(255);
-  char *tmp = nullptr;
-  int rc = scratch_alloc(reinterpret_cast<void **>(&tmp), part_bytes + tsum_bytes + positions * sizeof(Position), st);
-  if (rc != FOPD_OK) return rc;
-  d.part = reinterpret_cast<float2 *>(tmp);
-  d.tsum = reinterpret_cast<double *>(tmp + part_bytes);
-  d.pos = reinterpret_cast<Position *>(tmp + part_bytes + tsum_bytes);
-  const int64_t items = rows * ((d.n_tiles + kTileWarps - 1) / kTileWarps);
-  rollout_tiles_kernel<DT><<<(unsigned)(items < kMaxGrid ? items : kMaxGrid), kTileWarps * 32, 0, st>>>(d, items);
-  rc = launch_ok();
-  if (rc == FOPD_OK) {
-    rollout_finish_kernel<DT><<<(unsigned)d.B, kFinishThreads, 0, st>>>(d, tokens, logprob, mask, n_accepted, status);
-    rc = launch_ok();
+// CTAs that share a row, a position or a sequence: as many as keep `units` clusters of them resident at once.
+int cluster_for(int64_t units) {
+  int c = kRollMaxCluster;
+  while (c > 1 && units * c > kRollResident) c /= 2;
+  return c;
+}
+
+template <class Kernel>
+int launch_clusters(Kernel kernel, const RolloutDev &d, int64_t units, int c, cudaStream_t st) {
+  if (units * c > INT32_MAX) return FOPD_ERR_SIZE;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = c;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(units * c));
+  cfg.blockDim = dim3(kRollThreads);
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, d) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return FOPD_ERR_CUDA;
   }
+  return FOPD_OK;
+}
+
+// Tiles of a row, and how many of them share a slot when c CTAs have the row between them.
+template <int DT>
+void set_tiles(RolloutDev *d, int c) {
+  d->n_tiles = (d->vocab + TileShape<DT>::kElems - 1) / TileShape<DT>::kElems;
+  const int64_t slots = (int64_t)c * kTileSlots;
+  d->span = (int)((d->n_tiles + slots - 1) / slots);
+}
+
+// Relative error of a row's fp32 sum and of one weight.  An exponent y = x c - max c has two roundings, of c and of the
+// result: 2 * 2^-24 ln 2 |y|.  The mean of |y| over the distribution is its entropy less its min-entropy in bits, at
+// most (1 - s) log2(s (V - 1) / (1 - s)) for some s: 0.74 log2 V covers V <= 2^18, 0.82 log2 V all up to 2^30.  Two ex2
+// (2^-22 each) and a few roundings come on top.
+double sum_error(int64_t vocab) {
+  const double bits = std::log2((double)vocab), y = (vocab <= (1 << 18) ? 0.74 : 0.82) * bits + 0.5;
+  return 8.3e-8 * y + 8e-7;
+}
+
+template <int DT>
+int launch_draw(RolloutDev d, cudaStream_t st) {
+  const int c = cluster_for(d.B);
+  set_tiles<DT>(&d, c);
+  return d.ct64 == 0.0 ? launch_clusters(draw_kernel<DT, true>, d, d.B, c, st)
+                       : launch_clusters(draw_kernel<DT, false>, d, d.B, c, st);
+}
+
+template <int DT>
+int launch_verify(RolloutDev d, cudaStream_t st) {
+  const bool best = d.ct64 == 0.0;
+  const int64_t positions = (int64_t)d.B * (d.K + 1);
+  const int c = cluster_for(positions);
+  const bool look = positions > kRollResident;  // later positions start when earlier ones have been decided
+  const size_t pos_bytes = ((size_t)positions * sizeof(Position) + 255) & ~size_t(255);
+  char *tmp = nullptr;
+  int rc = scratch_alloc(reinterpret_cast<void **>(&tmp), pos_bytes + (look ? (size_t)d.B * sizeof(int32_t) : 0), st);
+  if (rc != FOPD_OK) return rc;
+  d.pos = reinterpret_cast<Position *>(tmp);
+  if (look) {
+    d.stop = reinterpret_cast<int32_t *>(tmp + pos_bytes);
+    if (cudaMemsetAsync(d.stop, 0x7f, (size_t)d.B * sizeof(int32_t), st) != cudaSuccess) rc = FOPD_ERR_CUDA;
+  }
+  set_tiles<DT>(&d, c);
+  if (rc == FOPD_OK)
+    rc = best ? launch_clusters(verify_sweep_kernel<DT, true>, d, positions, c, st)
+              : launch_clusters(verify_sweep_kernel<DT, false>, d, positions, c, st);
+  const int cf = best ? 1 : cluster_for(d.B);
+  set_tiles<DT>(&d, cf);
+  if (rc == FOPD_OK)
+    rc = best ? launch_clusters(verify_finish_kernel<DT, true>, d, d.B, cf, st)
+              : launch_clusters(verify_finish_kernel<DT, false>, d, d.B, cf, st);
   if (cudaFreeAsync(tmp, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   return rc;
 }
@@ -73,16 +128,23 @@ int fopd_verify_draft(const fopd_draft *d, int32_t *tokens, float *logprob, uint
   r.drow = d->draft_row_stride * esz;
   r.B = d->B;
   r.K = d->K;
-  r.best = d->temperature == 0.f;
+  r.tokens = tokens;
+  r.logprob = logprob;
+  r.mask = mask;
+  r.n_accepted = n_accepted;
+  r.status = status;
+  r.eps = sum_error(d->vocab);
   // a target without temperature never asks for the draft's probabilities: x is accepted if it is the best token
-  r.kind = d->K == 0 || r.best ? kDraftNone : !d->draft ? kDraftCertain : d->draft_temperature == 0.f ? kDraftBest : kDraftRows;
-  r.it = r.best ? 0.0 : 1.0 / (double)d->temperature;
-  r.id = r.kind == kDraftRows ? 1.0 / (double)d->draft_temperature : 0.0;
-  r.ct = (float)(r.it * 1.4426950408889634);
-  r.cd = (float)(r.id * 1.4426950408889634);
+  const bool best = d->temperature == 0.f;
+  r.kind = best || d->K == 0 ? kDraftNone : !d->draft ? kDraftCertain : d->draft_temperature == 0.f ? kDraftBest : kDraftRows;
+  r.ct64 = best ? 0.0 : 1.4426950408889634074 / (double)d->temperature;
+  r.cd64 = r.kind == kDraftRows ? 1.4426950408889634074 / (double)d->draft_temperature : 0.0;
+  r.ct = (float)r.ct64;
+  r.cd = (float)r.cd64;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return d->dtype == FOPD_BF16 ? launch_rollout<FOPD_BF16>(r, tokens, logprob, mask, n_accepted, status, st)
-                               : launch_rollout<FOPD_F32>(r, tokens, logprob, mask, n_accepted, status, st);
+  const bool bf16 = d->dtype == FOPD_BF16;
+  if (d->K == 0) return bf16 ? launch_draw<FOPD_BF16>(r, st) : launch_draw<FOPD_F32>(r, st);
+  return bf16 ? launch_verify<FOPD_BF16>(r, st) : launch_verify<FOPD_F32>(r, st);
 }
 
 int fopd_draw_tokens(const void *logits, const double *uniform, int64_t n_rows, int64_t vocab, int64_t row_stride,
