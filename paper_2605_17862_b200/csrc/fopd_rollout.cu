@@ -15,10 +15,11 @@ int cluster_for(int64_t units) {
   return c;
 }
 
+// early: the kernel may be set up while the one before it on the stream is still running (it waits for it itself).
 template <class Kernel>
-int launch_clusters(Kernel kernel, const RolloutDev &d, int64_t units, int c, cudaStream_t st) {
+int launch_clusters(Kernel kernel, const RolloutDev &d, int64_t units, int c, cudaStream_t st, bool early = false) {
   if (units * c > INT32_MAX) return FOPD_ERR_SIZE;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = c;
   attr[0].val.clusterDim.y = 1;
@@ -28,7 +29,9 @@ int launch_clusters(Kernel kernel, const RolloutDev &d, int64_t units, int c, cu
   cfg.blockDim = dim3(kRollThreads);
   cfg.stream = st;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = early ? 2 : 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   if (cudaLaunchKernelEx(&cfg, kernel, d) != cudaSuccess) {
     (void)cudaGetLastError();
     return FOPD_ERR_CUDA;
@@ -36,27 +39,28 @@ int launch_clusters(Kernel kernel, const RolloutDev &d, int64_t units, int c, cu
   return FOPD_OK;
 }
 
-// Tiles of a row, and how many of them share a slot when c CTAs have the row between them.
+// Parts of a row, and how many of them share a slot when c CTAs have the row between them: one where warps are to have
+// few parts each, two (one vector of a slot for each thread of the search) where a CTA has a row of its own.
 template <int DT>
-void set_tiles(RolloutDev *d, int c) {
-  d->n_tiles = (d->vocab + TileShape<DT>::kElems - 1) / TileShape<DT>::kElems;
-  const int64_t slots = (int64_t)c * kTileSlots;
-  d->span = (int)((d->n_tiles + slots - 1) / slots);
+void set_parts(RolloutDev *d, int c) {
+  d->n_parts = (d->vocab + kPartElems<DT> - 1) / kPartElems<DT>;
+  const int64_t slots = (int64_t)c * kSlots, least = (d->n_parts + slots - 1) / slots;
+  d->span = (int)(least > 2 ? least : c > 1 ? least : 2);
 }
 
 // Relative error of a row's fp32 sum and of one weight.  An exponent y = x c - max c has two roundings, of c and of the
 // result: 2 * 2^-24 ln 2 |y|.  The mean of |y| over the distribution is its entropy less its min-entropy in bits, at
 // most (1 - s) log2(s (V - 1) / (1 - s)) for some s: 0.74 log2 V covers V <= 2^18, 0.82 log2 V all up to 2^30.  Two ex2
-// (2^-22 each) and a few roundings come on top.
+// (2^-22 each) and eight roundings (2^-24) come on top.
 double sum_error(int64_t vocab) {
   const double bits = std::log2((double)vocab), y = (vocab <= (1 << 18) ? 0.74 : 0.82) * bits + 0.5;
-  return 8.3e-8 * y + 8e-7;
+  return 8.3e-8 * y + 1e-6;
 }
 
 template <int DT>
 int launch_draw(RolloutDev d, cudaStream_t st) {
   const int c = cluster_for(d.B);
-  set_tiles<DT>(&d, c);
+  set_parts<DT>(&d, c);
   return d.ct64 == 0.0 ? launch_clusters(draw_kernel<DT, true>, d, d.B, c, st)
                        : launch_clusters(draw_kernel<DT, false>, d, d.B, c, st);
 }
@@ -76,15 +80,15 @@ int launch_verify(RolloutDev d, cudaStream_t st) {
     d.stop = reinterpret_cast<int32_t *>(tmp + pos_bytes);
     if (cudaMemsetAsync(d.stop, 0x7f, (size_t)d.B * sizeof(int32_t), st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   }
-  set_tiles<DT>(&d, c);
+  set_parts<DT>(&d, c);
   if (rc == FOPD_OK)
     rc = best ? launch_clusters(verify_sweep_kernel<DT, true>, d, positions, c, st)
               : launch_clusters(verify_sweep_kernel<DT, false>, d, positions, c, st);
   const int cf = best ? 1 : cluster_for(d.B);
-  set_tiles<DT>(&d, cf);
+  set_parts<DT>(&d, cf);
   if (rc == FOPD_OK)
-    rc = best ? launch_clusters(verify_finish_kernel<DT, true>, d, d.B, cf, st)
-              : launch_clusters(verify_finish_kernel<DT, false>, d, d.B, cf, st);
+    rc = best ? launch_clusters(verify_finish_kernel<DT, true>, d, d.B, cf, st, true)
+              : launch_clusters(verify_finish_kernel<DT, false>, d, d.B, cf, st, true);
   if (cudaFreeAsync(tmp, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   return rc;
 }

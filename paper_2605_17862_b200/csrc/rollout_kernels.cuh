@@ -7,9 +7,9 @@
 // sweeps run in fp32 with a bound on their error, and a decision that lies within it is made again in
 // fp64: a few per cent of the draws.
 //
-// A row is cut into tiles of 256 16-byte vectors, one warp each; a cluster of C CTAs shares a row (or
-// a pair of rows), C such that few rows still fill the GPU.  A search goes over the CTAs' sums, the
-// owner's tile sums and the elements of one tile.
+// A row is cut into parts of 128 16-byte vectors, four for each lane of a warp, and a few parts make a
+// slot; a cluster of C CTAs shares a row (or a pair of rows), C such that few rows still fill the GPU.
+// A search goes over the CTAs' sums, the owner's slot sums and the elements of one slot.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -22,8 +22,10 @@ namespace cg = cooperative_groups;
 
 constexpr int kRollThreads = 256;
 constexpr int kRollWarps = kRollThreads / 32;
-constexpr int kTileVecs = 8;        // 16-byte vectors of a tile per lane of a warp
-constexpr int kTileSlots = 512;     // tiles per CTA; a longer row takes `span` tiles a slot
+constexpr int kLoadVecs = 4;        // 16-byte vectors of a part per lane of a warp, in flight together
+constexpr int kPartVecs = 32 * kLoadVecs;
+constexpr int kStages = 2;          // parts of a warp on their way to shared memory
+constexpr int kSlots = 256;         // slots per CTA
 constexpr int kRollMaxCluster = 8;
 constexpr int kRollResident = 592;  // CTAs of these kernels that 148 SMs hold at once (64 registers)
 
@@ -47,16 +49,16 @@ struct RolloutDev {
   const char *target, *draft;
   const int32_t *drafted, *n_draft;
   const double *uniform;
-  int64_t vocab, n_tiles;
+  int64_t vocab, n_parts;
   int64_t tseq, trow, dseq, drow;  // bytes
   int32_t B, K;
-  int kind;         // DraftKind
-  int span;         // tiles per slot
-  float ct, cd;     // log2(e) / temperature in fp32
+  int kind;            // DraftKind
+  int span;            // parts per slot
+  float ct, cd;        // log2(e) / temperature in fp32
   double ct64, cd64;
-  double eps;       // relative error of a row's fp32 sum (and of a weight)
-  Position *pos;    // [B, K + 1]
-  int32_t *stop;    // [B] the lowest position known not to be accepted, or NULL: nobody looks
+  double eps;          // relative error of a row's fp32 sum (and of a weight)
+  Position *pos;       // [B, K + 1]
+  int32_t *stop;       // [B] the lowest position known not to be accepted, or NULL: nobody looks
   int32_t *tokens;
   float *logprob;
   uint8_t *mask;
@@ -65,10 +67,7 @@ struct RolloutDev {
 };
 
 template <int DT>
-struct TileShape {
-  static constexpr int kElems = 32 * kTileVecs * Elem<DT>::kPerVec;
-  static_assert(32 * kTileVecs == kRollThreads, "a tile is one vector for each thread of a CTA");
-};
+constexpr int kPartElems = kPartVecs *Elem<DT>::kPerVec;
 
 __device__ __forceinline__ float warp_max(float x) {
   float r;
@@ -80,6 +79,16 @@ __device__ __forceinline__ double warp_sum(double x) {
   for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
   return x;
 }
+__device__ __forceinline__ double warp_scan(double x) {  // inclusive
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const double y = __shfl_up_sync(0xffffffffu, x, off);
+    if ((threadIdx.x & 31) >= off) x += y;
+  }
+  return x;
+}
+// 1 / T from log2(e) / T
+__device__ __forceinline__ double inv_temperature(double c) { return 0.69314718055994530942 * c; }
 
 // ---- loads ------------------------------------------------------------------------------------------
 
@@ -104,28 +113,196 @@ __device__ __forceinline__ uint4 row_vec(const char *row, int64_t i, int64_t V) 
   return E::pack(x);
 }
 
+// Copies a lane's vectors of one part of a row to where the same lane will read them; one group of asynchronous copies.
 template <int DT>
-__device__ __forceinline__ void load_tile(uint4 (&raw)[kTileVecs], const char *row, int64_t tile, int64_t V) {
-  const int64_t i0 = tile * (32 * kTileVecs) + (threadIdx.x & 31);
-  if ((tile + 1) * TileShape<DT>::kElems <= V) {
+__device__ __forceinline__ void copy_part(uint4 *to, const char *row, int64_t part, int64_t V) {
+  const int lane = threadIdx.x & 31;
+  const int64_t i0 = part * kPartVecs + lane;
+  if ((part + 1) * kPartElems<DT> <= V) {
     const uint4 *p = reinterpret_cast<const uint4 *>(row) + i0;
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to + lane);
 #pragma unroll
-    for (int v = 0; v < kTileVecs; ++v) raw[v] = ld_row(p + v * 32);
+    for (int v = 0; v < kLoadVecs; ++v)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + v * 512), "l"(p + v * 32) : "memory");
   } else {
 #pragma unroll
-    for (int v = 0; v < kTileVecs; ++v) raw[v] = row_vec<DT>(row, i0 + v * 32, V);
+    for (int v = 0; v < kLoadVecs; ++v) to[v * 32 + lane] = row_vec<DT>(row, i0 + v * 32, V);
   }
 }
 
-// ---- fp32 sums --------------------------------------------------------------------------------------
+// ---- 2^y in fp64 ------------------------------------------------------------------------------------
 
+// y rounded to sixteenths, 2^{j/16} from a table in shared memory (sixteen entries lie in sixteen banks) and six terms
+// of the Taylor series of 2^f, |f| <= 1/32: error below 1e-15.
+__constant__ double kSixteenths[16] = {
+    1.0, 1.0442737824274138, 1.0905077326652577, 1.1387886347566916, 1.189207115002721, 1.241857812073484,
+    1.2968395546510096, 1.3542555469368927, 1.4142135623730951, 1.4768261459394993, 1.5422108254079407,
+    1.6104903319492543, 1.681792830507429, 1.7562521603732995, 1.8340080864093424, 1.9152065613971474};
+__device__ __forceinline__ void fill_exp64(double *tab) {
+  if (threadIdx.x < 16) tab[threadIdx.x] = kSixteenths[threadIdx.x];
+}
+
+// 2^{d c} with the product inside the fused multiply-adds; d c <= 0.  Below 2^-1000 whatever comes out is to be dropped.
+__device__ __forceinline__ double exp64_raw(double d, double c, const double *tab) {
+  constexpr double kRound = 6755399441055744.0 / 16;  // 1.5 * 2^52 / 16: adding it rounds to sixteenths
+  const double t = fma(d, c, kRound);
+  const double f = fma(d, c, kRound - t);
+  const int n = __double2loint(t);
+  double p = 1.540353039338161e-4;
+  p = fma(p, f, 1.3333558146428443e-3);
+  p = fma(p, f, 9.618129107628477e-3);
+  p = fma(p, f, 5.550410866482158e-2);
+  p = fma(p, f, 2.4022650695910072e-1);
+  p = fma(p, f, 6.931471805599453e-1);
+  p = fma(p, f, 1.0);
+  p *= tab[n & 15];
+  return __hiloint2double(__double2hiint(p) + ((n >> 4) << 20), __double2loint(p));
+}
+// The same without a table, for a value here and there: y rounded to a whole number, eleven terms, |f| <= 1/2: 1e-14.
+__device__ __forceinline__ double exp64(double d, double c) {
+  constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52
+  const double t = fma(d, c, kRound);
+  const double f = fma(d, c, kRound - t);
+  double p = 4.4455382718708116e-10;
+  p = fma(p, f, 7.054911620801123e-9);
+  p = fma(p, f, 1.01780860092397e-7);
+  p = fma(p, f, 1.321548679014431e-6);
+  p = fma(p, f, 1.5252733804059841e-5);
+  p = fma(p, f, 1.540353039338161e-4);
+  p = fma(p, f, 1.3333558146428443e-3);
+  p = fma(p, f, 9.618129107628477e-3);
+  p = fma(p, f, 5.550410866482158e-2);
+  p = fma(p, f, 2.4022650695910072e-1);
+  p = fma(p, f, 6.931471805599453e-1);
+  p = fma(p, f, 1.0);
+  p = __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
+  return d * c >= -1000.0 ? p : 0.0;  // (not a number counts as nothing: the sum it belongs to tells)
+}
+// The same of an element x and a row's maximum; least: below it the result is nothing (-infinity has no fraction).
+__device__ __forceinline__ double weight64(float x, double m, double c, float least, const double *tab) {
+  const double p = exp64_raw((double)x - m, c, tab);
+  return x >= least ? p : 0.0;
+}
+__device__ __forceinline__ float least_of(float m, double c) { return (float)((double)m - 1000.0 / c); }
+
+// ---- sweeps -----------------------------------------------------------------------------------------
+
+// Two fp32 in one register pair: one instruction works on both.
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 pair(float lo, float hi) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void split(f32x2 x, float &lo, float &hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x));
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 exp2_2(f32x2 y) {
+  float lo, hi;
+  split(y, lo, hi);
+  return pair(ex2(lo), ex2(hi));
+}
+// Element pairs of a vector.
+template <int DT>
+__device__ __forceinline__ void unpack2(const uint4 &v, f32x2 (&x)[Elem<DT>::kPerVec / 2]) {
+  float f[Elem<DT>::kPerVec];
+  Elem<DT>::unpack(v, f);
+#pragma unroll
+  for (int k = 0; k < Elem<DT>::kPerVec / 2; ++k) x[k] = pair(f[2 * k], f[2 * k + 1]);
+}
 template <int N>
-__device__ __forceinline__ float tree_sum(float (&x)[N]) {
+__device__ __forceinline__ f32x2 tree_sum2(f32x2 (&x)[N]) {
 #pragma unroll
   for (int n = N / 2; n > 0; n >>= 1)
 #pragma unroll
-    for (int k = 0; k < n; ++k) x[k] += x[k + n];
+    for (int k = 0; k < n; ++k) x[k] = add2(x[k], x[k + n]);
   return x[0];
+}
+__device__ __forceinline__ float both(f32x2 x) {
+  float lo, hi;
+  split(x, lo, hi);
+  return lo + hi;
+}
+
+// Largest element of some vectors, without unpacking bf16.
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <int DT, int N>
+__device__ __forceinline__ float max_vecs(const uint4 (&raw)[N]) {
+  if (DT == FOPD_BF16) {
+    uint32_t m = 0xff80ff80u;
+#pragma unroll
+    for (int v = 0; v < N; ++v)
+      m = max_bf16x2(m, max_bf16x2(max_bf16x2(raw[v].x, raw[v].y), max_bf16x2(raw[v].z, raw[v].w)));
+    return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+  }
+  float m = -INFINITY;
+#pragma unroll
+  for (int v = 0; v < N; ++v)
+    m = max3(max3(m, __uint_as_float(raw[v].x), __uint_as_float(raw[v].y)), __uint_as_float(raw[v].z), __uint_as_float(raw[v].w));
+  return m;
+}
+
+__device__ __forceinline__ RowSum nothing() { return {-INFINITY, INT32_MAX, 0.0}; }
+
+// Sums of a row, tile after tile: {max, sum 2^{(x - max) c}} with the maximum the warp's and the sum the lane's own.
+// The exponent is x c - fl(max c) in one fused multiply-add; what fl() took away is the same for all elements and put
+// back at the end.  -infinity everywhere gives {-inf, 0}; a NaN or +inf makes the sum NaN.
+template <int DT>
+__device__ __forceinline__ void add_part(RowSum &acc, const uint4 (&raw)[kLoadVecs], float c, double c64) {
+  using E = Elem<DT>;
+  constexpr int P = E::kPerVec;
+  float m = warp_max(max_vecs<DT>(raw));
+  if (m > acc.m) {
+    if (acc.m != -INFINITY) acc.z *= exp64((double)acc.m - m, c64);
+    acc.m = m;
+  }
+  m = acc.m;
+  const float mc = m == -INFINITY ? 0.f : m * c;
+  double z;
+  if (fabsf(mc) <= 1e38f) {
+    const f32x2 c2 = pair(c, c), mc2 = pair(-mc, -mc);
+    f32x2 sums[kLoadVecs];
+#pragma unroll
+    for (int v = 0; v < kLoadVecs; ++v) {
+      f32x2 x[P / 2];
+      unpack2<DT>(raw[v], x);
+#pragma unroll
+      for (int k = 0; k < P / 2; ++k) x[k] = exp2_2(fma2(x[k], c2, mc2));
+      sums[v] = tree_sum2<P / 2>(x);
+    }
+    float s = both(tree_sum2<kLoadVecs>(sums));
+    if (m != -INFINITY) s *= ex2(-fmaf(m, c, -mc));
+    z = (double)s;
+  } else {  // max c is beyond fp32 (or max is infinite: NaN)
+    z = 0.0;
+#pragma unroll  // (a loop would put raw[] into local memory)
+    for (int v = 0; v < kLoadVecs; ++v) {
+      float x[P];
+      E::unpack(raw[v], x);
+#pragma unroll
+      for (int k = 0; k < P; ++k) z += (double)ex2((x[k] - m) * c);
+    }
+  }
+  acc.z += z;
 }
 
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -134,104 +311,100 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
-// {max, lowest index of it} of one tile, in every lane; a NaN anywhere gives NaN.
+// {max, lowest index of it} so far, in every lane; a NaN anywhere gives NaN.
 template <int DT>
-__device__ __forceinline__ RowSum tile_best(const char *row, int64_t tile, int64_t V) {
+__device__ __forceinline__ void add_best(RowSum &acc, const uint4 (&raw)[kLoadVecs], int64_t part) {
   using E = Elem<DT>;
   constexpr int P = E::kPerVec;
-  uint4 raw[kTileVecs];
-  load_tile<DT>(raw, row, tile, V);
   float m = -INFINITY;
 #pragma unroll
-  for (int v = 0; v < kTileVecs; ++v) {
+  for (int v = 0; v < kLoadVecs; ++v) {
     float x[P];
     E::unpack(raw[v], x);
 #pragma unroll
     for (int k = 0; k < P; ++k) m = max_nan(m, x[k]);
   }
-  if (__any_sync(0xffffffffu, isnan(m))) return {NAN, INT32_MAX, 1.0};
+  if (__any_sync(0xffffffffu, isnan(m))) {
+    acc.m = NAN;
+    return;
+  }
   const float top = warp_max(m);
+  if (!(top > acc.m)) return;  // (earlier parts hold lower indices; a NaN stays)
   int32_t at = INT32_MAX;
   if (m == top) {
 #pragma unroll
-    for (int v = kTileVecs - 1; v >= 0; --v) {
+    for (int v = kLoadVecs - 1; v >= 0; --v) {
       float x[P];
       E::unpack(raw[v], x);
 #pragma unroll
       for (int k = P - 1; k >= 0; --k)
-        if (x[k] == top) at = (int32_t)((tile * (32 * kTileVecs) + v * 32 + (threadIdx.x & 31)) * P + k);
+        if (x[k] == top) at = (int32_t)((part * kPartVecs + v * 32 + (threadIdx.x & 31)) * P + k);
     }
   }
-  return {top, (int32_t)__reduce_min_sync(0xffffffffu, at), 1.0};
+  acc.best = (int32_t)__reduce_min_sync(0xffffffffu, at);
+  acc.m = top;
 }
 
-// Sums of a row, tile after tile: {max, sum 2^{(x - max) c}} with the maximum the warp's and the sum the lane's own.
-// The exponent is x c - fl(max c) in one fused multiply-add; what fl() took away is the same for all elements and put
-// back at the end.  -infinity everywhere gives {-inf, 0}; a NaN or +inf makes the sum NaN.
-template <int DT>
-__device__ __forceinline__ void add_tile(RowSum &acc, const char *row, int64_t tile, int64_t V, float c, double c64) {
-  using E = Elem<DT>;
-  constexpr int P = E::kPerVec;
-  uint4 raw[kTileVecs];
-  load_tile<DT>(raw, row, tile, V);
-  float m = -INFINITY;
+// A warp's sweep over the slots first, first + step, ... below end of a row, `parts` parts each.  The next kStages parts
+// are on their way to the warp's corner of shared memory while one is worked on: with registers as their landing place
+// an SM had 64 KB in flight, which was not enough (4.9 TB/s).  flush(slot, acc) closes a slot.
+template <int DT, bool kBest, class Flush>
+__device__ __forceinline__ void sweep(RowSum &acc, const char *row, int64_t V, int64_t first, int64_t end, int64_t step,
+                                      int parts, float c, double c64, uint4 *ring, Flush flush) {
+  if (first >= end) return;
+  const int lane = threadIdx.x & 31;
+  int64_t ahead = first;  // the next part to ask for: slot and part in it
+  int ahead_p = 0;
 #pragma unroll
-  for (int v = 0; v < kTileVecs; ++v) {
-    float x[P];
-    E::unpack(raw[v], x);
-    m = fmaxf(m, max_of<P>(x));
-  }
-  m = warp_max(m);
-  if (m > acc.m) {
-    acc.z = acc.m == -INFINITY ? acc.z : acc.z * exp2(((double)acc.m - m) * c64);
-    acc.m = m;
-  }
-  m = acc.m;
-  const float mc = m == -INFINITY ? 0.f : m * c;
-  double z = 0.0;
-  if (fabsf(mc) <= 1e38f) {
-#pragma unroll
-    for (int v = 0; v < kTileVecs; ++v) {
-      float x[P];
-      E::unpack(raw[v], x);
-#pragma unroll
-      for (int k = 0; k < P; ++k) x[k] = ex2(fmaf(x[k], c, -mc));
-      z += (double)tree_sum<P>(x);
-    }
-    if (m != -INFINITY) z *= (double)ex2(-fmaf(m, c, -mc));
-  } else {  // max c is beyond fp32 (or max is infinite: NaN)
-    for (int v = 0; v < kTileVecs; ++v) {
-      float x[P];
-      E::unpack(raw[v], x);
-#pragma unroll
-      for (int k = 0; k < P; ++k) x[k] = ex2((x[k] - m) * c);
-      z += (double)tree_sum<P>(x);
+  for (int k = 0; k < kStages; ++k) {
+    if (ahead < end) copy_part<DT>(ring + k * kPartVecs, row, ahead * parts + ahead_p, V);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (++ahead_p == parts) {
+      ahead_p = 0;
+      ahead += step;
     }
   }
-  acc.z += z;
-}
-
-// Two parts of a row as one.  (2^y in fp64: a few hundred merges a row, and their error stays out of the bound.)
-__device__ __forceinline__ RowSum merge(const RowSum &a, const RowSum &b, double c) {
-  if (b.m == -INFINITY && !isnan(b.z)) return a;
-  if (a.m == -INFINITY && !isnan(a.z)) return b;
-  if (a.m >= b.m) return {a.m, a.best, a.z + b.z * exp2(((double)b.m - a.m) * c)};
-  return {b.m, b.best, b.z + a.z * exp2(((double)a.m - b.m) * c)};  // (NaN maxima: is_distribution sees them)
-}
-__device__ __forceinline__ RowSum merge_best(const RowSum &a, const RowSum &b) {
-  const bool first = isnan(a.m) || (!isnan(b.m) && (a.m > b.m || (a.m == b.m && a.best <= b.best)));
-  return first ? a : b;
-}
-__device__ __forceinline__ RowSum nothing() { return {-INFINITY, INT32_MAX, 0.0}; }
-
-__device__ __forceinline__ RowSum shfl_xor(const RowSum &a, int lanes) {
-  return {__shfl_xor_sync(0xffffffffu, a.m, lanes), __shfl_xor_sync(0xffffffffu, a.best, lanes),
-          __shfl_xor_sync(0xffffffffu, a.z, lanes)};
-}
-template <bool kBest>
-__device__ __forceinline__ RowSum warp_merge(RowSum a, double c) {
+  uint4 *stage = ring;
+  for (int64_t slot = first; slot < end; slot += step) {
+#pragma unroll 1
+    for (int p = 0; p < parts; ++p) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+      uint4 raw[kLoadVecs];
 #pragma unroll
-  for (int off = 16; off > 0; off >>= 1) a = kBest ? merge_best(a, shfl_xor(a, off)) : merge(a, shfl_xor(a, off), c);
+      for (int v = 0; v < kLoadVecs; ++v) raw[v] = stage[v * 32 + lane];
+      if (ahead < end) copy_part<DT>(stage, row, ahead * parts + ahead_p, V);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      if (++ahead_p == parts) {
+        ahead_p = 0;
+        ahead += step;
+      }
+      stage = stage + kPartVecs == ring + kStages * kPartVecs ? ring : stage + kPartVecs;
+      if (kBest) add_best<DT>(acc, raw, slot * parts + p);
+      else add_part<DT>(acc, raw, c, c64);
+    }
+    flush(slot, acc);
+  }
+}
+
+// The lanes' parts of a row as one, in every lane (2^y in fp64: its error stays out of the bound).
+__device__ __forceinline__ double part_of(const RowSum &a, float m, double c) {
+  return a.m == m ? a.z : a.z * exp64((double)a.m - m, c);
+}
+__device__ __forceinline__ RowSum warp_merge(const RowSum &a, double c) {
+  const float m = warp_max(a.m);
+  return {m, 0, warp_sum(part_of(a, m, c))};
+}
+__device__ __forceinline__ RowSum warp_merge_best(RowSum a) {
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) {
+    const float m = __shfl_xor_sync(0xffffffffu, a.m, off);
+    const int32_t at = __shfl_xor_sync(0xffffffffu, a.best, off);
+    const bool keep = isnan(a.m) || (!isnan(m) && (a.m > m || (a.m == m && a.best <= at)));
+    if (!keep) {
+      a.m = m;
+      a.best = at;
+    }
+  }
   return a;
 }
 
@@ -239,34 +412,7 @@ __device__ __forceinline__ bool is_distribution(const RowSum &r) {
   return r.m > -INFINITY && r.m < INFINITY && r.z > 0.0 && r.z < INFINITY;
 }
 
-// ---- fp64 weights -----------------------------------------------------------------------------------
-
-// 2^{(x - m) c}: the exponent rounded to sixteenths, 2^{j/16} from a table in shared memory (sixteen entries lie in
-// sixteen banks) and six terms of the Taylor series of 2^f, |f| <= 1/32: error below 1e-15.
-struct Exp64 {
-  const double *tab;
-  __device__ __forceinline__ double operator()(float x, double m, double c, float least) const {
-    constexpr double kRound = 6755399441055744.0 / 16;  // 1.5 * 2^52 / 16: adding it rounds to sixteenths
-    const double d = (double)x - m;
-    const double t = fma(d, c, kRound);
-    const double f = fma(d, c, kRound - t);
-    const int n = __double2loint(t);
-    double p = 1.5403530393381608e-4;
-    p = fma(p, f, 1.3333558146428443e-3);
-    p = fma(p, f, 9.6181291076284772e-3);
-    p = fma(p, f, 5.5504108664821580e-2);
-    p = fma(p, f, 2.4022650695910071e-1);
-    p = fma(p, f, 6.9314718055994531e-1);
-    p = fma(p, f, 1.0);
-    p *= tab[n & 15];
-    p = __hiloint2double(__double2hiint(p) + ((n >> 4) << 20), __double2loint(p));
-    return x >= least ? p : 0.0;  // 2^-1000 and less is nothing (and -infinity has no f)
-  }
-};
-__device__ __forceinline__ void fill_exp64(double *tab) {
-  if (threadIdx.x < 16) tab[threadIdx.x] = exp2((double)threadIdx.x / 16.0);
-}
-__device__ __forceinline__ float least_of(float m, double c) { return (float)((double)m - 1000.0 / c); }
+// ---- weights ----------------------------------------------------------------------------------------
 
 // Weights of the distribution a token is drawn from, a vector of elements at a time.
 enum WeightKind { kWPlain = 0, kWWithout = 1, kWRest = 2 };
@@ -280,54 +426,66 @@ struct Weights {
   RowSum ts, qs;
   float ct, cd;
   double ct64, cd64;
+  const double *tab;
   // derived
   float mct, mcd, a, b;  // fl(max c); 2^{what fl() took} / sum
   float least_t, least_q;
   double ia, ib;         // 1 / sum
-  Exp64 e;
 
   __device__ __forceinline__ void derive() {
     mct = ts.m * ct;
-    a = kind == kWRest ? (float)((double)ex2(-fmaf(ts.m, ct, -mct)) / ts.z) : 1.f;
     least_t = least_of(ts.m, ct64);
-    ia = 1.0 / ts.z;
     if (kind == kWRest) {
+      a = (float)((double)ex2(-fmaf(ts.m, ct, -mct)) / ts.z);
+      ia = 1.0 / ts.z;
       mcd = qs.m * cd;
       b = (float)((double)ex2(-fmaf(qs.m, cd, -mcd)) / qs.z);
       least_q = least_of(qs.m, cd64);
       ib = 1.0 / qs.z;
     }
   }
-  // fp32's exponent cannot be formed (see tile_sum)
+  // fp32's exponent cannot be formed (see add_tile)
   __device__ __forceinline__ bool beyond() const {
     return !(fabsf(mct) <= 1e38f) || (kind == kWRest && !(fabsf(mcd) <= 1e38f));
   }
-
-  __device__ __forceinline__ void fast(int64_t i, const uint4 &rt, const uint4 &rq, float (&w)[P]) const {
-    float x[P];
-    Elem<DT>::unpack(rt, x);
+  __device__ __forceinline__ void load(int64_t i, uint4 &rt, uint4 &rq) const {
+    rt = row_vec<DT>(t, i, V);
+    rq = kind == kWRest ? row_vec<DT>(q, i, V) : make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ void fast(int64_t i, const uint4 &rt, const uint4 &rq, f32x2 (&w)[P / 2]) const {
+    const f32x2 c2 = pair(ct, ct), m2 = pair(-mct, -mct);
+    unpack2<DT>(rt, w);
 #pragma unroll
-    for (int k = 0; k < P; ++k) w[k] = ex2(fmaf(x[k], ct, -mct));
+    for (int k = 0; k < P / 2; ++k) w[k] = exp2_2(fma2(w[k], c2, m2));
     if (kind == kWRest) {
-      Elem<DT>::unpack(rq, x);
+      const f32x2 d2 = pair(cd, cd), n2 = pair(-mcd, -mcd), a2 = pair(a, a), b2 = pair(-b, -b);
+      f32x2 x[P / 2];
+      unpack2<DT>(rq, x);
 #pragma unroll
-      for (int k = 0; k < P; ++k) w[k] = fmaxf(fmaf(w[k], a, -b * ex2(fmaf(x[k], cd, -mcd))), 0.f);
-    } else if (kind == kWWithout) {
+      for (int k = 0; k < P / 2; ++k) {
+        float lo, hi;
+        split(fma2(w[k], a2, mul2(exp2_2(fma2(x[k], d2, n2)), b2)), lo, hi);
+        w[k] = pair(fmaxf(lo, 0.f), fmaxf(hi, 0.f));
+      }
+    } else if (kind == kWWithout && without / P == i) {
 #pragma unroll
-      for (int k = 0; k < P; ++k)
-        if (i * P + k == without) w[k] = 0.f;
+      for (int k = 0; k < P / 2; ++k) {
+        float lo, hi;
+        split(w[k], lo, hi);
+        w[k] = pair(2 * k == without % P ? 0.f : lo, 2 * k + 1 == without % P ? 0.f : hi);
+      }
     }
   }
   __device__ __forceinline__ void exact(int64_t i, const uint4 &rt, const uint4 &rq, double (&w)[P]) const {
     float x[P];
     Elem<DT>::unpack(rt, x);
 #pragma unroll
-    for (int k = 0; k < P; ++k) w[k] = e(x[k], ts.m, ct64, least_t);
+    for (int k = 0; k < P; ++k) w[k] = weight64(x[k], ts.m, ct64, least_t, tab);
     if (kind == kWRest) {
       Elem<DT>::unpack(rq, x);
 #pragma unroll
       for (int k = 0; k < P; ++k)  // (both products rounded alike: equal rows leave exactly nothing)
-        w[k] = fmax(__dsub_rn(__dmul_rn(w[k], ia), __dmul_rn(e(x[k], qs.m, cd64, least_q), ib)), 0.0);
+        w[k] = fmax(__dsub_rn(__dmul_rn(w[k], ia), __dmul_rn(weight64(x[k], qs.m, cd64, least_q, tab), ib)), 0.0);
     } else if (kind == kWWithout) {
 #pragma unroll
       for (int k = 0; k < P; ++k)
@@ -336,8 +494,7 @@ struct Weights {
   }
   // sum of a vector's weights, in fp64 from the vector up
   template <bool kExact>
-  __device__ __forceinline__ double vec_sum(int64_t i) const {
-    const uint4 rt = row_vec<DT>(t, i, V), rq = kind == kWRest ? row_vec<DT>(q, i, V) : make_uint4(0, 0, 0, 0);
+  __device__ __forceinline__ double sum(int64_t i, const uint4 &rt, const uint4 &rq) const {
     if (kExact) {
       double w[P], s = 0.0;
       exact(i, rt, rq, w);
@@ -345,44 +502,51 @@ struct Weights {
       for (int k = 0; k < P; ++k) s += w[k];
       return s;
     }
-    float w[P];
+    f32x2 w[P / 2];
     fast(i, rt, rq, w);
-    return (double)tree_sum<P>(w);
+    return (double)both(tree_sum2<P / 2>(w));
   }
 };
 
 // ---- a CTA's and a cluster's tools ------------------------------------------------------------------
 
+__device__ __forceinline__ void roll_sync(cg::cluster_group &cl) {
+  if (cl.num_blocks() > 1) cl.sync();
+  else __syncthreads();
+}
+
+// CTAs of a cluster write into one another's shared memory before a barrier of the cluster and read their own behind
+// it; so a CTA may leave when it has passed its last barrier.
 struct RollShared {
-  double tz[kTileSlots];  // tile sums of this CTA
-  float tm[kTileSlots];
+  uint4 ring[kRollWarps][kStages * kPartVecs];
+  double tz[kSlots];  // slot sums of this CTA, relative to 2^{tm c} where they come from the sweep
+  float tm[kSlots];
   double scan[kRollWarps];
   double tab[16];
   RowSum part[2][kRollWarps];
-  RowSum pub[2][2];       // what other CTAs of the cluster read: [exchange parity][row]
+  RowSum pub[2][kRollMaxCluster];  // the CTAs' totals, by parity of the exchange
+  double sums[2][kRollMaxCluster];
+  RowSum total;
   double before, goal;
   int64_t slot;
-  int32_t owner, result, flag[2];
+  float logit;  // of the element found
+  int32_t owner, result, thread, unsure, stop;
 };
 
-// This CTA's slots of a row: [lo, hi) of ceil(n_tiles / span), contiguous and in rank order.
+// This CTA's slots of a row: [lo, hi) of ceil(n_parts / span), contiguous and in rank order.
 struct Slots {
   int64_t lo, hi;
 };
 __device__ __forceinline__ Slots my_slots(const RolloutDev &d, int rank, int size) {
-  const int64_t n = (d.n_tiles + d.span - 1) / d.span, per = (n + size - 1) / size;
+  const int64_t n = (d.n_parts + d.span - 1) / d.span, per = (n + size - 1) / size;
   const int64_t lo = rank * per, hi = lo + per;
   return {lo < n ? lo : n, hi < n ? hi : n};
 }
 
-// Inclusive scan over the CTA's threads.
+// Inclusive scan over the CTA's threads; the warps' sums stay in scan[] until the next call.
 __device__ __forceinline__ double cta_scan(double x, double *scan) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-  for (int off = 1; off < 32; off <<= 1) {
-    const double y = __shfl_up_sync(0xffffffffu, x, off);
-    if (lane >= off) x += y;
-  }
+  x = warp_scan(x);
   __syncthreads();
   if (lane == 31) scan[warp] = x;
   __syncthreads();
@@ -395,35 +559,45 @@ __device__ __forceinline__ double cta_scan(double x, double *scan) {
 
 constexpr int32_t kUnsure = -2;  // within the bound, or another CTA's
 
-// The element of tiles [tile0, tile0 + span) whose running sum (starting at `before`) passes `goal`; where rounding
-// leaves none, the last one with a weight.  Same result in every thread.
+// The element of slot `slot` whose running sum (starting at `before`) passes `goal`; where rounding leaves none, the
+// last one with a weight.  Same result in every thread; its logit is left in sh.logit.
 template <int DT, bool kExact>
-__device__ int32_t cta_find(const Weights<DT> &w, const RolloutDev &d, int64_t tile0, double before, double goal,
+__device__ int32_t cta_find(const Weights<DT> &w, const RolloutDev &d, int64_t slot, double before, double goal,
                             double bound, RollShared &sh) {
   constexpr int P = Weights<DT>::P;
   if (threadIdx.x == 0) sh.result = kUnsure;
-  const int64_t tiles = min((int64_t)d.span, d.n_tiles - tile0);
-  int64_t last = 0;  // the last tile with a weight, and the running sum before it
+  const int64_t vec0 = slot * d.span * kPartVecs, vecs = min((int64_t)d.span, d.n_parts - slot * d.span) * kPartVecs;
+  const int64_t rounds = (vecs + kRollThreads - 1) / kRollThreads;  // a vector for each thread
+  int64_t last = 0;  // the last round with a weight, and the running sum before it
   double last_before = before;
-  for (int64_t s = 0; s <= tiles; ++s) {
-    const bool back = s == tiles;  // no tile passes: the last weight it is
-    const int64_t i = (tile0 + (back ? last : s)) * kRollThreads + threadIdx.x;
+  for (int64_t s = 0; s <= rounds; ++s) {
+    const bool back = s == rounds;  // no round passes: the last weight it is
+    const int64_t o = (back ? last : s) * kRollThreads + threadIdx.x, i = vec0 + o;
     if (back) before = last_before;
     double x[P], sum = 0.0;
-    const uint4 rt = row_vec<DT>(w.t, i, d.vocab),
-                rq = w.kind == kWRest ? row_vec<DT>(w.q, i, d.vocab) : make_uint4(0, 0, 0, 0);
+    uint4 rt = make_uint4(0, 0, 0, 0), rq = rt;
+    if (o < vecs) w.load(i, rt, rq);
     if (kExact) {
       w.exact(i, rt, rq, x);
     } else {
-      float y[P];
+      f32x2 y[P / 2];
       w.fast(i, rt, rq, y);
 #pragma unroll
-      for (int k = 0; k < P; ++k) x[k] = (double)y[k];
+      for (int k = 0; k < P / 2; ++k) {
+        float lo, hi;
+        split(y[k], lo, hi);
+        x[2 * k] = (double)lo;
+        x[2 * k + 1] = (double)hi;
+      }
     }
 #pragma unroll
-    for (int k = 0; k < P; ++k) sum += x[k];
+    for (int k = 0; k < P; ++k) {
+      if (o >= vecs) x[k] = 0.0;
+      sum += x[k];
+    }
     const double incl = before + cta_scan(sum, sh.scan);
     const bool here = sum > 0.0 && (back || incl > goal);
+    if (threadIdx.x == 0) sh.thread = back ? -1 : kRollThreads;
     if (!__syncthreads_or(here)) {
       if (__syncthreads_or(sum > 0.0)) {
         last = s;
@@ -433,24 +607,25 @@ __device__ int32_t cta_find(const Weights<DT> &w, const RolloutDev &d, int64_t t
       for (int k = 0; k < kRollWarps; ++k) before += sh.scan[k];
       continue;
     }
-    if (threadIdx.x == 0) sh.flag[0] = back ? -1 : kRollThreads;
+    if (here && back) atomicMax(&sh.thread, (int)threadIdx.x);
+    else if (here) atomicMin(&sh.thread, (int)threadIdx.x);
     __syncthreads();
-    if (here && back) atomicMax(&sh.flag[0], (int)threadIdx.x);
-    else if (here) atomicMin(&sh.flag[0], (int)threadIdx.x);
-    __syncthreads();
-    if (sh.flag[0] == (int)threadIdx.x) {
+    if (sh.thread == (int)threadIdx.x) {
       double run = incl - sum, at_before = run, at_after = run;
-      int32_t at = kUnsure;
+      int at = -1;
 #pragma unroll
       for (int k = 0; k < P; ++k) {
         if (x[k] > 0.0 && (at < 0 || at_after <= goal)) {
-          at = (int32_t)(i * P + k);
+          at = k;
           at_before = run;
           at_after = run + x[k];
         }
         run += x[k];
       }
-      if (kExact || (goal - at_before > bound && at_after - goal > bound)) sh.result = at;
+      if (kExact || (goal - at_before > bound && at_after - goal > bound)) {
+        sh.result = (int32_t)(i * P + at);
+        sh.logit = Elem<DT>::load1(w.t, i * P + at);
+      }
     }
     break;
   }
@@ -458,11 +633,10 @@ __device__ int32_t cta_find(const Weights<DT> &w, const RolloutDev &d, int64_t t
   return sh.result;
 }
 
-// Search over the cluster.  On entry this CTA's slots have their sums in sh.tz relative to 2^{tm c} (or all to the same
-// reference: relative false).  The CTAs exchange their totals; the owner of the goal looks through its slots, then its
-// tile.  Returns the token in the owner's threads and elsewhere kUnsure; *total in all.  Whether the cluster is to do
-// it again in fp64 comes back in *again.  One cluster barrier before the search and, in fp32, one behind it; the other
-// CTAs' shared memory may still be read after the last one.  kRelative: w gets the row's sum.
+// Search over the cluster.  On entry this CTA's slots have their sums in sh.tz: relative to 2^{tm c} (kRelative: w then
+// gets the row's sum) or all to one reference.  The CTAs exchange their totals; the owner of the goal looks through its
+// slots, then through one slot's elements.  Returns the token in the owner's threads and elsewhere kUnsure, the total
+// and whether the cluster is to do it again in fp64 in all threads.
 template <int DT, bool kExact, bool kRelative>
 __device__ int32_t cluster_search(cg::cluster_group &cl, Weights<DT> &w, const RolloutDev &d, Slots sl, double v,
                                   double bound_rel, double bound_abs, int parity, RollShared &sh, RowSum *total,
@@ -471,91 +645,86 @@ __device__ int32_t cluster_search(cg::cluster_group &cl, Weights<DT> &w, const R
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int n = (int)(sl.hi - sl.lo);
   if (warp == 0) {
-    RowSum r = nothing();
+    // a lane takes a run of slots
+    const int per = (n + 31) / 32, lo = min(n, lane * per), hi = min(n, lo + per);
+    RowSum own = {0.f, 0, 0.0};
     if (kRelative) {
-      for (int t = lane; t < n; t += 32) r = merge(r, RowSum{sh.tm[t], 0, sh.tz[t]}, d.ct64);
-      r = warp_merge<false>(r, d.ct64);
-    } else {
-      double s = 0.0;
-      for (int t = lane; t < n; t += 32) s += sh.tz[t];
-      r = {0.f, 0, warp_sum(s)};
+      own.m = -INFINITY;
+      for (int t = lo; t < hi; ++t) own.m = fmaxf(own.m, sh.tm[t]);
+      own.m = warp_max(own.m);
     }
-    if (lane == 0) sh.pub[parity][0] = r;
-  }
-  cl.sync();
-  if (warp == 0) {
-    RowSum mine = nothing();
-    if (lane < size) mine = *cl.map_shared_rank(&sh.pub[parity][0], lane);
-    const RowSum all = warp_merge<false>(mine, d.ct64);
-    const double part = lane < size && mine.z > 0.0 ? mine.z * exp2(((double)mine.m - all.m) * d.ct64) : 0.0;
-    double incl = part;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const double y = __shfl_up_sync(0xffffffffu, incl, off);
-      if (lane >= off) incl += y;
+    double s = 0.0;
+    for (int t = lo; t < hi; ++t) {
+      double x = sh.tz[t];
+      if (kRelative) sh.tz[t] = x = part_of({sh.tm[t], 0, x}, own.m, d.ct64);
+      s += x;
     }
-    double sum = __shfl_sync(0xffffffffu, incl, 31);
-    const double goal = v * sum;
-    if (isnan(all.z)) sum = all.z;
-    const unsigned pass = __ballot_sync(0xffffffffu, part > 0.0 && incl > goal), has = __ballot_sync(0xffffffffu, part > 0.0);
-    const int owner = pass ? __ffs(pass) - 1 : has ? 31 - __clz(has) : 0;
-    const double before = __shfl_sync(0xffffffffu, incl - part, owner);
+    const double incl = warp_scan(s);
+    own.z = __shfl_sync(0xffffffffu, incl, 31);
+    RowSum all = own;
+    double goal = v * own.z, before = 0.0, scale = 1.0;
+    int owner = 0;
+    if (size > 1) {
+      if (lane < size) *cl.map_shared_rank(&sh.pub[parity][rank], lane) = own;
+      cl.sync();
+      const RowSum mine = lane < size ? sh.pub[parity][lane] : nothing();
+      all.m = warp_max(mine.m);
+      const double part = part_of(mine, all.m, d.ct64), run = warp_scan(part);
+      all.z = __shfl_sync(0xffffffffu, run, 31);
+      goal = v * all.z;
+      const unsigned pass = __ballot_sync(0xffffffffu, part > 0.0 && run > goal),
+                     has = __ballot_sync(0xffffffffu, part > 0.0);
+      owner = pass ? __ffs(pass) - 1 : has ? 31 - __clz(has) : 0;
+      before = __shfl_sync(0xffffffffu, run - part, owner);
+      scale = part_of({own.m, 0, 1.0}, all.m, d.ct64);
+    }
     if (lane == 0) {
-      sh.pub[parity][1] = {all.m, 0, sum};
+      sh.total = all;
       sh.owner = owner;
       sh.goal = goal;
-      sh.before = before;
     }
-    __syncwarp();
-    if (owner == rank && is_distribution({all.m, 0, sum})) {  // this CTA's slots
-      double run = before;
-      int64_t slot = -1, last = -1;
-      double at = run, last_at = run;
-      for (int base = 0; base < n && slot < 0; base += 32) {
-        const int t = base + lane;
-        const double x = t < n && sh.tz[t] > 0.0
-                             ? sh.tz[t] * (kRelative ? exp2(((double)sh.tm[t] - all.m) * d.ct64) : 1.0) : 0.0;
-        double in = x;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-          const double y = __shfl_up_sync(0xffffffffu, in, off);
-          if (lane >= off) in += y;
+    if (owner == rank && is_distribution(all)) {  // the first run that passes, or the last one with a weight
+      const unsigned pass = __ballot_sync(0xffffffffu, s > 0.0 && before + scale * incl > goal),
+                     has = __ballot_sync(0xffffffffu, s > 0.0);
+      if (lane == (pass ? __ffs(pass) - 1 : 31 - __clz(has))) {
+        double run = before + scale * (incl - s), at = run;
+        int slot = lo;
+        for (int t = lo; t < hi; ++t) {
+          const double x = sh.tz[t] * scale;
+          if (x > 0.0) {
+            slot = t;
+            at = run;
+            if (run + x > goal) break;
+          }
+          run += x;
         }
-        const unsigned p = __ballot_sync(0xffffffffu, x > 0.0 && run + in > goal), h = __ballot_sync(0xffffffffu, x > 0.0);
-        const int l = p ? __ffs(p) - 1 : h ? 31 - __clz(h) : -1;
-        const double b = __shfl_sync(0xffffffffu, run + in - x, l < 0 ? 0 : l);
-        if (p) {
-          slot = base + l;
-          at = b;
-        } else if (h) {
-          last = base + l;
-          last_at = b;
-        }
-        run += __shfl_sync(0xffffffffu, in, 31);
-      }
-      if (lane == 0) {
-        sh.slot = sl.lo + (slot >= 0 ? slot : last);
-        sh.before = slot >= 0 ? at : last_at;
+        sh.slot = sl.lo + slot;
+        sh.before = at;
       }
     }
+  } else if (size > 1) {
+    cl.sync();
   }
   __syncthreads();
-  *total = sh.pub[parity][1];
+  *total = sh.total;
   int32_t token = kUnsure;
-  const bool good = is_distribution(*total);
-  if (good && sh.owner == rank) {
+  const bool good = is_distribution(*total), mine = good && sh.owner == rank;
+  if (mine) {
     if (kRelative) {
       w.ts = *total;
       w.derive();
     }
-    const double bound = bound_rel * total->z + bound_abs;
-    token = cta_find<DT, kExact>(w, d, sh.slot * d.span, sh.before, sh.goal, bound, sh);
-    if (threadIdx.x == 0) sh.flag[1] = token == kUnsure;
+    token = cta_find<DT, kExact>(w, d, sh.slot, sh.before, sh.goal, bound_rel * total->z + bound_abs, sh);
   }
   *again = false;
   if (!kExact) {
-    cl.sync();
-    if (good) *again = *cl.map_shared_rank(&sh.flag[1], sh.owner) != 0;
+    if (size == 1) {
+      *again = good && token == kUnsure;
+    } else {
+      if (mine && (int)threadIdx.x < size) *cl.map_shared_rank(&sh.unsure, threadIdx.x) = token == kUnsure;
+      cl.sync();
+      *again = good && sh.unsure;
+    }
   }
   return token;
 }
@@ -566,20 +735,25 @@ __device__ __forceinline__ void cta_slot_sums(const Weights<DT> &w, const Rollou
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int64_t t = sl.lo + warp; t < sl.hi; t += kRollWarps) {
     double s = 0.0;
-    const int64_t end = min((t + 1) * d.span, d.n_tiles);
-    for (int64_t tile = t * d.span; tile < end; ++tile)
+    const int64_t end = min((t + 1) * d.span, d.n_parts) * kPartVecs;
+    constexpr int kU = 2;
+    for (int64_t i = t * d.span * kPartVecs + lane; i < end; i += 32 * kU) {
+      uint4 rt[kU], rq[kU];
 #pragma unroll
-      for (int v = 0; v < kTileVecs; ++v) s += w.template vec_sum<kExact>(tile * kRollThreads + v * 32 + lane);
+      for (int u = 0; u < kU; ++u) w.load(i + 32 * u, rt[u], rq[u]);
+#pragma unroll
+      for (int u = 0; u < kU; ++u) s += w.template sum<kExact>(i + 32 * u, rt[u], rq[u]);
+    }
     s = warp_sum(s);
     if (lane == 0) sh.tz[t - sl.lo] = s;
   }
   __syncthreads();
 }
 
-// A row's sum of exponentials in fp64, over the cluster, in every thread.
+// A row's sum of exponentials in fp64, over the cluster, in every thread.  parity alternates from call to call.
 template <int DT>
 __device__ double cluster_exact_sum(cg::cluster_group &cl, const char *row, float m, double c, const RolloutDev &d,
-                                    Slots sl, RollShared &sh) {
+                                    Slots sl, int &parity, RollShared &sh) {
   Weights<DT> w = {};
   w.t = row;
   w.V = d.vocab;
@@ -587,23 +761,26 @@ __device__ double cluster_exact_sum(cg::cluster_group &cl, const char *row, floa
   w.ts = {m, 0, 1.0};
   w.ct64 = c;
   w.least_t = least_of(m, c);
-  w.e.tab = sh.tab;
+  w.tab = sh.tab;
   cta_slot_sums<DT, true>(w, d, sl, sh);
+  const int size = (int)cl.num_blocks();
   if (threadIdx.x < 32) {
     double s = 0.0;
     for (int t = threadIdx.x; t < (int)(sl.hi - sl.lo); t += 32) s += sh.tz[t];
     s = warp_sum(s);
-    if (threadIdx.x == 0) sh.pub[0][0].z = s;
+    if ((int)threadIdx.x < size) *cl.map_shared_rank(&sh.sums[parity][cl.block_rank()], threadIdx.x) = s;
   }
-  cl.sync();
+  roll_sync(cl);
   double s = 0.0;
-  for (unsigned k = 0; k < cl.num_blocks(); ++k) s += cl.map_shared_rank(&sh.pub[0][0], k)->z;
-  cl.sync();  // the sums have been read
+  for (int k = 0; k < size; ++k) s += sh.sums[parity][k];
+  parity ^= 1;
   return s;
 }
 
-// 1 / T from log2(e) / T
-__device__ __forceinline__ double inv_temperature(double c) { return 0.69314718055994530942 * c; }
+// log p of an element of a row from its logit and the row's sum: the difference in fp64, the log's error is 1e-6 of it.
+__device__ __forceinline__ float log_prob(float logit, const RowSum &r, double c64) {
+  return (float)(((double)logit - r.m) * inv_temperature(c64) - (double)logf((float)r.z));
+}
 
 // ---- draws: a cluster per row -----------------------------------------------------------------------
 
@@ -616,84 +793,75 @@ __global__ void __launch_bounds__(kRollThreads, 4) draw_kernel(const __grid_cons
   const int64_t n = blockIdx.x / size;
   const char *row = d.target + n * d.tseq;
   const Slots sl = my_slots(d, rank, size);
-  RowSum best = nothing();
-  for (int64_t t = sl.lo + warp; t < sl.hi; t += kRollWarps) {
-    RowSum r = nothing();
-    const int64_t end = min((t + 1) * d.span, d.n_tiles);
-    for (int64_t tile = t * d.span; tile < end; ++tile) {
-      if (kBest) best = merge_best(best, tile_best<DT>(row, tile, d.vocab));
-      else add_tile<DT>(r, row, tile, d.vocab, d.ct, d.ct64);
-    }
-    if (!kBest) {
-      r.z = warp_sum(r.z);
-      if (lane == 0) {
-        sh.tm[t - sl.lo] = r.m;
-        sh.tz[t - sl.lo] = r.z;
-      }
-    }
-  }
+  const double v = kBest ? 0.0 : d.uniform[n];
+  RowSum acc = nothing();
+  sweep<DT, kBest>(acc, row, d.vocab, sl.lo + warp, sl.hi, kRollWarps, d.span, d.ct, d.ct64, sh.ring[warp],
+                   [&](int64_t slot, RowSum &r) {
+                     if (kBest) return;
+                     r.z = warp_sum(r.z);
+                     if (lane == 0) {
+                       sh.tm[slot - sl.lo] = r.m;
+                       sh.tz[slot - sl.lo] = r.z;
+                     }
+                     r = nothing();
+                   });
+  int32_t token = kUnsure;
+  float lp = 0.f;
+  bool good;
+  int bits = FOPD_DEV_BAD_LOGITS;
   if (kBest) {
-    if (lane == 0) sh.part[0][warp] = best;
+    if (lane == 0) sh.part[0][warp] = acc;
     __syncthreads();
     if (warp == 0) {
-      const RowSum r = warp_merge<true>(lane < kRollWarps ? sh.part[0][lane] : nothing(), 0.0);
-      if (lane == 0) sh.pub[0][0] = r;
+      const RowSum r = warp_merge_best(lane < kRollWarps ? sh.part[0][lane] : nothing());
+      if (lane < size) *cl.map_shared_rank(&sh.pub[0][rank], lane) = r;
     }
-    cl.sync();
-    if (rank == 0 && warp == 0) {
-      const RowSum r = warp_merge<true>(lane < size ? *cl.map_shared_rank(&sh.pub[0][0], lane) : nothing(), 0.0);
-      if (lane == 0) {
-        const bool good = r.m > -INFINITY && r.m < INFINITY;
-        d.tokens[n] = good ? r.best : -1;
-        if (d.logprob) d.logprob[n] = 0.f;
-        if (d.mask) d.mask[n] = good ? 1 : 0;
-        if (d.n_accepted) d.n_accepted[n] = 0;
-        if (!good && d.status) atomicOr(d.status, FOPD_DEV_BAD_LOGITS);
-      }
+    roll_sync(cl);
+    RowSum r = nothing();
+    if (warp == 0) r = warp_merge_best(lane < size ? sh.pub[0][lane] : nothing());
+    good = r.m > -INFINITY && r.m < INFINITY;  // (warp 0)
+    if (rank == 0 && good) token = r.best;
+  } else {
+    __syncthreads();
+    const bool v_ok = v >= 0.0 && v < 1.0;
+    Weights<DT> w = {};
+    w.t = row;
+    w.V = d.vocab;
+    w.kind = kWPlain;
+    w.without = -1;
+    w.ct = d.ct;
+    w.ct64 = d.ct64;
+    w.tab = sh.tab;
+    RowSum total;
+    bool again;
+    token = cluster_search<DT, false, true>(cl, w, d, sl, v_ok ? v : 0.0, 2 * d.eps, 0.0, 0, sh, &total, &again);
+    good = is_distribution(total) && v_ok;
+    if (is_distribution(total)) bits = FOPD_DEV_BAD_UNIFORM;
+    if (again && good) {
+      fill_exp64(sh.tab);
+      __syncthreads();
+      w.ts = total;
+      w.derive();
+      cta_slot_sums<DT, true>(w, d, sl, sh);
+      RowSum exact_total;
+      bool never;
+      token = cluster_search<DT, true, false>(cl, w, d, sl, v, 0.0, 0.0, 1, sh, &exact_total, &never);
     }
-    cl.sync();  // nobody leaves while its shared memory is read
-    return;
+    if (good && token >= 0 && threadIdx.x == 0) lp = log_prob(sh.logit, total, d.ct64);
   }
-  fill_exp64(sh.tab);
-  __syncthreads();
-  const double v = d.uniform[n];
-  const bool v_ok = v >= 0.0 && v < 1.0;
-  Weights<DT> w = {};
-  w.t = row;
-  w.V = d.vocab;
-  w.kind = kWPlain;
-  w.without = -1;
-  w.ct = d.ct;
-  w.ct64 = d.ct64;
-  w.e.tab = sh.tab;
-  RowSum total;
-  bool again;
-  int32_t token = cluster_search<DT, false, true>(cl, w, d, sl, v_ok ? v : 0.0, 2 * d.eps, 0.0, 0, sh, &total, &again);
-  const bool good = is_distribution(total) && v_ok;
-  const double z = total.z;
-  if (again && good) {
-    w.ts = total;
-    w.derive();
-    cta_slot_sums<DT, true>(w, d, sl, sh);
-    RowSum exact_total;
-    bool never;
-    token = cluster_search<DT, true, false>(cl, w, d, sl, v, 0.0, 0.0, 1, sh, &exact_total, &never);
-  }
-  if (good && token >= 0 && threadIdx.x == 0) {
+  if (threadIdx.x == 0 && good && token >= 0) {
     d.tokens[n] = token;
-    if (d.logprob)
-      d.logprob[n] = (float)(((double)Elem<DT>::load1(row, token) - total.m) * inv_temperature(d.ct64) - log(z));
+    if (d.logprob) d.logprob[n] = lp;
   }
-  if (!good && rank == 0 && threadIdx.x == 0) {
-    d.tokens[n] = -1;
-    if (d.logprob) d.logprob[n] = 0.f;
-    if (d.status) atomicOr(d.status, is_distribution(total) ? FOPD_DEV_BAD_UNIFORM : FOPD_DEV_BAD_LOGITS);
-  }
-  if (rank == 0 && threadIdx.x == 0) {
+  if (threadIdx.x == 0 && rank == 0) {
+    if (!good) {
+      d.tokens[n] = -1;
+      if (d.logprob) d.logprob[n] = 0.f;
+      if (d.status) atomicOr(d.status, bits);
+    }
     if (d.mask) d.mask[n] = good ? 1 : 0;
     if (d.n_accepted) d.n_accepted[n] = 0;
   }
-  cl.sync();  // nobody leaves while its shared memory is read
 }
 
 // ---- verification -----------------------------------------------------------------------------------
@@ -705,7 +873,8 @@ __device__ __forceinline__ int32_t drafts_of(const RolloutDev &d, int32_t b) {
 
 // Decides on one position from its rows' sums.
 template <int DT>
-__device__ __forceinline__ void judge(const RolloutDev &d, int32_t b, int32_t j, int32_t n, bool target_best, Position &o) {
+__device__ __forceinline__ void judge(const RolloutDev &d, int32_t b, int32_t j, int32_t n, bool target_best,
+                                      Position &o) {
   using E = Elem<DT>;
   o.lp = 0.f;
   o.state = is_distribution(o.t) ? kEnd : kBadRow;
@@ -719,12 +888,12 @@ __device__ __forceinline__ void judge(const RolloutDev &d, int32_t b, int32_t j,
   } else if (!(u >= 0.0 && u < 1.0)) {
     o.state = kBadUniform;
   } else {
-    const double y = ((double)E::load1(d.target + b * d.tseq + j * d.trow, x) - o.t.m) * inv_temperature(d.ct64);
-    const double p = exp(y) / o.t.z;
-    o.lp = (float)(y - log(o.t.z));
+    const float logit = E::load1(d.target + b * d.tseq + j * d.trow, x);
+    const double p = exp64((double)logit - o.t.m, d.ct64) / o.t.z;
+    o.lp = log_prob(logit, o.t, d.ct64);
     double q = 1.0;
     if (d.kind == kDraftRows)
-      q = exp(((double)E::load1(d.draft + b * d.dseq + j * d.drow, x) - o.q.m) * inv_temperature(d.cd64)) / o.q.z;
+      q = exp64((double)E::load1(d.draft + b * d.dseq + j * d.drow, x) - o.q.m, d.cd64) / o.q.z;
     else if (d.kind == kDraftBest)
       q = x == o.q.best ? 1.0 : 0.0;
     const double uq = u * q;
@@ -739,6 +908,7 @@ __device__ __forceinline__ void judge(const RolloutDev &d, int32_t b, int32_t j,
 template <int DT, bool kBest>
 __global__ void __launch_bounds__(kRollThreads, 4) verify_sweep_kernel(const __grid_constant__ RolloutDev d) {
   __shared__ RollShared sh;
+  asm volatile("griddepcontrol.launch_dependents;");  // the finish may be set up beside the last positions
   cg::cluster_group cl = cg::this_cluster();
   const int rank = (int)cl.block_rank(), size = (int)cl.num_blocks();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -749,45 +919,39 @@ __global__ void __launch_bounds__(kRollThreads, 4) verify_sweep_kernel(const __g
   // (one thread looks: the value may change between two looks)
   if (d.stop && __syncthreads_or(threadIdx.x == 0 && *(volatile const int32_t *)(d.stop + b) < j)) return;
   const char *trow = d.target + b * d.tseq + j * d.trow, *qrow = d.draft + b * d.dseq + j * d.drow;
-  const bool want_q = j < n && (d.kind == kDraftRows || d.kind == kDraftBest);
+  const bool q_best = d.kind == kDraftBest, want_q = j < n && (d.kind == kDraftRows || q_best);
   RowSum t = nothing(), q = nothing();
-  for (int64_t tile = rank * kRollWarps + warp; tile < d.n_tiles; tile += size * kRollWarps) {
-    if (kBest) t = merge_best(t, tile_best<DT>(trow, tile, d.vocab));
-    else add_tile<DT>(t, trow, tile, d.vocab, d.ct, d.ct64);
-  }
+  const int64_t first = rank * kRollWarps + warp, step = size * kRollWarps;
+  const auto nop = [](int64_t, RowSum &) {};
+  sweep<DT, kBest>(t, trow, d.vocab, first, d.n_parts, step, 1, d.ct, d.ct64, sh.ring[warp], nop);
   if (want_q) {
-    if (d.kind == kDraftBest)
-      for (int64_t tile = rank * kRollWarps + warp; tile < d.n_tiles; tile += size * kRollWarps)
-        q = merge_best(q, tile_best<DT>(qrow, tile, d.vocab));
-    else
-      for (int64_t tile = rank * kRollWarps + warp; tile < d.n_tiles; tile += size * kRollWarps)
-        add_tile<DT>(q, qrow, tile, d.vocab, d.cd, d.cd64);
+    if (q_best) sweep<DT, true>(q, qrow, d.vocab, first, d.n_parts, step, 1, d.cd, d.cd64, sh.ring[warp], nop);
+    else sweep<DT, false>(q, qrow, d.vocab, first, d.n_parts, step, 1, d.cd, d.cd64, sh.ring[warp], nop);
   }
   if (!kBest) t.z = warp_sum(t.z);
-  if (d.kind == kDraftRows) q.z = warp_sum(q.z);
+  if (!q_best) q.z = warp_sum(q.z);
   if (lane == 0) {
     sh.part[0][warp] = t;
     sh.part[1][warp] = q;
   }
   __syncthreads();
-  const bool q_best = d.kind == kDraftBest;
   if (warp == 0) {
     t = lane < kRollWarps ? sh.part[0][lane] : nothing();
     q = lane < kRollWarps ? sh.part[1][lane] : nothing();
-    t = kBest ? warp_merge<true>(t, 0.0) : warp_merge<false>(t, d.ct64);
-    if (want_q) q = q_best ? warp_merge<true>(q, 0.0) : warp_merge<false>(q, d.cd64);
-    if (lane == 0) {
-      sh.pub[0][0] = t;
-      sh.pub[0][1] = q;
+    t = kBest ? warp_merge_best(t) : warp_merge(t, d.ct64);
+    if (want_q) q = q_best ? warp_merge_best(q) : warp_merge(q, d.cd64);
+    if (lane == 0 && size > 1) {
+      *cl.map_shared_rank(&sh.pub[0][rank], 0) = t;
+      *cl.map_shared_rank(&sh.pub[1][rank], 0) = q;
     }
   }
   if (size > 1) {
     cl.sync();
     if (rank == 0 && warp == 0) {
-      t = lane < size ? *cl.map_shared_rank(&sh.pub[0][0], lane) : nothing();
-      q = lane < size ? *cl.map_shared_rank(&sh.pub[0][1], lane) : nothing();
-      t = kBest ? warp_merge<true>(t, 0.0) : warp_merge<false>(t, d.ct64);
-      if (want_q) q = q_best ? warp_merge<true>(q, 0.0) : warp_merge<false>(q, d.cd64);
+      t = lane < size ? sh.pub[0][lane] : nothing();
+      q = lane < size ? sh.pub[1][lane] : nothing();
+      t = kBest ? warp_merge_best(t) : warp_merge(t, d.ct64);
+      if (want_q) q = q_best ? warp_merge_best(q) : warp_merge(q, d.cd64);
     }
   }
   if (rank == 0 && threadIdx.x == 0) {
@@ -800,7 +964,6 @@ __global__ void __launch_bounds__(kRollThreads, 4) verify_sweep_kernel(const __g
     d.pos[(int64_t)b * (d.K + 1) + j] = o;
     if (d.stop && j < n && o.state != kAccept && o.state != kOpen) atomicMin(d.stop + b, j);
   }
-  if (size > 1) cl.sync();
 }
 
 // A cluster per sequence: the first position that is not accepted (an open one is settled in fp64), the new token,
@@ -809,7 +972,6 @@ template <int DT, bool kBest>
 __global__ void __launch_bounds__(kRollThreads, 2) verify_finish_kernel(const __grid_constant__ RolloutDev d) {
   using E = Elem<DT>;
   __shared__ RollShared sh;
-  __shared__ int stop;
   cg::cluster_group cl = cg::this_cluster();
   const int rank = (int)cl.block_rank(), size = (int)cl.num_blocks();
   const int32_t b = blockIdx.x / size;
@@ -817,69 +979,69 @@ __global__ void __launch_bounds__(kRollThreads, 2) verify_finish_kernel(const __
   int bits = d.n_draft && d.n_draft[b] != n ? FOPD_DEV_BAD_LENGTH : 0;
   const Position *pos = d.pos + (int64_t)b * W;
   const Slots sl = my_slots(d, rank, size);
-  if (!kBest) fill_exp64(sh.tab);
+  fill_exp64(sh.tab);
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // the sweep's positions are there
   const int32_t limit = d.stop && d.stop[b] < n ? d.stop[b] : n;  // positions behind it may have been left out
 
   int32_t j = 0;
-  int state;
+  int state, parity = 0;
   for (int32_t from = 0;; from = j + 1) {
-    if (threadIdx.x == 0) stop = limit;
+    if (threadIdx.x == 0) sh.stop = limit;
     __syncthreads();
     for (int32_t k = from + threadIdx.x; k < limit; k += kRollThreads)
       if (pos[k].state != kAccept) {
-        atomicMin(&stop, k);
+        atomicMin(&sh.stop, k);
         break;
       }
     __syncthreads();
-    j = stop;
+    j = sh.stop;
     __syncthreads();
     state = pos[j].state;
     if (kBest || state != kOpen) break;
-    const int64_t at = (int64_t)b * d.K + j;
-    const int32_t x = d.drafted[at];
+    const int32_t x = d.drafted[(int64_t)b * d.K + j];
     const char *trow = d.target + b * d.tseq + j * d.trow, *qrow = d.draft + b * d.dseq + j * d.drow;
-    const double p = exp(((double)E::load1(trow, x) - pos[j].t.m) * inv_temperature(d.ct64)) /
-                     cluster_exact_sum<DT>(cl, trow, pos[j].t.m, d.ct64, d, sl, sh);
+    const double p = exp64((double)E::load1(trow, x) - pos[j].t.m, d.ct64) /
+                     cluster_exact_sum<DT>(cl, trow, pos[j].t.m, d.ct64, d, sl, parity, sh);
     double q = 1.0;  // (kDraftBest: or 0 and then never open)
     if (d.kind == kDraftRows)
-      q = exp(((double)E::load1(qrow, x) - pos[j].q.m) * inv_temperature(d.cd64)) /
-          cluster_exact_sum<DT>(cl, qrow, pos[j].q.m, d.cd64, d, sl, sh);
+      q = exp64((double)E::load1(qrow, x) - pos[j].q.m, d.cd64) /
+          cluster_exact_sum<DT>(cl, qrow, pos[j].q.m, d.cd64, d, sl, parity, sh);
     if (!(d.uniform[(int64_t)b * W + j] * q < p)) {
       state = kReject;
       break;
     }
   }
 
-  int32_t token = -1;  // in the threads that know it
+  int32_t token = kUnsure;  // in the threads that know it
   float lp = 0.f;
+  bool there = false;       // a token comes out
   const double v = d.uniform[(int64_t)b * W + d.K];
-  bool there = false;  // a token comes out
   if (state == kBadToken) bits |= FOPD_DEV_BAD_TOKEN;
   if (state == kBadRow) {
     bits |= FOPD_DEV_BAD_LOGITS;
     if (j < n && is_distribution(pos[j].t) && (uint32_t)d.drafted[(int64_t)b * d.K + j] >= (uint64_t)d.vocab)
       bits |= FOPD_DEV_BAD_TOKEN;
-  } else if (state == kBadUniform) bits |= FOPD_DEV_BAD_UNIFORM;
-  else if (kBest) {
-    token = rank == 0 ? pos[j].t.best : -1;
+  } else if (state == kBadUniform) {
+    bits |= FOPD_DEV_BAD_UNIFORM;
+  } else if (kBest) {
+    if (rank == 0) token = pos[j].t.best;
     there = true;
-  } else if (!(v >= 0.0 && v < 1.0)) bits |= FOPD_DEV_BAD_UNIFORM;
-  else {
+  } else if (!(v >= 0.0 && v < 1.0)) {
+    bits |= FOPD_DEV_BAD_UNIFORM;
+  } else {
     there = true;
+    const RowSum t32 = pos[j].t, q32 = pos[j].q;
     Weights<DT> w = {};
     w.t = d.target + b * d.tseq + j * d.trow;
     w.q = d.draft + b * d.dseq + j * d.drow;
     w.V = d.vocab;
     w.kind = j == n ? kWPlain : d.kind == kDraftRows ? kWRest : kWWithout;
-    w.without = j == n ? -1 : d.kind == kDraftBest ? pos[j].q.best : d.kind == kDraftCertain ? d.drafted[(int64_t)b * d.K + j] : -1;
-    w.ts = pos[j].t;
-    w.qs = pos[j].q;
+    w.without = j == n ? -1 : d.kind == kDraftBest ? q32.best : d.kind == kDraftCertain ? d.drafted[(int64_t)b * d.K + j] : -1;
     w.ct = d.ct;
     w.cd = d.cd;
     w.ct64 = d.ct64;
     w.cd64 = d.cd64;
-    w.e.tab = sh.tab;
-    const RowSum t32 = w.ts, q32 = w.qs;
+    w.tab = sh.tab;
     RowSum total;
     for (int round = 0; round < 2; ++round) {  // the second one only where p - q is zero everywhere
       bool again = true;
@@ -888,31 +1050,24 @@ __global__ void __launch_bounds__(kRollThreads, 2) verify_finish_kernel(const __
       w.derive();
       if (!w.beyond()) {
         cta_slot_sums<DT, false>(w, d, sl, sh);
-        // p - q: both rows' weights and both their sums are off; else the row's sum as a whole counts, without what was
-        // taken away
-        token = cluster_search<DT, false, false>(cl, w, d, sl, v, 0.0, w.kind == kWRest ? 8 * d.eps : 2 * d.eps * t32.z, 0, sh,
-                                                 &total, &again);
+        // p - q: both rows' weights and both their sums are off; else the row's whole sum counts, with what was taken away
+        token = cluster_search<DT, false, false>(cl, w, d, sl, v, 0.0, w.kind == kWRest ? 8 * d.eps : 2 * d.eps * t32.z,
+                                                 0, sh, &total, &again);
         if (!is_distribution(total)) again = true;
       }
-      if (again) {
-        if (w.kind == kWRest) {
-          w.ts.z = cluster_exact_sum<DT>(cl, w.t, w.ts.m, d.ct64, d, sl, sh);
-          w.qs.z = cluster_exact_sum<DT>(cl, w.q, w.qs.m, d.cd64, d, sl, sh);
-          w.derive();
-        }
-        cta_slot_sums<DT, true>(w, d, sl, sh);
-        bool never;
-        token = cluster_search<DT, true, false>(cl, w, d, sl, v, 0.0, 0.0, 1, sh, &total, &never);
-        cl.sync();
-        if (!is_distribution(total)) {  // nothing left
-          w.kind = kWPlain;
-          continue;
-        }
+      if (!again) break;
+      if (w.kind == kWRest) {
+        w.ts.z = cluster_exact_sum<DT>(cl, w.t, w.ts.m, d.ct64, d, sl, parity, sh);
+        w.qs.z = cluster_exact_sum<DT>(cl, w.q, w.qs.m, d.cd64, d, sl, parity, sh);
+        w.derive();
       }
-      break;
+      cta_slot_sums<DT, true>(w, d, sl, sh);
+      bool never;
+      token = cluster_search<DT, true, false>(cl, w, d, sl, v, 0.0, 0.0, 1, sh, &total, &never);
+      if (is_distribution(total)) break;
+      w.kind = kWPlain;
     }
-    if (token >= 0 && threadIdx.x == 0)
-      lp = (float)(((double)E::load1(w.t, token) - t32.m) * inv_temperature(d.ct64) - log(t32.z));
+    if (token >= 0 && threadIdx.x == 0) lp = log_prob(sh.logit, t32, d.ct64);
   }
   const int64_t at = (int64_t)b * W;
   if (token >= 0 && threadIdx.x == 0) {
@@ -930,7 +1085,6 @@ __global__ void __launch_bounds__(kRollThreads, 2) verify_finish_kernel(const __
       if (d.mask) d.mask[at + k] = k < j ? 1 : 0;
     }
   }
-  cl.sync();  // nobody leaves while its shared memory is read
 }
 
 }  // namespace fopd
