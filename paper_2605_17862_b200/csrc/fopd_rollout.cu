@@ -48,47 +48,73 @@ void set_parts(RolloutDev *d, int c) {
   d->span = (int)(least > 2 ? least : c > 1 ? least : 2);
 }
 
-// Relative error of a row's fp32 sum and of one weight.  An exponent y = x c - max c has two roundings, of c and of the
-// result: 2 * 2^-24 ln 2 |y|.  The mean of |y| over the distribution is its entropy less its min-entropy in bits, at
-// most (1 - s) log2(s (V - 1) / (1 - s)) for some s: 0.74 log2 V covers V <= 2^18, 0.82 log2 V all up to 2^30.  Two ex2
-// (2^-22 each) and eight roundings (2^-24) come on top.
-double sum_error(int64_t vocab) {
+// Relative error of a row's fp32 sum and of one weight.  An exponent y = x c - max c is off by the rounding of c (known
+// here) and its own (2^-24 |y|).  The mean of |y| over the distribution is its entropy less its min-entropy in bits, at
+// most (1 - s) log2(s (V - 1) / (1 - s)) for some s: 0.74 log2 V covers V <= 2^18, 0.82 log2 V all up to 2^30.  An ex2
+// (2^-22) and six roundings (2^-24) come on top.
+double sum_error(int64_t vocab, float c, double c64) {
   const double bits = std::log2((double)vocab), y = (vocab <= (1 << 18) ? 0.74 : 0.82) * bits + 0.5;
-  return 8.3e-8 * y + 1e-6;
+  return 0.6932 * (5.97e-8 + std::fabs((double)c - c64) / c64) * y + 6.2e-7;
+}
+
+// Rows (or sequences) that fewer than kRollMaxCluster CTAs share are put on a list when fp32 does not decide them, and a
+// second launch goes through the list with clusters of that size.
+size_t later_bytes(int64_t units) { return ((size_t)units + 1) * sizeof(int32_t); }
+int64_t list_clusters(int64_t units) {
+  const int64_t most = kRollResident / kRollMaxCluster;
+  return units < most ? units : most;
 }
 
 template <int DT>
 int launch_draw(RolloutDev d, cudaStream_t st) {
   const int c = cluster_for(d.B);
   set_parts<DT>(&d, c);
-  return d.ct64 == 0.0 ? launch_clusters(draw_kernel<DT, true>, d, d.B, c, st)
-                       : launch_clusters(draw_kernel<DT, false>, d, d.B, c, st);
+  if (d.ct64 == 0.0) return launch_clusters(draw_kernel<DT, true, true>, d, d.B, c, st);
+  if (c == kRollMaxCluster) return launch_clusters(draw_kernel<DT, false, false>, d, d.B, c, st);
+  int rc = scratch_alloc(reinterpret_cast<void **>(&d.later), later_bytes(d.B), st);
+  if (rc != FOPD_OK) return rc;
+  if (cudaMemsetAsync(d.later, 0, sizeof(int32_t), st) != cudaSuccess) rc = FOPD_ERR_CUDA;
+  if (rc == FOPD_OK) rc = launch_clusters(draw_kernel<DT, false, true>, d, d.B, c, st);
+  set_parts<DT>(&d, kRollMaxCluster);
+  if (rc == FOPD_OK) rc = launch_clusters(draw_kernel<DT, false, false>, d, list_clusters(d.B), kRollMaxCluster, st, true);
+  if (cudaFreeAsync(d.later, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
+  return rc;
 }
 
 template <int DT>
 int launch_verify(RolloutDev d, cudaStream_t st) {
   const bool best = d.ct64 == 0.0;
   const int64_t positions = (int64_t)d.B * (d.K + 1);
-  const int c = cluster_for(positions);
+  const int c = cluster_for(positions), cf = best ? 1 : cluster_for(d.B);
   const bool look = positions > kRollResident;  // later positions start when earlier ones have been decided
+  const bool defer = !best && cf < kRollMaxCluster;
   const size_t pos_bytes = ((size_t)positions * sizeof(Position) + 255) & ~size_t(255);
+  const size_t stop_bytes = look ? (size_t)d.B * sizeof(int32_t) : 0;
   char *tmp = nullptr;
-  int rc = scratch_alloc(reinterpret_cast<void **>(&tmp), pos_bytes + (look ? (size_t)d.B * sizeof(int32_t) : 0), st);
+  int rc = scratch_alloc(reinterpret_cast<void **>(&tmp), pos_bytes + stop_bytes + (defer ? later_bytes(d.B) : 0), st);
   if (rc != FOPD_OK) return rc;
   d.pos = reinterpret_cast<Position *>(tmp);
   if (look) {
     d.stop = reinterpret_cast<int32_t *>(tmp + pos_bytes);
-    if (cudaMemsetAsync(d.stop, 0x7f, (size_t)d.B * sizeof(int32_t), st) != cudaSuccess) rc = FOPD_ERR_CUDA;
+    if (cudaMemsetAsync(d.stop, 0x7f, stop_bytes, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
+  }
+  if (defer) {
+    d.later = reinterpret_cast<int32_t *>(tmp + pos_bytes + stop_bytes);
+    if (cudaMemsetAsync(d.later, 0, sizeof(int32_t), st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   }
   set_parts<DT>(&d, c);
   if (rc == FOPD_OK)
     rc = best ? launch_clusters(verify_sweep_kernel<DT, true>, d, positions, c, st)
               : launch_clusters(verify_sweep_kernel<DT, false>, d, positions, c, st);
-  const int cf = best ? 1 : cluster_for(d.B);
   set_parts<DT>(&d, cf);
   if (rc == FOPD_OK)
-    rc = best ? launch_clusters(verify_finish_kernel<DT, true>, d, d.B, cf, st, true)
-              : launch_clusters(verify_finish_kernel<DT, false>, d, d.B, cf, st, true);
+    rc = best    ? launch_clusters(verify_finish_kernel<DT, true, true>, d, d.B, cf, st, true)
+         : defer ? launch_clusters(verify_finish_kernel<DT, false, true>, d, d.B, cf, st, true)
+                 : launch_clusters(verify_finish_kernel<DT, false, false>, d, d.B, cf, st, true);
+  if (rc == FOPD_OK && defer) {
+    set_parts<DT>(&d, kRollMaxCluster);
+    rc = launch_clusters(verify_finish_kernel<DT, false, false>, d, list_clusters(d.B), kRollMaxCluster, st, true);
+  }
   if (cudaFreeAsync(tmp, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   return rc;
 }
@@ -137,7 +163,6 @@ int fopd_verify_draft(const fopd_draft *d, int32_t *tokens, float *logprob, uint
   r.mask = mask;
   r.n_accepted = n_accepted;
   r.status = status;
-  r.eps = sum_error(d->vocab);
   // a target without temperature never asks for the draft's probabilities: x is accepted if it is the best token
   const bool best = d->temperature == 0.f;
   r.kind = best || d->K == 0 ? kDraftNone : !d->draft ? kDraftCertain : d->draft_temperature == 0.f ? kDraftBest : kDraftRows;
@@ -145,6 +170,8 @@ int fopd_verify_draft(const fopd_draft *d, int32_t *tokens, float *logprob, uint
   r.cd64 = r.kind == kDraftRows ? 1.4426950408889634074 / (double)d->draft_temperature : 0.0;
   r.ct = (float)r.ct64;
   r.cd = (float)r.cd64;
+  if (!best) r.eps = sum_error(d->vocab, r.ct, r.ct64);
+  if (r.kind == kDraftRows) r.eps = std::fmax(r.eps, sum_error(d->vocab, r.cd, r.cd64));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool bf16 = d->dtype == FOPD_BF16;
   if (d->K == 0) return bf16 ? launch_draw<FOPD_BF16>(r, st) : launch_draw<FOPD_F32>(r, st);

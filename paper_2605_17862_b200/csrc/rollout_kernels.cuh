@@ -58,6 +58,7 @@ struct RolloutDev {
   double ct64, cd64;
   double eps;          // relative error of a row's fp32 sum (and of a weight)
   Position *pos;       // [B, K + 1]
+  int32_t *later;      // rows (sequences) to be done again: how many, then which; NULL: none are put off
   int32_t *stop;       // [B] the lowest position known not to be accepted, or NULL: nobody looks
   int32_t *tokens;
   float *logprob;
@@ -132,32 +133,43 @@ __device__ __forceinline__ void copy_part(uint4 *to, const char *row, int64_t pa
 
 // ---- 2^y in fp64 ------------------------------------------------------------------------------------
 
-// y rounded to sixteenths, 2^{j/16} from a table in shared memory (sixteen entries lie in sixteen banks) and six terms
-// of the Taylor series of 2^f, |f| <= 1/32: error below 1e-15.
+// For every element of a row that is decided in fp64: y rounded to sixteenths, 2^{j/16} from a table in shared memory
+// (sixteen entries lie in sixteen banks) and the Chebyshev fit of degree five to 2^f on |f| <= 1/32: error 5e-15.  The
+// high word of the table's entry j is less by j << 16, so that adding n << 16 for y = n / 16 makes it 2^{n/16}.
 __constant__ double kSixteenths[16] = {
     1.0, 1.0442737824274138, 1.0905077326652577, 1.1387886347566916, 1.189207115002721, 1.241857812073484,
     1.2968395546510096, 1.3542555469368927, 1.4142135623730951, 1.4768261459394993, 1.5422108254079407,
     1.6104903319492543, 1.681792830507429, 1.7562521603732995, 1.8340080864093424, 1.9152065613971474};
 __device__ __forceinline__ void fill_exp64(double *tab) {
-  if (threadIdx.x < 16) tab[threadIdx.x] = kSixteenths[threadIdx.x];
+  if (threadIdx.x < 16) {
+    const double x = kSixteenths[threadIdx.x];
+    tab[threadIdx.x] = __hiloint2double(__double2hiint(x) - ((int)threadIdx.x << 16), __double2loint(x));
+  }
 }
-
-// 2^{d c} with the product inside the fused multiply-adds; d c <= 0.  Below 2^-1000 whatever comes out is to be dropped.
-__device__ __forceinline__ double exp64_raw(double d, double c, const double *tab) {
+// A weight is the product of the two; x is the element, m its row's maximum.  The difference is cut off at about -1000 / c
+// (`least`: the high word of that; of two negative numbers the larger word is the lower one), where a weight is 2^-1000.
+struct Weight64 {
+  double p, scale;
+};
+__device__ __forceinline__ Weight64 weight64(float x, double m, double c, uint32_t least, const double *tab) {
   constexpr double kRound = 6755399441055744.0 / 16;  // 1.5 * 2^52 / 16: adding it rounds to sixteenths
+  const double e0 = (double)x - m;
+  const double d = __hiloint2double((int)min((uint32_t)__double2hiint(e0), least), __double2loint(e0));
   const double t = fma(d, c, kRound);
   const double f = fma(d, c, kRound - t);
   const int n = __double2loint(t);
-  double p = 1.540353039338161e-4;
-  p = fma(p, f, 1.3333558146428443e-3);
-  p = fma(p, f, 9.618129107628477e-3);
-  p = fma(p, f, 5.550410866482158e-2);
-  p = fma(p, f, 2.4022650695910072e-1);
-  p = fma(p, f, 6.931471805599453e-1);
-  p = fma(p, f, 1.0);
-  p *= tab[n & 15];
-  return __hiloint2double(__double2hiint(p) + ((n >> 4) << 20), __double2loint(p));
+  double p = 0.0013333781576784268;
+  p = fma(p, f, 0.009618354747407538);
+  p = fma(p, f, 0.0555041086566393);
+  p = fma(p, f, 0.24022650687646874);
+  p = fma(p, f, 0.6931471805599457);
+  p = fma(p, f, 1.0000000000000044);
+  const double e = tab[n & 15];
+  return {p, __hiloint2double(__double2hiint(e) + (n << 16), __double2loint(e))};
 }
+constexpr double kNothing = 1.2e-271;  // 2^-900 of the largest weight: less counts as nothing, any number of them together
+__device__ __forceinline__ uint32_t least_of(double c) { return (uint32_t)__double2hiint(-1000.0 / c); }
+
 // The same without a table, for a value here and there: y rounded to a whole number, eleven terms, |f| <= 1/2: 1e-14.
 __device__ __forceinline__ double exp64(double d, double c) {
   constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52
@@ -178,13 +190,6 @@ __device__ __forceinline__ double exp64(double d, double c) {
   p = __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
   return d * c >= -1000.0 ? p : 0.0;  // (not a number counts as nothing: the sum it belongs to tells)
 }
-// The same of an element x and a row's maximum; least: below it the result is nothing (-infinity has no fraction).
-__device__ __forceinline__ double weight64(float x, double m, double c, float least, const double *tab) {
-  const double p = exp64_raw((double)x - m, c, tab);
-  return x >= least ? p : 0.0;
-}
-__device__ __forceinline__ float least_of(float m, double c) { return (float)((double)m - 1000.0 / c); }
-
 // ---- sweeps -----------------------------------------------------------------------------------------
 
 // Two fp32 in one register pair: one instruction works on both.
@@ -263,7 +268,20 @@ __device__ __forceinline__ float max_vecs(const uint4 (&raw)[N]) {
 
 __device__ __forceinline__ RowSum nothing() { return {-INFINITY, INT32_MAX, 0.0}; }
 
-// Sums of a row, tile after tile: {max, sum 2^{(x - max) c}} with the maximum the warp's and the sum the lane's own.
+// Rows whose max c is beyond this: its rounding in fp32 is no longer small (or max is infinite: NaN).  Out of line:
+// hardly any row comes here.
+constexpr float kFar = 1 << 20;
+template <int DT>
+__device__ __noinline__ double far_sum(uint4 raw, float m, float c) {
+  double z = 0.0;
+  float x[Elem<DT>::kPerVec];
+  Elem<DT>::unpack(raw, x);
+#pragma unroll
+  for (int k = 0; k < Elem<DT>::kPerVec; ++k) z += (double)ex2((x[k] - m) * c);
+  return z;
+}
+
+// Sums of a row, part after part: {max, sum 2^{(x - max) c}} with the maximum the warp's and the sum the lane's own.
 // The exponent is x c - fl(max c) in one fused multiply-add; what fl() took away is the same for all elements and put
 // back at the end.  -infinity everywhere gives {-inf, 0}; a NaN or +inf makes the sum NaN.
 template <int DT>
@@ -278,7 +296,7 @@ __device__ __forceinline__ void add_part(RowSum &acc, const uint4 (&raw)[kLoadVe
   m = acc.m;
   const float mc = m == -INFINITY ? 0.f : m * c;
   double z;
-  if (fabsf(mc) <= 1e38f) {
+  if (fabsf(mc) <= kFar) {
     const f32x2 c2 = pair(c, c), mc2 = pair(-mc, -mc);
     f32x2 sums[kLoadVecs];
 #pragma unroll
@@ -290,17 +308,13 @@ __device__ __forceinline__ void add_part(RowSum &acc, const uint4 (&raw)[kLoadVe
       sums[v] = tree_sum2<P / 2>(x);
     }
     float s = both(tree_sum2<kLoadVecs>(sums));
-    if (m != -INFINITY) s *= ex2(-fmaf(m, c, -mc));
-    z = (double)s;
-  } else {  // max c is beyond fp32 (or max is infinite: NaN)
+    // (what fl() took away is tiny unless the logits are far from zero)
+    const float took = m == -INFINITY ? 0.f : fmaf(m, c, -mc);
+    z = fabsf(took) < 1.2e-4f ? (double)fmaf(-took * kLn2, s, s) : (double)s * exp64(-(double)took, 1.0);
+  } else {
     z = 0.0;
-#pragma unroll  // (a loop would put raw[] into local memory)
-    for (int v = 0; v < kLoadVecs; ++v) {
-      float x[P];
-      E::unpack(raw[v], x);
 #pragma unroll
-      for (int k = 0; k < P; ++k) z += (double)ex2((x[k] - m) * c);
-    }
+    for (int v = 0; v < kLoadVecs; ++v) z += far_sum<DT>(raw[v], m, c);
   }
   acc.z += z;
 }
@@ -409,55 +423,62 @@ __device__ __forceinline__ RowSum warp_merge_best(RowSum a) {
 }
 
 __device__ __forceinline__ bool is_distribution(const RowSum &r) {
-  return r.m > -INFINITY && r.m < INFINITY && r.z > 0.0 && r.z < INFINITY;
+  return r.m > -INFINITY && r.m < INFINITY && r.z > kNothing && r.z < INFINITY;
 }
 
 // ---- weights ----------------------------------------------------------------------------------------
 
-// Weights of the distribution a token is drawn from, a vector of elements at a time.
-enum WeightKind { kWPlain = 0, kWWithout = 1, kWRest = 2 };
+// Weights of the distribution a token is drawn from, a vector of elements at a time: e^{t} of the target's row, without
+// one element (`without` >= 0), or max(p - q, 0) (`rest`).
 template <int DT>
 struct Weights {
   static constexpr int P = Elem<DT>::kPerVec;
   const char *t, *q;  // rows
   int64_t V;
-  int kind;           // WeightKind
-  int32_t without;    // kWWithout: the element of which everything is taken away
+  bool rest;
+  int32_t without;
   RowSum ts, qs;
   float ct, cd;
   double ct64, cd64;
   const double *tab;
   // derived
   float mct, mcd, a, b;  // fl(max c); 2^{what fl() took} / sum
-  float least_t, least_q;
+  uint32_t least_t, least_q;
   double ia, ib;         // 1 / sum
 
   __device__ __forceinline__ void derive() {
     mct = ts.m * ct;
-    least_t = least_of(ts.m, ct64);
-    if (kind == kWRest) {
-      a = (float)((double)ex2(-fmaf(ts.m, ct, -mct)) / ts.z);
+    least_t = least_of(ct64);
+    if (rest) {
+      a = (float)(exp64(-(double)fmaf(ts.m, ct, -mct), 1.0) / ts.z);
       ia = 1.0 / ts.z;
       mcd = qs.m * cd;
-      b = (float)((double)ex2(-fmaf(qs.m, cd, -mcd)) / qs.z);
-      least_q = least_of(qs.m, cd64);
+      b = (float)(exp64(-(double)fmaf(qs.m, cd, -mcd), 1.0) / qs.z);
+      least_q = least_of(cd64);
       ib = 1.0 / qs.z;
     }
   }
-  // fp32's exponent cannot be formed (see add_tile)
-  __device__ __forceinline__ bool beyond() const {
-    return !(fabsf(mct) <= 1e38f) || (kind == kWRest && !(fabsf(mcd) <= 1e38f));
-  }
+  // fp32's exponent cannot be formed (see add_part)
+  __device__ __forceinline__ bool beyond() const { return !(fabsf(mct) <= kFar) || (rest && !(fabsf(mcd) <= kFar)); }
+
   __device__ __forceinline__ void load(int64_t i, uint4 &rt, uint4 &rq) const {
     rt = row_vec<DT>(t, i, V);
-    rq = kind == kWRest ? row_vec<DT>(q, i, V) : make_uint4(0, 0, 0, 0);
+    if (rest) rq = row_vec<DT>(q, i, V);
+    if (without >= 0 && without / P == i) {  // its logit becomes -infinity
+      float x[P];
+      Elem<DT>::unpack(rt, x);
+#pragma unroll
+      for (int k = 0; k < P; ++k) x[k] = k == without % P ? -INFINITY : x[k];
+      rt = Elem<DT>::pack(x);
+    }
   }
-  __device__ __forceinline__ void fast(int64_t i, const uint4 &rt, const uint4 &rq, f32x2 (&w)[P / 2]) const {
+  __device__ __forceinline__ double fast_sum(const uint4 &rt, const uint4 &rq) const {
+    f32x2 w[P / 2];
     const f32x2 c2 = pair(ct, ct), m2 = pair(-mct, -mct);
     unpack2<DT>(rt, w);
 #pragma unroll
     for (int k = 0; k < P / 2; ++k) w[k] = exp2_2(fma2(w[k], c2, m2));
-    if (kind == kWRest) {
+    if (rest) {
       const f32x2 d2 = pair(cd, cd), n2 = pair(-mcd, -mcd), a2 = pair(a, a), b2 = pair(-b, -b);
       f32x2 x[P / 2];
       unpack2<DT>(rq, x);
@@ -467,44 +488,40 @@ struct Weights {
         split(fma2(w[k], a2, mul2(exp2_2(fma2(x[k], d2, n2)), b2)), lo, hi);
         w[k] = pair(fmaxf(lo, 0.f), fmaxf(hi, 0.f));
       }
-    } else if (kind == kWWithout && without / P == i) {
-#pragma unroll
-      for (int k = 0; k < P / 2; ++k) {
-        float lo, hi;
-        split(w[k], lo, hi);
-        w[k] = pair(2 * k == without % P ? 0.f : lo, 2 * k + 1 == without % P ? 0.f : hi);
-      }
     }
-  }
-  __device__ __forceinline__ void exact(int64_t i, const uint4 &rt, const uint4 &rq, double (&w)[P]) const {
-    float x[P];
-    Elem<DT>::unpack(rt, x);
-#pragma unroll
-    for (int k = 0; k < P; ++k) w[k] = weight64(x[k], ts.m, ct64, least_t, tab);
-    if (kind == kWRest) {
-      Elem<DT>::unpack(rq, x);
-#pragma unroll
-      for (int k = 0; k < P; ++k)  // (both products rounded alike: equal rows leave exactly nothing)
-        w[k] = fmax(__dsub_rn(__dmul_rn(w[k], ia), __dmul_rn(weight64(x[k], qs.m, cd64, least_q, tab), ib)), 0.0);
-    } else if (kind == kWWithout) {
-#pragma unroll
-      for (int k = 0; k < P; ++k)
-        if (i * P + k == without) w[k] = 0.0;
-    }
-  }
-  // sum of a vector's weights, in fp64 from the vector up
-  template <bool kExact>
-  __device__ __forceinline__ double sum(int64_t i, const uint4 &rt, const uint4 &rq) const {
-    if (kExact) {
-      double w[P], s = 0.0;
-      exact(i, rt, rq, w);
-#pragma unroll
-      for (int k = 0; k < P; ++k) s += w[k];
-      return s;
-    }
-    f32x2 w[P / 2];
-    fast(i, rt, rq, w);
     return (double)both(tree_sum2<P / 2>(w));
+  }
+  // (both products are rounded alike: equal rows leave exactly nothing)
+  __device__ __forceinline__ double difference(const Weight64 &p, const Weight64 &r) const {
+    const double d = __dsub_rn(__dmul_rn(__dmul_rn(p.p, p.scale), ia), __dmul_rn(__dmul_rn(r.p, r.scale), ib));
+    const int keep = ~(__double2hiint(d) >> 31);
+    return __hiloint2double(__double2hiint(d) & keep, __double2loint(d) & keep);
+  }
+  template <bool kRest>
+  __device__ __forceinline__ double exact_sum(const uint4 &rt, const uint4 &rq) const {
+    float x[P], y[P];
+    Elem<DT>::unpack(rt, x);
+    if (kRest) Elem<DT>::unpack(rq, y);
+    double s = 0.0;
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+      const Weight64 p = weight64(x[k], ts.m, ct64, least_t, tab);
+      if (kRest) s += difference(p, weight64(y[k], qs.m, cd64, least_q, tab));
+      else s = fma(p.p, p.scale, s);
+    }
+    return s;
+  }
+  // one element in fp64, or in fp32
+  template <bool kExact>
+  __device__ __forceinline__ double element(int64_t i) const {
+    if (i >= V || i == without) return 0.0;
+    const float x = Elem<DT>::load1(t, i);
+    if (kExact) {
+      const Weight64 p = weight64(x, ts.m, ct64, least_t, tab);
+      return rest ? difference(p, weight64(Elem<DT>::load1(q, i), qs.m, cd64, least_q, tab)) : p.p * p.scale;
+    }
+    const float p = ex2(fmaf(x, ct, -mct));
+    return rest ? (double)fmaxf(fmaf(p, a, -b * ex2(fmaf(Elem<DT>::load1(q, i), cd, -mcd))), 0.f) : (double)p;
   }
 };
 
@@ -574,32 +591,18 @@ __device__ int32_t cta_find(const Weights<DT> &w, const RolloutDev &d, int64_t s
     const bool back = s == rounds;  // no round passes: the last weight it is
     const int64_t o = (back ? last : s) * kRollThreads + threadIdx.x, i = vec0 + o;
     if (back) before = last_before;
-    double x[P], sum = 0.0;
-    uint4 rt = make_uint4(0, 0, 0, 0), rq = rt;
-    if (o < vecs) w.load(i, rt, rq);
-    if (kExact) {
-      w.exact(i, rt, rq, x);
-    } else {
-      f32x2 y[P / 2];
-      w.fast(i, rt, rq, y);
-#pragma unroll
-      for (int k = 0; k < P / 2; ++k) {
-        float lo, hi;
-        split(y[k], lo, hi);
-        x[2 * k] = (double)lo;
-        x[2 * k + 1] = (double)hi;
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < P; ++k) {
-      if (o >= vecs) x[k] = 0.0;
-      sum += x[k];
+    double sum = 0.0;
+    if (o < vecs) {
+      uint4 rt, rq;
+      w.load(i, rt, rq);
+      if (!kExact) sum = w.fast_sum(rt, rq);
+      else sum = w.rest ? w.template exact_sum<true>(rt, rq) : w.template exact_sum<false>(rt, rq);
     }
     const double incl = before + cta_scan(sum, sh.scan);
-    const bool here = sum > 0.0 && (back || incl > goal);
+    const bool here = sum > kNothing && (back || incl > goal);
     if (threadIdx.x == 0) sh.thread = back ? -1 : kRollThreads;
     if (!__syncthreads_or(here)) {
-      if (__syncthreads_or(sum > 0.0)) {
+      if (__syncthreads_or(sum > kNothing)) {
         last = s;
         last_before = before;
       }
@@ -613,16 +616,17 @@ __device__ int32_t cta_find(const Weights<DT> &w, const RolloutDev &d, int64_t s
     if (sh.thread == (int)threadIdx.x) {
       double run = incl - sum, at_before = run, at_after = run;
       int at = -1;
-#pragma unroll
+#pragma unroll 1
       for (int k = 0; k < P; ++k) {
-        if (x[k] > 0.0 && (at < 0 || at_after <= goal)) {
+        const double x = w.template element<kExact>(i * P + k);
+        if (x > kNothing) {
           at = k;
           at_before = run;
-          at_after = run + x[k];
+          run = at_after = run + x;
+          if (run > goal) break;
         }
-        run += x[k];
       }
-      if (kExact || (goal - at_before > bound && at_after - goal > bound)) {
+      if (at >= 0 && (kExact || (goal - at_before > bound && at_after - goal > bound))) {
         sh.result = (int32_t)(i * P + at);
         sh.logit = Elem<DT>::load1(w.t, i * P + at);
       }
@@ -638,7 +642,7 @@ __device__ int32_t cta_find(const Weights<DT> &w, const RolloutDev &d, int64_t s
 // slots, then through one slot's elements.  Returns the token in the owner's threads and elsewhere kUnsure, the total
 // and whether the cluster is to do it again in fp64 in all threads.
 template <int DT, bool kExact, bool kRelative>
-__device__ int32_t cluster_search(cg::cluster_group &cl, Weights<DT> &w, const RolloutDev &d, Slots sl, double v,
+__device__ __forceinline__ int32_t cluster_search(cg::cluster_group &cl, Weights<DT> &w, const RolloutDev &d, Slots sl, double v,
                                   double bound_rel, double bound_abs, int parity, RollShared &sh, RowSum *total,
                                   bool *again) {
   const int rank = (int)cl.block_rank(), size = (int)cl.num_blocks();
@@ -672,8 +676,8 @@ __device__ int32_t cluster_search(cg::cluster_group &cl, Weights<DT> &w, const R
       const double part = part_of(mine, all.m, d.ct64), run = warp_scan(part);
       all.z = __shfl_sync(0xffffffffu, run, 31);
       goal = v * all.z;
-      const unsigned pass = __ballot_sync(0xffffffffu, part > 0.0 && run > goal),
-                     has = __ballot_sync(0xffffffffu, part > 0.0);
+      const unsigned pass = __ballot_sync(0xffffffffu, part > kNothing && run > goal),
+                     has = __ballot_sync(0xffffffffu, part > kNothing);
       owner = pass ? __ffs(pass) - 1 : has ? 31 - __clz(has) : 0;
       before = __shfl_sync(0xffffffffu, run - part, owner);
       scale = part_of({own.m, 0, 1.0}, all.m, d.ct64);
@@ -684,14 +688,14 @@ __device__ int32_t cluster_search(cg::cluster_group &cl, Weights<DT> &w, const R
       sh.goal = goal;
     }
     if (owner == rank && is_distribution(all)) {  // the first run that passes, or the last one with a weight
-      const unsigned pass = __ballot_sync(0xffffffffu, s > 0.0 && before + scale * incl > goal),
-                     has = __ballot_sync(0xffffffffu, s > 0.0);
+      const unsigned pass = __ballot_sync(0xffffffffu, s * scale > kNothing && before + scale * incl > goal),
+                     has = __ballot_sync(0xffffffffu, s * scale > kNothing);
       if (lane == (pass ? __ffs(pass) - 1 : 31 - __clz(has))) {
         double run = before + scale * (incl - s), at = run;
         int slot = lo;
         for (int t = lo; t < hi; ++t) {
           const double x = sh.tz[t] * scale;
-          if (x > 0.0) {
+          if (x > kNothing) {
             slot = t;
             at = run;
             if (run + x > goal) break;
@@ -729,20 +733,44 @@ __device__ int32_t cluster_search(cg::cluster_group &cl, Weights<DT> &w, const R
   return token;
 }
 
-// Slot sums of the weights in fp32 or fp64, relative to one reference.
-template <int DT, bool kExact>
-__device__ __forceinline__ void cta_slot_sums(const Weights<DT> &w, const RolloutDev &d, Slots sl, RollShared &sh) {
+// Slot sums of the weights in fp32, relative to one reference.
+template <int DT>
+__device__ __forceinline__ void cta_fast_sums(const Weights<DT> &w, const RolloutDev &d, Slots sl, RollShared &sh) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   for (int64_t t = sl.lo + warp; t < sl.hi; t += kRollWarps) {
     double s = 0.0;
     const int64_t end = min((t + 1) * d.span, d.n_parts) * kPartVecs;
-    constexpr int kU = 2;
+    constexpr int kU = 4;
+    static_assert(kPartVecs % (32 * kU) == 0, "whole rounds");
     for (int64_t i = t * d.span * kPartVecs + lane; i < end; i += 32 * kU) {
       uint4 rt[kU], rq[kU];
 #pragma unroll
       for (int u = 0; u < kU; ++u) w.load(i + 32 * u, rt[u], rq[u]);
 #pragma unroll
-      for (int u = 0; u < kU; ++u) s += w.template sum<kExact>(i + 32 * u, rt[u], rq[u]);
+      for (int u = 0; u < kU; ++u) s += w.fast_sum(rt[u], rq[u]);
+    }
+    s = warp_sum(s);
+    if (lane == 0) sh.tz[t - sl.lo] = s;
+  }
+  __syncthreads();
+}
+// The same in fp64; the next vector is on its way while one is worked on.
+template <int DT, bool kRest>
+__device__ __forceinline__ void cta_exact_sums(const Weights<DT> &w, const RolloutDev &d, Slots sl, RollShared &sh) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll 1
+  for (int64_t t = sl.lo + warp; t < sl.hi; t += kRollWarps) {
+    double s = 0.0;
+    const int64_t end = min((t + 1) * d.span, d.n_parts) * kPartVecs;
+    int64_t i = t * d.span * kPartVecs + lane;
+    uint4 rt, rq, nt, nq;
+    w.load(i, nt, nq);
+#pragma unroll 1
+    for (; i < end; i += 32) {
+      rt = nt;
+      rq = nq;
+      if (i + 32 < end) w.load(i + 32, nt, nq);
+      s += w.template exact_sum<kRest>(rt, rq);
     }
     s = warp_sum(s);
     if (lane == 0) sh.tz[t - sl.lo] = s;
@@ -752,17 +780,17 @@ __device__ __forceinline__ void cta_slot_sums(const Weights<DT> &w, const Rollou
 
 // A row's sum of exponentials in fp64, over the cluster, in every thread.  parity alternates from call to call.
 template <int DT>
-__device__ double cluster_exact_sum(cg::cluster_group &cl, const char *row, float m, double c, const RolloutDev &d,
+__device__ __noinline__ double cluster_exact_sum(cg::cluster_group &cl, const char *row, float m, double c, const RolloutDev &d,
                                     Slots sl, int &parity, RollShared &sh) {
   Weights<DT> w = {};
   w.t = row;
   w.V = d.vocab;
-  w.kind = kWPlain;
+  w.without = -1;
   w.ts = {m, 0, 1.0};
   w.ct64 = c;
-  w.least_t = least_of(m, c);
+  w.least_t = least_of(c);
   w.tab = sh.tab;
-  cta_slot_sums<DT, true>(w, d, sl, sh);
+  cta_exact_sums<DT, false>(w, d, sl, sh);
   const int size = (int)cl.num_blocks();
   if (threadIdx.x < 32) {
     double s = 0.0;
@@ -784,83 +812,101 @@ __device__ __forceinline__ float log_prob(float logit, const RowSum &r, double c
 
 // ---- draws: a cluster per row -----------------------------------------------------------------------
 
-template <int DT, bool kBest>
-__global__ void __launch_bounds__(kRollThreads, 4) draw_kernel(const __grid_constant__ RolloutDev d) {
+// kDefer: one CTA a row; a row that fp32 does not decide is put on a list.  Otherwise the cluster decides it at once,
+// the rows of the grid or, with d.later, those of the list.  (Eight CTAs take an eighth of the time for a row in fp64:
+// put off, the few rows that need it do not hold up the end of a long grid.)
+template <int DT, bool kBest, bool kDefer>
+__global__ void __launch_bounds__(kRollThreads, kDefer ? 4 : 2) draw_kernel(const __grid_constant__ RolloutDev d) {
   __shared__ RollShared sh;
   cg::cluster_group cl = cg::this_cluster();
   const int rank = (int)cl.block_rank(), size = (int)cl.num_blocks();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t n = blockIdx.x / size;
-  const char *row = d.target + n * d.tseq;
   const Slots sl = my_slots(d, rank, size);
-  const double v = kBest ? 0.0 : d.uniform[n];
-  RowSum acc = nothing();
-  sweep<DT, kBest>(acc, row, d.vocab, sl.lo + warp, sl.hi, kRollWarps, d.span, d.ct, d.ct64, sh.ring[warp],
-                   [&](int64_t slot, RowSum &r) {
-                     if (kBest) return;
-                     r.z = warp_sum(r.z);
-                     if (lane == 0) {
-                       sh.tm[slot - sl.lo] = r.m;
-                       sh.tz[slot - sl.lo] = r.z;
-                     }
-                     r = nothing();
-                   });
-  int32_t token = kUnsure;
-  float lp = 0.f;
-  bool good;
-  int bits = FOPD_DEV_BAD_LOGITS;
-  if (kBest) {
-    if (lane == 0) sh.part[0][warp] = acc;
+  asm volatile("griddepcontrol.launch_dependents;");
+  if (!kBest && !kDefer) {
+    fill_exp64(sh.tab);
     __syncthreads();
-    if (warp == 0) {
-      const RowSum r = warp_merge_best(lane < kRollWarps ? sh.part[0][lane] : nothing());
-      if (lane < size) *cl.map_shared_rank(&sh.pub[0][rank], lane) = r;
-    }
-    roll_sync(cl);
-    RowSum r = nothing();
-    if (warp == 0) r = warp_merge_best(lane < size ? sh.pub[0][lane] : nothing());
-    good = r.m > -INFINITY && r.m < INFINITY;  // (warp 0)
-    if (rank == 0 && good) token = r.best;
-  } else {
-    __syncthreads();
-    const bool v_ok = v >= 0.0 && v < 1.0;
-    Weights<DT> w = {};
-    w.t = row;
-    w.V = d.vocab;
-    w.kind = kWPlain;
-    w.without = -1;
-    w.ct = d.ct;
-    w.ct64 = d.ct64;
-    w.tab = sh.tab;
-    RowSum total;
-    bool again;
-    token = cluster_search<DT, false, true>(cl, w, d, sl, v_ok ? v : 0.0, 2 * d.eps, 0.0, 0, sh, &total, &again);
-    good = is_distribution(total) && v_ok;
-    if (is_distribution(total)) bits = FOPD_DEV_BAD_UNIFORM;
-    if (again && good) {
-      fill_exp64(sh.tab);
+  }
+  const bool listed = !kDefer && d.later;
+  if (listed) asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int32_t count = listed ? d.later[0] : d.B;
+  int parity = 0;
+  for (int32_t k = blockIdx.x / size; k < count; k += gridDim.x / size) {
+    const int64_t n = listed ? d.later[1 + k] : k;
+    const char *row = d.target + n * d.tseq;
+    const double v = kBest ? 0.0 : d.uniform[n];
+    RowSum acc = nothing();
+    sweep<DT, kBest>(acc, row, d.vocab, sl.lo + warp, sl.hi, kRollWarps, d.span, d.ct, d.ct64, sh.ring[warp],
+                     [&](int64_t slot, RowSum &r) {
+                       if (kBest) return;
+                       r.z = warp_sum(r.z);
+                       if (lane == 0) {
+                         sh.tm[slot - sl.lo] = r.m;
+                         sh.tz[slot - sl.lo] = r.z;
+                       }
+                       r = nothing();
+                     });
+    int32_t token = kUnsure;
+    float lp = 0.f;
+    bool good;
+    int bits = FOPD_DEV_BAD_LOGITS;
+    if (kBest) {
+      if (lane == 0) sh.part[0][warp] = acc;
       __syncthreads();
-      w.ts = total;
-      w.derive();
-      cta_slot_sums<DT, true>(w, d, sl, sh);
-      RowSum exact_total;
-      bool never;
-      token = cluster_search<DT, true, false>(cl, w, d, sl, v, 0.0, 0.0, 1, sh, &exact_total, &never);
+      if (warp == 0) {
+        const RowSum r = warp_merge_best(lane < kRollWarps ? sh.part[0][lane] : nothing());
+        if (lane < size) *cl.map_shared_rank(&sh.pub[0][rank], lane) = r;
+      }
+      roll_sync(cl);
+      RowSum r = nothing();
+      if (warp == 0) r = warp_merge_best(lane < size ? sh.pub[0][lane] : nothing());
+      good = r.m > -INFINITY && r.m < INFINITY;  // (warp 0)
+      if (rank == 0 && good) token = r.best;
+    } else {
+      __syncthreads();
+      const bool v_ok = v >= 0.0 && v < 1.0;
+      Weights<DT> w = {};
+      w.t = row;
+      w.V = d.vocab;
+      w.without = -1;
+      w.ct = d.ct;
+      w.ct64 = d.ct64;
+      w.tab = sh.tab;
+      RowSum total;
+      bool again;
+      token = cluster_search<DT, false, true>(cl, w, d, sl, v_ok ? v : 0.0, 2 * d.eps, 0.0, parity, sh, &total, &again);
+      parity ^= 1;
+      good = is_distribution(total) && v_ok;
+      if (is_distribution(total)) bits = FOPD_DEV_BAD_UNIFORM;
+      if (again && good) {
+        if (kDefer) {
+          if (rank == 0 && threadIdx.x == 0) d.later[1 + atomicAdd(d.later, 1)] = (int32_t)n;
+          continue;
+        }
+        w.ts = total;
+        w.derive();
+        cta_exact_sums<DT, false>(w, d, sl, sh);
+        RowSum exact_total;
+        bool never;
+        token = cluster_search<DT, true, false>(cl, w, d, sl, v, 0.0, 0.0, parity, sh, &exact_total, &never);
+        parity ^= 1;
+      }
+      if (good && token >= 0 && threadIdx.x == 0) lp = log_prob(sh.logit, total, d.ct64);
     }
-    if (good && token >= 0 && threadIdx.x == 0) lp = log_prob(sh.logit, total, d.ct64);
-  }
-  if (threadIdx.x == 0 && good && token >= 0) {
-    d.tokens[n] = token;
-    if (d.logprob) d.logprob[n] = lp;
-  }
-  if (threadIdx.x == 0 && rank == 0) {
-    if (!good) {
-      d.tokens[n] = -1;
-      if (d.logprob) d.logprob[n] = 0.f;
-      if (d.status) atomicOr(d.status, bits);
+    if (threadIdx.x == 0 && good && token >= 0) {
+      d.tokens[n] = token;
+      if (d.logprob) d.logprob[n] = lp;
     }
-    if (d.mask) d.mask[n] = good ? 1 : 0;
-    if (d.n_accepted) d.n_accepted[n] = 0;
+    if (threadIdx.x == 0 && rank == 0) {
+      if (!good) {
+        d.tokens[n] = -1;
+        if (d.logprob) d.logprob[n] = 0.f;
+        if (d.status) atomicOr(d.status, bits);
+      }
+      if (d.mask) d.mask[n] = good ? 1 : 0;
+      if (d.n_accepted) d.n_accepted[n] = 0;
+    }
+    if (k + (int32_t)(gridDim.x / size) < count) roll_sync(cl);  // the next row writes what this one has read
   }
 }
 
@@ -966,21 +1012,15 @@ __global__ void __launch_bounds__(kRollThreads, 4) verify_sweep_kernel(const __g
   }
 }
 
-// A cluster per sequence: the first position that is not accepted (an open one is settled in fp64), the new token,
-// the outputs.
-template <int DT, bool kBest>
-__global__ void __launch_bounds__(kRollThreads, 2) verify_finish_kernel(const __grid_constant__ RolloutDev d) {
+// One sequence of the finish, by a cluster.
+template <int DT, bool kBest, bool kDefer>
+__device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const RolloutDev &d, int32_t b, RollShared &sh) {
   using E = Elem<DT>;
-  __shared__ RollShared sh;
-  cg::cluster_group cl = cg::this_cluster();
   const int rank = (int)cl.block_rank(), size = (int)cl.num_blocks();
-  const int32_t b = blockIdx.x / size;
   const int32_t n = drafts_of(d, b), W = d.K + 1;
   int bits = d.n_draft && d.n_draft[b] != n ? FOPD_DEV_BAD_LENGTH : 0;
   const Position *pos = d.pos + (int64_t)b * W;
   const Slots sl = my_slots(d, rank, size);
-  fill_exp64(sh.tab);
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // the sweep's positions are there
   const int32_t limit = d.stop && d.stop[b] < n ? d.stop[b] : n;  // positions behind it may have been left out
 
   int32_t j = 0;
@@ -998,6 +1038,10 @@ __global__ void __launch_bounds__(kRollThreads, 2) verify_finish_kernel(const __
     __syncthreads();
     state = pos[j].state;
     if (kBest || state != kOpen) break;
+    if (kDefer) {
+      if (rank == 0 && threadIdx.x == 0) d.later[1 + atomicAdd(d.later, 1)] = b;
+      return;
+    }
     const int32_t x = d.drafted[(int64_t)b * d.K + j];
     const char *trow = d.target + b * d.tseq + j * d.trow, *qrow = d.draft + b * d.dseq + j * d.drow;
     const double p = exp64((double)E::load1(trow, x) - pos[j].t.m, d.ct64) /
@@ -1035,7 +1079,7 @@ __global__ void __launch_bounds__(kRollThreads, 2) verify_finish_kernel(const __
     w.t = d.target + b * d.tseq + j * d.trow;
     w.q = d.draft + b * d.dseq + j * d.drow;
     w.V = d.vocab;
-    w.kind = j == n ? kWPlain : d.kind == kDraftRows ? kWRest : kWWithout;
+    w.rest = j < n && d.kind == kDraftRows;
     w.without = j == n ? -1 : d.kind == kDraftBest ? q32.best : d.kind == kDraftCertain ? d.drafted[(int64_t)b * d.K + j] : -1;
     w.ct = d.ct;
     w.cd = d.cd;
@@ -1049,23 +1093,30 @@ __global__ void __launch_bounds__(kRollThreads, 2) verify_finish_kernel(const __
       w.qs = q32;
       w.derive();
       if (!w.beyond()) {
-        cta_slot_sums<DT, false>(w, d, sl, sh);
+        cta_fast_sums<DT>(w, d, sl, sh);
         // p - q: both rows' weights and both their sums are off; else the row's whole sum counts, with what was taken away
-        token = cluster_search<DT, false, false>(cl, w, d, sl, v, 0.0, w.kind == kWRest ? 8 * d.eps : 2 * d.eps * t32.z,
-                                                 0, sh, &total, &again);
+        token = cluster_search<DT, false, false>(cl, w, d, sl, v, 0.0, w.rest ? 9 * d.eps : 2 * d.eps * t32.z, 0, sh,
+                                                 &total, &again);
         if (!is_distribution(total)) again = true;
       }
       if (!again) break;
-      if (w.kind == kWRest) {
+      if (kDefer) {
+        if (rank == 0 && threadIdx.x == 0) d.later[1 + atomicAdd(d.later, 1)] = b;
+        return;
+      }
+      if (w.rest) {
         w.ts.z = cluster_exact_sum<DT>(cl, w.t, w.ts.m, d.ct64, d, sl, parity, sh);
         w.qs.z = cluster_exact_sum<DT>(cl, w.q, w.qs.m, d.cd64, d, sl, parity, sh);
         w.derive();
+        cta_exact_sums<DT, true>(w, d, sl, sh);
+      } else {
+        cta_exact_sums<DT, false>(w, d, sl, sh);
       }
-      cta_slot_sums<DT, true>(w, d, sl, sh);
       bool never;
       token = cluster_search<DT, true, false>(cl, w, d, sl, v, 0.0, 0.0, 1, sh, &total, &never);
       if (is_distribution(total)) break;
-      w.kind = kWPlain;
+      w.rest = false;
+      w.without = -1;
     }
     if (token >= 0 && threadIdx.x == 0) lp = log_prob(sh.logit, t32, d.ct64);
   }
@@ -1084,6 +1135,24 @@ __global__ void __launch_bounds__(kRollThreads, 2) verify_finish_kernel(const __
       if (d.logprob) d.logprob[at + k] = k < j ? pos[k].lp : 0.f;
       if (d.mask) d.mask[at + k] = k < j ? 1 : 0;
     }
+  }
+}
+
+// A cluster per sequence: the first position that is not accepted (an open one is settled in fp64), the new token,
+// the outputs.  kDefer and d.later as for draws.
+template <int DT, bool kBest, bool kDefer>
+__global__ void __launch_bounds__(kRollThreads, kDefer ? 3 : 2) verify_finish_kernel(const __grid_constant__ RolloutDev d) {
+  __shared__ RollShared sh;
+  cg::cluster_group cl = cg::this_cluster();
+  if (!kBest && !kDefer) fill_exp64(sh.tab);
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // the sweep's positions are there, or the list
+  const int size = (int)cl.num_blocks();
+  const bool listed = !kDefer && d.later;
+  const int32_t count = listed ? d.later[0] : d.B;
+  for (int32_t k = blockIdx.x / size; k < count; k += gridDim.x / size) {
+    finish_sequence<DT, kBest, kDefer>(cl, d, listed ? d.later[1 + k] : k, sh);
+    if (k + (int32_t)(gridDim.x / size) < count) roll_sync(cl);  // the next one writes what this one has read
   }
 }
 
