@@ -8,10 +8,10 @@ namespace {
 
 bool temperature_ok(float t) { return t == 0.f || (t >= 1.f / 1024 && t <= 1024.f); }
 
-// CTAs that share a row, a position or a sequence: as many as keep `units` clusters of them resident at once.
-int cluster_for(int64_t units) {
+// CTAs that share a row, a position or a sequence: as many as keep `units` clusters of them within `most` CTAs.
+int cluster_for(int64_t units, int most) {
   int c = kRollMaxCluster;
-  while (c > 1 && units * c > kRollResident) c /= 2;
+  while (c > 1 && units * c > most) c /= 2;
   return c;
 }
 
@@ -57,26 +57,27 @@ double sum_error(int64_t vocab, float c, double c64) {
   return 0.6932 * (5.97e-8 + std::fabs((double)c - c64) / c64) * y + 6.2e-7;
 }
 
-// Rows (or sequences) that fewer than kRollMaxCluster CTAs share are put on a list when fp32 does not decide them, and a
-// second launch goes through the list with clusters of that size.
-size_t later_bytes(int64_t units) { return ((size_t)units + 1) * sizeof(int32_t); }
+size_t later_bytes(int64_t units) { return sizeof(Later) + (size_t)units * sizeof(LaterEntry); }
 int64_t list_clusters(int64_t units) {
-  const int64_t most = kRollResident / kRollMaxCluster;
+  const int64_t most = kRollWhole / kRollMaxCluster;
   return units < most ? units : most;
 }
+// Two launches (Mode) for more rows or sequences than clusters of eight of the whole kernel fit at once.
+bool two_launches(int64_t units) { return units * kRollMaxCluster > kRollWhole; }
 
 template <int DT>
 int launch_draw(RolloutDev d, cudaStream_t st) {
-  const int c = cluster_for(d.B);
+  const int c = cluster_for(d.B, kRollResident);
   set_parts<DT>(&d, c);
-  if (d.ct64 == 0.0) return launch_clusters(draw_kernel<DT, true, true>, d, d.B, c, st);
-  if (c == kRollMaxCluster) return launch_clusters(draw_kernel<DT, false, false>, d, d.B, c, st);
+  if (d.ct64 == 0.0) return launch_clusters(draw_kernel<DT, true, kFirst>, d, d.B, c, st);
+  if (!two_launches(d.B)) return launch_clusters(draw_kernel<DT, false, kWhole>, d, d.B, c, st);
   int rc = scratch_alloc(reinterpret_cast<void **>(&d.later), later_bytes(d.B), st);
   if (rc != FOPD_OK) return rc;
   if (cudaMemsetAsync(d.later, 0, sizeof(int32_t), st) != cudaSuccess) rc = FOPD_ERR_CUDA;
-  if (rc == FOPD_OK) rc = launch_clusters(draw_kernel<DT, false, true>, d, d.B, c, st);
+  if (rc == FOPD_OK) rc = launch_clusters(draw_kernel<DT, false, kFirst>, d, d.B, c, st);
   set_parts<DT>(&d, kRollMaxCluster);
-  if (rc == FOPD_OK) rc = launch_clusters(draw_kernel<DT, false, false>, d, list_clusters(d.B), kRollMaxCluster, st, true);
+  if (rc == FOPD_OK)
+    rc = launch_clusters(draw_kernel<DT, false, kSecond>, d, list_clusters(d.B), kRollMaxCluster, st, true);
   if (cudaFreeAsync(d.later, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   return rc;
 }
@@ -85,21 +86,22 @@ template <int DT>
 int launch_verify(RolloutDev d, cudaStream_t st) {
   const bool best = d.ct64 == 0.0;
   const int64_t positions = (int64_t)d.B * (d.K + 1);
-  const int c = cluster_for(positions), cf = best ? 1 : cluster_for(d.B);
-  const bool look = positions > kRollResident;  // later positions start when earlier ones have been decided
-  const bool defer = !best && cf < kRollMaxCluster;
+  // (a position's two rows on one CTA each leave the SMs with unequal shares unless there are many more of them)
+  const int c = cluster_for(positions, 4 * kRollResident), cf = best ? 1 : cluster_for(d.B, kRollResident);
+  const bool look = positions * c > kRollResident;  // later positions start when earlier ones have been decided
+  const bool two = !best && two_launches(d.B);
   const size_t pos_bytes = ((size_t)positions * sizeof(Position) + 255) & ~size_t(255);
-  const size_t stop_bytes = look ? (size_t)d.B * sizeof(int32_t) : 0;
+  const size_t stop_bytes = look ? ((size_t)d.B * sizeof(int32_t) + 255) & ~size_t(255) : 0;
   char *tmp = nullptr;
-  int rc = scratch_alloc(reinterpret_cast<void **>(&tmp), pos_bytes + stop_bytes + (defer ? later_bytes(d.B) : 0), st);
+  int rc = scratch_alloc(reinterpret_cast<void **>(&tmp), pos_bytes + stop_bytes + (two ? later_bytes(d.B) : 0), st);
   if (rc != FOPD_OK) return rc;
   d.pos = reinterpret_cast<Position *>(tmp);
   if (look) {
     d.stop = reinterpret_cast<int32_t *>(tmp + pos_bytes);
     if (cudaMemsetAsync(d.stop, 0x7f, stop_bytes, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   }
-  if (defer) {
-    d.later = reinterpret_cast<int32_t *>(tmp + pos_bytes + stop_bytes);
+  if (two) {
+    d.later = reinterpret_cast<Later *>(tmp + pos_bytes + stop_bytes);
     if (cudaMemsetAsync(d.later, 0, sizeof(int32_t), st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   }
   set_parts<DT>(&d, c);
@@ -108,12 +110,12 @@ int launch_verify(RolloutDev d, cudaStream_t st) {
               : launch_clusters(verify_sweep_kernel<DT, false>, d, positions, c, st);
   set_parts<DT>(&d, cf);
   if (rc == FOPD_OK)
-    rc = best    ? launch_clusters(verify_finish_kernel<DT, true, true>, d, d.B, cf, st, true)
-         : defer ? launch_clusters(verify_finish_kernel<DT, false, true>, d, d.B, cf, st, true)
-                 : launch_clusters(verify_finish_kernel<DT, false, false>, d, d.B, cf, st, true);
-  if (rc == FOPD_OK && defer) {
+    rc = best  ? launch_clusters(verify_finish_kernel<DT, true, kFirst>, d, d.B, cf, st, true)
+         : two ? launch_clusters(verify_finish_kernel<DT, false, kFirst>, d, d.B, cf, st, true)
+               : launch_clusters(verify_finish_kernel<DT, false, kWhole>, d, d.B, cf, st, true);
+  if (rc == FOPD_OK && two) {
     set_parts<DT>(&d, kRollMaxCluster);
-    rc = launch_clusters(verify_finish_kernel<DT, false, false>, d, list_clusters(d.B), kRollMaxCluster, st, true);
+    rc = launch_clusters(verify_finish_kernel<DT, false, kSecond>, d, list_clusters(d.B), kRollMaxCluster, st, true);
   }
   if (cudaFreeAsync(tmp, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   return rc;

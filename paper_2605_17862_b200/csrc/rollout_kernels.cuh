@@ -27,7 +27,8 @@ constexpr int kPartVecs = 32 * kLoadVecs;
 constexpr int kStages = 2;          // parts of a warp on their way to shared memory
 constexpr int kSlots = 256;         // slots per CTA
 constexpr int kRollMaxCluster = 8;
-constexpr int kRollResident = 592;  // CTAs of these kernels that 148 SMs hold at once (64 registers)
+constexpr int kRollResident = 592;  // CTAs of these kernels that 148 SMs hold at once (64 registers),
+constexpr int kRollWhole = 296;     // and of those with the fp64 part in them (128 registers)
 
 enum DraftKind { kDraftNone = 0, kDraftCertain = 1, kDraftRows = 2, kDraftBest = 3 };
 enum PosState { kAccept = 0, kReject = 1, kOpen = 2, kBadRow = 3, kBadUniform = 4, kEnd = 5, kBadToken = 6 };
@@ -45,6 +46,20 @@ struct Position {
   int32_t state;
 };
 
+// Rows (sequences) to be decided in fp64 by a later launch.
+struct LaterEntry {
+  int32_t unit;
+  float m;   // the row's sum (draws)
+  double z;
+};
+struct Later {
+  int32_t count, pad[3];
+  LaterEntry e[1];  // as many as there are rows
+};
+// What a launch of a draw or of a finish does: everything; the fp32 part, putting off what it does not decide; the fp64
+// part of what was put off.
+enum Mode { kWhole = 0, kFirst = 1, kSecond = 2 };
+
 struct RolloutDev {
   const char *target, *draft;
   const int32_t *drafted, *n_draft;
@@ -58,7 +73,7 @@ struct RolloutDev {
   double ct64, cd64;
   double eps;          // relative error of a row's fp32 sum (and of a weight)
   Position *pos;       // [B, K + 1]
-  int32_t *later;      // rows (sequences) to be done again: how many, then which; NULL: none are put off
+  Later *later;        // kFirst, kSecond
   int32_t *stop;       // [B] the lowest position known not to be accepted, or NULL: nobody looks
   int32_t *tokens;
   float *logprob;
@@ -114,22 +129,24 @@ __device__ __forceinline__ uint4 row_vec(const char *row, int64_t i, int64_t V) 
   return E::pack(x);
 }
 
-// Copies a lane's vectors of one part of a row to where the same lane will read them; one group of asynchronous copies.
-template <int DT>
-__device__ __forceinline__ void copy_part(uint4 *to, const char *row, int64_t part, int64_t V) {
+// Asynchronous copies of n times 32 vectors of a row, from vector i0 on, to where the lane that asks for them will read
+// them.
+template <int DT, int N>
+__device__ __forceinline__ void copy_vecs(uint4 *to, const char *row, int64_t i0, int64_t V) {
   const int lane = threadIdx.x & 31;
-  const int64_t i0 = part * kPartVecs + lane;
-  if ((part + 1) * kPartElems<DT> <= V) {
-    const uint4 *p = reinterpret_cast<const uint4 *>(row) + i0;
+  if ((i0 + 32 * N) * Elem<DT>::kPerVec <= V) {
+    const uint4 *p = reinterpret_cast<const uint4 *>(row) + i0 + lane;
     const uint32_t at = (uint32_t)__cvta_generic_to_shared(to + lane);
 #pragma unroll
-    for (int v = 0; v < kLoadVecs; ++v)
+    for (int v = 0; v < N; ++v)
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + v * 512), "l"(p + v * 32) : "memory");
   } else {
 #pragma unroll
-    for (int v = 0; v < kLoadVecs; ++v) to[v * 32 + lane] = row_vec<DT>(row, i0 + v * 32, V);
+    for (int v = 0; v < N; ++v) to[v * 32 + lane] = row_vec<DT>(row, i0 + v * 32 + lane, V);
   }
 }
+__device__ __forceinline__ void copies_asked() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void oldest_copy() { asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory"); }
 
 // ---- 2^y in fp64 ------------------------------------------------------------------------------------
 
@@ -371,8 +388,8 @@ __device__ __forceinline__ void sweep(RowSum &acc, const char *row, int64_t V, i
   int ahead_p = 0;
 #pragma unroll
   for (int k = 0; k < kStages; ++k) {
-    if (ahead < end) copy_part<DT>(ring + k * kPartVecs, row, ahead * parts + ahead_p, V);
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (ahead < end) copy_vecs<DT, kLoadVecs>(ring + k * kPartVecs, row, (ahead * parts + ahead_p) * kPartVecs, V);
+    copies_asked();
     if (++ahead_p == parts) {
       ahead_p = 0;
       ahead += step;
@@ -382,12 +399,12 @@ __device__ __forceinline__ void sweep(RowSum &acc, const char *row, int64_t V, i
   for (int64_t slot = first; slot < end; slot += step) {
 #pragma unroll 1
     for (int p = 0; p < parts; ++p) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+      oldest_copy();
       uint4 raw[kLoadVecs];
 #pragma unroll
       for (int v = 0; v < kLoadVecs; ++v) raw[v] = stage[v * 32 + lane];
-      if (ahead < end) copy_part<DT>(stage, row, ahead * parts + ahead_p, V);
-      asm volatile("cp.async.commit_group;" ::: "memory");
+      if (ahead < end) copy_vecs<DT, kLoadVecs>(stage, row, (ahead * parts + ahead_p) * kPartVecs, V);
+      copies_asked();
       if (++ahead_p == parts) {
         ahead_p = 0;
         ahead += step;
@@ -461,10 +478,8 @@ struct Weights {
   // fp32's exponent cannot be formed (see add_part)
   __device__ __forceinline__ bool beyond() const { return !(fabsf(mct) <= kFar) || (rest && !(fabsf(mcd) <= kFar)); }
 
-  __device__ __forceinline__ void load(int64_t i, uint4 &rt, uint4 &rq) const {
-    rt = row_vec<DT>(t, i, V);
-    if (rest) rq = row_vec<DT>(q, i, V);
-    if (without >= 0 && without / P == i) {  // its logit becomes -infinity
+  __device__ __forceinline__ void take_away(int64_t i, uint4 &rt) const {  // a logit becomes -infinity
+    if (without >= 0 && without / P == i) {
       float x[P];
       Elem<DT>::unpack(rt, x);
 #pragma unroll
@@ -472,13 +487,14 @@ struct Weights {
       rt = Elem<DT>::pack(x);
     }
   }
+  template <bool kRest>
   __device__ __forceinline__ double fast_sum(const uint4 &rt, const uint4 &rq) const {
     f32x2 w[P / 2];
     const f32x2 c2 = pair(ct, ct), m2 = pair(-mct, -mct);
     unpack2<DT>(rt, w);
 #pragma unroll
     for (int k = 0; k < P / 2; ++k) w[k] = exp2_2(fma2(w[k], c2, m2));
-    if (rest) {
+    if (kRest) {
       const f32x2 d2 = pair(cd, cd), n2 = pair(-mcd, -mcd), a2 = pair(a, a), b2 = pair(-b, -b);
       f32x2 x[P / 2];
       unpack2<DT>(rq, x);
@@ -510,6 +526,10 @@ struct Weights {
       else s = fma(p.p, p.scale, s);
     }
     return s;
+  }
+  template <bool kExact, bool kRest>
+  __device__ __forceinline__ double sum(const uint4 &rt, const uint4 &rq) const {
+    return kExact ? exact_sum<kRest>(rt, rq) : fast_sum<kRest>(rt, rq);
   }
   // one element in fp64, or in fp32
   template <bool kExact>
@@ -593,10 +613,14 @@ __device__ int32_t cta_find(const Weights<DT> &w, const RolloutDev &d, int64_t s
     if (back) before = last_before;
     double sum = 0.0;
     if (o < vecs) {
-      uint4 rt, rq;
-      w.load(i, rt, rq);
-      if (!kExact) sum = w.fast_sum(rt, rq);
-      else sum = w.rest ? w.template exact_sum<true>(rt, rq) : w.template exact_sum<false>(rt, rq);
+      uint4 rt = row_vec<DT>(w.t, i, d.vocab), rq;
+      w.take_away(i, rt);
+      if (w.rest) {
+        rq = row_vec<DT>(w.q, i, d.vocab);
+        sum = w.template sum<kExact, true>(rt, rq);
+      } else {
+        sum = w.template sum<kExact, false>(rt, rq);
+      }
     }
     const double incl = before + cta_scan(sum, sh.scan);
     const bool here = sum > kNothing && (back || incl > goal);
@@ -733,47 +757,46 @@ __device__ __forceinline__ int32_t cluster_search(cg::cluster_group &cl, Weights
   return token;
 }
 
-// Slot sums of the weights in fp32, relative to one reference.
-template <int DT>
-__device__ __forceinline__ void cta_fast_sums(const Weights<DT> &w, const RolloutDev &d, Slots sl, RollShared &sh) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int64_t t = sl.lo + warp; t < sl.hi; t += kRollWarps) {
+// Slot sums of the weights, relative to one reference.  As in sweep(), the next vectors are on their way meanwhile; a
+// stage holds two of the target's and two of the draft's for each lane.
+template <int DT, bool kExact, bool kRest>
+__device__ __forceinline__ void cta_sums(const Weights<DT> &w, const RolloutDev &d, Slots sl, RollShared &sh) {
+  static_assert(kLoadVecs == 4, "two vectors of each row fill a stage");
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, steps = d.span * (kPartVecs / 64);
+  uint4 *ring = sh.ring[warp], *stage = ring;
+  int64_t ahead = sl.lo + warp;
+  int ahead_u = 0;
+  const auto ask = [&](uint4 *to) {
+    if (ahead < sl.hi) {
+      const int64_t i0 = (ahead * steps + ahead_u) * 64;
+      copy_vecs<DT, 2>(to, w.t, i0, w.V);
+      if (kRest) copy_vecs<DT, 2>(to + 64, w.q, i0, w.V);
+    }
+    copies_asked();
+    if (++ahead_u == steps) {
+      ahead_u = 0;
+      ahead += kRollWarps;
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < kStages; ++k) ask(ring + k * kPartVecs);
+  for (int64_t slot = sl.lo + warp; slot < sl.hi; slot += kRollWarps) {
     double s = 0.0;
-    const int64_t end = min((t + 1) * d.span, d.n_parts) * kPartVecs;
-    constexpr int kU = 4;
-    static_assert(kPartVecs % (32 * kU) == 0, "whole rounds");
-    for (int64_t i = t * d.span * kPartVecs + lane; i < end; i += 32 * kU) {
-      uint4 rt[kU], rq[kU];
-#pragma unroll
-      for (int u = 0; u < kU; ++u) w.load(i + 32 * u, rt[u], rq[u]);
-#pragma unroll
-      for (int u = 0; u < kU; ++u) s += w.fast_sum(rt[u], rq[u]);
+#pragma unroll 1
+    for (int u = 0; u < steps; ++u) {
+      oldest_copy();
+#pragma unroll(kExact ? 1 : 2)
+      for (int v = 0; v < 2; ++v) {
+        uint4 rt = stage[v * 32 + lane], rq = rt;
+        if (kRest) rq = stage[64 + v * 32 + lane];
+        else w.take_away((slot * steps + u) * 64 + v * 32 + lane, rt);
+        s += w.template sum<kExact, kRest>(rt, rq);
+      }
+      ask(stage);
+      stage = stage + kPartVecs == ring + kStages * kPartVecs ? ring : stage + kPartVecs;
     }
     s = warp_sum(s);
-    if (lane == 0) sh.tz[t - sl.lo] = s;
-  }
-  __syncthreads();
-}
-// The same in fp64; the next vector is on its way while one is worked on.
-template <int DT, bool kRest>
-__device__ __forceinline__ void cta_exact_sums(const Weights<DT> &w, const RolloutDev &d, Slots sl, RollShared &sh) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll 1
-  for (int64_t t = sl.lo + warp; t < sl.hi; t += kRollWarps) {
-    double s = 0.0;
-    const int64_t end = min((t + 1) * d.span, d.n_parts) * kPartVecs;
-    int64_t i = t * d.span * kPartVecs + lane;
-    uint4 rt, rq, nt, nq;
-    w.load(i, nt, nq);
-#pragma unroll 1
-    for (; i < end; i += 32) {
-      rt = nt;
-      rq = nq;
-      if (i + 32 < end) w.load(i + 32, nt, nq);
-      s += w.template exact_sum<kRest>(rt, rq);
-    }
-    s = warp_sum(s);
-    if (lane == 0) sh.tz[t - sl.lo] = s;
+    if (lane == 0) sh.tz[slot - sl.lo] = s;
   }
   __syncthreads();
 }
@@ -790,7 +813,7 @@ __device__ __noinline__ double cluster_exact_sum(cg::cluster_group &cl, const ch
   w.ct64 = c;
   w.least_t = least_of(c);
   w.tab = sh.tab;
-  cta_exact_sums<DT, false>(w, d, sl, sh);
+  cta_sums<DT, true, false>(w, d, sl, sh);
   const int size = (int)cl.num_blocks();
   if (threadIdx.x < 32) {
     double s = 0.0;
@@ -812,40 +835,39 @@ __device__ __forceinline__ float log_prob(float logit, const RowSum &r, double c
 
 // ---- draws: a cluster per row -----------------------------------------------------------------------
 
-// kDefer: one CTA a row; a row that fp32 does not decide is put on a list.  Otherwise the cluster decides it at once,
-// the rows of the grid or, with d.later, those of the list.  (Eight CTAs take an eighth of the time for a row in fp64:
-// put off, the few rows that need it do not hold up the end of a long grid.)
-template <int DT, bool kBest, bool kDefer>
-__global__ void __launch_bounds__(kRollThreads, kDefer ? 4 : 2) draw_kernel(const __grid_constant__ RolloutDev d) {
+// In the two modes of a long grid a row that fp32 does not decide waits for the second launch, where eight CTAs share it:
+// one CTA needs 100 us for it in fp64, and a few of those would hold up the end of the grid.
+template <int DT, bool kBest, int kMode>
+__global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) draw_kernel(const __grid_constant__ RolloutDev d) {
   __shared__ RollShared sh;
   cg::cluster_group cl = cg::this_cluster();
   const int rank = (int)cl.block_rank(), size = (int)cl.num_blocks();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const Slots sl = my_slots(d, rank, size);
   asm volatile("griddepcontrol.launch_dependents;");
-  if (!kBest && !kDefer) {
+  if (kMode != kFirst) {
     fill_exp64(sh.tab);
     __syncthreads();
   }
-  const bool listed = !kDefer && d.later;
-  if (listed) asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int32_t count = listed ? d.later[0] : d.B;
+  if (kMode == kSecond) asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int32_t count = kMode == kSecond ? d.later->count : d.B, step = (int32_t)(gridDim.x / size);
   int parity = 0;
-  for (int32_t k = blockIdx.x / size; k < count; k += gridDim.x / size) {
-    const int64_t n = listed ? d.later[1 + k] : k;
+  for (int32_t k = blockIdx.x / size; k < count; k += step) {
+    const int64_t n = kMode == kSecond ? d.later->e[k].unit : k;
     const char *row = d.target + n * d.tseq;
     const double v = kBest ? 0.0 : d.uniform[n];
     RowSum acc = nothing();
-    sweep<DT, kBest>(acc, row, d.vocab, sl.lo + warp, sl.hi, kRollWarps, d.span, d.ct, d.ct64, sh.ring[warp],
-                     [&](int64_t slot, RowSum &r) {
-                       if (kBest) return;
-                       r.z = warp_sum(r.z);
-                       if (lane == 0) {
-                         sh.tm[slot - sl.lo] = r.m;
-                         sh.tz[slot - sl.lo] = r.z;
-                       }
-                       r = nothing();
-                     });
+    if (kMode != kSecond)
+      sweep<DT, kBest>(acc, row, d.vocab, sl.lo + warp, sl.hi, kRollWarps, d.span, d.ct, d.ct64, sh.ring[warp],
+                       [&](int64_t slot, RowSum &r) {
+                         if (kBest) return;
+                         r.z = warp_sum(r.z);
+                         if (lane == 0) {
+                           sh.tm[slot - sl.lo] = r.m;
+                           sh.tz[slot - sl.lo] = r.z;
+                         }
+                         r = nothing();
+                       });
     int32_t token = kUnsure;
     float lp = 0.f;
     bool good;
@@ -863,7 +885,6 @@ __global__ void __launch_bounds__(kRollThreads, kDefer ? 4 : 2) draw_kernel(cons
       good = r.m > -INFINITY && r.m < INFINITY;  // (warp 0)
       if (rank == 0 && good) token = r.best;
     } else {
-      __syncthreads();
       const bool v_ok = v >= 0.0 && v < 1.0;
       Weights<DT> w = {};
       w.t = row;
@@ -873,19 +894,24 @@ __global__ void __launch_bounds__(kRollThreads, kDefer ? 4 : 2) draw_kernel(cons
       w.ct64 = d.ct64;
       w.tab = sh.tab;
       RowSum total;
-      bool again;
-      token = cluster_search<DT, false, true>(cl, w, d, sl, v_ok ? v : 0.0, 2 * d.eps, 0.0, parity, sh, &total, &again);
-      parity ^= 1;
+      bool again = true;
+      if (kMode == kSecond) {
+        total = {d.later->e[k].m, 0, d.later->e[k].z};
+      } else {
+        __syncthreads();
+        token = cluster_search<DT, false, true>(cl, w, d, sl, v_ok ? v : 0.0, 2 * d.eps, 0.0, parity, sh, &total, &again);
+        parity ^= 1;
+      }
       good = is_distribution(total) && v_ok;
       if (is_distribution(total)) bits = FOPD_DEV_BAD_UNIFORM;
       if (again && good) {
-        if (kDefer) {
-          if (rank == 0 && threadIdx.x == 0) d.later[1 + atomicAdd(d.later, 1)] = (int32_t)n;
+        if (kMode == kFirst) {
+          if (rank == 0 && threadIdx.x == 0) d.later->e[atomicAdd(&d.later->count, 1)] = {(int32_t)n, total.m, total.z};
           continue;
         }
         w.ts = total;
         w.derive();
-        cta_exact_sums<DT, false>(w, d, sl, sh);
+        cta_sums<DT, true, false>(w, d, sl, sh);
         RowSum exact_total;
         bool never;
         token = cluster_search<DT, true, false>(cl, w, d, sl, v, 0.0, 0.0, parity, sh, &exact_total, &never);
@@ -906,7 +932,7 @@ __global__ void __launch_bounds__(kRollThreads, kDefer ? 4 : 2) draw_kernel(cons
       if (d.mask) d.mask[n] = good ? 1 : 0;
       if (d.n_accepted) d.n_accepted[n] = 0;
     }
-    if (k + (int32_t)(gridDim.x / size) < count) roll_sync(cl);  // the next row writes what this one has read
+    if (k + step < count) roll_sync(cl);  // the next row writes what this one has read
   }
 }
 
@@ -949,8 +975,8 @@ __device__ __forceinline__ void judge(const RolloutDev &d, int32_t b, int32_t j,
 }
 
 // A cluster per position, earlier positions of all sequences first: sums of the target's and the draft's row, and the
-// decision.  With d.stop (one CTA a position, more positions than fit at once) a position behind a rejection that is
-// known by then is left out.
+// decision.  With d.stop (more positions than fit at once) a position behind a rejection that is known by then is left
+// out.
 template <int DT, bool kBest>
 __global__ void __launch_bounds__(kRollThreads, 4) verify_sweep_kernel(const __grid_constant__ RolloutDev d) {
   __shared__ RollShared sh;
@@ -962,8 +988,14 @@ __global__ void __launch_bounds__(kRollThreads, 4) verify_sweep_kernel(const __g
   const int32_t j = (int32_t)(id / d.B), b = (int32_t)(id % d.B);
   const int32_t n = drafts_of(d, b);
   if (j > n) return;  // (all CTAs of the cluster alike)
-  // (one thread looks: the value may change between two looks)
-  if (d.stop && __syncthreads_or(threadIdx.x == 0 && *(volatile const int32_t *)(d.stop + b) < j)) return;
+  if (d.stop) {  // one thread looks for the whole cluster: the value may change between two looks
+    if (rank == 0 && threadIdx.x == 0) {
+      const int32_t seen = *(volatile const int32_t *)(d.stop + b);
+      for (int r = 0; r < size; ++r) *cl.map_shared_rank(&sh.stop, r) = seen;
+    }
+    roll_sync(cl);
+    if (sh.stop < j) return;
+  }
   const char *trow = d.target + b * d.tseq + j * d.trow, *qrow = d.draft + b * d.dseq + j * d.drow;
   const bool q_best = d.kind == kDraftBest, want_q = j < n && (d.kind == kDraftRows || q_best);
   RowSum t = nothing(), q = nothing();
@@ -1013,7 +1045,7 @@ __global__ void __launch_bounds__(kRollThreads, 4) verify_sweep_kernel(const __g
 }
 
 // One sequence of the finish, by a cluster.
-template <int DT, bool kBest, bool kDefer>
+template <int DT, bool kBest, int kMode>
 __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const RolloutDev &d, int32_t b, RollShared &sh) {
   using E = Elem<DT>;
   const int rank = (int)cl.block_rank(), size = (int)cl.num_blocks();
@@ -1038,8 +1070,8 @@ __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const Rol
     __syncthreads();
     state = pos[j].state;
     if (kBest || state != kOpen) break;
-    if (kDefer) {
-      if (rank == 0 && threadIdx.x == 0) d.later[1 + atomicAdd(d.later, 1)] = b;
+    if (kMode == kFirst) {
+      if (rank == 0 && threadIdx.x == 0) d.later->e[atomicAdd(&d.later->count, 1)].unit = b;
       return;
     }
     const int32_t x = d.drafted[(int64_t)b * d.K + j];
@@ -1092,25 +1124,26 @@ __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const Rol
       w.ts = t32;
       w.qs = q32;
       w.derive();
-      if (!w.beyond()) {
-        cta_fast_sums<DT>(w, d, sl, sh);
+      if (kMode != kSecond && !w.beyond()) {
+        if (w.rest) cta_sums<DT, false, true>(w, d, sl, sh);
+        else cta_sums<DT, false, false>(w, d, sl, sh);
         // p - q: both rows' weights and both their sums are off; else the row's whole sum counts, with what was taken away
         token = cluster_search<DT, false, false>(cl, w, d, sl, v, 0.0, w.rest ? 9 * d.eps : 2 * d.eps * t32.z, 0, sh,
                                                  &total, &again);
         if (!is_distribution(total)) again = true;
       }
       if (!again) break;
-      if (kDefer) {
-        if (rank == 0 && threadIdx.x == 0) d.later[1 + atomicAdd(d.later, 1)] = b;
+      if (kMode == kFirst) {
+        if (rank == 0 && threadIdx.x == 0) d.later->e[atomicAdd(&d.later->count, 1)].unit = b;
         return;
       }
       if (w.rest) {
         w.ts.z = cluster_exact_sum<DT>(cl, w.t, w.ts.m, d.ct64, d, sl, parity, sh);
         w.qs.z = cluster_exact_sum<DT>(cl, w.q, w.qs.m, d.cd64, d, sl, parity, sh);
         w.derive();
-        cta_exact_sums<DT, true>(w, d, sl, sh);
+        cta_sums<DT, true, true>(w, d, sl, sh);
       } else {
-        cta_exact_sums<DT, false>(w, d, sl, sh);
+        cta_sums<DT, true, false>(w, d, sl, sh);
       }
       bool never;
       token = cluster_search<DT, true, false>(cl, w, d, sl, v, 0.0, 0.0, 1, sh, &total, &never);
@@ -1139,20 +1172,19 @@ __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const Rol
 }
 
 // A cluster per sequence: the first position that is not accepted (an open one is settled in fp64), the new token,
-// the outputs.  kDefer and d.later as for draws.
-template <int DT, bool kBest, bool kDefer>
-__global__ void __launch_bounds__(kRollThreads, kDefer ? 3 : 2) verify_finish_kernel(const __grid_constant__ RolloutDev d) {
+// the outputs.  Modes as for draws.
+template <int DT, bool kBest, int kMode>
+__global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) verify_finish_kernel(const __grid_constant__ RolloutDev d) {
   __shared__ RollShared sh;
   cg::cluster_group cl = cg::this_cluster();
-  if (!kBest && !kDefer) fill_exp64(sh.tab);
+  if (!kBest && kMode != kFirst) fill_exp64(sh.tab);
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the sweep's positions are there, or the list
   const int size = (int)cl.num_blocks();
-  const bool listed = !kDefer && d.later;
-  const int32_t count = listed ? d.later[0] : d.B;
-  for (int32_t k = blockIdx.x / size; k < count; k += gridDim.x / size) {
-    finish_sequence<DT, kBest, kDefer>(cl, d, listed ? d.later[1 + k] : k, sh);
-    if (k + (int32_t)(gridDim.x / size) < count) roll_sync(cl);  // the next one writes what this one has read
+  const int32_t count = kMode == kSecond ? d.later->count : d.B, step = (int32_t)(gridDim.x / size);
+  for (int32_t k = blockIdx.x / size; k < count; k += step) {
+    finish_sequence<DT, kBest, kMode>(cl, d, kMode == kSecond ? d.later->e[k].unit : k, sh);
+    if (k + step < count) roll_sync(cl);  // the next one writes what this one has read
   }
 }
 
