@@ -58,10 +58,7 @@ double sum_error(int64_t vocab, float c, double c64) {
 }
 
 size_t later_bytes(int64_t units) { return sizeof(Later) + (size_t)units * sizeof(LaterEntry); }
-int64_t list_clusters(int64_t units) {
-  const int64_t most = kRollWhole / kRollMaxCluster;
-  return units < most ? units : most;
-}
+int64_t list_clusters(int64_t units, int c) { return units < kRollWhole / c ? units : kRollWhole / c; }
 // Two launches (Mode) for more rows or sequences than clusters of eight of the whole kernel fit at once.
 bool two_launches(int64_t units) { return units * kRollMaxCluster > kRollWhole; }
 
@@ -75,9 +72,9 @@ int launch_draw(RolloutDev d, cudaStream_t st) {
   if (rc != FOPD_OK) return rc;
   if (cudaMemsetAsync(d.later, 0, sizeof(int32_t), st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   if (rc == FOPD_OK) rc = launch_clusters(draw_kernel<DT, false, kFirst>, d, d.B, c, st);
-  set_parts<DT>(&d, kRollMaxCluster);
+  set_parts<DT>(&d, kDrawList);
   if (rc == FOPD_OK)
-    rc = launch_clusters(draw_kernel<DT, false, kSecond>, d, list_clusters(d.B), kRollMaxCluster, st, true);
+    rc = launch_clusters(draw_kernel<DT, false, kSecond>, d, list_clusters(d.B, kDrawList), kDrawList, st, true);
   if (cudaFreeAsync(d.later, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   return rc;
 }
@@ -86,36 +83,48 @@ template <int DT>
 int launch_verify(RolloutDev d, cudaStream_t st) {
   const bool best = d.ct64 == 0.0;
   const int64_t positions = (int64_t)d.B * (d.K + 1);
-  // (a position's two rows on one CTA each leave the SMs with unequal shares unless there are many more of them)
-  const int c = cluster_for(positions, 4 * kRollResident), cf = best ? 1 : cluster_for(d.B, kRollResident);
+  const int64_t parts = (d.vocab + kPartElems<DT> - 1) / kPartElems<DT>;
+  // Up to four times what fits at once, a cluster per position (rows of unequal need are then shared out evenly); more
+  // positions: clusters that stay, so few that a rejection is known before much behind it has been swept.
+  bool stay = positions > 4 * kRollResident;
+  int c = stay ? cluster_for(d.B, kRollResident) : cluster_for(positions, 2 * kRollResident);
+  while (c > 1 && parts * 2 < c * kRollWarps * 2) c /= 2;  // a few parts for each warp
+  const int cf = best ? 1 : cluster_for(d.B, kRollResident);
   const bool look = positions * c > kRollResident;  // later positions start when earlier ones have been decided
+  int64_t clusters = positions;
+  if (stay) clusters = d.B * ((kRollResident / c + d.B - 1) / d.B);
   const bool two = !best && two_launches(d.B);
   const size_t pos_bytes = ((size_t)positions * sizeof(Position) + 255) & ~size_t(255);
   const size_t stop_bytes = look ? ((size_t)d.B * sizeof(int32_t) + 255) & ~size_t(255) : 0;
+  const size_t next_bytes = stay ? stop_bytes : 0;
   char *tmp = nullptr;
-  int rc = scratch_alloc(reinterpret_cast<void **>(&tmp), pos_bytes + stop_bytes + (two ? later_bytes(d.B) : 0), st);
+  int rc = scratch_alloc(reinterpret_cast<void **>(&tmp), pos_bytes + stop_bytes + next_bytes + (two ? later_bytes(d.B) : 0), st);
   if (rc != FOPD_OK) return rc;
   d.pos = reinterpret_cast<Position *>(tmp);
   if (look) {
     d.stop = reinterpret_cast<int32_t *>(tmp + pos_bytes);
     if (cudaMemsetAsync(d.stop, 0x7f, stop_bytes, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   }
+  if (stay) {
+    d.next = reinterpret_cast<int32_t *>(tmp + pos_bytes + stop_bytes);
+    if (cudaMemsetAsync(d.next, 0, next_bytes, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
+  }
   if (two) {
-    d.later = reinterpret_cast<Later *>(tmp + pos_bytes + stop_bytes);
+    d.later = reinterpret_cast<Later *>(tmp + pos_bytes + stop_bytes + next_bytes);
     if (cudaMemsetAsync(d.later, 0, sizeof(int32_t), st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   }
   set_parts<DT>(&d, c);
   if (rc == FOPD_OK)
-    rc = best ? launch_clusters(verify_sweep_kernel<DT, true>, d, positions, c, st)
-              : launch_clusters(verify_sweep_kernel<DT, false>, d, positions, c, st);
+    rc = best ? launch_clusters(verify_sweep_kernel<DT, true>, d, clusters, c, st)
+              : launch_clusters(verify_sweep_kernel<DT, false>, d, clusters, c, st);
   set_parts<DT>(&d, cf);
   if (rc == FOPD_OK)
     rc = best  ? launch_clusters(verify_finish_kernel<DT, true, kFirst>, d, d.B, cf, st, true)
          : two ? launch_clusters(verify_finish_kernel<DT, false, kFirst>, d, d.B, cf, st, true)
                : launch_clusters(verify_finish_kernel<DT, false, kWhole>, d, d.B, cf, st, true);
   if (rc == FOPD_OK && two) {
-    set_parts<DT>(&d, kRollMaxCluster);
-    rc = launch_clusters(verify_finish_kernel<DT, false, kSecond>, d, list_clusters(d.B), kRollMaxCluster, st, true);
+    set_parts<DT>(&d, kFinishList);
+    rc = launch_clusters(verify_finish_kernel<DT, false, kSecond>, d, list_clusters(d.B, kFinishList), kFinishList, st, true);
   }
   if (cudaFreeAsync(tmp, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   return rc;

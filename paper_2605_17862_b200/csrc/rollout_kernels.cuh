@@ -27,6 +27,8 @@ constexpr int kPartVecs = 32 * kLoadVecs;
 constexpr int kStages = 2;          // parts of a warp on their way to shared memory
 constexpr int kSlots = 256;         // slots per CTA
 constexpr int kRollMaxCluster = 8;
+constexpr int kDrawList = 4;        // CTAs that share a row in the second launch of a draw: clusters of four pack onto the SMs,
+constexpr int kFinishList = 8;      // of eight they leave some empty; but a finish has three passes to make one after another
 constexpr int kRollResident = 592;  // CTAs of these kernels that 148 SMs hold at once (64 registers),
 constexpr int kRollWhole = 296;     // and of those with the fp64 part in them (128 registers)
 
@@ -49,11 +51,11 @@ struct Position {
 // Rows (sequences) to be decided in fp64 by a later launch.
 struct LaterEntry {
   int32_t unit;
-  float m;   // the row's sum (draws)
-  double z;
+  float m;   // the row's sum and number (draws)
+  double z, v;
 };
 struct Later {
-  int32_t count, pad[3];
+  int32_t count, pad[7];
   LaterEntry e[1];  // as many as there are rows
 };
 // What a launch of a draw or of a finish does: everything; the fp32 part, putting off what it does not decide; the fp64
@@ -75,6 +77,7 @@ struct RolloutDev {
   Position *pos;       // [B, K + 1]
   Later *later;        // kFirst, kSecond
   int32_t *stop;       // [B] the lowest position known not to be accepted, or NULL: nobody looks
+  int32_t *next;       // [B] the next position to sweep, or NULL: the grid has a cluster for each
   int32_t *tokens;
   float *logprob;
   uint8_t *mask;
@@ -531,17 +534,15 @@ struct Weights {
   __device__ __forceinline__ double sum(const uint4 &rt, const uint4 &rq) const {
     return kExact ? exact_sum<kRest>(rt, rq) : fast_sum<kRest>(rt, rq);
   }
-  // one element in fp64, or in fp32
+  // one element's weight from its logits, in fp64 or in fp32
   template <bool kExact>
-  __device__ __forceinline__ double element(int64_t i) const {
-    if (i >= V || i == without) return 0.0;
-    const float x = Elem<DT>::load1(t, i);
+  __device__ __forceinline__ double element(float x, float y) const {
     if (kExact) {
       const Weight64 p = weight64(x, ts.m, ct64, least_t, tab);
-      return rest ? difference(p, weight64(Elem<DT>::load1(q, i), qs.m, cd64, least_q, tab)) : p.p * p.scale;
+      return rest ? difference(p, weight64(y, qs.m, cd64, least_q, tab)) : p.p * p.scale;
     }
     const float p = ex2(fmaf(x, ct, -mct));
-    return rest ? (double)fmaxf(fmaf(p, a, -b * ex2(fmaf(Elem<DT>::load1(q, i), cd, -mcd))), 0.f) : (double)p;
+    return rest ? (double)fmaxf(fmaf(p, a, -b * ex2(fmaf(y, cd, -mcd))), 0.f) : (double)p;
   }
 };
 
@@ -551,6 +552,10 @@ __device__ __forceinline__ void roll_sync(cg::cluster_group &cl) {
   if (cl.num_blocks() > 1) cl.sync();
   else __syncthreads();
 }
+
+struct ExactSums {
+  double t, q;  // of a target's row and of a draft's
+};
 
 // CTAs of a cluster write into one another's shared memory before a barrier of the cluster and read their own behind
 // it; so a CTA may leave when it has passed its last barrier.
@@ -562,12 +567,13 @@ struct RollShared {
   double tab[16];
   RowSum part[2][kRollWarps];
   RowSum pub[2][kRollMaxCluster];  // the CTAs' totals, by parity of the exchange
-  double sums[2][kRollMaxCluster];
+  ExactSums sums[2][kRollMaxCluster * kRollWarps];  // the warps' exact sums, by parity
   RowSum total;
   double before, goal;
   int64_t slot;
-  float logit;  // of the element found
-  int32_t owner, result, thread, unsure, stop;
+  uint4 found[2];  // the vectors that hold the element found, and its logit
+  float logit;
+  int32_t owner, result, thread, unsure, stop, take[2];
 };
 
 // This CTA's slots of a row: [lo, hi) of ceil(n_parts / span), contiguous and in rank order.
@@ -612,8 +618,9 @@ __device__ int32_t cta_find(const Weights<DT> &w, const RolloutDev &d, int64_t s
     const int64_t o = (back ? last : s) * kRollThreads + threadIdx.x, i = vec0 + o;
     if (back) before = last_before;
     double sum = 0.0;
+    uint4 rt, rq;
     if (o < vecs) {
-      uint4 rt = row_vec<DT>(w.t, i, d.vocab), rq;
+      rt = row_vec<DT>(w.t, i, d.vocab);
       w.take_away(i, rt);
       if (w.rest) {
         rq = row_vec<DT>(w.q, i, d.vocab);
@@ -637,22 +644,24 @@ __device__ int32_t cta_find(const Weights<DT> &w, const RolloutDev &d, int64_t s
     if (here && back) atomicMax(&sh.thread, (int)threadIdx.x);
     else if (here) atomicMin(&sh.thread, (int)threadIdx.x);
     __syncthreads();
-    if (sh.thread == (int)threadIdx.x) {
-      double run = incl - sum, at_before = run, at_after = run;
-      int at = -1;
-#pragma unroll 1
-      for (int k = 0; k < P; ++k) {
-        const double x = w.template element<kExact>(i * P + k);
-        if (x > kNothing) {
-          at = k;
-          at_before = run;
-          run = at_after = run + x;
-          if (run > goal) break;
-        }
+    if (sh.thread >> 5 == (int)threadIdx.x >> 5) {  // its warp: a lane for each element
+      const int lane = threadIdx.x & 31;
+      if (sh.thread == (int)threadIdx.x) {
+        sh.found[0] = rt;
+        sh.found[1] = w.rest ? rq : rt;
       }
-      if (at >= 0 && (kExact || (goal - at_before > bound && at_after - goal > bound))) {
-        sh.result = (int32_t)(i * P + at);
-        sh.logit = Elem<DT>::load1(w.t, i * P + at);
+      __syncwarp();
+      const float logit = lane < P ? Elem<DT>::load1(&sh.found[0], lane) : 0.f;
+      const double x = lane < P ? w.template element<kExact>(logit, Elem<DT>::load1(&sh.found[1], lane)) : 0.0;
+      const int from = sh.thread & 31;
+      const double before_vec = __shfl_sync(0xffffffffu, incl - sum, from), after = before_vec + warp_scan(x);
+      const int64_t vec = __shfl_sync(0xffffffffu, i, from);
+      const unsigned pass = __ballot_sync(0xffffffffu, x > kNothing && after > goal),
+                     has = __ballot_sync(0xffffffffu, x > kNothing);
+      const int at = pass ? __ffs(pass) - 1 : 31 - __clz(has);
+      if (lane == at && (kExact || (goal - (after - x) > bound && after - goal > bound))) {
+        sh.result = (int32_t)(vec * P + at);
+        sh.logit = logit;
       }
     }
     break;
@@ -801,31 +810,77 @@ __device__ __forceinline__ void cta_sums(const Weights<DT> &w, const RolloutDev 
   __syncthreads();
 }
 
-// A row's sum of exponentials in fp64, over the cluster, in every thread.  parity alternates from call to call.
-template <int DT>
-__device__ __noinline__ double cluster_exact_sum(cg::cluster_group &cl, const char *row, float m, double c, const RolloutDev &d,
-                                    Slots sl, int &parity, RollShared &sh) {
-  Weights<DT> w = {};
-  w.t = row;
-  w.V = d.vocab;
-  w.without = -1;
-  w.ts = {m, 0, 1.0};
-  w.ct64 = c;
-  w.least_t = least_of(c);
-  w.tab = sh.tab;
-  cta_sums<DT, true, false>(w, d, sl, sh);
-  const int size = (int)cl.num_blocks();
-  if (threadIdx.x < 32) {
-    double s = 0.0;
-    for (int t = threadIdx.x; t < (int)(sl.hi - sl.lo); t += 32) s += sh.tz[t];
-    s = warp_sum(s);
-    if ((int)threadIdx.x < size) *cl.map_shared_rank(&sh.sums[parity][cl.block_rank()], threadIdx.x) = s;
+// The sums of exponentials of a target's row and, with q, of a draft's in fp64, over the cluster, in every thread.
+// parity alternates from call to call.
+template <int DT, bool kBoth>
+__device__ __forceinline__ ExactSums cta_exact_pair(const Weights<DT> &w, const RolloutDev &d, Slots sl, RollShared &sh) {
+  constexpr int P = Weights<DT>::P;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint4 *ring = sh.ring[warp], *stage = ring;
+  const int64_t end = min(sl.hi * d.span, d.n_parts) * (kPartVecs / 64);  // in steps of 64 vectors
+  int64_t ahead = sl.lo * d.span * (kPartVecs / 64) + warp;
+  const auto ask = [&](uint4 *to) {
+    if (ahead < end) {
+      copy_vecs<DT, 2>(to, w.t, ahead * 64, w.V);
+      if (kBoth) copy_vecs<DT, 2>(to + 64, w.q, ahead * 64, w.V);
+    }
+    copies_asked();
+    ahead += kRollWarps;
+  };
+#pragma unroll
+  for (int k = 0; k < kStages; ++k) ask(ring + k * kPartVecs);
+  ExactSums s = {0.0, 0.0};
+#pragma unroll 1
+  for (int64_t at = sl.lo * d.span * (kPartVecs / 64) + warp; at < end; at += kRollWarps) {
+    oldest_copy();
+#pragma unroll 1
+    for (int v = 0; v < 2; ++v) {
+      float x[P], y[P];
+      Elem<DT>::unpack(stage[v * 32 + lane], x);
+      if (kBoth) Elem<DT>::unpack(stage[64 + v * 32 + lane], y);
+#pragma unroll
+      for (int k = 0; k < P; ++k) {
+        const Weight64 p = weight64(x[k], w.ts.m, w.ct64, w.least_t, w.tab);
+        s.t = fma(p.p, p.scale, s.t);
+        if (kBoth) {
+          const Weight64 r = weight64(y[k], w.qs.m, w.cd64, w.least_q, w.tab);
+          s.q = fma(r.p, r.scale, s.q);
+        }
+      }
+    }
+    ask(stage);
+    stage = stage + kPartVecs == ring + kStages * kPartVecs ? ring : stage + kPartVecs;
   }
-  roll_sync(cl);
-  double s = 0.0;
-  for (int k = 0; k < size; ++k) s += sh.sums[parity][k];
-  parity ^= 1;
+  s.t = warp_sum(s.t);
+  if (kBoth) s.q = warp_sum(s.q);
   return s;
+}
+template <int DT>
+__device__ __noinline__ ExactSums cluster_exact_sums(cg::cluster_group &cl, const char *trow, float tm, const char *qrow,
+                                                     float qm, const RolloutDev &d, Slots sl, int &parity,
+                                                     RollShared &sh) {
+  Weights<DT> w = {};
+  w.t = trow;
+  w.q = qrow;
+  w.V = d.vocab;
+  w.ts = {tm, 0, 1.0};
+  w.qs = {qm, 0, 1.0};
+  w.ct64 = d.ct64;
+  w.cd64 = d.cd64;
+  w.least_t = least_of(d.ct64);
+  w.least_q = qrow ? least_of(d.cd64) : 0;
+  w.tab = sh.tab;
+  const ExactSums mine = qrow ? cta_exact_pair<DT, true>(w, d, sl, sh) : cta_exact_pair<DT, false>(w, d, sl, sh);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, size = (int)cl.num_blocks();
+  if (lane < size) cl.map_shared_rank(&sh.sums[parity][0], lane)[cl.block_rank() * kRollWarps + warp] = mine;
+  roll_sync(cl);
+  ExactSums s = {0.0, 0.0};
+  for (int k = lane; k < size * kRollWarps; k += 32) {
+    s.t += sh.sums[parity][k].t;
+    s.q += sh.sums[parity][k].q;
+  }
+  parity ^= 1;
+  return {warp_sum(s.t), warp_sum(s.q)};
 }
 
 // log p of an element of a row from its logit and the row's sum: the difference in fp64, the log's error is 1e-6 of it.
@@ -855,7 +910,7 @@ __global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) draw_ke
   for (int32_t k = blockIdx.x / size; k < count; k += step) {
     const int64_t n = kMode == kSecond ? d.later->e[k].unit : k;
     const char *row = d.target + n * d.tseq;
-    const double v = kBest ? 0.0 : d.uniform[n];
+    const double v = kBest ? 0.0 : kMode == kSecond ? d.later->e[k].v : d.uniform[n];
     RowSum acc = nothing();
     if (kMode != kSecond)
       sweep<DT, kBest>(acc, row, d.vocab, sl.lo + warp, sl.hi, kRollWarps, d.span, d.ct, d.ct64, sh.ring[warp],
@@ -906,7 +961,7 @@ __global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) draw_ke
       if (is_distribution(total)) bits = FOPD_DEV_BAD_UNIFORM;
       if (again && good) {
         if (kMode == kFirst) {
-          if (rank == 0 && threadIdx.x == 0) d.later->e[atomicAdd(&d.later->count, 1)] = {(int32_t)n, total.m, total.z};
+          if (rank == 0 && threadIdx.x == 0) d.later->e[atomicAdd(&d.later->count, 1)] = {(int32_t)n, total.m, total.z, v};
           continue;
         }
         w.ts = total;
@@ -974,37 +1029,64 @@ __device__ __forceinline__ void judge(const RolloutDev &d, int32_t b, int32_t j,
   if ((d.kind == kDraftRows || d.kind == kDraftBest) && o.state != kBadUniform && !is_distribution(o.q)) o.state = kBadRow;
 }
 
-// A cluster per position, earlier positions of all sequences first: sums of the target's and the draft's row, and the
-// decision.  With d.stop (more positions than fit at once) a position behind a rejection that is known by then is left
-// out.
+// A sequence's next position for the cluster, or -1: none is left, or all that are lie behind a rejection.  One thread
+// looks for all CTAs (the value may change between two looks).
+__device__ __forceinline__ int32_t take_position(cg::cluster_group &cl, const RolloutDev &d, int32_t b, int32_t j,
+                                                 RollShared &sh) {
+  if (!d.stop) return j <= drafts_of(d, b) ? j : -1;
+  if (cl.block_rank() == 0 && threadIdx.x == 0) {
+    if (d.next) j = atomicAdd(d.next + b, 1);
+    if (j > drafts_of(d, b) || *(volatile const int32_t *)(d.stop + b) < j) j = -1;
+    for (unsigned r = 0; r < cl.num_blocks(); ++r) *cl.map_shared_rank(&sh.take[0], r) = j;
+  }
+  roll_sync(cl);
+  return sh.take[0];
+}
+
+// One position: sums of the target's and the draft's row in one stream of parts, and the decision.
 template <int DT, bool kBest>
-__global__ void __launch_bounds__(kRollThreads, 4) verify_sweep_kernel(const __grid_constant__ RolloutDev d) {
-  __shared__ RollShared sh;
-  asm volatile("griddepcontrol.launch_dependents;");  // the finish may be set up beside the last positions
-  cg::cluster_group cl = cg::this_cluster();
+__device__ __forceinline__ void sweep_position(cg::cluster_group &cl, const RolloutDev &d, int32_t b, int32_t j,
+                                               RollShared &sh) {
   const int rank = (int)cl.block_rank(), size = (int)cl.num_blocks();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t id = blockIdx.x / size;
-  const int32_t j = (int32_t)(id / d.B), b = (int32_t)(id % d.B);
   const int32_t n = drafts_of(d, b);
-  if (j > n) return;  // (all CTAs of the cluster alike)
-  if (d.stop) {  // one thread looks for the whole cluster: the value may change between two looks
-    if (rank == 0 && threadIdx.x == 0) {
-      const int32_t seen = *(volatile const int32_t *)(d.stop + b);
-      for (int r = 0; r < size; ++r) *cl.map_shared_rank(&sh.stop, r) = seen;
-    }
-    roll_sync(cl);
-    if (sh.stop < j) return;
-  }
   const char *trow = d.target + b * d.tseq + j * d.trow, *qrow = d.draft + b * d.dseq + j * d.drow;
   const bool q_best = d.kind == kDraftBest, want_q = j < n && (d.kind == kDraftRows || q_best);
-  RowSum t = nothing(), q = nothing();
-  const int64_t first = rank * kRollWarps + warp, step = size * kRollWarps;
-  const auto nop = [](int64_t, RowSum &) {};
-  sweep<DT, kBest>(t, trow, d.vocab, first, d.n_parts, step, 1, d.ct, d.ct64, sh.ring[warp], nop);
-  if (want_q) {
-    if (q_best) sweep<DT, true>(q, qrow, d.vocab, first, d.n_parts, step, 1, d.cd, d.cd64, sh.ring[warp], nop);
-    else sweep<DT, false>(q, qrow, d.vocab, first, d.n_parts, step, 1, d.cd, d.cd64, sh.ring[warp], nop);
+  const int64_t total = want_q ? 2 * d.n_parts : d.n_parts, step = size * kRollWarps;
+  uint4 *ring = sh.ring[warp], *stage = ring;
+  int64_t ahead = rank * kRollWarps + warp;
+  const auto ask = [&](uint4 *to) {
+    if (ahead < total) {
+      const bool of_q = ahead >= d.n_parts;
+      copy_vecs<DT, kLoadVecs>(to, of_q ? qrow : trow, (of_q ? ahead - d.n_parts : ahead) * kPartVecs, d.vocab);
+    }
+    copies_asked();
+    ahead += step;
+  };
+#pragma unroll
+  for (int k = 0; k < kStages; ++k) ask(ring + k * kPartVecs);
+  RowSum t = nothing(), q = nothing();  // (q holds the row being swept, then the draft's)
+  bool in_q = false;
+#pragma unroll 1
+  for (int64_t part = rank * kRollWarps + warp; part < total; part += step) {
+    const bool of_q = part >= d.n_parts;
+    if (of_q && !in_q) {
+      t = q;
+      q = nothing();
+      in_q = true;
+    }
+    oldest_copy();
+    uint4 raw[kLoadVecs];
+#pragma unroll
+    for (int v = 0; v < kLoadVecs; ++v) raw[v] = stage[v * 32 + lane];
+    ask(stage);
+    stage = stage + kPartVecs == ring + kStages * kPartVecs ? ring : stage + kPartVecs;
+    if (kBest || (of_q && q_best)) add_best<DT>(q, raw, of_q ? part - d.n_parts : part);
+    else add_part<DT>(q, raw, of_q ? d.cd : d.ct, of_q ? d.cd64 : d.ct64);
+  }
+  if (!in_q) {
+    t = q;
+    q = nothing();
   }
   if (!kBest) t.z = warp_sum(t.z);
   if (!q_best) q.z = warp_sum(q.z);
@@ -1044,6 +1126,34 @@ __global__ void __launch_bounds__(kRollThreads, 4) verify_sweep_kernel(const __g
   }
 }
 
+// A cluster per position, earlier positions of all sequences first.  With d.stop (more positions than fit at once) a
+// position behind a rejection that is known by then is left out.  With d.next (many more) clusters stay and take a
+// sequence's next position each time, then look for work at a few other sequences.
+constexpr int kOthers = 8;
+template <int DT, bool kBest>
+__global__ void __launch_bounds__(kRollThreads, 4) verify_sweep_kernel(const __grid_constant__ RolloutDev d) {
+  __shared__ RollShared sh;
+  asm volatile("griddepcontrol.launch_dependents;");  // the finish may be set up beside the last positions
+  cg::cluster_group cl = cg::this_cluster();
+  const int64_t id = blockIdx.x / cl.num_blocks();
+  int32_t b = (int32_t)(id % d.B);
+  if (!d.next) {
+    const int32_t j = take_position(cl, d, b, (int32_t)(id / d.B), sh);
+    if (j >= 0) sweep_position<DT, kBest>(cl, d, b, j, sh);
+    return;
+  }
+  for (int others = 0; others <= kOthers;) {
+    const int32_t j = take_position(cl, d, b, 0, sh);
+    if (j >= 0) {
+      sweep_position<DT, kBest>(cl, d, b, j, sh);
+    } else {
+      ++others;
+      b = b + 1 < d.B ? b + 1 : 0;
+    }
+    roll_sync(cl);  // what this round has read is written in the next one
+  }
+}
+
 // One sequence of the finish, by a cluster.
 template <int DT, bool kBest, int kMode>
 __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const RolloutDev &d, int32_t b, RollShared &sh) {
@@ -1076,12 +1186,11 @@ __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const Rol
     }
     const int32_t x = d.drafted[(int64_t)b * d.K + j];
     const char *trow = d.target + b * d.tseq + j * d.trow, *qrow = d.draft + b * d.dseq + j * d.drow;
-    const double p = exp64((double)E::load1(trow, x) - pos[j].t.m, d.ct64) /
-                     cluster_exact_sum<DT>(cl, trow, pos[j].t.m, d.ct64, d, sl, parity, sh);
-    double q = 1.0;  // (kDraftBest: or 0 and then never open)
-    if (d.kind == kDraftRows)
-      q = exp64((double)E::load1(qrow, x) - pos[j].q.m, d.cd64) /
-          cluster_exact_sum<DT>(cl, qrow, pos[j].q.m, d.cd64, d, sl, parity, sh);
+    const bool rows = d.kind == kDraftRows;
+    const ExactSums z = cluster_exact_sums<DT>(cl, trow, pos[j].t.m, rows ? qrow : nullptr, pos[j].q.m, d, sl, parity, sh);
+    const double p = exp64((double)E::load1(trow, x) - pos[j].t.m, d.ct64) / z.t;
+    // (kDraftBest: q is 1, or 0 and then never open)
+    const double q = rows ? exp64((double)E::load1(qrow, x) - pos[j].q.m, d.cd64) / z.q : 1.0;
     if (!(d.uniform[(int64_t)b * W + j] * q < p)) {
       state = kReject;
       break;
@@ -1138,8 +1247,9 @@ __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const Rol
         return;
       }
       if (w.rest) {
-        w.ts.z = cluster_exact_sum<DT>(cl, w.t, w.ts.m, d.ct64, d, sl, parity, sh);
-        w.qs.z = cluster_exact_sum<DT>(cl, w.q, w.qs.m, d.cd64, d, sl, parity, sh);
+        const ExactSums z = cluster_exact_sums<DT>(cl, w.t, w.ts.m, w.q, w.qs.m, d, sl, parity, sh);
+        w.ts.z = z.t;
+        w.qs.z = z.q;
         w.derive();
         cta_sums<DT, true, true>(w, d, sl, sh);
       } else {
