@@ -70,7 +70,7 @@ int launch_draw(RolloutDev d, cudaStream_t st) {
   if (!two_launches(d.B)) return launch_clusters(draw_kernel<DT, false, kWhole>, d, d.B, c, st);
   int rc = scratch_alloc(reinterpret_cast<void **>(&d.later), later_bytes(d.B), st);
   if (rc != FOPD_OK) return rc;
-  if (cudaMemsetAsync(d.later, 0, sizeof(int32_t), st) != cudaSuccess) rc = FOPD_ERR_CUDA;
+  if (cudaMemsetAsync(d.later, kUnset & 0xff, sizeof(int32_t), st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   if (rc == FOPD_OK) rc = launch_clusters(draw_kernel<DT, false, kFirst>, d, d.B, c, st);
   set_parts<DT>(&d, kDrawList);
   if (rc == FOPD_OK)
@@ -101,18 +101,12 @@ int launch_verify(RolloutDev d, cudaStream_t st) {
   int rc = scratch_alloc(reinterpret_cast<void **>(&tmp), pos_bytes + stop_bytes + next_bytes + (two ? later_bytes(d.B) : 0), st);
   if (rc != FOPD_OK) return rc;
   d.pos = reinterpret_cast<Position *>(tmp);
-  if (look) {
-    d.stop = reinterpret_cast<int32_t *>(tmp + pos_bytes);
-    if (cudaMemsetAsync(d.stop, 0x7f, stop_bytes, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
-  }
-  if (stay) {
-    d.next = reinterpret_cast<int32_t *>(tmp + pos_bytes + stop_bytes);
-    if (cudaMemsetAsync(d.next, 0, next_bytes, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
-  }
-  if (two) {
-    d.later = reinterpret_cast<Later *>(tmp + pos_bytes + stop_bytes + next_bytes);
-    if (cudaMemsetAsync(d.later, 0, sizeof(int32_t), st) != cudaSuccess) rc = FOPD_ERR_CUDA;
-  }
+  if (look) d.stop = reinterpret_cast<int32_t *>(tmp + pos_bytes);
+  if (stay) d.next = reinterpret_cast<int32_t *>(tmp + pos_bytes + stop_bytes);
+  if (two) d.later = reinterpret_cast<Later *>(tmp + pos_bytes + stop_bytes + next_bytes);
+  // all counters in one go
+  const size_t unset = stop_bytes + next_bytes + (two ? sizeof(int32_t) : 0);
+  if (unset && cudaMemsetAsync(tmp + pos_bytes, kUnset & 0xff, unset, st) != cudaSuccess) rc = FOPD_ERR_CUDA;
   set_parts<DT>(&d, c);
   if (rc == FOPD_OK)
     rc = best ? launch_clusters(verify_sweep_kernel<DT, true>, d, clusters, c, st)

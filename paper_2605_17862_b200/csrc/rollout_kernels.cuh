@@ -54,8 +54,9 @@ struct LaterEntry {
   float m;   // the row's sum and number (draws)
   double z, v;
 };
+constexpr int32_t kUnset = 0x7f7f7f7f;  // what one memset leaves in all counters of a call
 struct Later {
-  int32_t count, pad[7];
+  int32_t count, pad[7];  // count starts at kUnset
   LaterEntry e[1];  // as many as there are rows
 };
 // What a launch of a draw or of a finish does: everything; the fp32 part, putting off what it does not decide; the fp64
@@ -77,7 +78,7 @@ struct RolloutDev {
   Position *pos;       // [B, K + 1]
   Later *later;        // kFirst, kSecond
   int32_t *stop;       // [B] the lowest position known not to be accepted, or NULL: nobody looks
-  int32_t *next;       // [B] the next position to sweep, or NULL: the grid has a cluster for each
+  int32_t *next;       // [B] kUnset + the next position to sweep, or NULL: the grid has a cluster for each
   int32_t *tokens;
   float *logprob;
   uint8_t *mask;
@@ -573,7 +574,7 @@ struct RollShared {
   int64_t slot;
   uint4 found[2];  // the vectors that hold the element found, and its logit
   float logit;
-  int32_t owner, result, thread, unsure, stop, take[2];
+  int32_t owner, result, thread, unsure, stop, take;
 };
 
 // This CTA's slots of a row: [lo, hi) of ceil(n_parts / span), contiguous and in rank order.
@@ -905,7 +906,7 @@ __global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) draw_ke
     __syncthreads();
   }
   if (kMode == kSecond) asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int32_t count = kMode == kSecond ? d.later->count : d.B, step = (int32_t)(gridDim.x / size);
+  const int32_t count = kMode == kSecond ? d.later->count - kUnset : d.B, step = (int32_t)(gridDim.x / size);
   int parity = 0;
   for (int32_t k = blockIdx.x / size; k < count; k += step) {
     const int64_t n = kMode == kSecond ? d.later->e[k].unit : k;
@@ -961,7 +962,7 @@ __global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) draw_ke
       if (is_distribution(total)) bits = FOPD_DEV_BAD_UNIFORM;
       if (again && good) {
         if (kMode == kFirst) {
-          if (rank == 0 && threadIdx.x == 0) d.later->e[atomicAdd(&d.later->count, 1)] = {(int32_t)n, total.m, total.z, v};
+          if (rank == 0 && threadIdx.x == 0) d.later->e[atomicAdd(&d.later->count, 1) - kUnset] = {(int32_t)n, total.m, total.z, v};
           continue;
         }
         w.ts = total;
@@ -998,32 +999,46 @@ __device__ __forceinline__ int32_t drafts_of(const RolloutDev &d, int32_t b) {
   return n < 0 ? 0 : n > d.K ? d.K : n;
 }
 
-// Decides on one position from its rows' sums.
+// What the decision on a draft needs besides the rows' sums, asked for before the sweep.
+struct Draft {
+  int32_t x;
+  double u;
+  float t, q;  // logits
+  bool there;
+};
 template <int DT>
-__device__ __forceinline__ void judge(const RolloutDev &d, int32_t b, int32_t j, int32_t n, bool target_best,
-                                      Position &o) {
-  using E = Elem<DT>;
+__device__ __forceinline__ Draft draft_of(const RolloutDev &d, int32_t b, int32_t j, int32_t n, const char *trow,
+                                          const char *qrow) {
+  Draft r = {-1, 0.0, 0.f, 0.f, false};
+  if (j < n) {
+    r.x = d.drafted[(int64_t)b * d.K + j];
+    r.u = d.uniform[(int64_t)b * (d.K + 1) + j];
+    r.there = r.x >= 0 && r.x < d.vocab;
+    if (r.there) {
+      r.t = Elem<DT>::load1(trow, r.x);
+      if (d.kind == kDraftRows) r.q = Elem<DT>::load1(qrow, r.x);
+    }
+  }
+  return r;
+}
+// Decides on one position.
+__device__ __forceinline__ void judge(const RolloutDev &d, const Draft &r, bool last, bool target_best, Position &o) {
   o.lp = 0.f;
   o.state = is_distribution(o.t) ? kEnd : kBadRow;
-  if (o.state == kBadRow || j == n) return;
-  const int32_t x = d.drafted[(int64_t)b * d.K + j];
-  const double u = d.uniform[(int64_t)b * (d.K + 1) + j];
-  if (x < 0 || x >= d.vocab) {
+  if (o.state == kBadRow || last) return;
+  if (!r.there) {
     o.state = kBadToken;
   } else if (target_best) {
-    o.state = x == o.t.best ? kAccept : kReject;
-  } else if (!(u >= 0.0 && u < 1.0)) {
+    o.state = r.x == o.t.best ? kAccept : kReject;
+  } else if (!(r.u >= 0.0 && r.u < 1.0)) {
     o.state = kBadUniform;
   } else {
-    const float logit = E::load1(d.target + b * d.tseq + j * d.trow, x);
-    const double p = exp64((double)logit - o.t.m, d.ct64) / o.t.z;
-    o.lp = log_prob(logit, o.t, d.ct64);
+    const double p = exp64((double)r.t - o.t.m, d.ct64) / o.t.z;
+    o.lp = log_prob(r.t, o.t, d.ct64);
     double q = 1.0;
-    if (d.kind == kDraftRows)
-      q = exp64((double)E::load1(d.draft + b * d.dseq + j * d.drow, x) - o.q.m, d.cd64) / o.q.z;
-    else if (d.kind == kDraftBest)
-      q = x == o.q.best ? 1.0 : 0.0;
-    const double uq = u * q;
+    if (d.kind == kDraftRows) q = exp64((double)r.q - o.q.m, d.cd64) / o.q.z;
+    else if (d.kind == kDraftBest) q = r.x == o.q.best ? 1.0 : 0.0;
+    const double uq = r.u * q;
     o.state = fabs(uq - p) < 4 * d.eps * fmax(uq, p) ? kOpen : uq < p ? kAccept : kReject;
   }
   if ((d.kind == kDraftRows || d.kind == kDraftBest) && o.state != kBadUniform && !is_distribution(o.q)) o.state = kBadRow;
@@ -1033,14 +1048,15 @@ __device__ __forceinline__ void judge(const RolloutDev &d, int32_t b, int32_t j,
 // looks for all CTAs (the value may change between two looks).
 __device__ __forceinline__ int32_t take_position(cg::cluster_group &cl, const RolloutDev &d, int32_t b, int32_t j,
                                                  RollShared &sh) {
-  if (!d.stop) return j <= drafts_of(d, b) ? j : -1;
+  if (!d.stop || (j == 0 && !d.next)) return j <= drafts_of(d, b) ? j : -1;
   if (cl.block_rank() == 0 && threadIdx.x == 0) {
-    if (d.next) j = atomicAdd(d.next + b, 1);
-    if (j > drafts_of(d, b) || *(volatile const int32_t *)(d.stop + b) < j) j = -1;
-    for (unsigned r = 0; r < cl.num_blocks(); ++r) *cl.map_shared_rank(&sh.take[0], r) = j;
+    const int32_t known = *(volatile const int32_t *)(d.stop + b);
+    if (d.next) j = atomicAdd(d.next + b, 1) - kUnset;
+    if (j > drafts_of(d, b) || known < j) j = -1;
+    for (unsigned r = 0; r < cl.num_blocks(); ++r) *cl.map_shared_rank(&sh.take, r) = j;
   }
   roll_sync(cl);
-  return sh.take[0];
+  return sh.take;
 }
 
 // One position: sums of the target's and the draft's row in one stream of parts, and the decision.
@@ -1065,6 +1081,8 @@ __device__ __forceinline__ void sweep_position(cg::cluster_group &cl, const Roll
   };
 #pragma unroll
   for (int k = 0; k < kStages; ++k) ask(ring + k * kPartVecs);
+  Draft draft = {};
+  if (rank == 0 && threadIdx.x == 0) draft = draft_of<DT>(d, b, j, n, trow, qrow);
   RowSum t = nothing(), q = nothing();  // (q holds the row being swept, then the draft's)
   bool in_q = false;
 #pragma unroll 1
@@ -1120,7 +1138,7 @@ __device__ __forceinline__ void sweep_position(cg::cluster_group &cl, const Roll
     if (q_best) q.z = 1.0;
     o.t = t;
     o.q = q;
-    judge<DT>(d, b, j, n, kBest, o);
+    judge(d, draft, j == n, kBest, o);
     d.pos[(int64_t)b * (d.K + 1) + j] = o;
     if (d.stop && j < n && o.state != kAccept && o.state != kOpen) atomicMin(d.stop + b, j);
   }
@@ -1181,7 +1199,7 @@ __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const Rol
     state = pos[j].state;
     if (kBest || state != kOpen) break;
     if (kMode == kFirst) {
-      if (rank == 0 && threadIdx.x == 0) d.later->e[atomicAdd(&d.later->count, 1)].unit = b;
+      if (rank == 0 && threadIdx.x == 0) d.later->e[atomicAdd(&d.later->count, 1) - kUnset].unit = b;
       return;
     }
     const int32_t x = d.drafted[(int64_t)b * d.K + j];
@@ -1243,7 +1261,7 @@ __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const Rol
       }
       if (!again) break;
       if (kMode == kFirst) {
-        if (rank == 0 && threadIdx.x == 0) d.later->e[atomicAdd(&d.later->count, 1)].unit = b;
+        if (rank == 0 && threadIdx.x == 0) d.later->e[atomicAdd(&d.later->count, 1) - kUnset].unit = b;
         return;
       }
       if (w.rest) {
@@ -1291,7 +1309,7 @@ __global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) verify_
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the sweep's positions are there, or the list
   const int size = (int)cl.num_blocks();
-  const int32_t count = kMode == kSecond ? d.later->count : d.B, step = (int32_t)(gridDim.x / size);
+  const int32_t count = kMode == kSecond ? d.later->count - kUnset : d.B, step = (int32_t)(gridDim.x / size);
   for (int32_t k = blockIdx.x / size; k < count; k += step) {
     finish_sequence<DT, kBest, kMode>(cl, d, kMode == kSecond ? d.later->e[k].unit : k, sh);
     if (k + step < count) roll_sync(cl);  // the next one writes what this one has read
