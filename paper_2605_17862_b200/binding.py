@@ -133,8 +133,10 @@ def _ptr(t):
 
 
 def _stream(stream=None):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    # (the raw handle of the current stream: torch.cuda.current_stream() takes longer than a small kernel)
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream
 
 
 def _check(rc: int, where: str):
@@ -322,37 +324,47 @@ def _dtype(t: torch.Tensor) -> int:
     return FOPD_F32
 
 
-def _check_out(t, dtype, shape, device):
-    """An output (or None): the entry points write whole contiguous arrays on the current device."""
-    assert t is None or (t.dtype == dtype and t.shape == shape and t.is_contiguous() and t.device == device)
+def _flat(t, dtype, n):
+    """An array of n elements as the library takes it: contiguous, on the device of the call's logits."""
+    return t.dtype == dtype and t.numel() == n and t.is_contiguous()
 
 
-def _check_status_word(status, device):
-    assert status is None or (status.dtype == torch.int32 and status.numel() >= 1 and status.device == device)
+def _out(t, dtype, n, device):
+    """Address of an output (or of None)."""
+    if t is None:
+        return None
+    assert _flat(t, dtype, n) and t.device == device
+    return t.data_ptr()
+
+
+def _status_word(status, device):
+    if status is None:
+        return None
+    assert status.dtype == torch.int32 and status.numel() >= 1 and status.device == device
+    return status.data_ptr()
 
 
 def _on_current_device(t):
     """The library launches on the current device."""
-    assert t.is_cuda and t.device.index == torch.cuda.current_device(), t.device
+    assert t.is_cuda and t.get_device() == torch._C._cuda_getDevice(), t.device
 
 
 def fopd_draw_tokens(logits, uniform, tokens, *, logprob=None, temperature=1.0, vocab=None, status=None, stream=None):
     """One token from each row of ``logits`` [n, V] by the given fp64 numbers ``uniform`` [n]: the
     inverse of the distribution function of softmax(logits / temperature) (temperature 0: the best
     token).  ``tokens`` int32 [n], ``logprob`` fp32 [n] or None."""
-    assert logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] <= 1)
-    n, cols = logits.shape
-    dev = logits.device
     _on_current_device(logits)
-    assert uniform.dtype == torch.float64 and uniform.shape == (n,) and uniform.is_contiguous() and uniform.device == dev
-    _check_out(tokens, torch.int32, (n,), dev)
-    _check_out(logprob, torch.float32, (n,), dev)
-    _check_status_word(status, dev)
+    n, cols = logits.shape
+    pitch, unit = logits.stride()
+    dev, bf16 = logits.device, logits.dtype == torch.bfloat16
+    assert (unit == 1 or cols <= 1) and (bf16 or logits.dtype == torch.float32)
+    assert _flat(uniform, torch.float64, n) and uniform.device == dev
     assert vocab is None or 0 < vocab <= cols
-    per = 16 // logits.element_size()
-    pitch = logits.stride(0) if n > 1 else -(-cols // per) * per
-    _check(lib().fopd_draw_tokens(logits.data_ptr(), uniform.data_ptr(), n, vocab or cols, pitch, _dtype(logits),
-                                  temperature, tokens.data_ptr(), _ptr(logprob), _ptr(status), _stream(stream)),
+    if n == 1:
+        pitch = (cols + 7) // 8 * 8
+    _check(lib().fopd_draw_tokens(logits.data_ptr(), uniform.data_ptr(), n, vocab or cols, pitch,
+                                  FOPD_BF16 if bf16 else FOPD_F32, temperature, _out(tokens, torch.int32, n, dev),
+                                  _out(logprob, torch.float32, n, dev), _status_word(status, dev), _stream(stream)),
            "fopd_draw_tokens")
 
 
@@ -362,30 +374,27 @@ def fopd_verify_draft(target, draft, draft_tokens, uniform, tokens, *, n_draft=N
     ``draft`` [B, K, V] or None (certain drafts), ``draft_tokens`` int32 [B, K], ``uniform`` fp64
     [B, K + 1], ``n_draft`` int32 [B] or None.  Outputs ``tokens`` int32, ``logprob`` fp32 and ``mask``
     uint8 [B, K + 1], ``n_accepted`` int32 [B]; all but the first may be None."""
-    assert target.dim() == 3 and (target.stride(2) == 1 or target.shape[2] <= 1)
-    B, W, cols = target.shape
-    K, dev = W - 1, target.device
     _on_current_device(target)
-    assert draft_tokens.dtype == torch.int32 and draft_tokens.shape == (B, K) and draft_tokens.is_contiguous()
-    assert uniform.dtype == torch.float64 and uniform.shape == (B, W) and uniform.is_contiguous()
+    B, W, cols = target.shape
+    seq, row, unit = target.stride()
+    K, dev, bf16 = W - 1, target.device, target.dtype == torch.bfloat16
+    assert (unit == 1 or cols <= 1) and (bf16 or target.dtype == torch.float32)
+    assert _flat(draft_tokens, torch.int32, B * K) and _flat(uniform, torch.float64, B * W)
     assert draft_tokens.device == dev and uniform.device == dev
+    draft_at, dseq, drow = None, 0, 0
     if draft is not None:
         assert draft.shape == (B, K, cols) and draft.dtype == target.dtype and draft.device == dev
-        assert draft.stride(2) == 1 or cols <= 1
-    if n_draft is not None:
-        assert n_draft.dtype == torch.int32 and n_draft.shape == (B,) and n_draft.is_contiguous() and n_draft.device == dev
-    _check_out(tokens, torch.int32, (B, W), dev)
-    _check_out(logprob, torch.float32, (B, W), dev)
-    _check_out(mask, torch.uint8, (B, W), dev)
-    _check_out(n_accepted, torch.int32, (B,), dev)
-    _check_status_word(status, dev)
+        draft_at = draft.data_ptr()
+        dseq, drow, unit = draft.stride()
+        assert unit == 1 or cols <= 1
     assert vocab is None or 0 < vocab <= cols
-    d = fopd_draft(target.data_ptr(), None if draft is None else draft.data_ptr(), draft_tokens.data_ptr(),
-                   None if n_draft is None else n_draft.data_ptr(), uniform.data_ptr(), vocab or cols,
-                   target.stride(0), target.stride(1), 0 if draft is None else draft.stride(0),
-                   0 if draft is None else draft.stride(1), B, K, _dtype(target), temperature, draft_temperature)
-    _check(lib().fopd_verify_draft(ctypes.byref(d), tokens.data_ptr(), _ptr(logprob), _ptr(mask), _ptr(n_accepted),
-                                   _ptr(status), _stream(stream)), "fopd_verify_draft")
+    d = fopd_draft(target.data_ptr(), draft_at, draft_tokens.data_ptr(), _out(n_draft, torch.int32, B, dev),
+                   uniform.data_ptr(), vocab or cols, seq, row, dseq, drow, B, K, FOPD_BF16 if bf16 else FOPD_F32,
+                   temperature, draft_temperature)
+    _check(lib().fopd_verify_draft(ctypes.byref(d), _out(tokens, torch.int32, B * W, dev),
+                                   _out(logprob, torch.float32, B * W, dev), _out(mask, torch.uint8, B * W, dev),
+                                   _out(n_accepted, torch.int32, B, dev), _status_word(status, dev), _stream(stream)),
+           "fopd_verify_draft")
 
 
 def _as_rows(t: torch.Tensor):
@@ -431,34 +440,39 @@ def grad_workspace(device) -> torch.Tensor:
     return torch.zeros(GRAD_WS, dtype=torch.float64, device=device)
 
 
-def _grad_args(grads, ws, status, scalars):
+def _grad_args(grads, ws):
     assert ws.dtype == torch.float64 and ws.numel() >= GRAD_WS and ws.is_contiguous()
     _on_current_device(ws)
     assert grads.device is None or grads.device == ws.device
-    _check_status_word(status, ws.device)
-    for t in scalars:
-        assert t is None or (t.dtype == torch.float32 and t.numel() >= 1 and t.device == ws.device)
+    return ws.device
+
+
+def _scalar(t, device):
+    if t is None:
+        return None
+    assert t.dtype == torch.float32 and t.numel() >= 1 and t.device == device
+    return t.data_ptr()
 
 
 def fopd_grad_norm(grads: GradientList, ws, *, norm=None, status=None, stream=None):
     """ws[0] += sum of squares; ``norm`` fp32 [1] = sqrt(ws[0])."""
-    _grad_args(grads, ws, status, (norm,))
-    _check(lib().fopd_grad_norm(grads.array, grads.n, ws.data_ptr(), _ptr(norm), _ptr(status), _stream(stream)),
-           "fopd_grad_norm")
+    dev = _grad_args(grads, ws)
+    _check(lib().fopd_grad_norm(grads.array, grads.n, ws.data_ptr(), _scalar(norm, dev), _status_word(status, dev),
+                                _stream(stream)), "fopd_grad_norm")
 
 
 def fopd_grad_scale(grads: GradientList, ws, max_norm, *, norm=None, coef=None, status=None, stream=None):
     """Every element times min(1, max_norm / sqrt(ws[0])), into ``outs`` or in place."""
-    _grad_args(grads, ws, status, (norm, coef))
-    _check(lib().fopd_grad_scale(grads.array, grads.n, ws.data_ptr(), float(max_norm), _ptr(norm), _ptr(coef),
-                                 _ptr(status), _stream(stream)), "fopd_grad_scale")
+    dev = _grad_args(grads, ws)
+    _check(lib().fopd_grad_scale(grads.array, grads.n, ws.data_ptr(), max_norm, _scalar(norm, dev),
+                                 _scalar(coef, dev), _status_word(status, dev), _stream(stream)), "fopd_grad_scale")
 
 
 def fopd_grad_clip(grads: GradientList, max_norm, ws, *, norm=None, coef=None, status=None, stream=None):
     """Norm of the whole set and scaling in one call."""
-    _grad_args(grads, ws, status, (norm, coef))
-    _check(lib().fopd_grad_clip(grads.array, grads.n, ws.data_ptr(), float(max_norm), _ptr(norm), _ptr(coef),
-                                _ptr(status), _stream(stream)), "fopd_grad_clip")
+    dev = _grad_args(grads, ws)
+    _check(lib().fopd_grad_clip(grads.array, grads.n, ws.data_ptr(), max_norm, _scalar(norm, dev),
+                                _scalar(coef, dev), _status_word(status, dev), _stream(stream)), "fopd_grad_clip")
 
 
 def fopd_check_status(status, stream=None) -> int:

@@ -9,7 +9,9 @@ namespace fopd {
 
 constexpr int kClipThreads = 256;
 constexpr int kClipTileBytes = 32768;  // a CTA's piece of a row of a tensor
-constexpr int kClipMaxGrid = 1480;     // partial sums of a launch fit the workspace
+constexpr int kClipVecs = 8;           // 16-byte vectors of a tile per thread, in flight together
+constexpr int kClipMaxGrid = 592;      // CTAs that stay, four to an SM; their partial sums fit the workspace
+static_assert(kClipTileBytes == kClipThreads * kClipVecs * 16, "a full tile is one round of loads");
 constexpr int kClipTicket = 1;         // ws[1]: counter of finished CTAs (left at zero by every launch)
 constexpr int kClipPartials = 8;       // ws[8 ..]: partial sums, one per CTA
 static_assert(kClipPartials + kClipMaxGrid <= FOPD_GRAD_WS, "the workspace holds the partial sums");
@@ -26,6 +28,7 @@ template <int N>
 struct ClipTable {
   int64_t n_tiles;
   int32_t n;
+  int32_t in_place;  // every tensor's out is its data
   ClipEntry e[N];
 };
 
@@ -54,7 +57,24 @@ __device__ __forceinline__ ClipTile tile_range(const ClipEntry &e, int64_t tile)
   return {row * e.row_stride + piece * per, (int)(left < per ? left : per)};
 }
 
+__device__ __forceinline__ uint4 ld_keep(const void *p) {  // (the scaling that follows reads it again)
+  return *reinterpret_cast<const uint4 *>(p);
+}
+
 // Sum of squares of n elements at p, per thread, in fp64 (|g| up to 3e38: its square is out of fp32's range).
+template <int DT>
+__device__ __forceinline__ double vec_squares(const uint4 &v) {
+  constexpr int P = Elem<DT>::kPerVec;
+  float x[P];
+  Elem<DT>::unpack(v, x);
+  double s = 0.0, r = 0.0;
+#pragma unroll
+  for (int k = 0; k < P; k += 2) {
+    s = fma((double)x[k], (double)x[k], s);
+    r = fma((double)x[k + 1], (double)x[k + 1], r);
+  }
+  return s + r;
+}
 template <int DT>
 __device__ __forceinline__ double tile_squares(const char *p, int n) {
   using E = Elem<DT>;
@@ -65,12 +85,14 @@ __device__ __forceinline__ double tile_squares(const char *p, int n) {
   const int nvec = (n - head) / P;
   const uint4 *v = reinterpret_cast<const uint4 *>(p + (size_t)head * E::kBytes);
   double s = 0.0;
-  for (int i = threadIdx.x; i < nvec; i += kClipThreads) {
-    float x[P];
-    E::unpack(ld_stream(v + i), x);
+  uint4 a[kClipVecs];
 #pragma unroll
-    for (int k = 0; k < P; ++k) s = fma((double)x[k], (double)x[k], s);
+  for (int u = 0; u < kClipVecs; ++u) {
+    const int i = threadIdx.x + u * kClipThreads;
+    a[u] = i < nvec ? ld_keep(v + i) : make_uint4(0, 0, 0, 0);
   }
+#pragma unroll
+  for (int u = 0; u < kClipVecs; ++u) s += vec_squares<DT>(a[u]);
   const int tail0 = head + nvec * P;
   const int k = (int)threadIdx.x < head ? (int)threadIdx.x : tail0 + ((int)threadIdx.x - head);
   if (k < n) {
@@ -83,10 +105,11 @@ __device__ __forceinline__ double tile_squares(const char *p, int n) {
 // grid <= kClipMaxGrid.  The CTAs' partial sums go to the workspace; the last CTA to finish adds them in the order
 // of the CTAs.  set != 0: ws[0] = the sum, else ws[0] += it.
 template <int N>
-__global__ void __launch_bounds__(kClipThreads)
+__global__ void __launch_bounds__(kClipThreads, 4)
     grad_norm_kernel(const __grid_constant__ ClipTable<N> t, double *ws, int set, float *norm, int32_t *status) {
   __shared__ double sh[kClipThreads];
   __shared__ int last;
+  asm volatile("griddepcontrol.launch_dependents;");
   double s = 0.0;
   for (int64_t tile = blockIdx.x; tile < t.n_tiles; tile += gridDim.x) {
     const ClipEntry &e = t.e[find_entry(t, tile)];
@@ -145,12 +168,22 @@ __device__ __forceinline__ void tile_scale(const char *p, char *o, int n, float 
   const int nvec = (n - head) / P;
   const uint4 *v = reinterpret_cast<const uint4 *>(p + (size_t)head * E::kBytes);
   uint4 *w = reinterpret_cast<uint4 *>(o + (size_t)head * E::kBytes);
-  for (int i = threadIdx.x; i < nvec; i += kClipThreads) {
-    float x[P];
-    E::unpack(ld_stream(v + i), x);
+  uint4 a[kClipVecs];
 #pragma unroll
-    for (int k = 0; k < P; ++k) x[k] *= c;
-    st_stream(w + i, E::pack(x));
+  for (int u = 0; u < kClipVecs; ++u) {
+    const int i = threadIdx.x + u * kClipThreads;
+    if (i < nvec) a[u] = ld_stream(v + i);
+  }
+#pragma unroll
+  for (int u = 0; u < kClipVecs; ++u) {
+    const int i = threadIdx.x + u * kClipThreads;
+    if (i < nvec) {
+      float x[P];
+      E::unpack(a[u], x);
+#pragma unroll
+      for (int k = 0; k < P; ++k) x[k] *= c;
+      st_stream(w + i, E::pack(x));
+    }
   }
   const int tail0 = head + nvec * P;
   const int k = (int)threadIdx.x < head ? (int)threadIdx.x : tail0 + ((int)threadIdx.x - head);
@@ -158,9 +191,10 @@ __device__ __forceinline__ void tile_scale(const char *p, char *o, int n, float 
 }
 
 template <int N>
-__global__ void __launch_bounds__(kClipThreads)
+__global__ void __launch_bounds__(kClipThreads, 4)
     grad_scale_kernel(const __grid_constant__ ClipTable<N> t, const double *ws, float max_norm, float *norm,
                       float *coef, int32_t *status) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // the norm kernel's sum (launched early behind it)
   const double sum = ws[FOPD_GRAD_WS_SUM];
   const float c = clip_coef(sum, max_norm);
   if (blockIdx.x == 0 && threadIdx.x == 0) {
@@ -168,7 +202,9 @@ __global__ void __launch_bounds__(kClipThreads)
     if (coef) coef[0] = c;
     if (status && !(sum <= 1.7976931348623157e308)) atomicOr(status, FOPD_DEV_NONFINITE);
   }
-  for (int64_t tile = blockIdx.x; tile < t.n_tiles; tile += gridDim.x) {
+  if (c == 1.f && t.in_place) return;
+  // from the end: what the norm has read last may still be in the L2
+  for (int64_t tile = t.n_tiles - 1 - blockIdx.x; tile >= 0; tile -= gridDim.x) {
     const ClipEntry &e = t.e[find_entry(t, tile)];
     if (c == 1.f && e.out == e.data) continue;
     const ClipTile r = tile_range(e, tile);

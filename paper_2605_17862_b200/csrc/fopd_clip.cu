@@ -9,9 +9,9 @@ using namespace fopd;
 
 namespace {
 
-// Tensors of one launch: the table is a kernel parameter (at most 32,764 bytes).  Small sets take the small table,
-// whose parameters are quicker to hand over.
-constexpr int kSmallTable = 64, kLargeTable = 580;
+// Tensors of one launch: the table is a kernel parameter (at most 32,764 bytes), in sizes so that small sets are quick to
+// hand over.
+constexpr int kLargestTable = 580;
 
 int check_tensors(const fopd_tensor *t, int32_t n, const double *ws) {
   if (n < 0) return FOPD_ERR_SIZE;
@@ -82,6 +82,7 @@ template <int N>
 void fill_table(const fopd_tensor *t, int32_t n, int32_t *next, ClipTable<N> *tab) {
   tab->n = 0;
   tab->n_tiles = 0;
+  tab->in_place = 1;
   for (; *next < n && tab->n < N; ++*next) {
     const fopd_tensor &x = t[*next];
     if (x.rows == 0 || x.cols == 0) continue;
@@ -90,6 +91,7 @@ void fill_table(const fopd_tensor *t, int32_t n, int32_t *next, ClipTable<N> *ta
     const int64_t rows = one_row ? 1 : x.rows;
     e.data = static_cast<const char *>(x.data);
     e.out = static_cast<char *>(x.out ? x.out : const_cast<void *>(x.data));
+    if (e.out != e.data) tab->in_place = 0;
     e.cols = one_row ? x.rows * x.cols : x.cols;
     e.row_stride = one_row ? e.cols : x.row_stride;
     e.tile0 = tab->n_tiles;
@@ -118,29 +120,45 @@ int launch_norm(const fopd_tensor *t, int32_t n, double *ws, int set, float *nor
   return FOPD_OK;
 }
 
+// early: set up while the norm kernel before it is still running (it waits for it itself).
 template <int N>
 int launch_scale(const fopd_tensor *t, int32_t n, const double *ws, float max_norm, float *norm, float *coef,
-                 int32_t *status, cudaStream_t st) {
+                 int32_t *status, cudaStream_t st, bool early) {
   ClipTable<N> tab;
   int32_t next = 0;
   do {
     fill_table<N>(t, n, &next, &tab);
-    grad_scale_kernel<N><<<clip_grid(tab.n_tiles), kClipThreads, 0, st>>>(tab, ws, max_norm, norm, coef, status);
-    const int rc = launch_ok();
-    if (rc != FOPD_OK) return rc;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(clip_grid(tab.n_tiles));
+    cfg.blockDim = dim3(kClipThreads);
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = early ? 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, grad_scale_kernel<N>, tab, ws, max_norm, norm, coef, status) != cudaSuccess) {
+      (void)cudaGetLastError();
+      return FOPD_ERR_CUDA;
+    }
+    early = false;
   } while (next < n);
   return FOPD_OK;
 }
 
-int norm_any(const fopd_tensor *t, int32_t n, double *ws, int set, float *norm, int32_t *status, cudaStream_t st) {
-  return n <= kSmallTable ? launch_norm<kSmallTable>(t, n, ws, set, norm, status, st)
-                          : launch_norm<kLargeTable>(t, n, ws, set, norm, status, st);
+template <int N>
+int launch_both(const fopd_tensor *t, int32_t n, double *ws, float max_norm, float *norm, float *coef, int32_t *status,
+                cudaStream_t st) {
+  const int rc = launch_norm<N>(t, n, ws, 1, nullptr, nullptr, st);
+  return rc != FOPD_OK ? rc : launch_scale<N>(t, n, ws, max_norm, norm, coef, status, st, n <= N);
 }
-int scale_any(const fopd_tensor *t, int32_t n, const double *ws, float max_norm, float *norm, float *coef,
-              int32_t *status, cudaStream_t st) {
-  return n <= kSmallTable ? launch_scale<kSmallTable>(t, n, ws, max_norm, norm, coef, status, st)
-                          : launch_scale<kLargeTable>(t, n, ws, max_norm, norm, coef, status, st);
-}
+
+// The smallest table for n tensors.
+#define FOPD_CLIP_TABLE(n, CALL)          \
+  ((n) <= 16    ? CALL(16)                 \
+   : (n) <= 64  ? CALL(64)                 \
+   : (n) <= 192 ? CALL(192)                \
+                : CALL(kLargestTable))
 
 int check_scale(const fopd_tensor *t, int32_t n, const double *ws, float max_norm) {
   const int rc = check_tensors(t, n, ws);
@@ -161,24 +179,30 @@ int fopd_grad_norm(const fopd_tensor *tensors, int32_t n_tensors, double *ws, fl
                    void *stream) {
   const int rc = check_tensors(tensors, n_tensors, ws);
   if (rc != FOPD_OK) return rc;
-  return norm_any(tensors, n_tensors, ws, 0, norm, status, static_cast<cudaStream_t>(stream));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+#define CALL(N) launch_norm<N>(tensors, n_tensors, ws, 0, norm, status, st)
+  return FOPD_CLIP_TABLE(n_tensors, CALL);
+#undef CALL
 }
 
 int fopd_grad_scale(const fopd_tensor *tensors, int32_t n_tensors, double *ws, float max_norm, float *norm,
                     float *coef, int32_t *status, void *stream) {
   const int rc = check_scale(tensors, n_tensors, ws, max_norm);
   if (rc != FOPD_OK) return rc;
-  return scale_any(tensors, n_tensors, ws, max_norm, norm, coef, status, static_cast<cudaStream_t>(stream));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+#define CALL(N) launch_scale<N>(tensors, n_tensors, ws, max_norm, norm, coef, status, st, false)
+  return FOPD_CLIP_TABLE(n_tensors, CALL);
+#undef CALL
 }
 
 int fopd_grad_clip(const fopd_tensor *tensors, int32_t n_tensors, double *ws, float max_norm, float *norm,
                    float *coef, int32_t *status, void *stream) {
-  int rc = check_scale(tensors, n_tensors, ws, max_norm);
+  const int rc = check_scale(tensors, n_tensors, ws, max_norm);
   if (rc != FOPD_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  rc = norm_any(tensors, n_tensors, ws, 1, nullptr, nullptr, st);
-  if (rc != FOPD_OK) return rc;
-  return scale_any(tensors, n_tensors, ws, max_norm, norm, coef, status, st);
+#define CALL(N) launch_both<N>(tensors, n_tensors, ws, max_norm, norm, coef, status, st)
+  return FOPD_CLIP_TABLE(n_tensors, CALL);
+#undef CALL
 }
 
 }  // extern "C"
