@@ -57,7 +57,8 @@ __device__ __forceinline__ ClipTile tile_range(const ClipEntry &e, int64_t tile)
   return {row * e.row_stride + piece * per, (int)(left < per ? left : per)};
 }
 
-__device__ __forceinline__ uint4 ld_keep(const void *p) {  // (the scaling that follows reads it again)
+// (an ordinary load: what the norm has read last the scaling finds in the L2, and it was faster there too)
+__device__ __forceinline__ uint4 ld_keep(const void *p) {
   return *reinterpret_cast<const uint4 *>(p);
 }
 
@@ -172,7 +173,7 @@ __device__ __forceinline__ void tile_scale(const char *p, char *o, int n, float 
 #pragma unroll
   for (int u = 0; u < kClipVecs; ++u) {
     const int i = threadIdx.x + u * kClipThreads;
-    if (i < nvec) a[u] = ld_stream(v + i);
+    if (i < nvec) a[u] = ld_keep(v + i);
   }
 #pragma unroll
   for (int u = 0; u < kClipVecs; ++u) {

@@ -51,17 +51,24 @@ bool disjoint_columns(const Range &a, const Range &b) {
 
 // Whether a written range meets another one (its own tensor's data exactly in place excepted).
 int check_overlap(const fopd_tensor *t, int32_t n) {
-  std::vector<Range> r;
-  r.reserve(2 * n);
-  bool sorted = true;
+  const auto before = [](const Range &a, const Range &b) { return a.lo < b.lo; };
+  // inputs (or in place) and outputs apart: each is usually in order already
+  std::vector<Range> in, out, r;
+  in.reserve(n);
   for (int32_t i = 0; i < n; ++i) {
     if (t[i].rows == 0 || t[i].cols == 0) continue;
     const bool in_place = !t[i].out || t[i].out == t[i].data;
-    r.push_back(range_of(t[i], t[i].data, i, in_place));
-    if (!in_place) r.push_back(range_of(t[i], t[i].out, i, true));
+    in.push_back(range_of(t[i], t[i].data, i, in_place));
+    if (!in_place) out.push_back(range_of(t[i], t[i].out, i, true));
   }
-  for (size_t i = 1; i < r.size() && sorted; ++i) sorted = r[i - 1].lo <= r[i].lo;
-  if (!sorted) std::sort(r.begin(), r.end(), [](const Range &a, const Range &b) { return a.lo < b.lo; });
+  for (std::vector<Range> *v : {&in, &out})
+    if (!std::is_sorted(v->begin(), v->end(), before)) std::sort(v->begin(), v->end(), before);
+  if (out.empty()) {
+    r.swap(in);
+  } else {
+    r.resize(in.size() + out.size());
+    std::merge(in.begin(), in.end(), out.begin(), out.end(), r.begin(), before);
+  }
   // open: ranges that reach beyond the start of the next one
   std::vector<Range> open;
   for (const Range &b : r) {
@@ -96,8 +103,8 @@ void fill_table(const fopd_tensor *t, int32_t n, int32_t *next, ClipTable<N> *ta
     e.row_stride = one_row ? e.cols : x.row_stride;
     e.tile0 = tab->n_tiles;
     e.dtype = x.dtype;
-    const int64_t per = kClipTileBytes / (x.dtype == FOPD_BF16 ? 2 : 4);
-    e.tiles_per_row = (int32_t)((e.cols + per - 1) / per);
+    const int64_t bytes = e.cols * (x.dtype == FOPD_BF16 ? 2 : 4);
+    e.tiles_per_row = (int32_t)((bytes + kClipTileBytes - 1) / kClipTileBytes);
     tab->n_tiles += rows * e.tiles_per_row;
   }
 }
@@ -107,13 +114,17 @@ unsigned clip_grid(int64_t n_tiles) {
 }
 
 template <int N>
+int launch_norm_table(const ClipTable<N> &tab, double *ws, int set, float *norm, int32_t *status, cudaStream_t st) {
+  grad_norm_kernel<N><<<clip_grid(tab.n_tiles), kClipThreads, 0, st>>>(tab, ws, set, norm, status);
+  return launch_ok();
+}
+template <int N>
 int launch_norm(const fopd_tensor *t, int32_t n, double *ws, int set, float *norm, int32_t *status, cudaStream_t st) {
   ClipTable<N> tab;
   int32_t next = 0;
   do {
     fill_table<N>(t, n, &next, &tab);
-    grad_norm_kernel<N><<<clip_grid(tab.n_tiles), kClipThreads, 0, st>>>(tab, ws, set, norm, status);
-    const int rc = launch_ok();
+    const int rc = launch_norm_table<N>(tab, ws, set, norm, status, st);
     if (rc != FOPD_OK) return rc;
     set = 0;
   } while (next < n);
@@ -122,26 +133,32 @@ int launch_norm(const fopd_tensor *t, int32_t n, double *ws, int set, float *nor
 
 // early: set up while the norm kernel before it is still running (it waits for it itself).
 template <int N>
+int launch_scale_table(const ClipTable<N> &tab, const double *ws, float max_norm, float *norm, float *coef,
+                       int32_t *status, cudaStream_t st, bool early) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(clip_grid(tab.n_tiles));
+  cfg.blockDim = dim3(kClipThreads);
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = early ? 1 : 0;
+  if (cudaLaunchKernelEx(&cfg, grad_scale_kernel<N>, tab, ws, max_norm, norm, coef, status) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return FOPD_ERR_CUDA;
+  }
+  return FOPD_OK;
+}
+template <int N>
 int launch_scale(const fopd_tensor *t, int32_t n, const double *ws, float max_norm, float *norm, float *coef,
-                 int32_t *status, cudaStream_t st, bool early) {
+                 int32_t *status, cudaStream_t st) {
   ClipTable<N> tab;
   int32_t next = 0;
   do {
     fill_table<N>(t, n, &next, &tab);
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(clip_grid(tab.n_tiles));
-    cfg.blockDim = dim3(kClipThreads);
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = early ? 1 : 0;
-    if (cudaLaunchKernelEx(&cfg, grad_scale_kernel<N>, tab, ws, max_norm, norm, coef, status) != cudaSuccess) {
-      (void)cudaGetLastError();
-      return FOPD_ERR_CUDA;
-    }
-    early = false;
+    const int rc = launch_scale_table<N>(tab, ws, max_norm, norm, coef, status, st, false);
+    if (rc != FOPD_OK) return rc;
   } while (next < n);
   return FOPD_OK;
 }
@@ -149,8 +166,15 @@ int launch_scale(const fopd_tensor *t, int32_t n, const double *ws, float max_no
 template <int N>
 int launch_both(const fopd_tensor *t, int32_t n, double *ws, float max_norm, float *norm, float *coef, int32_t *status,
                 cudaStream_t st) {
-  const int rc = launch_norm<N>(t, n, ws, 1, nullptr, nullptr, st);
-  return rc != FOPD_OK ? rc : launch_scale<N>(t, n, ws, max_norm, norm, coef, status, st, n <= N);
+  if (n > N) {
+    const int rc = launch_norm<N>(t, n, ws, 1, nullptr, nullptr, st);
+    return rc != FOPD_OK ? rc : launch_scale<N>(t, n, ws, max_norm, norm, coef, status, st);
+  }
+  ClipTable<N> tab;
+  int32_t next = 0;
+  fill_table<N>(t, n, &next, &tab);
+  const int rc = launch_norm_table<N>(tab, ws, 1, nullptr, nullptr, st);
+  return rc != FOPD_OK ? rc : launch_scale_table<N>(tab, ws, max_norm, norm, coef, status, st, true);
 }
 
 // The smallest table for n tensors.
@@ -190,7 +214,7 @@ int fopd_grad_scale(const fopd_tensor *tensors, int32_t n_tensors, double *ws, f
   const int rc = check_scale(tensors, n_tensors, ws, max_norm);
   if (rc != FOPD_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-#define CALL(N) launch_scale<N>(tensors, n_tensors, ws, max_norm, norm, coef, status, st, false)
+#define CALL(N) launch_scale<N>(tensors, n_tensors, ws, max_norm, norm, coef, status, st)
   return FOPD_CLIP_TABLE(n_tensors, CALL);
 #undef CALL
 }

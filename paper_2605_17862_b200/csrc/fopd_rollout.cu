@@ -59,15 +59,19 @@ double sum_error(int64_t vocab, float c, double c64) {
 
 size_t later_bytes(int64_t units) { return sizeof(Later) + (size_t)units * sizeof(LaterEntry); }
 int64_t list_clusters(int64_t units, int c) { return units < kRollWhole / c ? units : kRollWhole / c; }
-// Two launches (Mode) for more rows or sequences than clusters of eight of the whole kernel fit at once.
-bool two_launches(int64_t units) { return units * kRollMaxCluster > kRollWhole; }
+// Two launches (Mode) for more rows or sequences than clusters of c of the whole kernel fit at once.
+bool two_launches(int64_t units, int c) { return units * c > kRollWhole; }
 
 template <int DT>
 int launch_draw(RolloutDev d, cudaStream_t st) {
-  const int c = cluster_for(d.B, kRollResident);
+  int c = cluster_for(d.B, kRollResident);
   set_parts<DT>(&d, c);
   if (d.ct64 == 0.0) return launch_clusters(draw_kernel<DT, true, kFirst>, d, d.B, c, st);
-  if (!two_launches(d.B)) return launch_clusters(draw_kernel<DT, false, kWhole>, d, d.B, c, st);
+  if (!two_launches(d.B, kDrawList)) {
+    c = cluster_for(d.B, kRollWhole);
+    set_parts<DT>(&d, c);
+    return launch_clusters(draw_kernel<DT, false, kWhole>, d, d.B, c, st);
+  }
   int rc = scratch_alloc(reinterpret_cast<void **>(&d.later), later_bytes(d.B), st);
   if (rc != FOPD_OK) return rc;
   if (cudaMemsetAsync(d.later, kUnset & 0xff, sizeof(int32_t), st) != cudaSuccess) rc = FOPD_ERR_CUDA;
@@ -93,7 +97,7 @@ int launch_verify(RolloutDev d, cudaStream_t st) {
   const bool look = positions * c > kRollResident;  // later positions start when earlier ones have been decided
   int64_t clusters = positions;
   if (stay) clusters = d.B * ((kRollResident / c + d.B - 1) / d.B);
-  const bool two = !best && two_launches(d.B);
+  const bool two = !best && two_launches(d.B, kFinishList);
   const size_t pos_bytes = ((size_t)positions * sizeof(Position) + 255) & ~size_t(255);
   const size_t stop_bytes = look ? ((size_t)d.B * sizeof(int32_t) + 255) & ~size_t(255) : 0;
   const size_t next_bytes = stay ? stop_bytes : 0;
