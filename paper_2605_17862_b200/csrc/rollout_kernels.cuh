@@ -574,7 +574,7 @@ struct RollShared {
   int64_t slot;
   uint4 found[2];  // the vectors that hold the element found, and its logit
   float logit;
-  int32_t owner, result, thread, unsure, stop, take;
+  int32_t owner, result, thread, unsure, stop, take[2];
 };
 
 // This CTA's slots of a row: [lo, hi) of ceil(n_parts / span), contiguous and in rank order.
@@ -1044,19 +1044,50 @@ __device__ __forceinline__ void judge(const RolloutDev &d, const Draft &r, bool 
   if ((d.kind == kDraftRows || d.kind == kDraftBest) && o.state != kBadUniform && !is_distribution(o.q)) o.state = kBadRow;
 }
 
-// A sequence's next position for the cluster, or -1: none is left, or all that are lie behind a rejection.  One thread
-// looks for all CTAs (the value may change between two looks).
-__device__ __forceinline__ int32_t take_position(cg::cluster_group &cl, const RolloutDev &d, int32_t b, int32_t j,
-                                                 RollShared &sh) {
-  if (!d.stop || (j == 0 && !d.next)) return j <= drafts_of(d, b) ? j : -1;
+// Whether a position is to be swept: its sequence has it, and no rejection before it is known.  One thread looks for all
+// CTAs of the cluster (the value may change between two looks).
+__device__ __forceinline__ bool wanted(cg::cluster_group &cl, const RolloutDev &d, int32_t b, int32_t j, RollShared &sh) {
+  if (!d.stop || j == 0) return j <= drafts_of(d, b);
   if (cl.block_rank() == 0 && threadIdx.x == 0) {
     const int32_t known = *(volatile const int32_t *)(d.stop + b);
-    if (d.next) j = atomicAdd(d.next + b, 1) - kUnset;
-    if (j > drafts_of(d, b) || known < j) j = -1;
-    for (unsigned r = 0; r < cl.num_blocks(); ++r) *cl.map_shared_rank(&sh.take, r) = j;
+    for (unsigned r = 0; r < cl.num_blocks(); ++r)
+      *cl.map_shared_rank(&sh.take[0], r) = j <= drafts_of(d, b) && known >= j;
   }
   roll_sync(cl);
-  return sh.take;
+  return sh.take[0];
+}
+
+// The next position for a cluster that stays: of the sequence it is at, else of one of the 31 behind it.  {b, j} in
+// sh.take; j = -1: nothing is left there, or other clusters have it (one that takes a position comes back to the same
+// sequence, so no sequence is left with work and without a cluster).
+__device__ __forceinline__ void take_next(cg::cluster_group &cl, const RolloutDev &d, int32_t b, RollShared &sh) {
+  if (cl.block_rank() == 0 && threadIdx.x < 32) {
+    const int lane = threadIdx.x;
+    const int32_t at = (int32_t)(((int64_t)b + lane) % d.B);
+    int32_t take_b = b, take_j = -1;
+    for (int tries = 0; tries < 4; ++tries) {
+      int32_t left = -1;  // the last position that may be wanted
+      if (lane < d.B) left = min(drafts_of(d, at), *(volatile const int32_t *)(d.stop + at));
+      const bool some = lane < d.B && *(volatile const int32_t *)(d.next + at) - kUnset <= left;
+      const unsigned has = __ballot_sync(0xffffffffu, some);
+      if (!has) break;
+      const int from = __ffs(has) - 1;
+      int32_t j = -1;
+      if (lane == from) {
+        j = atomicAdd(d.next + at, 1) - kUnset;
+        if (j > left) j = -1;
+      }
+      take_j = __shfl_sync(0xffffffffu, j, from);
+      take_b = __shfl_sync(0xffffffffu, at, from);
+      if (take_j >= 0) break;
+    }
+    if (lane < (int)cl.num_blocks()) {
+      int32_t *to = cl.map_shared_rank(&sh.take[0], lane);
+      to[0] = take_b;
+      to[1] = take_j;
+    }
+  }
+  roll_sync(cl);
 }
 
 // One position: sums of the target's and the draft's row in one stream of parts, and the decision.
@@ -1145,9 +1176,8 @@ __device__ __forceinline__ void sweep_position(cg::cluster_group &cl, const Roll
 }
 
 // A cluster per position, earlier positions of all sequences first.  With d.stop (more positions than fit at once) a
-// position behind a rejection that is known by then is left out.  With d.next (many more) clusters stay and take a
-// sequence's next position each time, then look for work at a few other sequences.
-constexpr int kOthers = 8;
+// position behind a rejection that is known by then is left out.  With d.next (many more) clusters stay and take one
+// position after another.
 template <int DT, bool kBest>
 __global__ void __launch_bounds__(kRollThreads, 4) verify_sweep_kernel(const __grid_constant__ RolloutDev d) {
   __shared__ RollShared sh;
@@ -1156,18 +1186,16 @@ __global__ void __launch_bounds__(kRollThreads, 4) verify_sweep_kernel(const __g
   const int64_t id = blockIdx.x / cl.num_blocks();
   int32_t b = (int32_t)(id % d.B);
   if (!d.next) {
-    const int32_t j = take_position(cl, d, b, (int32_t)(id / d.B), sh);
-    if (j >= 0) sweep_position<DT, kBest>(cl, d, b, j, sh);
+    const int32_t j = (int32_t)(id / d.B);
+    if (wanted(cl, d, b, j, sh)) sweep_position<DT, kBest>(cl, d, b, j, sh);
     return;
   }
-  for (int others = 0; others <= kOthers;) {
-    const int32_t j = take_position(cl, d, b, 0, sh);
-    if (j >= 0) {
-      sweep_position<DT, kBest>(cl, d, b, j, sh);
-    } else {
-      ++others;
-      b = b + 1 < d.B ? b + 1 : 0;
-    }
+  for (;;) {
+    take_next(cl, d, b, sh);
+    const int32_t j = sh.take[1];
+    b = sh.take[0];
+    if (j < 0) return;
+    sweep_position<DT, kBest>(cl, d, b, j, sh);
     roll_sync(cl);  // what this round has read is written in the next one
   }
 }
