@@ -386,6 +386,102 @@ def test_rollout_calls_on_a_side_stream_in_a_graph_and_at_the_same_time():
     assert torch.equal(r1, want_rows)
 
 
+# ---- every way a call is cut up: one launch or two, clusters of one to eight CTAs, slots of several parts ----
+
+@pytest.mark.parametrize("n,V,dtype", [(8, 9001, BF16), (60, 4001, F32), (140, 9001, F32), (200, 9001, BF16), (700, 3001, BF16)])
+def test_draw_many_rows_that_fp32_does_not_decide(n, V, dtype):
+    """Flat rows: with all probabilities near 1/V a number close to a boundary is the rule; numbers 1e-9 beside one."""
+    x = rows_of((n,), V, dtype, n, scale=0.01)
+    u = uniforms(n, n + 1)
+    for r in range(0, n, 3):
+        c = np.cumsum(ro.probabilities(x[r].cpu(), 1.0))
+        u[r] = float(c[(r * 37) % (V - 1)]) + (1e-9 if r % 2 else -1e-9)
+    tokens = check_draw(x, u, 1.0)
+    assert len(set(tokens.tolist())) > n // 3
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_draw_and_verify_rows_of_millions(dtype):
+    V = 5_000_003
+    x = rows_of((2,), V, dtype, 301, scale=1.0)
+    x[1, 4_999_990] = 25.0
+    for T in (1.0, 0.0):
+        check_draw(x, torch.tensor([0.999999, 0.999], device=DEV, dtype=torch.float64), T)
+    check_draw(x, uniforms(2, 302), 2.0)
+    draft = (x[:1].float() + 0.1).to(dtype)
+    wide = torch.zeros((1, 1, x.stride(0)), device=DEV, dtype=dtype)
+    wide[0, 0, :V] = draft[0]
+    wide[0, 0, 77] = 30.0  # the draft is sure of a token that the target hardly has
+    check_verify(x.view(1, 2, V) if x.is_contiguous() else x.unsqueeze(0), wide[:, :, :V],
+                 torch.tensor([[77]], dtype=torch.int32, device=DEV), uniforms((1, 2), 303))
+
+
+def test_draw_many_rows_with_slots_of_several_parts():
+    n, V = 640, 540_001
+    x = torch.zeros((n, V + 7), device=DEV, dtype=BF16)[:, :V]
+    some = [0, 1, 311, 638, 639]
+    rows = rows_of((len(some),), V, BF16, 311)
+    for k, r in enumerate(some):
+        x[r] = rows[k]
+    u = uniforms(n, 312)
+    tokens, lp, bits = run_draw(x, u, 1.0)
+    want = {r: ro.draw(rows[k].cpu(), float(u[r]), 1.0)[0] for k, r in enumerate(some)}
+    assert bits == 0 and {r: int(tokens[r]) for r in some} == want
+    even = torch.ones(n, dtype=torch.bool, device=DEV)
+    even[some] = False
+    assert torch.equal(tokens[even].long(), (u[even] * V).floor().long())  # even rows: floor(v V)
+
+
+@pytest.mark.parametrize("B,K", [(3, 2), (50, 2), (100, 30)])
+@pytest.mark.parametrize("form", ["rows", "certain"])
+def test_verify_decisions_next_to_equality(B, K, form):
+    """u q within 1e-9 of p, on both sides: fp32 leaves these open.  (B, K) such that a position has a cluster, the
+    finish is cut in two launches, or clusters stay."""
+    V = 1300
+    target, draft = rows_of((B, K + 1), V, BF16, 321 + B, scale=1.0), rows_of((B, K), V, BF16, 322, scale=1.0)
+    drafted = torch.zeros((B, K), dtype=torch.int32, device=DEV)
+    u = uniforms((B, K + 1), 323)
+    for b in range(B):
+        for j in range(min(K, 3)):
+            p = ro.probabilities(target[b, j].cpu(), 1.0)
+            q = ro.probabilities(draft[b, j].cpu(), 1.0) if form == "rows" else np.ones(V)
+            x = int(np.argmax(q - p)) if form == "rows" else int(np.argmax(p))
+            drafted[b, j] = x
+            u[b, j] = float(p[x] / q[x]) * (1 + (1e-9 if (b + j) % 3 == 0 else -1e-9))
+    got = check_verify(target, draft if form == "rows" else None, drafted, u)
+    assert got["n_accepted"].min() == 0 and got["n_accepted"].max() >= 2
+
+
+@pytest.mark.parametrize("form,T", [("rows", 1.0), ("certain", 0.7), ("best", 1.0), ("rows", 0.0)])
+@pytest.mark.parametrize("B,K,V", [(45, 6, 1501), (1, 3000, 70), (300, 9, 333), (33, 100, 129)])
+def test_verify_forms_at_every_cut(form, T, B, K, V):
+    target = rows_of((B, K + 1), V, F32, 331 + B, scale=2.0)
+    draft = rows_of((B, K), V, F32, 332, scale=0.3)
+    draft += target[:, :K]
+    Td = 0.0 if form == "best" else 1.0
+    drafted = drafts_from(draft if T else target[:, :K], Td if T else 0.0, 333)
+    if form == "certain":
+        drafted = target[:, :K].argmax(-1).int()
+    u = uniforms((B, K + 1), 334) * 0.9
+    n_draft = torch.randint(K // 2, K + 1, (B,), generator=torch.Generator(device=DEV).manual_seed(B), device=DEV,
+                            dtype=torch.int32)
+    got = check_verify(target, None if form == "certain" else draft, drafted, u, n_draft=n_draft, T=T, Td=Td)
+    if T == 0:
+        assert got["n_accepted"].tolist() == n_draft.tolist()
+    again, _ = run_verify(target, None if form == "certain" else draft, drafted, u, n_draft=n_draft, T=T, Td=Td)
+    assert all(np.array_equal(got[k], again[k]) for k in got)  # whatever order the clusters came in
+
+
+def test_logits_far_from_zero_and_small_temperatures():
+    for dtype, offset in ((BF16, 3000.0), (F32, -3.0e4), (F32, 2.0e8), (F32, -3.0e38)):
+        x = rows_of((6,), 2500, dtype, 341)
+        x.add_(offset) if offset > -1e38 else x.fill_(offset)
+        check_draw(x, uniforms(6, 342), 1.0)
+    x = rows_of((20,), 2500, BF16, 343)
+    for T in (2.0 ** -10, 0.02, 1024.0):
+        check_draw(x, uniforms(20, 344), T)
+
+
 # ---- together, as a training program uses them ----
 
 @pytest.mark.parametrize("dtype,T", [(F32, 1.0), (BF16, 1.0)])
