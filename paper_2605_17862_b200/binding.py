@@ -426,11 +426,11 @@ class GradientList:
         self.device = self.tensors[0].device if self.n else None
         for i, t in enumerate(self.tensors):
             _on_current_device(t)
-            layout = _as_rows(t)
+            layout = (1, t.numel(), t.numel()) if t.is_contiguous() else _as_rows(t)
             assert layout is not None, f"tensor {i}: strides {t.stride()} of shape {tuple(t.shape)}"
             o = None if self.outs is None else self.outs[i]
             assert o is None or (o.shape == t.shape and o.dtype == t.dtype and o.device == t.device and
-                                 (o.stride() == t.stride() or (o.is_contiguous() and t.is_contiguous())))
+                                 ((o.is_contiguous() and t.is_contiguous()) or o.stride() == t.stride()))
             assert self.device == t.device
             self.array[i] = fopd_tensor(t.data_ptr(), None if o is None else o.data_ptr(), *layout, _dtype(t), 0)
 

@@ -16,13 +16,26 @@ constexpr int kClipTicket = 1;         // ws[1]: counter of finished CTAs (left 
 constexpr int kClipPartials = 8;       // ws[8 ..]: partial sums, one per CTA
 static_assert(kClipPartials + kClipMaxGrid <= FOPD_GRAD_WS, "the workspace holds the partial sums");
 
+// A tensor in a launch's table: 32 bytes, since handing over a launch's parameters takes the host 0.5 us per KB.  One
+// whose rows lie apart takes a second entry.
+enum ClipKind : uint8_t { kClipDense = 0, kClipRows = 1, kClipShortRows = 2, kClipMore = 3 };
 struct ClipEntry {
   const char *data;
   char *out;
-  int64_t cols, row_stride;  // elements
-  int64_t tile0;             // first tile of this tensor in the launch
-  int32_t tiles_per_row, dtype;
+  int64_t cols;    // elements of a row; of the whole tensor where it is dense
+  uint32_t tile0;  // first tile of this tensor in the launch
+  uint8_t kind;    // kClipRows: each row is cut into tiles; kClipShortRows: a tile is a few whole rows
+  uint8_t dtype;
+  uint16_t pad;
 };
+struct ClipMore {  // in the place of the entry behind a tensor with rows
+  int64_t rows, row_stride;  // (elements)
+  int64_t per;               // tiles of a row, or rows of a tile
+  uint32_t tile0;            // the same as its tensor's
+  uint8_t kind, dtype;
+  uint16_t pad;
+};
+static_assert(sizeof(ClipEntry) == 32 && sizeof(ClipMore) == 32, "one size");
 
 template <int N>
 struct ClipTable {
@@ -32,29 +45,36 @@ struct ClipTable {
   ClipEntry e[N];
 };
 
-// The tensor a tile belongs to (the last one whose first tile is not behind it).
+// The tensor a tile belongs to: the last one whose first tile is not behind it.
 template <int N>
-__device__ __forceinline__ int find_entry(const ClipTable<N> &t, int64_t tile) {
+__device__ __forceinline__ int find_entry(const ClipTable<N> &t, uint32_t tile) {
   int lo = 0, hi = t.n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (t.e[mid].tile0 <= tile) lo = mid;
     else hi = mid - 1;
   }
-  return lo;
+  return t.e[lo].kind == kClipMore ? lo - 1 : lo;
 }
 
-// A tile as a range of elements: [off, off + n) behind the tensor's base.
+// A tile: n elements in a row from element `off` of the tensor on, or (rows > 0) rows of n elements `stride` apart.
 struct ClipTile {
-  int64_t off;
-  int n;
+  int64_t off, stride;
+  int n, rows;
 };
-__device__ __forceinline__ ClipTile tile_range(const ClipEntry &e, int64_t tile) {
-  const int64_t local = tile - e.tile0;
-  const int64_t row = local / e.tiles_per_row, piece = local % e.tiles_per_row;
+template <int N>
+__device__ __forceinline__ ClipTile tile_range(const ClipTable<N> &t, int i, uint32_t tile) {
+  const ClipEntry &e = t.e[i];
   const int per = kClipTileBytes / (e.dtype == FOPD_BF16 ? 2 : 4);
-  const int64_t left = e.cols - piece * per;
-  return {row * e.row_stride + piece * per, (int)(left < per ? left : per)};
+  const int64_t local = tile - e.tile0;
+  if (e.kind == kClipDense) return {local * per, 0, (int)min((int64_t)per, e.cols - local * per), 0};
+  const ClipMore &m = reinterpret_cast<const ClipMore &>(t.e[i + 1]);
+  if (e.kind == kClipShortRows) {
+    const int64_t row = local * m.per;
+    return {row * m.row_stride, m.row_stride, (int)e.cols, (int)min(m.per, m.rows - row)};
+  }
+  const int64_t row = local / m.per, piece = local % m.per;
+  return {row * m.row_stride + piece * per, 0, (int)min((int64_t)per, e.cols - piece * per), 0};
 }
 
 // (an ordinary load: what the norm has read last the scaling finds in the L2, and it was faster there too)
@@ -77,9 +97,18 @@ __device__ __forceinline__ double vec_squares(const uint4 &v) {
   return s + r;
 }
 template <int DT>
-__device__ __forceinline__ double tile_squares(const char *p, int n) {
+__device__ __forceinline__ double tile_squares(const char *p, const ClipTile &r) {
   using E = Elem<DT>;
   constexpr int P = E::kPerVec;
+  const int n = r.n;
+  if (r.rows > 0) {  // rows too short for vectors
+    double s = 0.0;
+    for (int i = threadIdx.x; i < r.rows * n; i += kClipThreads) {
+      const double x = (double)E::load1(p, (i / n) * r.stride + i % n);
+      s = fma(x, x, s);
+    }
+    return s;
+  }
   // elements before the first 16-byte boundary, whole vectors, the rest
   int head = (int)(((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / E::kBytes);
   if (head > n) head = n;
@@ -113,10 +142,10 @@ __global__ void __launch_bounds__(kClipThreads, 4)
   asm volatile("griddepcontrol.launch_dependents;");
   double s = 0.0;
   for (int64_t tile = blockIdx.x; tile < t.n_tiles; tile += gridDim.x) {
-    const ClipEntry &e = t.e[find_entry(t, tile)];
-    const ClipTile r = tile_range(e, tile);
-    s += e.dtype == FOPD_BF16 ? tile_squares<FOPD_BF16>(e.data + r.off * 2, r.n)
-                              : tile_squares<FOPD_F32>(e.data + r.off * 4, r.n);
+    const int i = find_entry(t, (uint32_t)tile);
+    const ClipEntry &e = t.e[i];
+    const ClipTile r = tile_range(t, i, (uint32_t)tile);
+    s += e.dtype == FOPD_BF16 ? tile_squares<FOPD_BF16>(e.data + r.off * 2, r) : tile_squares<FOPD_F32>(e.data + r.off * 4, r);
   }
   sh[threadIdx.x] = s;
   __syncthreads();
@@ -157,9 +186,17 @@ __device__ __forceinline__ float clip_coef(double sum, float max_norm) {
 }
 
 template <int DT>
-__device__ __forceinline__ void tile_scale(const char *p, char *o, int n, float c) {
+__device__ __forceinline__ void tile_scale(const char *p, char *o, const ClipTile &r, float c) {
   using E = Elem<DT>;
   constexpr int P = E::kPerVec;
+  const int n = r.n;
+  if (r.rows > 0) {
+    for (int i = threadIdx.x; i < r.rows * n; i += kClipThreads) {
+      const int64_t at = (i / n) * r.stride + i % n;
+      E::store1(o, at, E::load1(p, at) * c);
+    }
+    return;
+  }
   if (((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(o)) & 15) != 0) {  // no common vector boundary
     for (int i = threadIdx.x; i < n; i += kClipThreads) E::store1(o, i, E::load1(p, i) * c);
     return;
@@ -206,11 +243,12 @@ __global__ void __launch_bounds__(kClipThreads, 4)
   if (c == 1.f && t.in_place) return;
   // from the end: what the norm has read last may still be in the L2
   for (int64_t tile = t.n_tiles - 1 - blockIdx.x; tile >= 0; tile -= gridDim.x) {
-    const ClipEntry &e = t.e[find_entry(t, tile)];
+    const int i = find_entry(t, (uint32_t)tile);
+    const ClipEntry &e = t.e[i];
     if (c == 1.f && e.out == e.data) continue;
-    const ClipTile r = tile_range(e, tile);
-    if (e.dtype == FOPD_BF16) tile_scale<FOPD_BF16>(e.data + r.off * 2, e.out + r.off * 2, r.n, c);
-    else tile_scale<FOPD_F32>(e.data + r.off * 4, e.out + r.off * 4, r.n, c);
+    const ClipTile r = tile_range(t, i, (uint32_t)tile);
+    if (e.dtype == FOPD_BF16) tile_scale<FOPD_BF16>(e.data + r.off * 2, e.out + r.off * 2, r, c);
+    else tile_scale<FOPD_F32>(e.data + r.off * 4, e.out + r.off * 4, r, c);
   }
 }
 

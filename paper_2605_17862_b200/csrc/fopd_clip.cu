@@ -11,7 +11,7 @@ namespace {
 
 // Tensors of one launch: the table is a kernel parameter (at most 32,764 bytes), in sizes so that small sets are quick to
 // hand over.
-constexpr int kLargestTable = 580;
+constexpr int kLargestTable = 1000;
 
 int check_tensors(const fopd_tensor *t, int32_t n, const double *ws) {
   if (n < 0) return FOPD_ERR_SIZE;
@@ -84,28 +84,47 @@ int check_overlap(const fopd_tensor *t, int32_t n) {
   return FOPD_OK;
 }
 
-// Fills a launch's table from tensors [*next, n); empty ones are left out.
+// Fills a launch's table from tensors [*next, n) as far as they go; empty ones are left out.
 template <int N>
 void fill_table(const fopd_tensor *t, int32_t n, int32_t *next, ClipTable<N> *tab) {
   tab->n = 0;
   tab->n_tiles = 0;
   tab->in_place = 1;
-  for (; *next < n && tab->n < N; ++*next) {
+  for (; *next < n; ++*next) {
     const fopd_tensor &x = t[*next];
     if (x.rows == 0 || x.cols == 0) continue;
+    const bool dense = x.rows == 1 || x.row_stride == x.cols;
+    if (tab->n + (dense ? 1 : 2) > N || tab->n_tiles > (int64_t)1 << 30) return;  // (one tensor has at most 2^30 tiles)
     ClipEntry &e = tab->e[tab->n++];
-    const bool one_row = x.rows == 1 || x.row_stride == x.cols;
-    const int64_t rows = one_row ? 1 : x.rows;
+    const int esz = x.dtype == FOPD_BF16 ? 2 : 4, per = kClipTileBytes / esz;
     e.data = static_cast<const char *>(x.data);
     e.out = static_cast<char *>(x.out ? x.out : const_cast<void *>(x.data));
+    e.cols = dense ? x.rows * x.cols : x.cols;
+    e.tile0 = (uint32_t)tab->n_tiles;
+    e.dtype = (uint8_t)x.dtype;
+    e.pad = 0;
     if (e.out != e.data) tab->in_place = 0;
-    e.cols = one_row ? x.rows * x.cols : x.cols;
-    e.row_stride = one_row ? e.cols : x.row_stride;
-    e.tile0 = tab->n_tiles;
-    e.dtype = x.dtype;
-    const int64_t bytes = e.cols * (x.dtype == FOPD_BF16 ? 2 : 4);
-    e.tiles_per_row = (int32_t)((bytes + kClipTileBytes - 1) / kClipTileBytes);
-    tab->n_tiles += rows * e.tiles_per_row;
+    if (dense) {
+      e.kind = kClipDense;
+      tab->n_tiles += (e.cols + per - 1) / per;
+      continue;
+    }
+    ClipMore &m = reinterpret_cast<ClipMore &>(tab->e[tab->n++]);
+    m.rows = x.rows;
+    m.row_stride = x.row_stride;
+    m.tile0 = e.tile0;
+    m.kind = kClipMore;
+    m.dtype = e.dtype;
+    m.pad = 0;
+    if (x.cols * 8 <= per) {  // eight rows and more in a tile
+      e.kind = kClipShortRows;
+      m.per = per / x.cols;
+      tab->n_tiles += (x.rows + m.per - 1) / m.per;
+    } else {
+      e.kind = kClipRows;
+      m.per = (x.cols + per - 1) / per;
+      tab->n_tiles += x.rows * m.per;
+    }
   }
 }
 
@@ -166,22 +185,23 @@ int launch_scale(const fopd_tensor *t, int32_t n, const double *ws, float max_no
 template <int N>
 int launch_both(const fopd_tensor *t, int32_t n, double *ws, float max_norm, float *norm, float *coef, int32_t *status,
                 cudaStream_t st) {
-  if (n > N) {
-    const int rc = launch_norm<N>(t, n, ws, 1, nullptr, nullptr, st);
-    return rc != FOPD_OK ? rc : launch_scale<N>(t, n, ws, max_norm, norm, coef, status, st);
-  }
   ClipTable<N> tab;
   int32_t next = 0;
   fill_table<N>(t, n, &next, &tab);
-  const int rc = launch_norm_table<N>(tab, ws, 1, nullptr, nullptr, st);
-  return rc != FOPD_OK ? rc : launch_scale_table<N>(tab, ws, max_norm, norm, coef, status, st, true);
+  if (next == n) {  // all in one table
+    const int rc = launch_norm_table<N>(tab, ws, 1, nullptr, nullptr, st);
+    return rc != FOPD_OK ? rc : launch_scale_table<N>(tab, ws, max_norm, norm, coef, status, st, true);
+  }
+  const int rc = launch_norm<N>(t, n, ws, 1, nullptr, nullptr, st);
+  return rc != FOPD_OK ? rc : launch_scale<N>(t, n, ws, max_norm, norm, coef, status, st);
 }
 
-// The smallest table for n tensors.
+// The smallest table for n tensors (most of which are dense).
 #define FOPD_CLIP_TABLE(n, CALL)          \
   ((n) <= 16    ? CALL(16)                 \
-   : (n) <= 64  ? CALL(64)                 \
-   : (n) <= 192 ? CALL(192)                \
+   : (n) <= 48  ? CALL(48)                 \
+   : (n) <= 112 ? CALL(112)                \
+   : (n) <= 256 ? CALL(256)                \
                 : CALL(kLargestTable))
 
 int check_scale(const fopd_tensor *t, int32_t n, const double *ws, float max_norm) {

@@ -84,7 +84,7 @@ def test_mixed_set_pitches_orders_and_empty_tensors():
     assert torch.equal(deep[:, :, :10], keep_d[:, :, :10]) and torch.equal(deep[:, :, 133:], keep_d[:, :, 133:])
 
 
-@pytest.mark.parametrize("count", [63, 64, 65, 579, 580, 581, 1500])
+@pytest.mark.parametrize("count", [16, 17, 48, 112, 113, 257, 999, 1000, 1001, 2500])
 def test_many_tensors(count):
     rng = np.random.RandomState(count)
     shapes = [((int(rng.randint(1, 400)),), BF16 if rng.rand() < 0.5 else F32) for _ in range(count)]
@@ -92,6 +92,26 @@ def test_many_tensors(count):
     outs = [torch.empty(s, dtype=d, device=DEV) for s, d in shapes]
     check_clip(gradients(shapes, count + 1), 0.5, outs)
     check_clip(gradients(shapes, count + 1), 1e6, outs)  # a plain copy
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cols,pitch", [(5, 1, 3), (70_001, 1, 2), (1000, 7, 8), (333, 1023, 1024), (100, 1024, 1100),
+                                             (99, 2047, 2048), (7, 2049, 4000), (3, 20_000, 20_001), (2, 8192, 8200)])
+def test_rows_at_a_pitch(rows, cols, pitch, dtype):
+    """Short rows share a tile, long ones are cut; what lies between the rows stays."""
+    buf = gradients([((rows, pitch), dtype)], rows + cols)[0]
+    keep = buf.clone()
+    check_clip([buf[:, :cols]], 1e-3)
+    assert torch.equal(buf[:, cols:], keep[:, cols:])
+    out = torch.full_like(buf, 3.0)
+    many = [buf[:, :cols]] * 1 + gradients([((rows, cols), dtype)], 5)
+    check_clip(many, 1e-3, [out[:, :cols], torch.empty_like(many[1])])
+    assert (out[:, cols:] == 3).all()
+
+
+def test_many_tensors_with_rows():
+    base = [gradients([((37, 40), BF16 if k % 2 else F32)], k)[0] for k in range(700)]
+    assert check_clip([b[:, 3:33] for b in base], 0.1) < 1
 
 
 def test_no_tensors():
