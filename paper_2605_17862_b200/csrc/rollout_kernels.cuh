@@ -155,8 +155,9 @@ __device__ __forceinline__ void oldest_copy() { asm volatile("cp.async.wait_grou
 // ---- 2^y in fp64 ------------------------------------------------------------------------------------
 
 // For every element of a row that is decided in fp64: y rounded to sixteenths, 2^{j/16} from a table in shared memory
-// (sixteen entries lie in sixteen banks) and the Chebyshev fit of degree five to 2^f on |f| <= 1/32: error 5e-15.  The
-// high word of the table's entry j is less by j << 16, so that adding n << 16 for y = n / 16 makes it 2^{n/16}.
+// (sixteen entries lie in sixteen banks) and 1 + f g(f), g the Chebyshev fit of degree four to (2^f - 1) / f on
+// |f| <= 1/32: error 1e-14, and exactly 1 for the maximum, so that even rows are summed without rounding.  The high word
+// of the table's entry j is less by j << 16, so that adding n << 16 for y = n / 16 makes it 2^{n/16}.
 __constant__ double kSixteenths[16] = {
     1.0, 1.0442737824274138, 1.0905077326652577, 1.1387886347566916, 1.189207115002721, 1.241857812073484,
     1.2968395546510096, 1.3542555469368927, 1.4142135623730951, 1.4768261459394993, 1.5422108254079407,
@@ -179,12 +180,12 @@ __device__ __forceinline__ Weight64 weight64(float x, double m, double c, uint32
   const double t = fma(d, c, kRound);
   const double f = fma(d, c, kRound - t);
   const int n = __double2loint(t);
-  double p = 0.0013333781576784268;
-  p = fma(p, f, 0.009618354747407538);
-  p = fma(p, f, 0.0555041086566393);
-  p = fma(p, f, 0.24022650687646874);
-  p = fma(p, f, 0.6931471805599457);
-  p = fma(p, f, 1.0000000000000044);
+  double p = 0.0013333744338239965;
+  p = fma(p, f, 0.009618317140580765);
+  p = fma(p, f, 0.05550410866027587);
+  p = fma(p, f, 0.24022650691319414);
+  p = fma(p, f, 0.6931471805599453);
+  p = fma(p, f, 1.0);
   const double e = tab[n & 15];
   return {p, __hiloint2double(__double2hiint(e) + (n << 16), __double2loint(e))};
 }
