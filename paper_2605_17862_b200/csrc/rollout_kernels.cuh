@@ -55,6 +55,7 @@ struct LaterEntry {
   double z, v;
 };
 constexpr int32_t kUnset = 0x7f7f7f7f;  // what one memset leaves in all counters of a call
+__device__ __forceinline__ int32_t since_unset(int32_t x) { return (int32_t)((uint32_t)x - (uint32_t)kUnset); }
 struct Later {
   int32_t count, pad[7];  // count starts at kUnset
   LaterEntry e[1];  // as many as there are rows
@@ -749,11 +750,15 @@ __device__ __forceinline__ int32_t cluster_search(cg::cluster_group &cl, Weights
   int32_t token = kUnsure;
   const bool good = is_distribution(*total), mine = good && sh.owner == rank;
   if (mine) {
-    if (kRelative) {
+    const double bound = bound_rel * total->z + bound_abs;
+    double scale = 1.0;
+    if (kRelative) {  // the slots' sums are free of the rounding of max c; the elements' weights all carry it
       w.ts = *total;
       w.derive();
+      scale = exp64((double)fmaf(w.ts.m, w.ct, -w.mct), 1.0);
     }
-    token = cta_find<DT, kExact>(w, d, sh.slot, sh.before, sh.goal, bound_rel * total->z + bound_abs, sh);
+    if (!kRelative || !w.beyond())
+      token = cta_find<DT, kExact>(w, d, sh.slot, sh.before * scale, sh.goal * scale, bound * scale, sh);
   }
   *again = false;
   if (!kExact) {
@@ -892,8 +897,9 @@ __device__ __forceinline__ float log_prob(float logit, const RowSum &r, double c
 
 // ---- draws: a cluster per row -----------------------------------------------------------------------
 
-// In the two modes of a long grid a row that fp32 does not decide waits for the second launch, where eight CTAs share it:
-// one CTA needs 100 us for it in fp64, and a few of those would hold up the end of the grid.
+// With more rows than fit at once a row that fp32 does not decide waits for the second launch, where kDrawList CTAs share
+// it: one CTA alone takes tens of microseconds for it in fp64, and a few of those held up the end of the grid (278 us
+// against 240 for 4,096 rows of 151,936).
 template <int DT, bool kBest, int kMode>
 __global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) draw_kernel(const __grid_constant__ RolloutDev d) {
   __shared__ RollShared sh;
@@ -907,9 +913,9 @@ __global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) draw_ke
     __syncthreads();
   }
   if (kMode == kSecond) asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int32_t count = kMode == kSecond ? d.later->count - kUnset : d.B, step = (int32_t)(gridDim.x / size);
+  const int64_t count = kMode == kSecond ? since_unset(d.later->count) : d.B, step = gridDim.x / size;
   int parity = 0;
-  for (int32_t k = blockIdx.x / size; k < count; k += step) {
+  for (int64_t k = blockIdx.x / size; k < count; k += step) {
     const int64_t n = kMode == kSecond ? d.later->e[k].unit : k;
     const char *row = d.target + n * d.tseq;
     const double v = kBest ? 0.0 : kMode == kSecond ? d.later->e[k].v : d.uniform[n];
@@ -963,7 +969,7 @@ __global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) draw_ke
       if (is_distribution(total)) bits = FOPD_DEV_BAD_UNIFORM;
       if (again && good) {
         if (kMode == kFirst) {
-          if (rank == 0 && threadIdx.x == 0) d.later->e[atomicAdd(&d.later->count, 1) - kUnset] = {(int32_t)n, total.m, total.z, v};
+          if (rank == 0 && threadIdx.x == 0) d.later->e[since_unset(atomicAdd(&d.later->count, 1))] = {(int32_t)n, total.m, total.z, v};
           continue;
         }
         w.ts = total;
@@ -1069,13 +1075,13 @@ __device__ __forceinline__ void take_next(cg::cluster_group &cl, const RolloutDe
     for (int tries = 0; tries < 4; ++tries) {
       int32_t left = -1;  // the last position that may be wanted
       if (lane < d.B) left = min(drafts_of(d, at), *(volatile const int32_t *)(d.stop + at));
-      const bool some = lane < d.B && *(volatile const int32_t *)(d.next + at) - kUnset <= left;
+      const bool some = lane < d.B && since_unset(*(volatile const int32_t *)(d.next + at)) <= left;
       const unsigned has = __ballot_sync(0xffffffffu, some);
       if (!has) break;
       const int from = __ffs(has) - 1;
       int32_t j = -1;
       if (lane == from) {
-        j = atomicAdd(d.next + at, 1) - kUnset;
+        j = since_unset(atomicAdd(d.next + at, 1));
         if (j > left) j = -1;
       }
       take_j = __shfl_sync(0xffffffffu, j, from);
@@ -1228,7 +1234,7 @@ __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const Rol
     state = pos[j].state;
     if (kBest || state != kOpen) break;
     if (kMode == kFirst) {
-      if (rank == 0 && threadIdx.x == 0) d.later->e[atomicAdd(&d.later->count, 1) - kUnset].unit = b;
+      if (rank == 0 && threadIdx.x == 0) d.later->e[since_unset(atomicAdd(&d.later->count, 1))].unit = b;
       return;
     }
     const int32_t x = d.drafted[(int64_t)b * d.K + j];
@@ -1284,13 +1290,14 @@ __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const Rol
         if (w.rest) cta_sums<DT, false, true>(w, d, sl, sh);
         else cta_sums<DT, false, false>(w, d, sl, sh);
         // p - q: both rows' weights and both their sums are off; else the row's whole sum counts, with what was taken away
-        token = cluster_search<DT, false, false>(cl, w, d, sl, v, 0.0, w.rest ? 9 * d.eps : 2 * d.eps * t32.z, 0, sh,
+        // (and up to a twentieth for the rounding of max c, which these weights carry)
+        token = cluster_search<DT, false, false>(cl, w, d, sl, v, 0.0, w.rest ? 9 * d.eps : 2.1 * d.eps * t32.z, 0, sh,
                                                  &total, &again);
         if (!is_distribution(total)) again = true;
       }
       if (!again) break;
       if (kMode == kFirst) {
-        if (rank == 0 && threadIdx.x == 0) d.later->e[atomicAdd(&d.later->count, 1) - kUnset].unit = b;
+        if (rank == 0 && threadIdx.x == 0) d.later->e[since_unset(atomicAdd(&d.later->count, 1))].unit = b;
         return;
       }
       if (w.rest) {
@@ -1338,9 +1345,9 @@ __global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) verify_
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the sweep's positions are there, or the list
   const int size = (int)cl.num_blocks();
-  const int32_t count = kMode == kSecond ? d.later->count - kUnset : d.B, step = (int32_t)(gridDim.x / size);
-  for (int32_t k = blockIdx.x / size; k < count; k += step) {
-    finish_sequence<DT, kBest, kMode>(cl, d, kMode == kSecond ? d.later->e[k].unit : k, sh);
+  const int64_t count = kMode == kSecond ? since_unset(d.later->count) : d.B, step = gridDim.x / size;
+  for (int64_t k = blockIdx.x / size; k < count; k += step) {
+    finish_sequence<DT, kBest, kMode>(cl, d, kMode == kSecond ? d.later->e[k].unit : (int32_t)k, sh);
     if (k + step < count) roll_sync(cl);  // the next one writes what this one has read
   }
 }

@@ -472,6 +472,18 @@ def test_verify_forms_at_every_cut(form, T, B, K, V):
     assert all(np.array_equal(got[k], again[k]) for k in got)  # whatever order the clusters came in
 
 
+@pytest.mark.parametrize("n,V,dtype,offset", [(400, 3001, F32, 1.0e5), (400, 3001, F32, -2.0e5), (300, 9001, BF16, 900.0),
+                                              (40, 70001, F32, 7.0e4), (60, 3001, F32, 3.0e6)])
+def test_many_draws_from_logits_far_from_zero(n, V, dtype, offset):
+    """The rounding of max c grows with the logits' offset; sums and elements have to agree on it."""
+    x = rows_of((n,), V, dtype, n + V, scale=1.0)
+    x.add_(offset)
+    check_draw(x, uniforms(n, 351), 1.0)
+    target, draft = x.as_strided((n // 4, 2, V), (4 * x.stride(0), x.stride(0), 1)), x[2::4].unsqueeze(1)
+    check_verify(target, draft, drafts_from(draft, 1.0, 352), uniforms((n // 4, 2), 353))
+    check_verify(target, None, drafts_from(draft, 1.0, 354), uniforms((n // 4, 2), 355))
+
+
 def test_logits_far_from_zero_and_small_temperatures():
     for dtype, offset in ((BF16, 3000.0), (F32, -3.0e4), (F32, 2.0e8), (F32, -3.0e38)):
         x = rows_of((6,), 2500, dtype, 341)
