@@ -474,7 +474,7 @@ int fopd_shard_loss_fwd_bwd(const fopd_chunk *shard, int64_t vocab_offset, int64
  *   status    device int32 status word, or NULL
  */
 int fopd_draw_tokens(const void *logits, const double *uniform, int64_t n_rows, int64_t vocab,
-                     int64_t row_stride, int32_t dtype, float temperature, int32_t *tokens,
+                     int64_t row_stride, int32_t dtype, double temperature, int32_t *tokens,
                      float *logprob, int32_t *status, void *stream);
 
 /* Drafts of B sequences, up to K each, with the logits rows they are checked against. */
@@ -489,10 +489,10 @@ typedef struct {
   int64_t vocab;
   int64_t target_seq_stride, target_row_stride; /* in elements; row strides >= vocab                    */
   int64_t draft_seq_stride, draft_row_stride;
+  double temperature;     /* of the target's distribution p                                             */
+  double draft_temperature; /* of the draft's distribution q                                            */
   int32_t B, K;           /* B >= 0, 0 <= K < 2^20                                                      */
   int32_t dtype;          /* fopd_dtype of both                                                         */
-  float temperature;      /* of the target's distribution p                                             */
-  float draft_temperature; /* of the draft's distribution q                                             */
 } fopd_draft;
 
 /*

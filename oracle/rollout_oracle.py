@@ -23,7 +23,7 @@ def probabilities(row, temperature):
         p = np.zeros_like(row)
         p[int(np.argmax(row))] = 1.0
         return p
-    w = np.exp((row - row.max()) / float(np.float32(temperature)))
+    w = np.exp((row - row.max()) / float(temperature))
     return w / math.fsum(w)
 
 

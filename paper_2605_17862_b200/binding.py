@@ -59,8 +59,8 @@ class fopd_draft(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("target", "draft", "tokens", "n_draft", "uniform")] + \
         [(n, ctypes.c_int64) for n in ("vocab", "target_seq_stride", "target_row_stride", "draft_seq_stride",
                                        "draft_row_stride")] + \
-        [("B", ctypes.c_int32), ("K", ctypes.c_int32), ("dtype", ctypes.c_int32), ("temperature", ctypes.c_float),
-         ("draft_temperature", ctypes.c_float)]
+        [("temperature", ctypes.c_double), ("draft_temperature", ctypes.c_double), ("B", ctypes.c_int32),
+         ("K", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 class fopd_tensor(ctypes.Structure):
@@ -109,7 +109,7 @@ def lib() -> ctypes.CDLL:
         L.fopd_step_host.argtypes = [ctypes.POINTER(fopd_chunk), i32, i32, vp, vp, vp, fopd_params,
                                      ctypes.POINTER(ctypes.c_void_p), ctypes.POINTER(fopd_host_outputs), vp,
                                      ctypes.c_uint64, vp]
-        L.fopd_draw_tokens.argtypes = [vp, vp, i64, i64, i64, i32, f32, vp, vp, vp, vp]
+        L.fopd_draw_tokens.argtypes = [vp, vp, i64, i64, i64, i32, ctypes.c_double, vp, vp, vp, vp]
         L.fopd_verify_draft.argtypes = [ctypes.POINTER(fopd_draft), vp, vp, vp, vp, vp, vp]
         L.fopd_grad_norm.argtypes = [vp, i32, vp, vp, vp, vp]
         L.fopd_grad_scale.argtypes = [vp, i32, vp, f32, vp, vp, vp, vp]
@@ -389,8 +389,8 @@ def fopd_verify_draft(target, draft, draft_tokens, uniform, tokens, *, n_draft=N
         assert unit == 1 or cols <= 1
     assert vocab is None or 0 < vocab <= cols
     d = fopd_draft(target.data_ptr(), draft_at, draft_tokens.data_ptr(), _out(n_draft, torch.int32, B, dev),
-                   uniform.data_ptr(), vocab or cols, seq, row, dseq, drow, B, K, FOPD_BF16 if bf16 else FOPD_F32,
-                   temperature, draft_temperature)
+                   uniform.data_ptr(), vocab or cols, seq, row, dseq, drow, temperature, draft_temperature, B, K,
+                   FOPD_BF16 if bf16 else FOPD_F32)
     _check(lib().fopd_verify_draft(ctypes.byref(d), _out(tokens, torch.int32, B * W, dev),
                                    _out(logprob, torch.float32, B * W, dev), _out(mask, torch.uint8, B * W, dev),
                                    _out(n_accepted, torch.int32, B, dev), _status_word(status, dev), _stream(stream)),

@@ -6,7 +6,7 @@ using namespace fopd;
 
 namespace {
 
-bool temperature_ok(float t) { return t == 0.f || (t >= 1.f / 1024 && t <= 1024.f); }
+bool temperature_ok(double t) { return t == 0.0 || (t >= 1.0 / 1024 && t <= 1024.0); }
 
 // CTAs that share a row, a position or a sequence: as many as keep `units` clusters of them within `most` CTAs.
 int cluster_for(int64_t units, int most) {
@@ -173,10 +173,10 @@ int fopd_verify_draft(const fopd_draft *d, int32_t *tokens, float *logprob, uint
   r.n_accepted = n_accepted;
   r.status = status;
   // a target without temperature never asks for the draft's probabilities: x is accepted if it is the best token
-  const bool best = d->temperature == 0.f;
-  r.kind = best || d->K == 0 ? kDraftNone : !d->draft ? kDraftCertain : d->draft_temperature == 0.f ? kDraftBest : kDraftRows;
-  r.ct64 = best ? 0.0 : 1.4426950408889634074 / (double)d->temperature;
-  r.cd64 = r.kind == kDraftRows ? 1.4426950408889634074 / (double)d->draft_temperature : 0.0;
+  const bool best = d->temperature == 0.0;
+  r.kind = best || d->K == 0 ? kDraftNone : !d->draft ? kDraftCertain : d->draft_temperature == 0.0 ? kDraftBest : kDraftRows;
+  r.ct64 = best ? 0.0 : 1.4426950408889634074 / d->temperature;
+  r.cd64 = r.kind == kDraftRows ? 1.4426950408889634074 / d->draft_temperature : 0.0;
   r.ct = (float)r.ct64;
   r.cd = (float)r.cd64;
   if (!best) r.eps = sum_error(d->vocab, r.ct, r.ct64);
@@ -188,7 +188,7 @@ int fopd_verify_draft(const fopd_draft *d, int32_t *tokens, float *logprob, uint
 }
 
 int fopd_draw_tokens(const void *logits, const double *uniform, int64_t n_rows, int64_t vocab, int64_t row_stride,
-                     int32_t dtype, float temperature, int32_t *tokens, float *logprob, int32_t *status,
+                     int32_t dtype, double temperature, int32_t *tokens, float *logprob, int32_t *status,
                      void *stream) {
   if (dtype != FOPD_BF16 && dtype != FOPD_F32) return FOPD_ERR_DTYPE;
   if (n_rows < 0 || n_rows > INT32_MAX || vocab <= 0 || row_stride < vocab) return FOPD_ERR_SIZE;

@@ -472,6 +472,21 @@ def test_verify_forms_at_every_cut(form, T, B, K, V):
     assert all(np.array_equal(got[k], again[k]) for k in got)  # whatever order the clusters came in
 
 
+@pytest.mark.parametrize("V,dtype,scale,T", [(32000, BF16, 3.0, 1.0), (32003, F32, 1.0, 0.3), (9001, BF16, 0.05, 0.7), (50001, F32, 5.0, 1.7)])
+def test_thousands_of_draws_against_torch_in_64_bits(V, dtype, scale, T):
+    n = 6000
+    x, u = rows_of((n,), V, dtype, V, scale=scale), uniforms(n, V + 1)
+    tokens, lp, bits = run_draw(x, u, T)
+    assert bits == 0
+    for at in range(0, n, 1000):
+        y = x[at:at + 1000].double() / T
+        c = torch.softmax(y, -1).cumsum(-1)
+        want = torch.searchsorted(c, (u[at:at + 1000] * c[:, -1]).unsqueeze(1), right=True).squeeze(1)
+        assert torch.equal(tokens[at:at + 1000].long(), want)
+        wl = (y.gather(1, want.unsqueeze(1)).squeeze(1) - y.logsumexp(-1)).cpu().numpy()
+        assert np.all(np.abs(lp[at:at + 1000].cpu().numpy() - wl) <= lp_tol(wl))
+
+
 @pytest.mark.parametrize("n,V,dtype,offset", [(400, 3001, F32, 1.0e5), (400, 3001, F32, -2.0e5), (300, 9001, BF16, 900.0),
                                               (40, 70001, F32, 7.0e4), (60, 3001, F32, 3.0e6)])
 def test_many_draws_from_logits_far_from_zero(n, V, dtype, offset):
