@@ -556,6 +556,15 @@ __device__ __forceinline__ void roll_sync(cg::cluster_group &cl) {
   else __syncthreads();
 }
 
+// A CTA's shared memory may be written by another one once it runs: each says so as it starts, and all wait for the
+// others before the first such write, where that is hidden behind loads (starting late costs nothing then).
+__device__ __forceinline__ void say_started(cg::cluster_group &cl) {
+  if (cl.num_blocks() > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
+}
+__device__ __forceinline__ void all_started(cg::cluster_group &cl) {
+  if (cl.num_blocks() > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+
 struct ExactSums {
   double t, q;  // of a target's row and of a draft's
 };
@@ -907,12 +916,16 @@ __global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) draw_ke
   const int rank = (int)cl.block_rank(), size = (int)cl.num_blocks();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const Slots sl = my_slots(d, rank, size);
+  say_started(cl);
   asm volatile("griddepcontrol.launch_dependents;");
   if (kMode != kFirst) {
     fill_exp64(sh.tab);
     __syncthreads();
   }
-  if (kMode == kSecond) asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (kMode == kSecond) {
+    all_started(cl);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+  }
   const int64_t count = kMode == kSecond ? since_unset(d.later->count) : d.B, step = gridDim.x / size;
   int parity = 0;
   for (int64_t k = blockIdx.x / size; k < count; k += step) {
@@ -931,6 +944,7 @@ __global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) draw_ke
                          }
                          r = nothing();
                        });
+    if (kMode != kSecond) all_started(cl);  // (one row to a cluster)
     int32_t token = kUnsure;
     float lp = 0.f;
     bool good;
@@ -1119,6 +1133,7 @@ __device__ __forceinline__ void sweep_position(cg::cluster_group &cl, const Roll
   };
 #pragma unroll
   for (int k = 0; k < kStages; ++k) ask(ring + k * kPartVecs);
+  if (!d.stop) all_started(cl);  // (with d.stop they have met before)
   Draft draft = {};
   if (rank == 0 && threadIdx.x == 0) draft = draft_of<DT>(d, b, j, n, trow, qrow);
   RowSum t = nothing(), q = nothing();  // (q holds the row being swept, then the draft's)
@@ -1190,11 +1205,14 @@ __global__ void __launch_bounds__(kRollThreads, 4) verify_sweep_kernel(const __g
   __shared__ RollShared sh;
   asm volatile("griddepcontrol.launch_dependents;");  // the finish may be set up beside the last positions
   cg::cluster_group cl = cg::this_cluster();
+  say_started(cl);
   const int64_t id = blockIdx.x / cl.num_blocks();
   int32_t b = (int32_t)(id % d.B);
+  if (d.stop) all_started(cl);  // (else hidden in the sweep)
   if (!d.next) {
     const int32_t j = (int32_t)(id / d.B);
     if (wanted(cl, d, b, j, sh)) sweep_position<DT, kBest>(cl, d, b, j, sh);
+    else if (!d.stop) all_started(cl);
     return;
   }
   for (;;) {
@@ -1341,8 +1359,10 @@ template <int DT, bool kBest, int kMode>
 __global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) verify_finish_kernel(const __grid_constant__ RolloutDev d) {
   __shared__ RollShared sh;
   cg::cluster_group cl = cg::this_cluster();
+  say_started(cl);
   if (!kBest && kMode != kFirst) fill_exp64(sh.tab);
   asm volatile("griddepcontrol.launch_dependents;");
+  all_started(cl);
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the sweep's positions are there, or the list
   const int size = (int)cl.num_blocks();
   const int64_t count = kMode == kSecond ? since_unset(d.later->count) : d.B, step = gridDim.x / size;

@@ -472,6 +472,30 @@ def test_verify_forms_at_every_cut(form, T, B, K, V):
     assert all(np.array_equal(got[k], again[k]) for k in got)  # whatever order the clusters came in
 
 
+@pytest.mark.parametrize("T", [1.0, 0.0])
+def test_small_clusters_that_start_while_the_gpu_is_full(T):
+    """Rows so short that most CTAs of a cluster have nothing to read and exchange their sums as soon as they run, beside
+    work on another stream that takes the places where the others are to start."""
+    V, B, K, R = 5, 4, 2, 40
+    x, u = rows_of((6,), V, F32, 341), uniforms(6, 342)
+    target, draft = rows_of((B, K + 1), V, BF16, 343), rows_of((B, K), V, BF16, 344)
+    drafted, uv = drafts_from(draft, 1.0, 345), uniforms((B, K + 1), 346)
+    want, want_v = check_draw(x, u, T), check_verify(target, draft, drafted, uv, T=T)["tokens"]
+    tokens = torch.zeros((R, 6), dtype=torch.int32, device=DEV)
+    out = torch.zeros((R, B, K + 1), dtype=torch.int32, device=DEV)
+    a = torch.randn(4096, 4096, device=DEV, dtype=BF16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for r in range(R):
+        a @ a
+        with torch.cuda.stream(side):
+            fb.fopd_draw_tokens(x, u, tokens[r], temperature=T)
+            fb.fopd_verify_draft(target, draft, drafted, uv, out[r], temperature=T)
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, want) for t in tokens)
+    assert all(np.array_equal(t, want_v) for t in out.cpu().numpy())
+
+
 @pytest.mark.parametrize("V,dtype,scale,T", [(32000, BF16, 3.0, 1.0), (32003, F32, 1.0, 0.3), (9001, BF16, 0.05, 0.7), (50001, F32, 5.0, 1.7)])
 def test_thousands_of_draws_against_torch_in_64_bits(V, dtype, scale, T):
     n = 6000
