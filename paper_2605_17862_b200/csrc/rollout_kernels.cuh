@@ -1299,6 +1299,7 @@ __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const Rol
     w.cd64 = d.cd64;
     w.tab = sh.tab;
     RowSum total;
+    int turn = 0;  // two searches in a row exchange in different places: what one has left may still be read in the next
     for (int round = 0; round < 2; ++round) {  // the second one only where p - q is zero everywhere
       bool again = true;
       w.ts = t32;
@@ -1309,8 +1310,9 @@ __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const Rol
         else cta_sums<DT, false, false>(w, d, sl, sh);
         // p - q: both rows' weights and both their sums are off; else the row's whole sum counts, with what was taken away
         // (and up to a twentieth for the rounding of max c, which these weights carry)
-        token = cluster_search<DT, false, false>(cl, w, d, sl, v, 0.0, w.rest ? 9 * d.eps : 2.1 * d.eps * t32.z, 0, sh,
+        token = cluster_search<DT, false, false>(cl, w, d, sl, v, 0.0, w.rest ? 9 * d.eps : 2.1 * d.eps * t32.z, turn, sh,
                                                  &total, &again);
+        turn ^= 1;
         if (!is_distribution(total)) again = true;
       }
       if (!again) break;
@@ -1328,7 +1330,8 @@ __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const Rol
         cta_sums<DT, true, false>(w, d, sl, sh);
       }
       bool never;
-      token = cluster_search<DT, true, false>(cl, w, d, sl, v, 0.0, 0.0, 1, sh, &total, &never);
+      token = cluster_search<DT, true, false>(cl, w, d, sl, v, 0.0, 0.0, turn, sh, &total, &never);
+      turn ^= 1;
       if (is_distribution(total)) break;
       w.rest = false;
       w.without = -1;

@@ -472,6 +472,23 @@ def test_verify_forms_at_every_cut(form, T, B, K, V):
     assert all(np.array_equal(got[k], again[k]) for k in got)  # whatever order the clusters came in
 
 
+@pytest.mark.parametrize("B,V,offset", [(400, 2600, 0.0), (400, 9, 0.0), (20, 2600, 3.0e6)])
+def test_verify_many_sequences_without_a_residual(B, V, offset):
+    """A drafted token that neither row can give, and equal rows: p - q is zero everywhere and one fp64 search comes right
+    behind another (in the second launch, and in the whole kernel where logits are out of the reach of fp32)."""
+    target = rows_of((B, 2), V, F32, 347)
+    target += offset
+    target[:, 0, V - 1] = -math.inf
+    draft = rows_of((B, 1), V, F32, 348)
+    draft[:] = target[:, :1]
+    drafted, u = torch.full((B, 1), V - 1, dtype=torch.int32, device=DEV), uniforms((B, 2), 349)
+    got = check_verify(target, draft, drafted, u)
+    assert got["n_accepted"].max() == 0
+    for _ in range(30):
+        again, bits = run_verify(target, draft, drafted, u)
+        assert bits == 0 and all(np.array_equal(got[k], again[k]) for k in got)
+
+
 @pytest.mark.parametrize("T", [1.0, 0.0])
 def test_small_clusters_that_start_while_the_gpu_is_full(T):
     """Rows so short that most CTAs of a cluster have nothing to read and exchange their sums as soon as they run, beside
