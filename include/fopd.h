@@ -107,7 +107,7 @@ typedef enum {
   FOPD_ERR_DTYPE = -4,  /* dtype is neither FOPD_BF16 nor FOPD_F32              */
   FOPD_ERR_PARAM = -5,  /* alpha/beta negative or a parameter not finite        */
   FOPD_ERR_CUDA = -6,   /* a CUDA runtime call failed (launch, allocation)      */
-  FOPD_ERR_ALIAS = -7,  /* dlogits overlaps student or teacher                  */
+  FOPD_ERR_ALIAS = -7,  /* dlogits overlaps student or teacher, an output an input */
   FOPD_ERR_DEVICE = -8, /* fopd_check_status: the device status word is non-zero */
   FOPD_ERR_KIND = -9    /* loss_kind unknown, or not supported by this entry point */
 } fopd_status;
@@ -467,6 +467,7 @@ int fopd_shard_loss_fwd_bwd(const fopd_chunk *shard, int64_t vocab_offset, int64
 /*
  * Draws one token from each row: tokens[n] = min { i : sum_{k <= i} p_k > uniform[n] }, the inverse of
  * the distribution function, and logprob[n] = log p_{tokens[n]}.
+ * Neither may lie on uniform (FOPD_ERR_ALIAS) or on the logits.
  *
  *   logits    [n_rows, vocab] at a pitch of row_stride elements, layout rules of fopd_chunk
  *   uniform   [n_rows] fp64
@@ -513,6 +514,7 @@ typedef struct {
  * FOPD_DEV_BAD_LENGTH and is taken as the nearer bound.  Only what is reached counts: rows behind the
  * first rejection may hold anything.  Long drafts (a whole response) cost the rows that are reached and
  * those in flight when the rejection is found.  With K = 0 draft, tokens and n_draft are not used.
+ * No output may lie on the drafted tokens, n_draft or uniform (FOPD_ERR_ALIAS), nor on the logits.
  */
 int fopd_verify_draft(const fopd_draft *d /* HOST */, int32_t *tokens, float *logprob, uint8_t *mask,
                       int32_t *n_accepted, int32_t *status, void *stream);

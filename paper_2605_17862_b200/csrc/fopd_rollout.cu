@@ -128,6 +128,24 @@ int launch_verify(RolloutDev d, cudaStream_t st) {
   return rc;
 }
 
+struct Span {
+  const void *p;
+  int64_t bytes;
+};
+// Whether an output lies on tokens, counts or numbers that are read: CTAs read these while others write those.
+bool outputs_meet_inputs(const fopd_draft *d, const int32_t *tokens, const float *logprob, const uint8_t *mask,
+                         const int32_t *n_accepted) {
+  const int64_t B = d->B, W = (int64_t)d->K + 1;
+  const Span in[] = {{d->uniform, B * W * 8}, {d->K > 0 ? d->tokens : nullptr, B * d->K * 4}, {d->K > 0 ? d->n_draft : nullptr, B * 4}};
+  const Span out[] = {{tokens, B * W * 4}, {logprob, B * W * 4}, {mask, B * W}, {n_accepted, B * 4}};
+  for (const Span &i : in)
+    for (const Span &o : out) {
+      const uintptr_t a = (uintptr_t)i.p, b = (uintptr_t)o.p;
+      if (a && b && a < b + (uintptr_t)o.bytes && b < a + (uintptr_t)i.bytes) return true;
+    }
+  return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -154,6 +172,7 @@ int fopd_verify_draft(const fopd_draft *d, int32_t *tokens, float *logprob, uint
   if (rows && (!aligned16(d->draft) || (d->K > 1 && (d->draft_row_stride * esz) % 16 != 0) ||
                (d->B > 1 && (d->draft_seq_stride * esz) % 16 != 0)))
     return FOPD_ERR_ALIGN;
+  if (outputs_meet_inputs(d, tokens, logprob, mask, n_accepted)) return FOPD_ERR_ALIAS;
   RolloutDev r = {};
   r.target = static_cast<const char *>(d->target);
   r.draft = static_cast<const char *>(d->draft);

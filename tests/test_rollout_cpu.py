@@ -118,6 +118,26 @@ def test_verify_checks_its_arguments_on_the_host(lib, kw, code):
     assert lib.fopd_verify_draft(ctypes.byref(d), vp(0x50000), None, None, None, None, None) == code
 
 
+@pytest.mark.parametrize("kw,outs,code", [
+    (dict(tokens=0x50000), {}, -7),                                  # tokens onto the drafted ones
+    (dict(tokens=0x50000 + 39), {}, -7), (dict(tokens=0x50000 - 31), {}, -7),
+    (dict(uniform=0x50000 + 39), {}, -7), (dict(n_draft=0x50000 - 7), {}, -7),
+    (dict(), dict(logprob=0x40000 + 79), -7), (dict(), dict(mask=0x30000 - 9), -7),
+    (dict(n_draft=0x60000), dict(n_accepted=0x60000), -7), (dict(n_draft=0x60000), dict(n_accepted=0x60000 + 7), -7),
+    (dict(K=0, uniform=0x50000), {}, -7), (dict(B=0, tokens=0x50000), {}, 0),
+])
+def test_outputs_on_inputs_are_refused(lib, kw, outs, code):
+    d = _draft(**kw)
+    out = [vp(outs[k]) if k in outs else None for k in ("logprob", "mask", "n_accepted")]
+    assert lib.fopd_verify_draft(ctypes.byref(d), vp(0x50000), *out, None, None) == code
+
+
+def test_draws_onto_their_numbers_are_refused(lib):
+    f = lib.fopd_draw_tokens
+    assert f(vp(0x10000), vp(0x40000), 2, 64, 64, 0, 1.0, vp(0x40000 + 15), None, None, None) == -7
+    assert f(vp(0x10000), vp(0x40000), 2, 64, 64, 0, 1.0, vp(0x50000), vp(0x40000 - 7), None, None) == -7
+
+
 def test_draw_and_null_arguments(lib):
     f = lib.fopd_draw_tokens
     ok = [vp(0x10000), vp(0x40000), 2, 64, 64, 0, 1.0, vp(0x50000), None, None, None]
