@@ -711,7 +711,8 @@ __device__ __forceinline__ int32_t cluster_search(cg::cluster_group &cl, Weights
     const double incl = warp_scan(s);
     own.z = __shfl_sync(0xffffffffu, incl, 31);
     RowSum all = own;
-    double goal = v * own.z, before = 0.0, scale = 1.0;
+    // (rounded down: a sum in fp64 is above that exactly if it is above v times the total)
+    double goal = __dmul_rd(v, own.z), before = 0.0, scale = 1.0;
     int owner = 0;
     if (size > 1) {
       if (lane < size) *cl.map_shared_rank(&sh.pub[parity][rank], lane) = own;
@@ -720,7 +721,7 @@ __device__ __forceinline__ int32_t cluster_search(cg::cluster_group &cl, Weights
       all.m = warp_max(mine.m);
       const double part = part_of(mine, all.m, d.ct64), run = warp_scan(part);
       all.z = __shfl_sync(0xffffffffu, run, 31);
-      goal = v * all.z;
+      goal = __dmul_rd(v, all.z);
       const unsigned pass = __ballot_sync(0xffffffffu, part > kNothing && run > goal),
                      has = __ballot_sync(0xffffffffu, part > kNothing);
       owner = pass ? __ffs(pass) - 1 : has ? 31 - __clz(has) : 0;

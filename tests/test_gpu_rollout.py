@@ -609,3 +609,26 @@ def test_draw_verify_loss_and_clip_in_one_run(dtype, T):
     assert np.all(np.abs(got - scaled[0]) <= np.abs(scaled[0]) * (step * 1.001 + 2.0 ** -22) + 1e-38)
     _, again = run(None)
     assert torch.equal(again, plain)  # without clipping a step is what it was
+
+
+# ---- numbers on and next to a boundary ----
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("V,n", [(7, 1), (9000, 1), (9000, 60), (70001, 1), (1531, 700)])
+def test_draw_even_rows_by_neighbours_of_a_boundary(V, n, dtype):
+    """Even rows have whole sums, so that the token of a number v is floor(v V) to the last bit of v: with V beyond a power
+    of two, v V rounds to a boundary from below it, too."""
+    from fractions import Fraction
+
+    x = rows_of((n,), V, dtype, 8)
+    x.fill_(-1.5)
+    k = np.random.RandomState(9).permutation(V - 1)[:200] + 1
+    v = np.concatenate([f(k / V) for f in (lambda y: y, lambda y: np.nextafter(y, 0), lambda y: np.nextafter(y, 1))])
+    want = [math.floor(Fraction(float(y)) * V) for y in v]
+    assert any(y * V == i + 1 for y, i in zip(v, want))  # numbers whose product rounds up to the next boundary
+    if n == 1:
+        got = [run_draw(x, torch.tensor([y], device=DEV), 1.0)[0].tolist()[0] for y in v]
+    else:
+        v, want = np.resize(v, -(-len(v) // n) * n), np.resize(want, -(-len(v) // n) * n).tolist()
+        got = sum((run_draw(x, torch.tensor(v[i:i + n], device=DEV), 1.0)[0].tolist() for i in range(0, len(v), n)), [])
+    assert got == want
