@@ -1260,10 +1260,11 @@ __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const Rol
     const char *trow = d.target + b * d.tseq + j * d.trow, *qrow = d.draft + b * d.dseq + j * d.drow;
     const bool rows = d.kind == kDraftRows;
     const ExactSums z = cluster_exact_sums<DT>(cl, trow, pos[j].t.m, rows ? qrow : nullptr, pos[j].q.m, d, sl, parity, sh);
-    const double p = exp64((double)E::load1(trow, x) - pos[j].t.m, d.ct64) / z.t;
-    // (kDraftBest: q is 1, or 0 and then never open)
-    const double q = rows ? exp64((double)E::load1(qrow, x) - pos[j].q.m, d.cd64) / z.q : 1.0;
-    if (!(d.uniform[(int64_t)b * W + j] * q < p)) {
+    // u q < p with both sums on the other side: where the weights and sums are exact (even rows), so is this, since
+    // a product rounded down is below a number exactly if the product is.  (kDraftBest: q is 1, or 0 and then never open)
+    const double wp = exp64((double)E::load1(trow, x) - pos[j].t.m, d.ct64);
+    const double wq = rows ? exp64((double)E::load1(qrow, x) - pos[j].q.m, d.cd64) : 1.0;
+    if (!(__dmul_rd(d.uniform[(int64_t)b * W + j], wq * z.t) < wp * (rows ? z.q : 1.0))) {
       state = kReject;
       break;
     }

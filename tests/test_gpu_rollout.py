@@ -632,3 +632,33 @@ def test_draw_even_rows_by_neighbours_of_a_boundary(V, n, dtype):
         v, want = np.resize(v, -(-len(v) // n) * n), np.resize(want, -(-len(v) // n) * n).tolist()
         got = sum((run_draw(x, torch.tensor(v[i:i + n], device=DEV), 1.0)[0].tolist() for i in range(0, len(v), n)), [])
     assert got == want
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("form", ["rows", "certain"])
+@pytest.mark.parametrize("B", [1, 40, 900])
+def test_verify_even_rows_by_neighbours_of_equality(B, form, dtype):
+    """Even rows of a target with a tokens and of a draft with fewer, b: a draft is accepted while u a < b, to the last
+    bit of u (b = 1 where it was certain)."""
+    from fractions import Fraction
+
+    V, rng = 6007, np.random.RandomState(10)
+    target, draft = rows_of((B, 2), V, dtype, 11), rows_of((B, 1), V, dtype, 12)
+    calls = 60 if B == 1 else 1
+    wrong = 0
+    for call in range(calls):
+        a = rng.randint(2, V + 1, B)
+        b = np.array([rng.randint(1, x) for x in a]) if form == "rows" else np.ones(B, dtype=int)
+        column = torch.arange(V, device=DEV)
+        even = lambda n: torch.where(column < torch.tensor(n, device=DEV).unsqueeze(1), 0.25, -math.inf).to(dtype)
+        target[:, 0], draft[:, 0] = even(a), even(b)
+        u = uniforms((B, 2), 13 + call)
+        at = b / a
+        first = np.stack([at, np.nextafter(at, 0), np.nextafter(at, 1)])[(np.arange(B) + call) % 3, np.arange(B)]
+        u[:, 0] = torch.tensor(first)
+        drafted = torch.zeros((B, 1), dtype=torch.int32, device=DEV)
+        got, bits = run_verify(target, draft if form == "rows" else None, drafted, u)
+        want = [int(Fraction(float(y)) * int(n) < int(m)) for y, n, m in zip(first, a, b)]
+        wrong += sum(int(y * (1 / m) < 1 / n) != w for y, n, m, w in zip(first, a, b, want))
+        assert bits == 0 and got["n_accepted"].tolist() == want
+    assert wrong > 0  # some of which two rounded probabilities would decide otherwise
