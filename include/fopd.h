@@ -459,7 +459,9 @@ int fopd_shard_loss_fwd_bwd(const fopd_chunk *shard, int64_t vocab_offset, int64
  * distribution that has everything on the lowest index of the largest logit.  Logits may be -infinity
  * (banned tokens: probability 0); the columns behind `vocab` in a row are not read.  Tokens are those of
  * exact arithmetic: the sweeps run in fp32 with a bound on their error, and whatever the bound does not
- * decide is decided again in fp64 (error ~1e-13 of a row's sum).  A row that is needed and holds NaN or
+ * decide is decided again in fp64 (error ~1e-13 of a row's sum).  There a weight below 2^-900 of its row's
+ * largest counts as zero: such a token comes out of no draw, and a draw from max(p - q, 0) takes p_j instead
+ * where all that is left is that small.  A row that is needed and holds NaN or
  * +infinity, or nothing but -infinity, sets FOPD_DEV_BAD_LOGITS, a number outside [0, 1) that is needed
  * FOPD_DEV_BAD_UNIFORM; that row's (sequence's) token is then -1 with log-prob 0 and mask 0.
  */

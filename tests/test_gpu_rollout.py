@@ -662,3 +662,104 @@ def test_verify_even_rows_by_neighbours_of_equality(B, form, dtype):
         wrong += sum(int(y * (1 / m) < 1 / n) != w for y, n, m, w in zip(first, a, b, want))
         assert bits == 0 and got["n_accepted"].tolist() == want
     assert wrong > 0  # some of which two rounded probabilities would decide otherwise
+
+
+# ---- weights at the cut: below 2^-900 of their row's largest they are zero ----
+
+GAPS = (890.0, 896.0, 899.0, 901.0, 905.0, 908.0, 912.0, 1000.0, 1100.0)  # bits below the largest
+
+
+def at_the_cut(x, T):
+    """Rows as the definition sees them: what lies below the cut is banned.  None of the tests' logits lies on the cut
+    itself (exponents are rounded to sixteenths there)."""
+    y = x.double()
+    bits = (y.amax(-1, keepdim=True) - y) / T / math.log(2)
+    assert not bool(((bits > 899.9) & (bits < 900.1)).any())
+    return torch.where(bits > 900.0, torch.full_like(x, -math.inf), x)
+
+
+def below(gap, T, dtype):
+    """A logit `gap` bits below 0, as far as the type has it."""
+    return float(torch.tensor(-gap * T * math.log(2), dtype=torch.float64).to(dtype))
+
+
+@pytest.mark.parametrize("dtype,T", [(BF16, 1.0), (F32, 0.01)])
+@pytest.mark.parametrize("V", [9001, 151936])
+def test_draws_where_only_tiny_weights_pass(V, dtype, T):
+    """A run of columns far below the rest and numbers that pass as soon as there is a weight: each alone among fewer
+    elements and more, in calls of one row (eight CTAs), of some (two launches) and of many (a CTA to a row)."""
+    heads = (1, 9, 300, V // 8, V - 1)
+    x = rows_of((2 * len(GAPS) * len(heads),), V, dtype, 1)
+    x.fill_(0.0)
+    for i in range(len(x)):
+        x[i, :heads[i // 2 % len(heads)]] = below(GAPS[i // 2 // len(heads)], T, dtype)
+    u = torch.zeros(len(x), dtype=torch.float64, device=DEV)
+    u[1::2] = 0.3
+    want = [ro.draw(r, float(v), T) for r, v in zip(at_the_cut(x, T).cpu(), u.cpu())]
+    wt, wl = [w[0] for w in want], np.array([w[1] for w in want])
+    assert len(set(wt[::2])) > 4  # the first column, and those behind the heads
+    tokens, lp, bits = run_draw(x, u, T)
+    assert tokens.tolist() == wt and bits == 0
+    assert np.all(np.abs(lp.cpu().numpy() - wl) <= lp_tol(wl))
+    for i in range(len(x)):
+        tokens, lp, bits = run_draw(x[i:i + 1], u[i:i + 1], T)
+        assert tokens.tolist() == wt[i:i + 1] and bits == 0 and abs(float(lp) - wl[i]) <= lp_tol(wl[i])
+    if V < 100000:
+        whole = x.as_strided((len(x), x.stride(0)), (x.stride(0), 1))
+        tokens, lp, bits = run_draw(whole.repeat(8, 1)[:, :V], u.repeat(8), T)
+        assert tokens.tolist() == wt * 8 and bits == 0
+
+
+@pytest.mark.parametrize("B", [1, 60, 700])
+@pytest.mark.parametrize("bad", [False, True])
+@pytest.mark.parametrize("dtype,T", [(BF16, 0.1), (F32, 1.0)])
+def test_residual_of_a_greedy_draft_at_the_cut(dtype, T, bad, B):
+    """The target is nearly certain of the draft's best token and the drafted one is banned (or no token): what is left
+    has the whole of its weight around the cut, in a few columns or in all."""
+    V = 9001
+    target, draft = rows_of((B, 2), V, dtype, 2), rows_of((B, 1), V, dtype, 3, scale=0.1)
+    drafted = torch.full((B, 1), V + 3 if bad else 5, dtype=torch.int32, device=DEV)
+    for b in range(B):
+        few = b // len(GAPS) % 3
+        target[b, 0] = below(GAPS[b % len(GAPS)], T, dtype) if few == 0 else -math.inf
+        if few == 1:
+            target[b, 0, 7000:7009] = below(GAPS[b % len(GAPS)], T, dtype)
+        if few == 2:
+            target[b, 0, 4100] = below(GAPS[b % len(GAPS)], T, dtype)
+        target[b, 0, 5] = -math.inf
+        target[b, 0, 77], draft[b, 0, 77] = 0.0, 9.0
+    u = uniforms((B, 2), 4)
+    u[::2, 1] = 0.0
+    got, bits = run_verify(target, draft, drafted, u, T=T, Td=0.0)
+    cut = at_the_cut(target, T).cpu()
+    for b in range(min(B, 3 * len(GAPS) * 2)):
+        out, lps, acc, why, was_bad = ro.verify(cut[b], draft[b].cpu(), drafted[b].cpu().numpy(), 1, u[b].cpu().numpy(), T, 0.0)
+        assert why == "" and acc == 0 and was_bad == bad
+        assert got["tokens"][b].tolist() == [out[0], -1] and got["mask"][b].tolist() == [1, 0] and got["n_accepted"][b] == 0
+        assert abs(got["logprob"][b, 0] - lps[0]) <= lp_tol(lps[0])
+    assert (got["mask"] == [1, 0]).all() and (got["tokens"][:, 0] >= 0).all() and (got["tokens"][:, 1] == -1).all()
+    assert bits == (1 if bad else 0)
+
+
+@pytest.mark.parametrize("B", [1, 60, 700])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_residual_of_rows_that_differ_at_the_cut(dtype, B):
+    """p and q are equal but for one element with a tiny p and no q; the drafted token is banned in both."""
+    V = 5003
+    target, draft = rows_of((B, 2), V, dtype, 5, scale=0.5), rows_of((B, 1), V, dtype, 6)
+    target[:, 0, 3] = -math.inf
+    target[:, 0, 9] = 4.0
+    draft.copy_(target[:, :1])
+    draft[:, 0, 4444] = -math.inf
+    for b in range(B):
+        target[b, 0, 4444] = float(torch.tensor(4.0 + below(GAPS[b % len(GAPS)], 1.0, F32), dtype=torch.float64).to(dtype))
+    u = uniforms((B, 2), 7)
+    drafted = torch.full((B, 1), 3, dtype=torch.int32, device=DEV)
+    got, bits = run_verify(target, draft, drafted, u)
+    assert bits == 0 and (got["mask"] == [1, 0]).all()
+    cut, seen = at_the_cut(target, 1.0).cpu(), set()
+    for b in range(min(B, 60)):
+        out, lps, acc, _, _ = ro.verify(cut[b], draft[b].cpu(), [3], 1, u[b].cpu().numpy(), 1.0, 1.0)
+        assert got["tokens"][b].tolist() == [out[0], -1] and abs(got["logprob"][b, 0] - lps[0]) <= lp_tol(lps[0])
+        seen.add(out[0] == 4444)
+    assert len(seen) == min(B, 2)
