@@ -552,7 +552,9 @@ int fopd_grad_norm(const fopd_tensor *tensors /* HOST */, int32_t n_tensors, dou
 /* out = coef data with coef from ws[0] and max_norm (finite, > 0); coef[0], norm[0] fp32 or NULL.  With coef = 1
  * in place nothing is read or written.  If the norm is infinite or NaN, FOPD_DEV_NONFINITE is set, coef is 1 and
  * the values are left (or copied) as they are.  Elements of two tensors of the set must not overlap, nor those of
- * an `out` and another tensor's data (FOPD_ERR_ALIAS where address ranges show it). */
+ * an `out` and another tensor's data: FOPD_ERR_ALIAS where their address ranges do, unless they are columns or
+ * rows of one wider matrix, that is at least one has rows at a pitch, and the greatest common divisor of the pitches
+ * (the one pitch, where the other tensor has no gaps) keeps their columns apart. */
 int fopd_grad_scale(const fopd_tensor *tensors /* HOST */, int32_t n_tensors, double *ws, float max_norm,
                     float *norm, float *coef, int32_t *status, void *stream);
 

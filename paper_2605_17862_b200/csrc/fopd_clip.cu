@@ -1,5 +1,6 @@
 // Gradient norm and clipping: argument checks, the set's table, launches.
 #include <algorithm>
+#include <numeric>
 #include <vector>
 
 #include "clip_kernels.cuh"
@@ -30,23 +31,28 @@ int check_tensors(const fopd_tensor *t, int32_t n, const double *ws) {
 }
 
 struct Range {
-  uintptr_t lo, hi, row;  // row: pitch in bytes (0: one row)
+  uintptr_t lo, hi, row;  // row: pitch in bytes (0: one row, or rows without a gap)
   uintptr_t width;        // bytes of a row
   int32_t tensor;
   bool written;
 };
 
 Range range_of(const fopd_tensor &t, const void *p, int32_t i, bool written) {
-  const uintptr_t esz = t.dtype == FOPD_BF16 ? 2 : 4, a = (uintptr_t)p, width = (uintptr_t)t.cols * esz;
-  const uintptr_t pitch = t.rows > 1 ? (uintptr_t)t.row_stride * esz : 0;
+  const bool dense = t.rows == 1 || t.row_stride == t.cols;
+  const uintptr_t esz = t.dtype == FOPD_BF16 ? 2 : 4, a = (uintptr_t)p;
+  const uintptr_t width = (uintptr_t)(dense ? t.rows * t.cols : t.cols) * esz, pitch = dense ? 0 : (uintptr_t)t.row_stride * esz;
   return {a, a + (uintptr_t)(t.rows - 1) * pitch + width, pitch, width, i, written};
 }
 
-// Column blocks of one wider matrix overlap as ranges but not as elements.
+// Column blocks and rows of one wider matrix overlap as ranges but not as elements.  The distance of a row of b behind a
+// row of a is b.lo - a.lo and any multiples of both pitches, that is of their greatest common divisor (the other's where
+// one has a single row): no row of b meets one of a if within that distance b's row lies behind a's and ends before the
+// next.  a starts first.
 bool disjoint_columns(const Range &a, const Range &b) {
-  if (a.row == 0 || a.row != b.row || a.lo > b.lo) return false;
-  const uintptr_t shift = (b.lo - a.lo) % a.row;
-  return shift >= a.width && shift + b.width <= a.row;
+  const uintptr_t pitch = std::gcd(a.row, b.row);
+  if (pitch == 0) return false;
+  const uintptr_t shift = (b.lo - a.lo) % pitch;
+  return shift >= a.width && shift + b.width <= pitch;
 }
 
 // Whether a written range meets another one (its own tensor's data exactly in place excepted).

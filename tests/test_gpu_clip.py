@@ -242,3 +242,37 @@ def test_refusals():
     with pytest.raises(AssertionError):
         fb.fopd_grad_clip(fb.GradientList([x]), 1.0, ws[:100])
     fb.fopd_grad_norm(fb.GradientList([x, x]), ws)  # reading twice is no harm
+
+
+def test_rows_and_columns_of_one_matrix():
+    """Blocks that share no element: a block of columns beside single rows, every second row, and pieces without a gap."""
+    for pick in [lambda w: [w[:, :8], w[3:4, 8:16]], lambda w: [w[3:4, 8:16], w[:, :8]], lambda w: [w[:, 8:], w[2, :7]],
+                 lambda w: [w[:, :8], w[::2, 8:20], w[1::2, 20:], w[1, 9:19]], lambda w: [w[1:9:2], w[:9:2]],
+                 lambda w: [w[:, :8], w[1::3, 8:31], w[5, 8:24].view(2, 8), w[6, 9]], lambda w: [w[:, :31], w[:, 31]]]:
+        whole = gradients([((12, 32), BF16)], 31)[0]
+        assert check_clip(pick(whole), 0.02) < 1
+
+
+def test_sets_of_random_blocks_are_refused_or_right():
+    """Random views of one buffer: where two share an element the set is refused, and a set that is taken comes out right."""
+    rng = np.random.RandomState(32)
+    taken = refused = 0
+    for _ in range(400):
+        whole = gradients([((1500,), F32)], 33)[0]
+        tensors, used, clash = [], np.zeros(1500, dtype=int), False
+        for _ in range(rng.randint(2, 4)):
+            pitch = int(rng.choice([12, 24, 24, 36, 48]))
+            cols, rows = int(rng.randint(1, 12)), int(rng.randint(1, 9))
+            at = int(rng.randint(0, 200))
+            tensors.append(whole.as_strided((rows, cols), (pitch, 1), at))
+            index = (at + pitch * np.arange(rows)[:, None] + np.arange(cols)).ravel()
+            clash |= bool(used[index].any())
+            used[index] = 1
+        try:
+            check_clip(tensors, 0.001)
+            taken += 1
+            assert not clash
+        except fb.FopdError as e:
+            assert e.code == -7
+            refused += 1
+    assert taken > 40 and refused > 40

@@ -194,6 +194,22 @@ def test_gradient_calls_check_their_arguments_on_the_host(lib):
     assert scale(a, _tensor(data=0x10000 + 14, cols=8, row_stride=32)) == -7
 
 
+def test_rows_and_columns_of_one_matrix_that_meet_are_refused(lib):
+    """bf16 blocks of a matrix with 32 columns (64 bytes)."""
+    def scale(*ts):
+        arr = (fb.fopd_tensor * len(ts))(*ts)
+        return lib.fopd_grad_scale(arr, len(ts), vp(0x80000), 1.0, None, None, None, None)
+
+    def block(row, col, rows, cols, stride=32):
+        return _tensor(data=0x10000 + 2 * (32 * row + col), rows=rows, cols=cols, row_stride=stride)
+
+    a = block(0, 8, 6, 8)
+    for other in [block(2, 15, 1, 4), block(2, 4, 1, 5), block(5, 8, 1, 8), block(1, 0, 1, 64), block(0, 0, 1, 9),
+                  block(1, 15, 3, 2, 64), block(0, 30, 3, 11, 64), block(2, 16, 2, 25, 64), block(3, 16, 4, 8, 8)]:
+        assert scale(a, other) == -7 and scale(other, a) == -7
+    assert scale(block(0, 0, 3, 8, 64), block(1, 4, 3, 8, 96)) == -7  # every second row and every third from row 1: row 4
+
+
 # ---- the binding's view of a tensor ----
 
 def test_layouts_of_tensors():
