@@ -121,7 +121,7 @@ typedef enum {
                                    that call are not to be trusted               */
 #define FOPD_DEV_BAD_LOGITS 32  /* a row to draw from holds NaN or +inf, or no finite logit */
 #define FOPD_DEV_BAD_UNIFORM 64 /* a given random number outside [0, 1)         */
-#define FOPD_DEV_NONFINITE 128  /* the gradients' norm is infinite or NaN       */
+#define FOPD_DEV_NONFINITE 128  /* a gradient is infinite or NaN (and so their norm) */
 
 /* alpha, beta >= 0 scale the two drift diagnostics (Eq. 11); xi is the gate
  * threshold (Eq. 13); lambda weights the rollout anchor (Eq. 16).  The paper
@@ -525,10 +525,13 @@ int fopd_verify_draft(const fopd_draft *d /* HOST */, int32_t *tokens, float *lo
  * Norm and clipping of a set of gradients (the chunks' dlogits, or the parameters' gradients behind them:
  * the step between Algorithm 1's gradient and its update).  With g all elements of all tensors:
  *
- *   norm = sqrt(sum g^2),   coef = min(1, max_norm / norm),   out = coef g  (rounded once to the type).
+ *   norm = sqrt(sum g^2),   coef = min(1, max_norm / norm),   out = coef g.
  *
  * Nothing is added to the norm before the division: a set above max_norm comes out with norm max_norm.
- * Squares are formed and summed in fp64 in a fixed order: no overflow, reproducible bit for bit.
+ * Squares are formed and summed in fp64 in a fixed order: no overflow, reproducible bit for bit.  Products are formed in fp32 with
+ * coef rounded to fp32, and rounded to the type; with a coef below 2^-126, fp32's normal numbers, in fp64 and rounded once.
+ * Status and coef go by the fp64 norm, which is finite for any finite set; handed out in fp32, a norm above 3.4e38 is +infinity and a
+ * coef below 2^-126 subnormal or 0.
  */
 typedef struct {
   const void *data;   /* [rows, cols] at a pitch of row_stride elements; aligned to its element          */
@@ -550,7 +553,7 @@ int fopd_grad_norm(const fopd_tensor *tensors /* HOST */, int32_t n_tensors, dou
                    int32_t *status, void *stream);
 
 /* out = coef data with coef from ws[0] and max_norm (finite, > 0); coef[0], norm[0] fp32 or NULL.  With coef = 1
- * in place nothing is read or written.  If the norm is infinite or NaN, FOPD_DEV_NONFINITE is set, coef is 1 and
+ * in place nothing is read or written.  If ws[0] is infinite or NaN (so was an element), FOPD_DEV_NONFINITE is set, coef is 1 and
  * the values are left (or copied) as they are.  Elements of two tensors of the set must not overlap, nor those of
  * an `out` and another tensor's data: FOPD_ERR_ALIAS where their address ranges do, unless they are columns or
  * rows of one wider matrix, that is at least one has rows at a pitch, and the greatest common divisor of the pitches

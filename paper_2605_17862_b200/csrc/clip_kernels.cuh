@@ -180,9 +180,28 @@ __global__ void __launch_bounds__(kClipThreads, 4)
 }
 
 // coef of a sum of squares (see fopd_grad_scale); 1 where the norm is not finite.
-__device__ __forceinline__ float clip_coef(double sum, float max_norm) {
+__device__ __forceinline__ double clip_coef(double sum, float max_norm) {
   const double norm = sqrt(sum);
-  return norm > (double)max_norm && norm <= 1.7976931348623157e308 ? (float)((double)max_norm / norm) : 1.f;
+  return norm > (double)max_norm && norm <= 1.7976931348623157e308 ? (double)max_norm / norm : 1.0;
+}
+
+// The scaling by a coefficient below fp32's normal numbers, where that has few bits or none: products in fp64, rounded
+// once.  Out of line, and element by element: hardly any set comes here.
+template <int N>
+__device__ __noinline__ void scale_tiny(const ClipTable<N> &t, double c) {
+  for (int64_t tile = blockIdx.x; tile < t.n_tiles; tile += gridDim.x) {
+    const int k = find_entry(t, (uint32_t)tile);
+    const ClipEntry &e = t.e[k];
+    const ClipTile r = tile_range(t, k, (uint32_t)tile);
+    const int n = (r.rows > 0 ? r.rows : 1) * r.n;
+    for (int i = threadIdx.x; i < n; i += kClipThreads) {
+      const int64_t at = r.off + (i / r.n) * r.stride + i % r.n;
+      if (e.dtype == FOPD_BF16)
+        reinterpret_cast<__nv_bfloat16 *>(e.out)[at] = __double2bfloat16((double)Elem<FOPD_BF16>::load1(e.data, at) * c);
+      else
+        reinterpret_cast<float *>(e.out)[at] = (float)((double)Elem<FOPD_F32>::load1(e.data, at) * c);
+    }
+  }
 }
 
 template <int DT>
@@ -234,13 +253,17 @@ __global__ void __launch_bounds__(kClipThreads, 4)
                       float *coef, int32_t *status) {
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the norm kernel's sum (launched early behind it)
   const double sum = ws[FOPD_GRAD_WS_SUM];
-  const float c = clip_coef(sum, max_norm);
+  const float c = (float)clip_coef(sum, max_norm);
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     if (norm) norm[0] = (float)sqrt(sum);
     if (coef) coef[0] = c;
     if (status && !(sum <= 1.7976931348623157e308)) atomicOr(status, FOPD_DEV_NONFINITE);
   }
   if (c == 1.f && t.in_place) return;
+  if (c < 0x1p-126f) {
+    scale_tiny(t, clip_coef(sum, max_norm));
+    return;
+  }
   // from the end: what the norm has read last may still be in the L2
   for (int64_t tile = t.n_tiles - 1 - blockIdx.x; tile >= 0; tile -= gridDim.x) {
     const int i = find_entry(t, (uint32_t)tile);

@@ -276,3 +276,49 @@ def test_sets_of_random_blocks_are_refused_or_right():
             assert e.code == -7
             refused += 1
     assert taken > 40 and refused > 40
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("scale,max_norm", [(1e38, 1e-3), (1e38, 1.0), (1e30, 1e-20), (3e37, 1e-37), (1e10, 1e-35), (2e37, 1e-3)])
+def test_coefficients_below_fp32(dtype, scale, max_norm):
+    """The coefficient is subnormal in fp32 or nothing there; the gradients come out with norm max_norm all the same.  An
+    output is rounded once from the fp64 product (relative error of that below 1e-14).  (At 1e38 some of the normal numbers
+    are infinite: that is said, and nothing is scaled.)"""
+    shapes = [((50_000,), dtype), ((37, 1000), dtype), ((9, 8), dtype), ((1,), dtype)]
+    for place in ("in", "out", "shifted"):
+        x = gradients(shapes, 34, scale)
+        x[2] = x[2][:, :5]
+        whole = [torch.empty(2 * t.numel() + 8, dtype=dtype, device=DEV) for t in x]
+        outs = None if place == "in" else [w[(k if place == "out" else 1):].as_strided(t.shape, t.stride())
+                                           for k, (w, t) in enumerate(zip(whole, x))]
+        if outs:
+            outs[2] = torch.empty(9, 8, dtype=dtype, device=DEV)[:, :5]
+        m = float(np.float32(max_norm))
+        want_norm, want_coef, want = ro.clip(x, m)
+        norm, coef, status = scalars()
+        fb.fopd_grad_clip(fb.GradientList(x, outs), m, fb.grad_workspace(DEV), norm=norm, coef=coef, status=status)
+        if not math.isfinite(want_norm):
+            assert scale == 1e38 and int(status.cpu()[0]) == 128 and float(coef) == 1 and float(norm) == math.inf
+            assert all(np.array_equal(o.cpu().double().numpy(), w) for o, w in zip(x if outs is None else outs, want))
+            continue
+        assert int(status.cpu()[0]) == 0
+        assert float(norm) == math.inf if want_norm > 3.5e38 else abs(float(norm) - want_norm) <= U32 * want_norm
+        assert want_coef < 2.0 ** -126 and abs(float(coef) - want_coef) <= 2.0 ** -150 * 1.01  # half the smallest subnormal
+        step, tiny = (2.0 ** -8, 2.0 ** -134) if dtype == BF16 else (2.0 ** -24, 2.0 ** -150)
+        for o, w in zip(x if outs is None else outs, want):
+            o = o.cpu().double().numpy()
+            assert np.all(np.abs(o - w) <= np.maximum(np.abs(w) * step, tiny) * (1 + 1e-10))
+
+
+@pytest.mark.parametrize("max_norm", [1.0, 1e38])
+def test_a_norm_beyond_fp32_is_finite(max_norm):
+    """Two fp32 gradients of 3e38 have a norm of 4.2e38: status and coefficient go by that, the fp32 norm is infinite."""
+    x = [torch.full((1,), 3e38, device=DEV), torch.full((1,), -3e38, device=DEV)]
+    norm, coef, status = scalars()
+    fb.fopd_grad_clip(fb.GradientList(x), max_norm, fb.grad_workspace(DEV), norm=norm, coef=coef, status=status)
+    want = float(np.float32(max_norm)) / math.sqrt(2)
+    assert int(status.cpu()[0]) == 0 and float(norm) == math.inf
+    assert abs(float(x[0]) - want) <= 4 * U32 * want and float(x[1]) == -float(x[0])
+    ws = fb.grad_workspace(DEV)
+    fb.fopd_grad_norm(fb.GradientList([torch.full((2,), 3e38, device=DEV)]), ws, norm=norm, status=status)
+    assert int(status.cpu()[0]) == 0 and float(norm) == math.inf and math.isfinite(float(ws[0]))
