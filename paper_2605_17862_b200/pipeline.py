@@ -150,6 +150,7 @@ class Rollout:
     mask: torch.Tensor
     n_accepted: torch.Tensor  # [B]
     status: torch.Tensor  # [1]
+    temperature: float = 1.0  # of the distribution that logprob belongs to
 
     @staticmethod
     def alloc(B: int, K: int, device) -> "Rollout":
@@ -161,21 +162,30 @@ class Rollout:
 def verify_rollout(target, draft, draft_tokens, uniform, out: Rollout, *, n_draft=None, temperature=1.0,
                    draft_temperature=1.0, vocab=None, stream=None) -> Rollout:
     """Drafted (or stale) tokens against the policy that has the logits ``target`` [B, K + 1, V]."""
+    out.temperature = float(temperature)
     fb.fopd_verify_draft(target, draft, draft_tokens, uniform, out.tokens, n_draft=n_draft, logprob=out.logprob,
                          mask=out.mask, n_accepted=out.n_accepted, temperature=temperature,
                          draft_temperature=draft_temperature, vocab=vocab, status=out.status, stream=stream)
     return out
 
 
-def rollout_chunk(target, teacher, out: Rollout, sample_id, vocab=None, loss_kind: int = fb.LOSS_FULL_KL) -> fb.Chunk:
+def rollout_chunk(target, teacher, out: Rollout, sample_id, vocab=None, loss_kind: int = fb.LOSS_FULL_KL, *,
+                  behav_logprob=None) -> fb.Chunk:
     """The B (K + 1) target rows of a rollout as a chunk of the loss, without a copy: the policy's own
     logits, the teacher's on the same positions, and the tokens, log-probs and mask that came out.
-    ``target`` and ``teacher`` have their rows at one pitch; ``sample_id`` [B] int32, non-decreasing."""
+    ``target`` and ``teacher`` have their rows at one pitch; ``sample_id`` [B] int32, non-decreasing.
+
+    The loss compares behaviour log-probs with the student's at temperature 1.  Those of a rollout at another temperature
+    belong to another distribution (a fresh sample would look stale), so that such a rollout needs ``behav_logprob``
+    [B, K + 1] fp32: log softmax(target) at its tokens, which fopd_token_stats_student gives as ``lp_s``."""
+    assert behav_logprob is not None or out.temperature == 1.0, \
+        f"log-probs at temperature {out.temperature}: give behav_logprob"
+    lp = out.logprob if behav_logprob is None else behav_logprob
     B, W, V = target.shape
     assert target.stride(0) == W * target.stride(1), "rows at one pitch"
     rows = lambda t: t.as_strided((B * W, V), (t.stride(1), 1))
     assert teacher is None or teacher.stride() == target.stride()
-    return fb.Chunk(rows(target), None if teacher is None else rows(teacher), out.logprob.view(-1), out.tokens.view(-1),
+    return fb.Chunk(rows(target), None if teacher is None else rows(teacher), lp.view(-1), out.tokens.view(-1),
                     out.mask.view(-1), sample_id.repeat_interleave(W), vocab, loss_kind)
 
 

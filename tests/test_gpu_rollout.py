@@ -763,3 +763,37 @@ def test_residual_of_rows_that_differ_at_the_cut(dtype, B):
         assert got["tokens"][b].tolist() == [out[0], -1] and abs(got["logprob"][b, 0] - lps[0]) <= lp_tol(lps[0])
         seen.add(out[0] == 4444)
     assert len(seen) == min(B, 2)
+
+
+@pytest.mark.parametrize("T", [1.0, 0.7, 0.0])
+def test_a_fresh_rollout_at_any_temperature_is_fresh(T):
+    """Sampled at T, a rollout's own log-probs are those of softmax(x / T); with the policy's at its tokens the ratio is 1
+    and there is no drift."""
+    B, K, V = 5, 4, 1203
+    target, teacher, draft = (rows_of(s, V, F32, k) for k, s in ((401, (B, K + 1)), (402, (B, K + 1)), (403, (B, K))))
+    draft.copy_(target[:, :K])
+    drafted = drafts_from(draft, T, 404)
+    out = pl.verify_rollout(target, draft, drafted, uniforms((B, K + 1), 405), pl.Rollout.alloc(B, K, DEV), temperature=T,
+                            draft_temperature=T)
+    assert int(out.status[0]) == 0 and out.temperature == T
+    sid = torch.arange(B, dtype=torch.int32, device=DEV)
+    if T == 1.0:
+        chunk = pl.rollout_chunk(target, teacher, out, sid)
+    else:
+        with pytest.raises(AssertionError):
+            pl.rollout_chunk(target, teacher, out, sid)
+        lp = torch.zeros((B, K + 1), device=DEV)
+        first = pl.rollout_chunk(target, None, out, sid, behav_logprob=lp)
+        own = torch.zeros_like(lp)
+        fb.fopd_token_stats_student(first, B, torch.zeros((B, 4), dtype=torch.float64, device=DEV), lp_s=own)
+        chunk = pl.rollout_chunk(target, teacher, out, sid, behav_logprob=own)
+    at = out.tokens.clamp(min=0).long().unsqueeze(2)
+    want = target.double().log_softmax(-1).gather(2, at).squeeze(2)
+    kept = out.mask.bool()
+    assert torch.allclose(chunk.behav_logprob.view(B, K + 1)[kept].double(), want[kept], rtol=1e-5, atol=1e-5)
+    buf, rows = pl.BatchBuffers(B, DEV), [pl.RowOutputs.alloc(B * (K + 1), DEV)]
+    pl.measure([chunk], buf, rows)
+    tau, H = torch.zeros(B, dtype=torch.int32, device=DEV), torch.full((B,), K + 1, dtype=torch.int32, device=DEV)
+    pl.freshness(buf, tau, H, None, fb.params())
+    assert fb.fopd_check_status(buf.status) == 0
+    assert torch.allclose(buf.f, torch.ones_like(buf.f), rtol=1e-4)

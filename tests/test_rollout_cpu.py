@@ -11,6 +11,7 @@ import torch
 from oracle import rollout_oracle as ro
 from paper_2605_17862_b200 import binding as fb
 from paper_2605_17862_b200 import build as fbuild
+from paper_2605_17862_b200 import pipeline as pl
 
 vp = ctypes.c_void_p
 
@@ -230,3 +231,20 @@ def test_cpu_tensors_are_refused():
         fb.fopd_draw_tokens(x, torch.zeros(2, dtype=torch.float64), torch.zeros(2, dtype=torch.int32))
     with pytest.raises(AssertionError):
         fb.GradientList([x])
+
+
+# ---- a rollout as a chunk of the loss ----
+
+def test_log_probs_at_another_temperature_are_not_taken_for_the_policys():
+    B, K, V = 2, 3, 16
+    target, teacher = torch.zeros(2, B, K + 1, V).unbind(0)
+    sid = torch.arange(B, dtype=torch.int32)
+    out = pl.Rollout.alloc(B, K, "cpu")
+    assert out.temperature == 1.0
+    assert pl.rollout_chunk(target, teacher, out, sid).behav_logprob.data_ptr() == out.logprob.data_ptr()
+    lp = torch.ones(B, K + 1)
+    for T in (0.7, 0.0):
+        out.temperature = T
+        with pytest.raises(AssertionError):
+            pl.rollout_chunk(target, teacher, out, sid)
+        assert torch.equal(pl.rollout_chunk(target, teacher, out, sid, behav_logprob=lp).behav_logprob, lp.view(-1))
