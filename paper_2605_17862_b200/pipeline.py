@@ -182,9 +182,12 @@ def rollout_chunk(target, teacher, out: Rollout, sample_id, vocab=None, loss_kin
         f"log-probs at temperature {out.temperature}: give behav_logprob"
     lp = out.logprob if behav_logprob is None else behav_logprob
     B, W, V = target.shape
-    assert target.stride(0) == W * target.stride(1), "rows at one pitch"
-    rows = lambda t: t.as_strided((B * W, V), (t.stride(1), 1))
-    assert teacher is None or teacher.stride() == target.stride()
+
+    def rows(t):  # (the stride of a dimension of one says nothing)
+        pitch = t.stride(0) if W == 1 else t.stride(1)
+        assert t.shape == target.shape and (B == 1 or W == 1 or t.stride(0) == W * pitch), "rows at one pitch"
+        return t.as_strided((B * W, V), (pitch, 1 if V == 1 else t.stride(2)))
+
     return fb.Chunk(rows(target), None if teacher is None else rows(teacher), lp.view(-1), out.tokens.view(-1),
                     out.mask.view(-1), sample_id.repeat_interleave(W), vocab, loss_kind)
 

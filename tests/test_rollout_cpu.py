@@ -248,3 +248,19 @@ def test_log_probs_at_another_temperature_are_not_taken_for_the_policys():
         with pytest.raises(AssertionError):
             pl.rollout_chunk(target, teacher, out, sid)
         assert torch.equal(pl.rollout_chunk(target, teacher, out, sid, behav_logprob=lp).behav_logprob, lp.view(-1))
+
+
+def test_rollouts_of_one_sequence_or_one_row_as_chunks():
+    """Views whose stride along a dimension of one is not what rows at one pitch would have."""
+    buf = torch.arange(2 * 5 * 16, dtype=torch.float32).view(2, 5, 16)
+    for target in (buf[:1, :3, :9], buf[1:, 1:4, :9], buf[:, :1, :9], buf[:, 4, :9].unsqueeze(1), buf[:1, :1, :9], buf[:, :, :9]):
+        B, W, V = target.shape
+        out = pl.Rollout.alloc(B, W - 1, "cpu")
+        chunk = pl.rollout_chunk(target, target.clone() if target.is_contiguous() else target, out, torch.arange(B))
+        assert torch.equal(chunk.student, target.reshape(B * W, V)) and torch.equal(chunk.teacher, chunk.student)
+        assert chunk.student.data_ptr() == target.data_ptr()
+    for bad in (buf[:, :3, :9], buf.transpose(0, 1)[:, :, :9]):
+        with pytest.raises(AssertionError):
+            pl.rollout_chunk(bad, None, pl.Rollout.alloc(bad.shape[0], bad.shape[1] - 1, "cpu"), torch.arange(bad.shape[0]))
+    with pytest.raises(AssertionError):  # the teacher's rows
+        pl.rollout_chunk(buf[:, :, :9], buf[:, :3, :9], pl.Rollout.alloc(2, 4, "cpu"), torch.arange(2))
