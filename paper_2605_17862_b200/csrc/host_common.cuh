@@ -87,7 +87,9 @@ static inline int scratch_alloc(void **ptr, size_t bytes, cudaStream_t st) {
     }
     pool = sp.pools[dev];
   }
-  return cudaMallocFromPoolAsync(ptr, bytes, pool, st) == cudaSuccess ? FOPD_OK : FOPD_ERR_CUDA;
+  if (cudaMallocFromPoolAsync(ptr, bytes, pool, st) == cudaSuccess) return FOPD_OK;
+  (void)cudaGetLastError();  // (out of memory is this call's error: the next one's launch_ok() is not to find it)
+  return FOPD_ERR_CUDA;
 }
 
 // Gives the memory the current device's pool holds but no pending call uses back to the driver.

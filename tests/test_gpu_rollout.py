@@ -797,3 +797,22 @@ def test_a_fresh_rollout_at_any_temperature_is_fresh(T):
     pl.freshness(buf, tau, H, None, fb.params())
     assert fb.fopd_check_status(buf.status) == 0
     assert torch.allclose(buf.f, torch.ones_like(buf.f), rtol=1e-4)
+
+
+def test_a_temporary_that_does_not_fit_is_this_calls_error_alone():
+    """4.2 G positions take 168 GB beside 67 GB of arguments: the call says so before it launches anything, and the next ones
+    (here and in torch) run."""
+    B, K, V = 4000, (1 << 20) - 1, 8
+    try:
+        target = torch.zeros((K + 1, V), device=DEV, dtype=BF16).expand(B, K + 1, V)
+        drafted, tokens = (torch.empty((B, K + w), device=DEV, dtype=torch.int32) for w in (0, 1))
+        u = torch.empty((B, K + 1), device=DEV, dtype=torch.float64)
+        with pytest.raises(fb.FopdError) as e:
+            fb.fopd_verify_draft(target, None, drafted, u, tokens)
+        assert e.value.code == -6
+    finally:
+        target = drafted = tokens = u = None
+        torch.cuda.empty_cache()
+    ws, x, norm = fb.grad_workspace(DEV), torch.full((9,), 2.0, device=DEV), torch.zeros(1, device=DEV)
+    fb.fopd_grad_norm(fb.GradientList([x]), ws, norm=norm)
+    assert float(norm) == 6.0 and float((x + x).sum()) == 36.0
