@@ -102,21 +102,23 @@ typedef enum { FOPD_LOSS_FULL_KL = 0, FOPD_LOSS_SAMPLED_KL = 1 } fopd_loss_kind;
 typedef enum {
   FOPD_OK = 0,
   FOPD_ERR_NULL = -1,   /* a required pointer is NULL                          */
-  FOPD_ERR_ALIGN = -2,  /* logits base or row pitch not 16-byte aligned         */
-  FOPD_ERR_SIZE = -3,   /* negative size, row_stride < vocab, vocab too large   */
+  FOPD_ERR_ALIGN = -2,  /* logits base or pitch, or workspace, not 16-byte aligned */
+  FOPD_ERR_SIZE = -3,   /* negative size, row_stride < vocab or cols, too large */
   FOPD_ERR_DTYPE = -4,  /* dtype is neither FOPD_BF16 nor FOPD_F32              */
-  FOPD_ERR_PARAM = -5,  /* alpha/beta negative or a parameter not finite        */
+  FOPD_ERR_PARAM = -5,  /* a parameter out of its range or not finite           */
   FOPD_ERR_CUDA = -6,   /* a CUDA runtime call failed (launch, allocation)      */
-  FOPD_ERR_ALIAS = -7,  /* dlogits overlaps student or teacher, an output an input */
+  FOPD_ERR_ALIAS = -7,  /* dlogits overlaps student or teacher, an output an input
+                           or another tensor of its set                         */
   FOPD_ERR_DEVICE = -8, /* fopd_check_status: the device status word is non-zero */
   FOPD_ERR_KIND = -9    /* loss_kind unknown, or not supported by this entry point */
 } fopd_status;
 
 /* Bits ORed into the device status word. */
-#define FOPD_DEV_BAD_TOKEN 1    /* mask = 1 row with token outside [0, vocab)   */
+#define FOPD_DEV_BAD_TOKEN 1    /* mask = 1 row, or draft, with token outside [0, vocab) */
 #define FOPD_DEV_BAD_SAMPLE 2   /* row with sample id outside [0, B)            */
 #define FOPD_DEV_BAD_TAU 4      /* staleness < 0                                */
-#define FOPD_DEV_BAD_LENGTH 8   /* seq_len <= 0 or aligned count > seq_len      */
+#define FOPD_DEV_BAD_LENGTH 8   /* seq_len <= 0 or aligned count > seq_len, n_draft
+                                   outside [0, K]                               */
 #define FOPD_DEV_TIMEOUT 16     /* a bounded in-kernel wait ran out; results of
                                    that call are not to be trusted               */
 #define FOPD_DEV_BAD_LOGITS 32  /* a row to draw from holds NaN or +inf, or no finite logit */

@@ -248,13 +248,14 @@ const char *fopd_strerror(int code) {
   switch (code) {
     case FOPD_OK: return "ok";
     case FOPD_ERR_NULL: return "a required pointer is NULL";
-    case FOPD_ERR_ALIGN: return "logits base, row pitch or workspace not 16-byte aligned";
-    case FOPD_ERR_SIZE: return "bad size (negative, row_stride < vocab, or too large)";
+    case FOPD_ERR_ALIGN: return "logits base, row or sequence pitch or workspace not 16-byte aligned, or a gradient not aligned to its element";
+    case FOPD_ERR_SIZE: return "bad size (negative, row_stride < vocab or cols, or too large)";
     case FOPD_ERR_DTYPE: return "dtype must be FOPD_BF16 or FOPD_F32";
-    case FOPD_ERR_PARAM: return "alpha/beta must be >= 0 and all parameters finite";
+    case FOPD_ERR_PARAM: return "a parameter out of range (alpha, beta >= 0; temperature 0 or 2^-10 to 2^10; max_norm > 0) or not finite";
     case FOPD_ERR_CUDA: return "a CUDA runtime call failed";
-    case FOPD_ERR_ALIAS: return "dlogits overlaps student or teacher";
-    case FOPD_ERR_DEVICE: return "device status word is non-zero (bad token/sample id, staleness, length or timeout)";
+    case FOPD_ERR_ALIAS: return "an output overlaps an input (dlogits: student or teacher) or another tensor of its set";
+    case FOPD_ERR_DEVICE: return "device status word is non-zero (bad token/sample id, staleness, length, logits or uniform number, a gradient that is not "
+                                 "finite, or timeout)";
     case FOPD_ERR_KIND: return "loss_kind unknown or not supported by this entry point";
     default: return "unknown fopd status";
   }

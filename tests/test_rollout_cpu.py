@@ -264,3 +264,10 @@ def test_rollouts_of_one_sequence_or_one_row_as_chunks():
             pl.rollout_chunk(bad, None, pl.Rollout.alloc(bad.shape[0], bad.shape[1] - 1, "cpu"), torch.arange(bad.shape[0]))
     with pytest.raises(AssertionError):  # the teacher's rows
         pl.rollout_chunk(buf[:, :, :9], buf[:, :3, :9], pl.Rollout.alloc(2, 4, "cpu"), torch.arange(2))
+
+
+@pytest.mark.parametrize("code,words", [(-2, ("16-byte", "gradient")), (-3, ("cols",)), (-5, ("temperature", "max_norm", "alpha")),
+                                        (-7, ("output", "set", "dlogits")), (-8, ("logits", "uniform", "gradient"))])
+def test_errors_name_what_these_calls_refuse(lib, code, words):
+    text = str(fb.FopdError(code, "f"))
+    assert all(w in text for w in words), text
