@@ -107,7 +107,7 @@ class GradientClip:
     def __init__(self, tensors, max_norm: float, outs=None):
         self.grads = fb.GradientList(tensors, outs)
         self.max_norm = float(max_norm)
-        dev = self.grads.device
+        dev = self.grads.device or torch.device("cuda", torch.cuda.current_device())  # (an empty set has none)
         self.ws = fb.grad_workspace(dev)
         self.norm, self.coef = (torch.zeros(1, dtype=torch.float32, device=dev) for _ in range(2))
 

@@ -322,3 +322,10 @@ def test_a_norm_beyond_fp32_is_finite(max_norm):
     ws = fb.grad_workspace(DEV)
     fb.fopd_grad_norm(fb.GradientList([torch.full((2,), 3e38, device=DEV)]), ws, norm=norm, status=status)
     assert int(status.cpu()[0]) == 0 and float(norm) == math.inf and math.isfinite(float(ws[0]))
+
+
+def test_clip_of_an_empty_set():
+    from paper_2605_17862_b200 import pipeline as pl
+
+    clip = pl.GradientClip([], 1.0)
+    assert float(clip()) == 0 and float(clip.coef) == 1
