@@ -816,3 +816,109 @@ def test_a_temporary_that_does_not_fit_is_this_calls_error_alone():
     ws, x, norm = fb.grad_workspace(DEV), torch.full((9,), 2.0, device=DEV), torch.zeros(1, device=DEV)
     fb.fopd_grad_norm(fb.GradientList([x]), ws, norm=norm)
     assert float(norm) == 6.0 and float((x + x).sum()) == 36.0
+
+
+# ---- the bound on the fp32 sums: decisions just outside it, and the log-probs it covers ----
+
+def sum_error(V, T):
+    """Relative error of an fp32 sum of exponentials and of one of them: an exponent y = x c - max c is off by the rounding
+    of c = fl(log2(e) / T) and by 2^-24 |y|, with the mean of |y| at most 0.74 log2 V + 0.5 for V <= 2^18; an ex2 (2^-22) and
+    six roundings (2^-24) come on top."""
+    c = math.log2(math.e) / T
+    return 0.6932 * (5.97e-8 + abs(float(np.float32(c)) - c) / c) * (0.74 * math.log2(V) + 0.5) + 6.2e-7
+
+
+def lp_bound(V, T, lp):
+    """The sum's error; its rounding to fp32; logf, within one unit of the last place of log Z <= log V; the result's rounding."""
+    return sum_error(V, T) + 2.0 ** -24 + 2.0 ** -23 * max(1.0, math.log(V)) + 2.0 ** -24 * np.abs(lp)
+
+
+def coarse_temperatures():
+    """Temperatures whose log2(e) / T is rounded furthest, up and down, and one."""
+    T = np.linspace(0.3, 1.9, 4001)
+    c = math.log2(math.e) / T
+    off = (c.astype(np.float32).astype(np.float64) - c) / c
+    return [float(T[off.argmax()]), float(T[off.argmin()]), 1.0]
+
+
+def steep(V, T, seed):
+    """Logits (fp32) of the largest mean exponent: one at the top, the rest even at the distance that maximises it, in a random
+    place; and the like with a spread, so that boundaries differ."""
+    w = 2.0 ** -np.linspace(0.1, math.log2(V) * 1.5, 400)
+    s = 1 / (1 + (V - 1) * w)
+    y = -float(np.log2(w)[((1 - s) * -np.log2(w)).argmax()])
+    rows = torch.full((4, V), -y * T * math.log(2), dtype=torch.float64)
+    g = torch.Generator().manual_seed(seed)
+    rows[2:] += torch.randn((2, V), generator=g, dtype=torch.float64) * 0.5 * T
+    rows[torch.arange(4), torch.randint(0, V, (4,), generator=g)] = 0.0
+    rows[1::2] += 11.3
+    return rows.float()
+
+
+@pytest.mark.parametrize("V", [1001, 32003, 151936])
+@pytest.mark.parametrize("which", [0, 1, 2])
+def test_draws_just_outside_the_bound(V, which):
+    """Numbers half to ten bounds from a boundary of the fp64 distribution, on either side: in fp32 where the bound lets a draw
+    be decided there, and a bound that were too small would give the neighbour."""
+    T = coarse_temperatures()[which]
+    eps, base = sum_error(V, T), torch.cat([steep(V, T, 21), torch.randn((4, V), generator=torch.Generator().manual_seed(22)) * 3])
+    per, per_vec = 40, 4
+    x = torch.zeros((8 * per, -(-V // per_vec) * per_vec), device=DEV)[:, :V]
+    x.copy_(base.to(DEV).repeat_interleave(per, 0))
+    p = (x[::per].double() / T).softmax(-1)
+    F = p.cumsum(-1)
+    F = F / F[:, -1:]
+    rng = np.random.RandomState(23 + which)
+    for dist in (0.5, 1.5, 2.05, 2.5, 3.0, 4.0, 10.0):
+        # half of the boundaries beside a large probability, where the neighbours are far away
+        top = p.topk(20, -1).indices.cpu().numpy()
+        k = np.stack([np.where(rng.rand(per) < 0.5, top[r, rng.randint(0, 20, per)] - rng.randint(0, 2, per),
+                               rng.randint(0, V - 1, per)) for r in range(8)]).clip(0, V - 2)
+        v = F.gather(1, torch.tensor(k, device=DEV)) + torch.tensor(rng.choice([-1, 1], k.shape), device=DEV) * dist * eps
+        v = v.clamp(0, 1 - 1e-9)
+        want = torch.searchsorted(F, v, right=True).clamp(max=V - 1)
+        tokens, lp, bits = run_draw(x, v.view(-1).contiguous(), T)
+        assert bits == 0 and torch.equal(tokens.long(), want.view(-1))
+        wl = p.gather(1, want).log().view(-1).cpu().numpy()
+        assert np.all(np.abs(lp.cpu().numpy() - wl) <= lp_bound(V, T, wl))
+
+
+@pytest.mark.parametrize("V", [1001, 32003])
+@pytest.mark.parametrize("which", [0, 1, 2])
+@pytest.mark.parametrize("form", ["rows", "certain"])
+def test_acceptance_just_outside_the_bound(V, which, form):
+    """u q a distance of half to twenty bounds from p, on either side, between rows of the largest mean exponent and even ones;
+    the log-probs of what is accepted within the bound."""
+    T, n = coarse_temperatures()[which], 96
+    Td = coarse_temperatures()[(which + 1) % 3]
+    eps = max(sum_error(V, T), sum_error(V, Td))
+    target, draft = (torch.zeros((n, w, -(-V // 4) * 4), device=DEV)[:, :, :V] for w in (2, 1))
+    a, b = steep(V, T, 31).to(DEV), steep(V, Td, 32).to(DEV)
+    target[:, 0], target[:, 1], draft[:, 0] = a.repeat(n // 4, 1), a[0], b.repeat_interleave(n // 4, 0)
+    draft[::3, 0] = 0.0
+    p, q = (target[:, 0].double() / T).log_softmax(-1), (draft[:, 0].double() / Td).log_softmax(-1)
+    if form == "certain":
+        q = torch.zeros_like(q)
+    rng = np.random.RandomState(33 + which)
+    for dist in (0.5, 2.0, 3.9, 4.1, 5.0, 8.0, 20.0):
+        x = torch.where(p < q, torch.rand(p.shape, device=DEV, generator=torch.Generator(device=DEV).manual_seed(int(dist * 10))), -1.0)
+        x = torch.where(torch.tensor(rng.rand(n) < 0.5, device=DEV), x.argmax(-1), torch.where(p < q, p, -math.inf).argmax(-1))
+        x = x.unsqueeze(1)
+        sign = torch.tensor(rng.choice([-1, 1], (n, 1)), device=DEV)
+        u = uniforms((n, 2), 34)
+        u[:, :1] = ((p - q).gather(1, x).exp() * (1 + sign * dist * eps)).clamp(0, 1 - 1e-9)
+        want = (u[:, :1].log() + q.gather(1, x) < p.gather(1, x)).view(-1).cpu().numpy()
+        assert want.any() and not want.all()
+        got, bits = run_verify(target, draft if form == "rows" else None, x.int(), u, T=T, Td=Td)
+        assert bits == 0 and np.array_equal(got["n_accepted"], want.astype(np.int32))
+        wl = p.gather(1, x).view(-1).cpu().numpy()
+        assert np.all(np.abs(got["logprob"][want, 0] - wl[want]) <= lp_bound(V, T, wl[want]))
+
+
+@pytest.mark.parametrize("V,dtype,T", [(151936, BF16, 1.0), (32003, F32, 0.37), (9, F32, 1.0), (70001, BF16, 1.7)])
+def test_log_probs_within_the_bound(V, dtype, T):
+    x, u = rows_of((200,), V, dtype, 41), uniforms(200, 42)
+    for n in (200, 1):
+        tokens, lp, bits = run_draw(x[:n], u[:n], T)
+        wl = (x[:n].double() / T).log_softmax(-1).gather(1, tokens.long().unsqueeze(1)).view(-1).cpu().numpy()
+        assert bits == 0 and np.all(np.abs(lp.cpu().numpy() - wl) <= lp_bound(V, T, wl))
