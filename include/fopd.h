@@ -470,7 +470,8 @@ int fopd_shard_loss_fwd_bwd(const fopd_chunk *shard, int64_t vocab_offset, int64
 
 /*
  * Draws one token from each row: tokens[n] = min { i : sum_{k <= i} p_k > uniform[n] }, the inverse of
- * the distribution function, and logprob[n] = log p_{tokens[n]}.
+ * the distribution function, and logprob[n] = log p_{tokens[n]}, never above 0.  Its error is below 6e-6 (1e-7 is usual) and
+ * the fp32 rounding; for p above 0.8 it is below 6e-6 of log p itself, down to 1e-15.
  * Neither may lie on uniform (FOPD_ERR_ALIAS) or on the logits.
  *
  *   logits    [n_rows, vocab] at a pitch of row_stride elements, layout rules of fopd_chunk

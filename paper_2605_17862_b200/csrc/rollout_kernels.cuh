@@ -310,21 +310,18 @@ __device__ __noinline__ double far_sum(uint4 raw, float m, float c) {
   return z;
 }
 
-// Sums of a row, part after part: {max, sum 2^{(x - max) c}} with the maximum the warp's and the sum the lane's own.
-// The exponent is x c - fl(max c) in one fused multiply-add; what fl() took away is the same for all elements and put
-// back at the end.  -infinity everywhere gives {-inf, 0}; a NaN or +inf makes the sum NaN.
+// A sum of weights 2^{x c - mc}, mc = fl(m c), with what fl() took away put back (tiny unless the logits are far from zero).
+__device__ __forceinline__ double put_back(float s, float m, float c, float mc) {
+  const float took = m == -INFINITY ? 0.f : fmaf(m, c, -mc);
+  return fabsf(took) < 1.2e-4f ? (double)fmaf(-took * kLn2, s, s) : (double)s * exp64(-(double)took, 1.0);
+}
+
+// A lane's sum of 2^{(x - m) c} over its vectors of a part.  The exponent is x c - fl(m c) in one fused multiply-add; what
+// fl() took away is the same for all elements and put back at the end.
 template <int DT>
-__device__ __forceinline__ void add_part(RowSum &acc, const uint4 (&raw)[kLoadVecs], float c, double c64) {
-  using E = Elem<DT>;
-  constexpr int P = E::kPerVec;
-  float m = warp_max(max_vecs<DT>(raw));
-  if (m > acc.m) {
-    if (acc.m != -INFINITY) acc.z *= exp64((double)acc.m - m, c64);
-    acc.m = m;
-  }
-  m = acc.m;
+__device__ __forceinline__ double lane_sum(const uint4 (&raw)[kLoadVecs], float m, float c) {
+  constexpr int P = Elem<DT>::kPerVec;
   const float mc = m == -INFINITY ? 0.f : m * c;
-  double z;
   if (fabsf(mc) <= kFar) {
     const f32x2 c2 = pair(c, c), mc2 = pair(-mc, -mc);
     f32x2 sums[kLoadVecs];
@@ -336,16 +333,24 @@ __device__ __forceinline__ void add_part(RowSum &acc, const uint4 (&raw)[kLoadVe
       for (int k = 0; k < P / 2; ++k) x[k] = exp2_2(fma2(x[k], c2, mc2));
       sums[v] = tree_sum2<P / 2>(x);
     }
-    float s = both(tree_sum2<kLoadVecs>(sums));
-    // (what fl() took away is tiny unless the logits are far from zero)
-    const float took = m == -INFINITY ? 0.f : fmaf(m, c, -mc);
-    z = fabsf(took) < 1.2e-4f ? (double)fmaf(-took * kLn2, s, s) : (double)s * exp64(-(double)took, 1.0);
-  } else {
-    z = 0.0;
-#pragma unroll
-    for (int v = 0; v < kLoadVecs; ++v) z += far_sum<DT>(raw[v], m, c);
+    return put_back(both(tree_sum2<kLoadVecs>(sums)), m, c, mc);
   }
-  acc.z += z;
+  double z = 0.0;
+#pragma unroll
+  for (int v = 0; v < kLoadVecs; ++v) z += far_sum<DT>(raw[v], m, c);
+  return z;
+}
+
+// Sums of a row, part after part: {max, sum 2^{(x - max) c}} with the maximum the warp's and the sum the lane's own.
+// -infinity everywhere gives {-inf, 0}; a NaN or +inf makes the sum NaN.
+template <int DT>
+__device__ __forceinline__ void add_part(RowSum &acc, const uint4 (&raw)[kLoadVecs], float c, double c64) {
+  const float m = warp_max(max_vecs<DT>(raw));
+  if (m > acc.m) {
+    if (acc.m != -INFINITY) acc.z *= exp64((double)acc.m - m, c64);
+    acc.m = m;
+  }
+  acc.z += lane_sum<DT>(raw, acc.m, c);
 }
 
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -909,8 +914,36 @@ __device__ __noinline__ ExactSums cluster_exact_sums(cg::cluster_group &cl, cons
   return {warp_sum(s.t), warp_sum(s.q)};
 }
 
-// log p of an element of a row from its logit and the row's sum: the difference in fp64, the log's error is 1e-6 of it.
-__device__ __forceinline__ float log_prob(float logit, const RowSum &r, double c64) {
+// The sum of a row without its largest element `at`, in every lane of a warp.  Beside a weight of 1 the fp32 sum of its
+// lane's vectors has lost what the others weigh (2^-24 of the whole); all other sums are free of it and have been added up
+// in fp64.  So that lane's sum is formed again, a lane for each of its elements and in the same order (lane_sum's trees),
+// taken out of the row's, and put back without the element.  (Out of line: inlined it makes the first launch of a finish
+// spill, 62.5 against 61.5 us for 64 sequences.)
+template <int DT>
+__device__ __noinline__ double sum_beside(const char *row, int64_t V, int32_t at, const RowSum &r, float c) {
+  constexpr int P = Elem<DT>::kPerVec;
+  const float mc = r.m * c;
+  if (!(fabsf(mc) <= kFar)) return fmax(r.z - 1.0, 0.0);  // (far_sum adds weight by weight in fp64)
+  const int e = (threadIdx.x & 31) % (kLoadVecs * P);
+  const int64_t vec = at / P, i = (vec / kPartVecs * kPartVecs + vec % 32 + e / P * 32) * P + e % P;
+  float with = i < V ? ex2(fmaf(Elem<DT>::load1(row, i), c, -mc)) : 0.f, without = i == at ? 0.f : with;
+  const auto add = [&](int off) {
+    with += __shfl_xor_sync(0xffffffffu, with, off);
+    without += __shfl_xor_sync(0xffffffffu, without, off);
+  };
+#pragma unroll
+  for (int off = P / 2; off > 1; off >>= 1) add(off);
+#pragma unroll
+  for (int off = kLoadVecs / 2 * P; off >= P; off >>= 1) add(off);
+  add(1);
+  return fmax(r.z - put_back(with, r.m, c, mc) + put_back(without, r.m, c, mc), 0.0);
+}
+// log p of element `at` of a row from its logit and the row's sum, by a warp: the difference in fp64, the log's error is
+// 1e-6 of it.  Towards p = 1 the row's sum is hardly more than 1 and its log no larger than its error: above 0.8 it comes
+// from the rest (about 1 us; below, the sum's error is 1e-6 of the log at most).
+template <int DT>
+__device__ __forceinline__ float log_prob(const char *row, int64_t V, int32_t at, float logit, const RowSum &r, float c, double c64) {
+  if (logit == r.m && r.z < 1.25) return 0.f - log1pf((float)sum_beside<DT>(row, V, at, r, c));
   return (float)(((double)logit - r.m) * inv_temperature(c64) - (double)logf((float)r.z));
 }
 
@@ -1004,7 +1037,7 @@ __global__ void __launch_bounds__(kRollThreads, kMode == kFirst ? 4 : 2) draw_ke
         token = cluster_search<DT, true, false>(cl, w, d, sl, v, 0.0, 0.0, parity, sh, &exact_total, &never);
         parity ^= 1;
       }
-      if (good && token >= 0 && threadIdx.x == 0) lp = log_prob(sh.logit, total, d.ct64);
+      if (good && token >= 0 && warp == 0) lp = log_prob<DT>(row, d.vocab, token, sh.logit, total, d.ct, d.ct64);
     }
     if (threadIdx.x == 0 && (good ? token != kUnsure : rank == 0)) {  // the CTA that has the token, or the first one
       if (!good) token = -1;
@@ -1047,8 +1080,9 @@ __device__ __forceinline__ Draft draft_of(const RolloutDev &d, int32_t b, int32_
   }
   return r;
 }
-// Decides on one position.
-__device__ __forceinline__ void judge(const RolloutDev &d, const Draft &r, bool last, bool target_best, Position &o) {
+// Decides on one position (a warp, all lanes alike).
+template <int DT>
+__device__ __forceinline__ void judge(const RolloutDev &d, const Draft &r, const char *trow, bool last, bool target_best, Position &o) {
   o.lp = 0.f;
   o.state = is_distribution(o.t) ? kEnd : kBadRow;
   if (o.state == kBadRow || last) return;
@@ -1060,12 +1094,12 @@ __device__ __forceinline__ void judge(const RolloutDev &d, const Draft &r, bool 
     o.state = kBadUniform;
   } else {
     const double p = exp64((double)r.t - o.t.m, d.ct64) / o.t.z;
-    o.lp = log_prob(r.t, o.t, d.ct64);
     double q = 1.0;
     if (d.kind == kDraftRows) q = exp64((double)r.q - o.q.m, d.cd64) / o.q.z;
     else if (d.kind == kDraftBest) q = r.x == o.q.best ? 1.0 : 0.0;
     const double uq = r.u * q;
     o.state = fabs(uq - p) < 4 * d.eps * fmax(uq, p) ? kOpen : uq < p ? kAccept : kReject;
+    if (o.state != kReject) o.lp = log_prob<DT>(trow, d.vocab, r.x, r.t, o.t, d.ct, d.ct64);
   }
   if ((d.kind == kDraftRows || d.kind == kDraftBest) && o.state != kBadUniform && !is_distribution(o.q)) o.state = kBadRow;
 }
@@ -1140,7 +1174,7 @@ __device__ __forceinline__ void sweep_position(cg::cluster_group &cl, const Roll
   for (int k = 0; k < kStages; ++k) ask(ring + k * kPartVecs);
   if (!d.stop) all_started(cl);  // (with d.stop they have met before)
   Draft draft = {};
-  if (rank == 0 && threadIdx.x == 0) draft = draft_of<DT>(d, b, j, n, trow, qrow);
+  if (rank == 0 && warp == 0) draft = draft_of<DT>(d, b, j, n, trow, qrow);
   RowSum t = nothing(), q = nothing();  // (q holds the row being swept, then the draft's)
   bool in_q = false;
 #pragma unroll 1
@@ -1190,15 +1224,15 @@ __device__ __forceinline__ void sweep_position(cg::cluster_group &cl, const Roll
       if (want_q) q = q_best ? warp_merge_best(q) : warp_merge(q, d.cd64);
     }
   }
-  if (rank == 0 && threadIdx.x == 0) {
+  if (rank == 0 && warp == 0) {
     Position o;
     if (kBest) t.z = 1.0;
     if (q_best) q.z = 1.0;
     o.t = t;
     o.q = q;
-    judge(d, draft, j == n, kBest, o);
-    d.pos[(int64_t)b * (d.K + 1) + j] = o;
-    if (d.stop && j < n && o.state != kAccept && o.state != kOpen) atomicMin(d.stop + b, j);
+    judge<DT>(d, draft, trow, j == n, kBest, o);
+    if (lane == 0) d.pos[(int64_t)b * (d.K + 1) + j] = o;
+    if (lane == 0 && d.stop && j < n && o.state != kAccept && o.state != kOpen) atomicMin(d.stop + b, j);
   }
 }
 
@@ -1342,7 +1376,7 @@ __device__ __forceinline__ void finish_sequence(cg::cluster_group &cl, const Rol
       w.rest = false;
       w.without = -1;
     }
-    if (token >= 0 && threadIdx.x == 0) lp = log_prob(sh.logit, t32, d.ct64);
+    if (token >= 0 && threadIdx.x < 32) lp = log_prob<DT>(w.t, d.vocab, token, sh.logit, t32, d.ct, d.ct64);
   }
   const int64_t at = (int64_t)b * W;
   if (token != kUnsure && threadIdx.x == 0) {

@@ -922,3 +922,60 @@ def test_log_probs_within_the_bound(V, dtype, T):
         tokens, lp, bits = run_draw(x[:n], u[:n], T)
         wl = (x[:n].double() / T).log_softmax(-1).gather(1, tokens.long().unsqueeze(1)).view(-1).cpu().numpy()
         assert bits == 0 and np.all(np.abs(lp.cpu().numpy() - wl) <= lp_bound(V, T, wl))
+
+
+# ---- log-probs of tokens that are nearly certain ----
+
+def near_certain(n, V, T, dtype, seed, offset):
+    """Rows whose largest element, in a random place, leaves the others about 1e-9 to 0.2 of its weight together."""
+    x = rows_of((n,), V, dtype, seed, scale=0.5 * T)
+    rest = torch.tensor([1e-9, 1e-6, 1e-4, 1e-2, 0.05, 0.2], dtype=torch.float64)[torch.arange(n) % 6]
+    x -= (T * torch.log((V - 1) / rest)).to(DEV).unsqueeze(1).to(dtype)
+    x += offset
+    at = torch.randint(0, V, (n,), generator=torch.Generator().manual_seed(seed + 1)).to(DEV)
+    x[torch.arange(n, device=DEV), at] = offset
+    assert bool((x.amax(-1) == x[torch.arange(n, device=DEV), at]).all())
+    return x, at
+
+
+def check_near_certain(x, at, lp, T):
+    """-log(1 + rest): the rest's weights are off by their exponents (2^-24 and the rounding of log2(e) / T, relative to y), an
+    ex2 (2^-22) and eight roundings on the way to an fp32 number, log1pf by two units of its last place; 1 + rest and what is
+    taken out of it have been added up in fp64, some ten times.  From a rest of a quarter on the log is that of the sum."""
+    n = torch.arange(len(x), device=DEV)
+    z = (x.double() - x[n, at].double().unsqueeze(1)) / T
+    w = z.exp()
+    w[n, at] = 0.0
+    rest = w.sum(-1)
+    y = (w * torch.where(w > 0, -z / math.log(2), 0.0)).sum(-1) / rest
+    c = math.log2(math.e) / T
+    rel = 0.6932 * (5.97e-8 + abs(float(np.float32(c)) - c) / c) * y + 2.0 ** -22 + 8 * 2.0 ** -24 + 2 * 2.0 ** -23
+    want = -torch.log1p(rest)
+    assert float(rest.max()) < 1.0
+    off = (lp.to(DEV).double() - want).abs()
+    tol = torch.where(rest < 0.25, rel * want.abs() + 1.5e-15, torch.tensor(lp_bound(x.shape[1], T, want.cpu().numpy()), device=DEV))
+    assert bool((off <= tol).all()), float((off / want.abs()).max())
+    assert bool((lp <= 0).all())
+
+
+@pytest.mark.parametrize("dtype,T,offset", [(BF16, 1.0, 0.0), (F32, 0.3577, 0.0), (F32, 1.0, 1e3), (BF16, 0.7, -64.0), (F32, 0.002, 3e4)])
+@pytest.mark.parametrize("V,n", [(151936, 1), (4099, 6), (32003, 60), (1025, 700), (6, 12)])
+def test_log_probs_of_drawn_tokens_that_are_nearly_certain(V, n, dtype, T, offset):
+    x, at = near_certain(n, V, T, dtype, 51, offset)
+    p = (x.double() / T).softmax(-1)
+    middle = p.cumsum(-1).gather(1, at.unsqueeze(1)) - 0.5 * p.gather(1, at.unsqueeze(1))
+    for v in (middle.view(-1).clamp(min=0.0), torch.full_like(middle.view(-1), 0.5)):
+        tokens, lp, bits = run_draw(x, v.contiguous(), T)
+        assert bits == 0 and torch.equal(tokens.long(), at)
+        check_near_certain(x, at, lp, T)
+
+
+@pytest.mark.parametrize("dtype,T,offset", [(BF16, 1.0, 0.0), (F32, 0.3577, 0.0), (F32, 1.0, 1e3)])
+@pytest.mark.parametrize("V,B,K,form", [(151936, 1, 5, "certain"), (4099, 40, 2, "rows"), (1025, 300, 5, "certain"), (700, 9, 400, "rows")])
+def test_log_probs_of_verified_tokens_that_are_nearly_certain(V, B, K, form, dtype, T, offset):
+    x, at = near_certain(B * (K + 1), V, T, dtype, 53, offset)
+    target, best = x.as_strided((B, K + 1, V), (x.stride(0) * (K + 1), x.stride(0), 1)), at.view(B, K + 1)
+    u = torch.full((B, K + 1), 0.5, dtype=torch.float64, device=DEV)
+    got, bits = run_verify(target, target[:, :K] if form == "rows" else None, best[:, :K].int().contiguous(), u, T=T, Td=T)
+    assert bits == 0 and np.array_equal(got["tokens"], best.cpu().numpy())
+    check_near_certain(x, at, torch.tensor(got["logprob"]).view(-1), T)
