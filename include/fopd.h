@@ -463,15 +463,15 @@ int fopd_shard_loss_fwd_bwd(const fopd_chunk *shard, int64_t vocab_offset, int64
  * exact arithmetic: the sweeps run in fp32 with a bound on their error, and whatever the bound does not
  * decide is decided again in fp64 (error ~1e-13 of a row's sum).  There a weight below 2^-900 of its row's
  * largest counts as zero: such a token comes out of no draw, and a draw from max(p - q, 0) takes p_j instead
- * where all that is left is that small.  A row that is needed and holds NaN or
- * +infinity, or nothing but -infinity, sets FOPD_DEV_BAD_LOGITS, a number outside [0, 1) that is needed
- * FOPD_DEV_BAD_UNIFORM; that row's (sequence's) token is then -1 with log-prob 0 and mask 0.
+ * where all that is left is that small.  A row that is needed and holds NaN or +infinity, or nothing but
+ * -infinity, sets FOPD_DEV_BAD_LOGITS, a number outside [0, 1) that is needed FOPD_DEV_BAD_UNIFORM; that
+ * row's (sequence's) token is then -1 with log-prob 0 and mask 0.
  */
 
 /*
  * Draws one token from each row: tokens[n] = min { i : sum_{k <= i} p_k > uniform[n] }, the inverse of
- * the distribution function, and logprob[n] = log p_{tokens[n]}, never above 0.  Its error is below 6e-6 (1e-7 is usual) and
- * the fp32 rounding; for p above 0.8 it is below 6e-6 of log p itself, down to 1e-15.
+ * the distribution function, and logprob[n] = log p_{tokens[n]}, never above 0.  Its error is below 6e-6
+ * (1e-7 is usual) and the fp32 rounding; for p above 0.8 it is below 6e-6 of log p itself, down to 1e-15.
  * Neither may lie on uniform (FOPD_ERR_ALIAS) or on the logits.
  *
  *   logits    [n_rows, vocab] at a pitch of row_stride elements, layout rules of fopd_chunk
@@ -531,10 +531,10 @@ int fopd_verify_draft(const fopd_draft *d /* HOST */, int32_t *tokens, float *lo
  *   norm = sqrt(sum g^2),   coef = min(1, max_norm / norm),   out = coef g.
  *
  * Nothing is added to the norm before the division: a set above max_norm comes out with norm max_norm.
- * Squares are formed and summed in fp64 in a fixed order: no overflow, reproducible bit for bit.  Products are formed in fp32 with
- * coef rounded to fp32, and rounded to the type; with a coef below 2^-126, fp32's normal numbers, in fp64 and rounded once.
- * Status and coef go by the fp64 norm, which is finite for any finite set; handed out in fp32, a norm above 3.4e38 is +infinity and a
- * coef below 2^-126 subnormal or 0.
+ * Squares are formed and summed in fp64 in a fixed order: no overflow, reproducible bit for bit.
+ * Products are formed in fp32 with coef rounded to fp32, and rounded to the type; with a coef below 2^-126,
+ * fp32's normal numbers, in fp64 and rounded once.  Status and coef go by the fp64 norm, which is finite for
+ * any finite set; handed out in fp32, a norm above 3.4e38 is +infinity and a coef below 2^-126 subnormal or 0.
  */
 typedef struct {
   const void *data;   /* [rows, cols] at a pitch of row_stride elements; aligned to its element          */

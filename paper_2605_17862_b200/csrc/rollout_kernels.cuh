@@ -917,8 +917,8 @@ __device__ __noinline__ ExactSums cluster_exact_sums(cg::cluster_group &cl, cons
 // The sum of a row without its largest element `at`, in every lane of a warp.  Beside a weight of 1 the fp32 sum of its
 // lane's vectors has lost what the others weigh (2^-24 of the whole); all other sums are free of it and have been added up
 // in fp64.  So that lane's sum is formed again, a lane for each of its elements and in the same order (lane_sum's trees),
-// taken out of the row's, and put back without the element.  (Out of line: 61.5 us for 64
-// sequences with drafts, inlined 62.5.)
+// taken out of the row's, and put back without the element.  (Out of line: 61.5 us for 64 sequences with drafts, inlined
+// 62.5.)
 template <int DT>
 __device__ __noinline__ double sum_beside(const char *row, int64_t V, int32_t at, const RowSum &r, float c) {
   constexpr int P = Elem<DT>::kPerVec;
