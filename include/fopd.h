@@ -569,6 +569,54 @@ int fopd_grad_clip(const fopd_tensor *tensors /* HOST */, int32_t n_tensors, dou
                    float *norm, float *coef, int32_t *status, void *stream);
 
 /*
+ * From hidden states: the log-probs of stored tokens and the gradient of a weighted cross entropy without the logits ever
+ * being kept.  With h_n the hidden state of row n and w_v the head's row of token v:
+ *
+ *   z_nv = h_n . w_v,   lse_n = log sum_v e^{z_nv},   logprob_n = z_{n,y_n} - lse_n           (Sec. 3.1, 4.1)
+ *   L = - sum_n coef_n logprob_n,   G_nv = dL/dz_nv = coef_n (e^{z_nv - lse_n} - 1[v = y_n])
+ *   d_hidden = G W,   d_weight = G^T H
+ *
+ * Uses: the behaviour log-probs of a chunk, rescoring it with another policy, supervised steps (coef_n = 1 / tokens), and every
+ * loss of the stored tokens' log-probs (FOPD_LOSS_SAMPLED_KL has coef_n = coef_i rho_n (log p_t - log p_s - lambda d_n)).
+ * Rows with mask = 0 or a token outside [0, vocab) (FOPD_DEV_BAD_TOKEN) get log-prob, lse and d_hidden +0 and add nothing to
+ * d_weight; with a mask their hidden states may hold anything, and the other rows alone cost time.  Otherwise hidden states and weights
+ * must be finite.  Results do not depend on the run: sums are formed in a fixed order.
+ */
+typedef struct {
+  const void *hidden;    /* [n_rows, dim] at a pitch of hidden_stride elements                       */
+  const void *weight;    /* [vocab, dim] at a pitch of weight_stride elements; bases and pitches of
+                            both in bytes multiples of 16                                            */
+  const int32_t *tokens; /* [n_rows]                                                                 */
+  const uint8_t *mask;   /* [n_rows] 1 = counts, or NULL: all do                                     */
+  int64_t n_rows, vocab, dim; /* n_rows, vocab <= 2^30, dim <= 2^20                                  */
+  int64_t hidden_stride, weight_stride; /* >= dim where there is more than one row                   */
+  int32_t dtype;         /* FOPD_BF16                                                                */
+  int32_t reserved;      /* 0                                                                        */
+} fopd_head;
+
+/* logprob [n_rows] fp32, never above 0, and lse [n_rows] fp32 or NULL.  Products and sums in fp32 (a row's pieces are joined in
+ * fp64); the log-prob of a nearly certain token comes from the sum of the others and keeps its relative accuracy.  The outputs must not lie on the inputs or on
+ * one another. */
+int fopd_head_logprob(const fopd_head *h /* HOST */, float *logprob, float *lse, int32_t *status, void *stream);
+
+/*
+ * The gradient, from what fopd_head_logprob gave for the same inputs: the logits are formed again, piece by piece of the
+ * vocabulary.
+ *
+ *   coef            [n_rows] fp32; rows with coef = 0 add nothing (with a mask they cost nothing either)
+ *   d_hidden        [n_rows, dim] in bf16 at a pitch of d_hidden_stride elements, or NULL
+ *   d_weight        [vocab, dim] in bf16 or fp32 (d_weight_dtype) at its pitch, or NULL (not both); layout rules of weight
+ *   add_d_weight    not 0: d_weight += instead of = (the sum over chunks; in fp32 best)
+ *
+ * G is rounded to bf16 once for the products (2^-9 of each entry at most, of the size of a bf16 result's own rounding); for
+ * a d_weight in fp32 what that leaves is kept and multiplied too (2^-17), which costs that product twice.  The temporary is up to
+ * 1.3 GB and fp32 sums of d_hidden's size, and with a mask a copy of the hidden states.  Outputs must not lie on inputs or on one another.
+ */
+int fopd_head_grad(const fopd_head *h /* HOST */, const float *logprob, const float *lse, const float *coef, void *d_hidden,
+                   int64_t d_hidden_stride, void *d_weight, int64_t d_weight_stride, int32_t d_weight_dtype,
+                   int32_t add_d_weight, int32_t *status, void *stream);
+
+/*
  * Gives back what the library holds on the current device between calls: trims
  * its memory pool to what pending work still uses and destroys the streams and
  * events of fopd_step_host (both come back on the next call that needs them).

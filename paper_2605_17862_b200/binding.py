@@ -24,7 +24,7 @@ EXPORTS = (
     "fopd_refresh_decision", "fopd_shard_stats", "fopd_shard_merge", "fopd_shard_loss_fwd_bwd",
     "fopd_loss_fwd_bwd_set_plan", "fopd_release_device_memory", "fopd_selftest_bounded_wait",
     "fopd_token_stats_student", "fopd_draw_tokens", "fopd_verify_draft", "fopd_grad_norm", "fopd_grad_scale",
-    "fopd_grad_clip",
+    "fopd_grad_clip", "fopd_head_logprob", "fopd_head_grad",
 )
 GRAD_WS = 2048  # doubles of the workspace of fopd_grad_norm, fopd_grad_scale and fopd_grad_clip
 
@@ -67,6 +67,12 @@ class fopd_tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_int64),
                 ("cols", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("dtype", ctypes.c_int32),
                 ("reserved", ctypes.c_int32)]
+
+
+class fopd_head(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("hidden", "weight", "tokens", "mask")] + \
+        [(n, ctypes.c_int64) for n in ("n_rows", "vocab", "dim", "hidden_stride", "weight_stride")] + \
+        [("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -114,6 +120,8 @@ def lib() -> ctypes.CDLL:
         L.fopd_grad_norm.argtypes = [vp, i32, vp, vp, vp, vp]
         L.fopd_grad_scale.argtypes = [vp, i32, vp, f32, vp, vp, vp, vp]
         L.fopd_grad_clip.argtypes = [vp, i32, vp, f32, vp, vp, vp, vp]
+        L.fopd_head_logprob.argtypes = [ctypes.POINTER(fopd_head), vp, vp, vp, vp]
+        L.fopd_head_grad.argtypes = [ctypes.POINTER(fopd_head), vp, vp, vp, vp, i64, vp, i64, i32, i32, vp, vp]
         for name in EXPORTS:
             getattr(L, name)
         _lib = L
@@ -473,6 +481,48 @@ def fopd_grad_clip(grads: GradientList, max_norm, ws, *, norm=None, coef=None, s
     dev = _grad_args(grads, ws)
     _check(lib().fopd_grad_clip(grads.array, grads.n, ws.data_ptr(), max_norm, _scalar(norm, dev),
                                 _scalar(coef, dev), _status_word(status, dev), _stream(stream)), "fopd_grad_clip")
+
+
+def _row_pitch(t, per=8):
+    """Pitch of a matrix whose rows lie whole in memory (a single row: any that the library takes)."""
+    rows, cols = t.shape
+    assert t.stride(1) == 1 or cols <= 1
+    return t.stride(0) if rows > 1 else -(-cols // per) * per
+
+
+def _head(hidden, weight, tokens, mask):
+    _on_current_device(hidden)
+    (n, dim), dev = hidden.shape, hidden.device
+    assert weight.dim() == 2 and weight.shape[1] == dim and weight.device == dev
+    assert hidden.dtype == torch.bfloat16 and weight.dtype == torch.bfloat16
+    assert _flat(tokens, torch.int32, n) and tokens.device == dev
+    return fopd_head(hidden.data_ptr(), weight.data_ptr(), tokens.data_ptr(), _out(mask, torch.uint8, n, dev), n,
+                     weight.shape[0], dim, _row_pitch(hidden), _row_pitch(weight), FOPD_BF16, 0)
+
+
+def fopd_head_logprob(hidden, weight, tokens, logprob, *, lse=None, mask=None, status=None, stream=None):
+    """Log-probs of ``tokens`` int32 [n] under softmax(hidden weight^T) without the logits: ``hidden`` bf16 [n, D],
+    ``weight`` bf16 [V, D] -> ``logprob``, ``lse`` fp32 [n] (the latter may be None).  ``mask`` uint8 [n] or None: rows
+    with 0 are not read and get 0."""
+    h, n, dev = _head(hidden, weight, tokens, mask), hidden.shape[0], hidden.device
+    assert logprob is not None
+    _check(lib().fopd_head_logprob(ctypes.byref(h), _out(logprob, torch.float32, n, dev), _out(lse, torch.float32, n, dev),
+                                   _status_word(status, dev), _stream(stream)), "fopd_head_logprob")
+
+
+def fopd_head_grad(hidden, weight, tokens, logprob, lse, coef, *, d_hidden=None, d_weight=None, add_d_weight=False, mask=None,
+                   status=None, stream=None):
+    """Gradient of -sum coef logprob: ``d_hidden`` bf16 [n, D] and ``d_weight`` bf16 or fp32 [V, D] (either may be None; the
+    latter is added to with ``add_d_weight``), from the ``logprob`` and ``lse`` that fopd_head_logprob gave."""
+    h, (n, dim), dev = _head(hidden, weight, tokens, mask), hidden.shape, hidden.device
+    for t in (logprob, lse, coef):
+        assert _flat(t, torch.float32, n) and t.device == dev
+    assert d_hidden is None or (d_hidden.shape == hidden.shape and d_hidden.dtype == torch.bfloat16 and d_hidden.device == dev)
+    assert d_weight is None or (d_weight.shape == weight.shape and d_weight.device == dev)
+    _check(lib().fopd_head_grad(ctypes.byref(h), logprob.data_ptr(), lse.data_ptr(), coef.data_ptr(), _ptr(d_hidden),
+                                0 if d_hidden is None else _row_pitch(d_hidden), _ptr(d_weight),
+                                0 if d_weight is None else _row_pitch(d_weight), FOPD_BF16 if d_weight is None else _dtype(d_weight),
+                                int(bool(add_d_weight)), _status_word(status, dev), _stream(stream)), "fopd_head_grad")
 
 
 def fopd_check_status(status, stream=None) -> int:

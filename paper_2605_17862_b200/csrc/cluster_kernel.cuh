@@ -43,6 +43,7 @@
 // results of that call are void).
 #pragma once
 
+#include "async.cuh"
 #include "stream_kernels.cuh"
 
 namespace fopd {
@@ -55,132 +56,11 @@ constexpr int kFusedMaxNV = 3, kFusedMaxWarps = 23;
 constexpr int kMaxClusterSize = 16;
 constexpr int kStudentBufs = 2, kTeacherBufs = 3;
 constexpr int kSliceBufs = kStudentBufs + kTeacherBufs;  // slices of shared memory per CTA
-constexpr long long kWaitCycles = 200000000;  // SM cycles one mbarrier wait may take before giving up (~0.1 s)
 // A logit below every real one, as a 32-bit pattern that reads the same way as one fp32 or as
 // two bf16: register slots a thread has no vector for are filled with it, so that they add
 // nothing to the sums (e^(x - max) = 0, x_s - x_t = 0) and need no branch.
 constexpr uint32_t kNoLogitBits = 0xff7fff7fu;
 
-// ------------------------------------------------------------------ PTX wrappers
-__device__ __forceinline__ uint32_t smem_u32(const void *p) {
-  return static_cast<uint32_t>(__cvta_generic_to_shared(p));
-}
-__device__ __forceinline__ uint32_t cluster_ctarank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ uint32_t cluster_nctarank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-// Arrival with release semantics (the default): what the arriving thread read or wrote before
-// it is ordered before whatever the thread that sees the phase complete does next.  Slice
-// buffers are handed back with it (the warp's reads of the buffer, then the arrival; the control
-// warp starts the copy that overwrites the buffer only after it has seen the phase complete).
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-// Stores into another CTA's shared memory that also credit their bytes to an mbarrier of
-// that CTA: the receiver's wait on the barrier covers the data, the sender needs no fence.
-__device__ __forceinline__ void st_async_v4(uint32_t cluster_addr, float a, float b, float c, float d,
-                                            uint32_t cluster_bar) {
-  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
-                   cluster_addr),
-               "f"(a), "f"(b), "f"(c), "f"(d), "r"(cluster_bar)
-               : "memory");
-}
-__device__ __forceinline__ void st_async_f32(uint32_t cluster_addr, float a, uint32_t cluster_bar) {
-  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];" ::"r"(cluster_addr),
-               "f"(a), "r"(cluster_bar)
-               : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n"
-      ".reg .pred p;\n"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-      "selp.u32 %0, 1, 0, p;\n"
-      "}\n"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n"
-      ".reg .pred p;\n"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-      "selp.u32 %0, 1, 0, p;\n"
-      "}\n"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-// Bounded waits: false if the phase did not complete within `limit` SM cycles.  try_wait itself
-// parks the thread for a while, so the loop is kept to the poll and a branch; the clock is
-// read once per kPollsPerClock polls.
-constexpr int kPollsPerClock = 64;
-__device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity, long long limit) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const long long t0 = clock64();
-  do {
-    for (int i = 0; i < kPollsPerClock; ++i)
-      if (mbar_try_wait(bar, parity)) return true;
-  } while (clock64() - t0 <= limit);
-  return false;
-}
-// The same for a warp whose polls should not take issue slots from its neighbours.
-__device__ __forceinline__ bool mbar_wait_bounded_sleeping(uint32_t bar, uint32_t parity, long long limit) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const long long t0 = clock64();
-  do {
-    for (int i = 0; i < kPollsPerClock; ++i) {
-      __nanosleep(64);
-      if (mbar_try_wait(bar, parity)) return true;
-    }
-  } while (clock64() - t0 <= limit);
-  return false;
-}
-__device__ __forceinline__ bool mbar_wait_cluster_bounded(uint32_t bar, uint32_t parity, long long limit) {
-  if (mbar_try_wait_cluster(bar, parity)) return true;
-  const long long t0 = clock64();
-  do {
-    for (int i = 0; i < kPollsPerClock; ++i) {
-      __nanosleep(64);
-      if (mbar_try_wait_cluster(bar, parity)) return true;
-    }
-  } while (clock64() - t0 <= limit);
-  return false;
-}
-__device__ __forceinline__ void bulk_load(uint32_t dst_smem, const void *src, uint32_t bytes, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst_smem),
-      "l"(src), "r"(bytes), "r"(bar)
-      : "memory");
-}
-__device__ __forceinline__ void cluster_arrive() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_wait() {
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t map_to_cta(uint32_t local_smem, uint32_t rank) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(local_smem), "r"(rank));
-  return r;
-}
 __device__ __forceinline__ uint4 lds128(uint32_t addr) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));

@@ -1,0 +1,274 @@
+// Log-probs from hidden states and head weights, and their gradient: argument checks, workspaces, launches.
+#include "head_kernels.cuh"
+#include "tensor_host.cuh"
+
+using namespace fopd;
+
+namespace {
+
+constexpr int64_t kPieceBytes = (int64_t)1 << 30;   // gradient of the logits kept at a time
+constexpr int64_t kSumBytes = (int64_t)256 << 20;   // sums of d_hidden, where the vocabulary is cut into splits
+
+int check_head(const fopd_head *h) {
+  if (!h) return FOPD_ERR_NULL;
+  if (h->dtype != FOPD_BF16) return FOPD_ERR_DTYPE;
+  const int64_t most = (int64_t)1 << 30;
+  if (h->n_rows < 0 || h->vocab <= 0 || h->dim <= 0 || h->n_rows > most || h->vocab > most || h->dim > (1 << 20)) return FOPD_ERR_SIZE;
+  if ((h->n_rows > 1 && h->hidden_stride < h->dim) || (h->vocab > 1 && h->weight_stride < h->dim)) return FOPD_ERR_SIZE;
+  if (h->hidden_stride > (int64_t)1 << 32 || h->weight_stride > (int64_t)1 << 32) return FOPD_ERR_SIZE;
+  if (h->n_rows == 0) return FOPD_OK;
+  if (!h->hidden || !h->weight || !h->tokens) return FOPD_ERR_NULL;
+  if (!aligned16(h->hidden) || !aligned16(h->weight) || (h->n_rows > 1 && h->hidden_stride % 8 != 0) ||
+      (h->vocab > 1 && h->weight_stride % 8 != 0))
+    return FOPD_ERR_ALIGN;
+  return FOPD_OK;
+}
+
+int64_t matrix_bytes(int64_t rows, int64_t cols, int64_t pitch, int64_t size) {
+  return rows > 0 ? ((rows - 1) * pitch + cols) * size : 0;
+}
+bool meets(const void *a, int64_t na, const void *b, int64_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return a && b && na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
+}
+// Whether an output meets one of the arrays that every call reads.
+bool meets_inputs(const fopd_head *h, const void *p, int64_t n) {
+  return meets(p, n, h->hidden, matrix_bytes(h->n_rows, h->dim, h->hidden_stride, 2)) ||
+         meets(p, n, h->weight, matrix_bytes(h->vocab, h->dim, h->weight_stride, 2)) || meets(p, n, h->tokens, h->n_rows * 4) ||
+         meets(p, n, h->mask, h->n_rows);
+}
+
+struct Temporary {
+  char *base = nullptr;
+  cudaStream_t st;
+  explicit Temporary(cudaStream_t s) : st(s) {}
+  int take(int64_t bytes) { return scratch_alloc(reinterpret_cast<void **>(&base), (size_t)bytes, st); }
+  int give(int rc) {
+    if (base && cudaFreeAsync(base, st) != cudaSuccess && rc == FOPD_OK) rc = FOPD_ERR_CUDA;
+    return rc;
+  }
+};
+
+// The rows of a call and where their hidden states are: the caller's, or with a mask a compacted copy.
+struct Prepared {
+  HeadRows rows;
+  CUtensorMap hidden, weight;
+};
+struct RowParts {
+  int64_t index = 0, active = 0, copy = 0;
+};
+RowParts row_parts(const fopd_head *h, Layout *lay) {
+  RowParts r;
+  if (!h->mask) return r;
+  r.index = lay->take(h->n_rows * 4);
+  r.active = lay->take(4);
+  r.copy = lay->take(round_up(h->n_rows, 64) * round_up(h->dim, 8) * 2);
+  return r;
+}
+int prepare_rows(const fopd_head *h, const RowParts &at, char *base, const float *coef, float *logprob, float *lse, int32_t *status,
+                 cudaStream_t st, Prepared *out) {
+  out->rows = {(int)h->n_rows, nullptr, nullptr};
+  const void *hidden = h->hidden;
+  int64_t rows = h->n_rows, pitch = h->n_rows > 1 ? h->hidden_stride : round_up(h->dim, 8);
+  if (h->mask) {
+    int *index = reinterpret_cast<int *>(base + at.index), *active = reinterpret_cast<int *>(base + at.active);
+    __nv_bfloat16 *copy = reinterpret_cast<__nv_bfloat16 *>(base + at.copy);
+    head_index_kernel<<<1, kHeadIndexThreads, 0, st>>>(h->mask, h->tokens, coef, (int)h->n_rows, h->vocab, index, active, logprob,
+                                                       lse, status);
+    rows = round_up(h->n_rows, 64);
+    head_gather_kernel<<<(unsigned)((rows + 7) / 8), 256, 0, st>>>(static_cast<const __nv_bfloat16 *>(h->hidden), pitch, index, active,
+                                                                    (int)h->dim, (int)round_up(h->dim, 8), copy);
+    if (launch_ok() != FOPD_OK) return FOPD_ERR_CUDA;
+    out->rows.index = index;
+    out->rows.active = active;
+    hidden = copy;
+    pitch = round_up(h->dim, 8);
+  }
+  int rc = make_map(&out->hidden, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, hidden, h->dim, rows, pitch * 2, 64, kBoxRows, true);
+  if (rc == FOPD_OK)
+    rc = make_map(&out->weight, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, h->weight, h->dim, h->vocab,
+                  (h->vocab > 1 ? h->weight_stride : round_up(h->dim, 8)) * 2, 64, kBoxRows, true);
+  return rc;
+}
+
+template <int kCtas, int kN>
+int run_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *status, int sms, cudaStream_t st) {
+  const int64_t v_tiles = (h->vocab + kN - 1) / kN, pitch = round_up(h->n_rows, kCtas * 128);
+  Layout lay;
+  const RowParts parts = row_parts(h, &lay);
+  const int64_t part = lay.take(v_tiles * pitch * 8), logit = lay.take(pitch * 4);
+  Temporary tmp(st);
+  int rc = tmp.take(lay.bytes);
+  if (rc != FOPD_OK) return rc;
+  Prepared pre;
+  rc = prepare_rows(h, parts, tmp.base, nullptr, logprob, lse, status, st, &pre);
+  if (rc == FOPD_OK) {
+    typename LogprobJob<kCtas, kN>::Params p;
+    p.hidden = pre.hidden;
+    p.weight = pre.weight;
+    p.l = {nullptr, nullptr, pre.rows, h->vocab, (int)((h->dim + 63) / 64), 0, (int)v_tiles};
+    p.tokens = h->tokens;
+    p.part = reinterpret_cast<float2 *>(tmp.base + part);
+    p.token_logit = reinterpret_cast<float *>(tmp.base + logit);
+    p.pitch = (int)pitch;
+    p.status = status;
+    rc = launch_product<kCtas, kN, LogprobJob>(p, pitch / (kCtas * 128) * v_tiles, sms, st);
+    if (rc == FOPD_OK) {
+      head_join_kernel<<<(unsigned)((h->n_rows + 31) / 32), 1024, 0, st>>>(pre.rows, p.part, p.token_logit, (int)v_tiles, (int)pitch,
+                                                                           h->tokens, h->vocab, logprob, lse, status);
+      rc = launch_ok();
+    }
+  }
+  return tmp.give(rc);
+}
+
+struct GradOut {
+  void *d_hidden;
+  int64_t d_hidden_stride;
+  void *d_weight;
+  int64_t d_weight_stride;
+  int32_t d_weight_dtype, add;
+};
+
+template <int kCtas, int kN>
+int run_grad(const fopd_head *h, const float *logprob, const float *lse, const float *coef, const GradOut &o, int32_t *status, int sms,
+             cudaStream_t st) {
+  constexpr int kRows = kCtas * 128;
+  const int64_t pitch = round_up(h->n_rows, kRows);
+  const int planes = o.d_weight && o.d_weight_dtype == FOPD_F32 ? 2 : 1;
+  // pieces of the vocabulary, alike, of whole tiles of both products that cut it
+  constexpr int64_t kUnit = kN > kRows ? kN : kRows;
+  int64_t piece = kPieceBytes / (pitch * 2 * planes) / kUnit * kUnit;
+  if (piece < kUnit) piece = kUnit;
+  const int64_t n_pieces = (h->vocab + piece - 1) / piece;
+  piece = round_up((h->vocab + n_pieces - 1) / n_pieces, kUnit);
+  const int64_t panels = piece / 64, lo = planes > 1 ? panels * pitch : 0;
+  if (panels * pitch * planes >= (int64_t)1 << 31) return FOPD_ERR_SIZE;  // (n_rows beyond 2^28)
+
+  // splits of d_hidden's contraction: no tile longer than a quarter of a CTA's share of the piece's work, where the sums fit
+  const int64_t d_tiles = (h->dim + kN - 1) / kN, h_tiles = pitch / kRows * d_tiles, w_tiles = piece / kRows * d_tiles;
+  const int64_t share = ((o.d_hidden ? h_tiles * panels : 0) + (o.d_weight ? w_tiles * planes * ((h->n_rows + 63) / 64) : 0)) / (sms / kCtas);
+  int64_t split_panels = share / 4 > 8 ? share / 4 : 8;
+  const int64_t sum_pitch = round_up(h->dim, 32), sum_each = pitch * sum_pitch * 4;
+  int64_t splits = (panels + split_panels - 1) / split_panels;
+  if (splits > kSumBytes / sum_each) splits = kSumBytes / sum_each;
+  if (splits < 1) splits = 1;
+  split_panels = (panels + splits - 1) / splits;
+  splits = (panels + split_panels - 1) / split_panels;
+  if (!o.d_hidden) splits = 0;
+
+  Layout lay;
+  const RowParts parts = row_parts(h, &lay);
+  const int64_t g_at = lay.take(panels * pitch * planes * 128), sum_at = lay.take(splits * sum_each);
+  Temporary tmp(st);
+  int rc = tmp.take(lay.bytes);
+  if (rc != FOPD_OK) return rc;
+  Prepared pre;
+  rc = prepare_rows(h, parts, tmp.base, coef, nullptr, nullptr, status, st, &pre);
+  typename GradLogitsJob<kCtas, kN>::Params g;
+  typename HeadGradsJob<kCtas, kN>::Params q;
+  if (rc == FOPD_OK)
+    rc = make_map(&g.panels_out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, 32, true);
+  if (rc == FOPD_OK)
+    rc = make_map(&q.panels, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, kBoxRows, true);
+  if (rc == FOPD_OK && o.d_hidden && h->mask &&
+      cudaMemset2DAsync(o.d_hidden, (size_t)(h->n_rows > 1 ? o.d_hidden_stride : round_up(h->dim, 8)) * 2, 0, (size_t)h->dim * 2,
+                        (size_t)h->n_rows, st) != cudaSuccess)
+    rc = FOPD_ERR_CUDA;
+  if (rc == FOPD_OK) {
+    g.hidden = q.hidden = pre.hidden;
+    g.weight = q.weight = pre.weight;
+    g.tokens = h->tokens;
+    g.logprob = logprob;
+    g.lse = lse;
+    g.coef = coef;
+    g.pitch = q.pitch = (int)pitch;
+    g.lo = q.lo = (int)lo;
+    g.status = q.status = status;
+    q.rows = pre.rows;
+    q.vocab = h->vocab;
+    q.dim = (int)h->dim;
+    q.splits = (int)splits;
+    q.split_panels = (int)split_panels;
+    q.sum = reinterpret_cast<float *>(tmp.base + sum_at);
+    q.sum_pitch = (int)sum_pitch;
+    q.d_weight = o.d_weight;
+    q.d_weight_pitch = o.d_weight_stride;
+    q.d_weight_f32 = o.d_weight_dtype == FOPD_F32;
+    q.add = o.add;
+    for (int64_t v0 = 0; rc == FOPD_OK && v0 < h->vocab; v0 += piece) {
+      const int64_t count = h->vocab - v0 < piece ? h->vocab - v0 : piece;
+      g.l = {nullptr, nullptr, pre.rows, h->vocab, (int)((h->dim + 63) / 64), (int)(v0 / kN), (int)((count + kN - 1) / kN)};
+      q.v0 = v0;
+      q.v_count = (int)count;
+      q.first = v0 == 0;
+      rc = launch_product<kCtas, kN, GradLogitsJob>(g, pitch / kRows * g.l.v_tiles, sms, st);
+      if (rc == FOPD_OK)
+        rc = launch_product<kCtas, kN, HeadGradsJob>(q, splits * h_tiles + (o.d_weight ? (count + kRows - 1) / kRows * d_tiles : 0), sms, st);
+    }
+  }
+  if (rc == FOPD_OK && o.d_hidden) {
+    head_hidden_kernel<<<row_grid(h->n_rows), 128, 0, st>>>(
+        pre.rows, q.sum, (int)splits, (int)pitch, (int)sum_pitch, h->tokens, logprob, coef, static_cast<const __nv_bfloat16 *>(h->weight),
+        h->weight_stride, h->vocab, (int)h->dim, o.d_hidden_stride, static_cast<__nv_bfloat16 *>(o.d_hidden));
+    rc = launch_ok();
+  }
+  return tmp.give(rc);
+}
+
+}  // namespace
+
+extern "C" {
+
+int fopd_head_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *status, void *stream) {
+  int rc = check_head(h);
+  if (rc != FOPD_OK || h->n_rows == 0) return rc;
+  if (!logprob) return FOPD_ERR_NULL;
+  const int64_t n = h->n_rows * 4;
+  if (meets_inputs(h, logprob, n) || meets_inputs(h, lse, n) || meets(logprob, n, lse, n)) return FOPD_ERR_ALIAS;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int sms = 0;
+  rc = current_sms(&sms);
+  if (rc != FOPD_OK) return rc;
+  return h->n_rows <= 128 ? run_logprob<1, 256>(h, logprob, lse, status, sms, st) : run_logprob<2, 256>(h, logprob, lse, status, sms, st);
+}
+
+int fopd_head_grad(const fopd_head *h, const float *logprob, const float *lse, const float *coef, void *d_hidden,
+                   int64_t d_hidden_stride, void *d_weight, int64_t d_weight_stride, int32_t d_weight_dtype, int32_t add_d_weight,
+                   int32_t *status, void *stream) {
+  int rc = check_head(h);
+  if (rc != FOPD_OK) return rc;
+  if (!d_hidden && !d_weight) return FOPD_ERR_NULL;
+  if (d_weight && d_weight_dtype != FOPD_BF16 && d_weight_dtype != FOPD_F32) return FOPD_ERR_DTYPE;
+  const int64_t wsize = d_weight_dtype == FOPD_F32 ? 4 : 2;
+  if (d_hidden && h->n_rows > 1 && d_hidden_stride < h->dim) return FOPD_ERR_SIZE;
+  if (d_weight && h->vocab > 1 && d_weight_stride < h->dim) return FOPD_ERR_SIZE;
+  if (d_hidden_stride > (int64_t)1 << 32 || d_weight_stride > (int64_t)1 << 32) return FOPD_ERR_SIZE;
+  if (!aligned16(d_hidden) || !aligned16(d_weight) || (d_hidden && h->n_rows > 1 && d_hidden_stride % 8 != 0) ||
+      (d_weight && h->vocab > 1 && d_weight_stride * wsize % 16 != 0))
+    return FOPD_ERR_ALIGN;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (h->n_rows == 0) {  // no row: the weights' gradient is zero
+    if (d_weight && !add_d_weight &&
+        cudaMemset2DAsync(d_weight, (size_t)(h->vocab > 1 ? d_weight_stride : h->dim) * wsize, 0, (size_t)(h->dim * wsize), (size_t)h->vocab,
+                          st) != cudaSuccess) {
+      (void)cudaGetLastError();
+      return FOPD_ERR_CUDA;
+    }
+    return FOPD_OK;
+  }
+  if (!logprob || !lse || !coef) return FOPD_ERR_NULL;
+  const int64_t nh = d_hidden ? matrix_bytes(h->n_rows, h->dim, d_hidden_stride, 2) : 0;
+  const int64_t nw = d_weight ? matrix_bytes(h->vocab, h->dim, d_weight_stride, wsize) : 0, n = h->n_rows * 4;
+  for (const void *in : {(const void *)logprob, (const void *)lse, (const void *)coef})
+    if (meets(d_hidden, nh, in, n) || meets(d_weight, nw, in, n)) return FOPD_ERR_ALIAS;
+  if (meets_inputs(h, d_hidden, nh) || meets_inputs(h, d_weight, nw) || meets(d_hidden, nh, d_weight, nw)) return FOPD_ERR_ALIAS;
+  int sms = 0;
+  rc = current_sms(&sms);
+  if (rc != FOPD_OK) return rc;
+  const GradOut o = {d_hidden, d_hidden_stride, d_weight, d_weight_stride, d_weight_dtype, add_d_weight ? 1 : 0};
+  return h->n_rows <= 128 ? run_grad<1, 256>(h, logprob, lse, coef, o, status, sms, st)
+                          : run_grad<2, 256>(h, logprob, lse, coef, o, status, sms, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,378 @@
+// Tensor-core products on sm_100a: PTX wrappers and the one kernel that every matrix product of the library runs in.
+//
+// A job (a struct with tile() and epilogue()) says what is multiplied and what becomes of the result.  The kernel stays on
+// the SM and takes tiles of kCtas * 128 x kN results in turn.  Warp 0 brings operand blocks in by TMA (64 of the contraction
+// at a time, 128-byte swizzle) through a ring of stages; one thread of warp 1 issues tcgen05.mma from there into one of two
+// accumulators in TMEM; warps 4 to 7 take the finished accumulator out, so that a tile's epilogue runs beside the next
+// tile's products.  With kCtas = 2 a pair of CTAs works on one tile: each holds half of both operands and half the
+// accumulator's rows, and shared memory is read once for twice the products (cta_group::2; 64 instead of 96 bytes per SM and
+// cycle at 256 columns, which with the copies coming in is what 1-CTA tiles are short of).
+//
+// Operands are 16-bit (both bf16 or both fp16), products and sums fp32.  Either operand may lie with the contraction along
+// its rows ("K-major") or across them; both come in boxes of 64 rows x 64 elements, so that one tensor map serves both.
+//
+// Every wait is bounded.  One that runs out raises a flag, the role leaves its loop, the others run out in turn, copies and
+// products in flight are waited for (again with a limit), TMEM is given back, FOPD_DEV_TIMEOUT goes to the status word.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_fp16.h>
+
+#include "async.cuh"
+#include "common.cuh"
+
+namespace fopd {
+
+// ------------------------------------------------------------------ TMA
+template <int kCtas>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+  if constexpr (kCtas == 2)  // (the barrier may be the other CTA's)
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y),
+               "r"(src)
+               : "memory");
+}
+__device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int kPending>
+__device__ __forceinline__ void tma_store_wait_read() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kPending) : "memory");
+}
+__device__ __forceinline__ void tma_store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
+// ------------------------------------------------------------------ TMEM and tcgen05
+template <int kCtas>
+__device__ __forceinline__ void tmem_alloc(uint32_t dst, uint32_t cols) {
+  if constexpr (kCtas == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+}
+template <int kCtas>
+__device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t cols) {
+  if constexpr (kCtas == 2)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
+  else
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+template <int kCtas>
+__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  if constexpr (kCtas == 2)
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+        : "memory");
+}
+// One arrival on the barrier at this offset, in both CTAs of a pair, once all products issued so far are done.
+template <int kCtas>
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+  if constexpr (kCtas == 2)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                 "h"((uint16_t)3)
+                 : "memory");
+  else
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// 32 columns of this warp's 32 rows: lane = row.  The values are there after tmem_wait on the same array.
+__device__ __forceinline__ void tmem_load(uint32_t (&r)[32], uint32_t addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, "
+      "[%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr));
+}
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[32]) {  // (the operands keep uses of the values behind the wait)
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
+                 "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
+                 "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+
+// ------------------------------------------------------------------ tiles
+constexpr int kBoxRows = 64;                    // rows of one TMA box of 64 16-bit elements
+constexpr int kBoxBytes = kBoxRows * 128;
+constexpr int kProductThreads = 256;
+constexpr int kEpilogueWarp0 = 4, kEpilogueWarps = 4;
+constexpr int kStageBufBytes = 32 * 128;        // an epilogue warp's staging buffer: its 32 rows x 128 bytes
+constexpr int kStageBufs = 2;
+constexpr uint32_t kTmemCols = 512;
+
+// One operand of a tile: where its boxes are.
+struct Operand {
+  const CUtensorMap *map;
+  int x, y;    // the first box of this CTA's part
+  int kx, ky;  // from one block of 64 along the contraction to the next
+  int cx, cy;  // from one box to the next across it
+  int lo;      // rows from a plane of the values to the plane of what their rounding left (two-plane operands)
+  bool across; // the contraction runs across the rows of the boxes
+};
+
+// The contraction may run over several pairs of planes: pass i takes a's second plane where bit i of a_lo is set, etc.
+struct Tile {
+  Operand a, b;
+  int k_blocks;  // 0: the product is zero
+  int passes;
+  uint32_t a_lo, b_lo;
+};
+
+__device__ __forceinline__ uint64_t smem_descriptor(uint32_t addr, bool across) {
+  // 128-byte swizzle: groups of 8 rows of 128 bytes, 1,024 bytes apart; across: 64 rows further is the next box
+  const uint64_t lbo = across ? kBoxBytes >> 4 : 1, sbo = 1024 >> 4;
+  return (uint64_t)((addr & 0x3ffff) >> 4) | (lbo << 16) | (sbo << 32) | (1ull << 46) | (2ull << 61);
+}
+
+template <int kCtas, int kN>
+struct ProductShape {
+  static constexpr int kBCols = kN / kCtas;  // of the tile's columns, this CTA's operand share
+  static constexpr int kABoxes = 128 / kBoxRows, kBBoxes = kBCols / kBoxRows;
+  static constexpr int kStageBytes = (kABoxes + kBBoxes) * kBoxBytes;
+  static constexpr int kStages = 192 * 1024 / kStageBytes;
+  static constexpr int kSmem = kStages * kStageBytes + kEpilogueWarps * kStageBufs * kStageBufBytes + 1024;
+};
+
+struct ProductShared {
+  unsigned long long full[8], empty[8], acc_full[2], acc_empty[2], drain;
+  uint32_t tmem;
+  int failed;
+};
+
+// What an epilogue warp is given.
+struct Accumulator {
+  uint32_t addr;     // TMEM address of the warp's 32 rows
+  int warp, lane;    // rows warp * 32 + lane of this CTA's 128
+  uint32_t staging;  // two staging buffers
+  bool zero;         // the product is zero, TMEM holds nothing
+};
+__device__ __forceinline__ void load_columns(const Accumulator &acc, int col, uint32_t (&r)[32]) {
+  if (acc.zero) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) r[i] = 0;
+    return;
+  }
+  tmem_load(r, acc.addr + col);
+  tmem_wait(r);
+}
+
+// Job: Params (a kernel parameter); Job(params); int64_t tiles(); void tile(int64_t i, int cta, Tile &);
+// void epilogue(int64_t i, int cta, const Accumulator &); int32_t *status(); static constexpr bool kFp16.
+template <int kCtas, int kN, class Job>
+__global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ typename Job::Params params) {
+  using Shape = ProductShape<kCtas, kN>;
+  extern __shared__ uint8_t product_smem[];
+  __shared__ ProductShared sh;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t base = (smem_u32(product_smem) + 1023u) & ~1023u;
+  const uint32_t staging = base + Shape::kStages * Shape::kStageBytes;
+  const int cta = kCtas == 2 ? (int)cluster_ctarank() : 0;
+  const int64_t first = blockIdx.x / kCtas, step = gridDim.x / kCtas;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < Shape::kStages; ++i) {
+      mbar_init(smem_u32(&sh.full[i]), 1);
+      mbar_init(smem_u32(&sh.empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&sh.acc_full[i]), 1);
+      mbar_init(smem_u32(&sh.acc_empty[i]), kCtas * kEpilogueWarps);
+    }
+    mbar_init(smem_u32(&sh.drain), 1);
+    sh.failed = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) tmem_alloc<kCtas>(smem_u32(&sh.tmem), kTmemCols);
+  tc_fence_before();
+  __syncthreads();
+  if constexpr (kCtas == 2) {
+    cluster_arrive();
+    cluster_wait();
+  }
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem;
+
+  Job job(params);
+  const int64_t n_tiles = job.tiles();
+
+  if (warp == 0) {
+    if (lane == 0) {
+      // ---- copies in
+      int stage = 0, used = 0;
+      uint32_t parity = 1;
+      bool ok = true;
+      for (int64_t i = first; ok && i < n_tiles; i += step) {
+        Tile t;
+        job.tile(i, cta, t);
+        for (int pass = 0; ok && pass < t.passes; ++pass) {
+          const int ya = t.a.y + ((t.a_lo >> pass & 1) ? t.a.lo : 0), yb = t.b.y + ((t.b_lo >> pass & 1) ? t.b.lo : 0);
+          for (int k = 0; k < t.k_blocks; ++k) {
+            if (!mbar_wait_bounded(smem_u32(&sh.empty[stage]), parity, kWaitCycles)) {
+              ok = false;
+              break;
+            }
+            uint32_t full = smem_u32(&sh.full[stage]);
+            if (cta == 0) mbar_expect_tx(full, kCtas * Shape::kStageBytes);
+            if constexpr (kCtas == 2) full = map_to_cta(full, 0);
+            uint32_t dst = base + stage * Shape::kStageBytes;
+#pragma unroll
+            for (int c = 0; c < Shape::kABoxes; ++c, dst += kBoxBytes)
+              tma_load<kCtas>(dst, t.a.map, t.a.x + k * t.a.kx + c * t.a.cx, ya + k * t.a.ky + c * t.a.cy, full);
+#pragma unroll
+            for (int c = 0; c < Shape::kBBoxes; ++c, dst += kBoxBytes)
+              tma_load<kCtas>(dst, t.b.map, t.b.x + k * t.b.kx + c * t.b.cx, yb + k * t.b.ky + c * t.b.cy, full);
+            if (used < Shape::kStages) ++used;
+            if (++stage == Shape::kStages) {
+              stage = 0;
+              parity ^= 1;
+            }
+          }
+        }
+      }
+      // Before this CTA may end, the stages it filled have been read (their last arrivals are in): behind the copies.
+      for (int i = 0; i < used; ++i) {
+        if (stage == 0) parity ^= 1;
+        stage = stage == 0 ? Shape::kStages - 1 : stage - 1;
+        if (!mbar_wait_bounded(smem_u32(&sh.empty[stage]), parity ^ 1, kWaitCycles)) ok = false;
+      }
+      if (!ok) sh.failed = 1;
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && cta == 0) {
+      // ---- products
+      int stage = 0;
+      uint32_t parity = 0, n = 0;
+      bool ok = true;
+      for (int64_t i = first; ok && i < n_tiles; i += step, ++n) {
+        Tile t;
+        job.tile(i, cta, t);
+        const uint32_t idesc = (1u << 4) | (Job::kFp16 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)t.a.across << 15) |
+                               ((uint32_t)t.b.across << 16) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(kCtas * 128 >> 4) << 24);
+        const uint32_t a_step = (t.a.across ? 16 * 128 : 32) >> 4, b_step = (t.b.across ? 16 * 128 : 32) >> 4;
+        const uint32_t buf = n & 1, d = tmem + buf * kN;
+        if (!mbar_wait_bounded(smem_u32(&sh.acc_empty[buf]), ((n >> 1) & 1) ^ 1, kWaitCycles)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const int blocks = t.passes * t.k_blocks;
+        for (int k = 0; k < blocks; ++k) {
+          if (!mbar_wait_bounded(smem_u32(&sh.full[stage]), parity, kWaitCycles)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t at = base + stage * Shape::kStageBytes;
+          const uint64_t a = smem_descriptor(at, t.a.across), b = smem_descriptor(at + Shape::kABoxes * kBoxBytes, t.b.across);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) tc_mma<kCtas>(d, a + j * a_step, b + j * b_step, idesc, k > 0 || j > 0);
+          tc_commit<kCtas>(smem_u32(&sh.empty[stage]));
+          if (++stage == Shape::kStages) {
+            stage = 0;
+            parity ^= 1;
+          }
+        }
+        if (ok) tc_commit<kCtas>(smem_u32(&sh.acc_full[buf]));
+      }
+      if (!ok) {  // let what has been issued end
+        sh.failed = 1;
+        tc_commit<kCtas>(smem_u32(&sh.drain));
+        mbar_wait_bounded(smem_u32(&sh.drain), 0, kWaitCycles);
+      }
+    }
+  } else if (warp >= kEpilogueWarp0) {
+    // ---- results out
+    Accumulator acc;
+    acc.warp = warp - kEpilogueWarp0;
+    acc.lane = lane;
+    acc.staging = staging + acc.warp * kStageBufs * kStageBufBytes;
+    uint32_t n = 0;
+    bool ok = true;
+    for (int64_t i = first; ok && i < n_tiles; i += step, ++n) {
+      const uint32_t buf = n & 1;
+      Tile t;
+      job.tile(i, cta, t);
+      if (!mbar_wait_bounded(smem_u32(&sh.acc_full[buf]), (n >> 1) & 1, kWaitCycles)) ok = false;
+      if (!__all_sync(0xffffffffu, ok)) {
+        ok = false;
+        sh.failed = 1;
+        break;
+      }
+      tc_fence_after();
+      acc.addr = tmem + buf * kN + ((uint32_t)(acc.warp * 32) << 16);
+      acc.zero = t.k_blocks == 0;
+      job.template epilogue<kN>(i, cta, acc);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        const uint32_t bar = smem_u32(&sh.acc_empty[buf]);
+        if constexpr (kCtas == 2) mbar_arrive_cluster(map_to_cta(bar, 0));
+        else mbar_arrive(bar);
+      }
+    }
+    if (lane == 0) tma_store_wait_all();
+  }
+
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if constexpr (kCtas == 2) {
+    cluster_arrive();
+    cluster_wait();
+  }
+  tc_fence_after();
+  if (warp == 2) tmem_free<kCtas>(tmem, kTmemCols);
+  if (threadIdx.x == 0 && sh.failed && job.status()) atomicOr(job.status(), FOPD_DEV_TIMEOUT);
+}
+
+// ------------------------------------------------------------------ results into rows of 64 16-bit elements
+// A warp's 32 rows x 64 results as a 128-byte-swizzled box, stored by TMA.
+template <class Convert>  // uint32_t Convert(float a, float b): two 16-bit results
+__device__ __forceinline__ void stage_half_box(uint32_t buf, int lane, int half, const float (&v)[32], Convert convert) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = convert(v[8 * j + 2 * e], v[8 * j + 2 * e + 1]);
+    const uint32_t piece = (uint32_t)(half * 4 + j) ^ (lane & 7);
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(buf + lane * 128 + piece * 16), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                 "r"(w[3])
+                 : "memory");
+  }
+}
+
+}  // namespace fopd
