@@ -617,6 +617,42 @@ int fopd_head_grad(const fopd_head *h /* HOST */, const float *logprob, const fl
                    int32_t add_d_weight, int32_t *status, void *stream);
 
 /*
+ * Orthogonalised updates: for every matrix M of a list (a layer's momentum, as a rule),
+ *
+ *   X = M / (|M|_F + eps);   for each step (a, b, c):  X <- (a I + b A + c A^2) X,  A = X X^T;   out = scale X
+ *
+ * (the Newton-Schulz products that take singular values s to a s + b s^3 + c s^5, towards one: the step of an optimiser that
+ * takes the orthogonal factor of its momentum for the update; customary are five steps of (3.4445, -4.7750, 2.0315), eps = 1e-7).
+ * Wide, tall and square matrices, any sizes and pitches, all in one call.
+ *
+ * The norm is summed in fp64.  X, A and their polynomial are held in fp16 under powers of two, 11 bits and two planes where roundings would be
+ * amplified by 32 or more; matrices whose result is fp32 in two planes throughout (22 bits; three products for each).  Products
+ * and sums are fp32.  Results do not depend on the run.  A matrix of zeros gives zeros; one that holds an infinity or NaN
+ * gives NaN and sets FOPD_DEV_NONFINITE, the others are not affected.  One whose norm is so far below eps that X's elements are
+ * below 2^-39 loses them.
+ */
+typedef struct {
+  const void *data;     /* [rows, cols] at a pitch of row_stride elements; aligned to its element          */
+  void *out;            /* where the result goes, at out_stride; may be data with the same type and pitch   */
+  int64_t rows, cols;   /* <= 2^24 each; or 0: nothing is done                                               */
+  int64_t row_stride, out_stride; /* >= cols where rows > 1                                                  */
+  float scale;          /* of the result, finite                                                             */
+  int32_t dtype, out_dtype; /* fopd_dtype, matrix by matrix                                                  */
+  int32_t reserved;     /* 0                                                                                 */
+} fopd_matrix;
+
+/*
+ *   coefficients   HOST [steps, 3], finite; 1 <= steps <= 16.  FOPD_ERR_PARAM where singular values of at most one would grow
+ *                  beyond 10^6.
+ *   eps            >= 0, finite
+ *
+ * The temporary is up to eight bytes per element of the list (twelve for fp32 results), in groups of 1 GiB or one matrix.  No
+ * result may overlap a matrix of the list or another result, as for fopd_grad_scale; in place it is allowed.
+ */
+int fopd_orthogonalise(const fopd_matrix *matrices /* HOST */, int32_t n_matrices, const float *coefficients /* HOST */,
+                       int32_t steps, float eps, int32_t *status, void *stream);
+
+/*
  * Gives back what the library holds on the current device between calls: trims
  * its memory pool to what pending work still uses and destroys the streams and
  * events of fopd_step_host (both come back on the next call that needs them).

@@ -24,7 +24,7 @@ EXPORTS = (
     "fopd_refresh_decision", "fopd_shard_stats", "fopd_shard_merge", "fopd_shard_loss_fwd_bwd",
     "fopd_loss_fwd_bwd_set_plan", "fopd_release_device_memory", "fopd_selftest_bounded_wait",
     "fopd_token_stats_student", "fopd_draw_tokens", "fopd_verify_draft", "fopd_grad_norm", "fopd_grad_scale",
-    "fopd_grad_clip", "fopd_head_logprob", "fopd_head_grad",
+    "fopd_grad_clip", "fopd_head_logprob", "fopd_head_grad", "fopd_orthogonalise",
 )
 GRAD_WS = 2048  # doubles of the workspace of fopd_grad_norm, fopd_grad_scale and fopd_grad_clip
 
@@ -75,6 +75,12 @@ class fopd_head(ctypes.Structure):
         [("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class fopd_matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p)] + \
+        [(n, ctypes.c_int64) for n in ("rows", "cols", "row_stride", "out_stride")] + \
+        [("scale", ctypes.c_float), ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -122,6 +128,7 @@ def lib() -> ctypes.CDLL:
         L.fopd_grad_clip.argtypes = [vp, i32, vp, f32, vp, vp, vp, vp]
         L.fopd_head_logprob.argtypes = [ctypes.POINTER(fopd_head), vp, vp, vp, vp]
         L.fopd_head_grad.argtypes = [ctypes.POINTER(fopd_head), vp, vp, vp, vp, i64, vp, i64, i32, i32, vp, vp]
+        L.fopd_orthogonalise.argtypes = [vp, i32, vp, i32, f32, vp, vp]
         for name in EXPORTS:
             getattr(L, name)
         _lib = L
@@ -523,6 +530,57 @@ def fopd_head_grad(hidden, weight, tokens, logprob, lse, coef, *, d_hidden=None,
                                 0 if d_hidden is None else _row_pitch(d_hidden), _ptr(d_weight),
                                 0 if d_weight is None else _row_pitch(d_weight), FOPD_BF16 if d_weight is None else _dtype(d_weight),
                                 int(bool(add_d_weight)), _status_word(status, dev), _stream(stream)), "fopd_head_grad")
+
+
+class MatrixList:
+    """The matrices of an fopd_orthogonalise call, marshalled once: keep it as long as they keep their memory (it holds them).
+    bf16 and fp32, mixed; the last two dimensions are a matrix's rows and columns, those before them count matrices.  Rows lie
+    whole in memory, or columns do (a transposed matrix: the result is transposed as well).  ``outs``: where the results go (same
+    shapes, bf16 or fp32, same order of dimensions in memory); None: in place.  ``scales``: of the results, one per tensor."""
+
+    def __init__(self, tensors, outs=None, scales=None):
+        self.tensors, self.outs = list(tensors), None if outs is None else list(outs)
+        scales = [1.0] * len(self.tensors) if scales is None else [float(s) for s in scales]
+        assert len(scales) == len(self.tensors) and (self.outs is None or len(self.outs) == len(self.tensors))
+        self.device = self.tensors[0].device if self.tensors else None
+        items = []
+        for i, t in enumerate(self.tensors):
+            o = t if self.outs is None else self.outs[i]
+            _on_current_device(t)
+            assert t.device == self.device == o.device and t.dim() >= 2 and o.shape == t.shape, i
+            t, o = t.detach(), o.detach()
+            if t.shape[-1] > 1 and t.stride(-1) != 1:  # columns whole: the transposed matrix
+                t, o = t.mT, o.mT
+            rows, cols = t.shape[-2:]
+            for x in (t, o):
+                assert cols <= 1 or x.stride(-1) == 1, f"matrix {i}: strides {x.stride()} of shape {tuple(x.shape)}"
+            if t.numel() == 0:
+                continue
+            # (of a single column the pitch is what counts, of a single row nothing)
+            pitches = [x.stride(-2) if rows > 1 else cols for x in (t, o)]
+            lead = [()]
+            for n in t.shape[:-2]:
+                lead = [k + (j,) for k in lead for j in range(n)]
+            for k in lead:
+                at = [x.data_ptr() + x.element_size() * sum(a * b for a, b in zip(k, x.stride())) for x in (t, o)]
+                items.append(fopd_matrix(at[0], at[1], rows, cols, pitches[0], pitches[1], scales[i], _dtype(t), _dtype(o), 0))
+        self.n = len(items)
+        self.array = (fopd_matrix * max(1, self.n))(*items)
+
+
+NEWTON_SCHULZ_COEFFICIENTS = ((3.4445, -4.7750, 2.0315),) * 5
+
+
+def fopd_orthogonalise(matrices: MatrixList, *, coefficients=NEWTON_SCHULZ_COEFFICIENTS, eps=1e-7, status=None, stream=None):
+    """Every matrix of the list through the Newton-Schulz steps of ``coefficients`` (a, b, c): out = scale times its orthogonal
+    factor, nearly (see ``fopd_orthogonalise`` in fopd.h)."""
+    flat = [float(x) for step in coefficients for x in step]
+    assert len(flat) == 3 * len(coefficients)
+    dev = matrices.device
+    if dev is not None:
+        assert dev.index == torch._C._cuda_getDevice(), dev
+    _check(lib().fopd_orthogonalise(matrices.array, matrices.n, (ctypes.c_float * max(1, len(flat)))(*flat), len(coefficients), eps,
+                                    None if dev is None else _status_word(status, dev), _stream(stream)), "fopd_orthogonalise")
 
 
 def fopd_check_status(status, stream=None) -> int:

@@ -1,10 +1,9 @@
 // Gradient norm and clipping: argument checks, the set's table, launches.
-#include <algorithm>
-#include <numeric>
 #include <vector>
 
 #include "clip_kernels.cuh"
 #include "host_common.cuh"
+#include "host_ranges.cuh"
 
 using namespace fopd;
 
@@ -30,64 +29,18 @@ int check_tensors(const fopd_tensor *t, int32_t n, const double *ws) {
   return FOPD_OK;
 }
 
-struct Range {
-  uintptr_t lo, hi, row;  // row: pitch in bytes (0: one row, or rows without a gap)
-  uintptr_t width;        // bytes of a row
-  int32_t tensor;
-  bool written;
-};
-
-Range range_of(const fopd_tensor &t, const void *p, int32_t i, bool written) {
-  const bool dense = t.rows == 1 || t.row_stride == t.cols;
-  const uintptr_t esz = t.dtype == FOPD_BF16 ? 2 : 4, a = (uintptr_t)p;
-  const uintptr_t width = (uintptr_t)(dense ? t.rows * t.cols : t.cols) * esz, pitch = dense ? 0 : (uintptr_t)t.row_stride * esz;
-  return {a, a + (uintptr_t)(t.rows - 1) * pitch + width, pitch, width, i, written};
-}
-
-// Column blocks and rows of one wider matrix overlap as ranges but not as elements.  The distance of a row of b behind a
-// row of a is b.lo - a.lo and any multiples of both pitches, that is of their greatest common divisor (the other's where
-// one has a single row): no row of b meets one of a if within that distance b's row lies behind a's and ends before the
-// next.  a starts first.
-bool disjoint_columns(const Range &a, const Range &b) {
-  const uintptr_t pitch = std::gcd(a.row, b.row);
-  if (pitch == 0) return false;
-  const uintptr_t shift = (b.lo - a.lo) % pitch;
-  return shift >= a.width && shift + b.width <= pitch;
-}
-
 // Whether a written range meets another one (its own tensor's data exactly in place excepted).
 int check_overlap(const fopd_tensor *t, int32_t n) {
-  const auto before = [](const Range &a, const Range &b) { return a.lo < b.lo; };
-  // inputs (or in place) and outputs apart: each is usually in order already
-  std::vector<Range> in, out, r;
+  std::vector<Range> in, out;
   in.reserve(n);
   for (int32_t i = 0; i < n; ++i) {
     if (t[i].rows == 0 || t[i].cols == 0) continue;
+    const uintptr_t esz = t[i].dtype == FOPD_BF16 ? 2 : 4;
     const bool in_place = !t[i].out || t[i].out == t[i].data;
-    in.push_back(range_of(t[i], t[i].data, i, in_place));
-    if (!in_place) out.push_back(range_of(t[i], t[i].out, i, true));
+    in.push_back(range_of(t[i].data, t[i].rows, t[i].cols, t[i].row_stride, esz, i, in_place));
+    if (!in_place) out.push_back(range_of(t[i].out, t[i].rows, t[i].cols, t[i].row_stride, esz, i, true));
   }
-  for (std::vector<Range> *v : {&in, &out})
-    if (!std::is_sorted(v->begin(), v->end(), before)) std::sort(v->begin(), v->end(), before);
-  if (out.empty()) {
-    r.swap(in);
-  } else {
-    r.resize(in.size() + out.size());
-    std::merge(in.begin(), in.end(), out.begin(), out.end(), r.begin(), before);
-  }
-  // open: ranges that reach beyond the start of the next one
-  std::vector<Range> open;
-  for (const Range &b : r) {
-    size_t k = 0;
-    for (const Range &a : open) {
-      if (a.hi <= b.lo) continue;
-      if ((a.written || b.written) && !disjoint_columns(a, b)) return FOPD_ERR_ALIAS;
-      open[k++] = a;
-    }
-    open.resize(k);
-    open.push_back(b);
-  }
-  return FOPD_OK;
+  return check_ranges(in, out);
 }
 
 // Fills a launch's table from tensors [*next, n) as far as they go; empty ones are left out.

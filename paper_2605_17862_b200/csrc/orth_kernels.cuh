@@ -1,0 +1,444 @@
+// Orthogonalised updates: Newton-Schulz products over a list of matrices (sm_100a).
+//
+//   X = M / (|M| + eps);  steps times:  A = X X^T,  P = a I + b A + c A^2,  X <- P X;   out = scale X
+//
+// (X^T X and X P for a matrix with more rows than columns.)  A singular value s of X becomes a s + b s^3 + c s^5 in each step.
+//
+// Numbers.  The steps amplify small singular values, and with them whatever rounding has put there: by up to a^steps (485 for
+// five steps of 3.4445).  In bf16 the rounding of X in the first steps comes out as 1 % of the result and, where a few strong directions
+// stand above the others, as 10 % and more.  So X, A and P are held in fp16 under powers of two that keep them just below its largest
+// number (11 bits, everything down to 2^-29 of the largest normal): an eighth of bf16's rounding at the same rate.  X has a second
+// plane of what the rounding left (together 22 bits) while the steps still ahead amplify by 32 or more, and P X then takes both; the
+// rounding of A and P is harmless, as it multiplies what is there.  Results in fp32 have two planes throughout, three products each.
+// The scales follow from a bound on the largest singular value in each step, which the host takes from the coefficients.
+//
+// Everything lies in one workspace in panels of 64 columns ([panel][rows][64], rows and columns padded with zeros to 64), so that one
+// tensor map serves every operand, along its rows or across them, and tiles need no edges.  A and A^2 are symmetric: the
+// tiles on and below the diagonal are computed and stored twice.
+#pragma once
+
+#include "tensor_core.cuh"
+
+namespace fopd {
+
+struct OrthMatrix {
+  const void *data;
+  void *out;
+  int64_t pitch, out_pitch;
+  int rows, cols;      // of the matrix
+  int rp, cp, mp;      // padded to 64; mp: the shorter side
+  int x[2], x_lo;      // workspace rows (of 64 elements) where X starts (two in turn), and from its first plane to the second
+  int a, p, m_lo;      // the same for A and P
+  uint32_t two_planes; // bit k: X of step k has its second plane
+  int sym_tile, x_tile;  // first tile of the matrix
+  int norm_block, norm_blocks, load_block;
+  float scale;
+  uint8_t dtype, out_dtype, tall, full;
+};
+
+constexpr int kNormChunk = 32768;  // elements to a block
+constexpr int kOrthThreads = 256;
+constexpr int kLoadCols = 256;     // a block of the load takes 64 rows of these
+
+struct OrthWorkspace {
+  OrthMatrix *table;
+  float *norm_factor;  // per matrix: 1 / ((|M| + eps) 2^e)
+  double *partial;     // per block of the norm
+  __half *planes;
+};
+
+template <int N>
+struct OrthTable {
+  int n;
+  OrthMatrix m[N];
+};
+
+// The entry whose range (by `first`) holds i.
+template <class First>
+__device__ __forceinline__ int find_entry(int n, int i, First first) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (first(mid) <= i) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ float load_element(const void *p, int64_t i, int dtype) {
+  return dtype == FOPD_BF16 ? Elem<FOPD_BF16>::load1(p, i) : Elem<FOPD_F32>::load1(p, i);
+}
+
+__device__ __forceinline__ double block_sum(double s, double *scratch) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = s;
+  __syncthreads();
+  double t = 0.0;
+  for (int w = 0; w < kOrthThreads / 32; ++w) t += scratch[w];
+  __syncthreads();
+  return t;
+}
+
+// Sums of squares in fp64, a block to 32,768 elements; the table goes to the workspace for the launches that follow.
+template <int N>
+__global__ void __launch_bounds__(kOrthThreads) orth_norm_kernel(const __grid_constant__ OrthTable<N> tab, OrthWorkspace ws) {
+  __shared__ double scratch[kOrthThreads / 32];
+  const int k = find_entry(tab.n, (int)blockIdx.x, [&](int j) { return tab.m[j].norm_block; });
+  const OrthMatrix &m = tab.m[k];
+  if ((int)blockIdx.x == m.norm_block) {
+    const uint32_t *src = reinterpret_cast<const uint32_t *>(&m);
+    uint32_t *dst = reinterpret_cast<uint32_t *>(ws.table + k);
+    if (threadIdx.x < sizeof(OrthMatrix) / 4) dst[threadIdx.x] = src[threadIdx.x];
+  }
+  const int64_t all = (int64_t)m.rows * m.cols, from = (int64_t)((int)blockIdx.x - m.norm_block) * kNormChunk;
+  const int64_t to = from + kNormChunk < all ? from + kNormChunk : all;
+  double s = 0.0;
+  const int size = m.dtype == FOPD_BF16 ? 2 : 4, per = 16 / size;
+  const bool dense = m.rows == 1 || m.pitch == m.cols;
+  if (dense && ((uintptr_t)m.data & 15) == 0) {  // (chunks start at whole vectors)
+    const char *base = static_cast<const char *>(m.data);
+    for (int64_t i = from + threadIdx.x * per; i + per <= to; i += kOrthThreads * per) {
+      const uint4 v = *reinterpret_cast<const uint4 *>(base + i * size);
+      if (m.dtype == FOPD_BF16) {
+        float x[8];
+        Elem<FOPD_BF16>::unpack(v, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fma((double)x[e], (double)x[e], s);
+      } else {
+        float x[4];
+        Elem<FOPD_F32>::unpack(v, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = fma((double)x[e], (double)x[e], s);
+      }
+    }
+    const int64_t tail = from + (to - from) / per * per + threadIdx.x;
+    if (tail < to) {
+      const double x = load_element(base, tail, m.dtype);
+      s = fma(x, x, s);
+    }
+  } else {
+    for (int64_t i = from + threadIdx.x; i < to; i += kOrthThreads) {
+      const int64_t r = i / m.cols;
+      const double x = load_element(m.data, r * m.pitch + (i - r * m.cols), m.dtype);
+      s = fma(x, x, s);
+    }
+  }
+  s = block_sum(s, scratch);
+  if (threadIdx.x == 0) ws.partial[blockIdx.x] = s;
+}
+
+__device__ __forceinline__ void split_half(float x, __half &hi, __half &lo) {
+  hi = __float2half_rn(x);
+  lo = __float2half_rn(x - __half2float(hi));
+}
+
+// Into the workspace times 2^e, with 2^e |M| in [2^14, 2^15): no element leaves fp16's range, and bf16 ones are exact down to 2^-24.
+// A block takes 64 rows x 256 columns and forms the norm from the partial sums itself (in order).
+__global__ void __launch_bounds__(kOrthThreads) orth_load_kernel(OrthWorkspace ws, int n, float eps, int32_t *status) {
+  __shared__ double scratch[kOrthThreads / 32];
+  const int k = find_entry(n, (int)blockIdx.x, [&](int j) { return ws.table[j].load_block; });
+  const OrthMatrix m = ws.table[k];
+  const int block = (int)blockIdx.x - m.load_block;
+  double s = 0.0;
+  for (int i = threadIdx.x; i < m.norm_blocks; i += kOrthThreads) s += ws.partial[m.norm_block + i];
+  const double norm = sqrt(block_sum(s, scratch));
+  int e = 0;
+  double factor = 0.0, scale;
+  const bool finite = norm <= 1.7e308;
+  if (finite && norm > 0.0) {
+    frexp(norm, &e);  // norm in [2^(e-1), 2^e)
+    e = 15 - e;
+    factor = 1.0 / ((norm + (double)eps) * exp2((double)e));
+  }
+  scale = finite ? exp2((double)e) : __longlong_as_double(0x7ff8000000000000ll);
+  if (block == 0 && threadIdx.x == 0) {
+    ws.norm_factor[k] = finite ? (float)factor : __int_as_float(0x7fffffff);
+    if (!finite && status) atomicOr(status, FOPD_DEV_NONFINITE);
+  }
+  const int col_blocks = (m.cp + kLoadCols - 1) / kLoadCols;
+  const int row0 = block / col_blocks * 64, col0 = block % col_blocks * kLoadCols;
+  const int size = m.dtype == FOPD_BF16 ? 2 : 4;
+  const bool two = m.two_planes & 1;
+  const bool aligned = (((uintptr_t)m.data | (uintptr_t)(m.rows > 1 ? m.pitch * size : 0)) & 15) == 0;
+  const float f = (float)scale;  // (2^e may be beyond fp32 for the smallest matrices: then in fp64)
+  const bool in_range = !finite || (e > -126 && e < 126);
+  for (int u = threadIdx.x; u < 64 * (kLoadCols / 8); u += kOrthThreads) {
+    const int c = col0 + (u / 64 / 8) * 64 + (u & 7) * 8, r = row0 + ((u >> 3) & 63);
+    if (c >= m.cp) continue;
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (r < m.rows) {
+      const int64_t at = r * m.pitch + c;
+      if (aligned && c + 8 <= m.cols) {
+        const char *p = static_cast<const char *>(m.data) + at * size;
+        if (m.dtype == FOPD_BF16) Elem<FOPD_BF16>::unpack(*reinterpret_cast<const uint4 *>(p), x);
+        else {
+          float y[4];
+          Elem<FOPD_F32>::unpack(*reinterpret_cast<const uint4 *>(p), y);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) x[q] = y[q];
+          Elem<FOPD_F32>::unpack(*reinterpret_cast<const uint4 *>(p + 16), y);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) x[4 + q] = y[q];
+        }
+      } else {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          if (c + q < m.cols) x[q] = load_element(m.data, at + q, m.dtype);
+      }
+    }
+    __half hi[8], lo[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) split_half(in_range ? x[q] * f : (float)((double)x[q] * scale), hi[q], lo[q]);
+    const int64_t row = (int64_t)m.x[0] + (int64_t)(c / 64) * m.rp + r;
+    *reinterpret_cast<uint4 *>(ws.planes + row * 64 + (c & 63)) = *reinterpret_cast<uint4 *>(hi);
+    if (two) *reinterpret_cast<uint4 *>(ws.planes + (row + m.x_lo) * 64 + (c & 63)) = *reinterpret_cast<uint4 *>(lo);
+  }
+}
+
+// ------------------------------------------------------------------ the products
+enum OrthPhase { kOrthGram = 0, kOrthPoly = 1, kOrthApply = 2 };
+
+// Factors of one step (powers of two but for the coefficients).  Values in the workspace are X 2^ex, A 2^ea, P 2^ep.
+struct OrthStep {
+  float gram;                   // from X's products to A's scale (first step: on top of norm_factor^2)
+  float poly_a, poly_b, poly_c; // P = a I + b A + c A^2, from A's values and A's products to P's scale
+  float apply;                  // from P X to the next X's scale; last step: to 1 (first step: on top of norm_factor)
+};
+
+template <int kCtas, int kN>
+struct OrthJob {
+  static constexpr bool kFp16 = true;
+  static constexpr int kRows = kCtas * 128;
+  static_assert(kN == kRows, "symmetric tiles");
+  struct Params {
+    CUtensorMap boxes, rows_out, mirror_out;
+    OrthWorkspace ws;
+    OrthStep step;
+    int n;
+    int64_t n_tiles;
+    int phase, index, last;
+    int32_t *status;
+  };
+  const Params &p;
+  int cur = 0;
+  uint32_t buf = 0;  // the staging buffer whose turn it is
+  __device__ explicit OrthJob(const Params &params) : p(params) {}
+  __device__ int64_t tiles() const { return p.n_tiles; }
+  __device__ int32_t *status() const { return p.status; }
+  __device__ __forceinline__ int first(int k) const { return p.phase == kOrthApply ? p.ws.table[k].x_tile : p.ws.table[k].sym_tile; }
+  // Matrix and place of tile i (tiles come in ascending order).
+  __device__ __forceinline__ const OrthMatrix &at(int64_t i, int &row0, int &col0) {
+    while (cur + 1 < p.n && first(cur + 1) <= i) ++cur;
+    const OrthMatrix &m = p.ws.table[cur];
+    const int t = (int)i - first(cur);
+    if (p.phase == kOrthApply) {
+      const int across = (m.cp + kN - 1) / kN;
+      row0 = t / across * kRows;
+      col0 = t % across * kN;
+    } else {
+      int r = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+      while (r * (r + 1) / 2 > t) --r;
+      while ((r + 1) * (r + 2) / 2 <= t) ++r;
+      row0 = r * kRows;
+      col0 = (t - r * (r + 1) / 2) * kN;
+    }
+    return m;
+  }
+  __device__ void tile(int64_t i, int cta, Tile &t) {
+    int row0, col0;
+    const OrthMatrix &m = at(i, row0, col0);
+    row0 += cta * 128;
+    col0 += cta * (kN / kCtas);
+    const bool x_two = p.phase != kOrthPoly && (m.two_planes >> p.index & 1);
+    const int x = m.x[p.index & 1];
+    // along: rows of the operand are rows of the plane; across: they are its columns
+    const auto along = [&](int y, int pitch, int r, int lo) { return Operand{&p.boxes, 0, y + r, 0, pitch, 0, 64, lo, false}; };
+    const auto across = [&](int y, int pitch, int r, int lo) { return Operand{&p.boxes, 0, y + r / 64 * pitch, 0, 64, 0, pitch, lo, true}; };
+    t.a_lo = t.b_lo = 0;
+    t.passes = 1;
+    if (p.phase == kOrthGram) {
+      t.a = m.tall ? across(x, m.rp, row0, m.x_lo) : along(x, m.rp, row0, m.x_lo);
+      t.b = m.tall ? across(x, m.rp, col0, m.x_lo) : along(x, m.rp, col0, m.x_lo);
+      t.k_blocks = (m.tall ? m.rp : m.cp) / 64;
+      if (m.full && x_two) t.passes = 3, t.b_lo = 2, t.a_lo = 4;
+    } else if (p.phase == kOrthPoly) {
+      t.a = along(m.a, m.mp, row0, m.m_lo);
+      t.b = along(m.a, m.mp, col0, m.m_lo);
+      t.k_blocks = m.mp / 64;
+      if (m.full) t.passes = 3, t.b_lo = 2, t.a_lo = 4;
+    } else {
+      t.k_blocks = m.mp / 64;
+      uint32_t p_lo = 0, x_lo = 0;
+      if (m.full) {
+        p_lo = 2;
+        t.passes = 2;
+        if (x_two) x_lo = 4, t.passes = 3;
+      } else if (x_two) {
+        x_lo = 2;
+        t.passes = 2;
+      }
+      if (m.tall) {
+        t.a = along(x, m.rp, row0, m.x_lo);
+        t.b = along(m.p, m.mp, col0, m.m_lo);
+        t.a_lo = x_lo, t.b_lo = p_lo;
+      } else {
+        t.a = along(m.p, m.mp, row0, m.m_lo);
+        t.b = across(x, m.rp, col0, m.x_lo);
+        t.a_lo = p_lo, t.b_lo = x_lo;
+      }
+    }
+  }
+
+  // 64 columns of this warp's rows to a plane (or two) by TMA.
+  __device__ __forceinline__ uint32_t next_buffer(const Accumulator &acc) {
+    const uint32_t at = acc.staging + buf * kStageBufBytes;
+    buf ^= 1;
+    if (acc.lane == 0) tma_store_wait_read<1>();
+    __syncwarp();
+    return at;
+  }
+  __device__ __forceinline__ void send(const CUtensorMap *map, int x, int y, uint32_t at, int lane) {
+    fence_async_shared();
+    __syncwarp();
+    if (lane == 0) {
+      tma_store(map, x, y, at);
+      tma_store_commit();
+    }
+  }
+  __device__ __forceinline__ void put_rows(const Accumulator &acc, const float (&v)[64], int y, bool lo) {
+    const uint32_t at = next_buffer(acc);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        __half2 h = __floats2half2_rn(v[8 * j + 2 * e], v[8 * j + 2 * e + 1]);
+        if (lo) h = __floats2half2_rn(v[8 * j + 2 * e] - __low2float(h), v[8 * j + 2 * e + 1] - __high2float(h));
+        w[e] = *reinterpret_cast<uint32_t *>(&h);
+      }
+      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + acc.lane * 128 + ((j ^ (acc.lane & 7)) * 16)), "r"(w[0]),
+                   "r"(w[1]), "r"(w[2]), "r"(w[3])
+                   : "memory");
+    }
+    send(&p.rows_out, 0, y, at, acc.lane);
+  }
+  // The same transposed: 64 rows of 32 elements.
+  __device__ __forceinline__ void put_mirror(const Accumulator &acc, const float (&v)[64], int x, int y, bool lo) {
+    const uint32_t at = next_buffer(acc);
+#pragma unroll
+    for (int j = 0; j < 64; ++j) {
+      __half h = __float2half_rn(v[j]);
+      if (lo) h = __float2half_rn(v[j] - __half2float(h));
+      asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + j * 64 + acc.lane * 2), "h"(__half_as_ushort(h)) : "memory");
+    }
+    send(&p.mirror_out, x, y, at, acc.lane);
+  }
+
+  template <int>
+  __device__ void epilogue(int64_t i, int cta, const Accumulator &acc) {
+    int row0, col0;
+    const OrthMatrix &m = at(i, row0, col0);
+    const bool below = p.phase != kOrthApply && row0 != col0;
+    row0 += cta * 128 + acc.warp * 32;
+    const int row = row0 + acc.lane;
+    if (p.phase == kOrthApply) {
+      const float f = (p.index == 0 ? p.ws.norm_factor[cur] : 1.f) * p.step.apply;
+      if (row0 >= m.rp) return;
+      if (p.last) {
+        const float g = f * m.scale;
+        for (int c = 0; c < kN; c += 32) {
+          if (col0 + c >= m.cols) break;
+          uint32_t r[32];
+          load_columns(acc, c, r);
+          if (row >= m.rows) continue;
+          float v[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]) * g;
+          if (m.out_dtype == FOPD_F32) put_result<FOPD_F32>(m, v, row, col0 + c);
+          else put_result<FOPD_BF16>(m, v, row, col0 + c);
+        }
+        return;
+      }
+      const int x = m.x[(p.index + 1) & 1];
+      const bool two = m.two_planes >> (p.index + 1) & 1;
+      for (int c = 0; c < kN; c += 64) {
+        if (col0 + c >= m.cp) break;
+        float v[64];
+        load64(acc, c, v, f);
+        const int y = x + (col0 + c) / 64 * m.rp + row0;
+        put_rows(acc, v, y, false);
+        if (two) put_rows(acc, v, y + m.x_lo, true);
+      }
+      return;
+    }
+    if (row0 >= m.mp) return;
+    const int to = p.phase == kOrthGram ? m.a : m.p;
+    float f = p.step.poly_c;
+    if (p.phase == kOrthGram) {
+      const float s = p.index == 0 ? p.ws.norm_factor[cur] : 1.f;
+      f = p.step.gram * s * s;
+    }
+    for (int c = 0; c < kN; c += 64) {
+      if (col0 + c >= m.mp) break;
+      float v[64];
+      load64(acc, c, v, f);
+      const int panel_row = (col0 + c) / 64 * m.mp + row0;
+      if (p.phase == kOrthPoly) {
+        for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) {
+          const uint4 *q = reinterpret_cast<const uint4 *>(p.ws.planes + ((int64_t)m.a + plane * m.m_lo + panel_row + acc.lane) * 64);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint4 w = __ldcg(q + j);
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&u[e]));
+              v[8 * j + 2 * e] = fmaf(p.step.poly_b, a.x, v[8 * j + 2 * e]);
+              v[8 * j + 2 * e + 1] = fmaf(p.step.poly_b, a.y, v[8 * j + 2 * e + 1]);
+            }
+          }
+        }
+        const int d = row - (col0 + c);
+        if (d >= 0 && d < 64) {
+#pragma unroll
+          for (int j = 0; j < 64; ++j)
+            if (j == d) v[j] += p.step.poly_a;
+        }
+      }
+      for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) {
+        put_rows(acc, v, to + plane * m.m_lo + panel_row, plane);
+        if (below) put_mirror(acc, v, row0 & 63, to + plane * m.m_lo + row0 / 64 * m.mp + col0 + c, plane);
+      }
+    }
+  }
+  __device__ __forceinline__ void load64(const Accumulator &acc, int c, float (&v)[64], float f) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t r[32];
+      load_columns(acc, c + 32 * h, r);
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[32 * h + j] = __uint_as_float(r[j]) * f;
+    }
+  }
+  template <int DT>
+  __device__ __forceinline__ void put_result(const OrthMatrix &m, const float (&v)[32], int row, int col) const {
+    constexpr int kPer = Elem<DT>::kPerVec;
+    char *q = static_cast<char *>(m.out) + (row * m.out_pitch + col) * Elem<DT>::kBytes;
+    if (col + 32 <= m.cols && ((uintptr_t)q & 15) == 0) {
+#pragma unroll
+      for (int j = 0; j < 32; j += kPer) {
+        float x[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) x[e] = v[j + e];
+        *reinterpret_cast<uint4 *>(q + j * Elem<DT>::kBytes) = Elem<DT>::pack(x);
+      }
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (col + j < m.cols) Elem<DT>::store1(q, j, v[j]);
+  }
+};
+
+}  // namespace fopd

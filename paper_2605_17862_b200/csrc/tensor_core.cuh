@@ -186,6 +186,7 @@ __device__ __forceinline__ void load_columns(const Accumulator &acc, int col, ui
     for (int i = 0; i < 32; ++i) r[i] = 0;
     return;
   }
+  __syncwarp();
   tmem_load(r, acc.addr + col);
   tmem_wait(r);
 }
