@@ -96,7 +96,7 @@ int run_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *status,
   const int64_t v_tiles = (h->vocab + kN - 1) / kN, pitch = round_up(h->n_rows, kCtas * 128);
   Layout lay;
   const RowParts parts = row_parts(h, &lay);
-  const int64_t part = lay.take(v_tiles * pitch * 8), logit = lay.take(pitch * 4);
+  const int64_t part = lay.take(2 * v_tiles * pitch * 8), logit = lay.take(pitch * 4);
   Temporary tmp(st);
   int rc = tmp.take(lay.bytes);
   if (rc != FOPD_OK) return rc;
@@ -114,7 +114,7 @@ int run_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *status,
     p.status = status;
     rc = launch_product<kCtas, kN, LogprobJob>(p, pitch / (kCtas * 128) * v_tiles, sms, st);
     if (rc == FOPD_OK) {
-      head_join_kernel<<<(unsigned)((h->n_rows + 31) / 32), 1024, 0, st>>>(pre.rows, p.part, p.token_logit, (int)v_tiles, (int)pitch,
+      head_join_kernel<<<(unsigned)((h->n_rows + 31) / 32), 1024, 0, st>>>(pre.rows, p.part, p.token_logit, 2 * (int)v_tiles, (int)pitch,
                                                                            h->tokens, h->vocab, logprob, lse, status);
       rc = launch_ok();
     }

@@ -75,6 +75,7 @@ __global__ void __launch_bounds__(256) head_gather_kernel(const __nv_bfloat16 *h
 }
 
 // ------------------------------------------------------------------ tiles of logits
+constexpr int kLogitChunk = 8;  // blocks of 64 dimensions that a matrix instruction's accumulator adds up
 struct LogitTiles {
   const CUtensorMap *hidden, *weight;
   HeadRows rows;
@@ -105,13 +106,14 @@ __device__ __forceinline__ void logit_tile(const LogitTiles &l, int n_rows, int6
   t.a = {l.hidden, 0, row0 + cta * 128, 64, 0, 0, 64, 0, false};
   t.b = {l.weight, 0, (int)col0 + cta * (kN / kCtas), 64, 0, 0, 64, 0, false};
   t.k_blocks = l.k_blocks;
+  t.chunk = kLogitChunk;
   t.passes = 1;
   t.a_lo = t.b_lo = 0;
 }
 
 // ------------------------------------------------------------------ log-probs
-// A tile's epilogue: a thread per row, online maximum and sum over its 256 logits (exponents as in RowSweep), the stored
-// token's left out of the sum: the log-prob of a nearly certain token comes from the others' sum.
+// A tile's epilogue: two threads per row, each the maximum and the sum of exponentials of 128 logits (exponents as in RowSweep), the
+// stored token's left out of the sum: the log-prob of a nearly certain token comes from the others' sum.
 template <int kCtas, int kN>
 struct LogprobJob {
   static constexpr bool kFp16 = false;
@@ -119,7 +121,7 @@ struct LogprobJob {
     CUtensorMap hidden, weight;
     LogitTiles l;
     const int32_t *tokens;
-    float2 *part;  // [v_tiles][pitch]
+    float2 *part;  // [2 v_tiles][pitch]
     float *token_logit;
     int pitch;
     int32_t *status;
@@ -133,62 +135,46 @@ struct LogprobJob {
   }
   __device__ int64_t tiles() const { return logit_tiles<kCtas, kN>(l, n); }
   __device__ int32_t *status() const { return p.status; }
-  __device__ void tile(int64_t i, int cta, Tile &t) const { logit_tile<kCtas, kN>(l, n, i, cta, t); }
-  template <int>
-  __device__ void epilogue(int64_t i, int cta, const Accumulator &acc) const {
+  __device__ __forceinline__ void tile(int64_t i, int cta, Tile &t) const { logit_tile<kCtas, kN>(l, n, i, cta, t); }
+  __device__ __forceinline__ void epilogue(int64_t i, int cta, const Accumulator &acc, float (&z)[kN / 2]) const {
+    constexpr int kCols = kN / 2;
     int row0;
-    int64_t col0;
-    logit_tile_at<kCtas, kN>(l, n, i, row0, col0);
+    int64_t v0;
+    logit_tile_at<kCtas, kN>(l, n, i, row0, v0);
+    v0 += acc.half * kCols;
     const int row = row0 + cta * 128 + acc.warp * 32 + acc.lane;
     const int y = row < n ? p.tokens[l.rows.row(row)] : -1;
-    float m = kNegBig, c = kNegBig, s = 0.f;
-    for (int at = 0; at < kN; at += 32) {
-      if (col0 + at >= l.vocab) break;
-      uint32_t r[32];
-      load_columns(acc, at, r);
-      float z[32];
+    if (v0 + kCols > l.vocab) {
+      const int have = (int)max((int64_t)0, l.vocab - v0);
 #pragma unroll
-      for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(r[j]);
-      const int64_t v0 = col0 + at;
-      if (v0 + 32 > l.vocab) {
-        const int have = (int)(l.vocab - v0);
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (j >= have) z[j] = -INFINITY;
-      }
-      const int64_t mine = (int64_t)y - v0;
-      if (mine >= 0 && mine < 32) {
-        float zy = 0.f;
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (j == (int)mine) {
-            zy = z[j];
-            z[j] = -INFINITY;
-          }
-        if (y < l.vocab) p.token_logit[row] = zy;
-      }
-      float vm = z[0];
-#pragma unroll
-      for (int j = 1; j < 31; j += 2) vm = max3(vm, z[j], z[j + 1]);
-      vm = fmaxf(vm, z[31]);
-      if (vm > m) {
-        const float cn = vm * kLog2e;
-        s *= ex2(c - cn);
-        m = vm;
-        c = cn;
-      }
-      float s4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < 32; ++j) s4[j & 3] += ex2(fmaf(z[j], kLog2e, -c));
-      s += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+      for (int j = 0; j < kCols; ++j)
+        if (j >= have) z[j] = -INFINITY;
     }
-    const float fix = -fmaf(m, kLog2e, -c) * kLn2;
-    if (row < n) p.part[(int64_t)(col0 / kN) * p.pitch + row] = make_float2(m, __fmaf_rn(s, fix, s));
+    const int64_t mine = (int64_t)y - v0;
+    if (mine >= 0 && mine < kCols && y < l.vocab) {
+      float zy = 0.f;
+#pragma unroll
+      for (int j = 0; j < kCols; ++j)
+        if (j == (int)mine) {
+          zy = z[j];
+          z[j] = -INFINITY;
+        }
+      p.token_logit[row] = zy;
+    }
+    float m = kNegBig;
+#pragma unroll
+    for (int j = 0; j < kCols; j += 2) m = max3(m, z[j], z[j + 1]);
+    const float c = fmaxf(m * kLog2e, kNegBig);  // (a half behind the last token has no logit)
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) s[j & 3] += ex2(fmaf(z[j], kLog2e, -c));
+    const float sum = (s[0] + s[1]) + (s[2] + s[3]), fix = -fmaf(m, kLog2e, -c) * kLn2;
+    if (row < n) p.part[(v0 / kCols) * p.pitch + row] = make_float2(m, __fmaf_rn(sum, fix, sum));
   }
 };
 
 // Joins the pieces of 32 rows: 32 threads to a row's pieces, then in a fixed order; exponentials fp32, sums and logs fp64.
-__global__ void __launch_bounds__(1024) head_join_kernel(HeadRows rows, const float2 *part, const float *token_logit, int v_tiles,
+__global__ void __launch_bounds__(1024) head_join_kernel(HeadRows rows, const float2 *part, const float *token_logit, int pieces,
                                                          int pitch, const int32_t *tokens, int64_t vocab, float *logprob,
                                                          float *lse, int32_t *status) {
   __shared__ float sm[32][33];
@@ -198,7 +184,7 @@ __global__ void __launch_bounds__(1024) head_join_kernel(HeadRows rows, const fl
   float m = kNegBig;
   double s = 0.0;
   if (r < n)
-    for (int v = ty; v < v_tiles; v += 32) {
+    for (int v = ty; v < pieces; v += 32) {
       const float2 q = part[(int64_t)v * pitch + r];
       if (q.x > m) {
         s *= (double)ex2((m - q.x) * kLog2e);
@@ -246,19 +232,20 @@ struct GradLogitsJob {
   const Params &p;
   LogitTiles l;
   int n;
-  uint32_t buf = 0;  // the staging buffer whose turn it is (across tiles)
+  Staging staging;
   __device__ explicit GradLogitsJob(const Params &params) : p(params), l(params.l), n(params.l.rows.count()) {
     l.hidden = &p.hidden;
     l.weight = &p.weight;
   }
   __device__ int64_t tiles() const { return logit_tiles<kCtas, kN>(l, n); }
   __device__ int32_t *status() const { return p.status; }
-  __device__ void tile(int64_t i, int cta, Tile &t) const { logit_tile<kCtas, kN>(l, n, i, cta, t); }
-  template <int>
-  __device__ void epilogue(int64_t i, int cta, const Accumulator &acc) {
+  __device__ __forceinline__ void tile(int64_t i, int cta, Tile &t) const { logit_tile<kCtas, kN>(l, n, i, cta, t); }
+  __device__ __forceinline__ void epilogue(int64_t i, int cta, const Accumulator &acc, float (&g)[kN / 2]) {
+    constexpr int kCols = kN / 2;
     int row0;
-    int64_t col0;
-    logit_tile_at<kCtas, kN>(l, n, i, row0, col0);
+    int64_t v0;
+    logit_tile_at<kCtas, kN>(l, n, i, row0, v0);
+    v0 += acc.half * kCols;
     row0 += cta * 128 + acc.warp * 32;
     const int row = row0 + acc.lane;
     float lse = 0.f, coef = 0.f, at_token = 0.f;
@@ -272,61 +259,39 @@ struct GradLogitsJob {
         at_token = coef * expm1f(p.logprob[r]);  // p - 1 without the cancellation
       } else {
         y = -1;
-        if (p.status && col0 == 0) atomicOr(p.status, FOPD_DEV_BAD_TOKEN);
+        if (p.status && v0 == 0) atomicOr(p.status, FOPD_DEV_BAD_TOKEN);
       }
     }
     const bool live = coef != 0.f;
-    for (int panel = 0; panel < kN / 64; ++panel) {
-      const int64_t v0 = col0 + panel * 64;
-      if (v0 >= l.vocab) break;
-      float g[64];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t r[32];
-        load_columns(acc, panel * 64 + h * 32, r);
+    for (int j = 0; j < kCols; ++j) g[j] = live ? coef * ex2((g[j] - lse) * kLog2e) : 0.f;
+    const int64_t mine = (int64_t)y - v0;
+    if (live && mine >= 0 && mine < kCols) {
+      const int at = (int)mine;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) g[h * 32 + j] = live ? coef * ex2((__uint_as_float(r[j]) - lse) * kLog2e) : 0.f;
-      }
-      const int64_t mine = (int64_t)y - v0;
-      if (live && mine >= 0 && mine < 64) {
-#pragma unroll
-        for (int j = 0; j < 64; ++j)
-          if (j == (int)mine) g[j] = at_token;
-      }
-      if (v0 + 64 > l.vocab) {
-        const int have = (int)(l.vocab - v0);
-#pragma unroll
-        for (int j = 0; j < 64; ++j)
-          if (j >= have) g[j] = 0.f;
-      }
-      const int y_out = (int)((v0 - (int64_t)l.v_tile0 * kN) / 64) * p.pitch + row0;
-      for (int plane = 0; plane < (p.lo ? 2 : 1); ++plane) {
-        const uint32_t at = acc.staging + buf * kStageBufBytes;
-        buf ^= 1;
-        if (acc.lane == 0) tma_store_wait_read<1>();
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          uint32_t w[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float a = g[8 * j + 2 * e], b = g[8 * j + 2 * e + 1];
-            __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-            if (plane) h = __floats2bfloat162_rn(a - __low2float(h), b - __high2float(h));
-            w[e] = *reinterpret_cast<uint32_t *>(&h);
-          }
-          asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + acc.lane * 128 + ((j ^ (acc.lane & 7)) * 16)),
-                       "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
-                       : "memory");
-        }
-        fence_async_shared();
-        __syncwarp();
-        if (acc.lane == 0) {
-          tma_store(&p.panels_out, 0, y_out + plane * p.lo, at);
-          tma_store_commit();
-        }
-      }
+      for (int j = 0; j < kCols; ++j) asm("{\n.reg .pred p;\nsetp.eq.s32 p, %1, %2;\nselp.f32 %0, %3, %0, p;\n}" : "+f"(g[j]) : "r"(at), "r"(j), "f"(at_token));
     }
+    if (v0 + kCols > l.vocab) {
+      const int have = (int)max((int64_t)0, l.vocab - v0);
+#pragma unroll
+      for (int j = 0; j < kCols; ++j)
+        if (j >= have) g[j] = 0.f;
+    }
+    const int panel0 = (int)((v0 - (int64_t)l.v_tile0 * kN) / 64);
+    const auto put = [&](const float *g, int c) {
+      for (int plane = 0; plane < (v0 + c >= l.vocab ? 0 : p.lo ? 2 : 1); ++plane) {
+        const uint32_t at = staging.next(acc);
+        stage_box(at, acc.lane, [&](int j) {
+          const float a = g[2 * j], b = g[2 * j + 1];
+          __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+          if (plane) h = __floats2bfloat162_rn(a - __low2float(h), b - __high2float(h));
+          return *reinterpret_cast<uint32_t *>(&h);
+        });
+        staging.send(acc, &p.panels_out, 0, (panel0 + c / 64) * p.pitch + row0 + plane * p.lo, at);
+      }
+    };
+    put(g, 0);
+    if (kCols > 64) put(g + 64, 64);
   }
 };
 
@@ -365,7 +330,7 @@ struct HeadGradsJob {
   __device__ int64_t tiles() const { return n_hidden + (p.d_weight ? (int64_t)v_tiles * d_tiles : 0); }
   __device__ int32_t *status() const { return p.status; }
   // hidden: (split, row0, d0); weight: (-1, row of the piece, d0)
-  __device__ void at(int64_t i, int &split, int &row0, int &d0) const {
+  __device__ __forceinline__ void at(int64_t i, int &split, int &row0, int &d0) const {
     if (i < n_hidden) {
       split = (int)(i / ((int64_t)m_tiles * d_tiles));
       const int r = (int)(i - (int64_t)split * m_tiles * d_tiles);
@@ -378,7 +343,7 @@ struct HeadGradsJob {
       d0 = (int)(i % d_tiles) * kN;
     }
   }
-  __device__ void tile(int64_t i, int cta, Tile &t) const {
+  __device__ __forceinline__ void tile(int64_t i, int cta, Tile &t) const {
     int split, row0, d0;
     at(i, split, row0, d0);
     row0 += cta * 128;
@@ -388,82 +353,45 @@ struct HeadGradsJob {
       t.a = {&p.panels, 0, first * p.pitch + row0, 0, p.pitch, 0, 64, 0, false};
       t.b = {&p.weight, d0, (int)p.v0 + first * 64, 0, 64, 64, 0, 0, true};
       t.k_blocks = max(0, min(p.split_panels, panels - first));
+      t.chunk = 0;
       t.passes = 1;
       t.a_lo = 0;
     } else {
       t.a = {&p.panels, 0, row0 / 64 * p.pitch, 0, 64, 0, p.pitch, p.lo, true};
       t.b = {&p.hidden, d0, 0, 0, 64, 64, 0, 0, true};
       t.k_blocks = (n + 63) / 64;
+      t.chunk = p.lo ? kLogitChunk : 0;
       t.passes = p.lo ? 2 : 1;
-      t.a_lo = 1;
-      if (!p.lo) t.a_lo = 0;
+      t.a_lo = p.lo ? 1 : 0;  // (the small terms first)
     }
     t.b_lo = 0;
   }
-  template <int>
-  __device__ void epilogue(int64_t i, int cta, const Accumulator &acc) const {
+  __device__ __forceinline__ void epilogue(int64_t i, int cta, const Accumulator &acc, float (&g)[kN / 2]) const {
     int split, row0, d0;
     at(i, split, row0, d0);
+    d0 += acc.half * (kN / 2);
     const int row = row0 + cta * 128 + acc.warp * 32 + acc.lane;
     if (split >= 0) {
-      float *out = p.sum + ((int64_t)split * p.pitch + row) * p.sum_pitch;
-      for (int c = 0; c < kN; c += 32) {
-        if (d0 + c >= p.dim) break;
-        uint32_t r[32];
-        load_columns(acc, c, r);
-        if (row < n) {  // (sum_pitch is a multiple of 32)
+      if (row >= n) return;
+      float *out = p.sum + ((int64_t)split * p.pitch + row) * p.sum_pitch + d0;
 #pragma unroll
-          for (int j = 0; j < 32; j += 4) {
-            float4 *q = reinterpret_cast<float4 *>(out + d0 + c + j);
-            float4 v = make_float4(__uint_as_float(r[j]), __uint_as_float(r[j + 1]), __uint_as_float(r[j + 2]), __uint_as_float(r[j + 3]));
-            if (!p.first) {
-              const float4 o = *q;
-              v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
-            }
-            *q = v;
-          }
+      for (int j = 0; j < kN / 2; j += 4) {
+        if (d0 + j >= p.dim) continue;  // (sum_pitch is a multiple of 32)
+        float4 *q = reinterpret_cast<float4 *>(out + j);
+        float4 v = make_float4(g[j], g[j + 1], g[j + 2], g[j + 3]);
+        if (!p.first) {
+          const float4 o = *q;
+          v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
         }
+        *q = v;
       }
       return;
     }
-    const bool on = row < p.v_count;
+    if (row >= p.v_count) return;
     const int64_t at = (p.v0 + row) * p.d_weight_pitch + d0;
-    for (int c = 0; c < kN; c += 32) {
-      if (d0 + c >= p.dim) break;
-      uint32_t r[32];
-      load_columns(acc, c, r);
-      if (!on) continue;
-      float g[32];
-#pragma unroll
-      for (int j = 0; j < 32; ++j) g[j] = __uint_as_float(r[j]);
-      if (p.d_weight_f32) store32<FOPD_F32>(g, at + c, d0 + c);
-      else store32<FOPD_BF16>(g, at + c, d0 + c);
-    }
-  }
-  template <int DT>
-  __device__ __forceinline__ void store32(float (&g)[32], int64_t at, int d) const {
-    constexpr int kPer = Elem<DT>::kPerVec;
-    char *q = static_cast<char *>(p.d_weight) + at * Elem<DT>::kBytes;
-    if (d + 32 <= p.dim) {
-#pragma unroll
-      for (int j = 0; j < 32; j += kPer) {
-        float x[kPer];
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) x[e] = g[j + e];
-        uint4 *w = reinterpret_cast<uint4 *>(q + j * Elem<DT>::kBytes);
-        if (p.add) {
-          float o[kPer];
-          Elem<DT>::unpack(*w, o);
-#pragma unroll
-          for (int e = 0; e < kPer; ++e) x[e] += o[e];
-        }
-        *w = Elem<DT>::pack(x);
-      }
-      return;
-    }
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (d + j < p.dim) Elem<DT>::store1(q, j, p.add ? g[j] + Elem<DT>::load1(q, j) : g[j]);
+    char *out = static_cast<char *>(p.d_weight);
+    if (p.d_weight_f32) store_row<FOPD_F32, kN / 2>(out + at * 4, g, d0, p.dim, p.add);
+    else store_row<FOPD_BF16, kN / 2>(out + at * 2, g, d0, p.dim, p.add);
   }
 };
 

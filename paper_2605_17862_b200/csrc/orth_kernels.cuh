@@ -38,6 +38,7 @@ struct OrthMatrix {
 
 constexpr int kNormChunk = 32768;  // elements to a block
 constexpr int kOrthThreads = 256;
+constexpr int kOrthChunk = 4;       // blocks of 64 that an accumulator adds up where the result is fp32
 constexpr int kLoadCols = 256;     // a block of the load takes 64 rows of these
 
 struct OrthWorkspace {
@@ -222,7 +223,7 @@ struct OrthJob {
   };
   const Params &p;
   int cur = 0;
-  uint32_t buf = 0;  // the staging buffer whose turn it is
+  Staging staging;
   __device__ explicit OrthJob(const Params &params) : p(params) {}
   __device__ int64_t tiles() const { return p.n_tiles; }
   __device__ int32_t *status() const { return p.status; }
@@ -245,7 +246,7 @@ struct OrthJob {
     }
     return m;
   }
-  __device__ void tile(int64_t i, int cta, Tile &t) {
+  __device__ __forceinline__ void tile(int64_t i, int cta, Tile &t) {
     int row0, col0;
     const OrthMatrix &m = at(i, row0, col0);
     row0 += cta * 128;
@@ -257,27 +258,22 @@ struct OrthJob {
     const auto across = [&](int y, int pitch, int r, int lo) { return Operand{&p.boxes, 0, y + r / 64 * pitch, 0, 64, 0, pitch, lo, true}; };
     t.a_lo = t.b_lo = 0;
     t.passes = 1;
+    t.chunk = m.full ? kOrthChunk : 0;
     if (p.phase == kOrthGram) {
       t.a = m.tall ? across(x, m.rp, row0, m.x_lo) : along(x, m.rp, row0, m.x_lo);
       t.b = m.tall ? across(x, m.rp, col0, m.x_lo) : along(x, m.rp, col0, m.x_lo);
       t.k_blocks = (m.tall ? m.rp : m.cp) / 64;
-      if (m.full && x_two) t.passes = 3, t.b_lo = 2, t.a_lo = 4;
+      if (m.full && x_two) t.passes = 3, t.b_lo = 1, t.a_lo = 2;
     } else if (p.phase == kOrthPoly) {
       t.a = along(m.a, m.mp, row0, m.m_lo);
       t.b = along(m.a, m.mp, col0, m.m_lo);
       t.k_blocks = m.mp / 64;
-      if (m.full) t.passes = 3, t.b_lo = 2, t.a_lo = 4;
+      if (m.full) t.passes = 3, t.b_lo = 1, t.a_lo = 2;
     } else {
       t.k_blocks = m.mp / 64;
-      uint32_t p_lo = 0, x_lo = 0;
-      if (m.full) {
-        p_lo = 2;
-        t.passes = 2;
-        if (x_two) x_lo = 4, t.passes = 3;
-      } else if (x_two) {
-        x_lo = 2;
-        t.passes = 2;
-      }
+      uint32_t p_lo = 0, x_lo = 0;  // (the small terms first)
+      if (m.full) p_lo = 1u << (t.passes++ - 1);
+      if (x_two) x_lo = 1u << (t.passes++ - 1);
       if (m.tall) {
         t.a = along(x, m.rp, row0, m.x_lo);
         t.b = along(m.p, m.mp, col0, m.m_lo);
@@ -290,99 +286,72 @@ struct OrthJob {
     }
   }
 
-  // 64 columns of this warp's rows to a plane (or two) by TMA.
-  __device__ __forceinline__ uint32_t next_buffer(const Accumulator &acc) {
-    const uint32_t at = acc.staging + buf * kStageBufBytes;
-    buf ^= 1;
-    if (acc.lane == 0) tma_store_wait_read<1>();
-    __syncwarp();
-    return at;
-  }
-  __device__ __forceinline__ void send(const CUtensorMap *map, int x, int y, uint32_t at, int lane) {
-    fence_async_shared();
-    __syncwarp();
-    if (lane == 0) {
-      tma_store(map, x, y, at);
-      tma_store_commit();
-    }
-  }
-  __device__ __forceinline__ void put_rows(const Accumulator &acc, const float (&v)[64], int y, bool lo) {
-    const uint32_t at = next_buffer(acc);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      uint32_t w[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        __half2 h = __floats2half2_rn(v[8 * j + 2 * e], v[8 * j + 2 * e + 1]);
-        if (lo) h = __floats2half2_rn(v[8 * j + 2 * e] - __low2float(h), v[8 * j + 2 * e + 1] - __high2float(h));
-        w[e] = *reinterpret_cast<uint32_t *>(&h);
-      }
-      asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + acc.lane * 128 + ((j ^ (acc.lane & 7)) * 16)), "r"(w[0]),
-                   "r"(w[1]), "r"(w[2]), "r"(w[3])
-                   : "memory");
-    }
-    send(&p.rows_out, 0, y, at, acc.lane);
+  // 64 columns of this warp's rows to a plane: the values, or what their rounding leaves.
+  __device__ __forceinline__ void put_rows(const Accumulator &acc, const float *v, int y, bool lo) {
+    const uint32_t at = staging.next(acc);
+    stage_box(at, acc.lane, [&](int j) {
+      __half2 h = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+      if (lo) h = __floats2half2_rn(v[2 * j] - __low2float(h), v[2 * j + 1] - __high2float(h));
+      return *reinterpret_cast<uint32_t *>(&h);
+    });
+    staging.send(acc, &p.rows_out, 0, y, at);
   }
   // The same transposed: 64 rows of 32 elements.
-  __device__ __forceinline__ void put_mirror(const Accumulator &acc, const float (&v)[64], int x, int y, bool lo) {
-    const uint32_t at = next_buffer(acc);
+  __device__ __forceinline__ void put_mirror(const Accumulator &acc, const float *v, int x, int y, bool lo) {
+    const uint32_t at = staging.next(acc);
 #pragma unroll
     for (int j = 0; j < 64; ++j) {
       __half h = __float2half_rn(v[j]);
       if (lo) h = __float2half_rn(v[j] - __half2float(h));
       asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + j * 64 + acc.lane * 2), "h"(__half_as_ushort(h)) : "memory");
     }
-    send(&p.mirror_out, x, y, at, acc.lane);
+    staging.send(acc, &p.mirror_out, x, y, at);
   }
 
-  template <int>
-  __device__ void epilogue(int64_t i, int cta, const Accumulator &acc) {
+  __device__ __forceinline__ void epilogue(int64_t i, int cta, const Accumulator &acc, float (&v)[kN / 2]) {
+    constexpr int kCols = kN / 2;
     int row0, col0;
     const OrthMatrix &m = at(i, row0, col0);
     const bool below = p.phase != kOrthApply && row0 != col0;
     row0 += cta * 128 + acc.warp * 32;
+    col0 += acc.half * kCols;
     const int row = row0 + acc.lane;
     if (p.phase == kOrthApply) {
-      const float f = (p.index == 0 ? p.ws.norm_factor[cur] : 1.f) * p.step.apply;
-      if (row0 >= m.rp) return;
-      if (p.last) {
-        const float g = f * m.scale;
-        for (int c = 0; c < kN; c += 32) {
-          if (col0 + c >= m.cols) break;
-          uint32_t r[32];
-          load_columns(acc, c, r);
-          if (row >= m.rows) continue;
-          float v[32];
+      if (row0 >= m.rp || col0 >= m.cp) return;
+      const float f = (p.index == 0 ? p.ws.norm_factor[cur] : 1.f) * p.step.apply * (p.last ? m.scale : 1.f);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]) * g;
-          if (m.out_dtype == FOPD_F32) put_result<FOPD_F32>(m, v, row, col0 + c);
-          else put_result<FOPD_BF16>(m, v, row, col0 + c);
-        }
+      for (int j = 0; j < kCols; ++j) v[j] *= f;
+      if (p.last) {
+        if (row >= m.rows) return;
+        const int64_t at = row * m.out_pitch + col0;
+        char *out = static_cast<char *>(m.out);
+        if (m.out_dtype == FOPD_F32) store_row<FOPD_F32, kCols>(out + at * 4, v, col0, m.cols, false);
+        else store_row<FOPD_BF16, kCols>(out + at * 2, v, col0, m.cols, false);
         return;
       }
       const int x = m.x[(p.index + 1) & 1];
       const bool two = m.two_planes >> (p.index + 1) & 1;
-      for (int c = 0; c < kN; c += 64) {
-        if (col0 + c >= m.cp) break;
-        float v[64];
-        load64(acc, c, v, f);
+#pragma unroll
+      for (int c = 0; c < kCols; c += 64) {
+        if (col0 + c >= m.cp) continue;
         const int y = x + (col0 + c) / 64 * m.rp + row0;
-        put_rows(acc, v, y, false);
-        if (two) put_rows(acc, v, y + m.x_lo, true);
+        put_rows(acc, v + c, y, false);
+        if (two) put_rows(acc, v + c, y + m.x_lo, true);
       }
       return;
     }
-    if (row0 >= m.mp) return;
+    if (row0 >= m.mp || col0 >= m.mp) return;
     const int to = p.phase == kOrthGram ? m.a : m.p;
     float f = p.step.poly_c;
     if (p.phase == kOrthGram) {
       const float s = p.index == 0 ? p.ws.norm_factor[cur] : 1.f;
       f = p.step.gram * s * s;
     }
-    for (int c = 0; c < kN; c += 64) {
-      if (col0 + c >= m.mp) break;
-      float v[64];
-      load64(acc, c, v, f);
+#pragma unroll
+    for (int c = 0; c < kCols; c += 64) {
+      if (col0 + c >= m.mp) continue;
+#pragma unroll
+      for (int j = 0; j < 64; ++j) v[c + j] *= f;
       const int panel_row = (col0 + c) / 64 * m.mp + row0;
       if (p.phase == kOrthPoly) {
         for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) {
@@ -394,8 +363,8 @@ struct OrthJob {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&u[e]));
-              v[8 * j + 2 * e] = fmaf(p.step.poly_b, a.x, v[8 * j + 2 * e]);
-              v[8 * j + 2 * e + 1] = fmaf(p.step.poly_b, a.y, v[8 * j + 2 * e + 1]);
+              v[c + 8 * j + 2 * e] = fmaf(p.step.poly_b, a.x, v[c + 8 * j + 2 * e]);
+              v[c + 8 * j + 2 * e + 1] = fmaf(p.step.poly_b, a.y, v[c + 8 * j + 2 * e + 1]);
             }
           }
         }
@@ -403,41 +372,14 @@ struct OrthJob {
         if (d >= 0 && d < 64) {
 #pragma unroll
           for (int j = 0; j < 64; ++j)
-            if (j == d) v[j] += p.step.poly_a;
+            if (j == d) v[c + j] += p.step.poly_a;
         }
       }
       for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) {
-        put_rows(acc, v, to + plane * m.m_lo + panel_row, plane);
-        if (below) put_mirror(acc, v, row0 & 63, to + plane * m.m_lo + row0 / 64 * m.mp + col0 + c, plane);
+        put_rows(acc, v + c, to + plane * m.m_lo + panel_row, plane);
+        if (below) put_mirror(acc, v + c, row0 & 63, to + plane * m.m_lo + row0 / 64 * m.mp + col0 + c, plane);
       }
     }
-  }
-  __device__ __forceinline__ void load64(const Accumulator &acc, int c, float (&v)[64], float f) const {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t r[32];
-      load_columns(acc, c + 32 * h, r);
-#pragma unroll
-      for (int j = 0; j < 32; ++j) v[32 * h + j] = __uint_as_float(r[j]) * f;
-    }
-  }
-  template <int DT>
-  __device__ __forceinline__ void put_result(const OrthMatrix &m, const float (&v)[32], int row, int col) const {
-    constexpr int kPer = Elem<DT>::kPerVec;
-    char *q = static_cast<char *>(m.out) + (row * m.out_pitch + col) * Elem<DT>::kBytes;
-    if (col + 32 <= m.cols && ((uintptr_t)q & 15) == 0) {
-#pragma unroll
-      for (int j = 0; j < 32; j += kPer) {
-        float x[kPer];
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) x[e] = v[j + e];
-        *reinterpret_cast<uint4 *>(q + j * Elem<DT>::kBytes) = Elem<DT>::pack(x);
-      }
-      return;
-    }
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (col + j < m.cols) Elem<DT>::store1(q, j, v[j]);
   }
 };
 

@@ -3,13 +3,17 @@
 // A job (a struct with tile() and epilogue()) says what is multiplied and what becomes of the result.  The kernel stays on
 // the SM and takes tiles of kCtas * 128 x kN results in turn.  Warp 0 brings operand blocks in by TMA (64 of the contraction
 // at a time, 128-byte swizzle) through a ring of stages; one thread of warp 1 issues tcgen05.mma from there into one of two
-// accumulators in TMEM; warps 4 to 7 take the finished accumulator out, so that a tile's epilogue runs beside the next
-// tile's products.  With kCtas = 2 a pair of CTAs works on one tile: each holds half of both operands and half the
+// (four) accumulators in TMEM; warps 4 to 11 take a finished accumulator into registers, hand it back and work on from
+// there, beside the next products.  With kCtas = 2 a pair of CTAs works on one tile: each holds half of both operands and half the
 // accumulator's rows, and shared memory is read once for twice the products (cta_group::2; 64 instead of 96 bytes per SM and
 // cycle at 256 columns, which with the copies coming in is what 1-CTA tiles are short of).
 //
 // Operands are 16-bit (both bf16 or both fp16), products and sums fp32.  Either operand may lie with the contraction along
 // its rows ("K-major") or across them; both come in boxes of 64 rows x 64 elements, so that one tensor map serves both.
+//
+// A matrix instruction does not round what it adds to the accumulator, it cuts it off: over K terms sums come out smaller by up to
+// K / 16 units of 2^-24.  A tile may therefore have its accumulator taken out every `chunk` blocks and added up in registers,
+// rounded to nearest; what that costs is hidden behind the products (at 8 blocks no difference in time was measured).
 //
 // Every wait is bounded.  One that runs out raises a flag, the role leaves its loop, the others run out in turn, copies and
 // products in flight are waited for (again with a limit), TMEM is given back, FOPD_DEV_TIMEOUT goes to the status word.
@@ -128,11 +132,13 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
 // ------------------------------------------------------------------ tiles
 constexpr int kBoxRows = 64;                    // rows of one TMA box of 64 16-bit elements
 constexpr int kBoxBytes = kBoxRows * 128;
-constexpr int kProductThreads = 256;
-constexpr int kEpilogueWarp0 = 4, kEpilogueWarps = 4;
+constexpr int kProductThreads = 384;
+constexpr int kEpilogueWarp0 = 4, kEpilogueWarps = 8;  // two to each quarter of the rows, half of the columns each
 constexpr int kStageBufBytes = 32 * 128;        // an epilogue warp's staging buffer: its 32 rows x 128 bytes
 constexpr int kStageBufs = 2;
 constexpr uint32_t kTmemCols = 512;
+// Registers: 384 threads x 168 at launch; 128 x 64 + 256 x 216 = 63,488 of those 64,512 afterwards.
+constexpr int kRoleRegs = 64, kEpilogueRegs = 216;
 
 // One operand of a tile: where its boxes are.
 struct Operand {
@@ -148,6 +154,7 @@ struct Operand {
 struct Tile {
   Operand a, b;
   int k_blocks;  // 0: the product is zero
+  int chunk;     // blocks (of all passes) to an accumulator, 0: all
   int passes;
   uint32_t a_lo, b_lo;
 };
@@ -163,36 +170,42 @@ struct ProductShape {
   static constexpr int kBCols = kN / kCtas;  // of the tile's columns, this CTA's operand share
   static constexpr int kABoxes = 128 / kBoxRows, kBBoxes = kBCols / kBoxRows;
   static constexpr int kStageBytes = (kABoxes + kBBoxes) * kBoxBytes;
-  static constexpr int kStages = 192 * 1024 / kStageBytes;
+  static constexpr int kStages = 160 * 1024 / kStageBytes;
+  static constexpr int kAccs = (int)kTmemCols / kN;
   static constexpr int kSmem = kStages * kStageBytes + kEpilogueWarps * kStageBufs * kStageBufBytes + 1024;
 };
 
 struct ProductShared {
-  unsigned long long full[8], empty[8], acc_full[2], acc_empty[2], drain;
+  unsigned long long full[8], empty[8], acc_full[4], acc_empty[4], drain;
   uint32_t tmem;
   int failed;
 };
 
-// What an epilogue warp is given.
+// What an epilogue warp is given beside its values: columns half * kN / 2 and following of rows warp * 32 + lane of this CTA's 128.
 struct Accumulator {
-  uint32_t addr;     // TMEM address of the warp's 32 rows
-  int warp, lane;    // rows warp * 32 + lane of this CTA's 128
+  int warp, lane, half;
   uint32_t staging;  // two staging buffers
-  bool zero;         // the product is zero, TMEM holds nothing
 };
-__device__ __forceinline__ void load_columns(const Accumulator &acc, int col, uint32_t (&r)[32]) {
-  if (acc.zero) {
+// Takes a part of an accumulator: v = or += its columns.
+template <int kCols>
+__device__ __forceinline__ void take_columns(float (&v)[kCols], uint32_t addr, bool add) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) r[i] = 0;
-    return;
+  for (int c = 0; c < kCols; c += 32) {
+    uint32_t r[32];
+    tmem_load(r, addr + c);
+    tmem_wait(r);
+    if (add) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[c + j] += __uint_as_float(r[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[c + j] = __uint_as_float(r[j]);
+    }
   }
-  __syncwarp();
-  tmem_load(r, acc.addr + col);
-  tmem_wait(r);
 }
 
 // Job: Params (a kernel parameter); Job(params); int64_t tiles(); void tile(int64_t i, int cta, Tile &);
-// void epilogue(int64_t i, int cta, const Accumulator &); int32_t *status(); static constexpr bool kFp16.
+// void epilogue(int64_t i, int cta, const Accumulator &, float (&v)[kN / 2]); int32_t *status(); static constexpr bool kFp16.
 template <int kCtas, int kN, class Job>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ typename Job::Params params) {
   using Shape = ProductShape<kCtas, kN>;
@@ -209,7 +222,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       mbar_init(smem_u32(&sh.full[i]), 1);
       mbar_init(smem_u32(&sh.empty[i]), 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < Shape::kAccs; ++i) {
       mbar_init(smem_u32(&sh.acc_full[i]), 1);
       mbar_init(smem_u32(&sh.acc_empty[i]), kCtas * kEpilogueWarps);
     }
@@ -230,8 +243,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   Job job(params);
   const int64_t n_tiles = job.tiles();
 
-  if (warp == 0) {
-    if (lane == 0) {
+  if (warp < kEpilogueWarp0) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRoleRegs));
+    if (warp == 0 && lane == 0) {
       // ---- copies in
       int stage = 0, used = 0;
       uint32_t parity = 1;
@@ -272,42 +286,51 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       }
       if (!ok) sh.failed = 1;
     }
-  } else if (warp == 1) {
-    if (lane == 0 && cta == 0) {
+    if (warp == 1 && lane == 0 && cta == 0) {
       // ---- products
       int stage = 0;
-      uint32_t parity = 0, n = 0;
+      uint32_t parity = 0, buf = 0, turn = 1;  // turn: parity of acc_empty
       bool ok = true;
-      for (int64_t i = first; ok && i < n_tiles; i += step, ++n) {
+      for (int64_t i = first; ok && i < n_tiles; i += step) {
         Tile t;
         job.tile(i, cta, t);
         const uint32_t idesc = (1u << 4) | (Job::kFp16 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)t.a.across << 15) |
                                ((uint32_t)t.b.across << 16) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(kCtas * 128 >> 4) << 24);
         const uint32_t a_step = (t.a.across ? 16 * 128 : 32) >> 4, b_step = (t.b.across ? 16 * 128 : 32) >> 4;
-        const uint32_t buf = n & 1, d = tmem + buf * kN;
-        if (!mbar_wait_bounded(smem_u32(&sh.acc_empty[buf]), ((n >> 1) & 1) ^ 1, kWaitCycles)) {
-          ok = false;
-          break;
-        }
-        tc_fence_after();
-        const int blocks = t.passes * t.k_blocks;
-        for (int k = 0; k < blocks; ++k) {
-          if (!mbar_wait_bounded(smem_u32(&sh.full[stage]), parity, kWaitCycles)) {
+        const int blocks = t.passes * t.k_blocks, chunk = t.chunk > 0 ? t.chunk : blocks;
+        int done = 0;
+        do {
+          if (!mbar_wait_bounded(smem_u32(&sh.acc_empty[buf]), turn, kWaitCycles)) {
             ok = false;
             break;
           }
           tc_fence_after();
-          const uint32_t at = base + stage * Shape::kStageBytes;
-          const uint64_t a = smem_descriptor(at, t.a.across), b = smem_descriptor(at + Shape::kABoxes * kBoxBytes, t.b.across);
+          const uint32_t d = tmem + buf * kN;
+          const int end = min(blocks, done + chunk);
+          for (int k = done; k < end; ++k) {
+            if (!mbar_wait_bounded(smem_u32(&sh.full[stage]), parity, kWaitCycles)) {
+              ok = false;
+              break;
+            }
+            tc_fence_after();
+            const uint32_t at = base + stage * Shape::kStageBytes;
+            const uint64_t a = smem_descriptor(at, t.a.across), b = smem_descriptor(at + Shape::kABoxes * kBoxBytes, t.b.across);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) tc_mma<kCtas>(d, a + j * a_step, b + j * b_step, idesc, k > 0 || j > 0);
-          tc_commit<kCtas>(smem_u32(&sh.empty[stage]));
-          if (++stage == Shape::kStages) {
-            stage = 0;
-            parity ^= 1;
+            for (int j = 0; j < 4; ++j) tc_mma<kCtas>(d, a + j * a_step, b + j * b_step, idesc, k > done || j > 0);
+            tc_commit<kCtas>(smem_u32(&sh.empty[stage]));
+            if (++stage == Shape::kStages) {
+              stage = 0;
+              parity ^= 1;
+            }
           }
-        }
-        if (ok) tc_commit<kCtas>(smem_u32(&sh.acc_full[buf]));
+          if (!ok) break;
+          tc_commit<kCtas>(smem_u32(&sh.acc_full[buf]));
+          if (++buf == Shape::kAccs) {
+            buf = 0;
+            turn ^= 1;
+          }
+          done = end;
+        } while (done < blocks);
       }
       if (!ok) {  // let what has been issued end
         sh.failed = 1;
@@ -315,35 +338,54 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         mbar_wait_bounded(smem_u32(&sh.drain), 0, kWaitCycles);
       }
     }
-  } else if (warp >= kEpilogueWarp0) {
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpilogueRegs));
     // ---- results out
     Accumulator acc;
-    acc.warp = warp - kEpilogueWarp0;
+    acc.warp = (warp - kEpilogueWarp0) & 3;
+    acc.half = (warp - kEpilogueWarp0) >> 2;
     acc.lane = lane;
-    acc.staging = staging + acc.warp * kStageBufs * kStageBufBytes;
-    uint32_t n = 0;
+    acc.staging = staging + (warp - kEpilogueWarp0) * kStageBufs * kStageBufBytes;
+    const uint32_t mine = tmem + ((uint32_t)(acc.warp * 32) << 16) + acc.half * (kN / 2);
+    uint32_t buf = 0, turn = 0;
     bool ok = true;
-    for (int64_t i = first; ok && i < n_tiles; i += step, ++n) {
-      const uint32_t buf = n & 1;
-      Tile t;
-      job.tile(i, cta, t);
-      if (!mbar_wait_bounded(smem_u32(&sh.acc_full[buf]), (n >> 1) & 1, kWaitCycles)) ok = false;
-      if (!__all_sync(0xffffffffu, ok)) {
-        ok = false;
-        sh.failed = 1;
-        break;
+    for (int64_t i = first; ok && i < n_tiles; i += step) {
+      float v[kN / 2];
+      int blocks, chunk;
+      {
+        Tile t;
+        job.tile(i, cta, t);
+        blocks = t.passes * t.k_blocks;
+        chunk = t.chunk > 0 ? t.chunk : blocks;
       }
-      tc_fence_after();
-      acc.addr = tmem + buf * kN + ((uint32_t)(acc.warp * 32) << 16);
-      acc.zero = t.k_blocks == 0;
-      job.template epilogue<kN>(i, cta, acc);
-      tc_fence_before();
+      int done = 0;
+      do {
+        if (!mbar_wait_bounded(smem_u32(&sh.acc_full[buf]), turn, kWaitCycles)) ok = false;
+        if (!__all_sync(0xffffffffu, ok)) {
+          ok = false;
+          sh.failed = 1;
+          break;
+        }
+        tc_fence_after();
+        if (blocks > 0) take_columns(v, mine + buf * kN, done > 0);
+        else
+#pragma unroll
+          for (int j = 0; j < kN / 2; ++j) v[j] = 0.f;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          const uint32_t bar = smem_u32(&sh.acc_empty[buf]);
+          if constexpr (kCtas == 2) mbar_arrive_cluster(map_to_cta(bar, 0));
+          else mbar_arrive(bar);
+        }
+        if (++buf == Shape::kAccs) {
+          buf = 0;
+          turn ^= 1;
+        }
+        done += chunk;
+      } while (done < blocks);
+      if (ok) job.epilogue(i, cta, acc, v);
       __syncwarp();
-      if (lane == 0) {
-        const uint32_t bar = smem_u32(&sh.acc_empty[buf]);
-        if constexpr (kCtas == 2) mbar_arrive_cluster(map_to_cta(bar, 0));
-        else mbar_arrive(bar);
-      }
     }
     if (lane == 0) tma_store_wait_all();
   }
@@ -360,19 +402,59 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   if (threadIdx.x == 0 && sh.failed && job.status()) atomicOr(job.status(), FOPD_DEV_TIMEOUT);
 }
 
-// ------------------------------------------------------------------ results into rows of 64 16-bit elements
-// A warp's 32 rows x 64 results as a 128-byte-swizzled box, stored by TMA.
-template <class Convert>  // uint32_t Convert(float a, float b): two 16-bit results
-__device__ __forceinline__ void stage_half_box(uint32_t buf, int lane, int half, const float (&v)[32], Convert convert) {
+// ------------------------------------------------------------------ results out
+// 64 columns of a warp's rows as a 128-byte-swizzled box of 16-bit values: pack(j) gives columns 2 j and 2 j + 1.
+template <class Pack>
+__device__ __forceinline__ void stage_box(uint32_t at, int lane, Pack pack) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    uint32_t w[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = convert(v[8 * j + 2 * e], v[8 * j + 2 * e + 1]);
-    const uint32_t piece = (uint32_t)(half * 4 + j) ^ (lane & 7);
-    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(buf + lane * 128 + piece * 16), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-                 "r"(w[3])
+  for (int j = 0; j < 8; ++j)
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + lane * 128 + ((j ^ (lane & 7)) * 16)), "r"(pack(4 * j)),
+                 "r"(pack(4 * j + 1)), "r"(pack(4 * j + 2)), "r"(pack(4 * j + 3))
                  : "memory");
+}
+// A warp's staging buffers in turn: the one whose store was read from before the last.
+struct Staging {
+  uint32_t turn = 0;
+  __device__ __forceinline__ uint32_t next(const Accumulator &acc) {
+    const uint32_t at = acc.staging + turn * kStageBufBytes;
+    turn ^= 1;
+    if (acc.lane == 0) tma_store_wait_read<1>();
+    __syncwarp();
+    return at;
+  }
+  __device__ __forceinline__ void send(const Accumulator &acc, const CUtensorMap *map, int x, int y, uint32_t at) {
+    fence_async_shared();
+    __syncwarp();
+    if (acc.lane == 0) {
+      tma_store(map, x, y, at);
+      tma_store_commit();
+    }
+  }
+};
+// kCount results of a row from element `col` on, of which the row has `cols`; wide stores where they are aligned.
+template <int DT, int kCount>
+__device__ __forceinline__ void store_row(char *q, const float *g, int col, int cols, bool add) {
+  constexpr int kPer = Elem<DT>::kPerVec;
+  const bool aligned = ((uintptr_t)q & 15) == 0;
+#pragma unroll
+  for (int j = 0; j < kCount; j += kPer) {
+    if (aligned && col + j + kPer <= cols) {
+      float x[kPer];
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) x[e] = g[j + e];
+      uint4 *w = reinterpret_cast<uint4 *>(q + j * Elem<DT>::kBytes);
+      if (add) {
+        float o[kPer];
+        Elem<DT>::unpack(*w, o);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) x[e] += o[e];
+      }
+      *w = Elem<DT>::pack(x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kPer; ++e)
+        if (col + j + e < cols) Elem<DT>::store1(q, j + e, add ? g[j + e] + Elem<DT>::load1(q, j + e) : g[j + e]);
+    }
   }
 }
 
