@@ -38,7 +38,7 @@ struct OrthMatrix {
 
 constexpr int kNormChunk = 32768;  // elements to a block
 constexpr int kOrthThreads = 256;
-constexpr int kOrthChunk = 4;       // blocks of 64 that an accumulator adds up where the result is fp32
+constexpr int kOrthChunk = 2;       // blocks of 64 that an accumulator adds up where the result is fp32
 constexpr int kLoadCols = 256;     // a block of the load takes 64 rows of these
 
 struct OrthWorkspace {

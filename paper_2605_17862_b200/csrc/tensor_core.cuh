@@ -186,21 +186,16 @@ struct Accumulator {
   int warp, lane, half;
   uint32_t staging;  // two staging buffers
 };
-// Takes a part of an accumulator: v = or += its columns.
-template <int kCols>
-__device__ __forceinline__ void take_columns(float (&v)[kCols], uint32_t addr, bool add) {
+// Takes a part of an accumulator: v += its columns, or v = them (or zero).
+template <bool kAdd, int kCols>
+__device__ __forceinline__ void take_columns(float (&v)[kCols], uint32_t addr, bool zero) {
 #pragma unroll
   for (int c = 0; c < kCols; c += 32) {
     uint32_t r[32];
     tmem_load(r, addr + c);
     tmem_wait(r);
-    if (add) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[c + j] += __uint_as_float(r[j]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 32; ++j) v[c + j] = __uint_as_float(r[j]);
-    }
+    for (int j = 0; j < 32; ++j) v[c + j] = kAdd ? v[c + j] + __uint_as_float(r[j]) : zero ? 0.f : __uint_as_float(r[j]);
   }
 }
 
@@ -349,8 +344,25 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     const uint32_t mine = tmem + ((uint32_t)(acc.warp * 32) << 16) + acc.half * (kN / 2);
     uint32_t buf = 0, turn = 0;
     bool ok = true;
-    for (int64_t i = first; ok && i < n_tiles; i += step) {
-      float v[kN / 2];
+    const auto wait = [&] {
+      ok = __all_sync(0xffffffffu, mbar_wait_bounded(smem_u32(&sh.acc_full[buf]), turn, kWaitCycles));
+      tc_fence_after();
+      return ok;
+    };
+    const auto give_back = [&] {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        const uint32_t bar = smem_u32(&sh.acc_empty[buf]);
+        if constexpr (kCtas == 2) mbar_arrive_cluster(map_to_cta(bar, 0));
+        else mbar_arrive(bar);
+      }
+      if (++buf == Shape::kAccs) {
+        buf = 0;
+        turn ^= 1;
+      }
+    };
+    for (int64_t i = first; i < n_tiles; i += step) {
       int blocks, chunk;
       {
         Tile t;
@@ -358,35 +370,20 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         blocks = t.passes * t.k_blocks;
         chunk = t.chunk > 0 ? t.chunk : blocks;
       }
-      int done = 0;
-      do {
-        if (!mbar_wait_bounded(smem_u32(&sh.acc_full[buf]), turn, kWaitCycles)) ok = false;
-        if (!__all_sync(0xffffffffu, ok)) {
-          ok = false;
-          sh.failed = 1;
-          break;
-        }
-        tc_fence_after();
-        if (blocks > 0) take_columns(v, mine + buf * kN, done > 0);
-        else
-#pragma unroll
-          for (int j = 0; j < kN / 2; ++j) v[j] = 0.f;
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          const uint32_t bar = smem_u32(&sh.acc_empty[buf]);
-          if constexpr (kCtas == 2) mbar_arrive_cluster(map_to_cta(bar, 0));
-          else mbar_arrive(bar);
-        }
-        if (++buf == Shape::kAccs) {
-          buf = 0;
-          turn ^= 1;
-        }
-        done += chunk;
-      } while (done < blocks);
-      if (ok) job.epilogue(i, cta, acc, v);
+      if (!wait()) break;
+      float v[kN / 2];
+      take_columns<false>(v, mine + buf * kN, blocks == 0);
+      give_back();
+      for (int done = chunk; done < blocks; done += chunk) {
+        if (!wait()) break;
+        take_columns<true>(v, mine + buf * kN, false);
+        give_back();
+      }
+      if (!ok) break;
+      job.epilogue(i, cta, acc, v);
       __syncwarp();
     }
+    if (!ok) sh.failed = 1;
     if (lane == 0) tma_store_wait_all();
   }
 
