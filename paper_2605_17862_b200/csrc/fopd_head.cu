@@ -112,7 +112,7 @@ int run_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *status,
     p.token_logit = reinterpret_cast<float *>(tmp.base + logit);
     p.pitch = (int)pitch;
     p.status = status;
-    rc = launch_product<kCtas, kN, LogprobJob>(p, pitch / (kCtas * 128) * v_tiles, sms, st);
+    rc = launch_product<kCtas, kN, LogprobJob<kCtas, kN>>(p, pitch / (kCtas * 128) * v_tiles, sms, st);
     if (rc == FOPD_OK) {
       head_join_kernel<<<(unsigned)((h->n_rows + 31) / 32), 1024, 0, st>>>(pre.rows, p.part, p.token_logit, 2 * (int)v_tiles, (int)pitch,
                                                                            h->tokens, h->vocab, logprob, lse, status);
@@ -202,9 +202,9 @@ int run_grad(const fopd_head *h, const float *logprob, const float *lse, const f
       q.v0 = v0;
       q.v_count = (int)count;
       q.first = v0 == 0;
-      rc = launch_product<kCtas, kN, GradLogitsJob>(g, pitch / kRows * g.l.v_tiles, sms, st);
+      rc = launch_product<kCtas, kN, GradLogitsJob<kCtas, kN>>(g, pitch / kRows * g.l.v_tiles, sms, st);
       if (rc == FOPD_OK)
-        rc = launch_product<kCtas, kN, HeadGradsJob>(q, splits * h_tiles + (o.d_weight ? (count + kRows - 1) / kRows * d_tiles : 0), sms, st);
+        rc = launch_product<kCtas, kN, HeadGradsJob<kCtas, kN>>(q, splits * h_tiles + (o.d_weight ? (count + kRows - 1) / kRows * d_tiles : 0), sms, st);
     }
   }
   if (rc == FOPD_OK && o.d_hidden) {

@@ -10,8 +10,8 @@ using namespace fopd;
 
 namespace {
 
-constexpr int kMostSteps = 16;
-constexpr int kGroup = 250;                               // matrices of one table
+constexpr int kMostSteps = kOrthMostSteps;
+constexpr int kGroup = 240;                               // matrices of one table
 constexpr int64_t kGroupBytes = (int64_t)1 << 30;         // workspace of one group, unless a single matrix takes more
 constexpr float kLoud = 32.f;                             // amplification ahead from which X keeps its second plane
 
@@ -102,8 +102,8 @@ int make_scales(const float *coefficients, int32_t steps, Scales *s) {
   return FOPD_OK;
 }
 
-// One matrix's entry but for where it starts; the workspace rows it takes.
-OrthMatrix describe(const fopd_matrix &m, const Scales &s, int32_t steps, int64_t *rows) {
+// One matrix's entry but for where it starts.
+OrthMatrix describe(const fopd_matrix &m, const Scales &s, int32_t steps) {
   OrthMatrix o = {};
   o.data = m.data;
   o.out = m.out;
@@ -136,50 +136,53 @@ OrthMatrix describe(const fopd_matrix &m, const Scales &s, int32_t steps, int64_
   at += a * (1 + o.full);
   o.p = (int)at;
   at += a * (1 + o.full);
-  *rows = at;
+  o.space = (int)at;
   return o;
 }
 
+// The launches of one group.
+struct Group {
+  OrthWorkspace ws;
+  CUtensorMap boxes, rows_out, mirror_out;
+  int norm_blocks, load_blocks;
+  int64_t sym_tiles, x_tiles;
+  bool pairs;  // tiles of 256 x 256 on pairs of CTAs
+};
 template <int N>
-int launch_norm(const std::vector<OrthMatrix> &g, const OrthWorkspace &ws, int blocks, cudaStream_t st) {
+int run_table(const std::vector<OrthMatrix> &g, const Group &o, const Scales &s, int32_t steps, float eps, int32_t *status, int sms,
+              cudaStream_t st) {
   OrthTable<N> tab;
   tab.n = (int)g.size();
   std::copy(g.begin(), g.end(), tab.m);
-  orth_norm_kernel<N><<<(unsigned)blocks, kOrthThreads, 0, st>>>(tab, ws);
-  return launch_ok();
+  orth_norm_kernel<N><<<(unsigned)o.norm_blocks, kOrthThreads, 0, st>>>(tab, o.ws);
+  orth_load_kernel<N><<<(unsigned)o.load_blocks, kOrthThreads, 0, st>>>(tab, o.ws, eps, status);
+  if (launch_ok() != FOPD_OK) return FOPD_ERR_CUDA;
+  const auto run = [&](auto p, auto launch) {
+    p.boxes = o.boxes;
+    p.rows_out = o.rows_out;
+    p.mirror_out = o.mirror_out;
+    p.ws = o.ws;
+    std::copy(s.step, s.step + steps, p.step);
+    p.tab = tab;
+    p.steps = steps;
+    p.sym_tiles = (int)o.sym_tiles;
+    p.x_tiles = (int)o.x_tiles;
+    p.status = status;
+    return launch(p, std::max(o.x_tiles, o.sym_tiles), sms, st);
+  };
+  using Pairs = OrthJob<2, 256, N>;
+  using Single = OrthJob<1, 128, N>;
+  return o.pairs ? run(typename Pairs::Params(), launch_product<2, 256, Pairs>) : run(typename Single::Params(), launch_product<1, 128, Single>);
 }
 
-template <int kCtas, int kN>
-int run_steps(std::vector<OrthMatrix> &g, const OrthWorkspace &ws, const CUtensorMap *maps, const Scales &s, int32_t steps,
-              int64_t sym_tiles, int64_t x_tiles, int32_t *status, int sms, cudaStream_t st) {
-  typename OrthJob<kCtas, kN>::Params p;
-  p.boxes = maps[0];
-  p.rows_out = maps[1];
-  p.mirror_out = maps[2];
-  p.ws = ws;
-  p.n = (int)g.size();
-  p.status = status;
-  for (int k = 0; k < steps; ++k) {
-    p.step = s.step[k];
-    p.index = k;
-    p.last = k + 1 == steps;
-    for (int phase = kOrthGram; phase <= kOrthApply; ++phase) {
-      p.phase = phase;
-      p.n_tiles = phase == kOrthApply ? x_tiles : sym_tiles;
-      const int rc = launch_product<kCtas, kN, OrthJob>(p, p.n_tiles, sms, st);
-      if (rc != FOPD_OK) return rc;
-    }
-  }
-  return FOPD_OK;
-}
-
-int run_group(std::vector<OrthMatrix> &g, const std::vector<int64_t> &rows, const Scales &s, int32_t steps, float eps, int32_t *status,
-              int sms, cudaStream_t st) {
+int run_group(std::vector<OrthMatrix> &g, const Scales &s, int32_t steps, float eps, int32_t *status, int sms, cudaStream_t st) {
+  // the largest first: their phases take longest, and the small ones' tiles fill what is left
+  std::stable_sort(g.begin(), g.end(), [](const OrthMatrix &a, const OrthMatrix &b) { return (int64_t)a.rp * a.cp > (int64_t)b.rp * b.cp; });
   int64_t at = 0, norm_blocks = 0, load_blocks = 0, wide_tiles = 0;
   for (size_t i = 0; i < g.size(); ++i) {
     OrthMatrix &m = g[i];
     m.x[0] += (int)at, m.x[1] += (int)at, m.a += (int)at, m.p += (int)at;
-    at += rows[i];
+    at += m.space;
     m.norm_block = (int)norm_blocks;
     m.norm_blocks = (int)(((int64_t)m.rows * m.cols + kNormChunk - 1) / kNormChunk);
     norm_blocks += m.norm_blocks;
@@ -198,29 +201,28 @@ int run_group(std::vector<OrthMatrix> &g, const std::vector<int64_t> &rows, cons
     x_tiles += ((int64_t)(m.rp + tile - 1) / tile) * ((m.cp + tile - 1) / tile);
   }
   Layout lay;
-  const int64_t planes = lay.take(at * 128), table = lay.take((int64_t)g.size() * sizeof(OrthMatrix)),
-                factor = lay.take((int64_t)g.size() * 4), partial = lay.take(norm_blocks * 8);
+  const int64_t planes = lay.take(at * 128), factor = lay.take((int64_t)g.size() * 4), done = lay.take(((int64_t)g.size() + 1) * 4),
+                partial = lay.take(norm_blocks * 8);
   char *base = nullptr;
   int rc = scratch_alloc(reinterpret_cast<void **>(&base), (size_t)lay.bytes, st);
   if (rc != FOPD_OK) return rc;
-  const OrthWorkspace ws = {reinterpret_cast<OrthMatrix *>(base + table), reinterpret_cast<float *>(base + factor),
-                            reinterpret_cast<double *>(base + partial), reinterpret_cast<__half *>(base + planes)};
-  CUtensorMap maps[3];
-  rc = make_map(&maps[0], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, ws.planes, 64, at, 128, 64, kBoxRows, true);
-  if (rc == FOPD_OK) rc = make_map(&maps[1], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, ws.planes, 64, at, 128, 64, 32, true);
-  if (rc == FOPD_OK) rc = make_map(&maps[2], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, ws.planes, 64, at, 128, 32, 64, false);
+  Group o;
+  o.ws = {reinterpret_cast<float *>(base + factor), reinterpret_cast<int *>(base + done), reinterpret_cast<double *>(base + partial),
+          reinterpret_cast<__half *>(base + planes)};
+  o.norm_blocks = (int)norm_blocks;
+  o.load_blocks = (int)load_blocks;
+  o.sym_tiles = sym_tiles;
+  o.x_tiles = x_tiles;
+  o.pairs = tile == 256;
+  rc = make_map(&o.boxes, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, o.ws.planes, 64, at, 128, 64, kBoxRows, true);
+  if (rc == FOPD_OK) rc = make_map(&o.rows_out, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, o.ws.planes, 64, at, 128, 64, 32, true);
+  if (rc == FOPD_OK) rc = make_map(&o.mirror_out, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, o.ws.planes, 64, at, 128, 32, 64, false);
   if (rc == FOPD_OK) {
-    const int n = (int)g.size();
-    rc = n <= 8 ? launch_norm<8>(g, ws, (int)norm_blocks, st)
-                : n <= 64 ? launch_norm<64>(g, ws, (int)norm_blocks, st) : launch_norm<kGroup>(g, ws, (int)norm_blocks, st);
+    const size_t n = g.size();
+    rc = n <= 8    ? run_table<8>(g, o, s, steps, eps, status, sms, st)
+         : n <= 64 ? run_table<64>(g, o, s, steps, eps, status, sms, st)
+                   : run_table<kGroup>(g, o, s, steps, eps, status, sms, st);
   }
-  if (rc == FOPD_OK) {
-    orth_load_kernel<<<(unsigned)load_blocks, kOrthThreads, 0, st>>>(ws, (int)g.size(), eps, status);
-    rc = launch_ok();
-  }
-  if (rc == FOPD_OK)
-    rc = tile == 256 ? run_steps<2, 256>(g, ws, maps, s, steps, sym_tiles, x_tiles, status, sms, st)
-                     : run_steps<1, 128>(g, ws, maps, s, steps, sym_tiles, x_tiles, status, sms, st);
   if (cudaFreeAsync(base, st) != cudaSuccess && rc == FOPD_OK) rc = FOPD_ERR_CUDA;
   return rc;
 }
@@ -243,25 +245,21 @@ int fopd_orthogonalise(const fopd_matrix *matrices, int32_t n, const float *coef
     if (rc != FOPD_OK) return rc;
     int sms = 0;
     std::vector<OrthMatrix> group;
-    std::vector<int64_t> rows;
     int64_t total = 0;
     for (int32_t i = 0; i < n; ++i) {
       if (matrices[i].rows == 0 || matrices[i].cols == 0) continue;
       if (sms == 0 && (rc = current_sms(&sms)) != FOPD_OK) return rc;
-      int64_t r = 0;
-      const OrthMatrix m = describe(matrices[i], s, steps, &r);
-      if (!group.empty() && ((int)group.size() == kGroup || (total + r) * 128 > kGroupBytes)) {
-        rc = run_group(group, rows, s, steps, eps, status, sms, static_cast<cudaStream_t>(stream));
+      const OrthMatrix m = describe(matrices[i], s, steps);
+      if (!group.empty() && ((int)group.size() == kGroup || (total + m.space) * 128 > kGroupBytes)) {
+        rc = run_group(group, s, steps, eps, status, sms, static_cast<cudaStream_t>(stream));
         if (rc != FOPD_OK) return rc;
         group.clear();
-        rows.clear();
         total = 0;
       }
       group.push_back(m);
-      rows.push_back(r);
-      total += r;
+      total += m.space;
     }
-    return group.empty() ? FOPD_OK : run_group(group, rows, s, steps, eps, status, sms, static_cast<cudaStream_t>(stream));
+    return group.empty() ? FOPD_OK : run_group(group, s, steps, eps, status, sms, static_cast<cudaStream_t>(stream));
   } catch (...) {  // host memory for the table
     return FOPD_ERR_CUDA;
   }

@@ -116,7 +116,7 @@ __device__ __forceinline__ void logit_tile(const LogitTiles &l, int n_rows, int6
 // stored token's left out of the sum: the log-prob of a nearly certain token comes from the others' sum.
 template <int kCtas, int kN>
 struct LogprobJob {
-  static constexpr bool kFp16 = false;
+  static constexpr bool kFp16 = false, kClaimed = false;
   struct Params {
     CUtensorMap hidden, weight;
     LogitTiles l;
@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(1024) head_join_kernel(HeadRows rows, const fl
 // bf16 results' own.
 template <int kCtas, int kN>
 struct GradLogitsJob {
-  static constexpr bool kFp16 = false;
+  static constexpr bool kFp16 = false, kClaimed = false;
   struct Params {
     CUtensorMap hidden, weight, panels_out;
     LogitTiles l;
@@ -300,7 +300,7 @@ struct GradLogitsJob {
 // (in the workspace, in a fixed order); d_weight's run along the rows and are finished.
 template <int kCtas, int kN>
 struct HeadGradsJob {
-  static constexpr bool kFp16 = false;
+  static constexpr bool kFp16 = false, kClaimed = false;
   struct Params {
     CUtensorMap hidden, weight, panels;
     HeadRows rows;

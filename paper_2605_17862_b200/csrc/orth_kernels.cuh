@@ -30,6 +30,7 @@ struct OrthMatrix {
   int x[2], x_lo;      // workspace rows (of 64 elements) where X starts (two in turn), and from its first plane to the second
   int a, p, m_lo;      // the same for A and P
   uint32_t two_planes; // bit k: X of step k has its second plane
+  int space;           // workspace rows of all of it
   int sym_tile, x_tile;  // first tile of the matrix
   int norm_block, norm_blocks, load_block;
   float scale;
@@ -42,12 +43,14 @@ constexpr int kOrthChunk = 2;       // blocks of 64 that an accumulator adds up 
 constexpr int kLoadCols = 256;     // a block of the load takes 64 rows of these
 
 struct OrthWorkspace {
-  OrthMatrix *table;
   float *norm_factor;  // per matrix: 1 / ((|M| + eps) 2^e)
+  int *done;           // per matrix: units of finished tiles (one for each epilogue warp); behind the last one the tiles claimed
   double *partial;     // per block of the norm
   __half *planes;
 };
 
+// The list travels as a kernel parameter (at most 32,764 bytes), in sizes so that short lists are quick to hand over: all that
+// the products' tiles need of it comes through the constant cache, which waiting for other tiles' results leaves alone.
 template <int N>
 struct OrthTable {
   int n;
@@ -81,17 +84,12 @@ __device__ __forceinline__ double block_sum(double s, double *scratch) {
   return t;
 }
 
-// Sums of squares in fp64, a block to 32,768 elements; the table goes to the workspace for the launches that follow.
+// Sums of squares in fp64, a block to 32,768 elements.
 template <int N>
 __global__ void __launch_bounds__(kOrthThreads) orth_norm_kernel(const __grid_constant__ OrthTable<N> tab, OrthWorkspace ws) {
   __shared__ double scratch[kOrthThreads / 32];
   const int k = find_entry(tab.n, (int)blockIdx.x, [&](int j) { return tab.m[j].norm_block; });
   const OrthMatrix &m = tab.m[k];
-  if ((int)blockIdx.x == m.norm_block) {
-    const uint32_t *src = reinterpret_cast<const uint32_t *>(&m);
-    uint32_t *dst = reinterpret_cast<uint32_t *>(ws.table + k);
-    if (threadIdx.x < sizeof(OrthMatrix) / 4) dst[threadIdx.x] = src[threadIdx.x];
-  }
   const int64_t all = (int64_t)m.rows * m.cols, from = (int64_t)((int)blockIdx.x - m.norm_block) * kNormChunk;
   const int64_t to = from + kNormChunk < all ? from + kNormChunk : all;
   double s = 0.0;
@@ -136,10 +134,12 @@ __device__ __forceinline__ void split_half(float x, __half &hi, __half &lo) {
 
 // Into the workspace times 2^e, with 2^e |M| in [2^14, 2^15): no element leaves fp16's range, and bf16 ones are exact down to 2^-24.
 // A block takes 64 rows x 256 columns and forms the norm from the partial sums itself (in order).
-__global__ void __launch_bounds__(kOrthThreads) orth_load_kernel(OrthWorkspace ws, int n, float eps, int32_t *status) {
+template <int N>
+__global__ void __launch_bounds__(kOrthThreads) orth_load_kernel(const __grid_constant__ OrthTable<N> tab, OrthWorkspace ws, float eps,
+                                                                 int32_t *status) {
   __shared__ double scratch[kOrthThreads / 32];
-  const int k = find_entry(n, (int)blockIdx.x, [&](int j) { return ws.table[j].load_block; });
-  const OrthMatrix m = ws.table[k];
+  const int k = find_entry(tab.n, (int)blockIdx.x, [&](int j) { return tab.m[j].load_block; });
+  const OrthMatrix &m = tab.m[k];
   const int block = (int)blockIdx.x - m.load_block;
   double s = 0.0;
   for (int i = threadIdx.x; i < m.norm_blocks; i += kOrthThreads) s += ws.partial[m.norm_block + i];
@@ -154,6 +154,8 @@ __global__ void __launch_bounds__(kOrthThreads) orth_load_kernel(OrthWorkspace w
   }
   scale = finite ? exp2((double)e) : __longlong_as_double(0x7ff8000000000000ll);
   if (block == 0 && threadIdx.x == 0) {
+    ws.done[k] = 0;
+    if (k == 0) ws.done[tab.n] = 0;
     ws.norm_factor[k] = finite ? (float)factor : __int_as_float(0x7fffffff);
     if (!finite && status) atomicOr(status, FOPD_DEV_NONFINITE);
   }
@@ -198,7 +200,11 @@ __global__ void __launch_bounds__(kOrthThreads) orth_load_kernel(OrthWorkspace w
 }
 
 // ------------------------------------------------------------------ the products
+// All steps of all matrices in one launch.  Tiles are numbered step by step and in a step phase by phase over the whole list; one
+// that needs the results of the phase before waits for that phase of its own matrix only, so that the tail of one matrix's phase runs
+// beside the other matrices' tiles, and a phase of a single matrix costs a signal through the L2 instead of a launch.
 enum OrthPhase { kOrthGram = 0, kOrthPoly = 1, kOrthApply = 2 };
+constexpr int kOrthMostSteps = 16;
 
 // Factors of one step (powers of two but for the coefficients).  Values in the workspace are X 2^ex, A 2^ea, P 2^ep.
 struct OrthStep {
@@ -207,64 +213,91 @@ struct OrthStep {
   float apply;                  // from P X to the next X's scale; last step: to 1 (first step: on top of norm_factor)
 };
 
-template <int kCtas, int kN>
+template <int kCtas, int kN, int N>
 struct OrthJob {
-  static constexpr bool kFp16 = true;
+  static constexpr bool kFp16 = true, kClaimed = true;
   static constexpr int kRows = kCtas * 128;
   static_assert(kN == kRows, "symmetric tiles");
   struct Params {
     CUtensorMap boxes, rows_out, mirror_out;
     OrthWorkspace ws;
-    OrthStep step;
-    int n;
-    int64_t n_tiles;
-    int phase, index, last;
+    OrthStep step[kOrthMostSteps];
+    OrthTable<N> tab;
+    int steps;
+    int sym_tiles, x_tiles;  // of the list, in each step
     int32_t *status;
   };
+  struct Place {
+    int k, step, phase, row0, col0;
+    bool last;
+  };
   const Params &p;
-  int cur = 0;
   Staging staging;
   __device__ explicit OrthJob(const Params &params) : p(params) {}
-  __device__ int64_t tiles() const { return p.n_tiles; }
+  __device__ int64_t tiles() const { return (int64_t)p.steps * (2 * p.sym_tiles + p.x_tiles); }
   __device__ int32_t *status() const { return p.status; }
-  __device__ __forceinline__ int first(int k) const { return p.phase == kOrthApply ? p.ws.table[k].x_tile : p.ws.table[k].sym_tile; }
-  // Matrix and place of tile i (tiles come in ascending order).
-  __device__ __forceinline__ const OrthMatrix &at(int64_t i, int &row0, int &col0) {
-    while (cur + 1 < p.n && first(cur + 1) <= i) ++cur;
-    const OrthMatrix &m = p.ws.table[cur];
-    const int t = (int)i - first(cur);
-    if (p.phase == kOrthApply) {
-      const int across = (m.cp + kN - 1) / kN;
-      row0 = t / across * kRows;
-      col0 = t % across * kN;
+  __device__ int *counter() const { return p.ws.done + p.tab.n; }
+  __device__ __forceinline__ Place place(int64_t i) const {
+    Place o;
+    const int per = 2 * p.sym_tiles + p.x_tiles;
+    o.step = (int)(i / per);
+    o.last = o.step + 1 == p.steps;
+    int t = (int)(i - (int64_t)o.step * per);
+    o.phase = t < p.sym_tiles ? kOrthGram : t < 2 * p.sym_tiles ? kOrthPoly : kOrthApply;
+    t -= o.phase * p.sym_tiles;
+    const OrthMatrix *tab = p.tab.m;
+    if (o.phase == kOrthApply) {
+      o.k = find_entry(p.tab.n, t, [&](int j) { return tab[j].x_tile; });
+      t -= tab[o.k].x_tile;
+      const int across = (tab[o.k].cp + kN - 1) / kN;
+      o.row0 = t / across * kRows;
+      o.col0 = t % across * kN;
     } else {
+      o.k = find_entry(p.tab.n, t, [&](int j) { return tab[j].sym_tile; });
+      t -= tab[o.k].sym_tile;
       int r = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
       while (r * (r + 1) / 2 > t) --r;
       while ((r + 1) * (r + 2) / 2 <= t) ++r;
-      row0 = r * kRows;
-      col0 = (t - r * (r + 1) / 2) * kN;
+      o.row0 = r * kRows;
+      o.col0 = (t - r * (r + 1) / 2) * kN;
     }
-    return m;
+    return o;
   }
-  __device__ __forceinline__ void tile(int64_t i, int cta, Tile &t) {
-    int row0, col0;
-    const OrthMatrix &m = at(i, row0, col0);
-    row0 += cta * 128;
-    col0 += cta * (kN / kCtas);
-    const bool x_two = p.phase != kOrthPoly && (m.two_planes >> p.index & 1);
-    const int x = m.x[p.index & 1];
+  // Units of a matrix's tiles before this phase.
+  __device__ __forceinline__ int units_before(const Place &o, const OrthMatrix &m) const {
+    const int s = (m.mp + kN - 1) / kN, sym = s * (s + 1) / 2, x = ((m.rp + kRows - 1) / kRows) * ((m.cp + kN - 1) / kN);
+    return kCtas * kEpilogueWarps * (o.step * (2 * sym + x) + o.phase * sym);
+  }
+  __device__ __forceinline__ bool ready(int64_t i, long long limit) const {
+    const Place o = place(i);
+    const int want = units_before(o, p.tab.m[o.k]);
+    const int *done = p.ws.done + o.k;
+    if (load_acquire(done) < want) {
+      const long long t0 = clock64();
+      while (load_acquire(done) < want)
+        if (clock64() - t0 > limit) return false;
+    }
+    fence_async_global();  // (the copies that follow are of another proxy than the load)
+    return true;
+  }
+  __device__ __forceinline__ void tile(int64_t i, int cta, Tile &t) const {
+    const Place o = place(i);
+    const OrthMatrix &m = p.tab.m[o.k];
+    const int row0 = o.row0 + cta * 128, col0 = o.col0 + cta * (kN / kCtas);
+    const bool x_two = m.two_planes >> o.step & 1;
+    const int x = m.x[o.step & 1];
     // along: rows of the operand are rows of the plane; across: they are its columns
     const auto along = [&](int y, int pitch, int r, int lo) { return Operand{&p.boxes, 0, y + r, 0, pitch, 0, 64, lo, false}; };
     const auto across = [&](int y, int pitch, int r, int lo) { return Operand{&p.boxes, 0, y + r / 64 * pitch, 0, 64, 0, pitch, lo, true}; };
     t.a_lo = t.b_lo = 0;
     t.passes = 1;
     t.chunk = m.full ? kOrthChunk : 0;
-    if (p.phase == kOrthGram) {
+    if (o.phase == kOrthGram) {
       t.a = m.tall ? across(x, m.rp, row0, m.x_lo) : along(x, m.rp, row0, m.x_lo);
       t.b = m.tall ? across(x, m.rp, col0, m.x_lo) : along(x, m.rp, col0, m.x_lo);
       t.k_blocks = (m.tall ? m.rp : m.cp) / 64;
       if (m.full && x_two) t.passes = 3, t.b_lo = 1, t.a_lo = 2;
-    } else if (p.phase == kOrthPoly) {
+    } else if (o.phase == kOrthPoly) {
       t.a = along(m.a, m.mp, row0, m.m_lo);
       t.b = along(m.a, m.mp, col0, m.m_lo);
       t.k_blocks = m.mp / 64;
@@ -309,43 +342,57 @@ struct OrthJob {
   }
 
   __device__ __forceinline__ void epilogue(int64_t i, int cta, const Accumulator &acc, float (&v)[kN / 2]) {
+    const Place o = place(i);
+    const OrthMatrix &m = p.tab.m[o.k];
+    const int row0 = o.row0 + cta * 128 + acc.warp * 32, col0 = o.col0 + acc.half * (kN / 2);
+    if (o.phase == kOrthApply) put_x(o, m, row0, col0, acc, v);
+    else put_square(o, m, row0, col0, acc, v);
+    if (acc.lane == 0 && !(o.last && o.phase == kOrthApply)) {  // written, then counted
+      tma_store_wait_all();
+      __threadfence();
+      add_release(p.ws.done + o.k, 1);
+    }
+  }
+  __device__ __forceinline__ void put_x(const Place &o, const OrthMatrix &m, int row0, int col0, const Accumulator &acc, float (&v)[kN / 2]) {
     constexpr int kCols = kN / 2;
-    int row0, col0;
-    const OrthMatrix &m = at(i, row0, col0);
-    const bool below = p.phase != kOrthApply && row0 != col0;
-    row0 += cta * 128 + acc.warp * 32;
-    col0 += acc.half * kCols;
-    const int row = row0 + acc.lane;
-    if (p.phase == kOrthApply) {
-      if (row0 >= m.rp || col0 >= m.cp) return;
-      const float f = (p.index == 0 ? p.ws.norm_factor[cur] : 1.f) * p.step.apply * (p.last ? m.scale : 1.f);
+    if (row0 >= m.rp || col0 >= m.cp) return;
+    const float f = (o.step == 0 ? p.ws.norm_factor[o.k] : 1.f) * p.step[o.step].apply * (o.last ? m.scale : 1.f);
 #pragma unroll
-      for (int j = 0; j < kCols; ++j) v[j] *= f;
-      if (p.last) {
-        if (row >= m.rows) return;
-        const int64_t at = row * m.out_pitch + col0;
-        char *out = static_cast<char *>(m.out);
-        if (m.out_dtype == FOPD_F32) store_row<FOPD_F32, kCols>(out + at * 4, v, col0, m.cols, false);
-        else store_row<FOPD_BF16, kCols>(out + at * 2, v, col0, m.cols, false);
-        return;
-      }
-      const int x = m.x[(p.index + 1) & 1];
-      const bool two = m.two_planes >> (p.index + 1) & 1;
-#pragma unroll
-      for (int c = 0; c < kCols; c += 64) {
-        if (col0 + c >= m.cp) continue;
-        const int y = x + (col0 + c) / 64 * m.rp + row0;
-        put_rows(acc, v + c, y, false);
-        if (two) put_rows(acc, v + c, y + m.x_lo, true);
-      }
+    for (int j = 0; j < kCols; ++j) v[j] *= f;
+    if (o.last) {
+      const int row = row0 + acc.lane;
+      if (row >= m.rows) return;
+      const int64_t at = row * m.out_pitch + col0;
+      char *out = static_cast<char *>(m.out);
+      if (m.out_dtype == FOPD_F32) store_row<FOPD_F32, kCols>(out + at * 4, v, col0, m.cols, false);
+      else store_row<FOPD_BF16, kCols>(out + at * 2, v, col0, m.cols, false);
       return;
     }
+    const int x = m.x[(o.step + 1) & 1];
+    const bool two = m.two_planes >> (o.step + 1) & 1;
+#pragma unroll
+    for (int c = 0; c < kCols; c += 64) {
+      if (col0 + c >= m.cp) continue;
+      const int y = x + (col0 + c) / 64 * m.rp + row0;
+      put_rows(acc, v + c, y, false);
+      if (two) put_rows(acc, v + c, y + m.x_lo, true);
+    }
+  }
+  __device__ __forceinline__ void put_square(const Place &o, const OrthMatrix &m, int row0, int col0, const Accumulator &acc,
+                                             float (&v)[kN / 2]) {
+    constexpr int kCols = kN / 2;
     if (row0 >= m.mp || col0 >= m.mp) return;
-    const int to = p.phase == kOrthGram ? m.a : m.p;
-    float f = p.step.poly_c;
-    if (p.phase == kOrthGram) {
-      const float s = p.index == 0 ? p.ws.norm_factor[cur] : 1.f;
-      f = p.step.gram * s * s;
+    const bool below = o.row0 != o.col0;
+    const OrthStep &step = p.step[o.step];
+    const int to = o.phase == kOrthGram ? m.a : m.p;
+    float f = step.poly_c;
+    if (o.phase == kOrthGram) {
+      const float s = o.step == 0 ? p.ws.norm_factor[o.k] : 1.f;
+      f = step.gram * s * s;
+    } else {
+      // (A was stored by other SMs: this warp reads it itself, so it looks at the count itself)
+      if (acc.lane == 0) load_acquire(p.ws.done + o.k);
+      __syncwarp();
     }
 #pragma unroll
     for (int c = 0; c < kCols; c += 64) {
@@ -353,7 +400,7 @@ struct OrthJob {
 #pragma unroll
       for (int j = 0; j < 64; ++j) v[c + j] *= f;
       const int panel_row = (col0 + c) / 64 * m.mp + row0;
-      if (p.phase == kOrthPoly) {
+      if (o.phase == kOrthPoly) {
         for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) {
           const uint4 *q = reinterpret_cast<const uint4 *>(p.ws.planes + ((int64_t)m.a + plane * m.m_lo + panel_row + acc.lane) * 64);
 #pragma unroll
@@ -363,16 +410,15 @@ struct OrthJob {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&u[e]));
-              v[c + 8 * j + 2 * e] = fmaf(p.step.poly_b, a.x, v[c + 8 * j + 2 * e]);
-              v[c + 8 * j + 2 * e + 1] = fmaf(p.step.poly_b, a.y, v[c + 8 * j + 2 * e + 1]);
+              v[c + 8 * j + 2 * e] = fmaf(step.poly_b, a.x, v[c + 8 * j + 2 * e]);
+              v[c + 8 * j + 2 * e + 1] = fmaf(step.poly_b, a.y, v[c + 8 * j + 2 * e + 1]);
             }
           }
         }
-        const int d = row - (col0 + c);
+        const int d = row0 + acc.lane - (col0 + c);
         if (d >= 0 && d < 64) {
 #pragma unroll
-          for (int j = 0; j < 64; ++j)
-            if (j == d) v[c + j] += p.step.poly_a;
+          for (int j = 0; j < 64; ++j) v[c + j] += j == d ? step.poly_a : 0.f;
         }
       }
       for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) {

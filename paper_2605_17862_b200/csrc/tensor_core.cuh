@@ -129,6 +129,24 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
+__device__ __forceinline__ void mbar_expect_tx_cluster(uint32_t cluster_bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(cluster_bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void st_async_s32(uint32_t cluster_addr, int v, uint32_t cluster_bar) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.s32 [%0], %1, [%2];" ::"r"(cluster_addr), "r"(v),
+               "r"(cluster_bar)
+               : "memory");
+}
+__device__ __forceinline__ int load_acquire(const int *p) {
+  int v;
+  asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void add_release(int *p, int v) {
+  asm volatile("red.release.gpu.global.add.s32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
+__device__ __forceinline__ void fence_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
+
 // ------------------------------------------------------------------ tiles
 constexpr int kBoxRows = 64;                    // rows of one TMA box of 64 16-bit elements
 constexpr int kBoxBytes = kBoxRows * 128;
@@ -175,8 +193,10 @@ struct ProductShape {
   static constexpr int kSmem = kStages * kStageBytes + kEpilogueWarps * kStageBufs * kStageBufBytes + 1024;
 };
 
+constexpr int kFeed = 4;  // tiles a CTA (pair) has claimed and some role has not yet taken note of
 struct ProductShared {
-  unsigned long long full[8], empty[8], acc_full[4], acc_empty[4], drain;
+  unsigned long long full[8], empty[8], acc_full[4], acc_empty[4], drain, feed_full[kFeed], feed_empty[kFeed];
+  int feed[kFeed];
   uint32_t tmem;
   int failed;
 };
@@ -199,8 +219,72 @@ __device__ __forceinline__ void take_columns(float (&v)[kCols], uint32_t addr, b
   }
 }
 
+// Which tiles a CTA (pair) works on, as each role sees them.  Either every step-th one, or, where tiles wait for others (kClaimed),
+// the next that no one has: the thread that brings the first CTA's operands in takes it from a counter when it has nothing
+// left to ask for, and passes it on through shared memory.  Tiles are claimed in an order in which each comes behind those it waits for,
+// and a claimed tile is worked on: whatever part of the grid is resident, the lowest unfinished tile can always go on.
+constexpr long long kLongWaitCycles = 2000000000;  // (~1 s: behind a claimed tile's wait for others)
+template <int kCtas, class Job>
+struct TileFeed {
+  static constexpr long long kLimit = Job::kClaimed ? kLongWaitCycles : kWaitCycles;
+  ProductShared &sh;
+  const int cta;
+  const int64_t n_tiles, step;
+  int64_t i;
+  uint32_t n = 0;
+  bool ok = true;
+  __device__ TileFeed(ProductShared &s, int c, int64_t tiles) : sh(s), cta(c), n_tiles(tiles), step(gridDim.x / kCtas), i((int64_t)(blockIdx.x / kCtas) - step) {}
+  // -1: no more, or a wait ran out (then ok is false)
+  __device__ __forceinline__ int64_t next_claimed(int *counter) {
+    const uint32_t slot = n % kFeed;
+    if (!mbar_wait_cluster_bounded(smem_u32(&sh.feed_empty[slot]), ((n / kFeed) & 1) ^ 1, kLimit)) {
+      ok = false;
+      return -1;
+    }
+    ++n;
+    int v = atomicAdd(counter, 1);
+    if (v >= n_tiles) v = -1;
+    if constexpr (kCtas == 1) {
+      sh.feed[slot] = v;
+      mbar_arrive(smem_u32(&sh.feed_full[slot]));
+    } else {
+      for (int r = 0; r < kCtas; ++r) {
+        const uint32_t bar = map_to_cta(smem_u32(&sh.feed_full[slot]), r);
+        mbar_expect_tx_cluster(bar, 4);
+        st_async_s32(map_to_cta(smem_u32(&sh.feed[slot]), r), v, bar);
+      }
+    }
+    return v;
+  }
+  template <bool kWarp>  // all lanes of a warp, or one thread
+  __device__ __forceinline__ int64_t next() {
+    if constexpr (!Job::kClaimed) {
+      i += step;
+      return i < n_tiles ? i : -1;
+    } else {
+      const uint32_t slot = n % kFeed;
+      bool here = mbar_wait_cluster_bounded(smem_u32(&sh.feed_full[slot]), (n / kFeed) & 1, kLimit);
+      if (kWarp) here = __all_sync(0xffffffffu, here);
+      if (!here) {
+        ok = false;
+        return -1;
+      }
+      ++n;
+      const int v = *reinterpret_cast<volatile int *>(&sh.feed[slot]);
+      if (kWarp) __syncwarp();
+      if (!kWarp || (threadIdx.x & 31) == 0) {
+        const uint32_t bar = smem_u32(&sh.feed_empty[slot]);
+        if constexpr (kCtas == 2) mbar_arrive_cluster(map_to_cta(bar, 0));
+        else mbar_arrive(bar);
+      }
+      return v;
+    }
+  }
+};
+
 // Job: Params (a kernel parameter); Job(params); int64_t tiles(); void tile(int64_t i, int cta, Tile &);
-// void epilogue(int64_t i, int cta, const Accumulator &, float (&v)[kN / 2]); int32_t *status(); static constexpr bool kFp16.
+// void epilogue(int64_t i, int cta, const Accumulator &, float (&v)[kN / 2]); int32_t *status(); static constexpr bool kFp16,
+// kClaimed; and where that is true int *counter() and bool ready(int64_t i, long long limit), which returns when what tile i reads is there.
 template <int kCtas, int kN, class Job>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ typename Job::Params params) {
   using Shape = ProductShape<kCtas, kN>;
@@ -210,7 +294,6 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   const uint32_t base = (smem_u32(product_smem) + 1023u) & ~1023u;
   const uint32_t staging = base + Shape::kStages * Shape::kStageBytes;
   const int cta = kCtas == 2 ? (int)cluster_ctarank() : 0;
-  const int64_t first = blockIdx.x / kCtas, step = gridDim.x / kCtas;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < Shape::kStages; ++i) {
@@ -220,6 +303,10 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     for (int i = 0; i < Shape::kAccs; ++i) {
       mbar_init(smem_u32(&sh.acc_full[i]), 1);
       mbar_init(smem_u32(&sh.acc_empty[i]), kCtas * kEpilogueWarps);
+    }
+    for (int i = 0; i < kFeed; ++i) {  // (read by the products' thread and the epilogues; the second CTA's copies in)
+      mbar_init(smem_u32(&sh.feed_full[i]), 1);
+      mbar_init(smem_u32(&sh.feed_empty[i]), kCtas * (1 + kEpilogueWarps));
     }
     mbar_init(smem_u32(&sh.drain), 1);
     sh.failed = 0;
@@ -236,7 +323,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   const uint32_t tmem = sh.tmem;
 
   Job job(params);
-  const int64_t n_tiles = job.tiles();
+  TileFeed<kCtas, Job> feed(sh, cta, job.tiles());
+  constexpr long long kLimit = TileFeed<kCtas, Job>::kLimit;
 
   if (warp < kEpilogueWarp0) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRoleRegs));
@@ -245,13 +333,21 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       int stage = 0, used = 0;
       uint32_t parity = 1;
       bool ok = true;
-      for (int64_t i = first; ok && i < n_tiles; i += step) {
+      while (ok) {
+        int64_t i;
+        if constexpr (Job::kClaimed) {
+          i = cta == 0 ? feed.next_claimed(job.counter()) : feed.template next<false>();
+          if (i >= 0 && !job.ready(i, kLimit)) ok = false;
+        } else {
+          i = feed.template next<false>();
+        }
+        if (i < 0 || !ok) break;
         Tile t;
         job.tile(i, cta, t);
         for (int pass = 0; ok && pass < t.passes; ++pass) {
           const int ya = t.a.y + ((t.a_lo >> pass & 1) ? t.a.lo : 0), yb = t.b.y + ((t.b_lo >> pass & 1) ? t.b.lo : 0);
           for (int k = 0; k < t.k_blocks; ++k) {
-            if (!mbar_wait_bounded(smem_u32(&sh.empty[stage]), parity, kWaitCycles)) {
+            if (!mbar_wait_bounded(smem_u32(&sh.empty[stage]), parity, kLimit)) {
               ok = false;
               break;
             }
@@ -279,14 +375,14 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         stage = stage == 0 ? Shape::kStages - 1 : stage - 1;
         if (!mbar_wait_bounded(smem_u32(&sh.empty[stage]), parity ^ 1, kWaitCycles)) ok = false;
       }
-      if (!ok) sh.failed = 1;
+      if (!ok || !feed.ok) sh.failed = 1;
     }
     if (warp == 1 && lane == 0 && cta == 0) {
       // ---- products
       int stage = 0;
       uint32_t parity = 0, buf = 0, turn = 1;  // turn: parity of acc_empty
       bool ok = true;
-      for (int64_t i = first; ok && i < n_tiles; i += step) {
+      for (int64_t i; ok && (i = feed.template next<false>()) >= 0;) {
         Tile t;
         job.tile(i, cta, t);
         const uint32_t idesc = (1u << 4) | (Job::kFp16 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)t.a.across << 15) |
@@ -295,7 +391,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         const int blocks = t.passes * t.k_blocks, chunk = t.chunk > 0 ? t.chunk : blocks;
         int done = 0;
         do {
-          if (!mbar_wait_bounded(smem_u32(&sh.acc_empty[buf]), turn, kWaitCycles)) {
+          if (!mbar_wait_bounded(smem_u32(&sh.acc_empty[buf]), turn, kLimit)) {
             ok = false;
             break;
           }
@@ -303,7 +399,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
           const uint32_t d = tmem + buf * kN;
           const int end = min(blocks, done + chunk);
           for (int k = done; k < end; ++k) {
-            if (!mbar_wait_bounded(smem_u32(&sh.full[stage]), parity, kWaitCycles)) {
+            if (!mbar_wait_bounded(smem_u32(&sh.full[stage]), parity, kLimit)) {
               ok = false;
               break;
             }
@@ -327,6 +423,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
           done = end;
         } while (done < blocks);
       }
+      if (!feed.ok) sh.failed = 1;
       if (!ok) {  // let what has been issued end
         sh.failed = 1;
         tc_commit<kCtas>(smem_u32(&sh.drain));
@@ -345,7 +442,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     uint32_t buf = 0, turn = 0;
     bool ok = true;
     const auto wait = [&] {
-      ok = __all_sync(0xffffffffu, mbar_wait_bounded(smem_u32(&sh.acc_full[buf]), turn, kWaitCycles));
+      ok = __all_sync(0xffffffffu, mbar_wait_bounded(smem_u32(&sh.acc_full[buf]), turn, kLimit));
       tc_fence_after();
       return ok;
     };
@@ -362,7 +459,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         turn ^= 1;
       }
     };
-    for (int64_t i = first; i < n_tiles; i += step) {
+    for (int64_t i; (i = feed.template next<true>()) >= 0;) {
       int blocks, chunk;
       {
         Tile t;
@@ -383,7 +480,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       job.epilogue(i, cta, acc, v);
       __syncwarp();
     }
-    if (!ok) sh.failed = 1;
+    if (!ok || !feed.ok) sh.failed = 1;
     if (lane == 0) tma_store_wait_all();
   }
 

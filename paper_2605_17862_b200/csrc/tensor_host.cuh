@@ -55,10 +55,10 @@ inline int current_sms(int *sms) {
 }
 
 // Launches a job on up to one CTA (pair) per SM (pair); most_tiles: at least as many as the job will have.
-template <int kCtas, int kN, template <int, int> class Job>
-int launch_product(const typename Job<kCtas, kN>::Params &params, int64_t most_tiles, int sms, cudaStream_t st) {
+template <int kCtas, int kN, class Job>
+int launch_product(const typename Job::Params &params, int64_t most_tiles, int sms, cudaStream_t st) {
   using Shape = ProductShape<kCtas, kN>;
-  auto *kernel = product_kernel<kCtas, kN, Job<kCtas, kN>>;
+  auto *kernel = product_kernel<kCtas, kN, Job>;
   static std::atomic<bool> ready[kMaxDevices];
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return FOPD_ERR_CUDA;
