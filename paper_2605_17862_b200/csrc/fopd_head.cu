@@ -52,7 +52,8 @@ struct Temporary {
 // The rows of a call and where their hidden states are: the caller's, or with a mask a compacted copy.
 struct Prepared {
   HeadRows rows;
-  CUtensorMap hidden, weight;
+  CUtensorMap hidden, weight;                // boxes across
+  CUtensorMap hidden_along, weight_along;
 };
 struct RowParts {
   int64_t index = 0, active = 0, copy = 0;
@@ -84,11 +85,13 @@ int prepare_rows(const fopd_head *h, const RowParts &at, char *base, const float
     hidden = copy;
     pitch = round_up(h->dim, 8);
   }
-  int rc = make_map(&out->hidden, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, hidden, h->dim, rows, pitch * 2, 64, kBoxRows, true);
-  if (rc == FOPD_OK)
-    rc = make_map(&out->weight, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, h->weight, h->dim, h->vocab,
-                  (h->vocab > 1 ? h->weight_stride : round_up(h->dim, 8)) * 2, 64, kBoxRows, true);
-  return rc;
+  const int64_t weight_pitch = h->vocab > 1 ? h->weight_stride : round_up(h->dim, 8);
+  const auto maps = [&](CUtensorMap *across, CUtensorMap *along, const void *at, int64_t n, int64_t stride) {
+    const int rc = make_map(across, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, at, h->dim, n, stride * 2, 64, kBoxRows, true);
+    return rc != FOPD_OK ? rc : make_map(along, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, at, h->dim, n, stride * 2, 64, 2 * kBoxRows, true);
+  };
+  const int rc = maps(&out->hidden, &out->hidden_along, hidden, rows, pitch);
+  return rc != FOPD_OK ? rc : maps(&out->weight, &out->weight_along, h->weight, h->vocab, weight_pitch);
 }
 
 template <int kCtas, int kN>
@@ -104,8 +107,8 @@ int run_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *status,
   rc = prepare_rows(h, parts, tmp.base, nullptr, logprob, lse, status, st, &pre);
   if (rc == FOPD_OK) {
     typename LogprobJob<kCtas, kN>::Params p;
-    p.hidden = pre.hidden;
-    p.weight = pre.weight;
+    p.hidden = pre.hidden_along;
+    p.weight = pre.weight_along;
     p.l = {nullptr, nullptr, pre.rows, h->vocab, (int)((h->dim + 63) / 64), 0, (int)v_tiles};
     p.tokens = h->tokens;
     p.part = reinterpret_cast<float2 *>(tmp.base + part);
@@ -171,13 +174,17 @@ int run_grad(const fopd_head *h, const float *logprob, const float *lse, const f
     rc = make_map(&g.panels_out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, 32, true);
   if (rc == FOPD_OK)
     rc = make_map(&q.panels, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, kBoxRows, true);
+  if (rc == FOPD_OK)
+    rc = make_map(&q.panels_along, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, 2 * kBoxRows, true);
   if (rc == FOPD_OK && o.d_hidden && h->mask &&
       cudaMemset2DAsync(o.d_hidden, (size_t)(h->n_rows > 1 ? o.d_hidden_stride : round_up(h->dim, 8)) * 2, 0, (size_t)h->dim * 2,
                         (size_t)h->n_rows, st) != cudaSuccess)
     rc = FOPD_ERR_CUDA;
   if (rc == FOPD_OK) {
-    g.hidden = q.hidden = pre.hidden;
-    g.weight = q.weight = pre.weight;
+    g.hidden = pre.hidden_along;
+    g.weight = pre.weight_along;
+    q.hidden = pre.hidden;
+    q.weight = pre.weight;
     g.tokens = h->tokens;
     g.logprob = logprob;
     g.lse = lse;

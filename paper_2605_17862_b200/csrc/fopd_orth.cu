@@ -143,7 +143,7 @@ OrthMatrix describe(const fopd_matrix &m, const Scales &s, int32_t steps) {
 // The launches of one group.
 struct Group {
   OrthWorkspace ws;
-  CUtensorMap boxes, rows_out, mirror_out;
+  CUtensorMap boxes, boxes_along, rows_out;
   int norm_blocks, load_blocks;
   int64_t sym_tiles, x_tiles;
   bool pairs;  // tiles of 256 x 256 on pairs of CTAs
@@ -159,8 +159,8 @@ int run_table(const std::vector<OrthMatrix> &g, const Group &o, const Scales &s,
   if (launch_ok() != FOPD_OK) return FOPD_ERR_CUDA;
   const auto run = [&](auto p, auto launch) {
     p.boxes = o.boxes;
+    p.boxes_along = o.boxes_along;
     p.rows_out = o.rows_out;
-    p.mirror_out = o.mirror_out;
     p.ws = o.ws;
     std::copy(s.step, s.step + steps, p.step);
     p.tab = tab;
@@ -216,7 +216,7 @@ int run_group(std::vector<OrthMatrix> &g, const Scales &s, int32_t steps, float 
   o.pairs = tile == 256;
   rc = make_map(&o.boxes, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, o.ws.planes, 64, at, 128, 64, kBoxRows, true);
   if (rc == FOPD_OK) rc = make_map(&o.rows_out, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, o.ws.planes, 64, at, 128, 64, 32, true);
-  if (rc == FOPD_OK) rc = make_map(&o.mirror_out, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, o.ws.planes, 64, at, 128, 32, 64, false);
+  if (rc == FOPD_OK) rc = make_map(&o.boxes_along, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, o.ws.planes, 64, at, 128, 64, 2 * kBoxRows, true);
   if (rc == FOPD_OK) {
     const size_t n = g.size();
     rc = n <= 8    ? run_table<8>(g, o, s, steps, eps, status, sms, st)

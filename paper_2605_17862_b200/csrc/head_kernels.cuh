@@ -103,8 +103,8 @@ __device__ __forceinline__ void logit_tile(const LogitTiles &l, int n_rows, int6
   int row0;
   int64_t col0;
   logit_tile_at<kCtas, kN>(l, n_rows, i, row0, col0);
-  t.a = {l.hidden, 0, row0 + cta * 128, 64, 0, 0, 64, 0, false};
-  t.b = {l.weight, 0, (int)col0 + cta * (kN / kCtas), 64, 0, 0, 64, 0, false};
+  t.a = {l.hidden, 0, row0 + cta * 128, 64, 0, 0, 128, 0, false};
+  t.b = {l.weight, 0, (int)col0 + cta * (kN / kCtas), 64, 0, 0, 128, 0, false};
   t.k_blocks = l.k_blocks;
   t.chunk = kLogitChunk;
   t.passes = 1;
@@ -302,7 +302,7 @@ template <int kCtas, int kN>
 struct HeadGradsJob {
   static constexpr bool kFp16 = false, kClaimed = false;
   struct Params {
-    CUtensorMap hidden, weight, panels;
+    CUtensorMap hidden, weight, panels, panels_along;
     HeadRows rows;
     int64_t vocab, v0;   // first column of the piece
     int dim, v_count;    // columns of the piece
@@ -350,7 +350,7 @@ struct HeadGradsJob {
     d0 += cta * (kN / kCtas);
     if (split >= 0) {
       const int panels = (p.v_count + 63) / 64, first = split * p.split_panels;
-      t.a = {&p.panels, 0, first * p.pitch + row0, 0, p.pitch, 0, 64, 0, false};
+      t.a = {&p.panels_along, 0, first * p.pitch + row0, 0, p.pitch, 0, 128, 0, false};
       t.b = {&p.weight, d0, (int)p.v0 + first * 64, 0, 64, 64, 0, 0, true};
       t.k_blocks = max(0, min(p.split_panels, panels - first));
       t.chunk = 0;

@@ -219,7 +219,7 @@ struct OrthJob {
   static constexpr int kRows = kCtas * 128;
   static_assert(kN == kRows, "symmetric tiles");
   struct Params {
-    CUtensorMap boxes, rows_out, mirror_out;
+    CUtensorMap boxes, boxes_along, rows_out;
     OrthWorkspace ws;
     OrthStep step[kOrthMostSteps];
     OrthTable<N> tab;
@@ -287,7 +287,7 @@ struct OrthJob {
     const bool x_two = m.two_planes >> o.step & 1;
     const int x = m.x[o.step & 1];
     // along: rows of the operand are rows of the plane; across: they are its columns
-    const auto along = [&](int y, int pitch, int r, int lo) { return Operand{&p.boxes, 0, y + r, 0, pitch, 0, 64, lo, false}; };
+    const auto along = [&](int y, int pitch, int r, int lo) { return Operand{&p.boxes_along, 0, y + r, 0, pitch, 0, 128, lo, false}; };
     const auto across = [&](int y, int pitch, int r, int lo) { return Operand{&p.boxes, 0, y + r / 64 * pitch, 0, 64, 0, pitch, lo, true}; };
     t.a_lo = t.b_lo = 0;
     t.passes = 1;
@@ -329,16 +329,18 @@ struct OrthJob {
     });
     staging.send(acc, &p.rows_out, 0, y, at);
   }
-  // The same transposed: 64 rows of 32 elements.
+  // The same transposed, to row `y` and following from column x on: neighbouring lanes exchange so that each has two rows' values of
+  // one column, and a store fills 64 bytes of two rows.
   __device__ __forceinline__ void put_mirror(const Accumulator &acc, const float *v, int x, int y, bool lo) {
-    const uint32_t at = staging.next(acc);
+    const bool odd = acc.lane & 1;
+    uint32_t *to = reinterpret_cast<uint32_t *>(p.ws.planes + ((int64_t)y + odd) * 64 + x + (acc.lane & ~1));
 #pragma unroll
-    for (int j = 0; j < 64; ++j) {
-      __half h = __float2half_rn(v[j]);
-      if (lo) h = __float2half_rn(v[j] - __half2float(h));
-      asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + j * 64 + acc.lane * 2), "h"(__half_as_ushort(h)) : "memory");
+    for (int j = 0; j < 64; j += 2) {
+      __half2 h = __floats2half2_rn(v[j], v[j + 1]);
+      if (lo) h = __floats2half2_rn(v[j] - __low2float(h), v[j + 1] - __high2float(h));
+      const uint32_t mine = *reinterpret_cast<uint32_t *>(&h), other = __shfl_xor_sync(0xffffffffu, mine, 1);
+      to[j * 32] = odd ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
     }
-    staging.send(acc, &p.mirror_out, x, y, at);
   }
 
   __device__ __forceinline__ void epilogue(int64_t i, int cta, const Accumulator &acc, float (&v)[kN / 2]) {
@@ -347,6 +349,7 @@ struct OrthJob {
     const int row0 = o.row0 + cta * 128 + acc.warp * 32, col0 = o.col0 + acc.half * (kN / 2);
     if (o.phase == kOrthApply) put_x(o, m, row0, col0, acc, v);
     else put_square(o, m, row0, col0, acc, v);
+    __syncwarp();
     if (acc.lane == 0 && !(o.last && o.phase == kOrthApply)) {  // written, then counted
       tma_store_wait_all();
       __threadfence();

@@ -27,6 +27,12 @@
 
 namespace fopd {
 
+__device__ __forceinline__ bool elect_one() {  // the same lane each time
+  uint32_t yes;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
+  return yes != 0;
+}
+
 // ------------------------------------------------------------------ TMA
 template <int kCtas>
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
@@ -148,7 +154,7 @@ __device__ __forceinline__ void add_release(int *p, int v) {
 __device__ __forceinline__ void fence_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
 
 // ------------------------------------------------------------------ tiles
-constexpr int kBoxRows = 64;                    // rows of one TMA box of 64 16-bit elements
+constexpr int kBoxRows = 64;                    // rows of one TMA box of 64 16-bit elements, across; along twice as many
 constexpr int kBoxBytes = kBoxRows * 128;
 constexpr int kProductThreads = 384;
 constexpr int kEpilogueWarp0 = 4, kEpilogueWarps = 8;  // two to each quarter of the rows, half of the columns each
@@ -158,12 +164,13 @@ constexpr uint32_t kTmemCols = 512;
 // Registers: 384 threads x 168 at launch; 128 x 64 + 256 x 216 = 63,488 of those 64,512 afterwards.
 constexpr int kRoleRegs = 64, kEpilogueRegs = 216;
 
-// One operand of a tile: where its boxes are.
+// One operand of a tile: where its boxes are.  Where the contraction runs along the rows a box is 128 rows of 64 elements, where it
+// runs across them 64 rows: 64 of the contraction and 64 of the tile.
 struct Operand {
   const CUtensorMap *map;
   int x, y;    // the first box of this CTA's part
-  int kx, ky;  // from one block of 64 along the contraction to the next
-  int cx, cy;  // from one box to the next across it
+  int kx, ky;  // from one block of 64 of the contraction to the next
+  int cx, cy;  // from one box to the next
   int lo;      // rows from a plane of the values to the plane of what their rounding left (two-plane operands)
   bool across; // the contraction runs across the rows of the boxes
 };
@@ -234,45 +241,41 @@ struct TileFeed {
   uint32_t n = 0;
   bool ok = true;
   __device__ TileFeed(ProductShared &s, int c, int64_t tiles) : sh(s), cta(c), n_tiles(tiles), step(gridDim.x / kCtas), i((int64_t)(blockIdx.x / kCtas) - step) {}
-  // -1: no more, or a wait ran out (then ok is false)
-  __device__ __forceinline__ int64_t next_claimed(int *counter) {
+  // (by all lanes of a warp) -1: no more, or a wait ran out (then ok is false)
+  __device__ __forceinline__ int64_t next_claimed(int *counter, bool elected) {
     const uint32_t slot = n % kFeed;
-    if (!mbar_wait_cluster_bounded(smem_u32(&sh.feed_empty[slot]), ((n / kFeed) & 1) ^ 1, kLimit)) {
-      ok = false;
-      return -1;
-    }
+    ok = __all_sync(0xffffffffu, mbar_wait_cluster_bounded(smem_u32(&sh.feed_empty[slot]), ((n / kFeed) & 1) ^ 1, kLimit));
+    if (!ok) return -1;
     ++n;
-    int v = atomicAdd(counter, 1);
+    int v = 0;
+    if (elected) v = atomicAdd(counter, 1);
+    v = __reduce_add_sync(0xffffffffu, v);
     if (v >= n_tiles) v = -1;
-    if constexpr (kCtas == 1) {
-      sh.feed[slot] = v;
-      mbar_arrive(smem_u32(&sh.feed_full[slot]));
-    } else {
-      for (int r = 0; r < kCtas; ++r) {
-        const uint32_t bar = map_to_cta(smem_u32(&sh.feed_full[slot]), r);
-        mbar_expect_tx_cluster(bar, 4);
-        st_async_s32(map_to_cta(smem_u32(&sh.feed[slot]), r), v, bar);
+    if (elected) {
+      if constexpr (kCtas == 1) {
+        *reinterpret_cast<volatile int *>(&sh.feed[slot]) = v;
+        mbar_arrive(smem_u32(&sh.feed_full[slot]));
+      } else {
+        for (int r = 0; r < kCtas; ++r) {
+          const uint32_t bar = map_to_cta(smem_u32(&sh.feed_full[slot]), r);
+          mbar_expect_tx_cluster(bar, 4);
+          st_async_s32(map_to_cta(smem_u32(&sh.feed[slot]), r), v, bar);
+        }
       }
     }
     return v;
   }
-  template <bool kWarp>  // all lanes of a warp, or one thread
   __device__ __forceinline__ int64_t next() {
     if constexpr (!Job::kClaimed) {
       i += step;
       return i < n_tiles ? i : -1;
     } else {
       const uint32_t slot = n % kFeed;
-      bool here = mbar_wait_cluster_bounded(smem_u32(&sh.feed_full[slot]), (n / kFeed) & 1, kLimit);
-      if (kWarp) here = __all_sync(0xffffffffu, here);
-      if (!here) {
-        ok = false;
-        return -1;
-      }
+      ok = __all_sync(0xffffffffu, mbar_wait_cluster_bounded(smem_u32(&sh.feed_full[slot]), (n / kFeed) & 1, kLimit));
+      if (!ok) return -1;
       ++n;
-      const int v = *reinterpret_cast<volatile int *>(&sh.feed[slot]);
-      if (kWarp) __syncwarp();
-      if (!kWarp || (threadIdx.x & 31) == 0) {
+      const int v = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile int *>(&sh.feed[slot]), 0);
+      if ((threadIdx.x & 31) == 0) {
         const uint32_t bar = smem_u32(&sh.feed_empty[slot]);
         if constexpr (kCtas == 2) mbar_arrive_cluster(map_to_cta(bar, 0));
         else mbar_arrive(bar);
@@ -290,7 +293,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
   using Shape = ProductShape<kCtas, kN>;
   extern __shared__ uint8_t product_smem[];
   __shared__ ProductShared sh;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t base = (smem_u32(product_smem) + 1023u) & ~1023u;
   const uint32_t staging = base + Shape::kStages * Shape::kStageBytes;
   const int cta = kCtas == 2 ? (int)cluster_ctarank() : 0;
@@ -320,7 +323,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     cluster_wait();
   }
   tc_fence_after();
-  const uint32_t tmem = sh.tmem;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
 
   Job job(params);
   TileFeed<kCtas, Job> feed(sh, cta, job.tiles());
@@ -328,39 +331,46 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
 
   if (warp < kEpilogueWarp0) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRoleRegs));
-    if (warp == 0 && lane == 0) {
+    // (whole warps go through these loops and one thread of each issues: what is the same in all lanes stays in uniform registers)
+    const bool elected = elect_one();
+    const uint32_t full = smem_u32(&sh.full[0]), empty = smem_u32(&sh.empty[0]);
+    if (warp == 0) {
       // ---- copies in
-      int stage = 0, used = 0;
-      uint32_t parity = 1;
+      uint32_t stage = 0, used = 0, parity = 1;
       bool ok = true;
-      while (ok) {
+      const uint32_t signal = kCtas == 2 ? map_to_cta(full, 0) : full;
+      while (true) {
         int64_t i;
         if constexpr (Job::kClaimed) {
-          i = cta == 0 ? feed.next_claimed(job.counter()) : feed.template next<false>();
-          if (i >= 0 && !job.ready(i, kLimit)) ok = false;
+          if (cta == 0) i = feed.next_claimed(job.counter(), elected);
+          else i = feed.next();
+          if (i >= 0) ok = job.ready(i, kLimit);
         } else {
-          i = feed.template next<false>();
+          i = feed.next();
         }
+        ok = __all_sync(0xffffffffu, ok);
         if (i < 0 || !ok) break;
         Tile t;
         job.tile(i, cta, t);
+        const int a_boxes = t.a.across ? Shape::kABoxes : Shape::kABoxes / 2, b_boxes = t.b.across ? Shape::kBBoxes : Shape::kBBoxes / 2;
+        const uint32_t a_step = t.a.across ? kBoxBytes : 2 * kBoxBytes, b_step = t.b.across ? kBoxBytes : 2 * kBoxBytes;
         for (int pass = 0; ok && pass < t.passes; ++pass) {
-          const int ya = t.a.y + ((t.a_lo >> pass & 1) ? t.a.lo : 0), yb = t.b.y + ((t.b_lo >> pass & 1) ? t.b.lo : 0);
+          int xa = t.a.x, ya = t.a.y + ((t.a_lo >> pass & 1) ? t.a.lo : 0);
+          int xb = t.b.x, yb = t.b.y + ((t.b_lo >> pass & 1) ? t.b.lo : 0);
           for (int k = 0; k < t.k_blocks; ++k) {
-            if (!mbar_wait_bounded(smem_u32(&sh.empty[stage]), parity, kLimit)) {
+            if (!mbar_wait_bounded(empty + stage * 8, parity, kLimit)) {
               ok = false;
               break;
             }
-            uint32_t full = smem_u32(&sh.full[stage]);
-            if (cta == 0) mbar_expect_tx(full, kCtas * Shape::kStageBytes);
-            if constexpr (kCtas == 2) full = map_to_cta(full, 0);
-            uint32_t dst = base + stage * Shape::kStageBytes;
-#pragma unroll
-            for (int c = 0; c < Shape::kABoxes; ++c, dst += kBoxBytes)
-              tma_load<kCtas>(dst, t.a.map, t.a.x + k * t.a.kx + c * t.a.cx, ya + k * t.a.ky + c * t.a.cy, full);
-#pragma unroll
-            for (int c = 0; c < Shape::kBBoxes; ++c, dst += kBoxBytes)
-              tma_load<kCtas>(dst, t.b.map, t.b.x + k * t.b.kx + c * t.b.cx, yb + k * t.b.ky + c * t.b.cy, full);
+            if (elected) {
+              if (cta == 0) mbar_expect_tx(full + stage * 8, kCtas * Shape::kStageBytes);
+              const uint32_t dst = base + stage * Shape::kStageBytes;
+              for (int c = 0; c < a_boxes; ++c)
+                tma_load<kCtas>(dst + c * a_step, t.a.map, xa + c * t.a.cx, ya + c * t.a.cy, signal + stage * 8);
+              for (int c = 0; c < b_boxes; ++c)
+                tma_load<kCtas>(dst + Shape::kABoxes * kBoxBytes + c * b_step, t.b.map, xb + c * t.b.cx, yb + c * t.b.cy, signal + stage * 8);
+            }
+            xa += t.a.kx, ya += t.a.ky, xb += t.b.kx, yb += t.b.ky;
             if (used < Shape::kStages) ++used;
             if (++stage == Shape::kStages) {
               stage = 0;
@@ -368,30 +378,32 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             }
           }
         }
+        ok = __all_sync(0xffffffffu, ok);
       }
       // Before this CTA may end, the stages it filled have been read (their last arrivals are in): behind the copies.
-      for (int i = 0; i < used; ++i) {
+      for (uint32_t j = 0; j < used; ++j) {
         if (stage == 0) parity ^= 1;
         stage = stage == 0 ? Shape::kStages - 1 : stage - 1;
-        if (!mbar_wait_bounded(smem_u32(&sh.empty[stage]), parity ^ 1, kWaitCycles)) ok = false;
+        if (!mbar_wait_bounded(empty + stage * 8, parity ^ 1, kLimit)) ok = false;
       }
       if (!ok || !feed.ok) sh.failed = 1;
     }
-    if (warp == 1 && lane == 0 && cta == 0) {
+    if (warp == 1 && cta == 0) {
       // ---- products
-      int stage = 0;
-      uint32_t parity = 0, buf = 0, turn = 1;  // turn: parity of acc_empty
+      const uint32_t acc_full = smem_u32(&sh.acc_full[0]), acc_empty = smem_u32(&sh.acc_empty[0]);
+      uint32_t stage = 0, parity = 0, buf = 0, turn = 1;  // turn: parity of acc_empty
       bool ok = true;
-      for (int64_t i; ok && (i = feed.template next<false>()) >= 0;) {
+      for (int64_t i; ok && (i = feed.next()) >= 0;) {
         Tile t;
         job.tile(i, cta, t);
         const uint32_t idesc = (1u << 4) | (Job::kFp16 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)t.a.across << 15) |
                                ((uint32_t)t.b.across << 16) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(kCtas * 128 >> 4) << 24);
         const uint32_t a_step = (t.a.across ? 16 * 128 : 32) >> 4, b_step = (t.b.across ? 16 * 128 : 32) >> 4;
+        const uint64_t a0 = smem_descriptor(base, t.a.across), b0 = smem_descriptor(base + Shape::kABoxes * kBoxBytes, t.b.across);
         const int blocks = t.passes * t.k_blocks, chunk = t.chunk > 0 ? t.chunk : blocks;
         int done = 0;
         do {
-          if (!mbar_wait_bounded(smem_u32(&sh.acc_empty[buf]), turn, kLimit)) {
+          if (!mbar_wait_bounded(acc_empty + buf * 8, turn, kLimit)) {
             ok = false;
             break;
           }
@@ -399,34 +411,36 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
           const uint32_t d = tmem + buf * kN;
           const int end = min(blocks, done + chunk);
           for (int k = done; k < end; ++k) {
-            if (!mbar_wait_bounded(smem_u32(&sh.full[stage]), parity, kLimit)) {
+            if (!mbar_wait_bounded(full + stage * 8, parity, kLimit)) {
               ok = false;
               break;
             }
             tc_fence_after();
-            const uint32_t at = base + stage * Shape::kStageBytes;
-            const uint64_t a = smem_descriptor(at, t.a.across), b = smem_descriptor(at + Shape::kABoxes * kBoxBytes, t.b.across);
+            const uint64_t a = a0 + stage * (Shape::kStageBytes >> 4), b = b0 + stage * (Shape::kStageBytes >> 4);
+            if (elected) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) tc_mma<kCtas>(d, a + j * a_step, b + j * b_step, idesc, k > done || j > 0);
-            tc_commit<kCtas>(smem_u32(&sh.empty[stage]));
+              for (int j = 0; j < 4; ++j) tc_mma<kCtas>(d, a + j * a_step, b + j * b_step, idesc, k > done || j > 0);
+              tc_commit<kCtas>(empty + stage * 8);
+            }
             if (++stage == Shape::kStages) {
               stage = 0;
               parity ^= 1;
             }
           }
           if (!ok) break;
-          tc_commit<kCtas>(smem_u32(&sh.acc_full[buf]));
+          if (elected) tc_commit<kCtas>(acc_full + buf * 8);
           if (++buf == Shape::kAccs) {
             buf = 0;
             turn ^= 1;
           }
           done = end;
         } while (done < blocks);
+        ok = __all_sync(0xffffffffu, ok);
       }
       if (!feed.ok) sh.failed = 1;
       if (!ok) {  // let what has been issued end
         sh.failed = 1;
-        tc_commit<kCtas>(smem_u32(&sh.drain));
+        if (elected) tc_commit<kCtas>(smem_u32(&sh.drain));
         mbar_wait_bounded(smem_u32(&sh.drain), 0, kWaitCycles);
       }
     }
@@ -459,7 +473,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         turn ^= 1;
       }
     };
-    for (int64_t i; (i = feed.template next<true>()) >= 0;) {
+    for (int64_t i; (i = feed.next()) >= 0;) {
       int blocks, chunk;
       {
         Tile t;
