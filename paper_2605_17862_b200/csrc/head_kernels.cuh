@@ -116,7 +116,8 @@ __device__ __forceinline__ void logit_tile(const LogitTiles &l, int n_rows, int6
 // stored token's left out of the sum: the log-prob of a nearly certain token comes from the others' sum.
 template <int kCtas, int kN>
 struct LogprobJob {
-  static constexpr bool kFp16 = false, kClaimed = false;
+  static constexpr bool kFp16 = false, kTurns = false, kClaimed = false;
+  using Ticket = TileNumber;
   struct Params {
     CUtensorMap hidden, weight;
     LogitTiles l;
@@ -135,12 +136,12 @@ struct LogprobJob {
   }
   __device__ int64_t tiles() const { return logit_tiles<kCtas, kN>(l, n); }
   __device__ int32_t *status() const { return p.status; }
-  __device__ __forceinline__ void tile(int64_t i, int cta, Tile &t) const { logit_tile<kCtas, kN>(l, n, i, cta, t); }
-  __device__ __forceinline__ void epilogue(int64_t i, int cta, const Accumulator &acc, float (&z)[kN / 2]) const {
+  __device__ __forceinline__ void tile(Ticket ticket, int cta, Tile &t) const { logit_tile<kCtas, kN>(l, n, ticket.i, cta, t); }
+  __device__ __forceinline__ void epilogue(Ticket ticket, int cta, const Accumulator &acc, float (&z)[kN / 2]) const {
     constexpr int kCols = kN / 2;
     int row0;
     int64_t v0;
-    logit_tile_at<kCtas, kN>(l, n, i, row0, v0);
+    logit_tile_at<kCtas, kN>(l, n, ticket.i, row0, v0);
     v0 += acc.half * kCols;
     const int row = row0 + cta * 128 + acc.warp * 32 + acc.lane;
     const int y = row < n ? p.tokens[l.rows.row(row)] : -1;
@@ -219,7 +220,8 @@ __global__ void __launch_bounds__(1024) head_join_kernel(HeadRows rows, const fl
 // bf16 results' own.
 template <int kCtas, int kN>
 struct GradLogitsJob {
-  static constexpr bool kFp16 = false, kClaimed = false;
+  static constexpr bool kFp16 = false, kTurns = false, kClaimed = false;
+  using Ticket = TileNumber;
   struct Params {
     CUtensorMap hidden, weight, panels_out;
     LogitTiles l;
@@ -239,12 +241,12 @@ struct GradLogitsJob {
   }
   __device__ int64_t tiles() const { return logit_tiles<kCtas, kN>(l, n); }
   __device__ int32_t *status() const { return p.status; }
-  __device__ __forceinline__ void tile(int64_t i, int cta, Tile &t) const { logit_tile<kCtas, kN>(l, n, i, cta, t); }
-  __device__ __forceinline__ void epilogue(int64_t i, int cta, const Accumulator &acc, float (&g)[kN / 2]) {
+  __device__ __forceinline__ void tile(Ticket ticket, int cta, Tile &t) const { logit_tile<kCtas, kN>(l, n, ticket.i, cta, t); }
+  __device__ __forceinline__ void epilogue(Ticket ticket, int cta, const Accumulator &acc, float (&g)[kN / 2]) {
     constexpr int kCols = kN / 2;
     int row0;
     int64_t v0;
-    logit_tile_at<kCtas, kN>(l, n, i, row0, v0);
+    logit_tile_at<kCtas, kN>(l, n, ticket.i, row0, v0);
     v0 += acc.half * kCols;
     row0 += cta * 128 + acc.warp * 32;
     const int row = row0 + acc.lane;
@@ -300,7 +302,8 @@ struct GradLogitsJob {
 // (in the workspace, in a fixed order); d_weight's run along the rows and are finished.
 template <int kCtas, int kN>
 struct HeadGradsJob {
-  static constexpr bool kFp16 = false, kClaimed = false;
+  static constexpr bool kFp16 = false, kTurns = false, kClaimed = false;
+  using Ticket = TileNumber;
   struct Params {
     CUtensorMap hidden, weight, panels, panels_along;
     HeadRows rows;
@@ -343,9 +346,9 @@ struct HeadGradsJob {
       d0 = (int)(i % d_tiles) * kN;
     }
   }
-  __device__ __forceinline__ void tile(int64_t i, int cta, Tile &t) const {
+  __device__ __forceinline__ void tile(Ticket ticket, int cta, Tile &t) const {
     int split, row0, d0;
-    at(i, split, row0, d0);
+    at(ticket.i, split, row0, d0);
     row0 += cta * 128;
     d0 += cta * (kN / kCtas);
     if (split >= 0) {
@@ -366,9 +369,9 @@ struct HeadGradsJob {
     }
     t.b_lo = 0;
   }
-  __device__ __forceinline__ void epilogue(int64_t i, int cta, const Accumulator &acc, float (&g)[kN / 2]) const {
+  __device__ __forceinline__ void epilogue(Ticket ticket, int cta, const Accumulator &acc, float (&g)[kN / 2]) const {
     int split, row0, d0;
-    at(i, split, row0, d0);
+    at(ticket.i, split, row0, d0);
     d0 += acc.half * (kN / 2);
     const int row = row0 + cta * 128 + acc.warp * 32 + acc.lane;
     if (split >= 0) {

@@ -13,8 +13,8 @@
 // The scales follow from a bound on the largest singular value in each step, which the host takes from the coefficients.
 //
 // Everything lies in one workspace in panels of 64 columns ([panel][rows][64], rows and columns padded with zeros to 64), so that one
-// tensor map serves every operand, along its rows or across them, and tiles need no edges.  A and A^2 are symmetric: the
-// tiles on and below the diagonal are computed and stored twice.
+// tensor map serves every operand, along its rows or across them, and tiles need no edges.  A and A^2 are symmetric: only the
+// tiles on and below the diagonal are computed and stored, and what lies above is read across out of those below.
 #pragma once
 
 #include "tensor_core.cuh"
@@ -215,7 +215,7 @@ struct OrthStep {
 
 template <int kCtas, int kN, int N>
 struct OrthJob {
-  static constexpr bool kFp16 = true, kClaimed = true;
+  static constexpr bool kFp16 = true, kTurns = true, kClaimed = true;
   static constexpr int kRows = kCtas * 128;
   static_assert(kN == kRows, "symmetric tiles");
   struct Params {
@@ -227,9 +227,15 @@ struct OrthJob {
     int sym_tiles, x_tiles;  // of the list, in each step
     int32_t *status;
   };
-  struct Place {
-    int k, step, phase, row0, col0;
-    bool last;
+  struct Ticket {
+    int i;
+    int k;              // matrix
+    int step_phase;     // 4 step + phase
+    uint32_t row_col;   // tile row << 16 | tile column (2^24 rows in tiles of 256)
+    __device__ __forceinline__ int step() const { return step_phase >> 2; }
+    __device__ __forceinline__ int phase() const { return step_phase & 3; }
+    __device__ __forceinline__ int row0() const { return (int)(row_col >> 16) * kRows; }
+    __device__ __forceinline__ int col0() const { return (int)(row_col & 0xffff) * kN; }
   };
   const Params &p;
   Staging staging;
@@ -237,39 +243,37 @@ struct OrthJob {
   __device__ int64_t tiles() const { return (int64_t)p.steps * (2 * p.sym_tiles + p.x_tiles); }
   __device__ int32_t *status() const { return p.status; }
   __device__ int *counter() const { return p.ws.done + p.tab.n; }
-  __device__ __forceinline__ Place place(int64_t i) const {
-    Place o;
-    const int per = 2 * p.sym_tiles + p.x_tiles;
-    o.step = (int)(i / per);
-    o.last = o.step + 1 == p.steps;
-    int t = (int)(i - (int64_t)o.step * per);
-    o.phase = t < p.sym_tiles ? kOrthGram : t < 2 * p.sym_tiles ? kOrthPoly : kOrthApply;
-    t -= o.phase * p.sym_tiles;
+  __device__ __forceinline__ bool last(const Ticket &o) const { return o.step() + 1 == p.steps; }
+  __device__ __forceinline__ Ticket ticket(int i) const {
+    Ticket o;
+    o.i = i;
+    const int per = 2 * p.sym_tiles + p.x_tiles, step = i / per;
+    int t = i - step * per;
+    const int phase = t < p.sym_tiles ? kOrthGram : t < 2 * p.sym_tiles ? kOrthPoly : kOrthApply;
+    t -= phase * p.sym_tiles;
+    o.step_phase = 4 * step + phase;
     const OrthMatrix *tab = p.tab.m;
-    if (o.phase == kOrthApply) {
+    if (phase == kOrthApply) {
       o.k = find_entry(p.tab.n, t, [&](int j) { return tab[j].x_tile; });
       t -= tab[o.k].x_tile;
       const int across = (tab[o.k].cp + kN - 1) / kN;
-      o.row0 = t / across * kRows;
-      o.col0 = t % across * kN;
+      o.row_col = (uint32_t)(t / across) << 16 | (uint32_t)(t % across);
     } else {
       o.k = find_entry(p.tab.n, t, [&](int j) { return tab[j].sym_tile; });
       t -= tab[o.k].sym_tile;
       int r = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
       while (r * (r + 1) / 2 > t) --r;
       while ((r + 1) * (r + 2) / 2 <= t) ++r;
-      o.row0 = r * kRows;
-      o.col0 = (t - r * (r + 1) / 2) * kN;
+      o.row_col = (uint32_t)r << 16 | (uint32_t)(t - r * (r + 1) / 2);
     }
     return o;
   }
   // Units of a matrix's tiles before this phase.
-  __device__ __forceinline__ int units_before(const Place &o, const OrthMatrix &m) const {
+  __device__ __forceinline__ int units_before(const Ticket &o, const OrthMatrix &m) const {
     const int s = (m.mp + kN - 1) / kN, sym = s * (s + 1) / 2, x = ((m.rp + kRows - 1) / kRows) * ((m.cp + kN - 1) / kN);
-    return kCtas * kEpilogueWarps * (o.step * (2 * sym + x) + o.phase * sym);
+    return kCtas * kEpilogueWarps * (o.step() * (2 * sym + x) + o.phase() * sym);
   }
-  __device__ __forceinline__ bool ready(int64_t i, long long limit) const {
-    const Place o = place(i);
+  __device__ __forceinline__ bool ready(const Ticket &o, long long limit) const {
     const int want = units_before(o, p.tab.m[o.k]);
     const int *done = p.ws.done + o.k;
     if (load_acquire(done) < want) {
@@ -280,26 +284,31 @@ struct OrthJob {
     fence_async_global();  // (the copies that follow are of another proxy than the load)
     return true;
   }
-  __device__ __forceinline__ void tile(int64_t i, int cta, Tile &t) const {
-    const Place o = place(i);
+  __device__ __forceinline__ void tile(const Ticket &o, int cta, Tile &t) const {
     const OrthMatrix &m = p.tab.m[o.k];
-    const int row0 = o.row0 + cta * 128, col0 = o.col0 + cta * (kN / kCtas);
-    const bool x_two = m.two_planes >> o.step & 1;
-    const int x = m.x[o.step & 1];
+    const int row0 = o.row0() + cta * 128, col0 = o.col0() + cta * (kN / kCtas);
+    const bool x_two = m.two_planes >> o.step() & 1;
+    const int x = m.x[o.step() & 1];
     // along: rows of the operand are rows of the plane; across: they are its columns
     const auto along = [&](int y, int pitch, int r, int lo) { return Operand{&p.boxes_along, 0, y + r, 0, pitch, 0, 128, lo, false}; };
     const auto across = [&](int y, int pitch, int r, int lo) { return Operand{&p.boxes, 0, y + r / 64 * pitch, 0, 64, 0, pitch, lo, true}; };
+    // a symmetric operand: rows `r` of the tile that starts at `first`
+    const auto symmetric = [&](int y, int r, int first, Operand &op, Turn &turn) {
+      op = along(y, m.mp, r, m.m_lo);
+      turn = {(first + kN) / 64, &p.boxes, y + r / 64 * m.mp, m.mp};
+    };
+    t.a_turn = t.b_turn = {1 << 30, &p.boxes, 0, 0};
     t.a_lo = t.b_lo = 0;
     t.passes = 1;
     t.chunk = m.full ? kOrthChunk : 0;
-    if (o.phase == kOrthGram) {
+    if (o.phase() == kOrthGram) {
       t.a = m.tall ? across(x, m.rp, row0, m.x_lo) : along(x, m.rp, row0, m.x_lo);
       t.b = m.tall ? across(x, m.rp, col0, m.x_lo) : along(x, m.rp, col0, m.x_lo);
       t.k_blocks = (m.tall ? m.rp : m.cp) / 64;
       if (m.full && x_two) t.passes = 3, t.b_lo = 1, t.a_lo = 2;
-    } else if (o.phase == kOrthPoly) {
-      t.a = along(m.a, m.mp, row0, m.m_lo);
-      t.b = along(m.a, m.mp, col0, m.m_lo);
+    } else if (o.phase() == kOrthPoly) {
+      symmetric(m.a, row0, o.row0(), t.a, t.a_turn);
+      symmetric(m.a, col0, o.col0(), t.b, t.b_turn);
       t.k_blocks = m.mp / 64;
       if (m.full) t.passes = 3, t.b_lo = 1, t.a_lo = 2;
     } else {
@@ -309,10 +318,10 @@ struct OrthJob {
       if (x_two) x_lo = 1u << (t.passes++ - 1);
       if (m.tall) {
         t.a = along(x, m.rp, row0, m.x_lo);
-        t.b = along(m.p, m.mp, col0, m.m_lo);
+        symmetric(m.p, col0, o.col0(), t.b, t.b_turn);
         t.a_lo = x_lo, t.b_lo = p_lo;
       } else {
-        t.a = along(m.p, m.mp, row0, m.m_lo);
+        symmetric(m.p, row0, o.row0(), t.a, t.a_turn);
         t.b = across(x, m.rp, col0, m.x_lo);
         t.a_lo = p_lo, t.b_lo = x_lo;
       }
@@ -329,40 +338,23 @@ struct OrthJob {
     });
     staging.send(acc, &p.rows_out, 0, y, at);
   }
-  // The same transposed, to row `y` and following from column x on: neighbouring lanes exchange so that each has two rows' values of
-  // one column, and a store fills 64 bytes of two rows.
-  __device__ __forceinline__ void put_mirror(const Accumulator &acc, const float *v, int x, int y, bool lo) {
-    const bool odd = acc.lane & 1;
-    uint32_t *to = reinterpret_cast<uint32_t *>(p.ws.planes + ((int64_t)y + odd) * 64 + x + (acc.lane & ~1));
-#pragma unroll
-    for (int j = 0; j < 64; j += 2) {
-      __half2 h = __floats2half2_rn(v[j], v[j + 1]);
-      if (lo) h = __floats2half2_rn(v[j] - __low2float(h), v[j + 1] - __high2float(h));
-      const uint32_t mine = *reinterpret_cast<uint32_t *>(&h), other = __shfl_xor_sync(0xffffffffu, mine, 1);
-      to[j * 32] = odd ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
-    }
-  }
-
-  __device__ __forceinline__ void epilogue(int64_t i, int cta, const Accumulator &acc, float (&v)[kN / 2]) {
-    const Place o = place(i);
+  __device__ __forceinline__ void epilogue(const Ticket &o, int cta, const Accumulator &acc, float (&v)[kN / 2]) {
     const OrthMatrix &m = p.tab.m[o.k];
-    const int row0 = o.row0 + cta * 128 + acc.warp * 32, col0 = o.col0 + acc.half * (kN / 2);
-    if (o.phase == kOrthApply) put_x(o, m, row0, col0, acc, v);
+    const int row0 = o.row0() + cta * 128 + acc.warp * 32, col0 = o.col0() + acc.half * (kN / 2);
+    if (o.phase() == kOrthApply) put_x(o, m, row0, col0, acc, v);
     else put_square(o, m, row0, col0, acc, v);
-    __syncwarp();
-    if (acc.lane == 0 && !(o.last && o.phase == kOrthApply)) {  // written, then counted
+    if (acc.lane == 0 && !(last(o) && o.phase() == kOrthApply)) {  // written, then counted
       tma_store_wait_all();
-      __threadfence();
       add_release(p.ws.done + o.k, 1);
     }
   }
-  __device__ __forceinline__ void put_x(const Place &o, const OrthMatrix &m, int row0, int col0, const Accumulator &acc, float (&v)[kN / 2]) {
+  __device__ __forceinline__ void put_x(const Ticket &o, const OrthMatrix &m, int row0, int col0, const Accumulator &acc, float (&v)[kN / 2]) {
     constexpr int kCols = kN / 2;
     if (row0 >= m.rp || col0 >= m.cp) return;
-    const float f = (o.step == 0 ? p.ws.norm_factor[o.k] : 1.f) * p.step[o.step].apply * (o.last ? m.scale : 1.f);
+    const float f = (o.step() == 0 ? p.ws.norm_factor[o.k] : 1.f) * p.step[o.step()].apply * (last(o) ? m.scale : 1.f);
 #pragma unroll
     for (int j = 0; j < kCols; ++j) v[j] *= f;
-    if (o.last) {
+    if (last(o)) {
       const int row = row0 + acc.lane;
       if (row >= m.rows) return;
       const int64_t at = row * m.out_pitch + col0;
@@ -371,8 +363,8 @@ struct OrthJob {
       else store_row<FOPD_BF16, kCols>(out + at * 2, v, col0, m.cols, false);
       return;
     }
-    const int x = m.x[(o.step + 1) & 1];
-    const bool two = m.two_planes >> (o.step + 1) & 1;
+    const int x = m.x[(o.step() + 1) & 1];
+    const bool two = m.two_planes >> (o.step() + 1) & 1;
 #pragma unroll
     for (int c = 0; c < kCols; c += 64) {
       if (col0 + c >= m.cp) continue;
@@ -381,16 +373,15 @@ struct OrthJob {
       if (two) put_rows(acc, v + c, y + m.x_lo, true);
     }
   }
-  __device__ __forceinline__ void put_square(const Place &o, const OrthMatrix &m, int row0, int col0, const Accumulator &acc,
+  __device__ __forceinline__ void put_square(const Ticket &o, const OrthMatrix &m, int row0, int col0, const Accumulator &acc,
                                              float (&v)[kN / 2]) {
     constexpr int kCols = kN / 2;
     if (row0 >= m.mp || col0 >= m.mp) return;
-    const bool below = o.row0 != o.col0;
-    const OrthStep &step = p.step[o.step];
-    const int to = o.phase == kOrthGram ? m.a : m.p;
+    const OrthStep &step = p.step[o.step()];
+    const int to = o.phase() == kOrthGram ? m.a : m.p;
     float f = step.poly_c;
-    if (o.phase == kOrthGram) {
-      const float s = o.step == 0 ? p.ws.norm_factor[o.k] : 1.f;
+    if (o.phase() == kOrthGram) {
+      const float s = o.step() == 0 ? p.ws.norm_factor[o.k] : 1.f;
       f = step.gram * s * s;
     } else {
       // (A was stored by other SMs: this warp reads it itself, so it looks at the count itself)
@@ -403,7 +394,7 @@ struct OrthJob {
 #pragma unroll
       for (int j = 0; j < 64; ++j) v[c + j] *= f;
       const int panel_row = (col0 + c) / 64 * m.mp + row0;
-      if (o.phase == kOrthPoly) {
+      if (o.phase() == kOrthPoly) {
         for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) {
           const uint4 *q = reinterpret_cast<const uint4 *>(p.ws.planes + ((int64_t)m.a + plane * m.m_lo + panel_row + acc.lane) * 64);
 #pragma unroll
@@ -424,10 +415,7 @@ struct OrthJob {
           for (int j = 0; j < 64; ++j) v[c + j] += j == d ? step.poly_a : 0.f;
         }
       }
-      for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) {
-        put_rows(acc, v + c, to + plane * m.m_lo + panel_row, plane);
-        if (below) put_mirror(acc, v + c, row0 & 63, to + plane * m.m_lo + row0 / 64 * m.mp + col0 + c, plane);
-      }
+      for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) put_rows(acc, v + c, to + plane * m.m_lo + panel_row, plane);
     }
   }
 };

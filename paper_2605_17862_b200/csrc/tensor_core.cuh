@@ -138,9 +138,9 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
 __device__ __forceinline__ void mbar_expect_tx_cluster(uint32_t cluster_bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(cluster_bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void st_async_s32(uint32_t cluster_addr, int v, uint32_t cluster_bar) {
-  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.s32 [%0], %1, [%2];" ::"r"(cluster_addr), "r"(v),
-               "r"(cluster_bar)
+__device__ __forceinline__ void st_async_v4(uint32_t cluster_addr, int4 v, uint32_t cluster_bar) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.s32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(cluster_addr),
+               "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "r"(cluster_bar)
                : "memory");
 }
 __device__ __forceinline__ int load_acquire(const int *p) {
@@ -174,19 +174,28 @@ struct Operand {
   int lo;      // rows from a plane of the values to the plane of what their rounding left (two-plane operands)
   bool across; // the contraction runs across the rows of the boxes
 };
+// A symmetric operand of which only the tiles on and below the diagonal are stored: from block `turn` of the contraction on it is
+// read across, out of the tiles below.
+struct Turn {
+  int at;      // past the last block: never
+  const CUtensorMap *map;
+  int y, cy;   // as in Operand, with x = kx = cx = 0 and ky = 64; y for block 0
+};
 
 // The contraction may run over several pairs of planes: pass i takes a's second plane where bit i of a_lo is set, etc.
 struct Tile {
   Operand a, b;
+  Turn a_turn, b_turn;  // where the job has symmetric operands
   int k_blocks;  // 0: the product is zero
   int chunk;     // blocks (of all passes) to an accumulator, 0: all
   int passes;
   uint32_t a_lo, b_lo;
 };
 
-__device__ __forceinline__ uint64_t smem_descriptor(uint32_t addr, bool across) {
-  // 128-byte swizzle: groups of 8 rows of 128 bytes, 1,024 bytes apart; across: 64 rows further is the next box
-  const uint64_t lbo = across ? kBoxBytes >> 4 : 1, sbo = 1024 >> 4;
+__device__ __forceinline__ uint64_t smem_descriptor(uint32_t addr) {
+  // 128-byte swizzle: groups of 8 rows of 128 bytes, 1,024 bytes apart; across: 64 rows further is the next box (along, this is not
+  // looked at)
+  const uint64_t lbo = kBoxBytes >> 4, sbo = 1024 >> 4;
   return (uint64_t)((addr & 0x3ffff) >> 4) | (lbo << 16) | (sbo << 32) | (1ull << 46) | (2ull << 61);
 }
 
@@ -203,7 +212,7 @@ struct ProductShape {
 constexpr int kFeed = 4;  // tiles a CTA (pair) has claimed and some role has not yet taken note of
 struct ProductShared {
   unsigned long long full[8], empty[8], acc_full[4], acc_empty[4], drain, feed_full[kFeed], feed_empty[kFeed];
-  int feed[kFeed];
+  int4 feed[kFeed];
   uint32_t tmem;
   int failed;
 };
@@ -226,10 +235,22 @@ __device__ __forceinline__ void take_columns(float (&v)[kCols], uint32_t addr, b
   }
 }
 
+template <int kCtas, int kBoxes>
+__device__ __forceinline__ void load_operand(const Operand &o, uint32_t at, uint32_t bar) {
+  if (o.across) {
+#pragma unroll
+    for (int c = 0; c < kBoxes; ++c) tma_load<kCtas>(at + c * kBoxBytes, o.map, o.x + c * o.cx, o.y + c * o.cy, bar);
+  } else {
+#pragma unroll
+    for (int c = 0; c < kBoxes / 2; ++c) tma_load<kCtas>(at + 2 * c * kBoxBytes, o.map, o.x + c * o.cx, o.y + c * o.cy, bar);
+  }
+}
+
 // Which tiles a CTA (pair) works on, as each role sees them.  Either every step-th one, or, where tiles wait for others (kClaimed),
 // the next that no one has: the thread that brings the first CTA's operands in takes it from a counter when it has nothing
 // left to ask for, and passes it on through shared memory.  Tiles are claimed in an order in which each comes behind those it waits for,
 // and a claimed tile is worked on: whatever part of the grid is resident, the lowest unfinished tile can always go on.
+// What the roles get is a ticket (16 bytes, `i` first: the tile, negative where there is no more).
 constexpr long long kLongWaitCycles = 2000000000;  // (~1 s: behind a claimed tile's wait for others)
 template <int kCtas, class Job>
 struct TileFeed {
@@ -240,54 +261,76 @@ struct TileFeed {
   int64_t i;
   uint32_t n = 0;
   bool ok = true;
+  using Ticket = typename Job::Ticket;
   __device__ TileFeed(ProductShared &s, int c, int64_t tiles) : sh(s), cta(c), n_tiles(tiles), step(gridDim.x / kCtas), i((int64_t)(blockIdx.x / kCtas) - step) {}
   // (by all lanes of a warp) -1: no more, or a wait ran out (then ok is false)
-  __device__ __forceinline__ int64_t next_claimed(int *counter, bool elected) {
+  __device__ __forceinline__ Ticket next_claimed(const Job &job, bool elected) {
     const uint32_t slot = n % kFeed;
     ok = __all_sync(0xffffffffu, mbar_wait_cluster_bounded(smem_u32(&sh.feed_empty[slot]), ((n / kFeed) & 1) ^ 1, kLimit));
-    if (!ok) return -1;
+    Ticket ticket = {};
+    ticket.i = -1;
+    if (!ok) return ticket;
     ++n;
     int v = 0;
-    if (elected) v = atomicAdd(counter, 1);
+    if (elected) v = atomicAdd(job.counter(), 1);
     v = __reduce_add_sync(0xffffffffu, v);
-    if (v >= n_tiles) v = -1;
+    if (v < n_tiles) ticket = job.ticket(v);
+    static_assert(sizeof(Ticket) == 16, "goes through shared memory as one vector");
     if (elected) {
+      const int4 bits = *reinterpret_cast<const int4 *>(&ticket);
       if constexpr (kCtas == 1) {
-        *reinterpret_cast<volatile int *>(&sh.feed[slot]) = v;
+        asm volatile("st.shared.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(smem_u32(&sh.feed[slot])), "r"(bits.x), "r"(bits.y), "r"(bits.z), "r"(bits.w)
+                     : "memory");
         mbar_arrive(smem_u32(&sh.feed_full[slot]));
       } else {
         for (int r = 0; r < kCtas; ++r) {
           const uint32_t bar = map_to_cta(smem_u32(&sh.feed_full[slot]), r);
-          mbar_expect_tx_cluster(bar, 4);
-          st_async_s32(map_to_cta(smem_u32(&sh.feed[slot]), r), v, bar);
+          mbar_expect_tx_cluster(bar, 16);
+          st_async_v4(map_to_cta(smem_u32(&sh.feed[slot]), r), bits, bar);
         }
       }
     }
-    return v;
+    return ticket;
   }
-  __device__ __forceinline__ int64_t next() {
+  __device__ __forceinline__ Ticket next() {
+    Ticket ticket = {};
     if constexpr (!Job::kClaimed) {
       i += step;
-      return i < n_tiles ? i : -1;
+      ticket.i = i < n_tiles ? i : -1;
+      return ticket;
     } else {
+      ticket.i = -1;
       const uint32_t slot = n % kFeed;
       ok = __all_sync(0xffffffffu, mbar_wait_cluster_bounded(smem_u32(&sh.feed_full[slot]), (n / kFeed) & 1, kLimit));
-      if (!ok) return -1;
+      if (!ok) return ticket;
       ++n;
-      const int v = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile int *>(&sh.feed[slot]), 0);
+      int4 bits;
+      asm volatile("ld.shared.v4.s32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(bits.x), "=r"(bits.y), "=r"(bits.z), "=r"(bits.w)
+                   : "r"(smem_u32(&sh.feed[slot]))
+                   : "memory");
+      bits.x = __shfl_sync(0xffffffffu, bits.x, 0);  // (the same in all lanes, and known to be)
+      bits.y = __shfl_sync(0xffffffffu, bits.y, 0);
+      bits.z = __shfl_sync(0xffffffffu, bits.z, 0);
+      bits.w = __shfl_sync(0xffffffffu, bits.w, 0);
+      ticket = *reinterpret_cast<const Ticket *>(&bits);
       if ((threadIdx.x & 31) == 0) {
         const uint32_t bar = smem_u32(&sh.feed_empty[slot]);
         if constexpr (kCtas == 2) mbar_arrive_cluster(map_to_cta(bar, 0));
         else mbar_arrive(bar);
       }
-      return v;
+      return ticket;
     }
   }
 };
 
-// Job: Params (a kernel parameter); Job(params); int64_t tiles(); void tile(int64_t i, int cta, Tile &);
-// void epilogue(int64_t i, int cta, const Accumulator &, float (&v)[kN / 2]); int32_t *status(); static constexpr bool kFp16,
-// kClaimed; and where that is true int *counter() and bool ready(int64_t i, long long limit), which returns when what tile i reads is there.
+// Job: Params (a kernel parameter); Job(params); Ticket; int64_t tiles(); void tile(ticket, int cta, Tile &);
+// void epilogue(ticket, int cta, const Accumulator &, float (&v)[kN / 2]); int32_t *status(); static constexpr bool kFp16, kTurns (it has
+// symmetric operands), kClaimed; and where that is true int *counter(), Ticket ticket(i) and bool ready(ticket, limit), which returns
+// when what the tile reads is there.
+struct TileNumber {
+  int64_t i;
+};
 template <int kCtas, int kN, class Job>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ typename Job::Params params) {
   using Shape = ProductShape<kCtas, kN>;
@@ -340,37 +383,38 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       bool ok = true;
       const uint32_t signal = kCtas == 2 ? map_to_cta(full, 0) : full;
       while (true) {
-        int64_t i;
+        typename Job::Ticket ticket;
         if constexpr (Job::kClaimed) {
-          if (cta == 0) i = feed.next_claimed(job.counter(), elected);
-          else i = feed.next();
-          if (i >= 0) ok = job.ready(i, kLimit);
+          if (cta == 0) ticket = feed.next_claimed(job, elected);
+          else ticket = feed.next();
+          if (ticket.i >= 0) ok = job.ready(ticket, kLimit);
         } else {
-          i = feed.next();
+          ticket = feed.next();
         }
         ok = __all_sync(0xffffffffu, ok);
-        if (i < 0 || !ok) break;
+        if (ticket.i < 0 || !ok) break;
         Tile t;
-        job.tile(i, cta, t);
-        const int a_boxes = t.a.across ? Shape::kABoxes : Shape::kABoxes / 2, b_boxes = t.b.across ? Shape::kBBoxes : Shape::kBBoxes / 2;
-        const uint32_t a_step = t.a.across ? kBoxBytes : 2 * kBoxBytes, b_step = t.b.across ? kBoxBytes : 2 * kBoxBytes;
+        job.tile(ticket, cta, t);
         for (int pass = 0; ok && pass < t.passes; ++pass) {
-          int xa = t.a.x, ya = t.a.y + ((t.a_lo >> pass & 1) ? t.a.lo : 0);
-          int xb = t.b.x, yb = t.b.y + ((t.b_lo >> pass & 1) ? t.b.lo : 0);
+          Operand a = t.a, b = t.b;
+          if (t.a_lo >> pass & 1) a.y += a.lo;
+          if (t.b_lo >> pass & 1) b.y += b.lo;
           for (int k = 0; k < t.k_blocks; ++k) {
+            if constexpr (Job::kTurns) {
+              if (k == t.a_turn.at) a = {t.a_turn.map, 0, t.a_turn.y + k * 64 + ((t.a_lo >> pass & 1) ? a.lo : 0), 0, 64, 0, t.a_turn.cy, a.lo, true};
+              if (k == t.b_turn.at) b = {t.b_turn.map, 0, t.b_turn.y + k * 64 + ((t.b_lo >> pass & 1) ? b.lo : 0), 0, 64, 0, t.b_turn.cy, b.lo, true};
+            }
             if (!mbar_wait_bounded(empty + stage * 8, parity, kLimit)) {
               ok = false;
               break;
             }
             if (elected) {
               if (cta == 0) mbar_expect_tx(full + stage * 8, kCtas * Shape::kStageBytes);
-              const uint32_t dst = base + stage * Shape::kStageBytes;
-              for (int c = 0; c < a_boxes; ++c)
-                tma_load<kCtas>(dst + c * a_step, t.a.map, xa + c * t.a.cx, ya + c * t.a.cy, signal + stage * 8);
-              for (int c = 0; c < b_boxes; ++c)
-                tma_load<kCtas>(dst + Shape::kABoxes * kBoxBytes + c * b_step, t.b.map, xb + c * t.b.cx, yb + c * t.b.cy, signal + stage * 8);
+              const uint32_t at = base + stage * Shape::kStageBytes, bar = signal + stage * 8;
+              load_operand<kCtas, Shape::kABoxes>(a, at, bar);
+              load_operand<kCtas, Shape::kBBoxes>(b, at + Shape::kABoxes * kBoxBytes, bar);
             }
-            xa += t.a.kx, ya += t.a.ky, xb += t.b.kx, yb += t.b.ky;
+            a.x += a.kx, a.y += a.ky, b.x += b.kx, b.y += b.ky;
             if (used < Shape::kStages) ++used;
             if (++stage == Shape::kStages) {
               stage = 0;
@@ -393,14 +437,17 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       const uint32_t acc_full = smem_u32(&sh.acc_full[0]), acc_empty = smem_u32(&sh.acc_empty[0]);
       uint32_t stage = 0, parity = 0, buf = 0, turn = 1;  // turn: parity of acc_empty
       bool ok = true;
-      for (int64_t i; ok && (i = feed.next()) >= 0;) {
+      for (typename Job::Ticket ticket; ok && (ticket = feed.next()).i >= 0;) {
         Tile t;
-        job.tile(i, cta, t);
-        const uint32_t idesc = (1u << 4) | (Job::kFp16 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)t.a.across << 15) |
-                               ((uint32_t)t.b.across << 16) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(kCtas * 128 >> 4) << 24);
-        const uint32_t a_step = (t.a.across ? 16 * 128 : 32) >> 4, b_step = (t.b.across ? 16 * 128 : 32) >> 4;
-        const uint64_t a0 = smem_descriptor(base, t.a.across), b0 = smem_descriptor(base + Shape::kABoxes * kBoxBytes, t.b.across);
+        job.tile(ticket, cta, t);
+        constexpr uint32_t kAlong = 32 >> 4, kAcross = 16 * 128 >> 4;  // descriptors: 16 of the contraction further
+        const uint32_t idesc0 = (1u << 4) | (Job::kFp16 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(kN >> 3) << 17) |
+                                ((uint32_t)(kCtas * 128 >> 4) << 24);
+        uint32_t idesc = idesc0 | ((uint32_t)t.a.across << 15) | ((uint32_t)t.b.across << 16);
+        uint32_t a_step = t.a.across ? kAcross : kAlong, b_step = t.b.across ? kAcross : kAlong;
+        const uint64_t a0 = smem_descriptor(base), b0 = smem_descriptor(base + Shape::kABoxes * kBoxBytes);
         const int blocks = t.passes * t.k_blocks, chunk = t.chunk > 0 ? t.chunk : blocks;
+        int in_pass = 0;
         int done = 0;
         do {
           if (!mbar_wait_bounded(acc_empty + buf * 8, turn, kLimit)) {
@@ -416,6 +463,14 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
               break;
             }
             tc_fence_after();
+            if constexpr (Job::kTurns) {
+              if (in_pass == t.k_blocks) in_pass = 0;
+              const bool across_a = t.a.across || in_pass >= t.a_turn.at, across_b = t.b.across || in_pass >= t.b_turn.at;
+              ++in_pass;
+              idesc = idesc0 | ((uint32_t)across_a << 15) | ((uint32_t)across_b << 16);
+              a_step = across_a ? kAcross : kAlong;
+              b_step = across_b ? kAcross : kAlong;
+            }
             const uint64_t a = a0 + stage * (Shape::kStageBytes >> 4), b = b0 + stage * (Shape::kStageBytes >> 4);
             if (elected) {
 #pragma unroll
@@ -473,11 +528,11 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         turn ^= 1;
       }
     };
-    for (int64_t i; (i = feed.next()) >= 0;) {
+    for (typename Job::Ticket ticket; (ticket = feed.next()).i >= 0;) {
       int blocks, chunk;
       {
         Tile t;
-        job.tile(i, cta, t);
+        job.tile(ticket, cta, t);
         blocks = t.passes * t.k_blocks;
         chunk = t.chunk > 0 ? t.chunk : blocks;
       }
@@ -491,7 +546,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         give_back();
       }
       if (!ok) break;
-      job.epilogue(i, cta, acc, v);
+      job.epilogue(ticket, cta, acc, v);
       __syncwarp();
     }
     if (!ok || !feed.ok) sh.failed = 1;
