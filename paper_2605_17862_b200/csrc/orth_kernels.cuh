@@ -239,6 +239,7 @@ struct OrthJob {
   };
   const Params &p;
   Staging staging;
+  uint32_t staged_turn = 0;  // parity of this warp's copies into its staging buffers
   __device__ explicit OrthJob(const Params &params) : p(params) {}
   __device__ int64_t tiles() const { return (int64_t)p.steps * (2 * p.sym_tiles + p.x_tiles); }
   __device__ int32_t *status() const { return p.status; }
@@ -338,15 +339,32 @@ struct OrthJob {
     });
     staging.send(acc, &p.rows_out, 0, y, at);
   }
-  __device__ __forceinline__ void epilogue(const Ticket &o, int cta, const Accumulator &acc, float (&v)[kN / 2]) {
+  // A plane of A's values at a warp's part of a tile of P: up to two panels into the staging buffers.
+  __device__ __forceinline__ void stage_square(const Ticket &o, const OrthMatrix &m, int cta, const Accumulator &acc, int plane) {
+    const int row0 = o.row0() + cta * 128 + acc.warp * 32, col0 = o.col0() + acc.half * (kN / 2);
+    const int panels = row0 >= m.mp ? 0 : max(0, min(kN / 128, (m.mp - col0) / 64));
+    if (acc.lane != 0 || panels == 0) return;
+    tma_store_wait_read<0>();
+    mbar_expect_tx(acc.staged, panels * kStageBufBytes);
+    for (int c = 0; c < panels; ++c)
+      tma_load<1>(acc.staging + c * kStageBufBytes, &p.rows_out, 0, m.a + plane * m.m_lo + (col0 / 64 + c) * m.mp + row0, acc.staged);
+  }
+  __device__ __forceinline__ bool prefetch(const Ticket &o, int cta, const Accumulator &acc, long long limit) {
+    if (o.phase() != kOrthPoly) return true;
+    const bool ok = __all_sync(0xffffffffu, ready(o, limit));
+    if (ok) stage_square(o, p.tab.m[o.k], cta, acc, 0);
+    return ok;
+  }
+  __device__ __forceinline__ bool epilogue(const Ticket &o, int cta, const Accumulator &acc, float (&v)[kN / 2]) {
     const OrthMatrix &m = p.tab.m[o.k];
     const int row0 = o.row0() + cta * 128 + acc.warp * 32, col0 = o.col0() + acc.half * (kN / 2);
     if (o.phase() == kOrthApply) put_x(o, m, row0, col0, acc, v);
-    else put_square(o, m, row0, col0, acc, v);
+    else if (!put_square(o, m, cta, row0, col0, acc, v)) return false;
     if (acc.lane == 0 && !(last(o) && o.phase() == kOrthApply)) {  // written, then counted
       tma_store_wait_all();
       add_release(p.ws.done + o.k, 1);
     }
+    return true;
   }
   __device__ __forceinline__ void put_x(const Ticket &o, const OrthMatrix &m, int row0, int col0, const Accumulator &acc, float (&v)[kN / 2]) {
     constexpr int kCols = kN / 2;
@@ -373,33 +391,34 @@ struct OrthJob {
       if (two) put_rows(acc, v + c, y + m.x_lo, true);
     }
   }
-  __device__ __forceinline__ void put_square(const Ticket &o, const OrthMatrix &m, int row0, int col0, const Accumulator &acc,
+  __device__ __forceinline__ bool put_square(const Ticket &o, const OrthMatrix &m, int cta, int row0, int col0, const Accumulator &acc,
                                              float (&v)[kN / 2]) {
     constexpr int kCols = kN / 2;
-    if (row0 >= m.mp || col0 >= m.mp) return;
+    if (row0 >= m.mp || col0 >= m.mp) return true;
     const OrthStep &step = p.step[o.step()];
     const int to = o.phase() == kOrthGram ? m.a : m.p;
     float f = step.poly_c;
     if (o.phase() == kOrthGram) {
       const float s = o.step() == 0 ? p.ws.norm_factor[o.k] : 1.f;
       f = step.gram * s * s;
-    } else {
-      // (A was stored by other SMs: this warp reads it itself, so it looks at the count itself)
-      if (acc.lane == 0) load_acquire(p.ws.done + o.k);
-      __syncwarp();
     }
 #pragma unroll
-    for (int c = 0; c < kCols; c += 64) {
-      if (col0 + c >= m.mp) continue;
+    for (int j = 0; j < kCols; ++j) v[j] *= f;
+    if (o.phase() == kOrthPoly) {
+      for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) {
+        if (plane) {
+          __syncwarp();  // (the first plane has been read by all lanes)
+          stage_square(o, m, cta, acc, 1);
+        }
+        const bool here = mbar_wait_bounded(acc.staged, staged_turn, kLongWaitCycles);
+        if (!__all_sync(0xffffffffu, here)) return false;
+        staged_turn ^= 1;
 #pragma unroll
-      for (int j = 0; j < 64; ++j) v[c + j] *= f;
-      const int panel_row = (col0 + c) / 64 * m.mp + row0;
-      if (o.phase() == kOrthPoly) {
-        for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) {
-          const uint4 *q = reinterpret_cast<const uint4 *>(p.ws.planes + ((int64_t)m.a + plane * m.m_lo + panel_row + acc.lane) * 64);
+        for (int c = 0; c < kCols; c += 64) {
+          if (col0 + c >= m.mp) continue;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const uint4 w = __ldcg(q + j);
+            const uint4 w = lds_vector(acc.staging + (c / 64) * kStageBufBytes + acc.lane * 128 + ((j ^ (acc.lane & 7)) * 16));
             const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -409,14 +428,21 @@ struct OrthJob {
             }
           }
         }
-        const int d = row0 + acc.lane - (col0 + c);
-        if (d >= 0 && d < 64) {
-#pragma unroll
-          for (int j = 0; j < 64; ++j) v[c + j] += j == d ? step.poly_a : 0.f;
-        }
       }
+      __syncwarp();  // (before the buffers are written again)
+      const int d = row0 + acc.lane - col0;
+      if (d >= 0 && d < kCols) {
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) v[j] += j == d ? step.poly_a : 0.f;
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < kCols; c += 64) {
+      if (col0 + c >= m.mp) continue;
+      const int panel_row = (col0 + c) / 64 * m.mp + row0;
       for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) put_rows(acc, v + c, to + plane * m.m_lo + panel_row, plane);
     }
+    return true;
   }
 };
 

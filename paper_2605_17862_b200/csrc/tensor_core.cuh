@@ -211,7 +211,7 @@ struct ProductShape {
 
 constexpr int kFeed = 4;  // tiles a CTA (pair) has claimed and some role has not yet taken note of
 struct ProductShared {
-  unsigned long long full[8], empty[8], acc_full[4], acc_empty[4], drain, feed_full[kFeed], feed_empty[kFeed];
+  unsigned long long full[8], empty[8], acc_full[4], acc_empty[4], drain, feed_full[kFeed], feed_empty[kFeed], staged[kEpilogueWarps];
   int4 feed[kFeed];
   uint32_t tmem;
   int failed;
@@ -221,6 +221,7 @@ struct ProductShared {
 struct Accumulator {
   int warp, lane, half;
   uint32_t staging;  // two staging buffers
+  uint32_t staged;   // a barrier for copies into them
 };
 // Takes a part of an accumulator: v += its columns, or v = them (or zero).
 template <bool kAdd, int kCols>
@@ -263,17 +264,16 @@ struct TileFeed {
   bool ok = true;
   using Ticket = typename Job::Ticket;
   __device__ TileFeed(ProductShared &s, int c, int64_t tiles) : sh(s), cta(c), n_tiles(tiles), step(gridDim.x / kCtas), i((int64_t)(blockIdx.x / kCtas) - step) {}
-  // (by all lanes of a warp) -1: no more, or a wait ran out (then ok is false)
-  __device__ __forceinline__ Ticket next_claimed(const Job &job, bool elected) {
+  // (by all lanes of a warp) the next claimed tile; `asked` is what the elected lane got from the counter, -1 if it has yet to ask
+  __device__ __forceinline__ Ticket next_claimed(const Job &job, bool elected, int asked) {
     const uint32_t slot = n % kFeed;
     ok = __all_sync(0xffffffffu, mbar_wait_cluster_bounded(smem_u32(&sh.feed_empty[slot]), ((n / kFeed) & 1) ^ 1, kLimit));
     Ticket ticket = {};
     ticket.i = -1;
     if (!ok) return ticket;
     ++n;
-    int v = 0;
-    if (elected) v = atomicAdd(job.counter(), 1);
-    v = __reduce_add_sync(0xffffffffu, v);
+    if (elected && asked < 0) asked = atomicAdd(job.counter(), 1);
+    const int v = __reduce_add_sync(0xffffffffu, elected ? asked : 0);
     if (v < n_tiles) ticket = job.ticket(v);
     static_assert(sizeof(Ticket) == 16, "goes through shared memory as one vector");
     if (elected) {
@@ -326,8 +326,9 @@ struct TileFeed {
 
 // Job: Params (a kernel parameter); Job(params); Ticket; int64_t tiles(); void tile(ticket, int cta, Tile &);
 // void epilogue(ticket, int cta, const Accumulator &, float (&v)[kN / 2]); int32_t *status(); static constexpr bool kFp16, kTurns (it has
-// symmetric operands), kClaimed; and where that is true int *counter(), Ticket ticket(i) and bool ready(ticket, limit), which returns
-// when what the tile reads is there.
+// symmetric operands), kClaimed; and where that is true int *counter(), Ticket ticket(i), bool ready(ticket, limit), which returns
+// when what the tile reads is there, and bool prefetch(ticket, cta, acc, limit), what an epilogue warp asks for beforehand (epilogue is bool then;
+// false: a wait ran out).
 struct TileNumber {
   int64_t i;
 };
@@ -354,6 +355,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       mbar_init(smem_u32(&sh.feed_full[i]), 1);
       mbar_init(smem_u32(&sh.feed_empty[i]), kCtas * (1 + kEpilogueWarps));
     }
+    for (int i = 0; i < kEpilogueWarps; ++i) mbar_init(smem_u32(&sh.staged[i]), 1);
     mbar_init(smem_u32(&sh.drain), 1);
     sh.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -380,21 +382,20 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     if (warp == 0) {
       // ---- copies in
       uint32_t stage = 0, used = 0, parity = 1;
+      int asked = -1;
       bool ok = true;
       const uint32_t signal = kCtas == 2 ? map_to_cta(full, 0) : full;
       while (true) {
         typename Job::Ticket ticket;
-        if constexpr (Job::kClaimed) {
-          if (cta == 0) ticket = feed.next_claimed(job, elected);
-          else ticket = feed.next();
-          if (ticket.i >= 0) ok = job.ready(ticket, kLimit);
-        } else {
-          ticket = feed.next();
-        }
-        ok = __all_sync(0xffffffffu, ok);
-        if (ticket.i < 0 || !ok) break;
+        if constexpr (Job::kClaimed) ticket = cta == 0 ? feed.next_claimed(job, elected, asked) : feed.next();
+        else ticket = feed.next();
+        if (ticket.i < 0) break;
         Tile t;
         job.tile(ticket, cta, t);
+        if constexpr (Job::kClaimed) ok = job.ready(ticket, kLimit);
+        ok = __all_sync(0xffffffffu, ok);
+        asked = -1;
+        int left = t.passes * t.k_blocks;
         for (int pass = 0; ok && pass < t.passes; ++pass) {
           Operand a = t.a, b = t.b;
           if (t.a_lo >> pass & 1) a.y += a.lo;
@@ -409,11 +410,15 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
               break;
             }
             if (elected) {
+              // (the next tile, a little before there is nothing left to ask for: the answer takes a while)
+              if constexpr (Job::kClaimed)
+                if (cta == 0 && asked < 0 && left <= 3) asked = atomicAdd(job.counter(), 1);
               if (cta == 0) mbar_expect_tx(full + stage * 8, kCtas * Shape::kStageBytes);
               const uint32_t at = base + stage * Shape::kStageBytes, bar = signal + stage * 8;
               load_operand<kCtas, Shape::kABoxes>(a, at, bar);
               load_operand<kCtas, Shape::kBBoxes>(b, at + Shape::kABoxes * kBoxBytes, bar);
             }
+            --left;
             a.x += a.kx, a.y += a.ky, b.x += b.kx, b.y += b.ky;
             if (used < Shape::kStages) ++used;
             if (++stage == Shape::kStages) {
@@ -507,6 +512,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     acc.half = (warp - kEpilogueWarp0) >> 2;
     acc.lane = lane;
     acc.staging = staging + (warp - kEpilogueWarp0) * kStageBufs * kStageBufBytes;
+    acc.staged = smem_u32(&sh.staged[warp - kEpilogueWarp0]);
     const uint32_t mine = tmem + ((uint32_t)(acc.warp * 32) << 16) + acc.half * (kN / 2);
     uint32_t buf = 0, turn = 0;
     bool ok = true;
@@ -536,6 +542,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         blocks = t.passes * t.k_blocks;
         chunk = t.chunk > 0 ? t.chunk : blocks;
       }
+      if constexpr (Job::kClaimed) {
+        if (!(ok = job.prefetch(ticket, cta, acc, kLimit))) break;
+      }
       if (!wait()) break;
       float v[kN / 2];
       take_columns<false>(v, mine + buf * kN, blocks == 0);
@@ -546,7 +555,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         give_back();
       }
       if (!ok) break;
-      job.epilogue(ticket, cta, acc, v);
+      if constexpr (Job::kClaimed) ok = job.epilogue(ticket, cta, acc, v);
+      else job.epilogue(ticket, cta, acc, v);
+      if (!ok) break;
       __syncwarp();
     }
     if (!ok || !feed.ok) sh.failed = 1;
@@ -574,6 +585,11 @@ __device__ __forceinline__ void stage_box(uint32_t at, int lane, Pack pack) {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at + lane * 128 + ((j ^ (lane & 7)) * 16)), "r"(pack(4 * j)),
                  "r"(pack(4 * j + 1)), "r"(pack(4 * j + 2)), "r"(pack(4 * j + 3))
                  : "memory");
+}
+__device__ __forceinline__ uint4 lds_vector(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
 }
 // A warp's staging buffers in turn: the one whose store was read from before the last.
 struct Staging {
