@@ -175,10 +175,33 @@ int run_table(const std::vector<OrthMatrix> &g, const Group &o, const Scales &s,
   return o.pairs ? run(typename Pairs::Params(), launch_product<2, 256, Pairs>) : run(typename Single::Params(), launch_product<1, 128, Single>);
 }
 
+// Tiles of 256 x 256 on pairs of CTAs, or of 128 x 128 on single ones?  In units of a pair's time for 256 x 256 x 64 products a single one's
+// 128 x 128 x 64 take 0.6 (where sums are taken out every other block 0.43: four accumulators hide that better than two).  Small tiles
+// waste less at the edges and are more in number; a phase takes as long as its share on each CTA, and no less than one tile.
+bool pairs_pay(const std::vector<OrthMatrix> &g, int sms) {
+  double cost[2];
+  for (int v = 0; v < 2; ++v) {
+    const int tile = v ? 256 : 128, slots = v ? sms / 2 : sms;
+    double units[3] = {0, 0, 0}, longest[3] = {0, 0, 0};
+    for (const OrthMatrix &m : g) {
+      const double t = (m.mp + tile - 1) / tile, n_sym = t * (t + 1) / 2, n_x = (double)((m.rp + tile - 1) / tile) * ((m.cp + tile - 1) / tile);
+      const double unit = v ? 1.0 : m.full ? 0.43 : 0.6, passes = m.full ? 3 : 1, other = m.tall ? m.rp : m.cp;
+      const double each[3] = {other / 64 * passes * unit, m.mp / 64 * passes * unit, m.mp / 64 * passes * unit};
+      for (int k = 0; k < 3; ++k) {
+        units[k] += (k < 2 ? n_sym : n_x) * each[k];
+        longest[k] = std::max(longest[k], each[k]);
+      }
+    }
+    cost[v] = 0;
+    for (int k = 0; k < 3; ++k) cost[v] += std::max(units[k] / slots, longest[k]);
+  }
+  return cost[1] <= cost[0];
+}
+
 int run_group(std::vector<OrthMatrix> &g, const Scales &s, int32_t steps, float eps, int32_t *status, int sms, cudaStream_t st) {
   // the largest first: their phases take longest, and the small ones' tiles fill what is left
   std::stable_sort(g.begin(), g.end(), [](const OrthMatrix &a, const OrthMatrix &b) { return (int64_t)a.rp * a.cp > (int64_t)b.rp * b.cp; });
-  int64_t at = 0, norm_blocks = 0, load_blocks = 0, wide_tiles = 0;
+  int64_t at = 0, norm_blocks = 0, load_blocks = 0;
   for (size_t i = 0; i < g.size(); ++i) {
     OrthMatrix &m = g[i];
     m.x[0] += (int)at, m.x[1] += (int)at, m.a += (int)at, m.p += (int)at;
@@ -188,10 +211,8 @@ int run_group(std::vector<OrthMatrix> &g, const Scales &s, int32_t steps, float 
     norm_blocks += m.norm_blocks;
     m.load_block = (int)load_blocks;
     load_blocks += (int64_t)(m.rp / 64) * ((m.cp + kLoadCols - 1) / kLoadCols);
-    wide_tiles += ((int64_t)(m.rp + 255) / 256) * ((m.cp + 255) / 256);
   }
-  // 256 x 256 tiles on pairs of CTAs where they occupy the pairs; else 128 x 128 on single ones, four times as many
-  const int tile = wide_tiles * 2 >= sms ? 256 : 128;
+  const int tile = pairs_pay(g, sms) ? 256 : 128;
   int64_t sym_tiles = 0, x_tiles = 0;
   for (OrthMatrix &m : g) {
     const int64_t t = (m.mp + tile - 1) / tile;

@@ -238,8 +238,8 @@ struct OrthJob {
     __device__ __forceinline__ int col0() const { return (int)(row_col & 0xffff) * kN; }
   };
   const Params &p;
-  Staging staging;
   uint32_t staged_turn = 0;  // parity of this warp's copies into its staging buffers
+  uint32_t order_turn = 1;   // and of the storing thread's handing them back
   __device__ explicit OrthJob(const Params &params) : p(params) {}
   __device__ int64_t tiles() const { return (int64_t)p.steps * (2 * p.sym_tiles + p.x_tiles); }
   __device__ int32_t *status() const { return p.status; }
@@ -329,74 +329,104 @@ struct OrthJob {
     }
   }
 
-  // 64 columns of this warp's rows to a plane: the values, or what their rounding leaves.
-  __device__ __forceinline__ void put_rows(const Accumulator &acc, const float *v, int y, bool lo) {
-    const uint32_t at = staging.next(acc);
-    stage_box(at, acc.lane, [&](int j) {
+  __device__ __forceinline__ const CUtensorMap *store_map() const { return &p.rows_out; }
+  __device__ __forceinline__ int *done_counts() const { return p.ws.done; }
+  // This warp's staging buffers are free.
+  __device__ __forceinline__ bool buffers(const Accumulator &acc) {
+    return __all_sync(0xffffffffu, mbar_wait_bounded(acc.order_empty, order_turn, kLongWaitCycles));
+  }
+  __device__ __forceinline__ void order(const Accumulator &acc, int which, int y, int z, int units) {
+    fence_async_shared();
+    __syncwarp();
+    if (acc.lane == 0) {
+      asm volatile("st.shared.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(acc.order), "r"(which), "r"(y), "r"(z), "r"(units) : "memory");
+      mbar_arrive(acc.order_full);
+    }
+    order_turn ^= 1;
+  }
+  __device__ __forceinline__ bool finish(const Accumulator &acc) {
+    const bool ok = buffers(acc);
+    order(acc, -1, -1, -1, 0);
+    return ok;
+  }
+  // 64 columns of this warp's rows into a staging buffer: the values, or what their rounding leaves.
+  __device__ __forceinline__ void stage(const Accumulator &acc, int buf, const float *v, bool lo) {
+    stage_box(acc.staging + buf * kStageBufBytes, acc.lane, [&](int j) {
       __half2 h = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
       if (lo) h = __floats2half2_rn(v[2 * j] - __low2float(h), v[2 * j + 1] - __high2float(h));
       return *reinterpret_cast<uint32_t *>(&h);
     });
-    staging.send(acc, &p.rows_out, 0, y, at);
   }
+  // All of a tile's columns (up to two panels) to one or two planes of a matrix at row y of its first panel, `pitch` rows to a panel;
+  // panels beyond `have` do not exist.
+  __device__ __forceinline__ bool put(const Ticket &o, const Accumulator &acc, const float (&v)[kN / 2], int have, int y, int pitch,
+                                      bool two, int lo) {
+    constexpr int kPanels = kN / 128;
+    if constexpr (kPanels == 1) {  // both planes in one round
+      if (!buffers(acc)) return false;
+      if (have > 0) {
+        stage(acc, 0, v, false);
+        if (two) stage(acc, 1, v, true);
+      }
+      order(acc, o.k, have > 0 ? y : -1, have > 0 && two ? y + lo : -1, 1);
+    } else {
+      for (int plane = 0; plane < (two ? 2 : 1); ++plane) {
+        if (!buffers(acc)) return false;
+        if (have > 0) stage(acc, 0, v, plane);
+        if (have > 1) stage(acc, 1, v + 64, plane);
+        const int at = y + plane * lo;
+        order(acc, o.k, have > 0 ? at : -1, have > 1 ? at + pitch : -1, plane == (two ? 1 : 0));
+      }
+    }
+    return true;
+  }
+
   // A plane of A's values at a warp's part of a tile of P: up to two panels into the staging buffers.
+  __device__ __forceinline__ int square_panels(const OrthMatrix &m, int row0, int col0) const {
+    return row0 >= m.mp ? 0 : max(0, min(kN / 128, (m.mp - col0) / 64));
+  }
   __device__ __forceinline__ void stage_square(const Ticket &o, const OrthMatrix &m, int cta, const Accumulator &acc, int plane) {
     const int row0 = o.row0() + cta * 128 + acc.warp * 32, col0 = o.col0() + acc.half * (kN / 2);
-    const int panels = row0 >= m.mp ? 0 : max(0, min(kN / 128, (m.mp - col0) / 64));
+    const int panels = square_panels(m, row0, col0);
     if (acc.lane != 0 || panels == 0) return;
-    tma_store_wait_read<0>();
     mbar_expect_tx(acc.staged, panels * kStageBufBytes);
     for (int c = 0; c < panels; ++c)
       tma_load<1>(acc.staging + c * kStageBufBytes, &p.rows_out, 0, m.a + plane * m.m_lo + (col0 / 64 + c) * m.mp + row0, acc.staged);
   }
   __device__ __forceinline__ bool prefetch(const Ticket &o, int cta, const Accumulator &acc, long long limit) {
     if (o.phase() != kOrthPoly) return true;
-    const bool ok = __all_sync(0xffffffffu, ready(o, limit));
+    const bool ok = __all_sync(0xffffffffu, ready(o, limit)) && buffers(acc);
     if (ok) stage_square(o, p.tab.m[o.k], cta, acc, 0);
     return ok;
   }
   __device__ __forceinline__ bool epilogue(const Ticket &o, int cta, const Accumulator &acc, float (&v)[kN / 2]) {
     const OrthMatrix &m = p.tab.m[o.k];
     const int row0 = o.row0() + cta * 128 + acc.warp * 32, col0 = o.col0() + acc.half * (kN / 2);
-    if (o.phase() == kOrthApply) put_x(o, m, row0, col0, acc, v);
-    else if (!put_square(o, m, cta, row0, col0, acc, v)) return false;
-    if (acc.lane == 0 && !(last(o) && o.phase() == kOrthApply)) {  // written, then counted
-      tma_store_wait_all();
-      add_release(p.ws.done + o.k, 1);
-    }
-    return true;
+    return o.phase() == kOrthApply ? put_x(o, m, row0, col0, acc, v) : put_square(o, m, cta, row0, col0, acc, v);
   }
-  __device__ __forceinline__ void put_x(const Ticket &o, const OrthMatrix &m, int row0, int col0, const Accumulator &acc, float (&v)[kN / 2]) {
+  __device__ __forceinline__ bool put_x(const Ticket &o, const OrthMatrix &m, int row0, int col0, const Accumulator &acc, float (&v)[kN / 2]) {
     constexpr int kCols = kN / 2;
-    if (row0 >= m.rp || col0 >= m.cp) return;
     const float f = (o.step() == 0 ? p.ws.norm_factor[o.k] : 1.f) * p.step[o.step()].apply * (last(o) ? m.scale : 1.f);
 #pragma unroll
     for (int j = 0; j < kCols; ++j) v[j] *= f;
     if (last(o)) {
       const int row = row0 + acc.lane;
-      if (row >= m.rows) return;
-      const int64_t at = row * m.out_pitch + col0;
-      char *out = static_cast<char *>(m.out);
-      if (m.out_dtype == FOPD_F32) store_row<FOPD_F32, kCols>(out + at * 4, v, col0, m.cols, false);
-      else store_row<FOPD_BF16, kCols>(out + at * 2, v, col0, m.cols, false);
-      return;
+      if (row < m.rows && col0 < m.cols) {
+        const int64_t at = row * m.out_pitch + col0;
+        char *out = static_cast<char *>(m.out);
+        if (m.out_dtype == FOPD_F32) store_row<FOPD_F32, kCols>(out + at * 4, v, col0, m.cols, false);
+        else store_row<FOPD_BF16, kCols>(out + at * 2, v, col0, m.cols, false);
+      }
+      return true;
     }
-    const int x = m.x[(o.step() + 1) & 1];
-    const bool two = m.two_planes >> (o.step() + 1) & 1;
-#pragma unroll
-    for (int c = 0; c < kCols; c += 64) {
-      if (col0 + c >= m.cp) continue;
-      const int y = x + (col0 + c) / 64 * m.rp + row0;
-      put_rows(acc, v + c, y, false);
-      if (two) put_rows(acc, v + c, y + m.x_lo, true);
-    }
+    return put(o, acc, v, row0 >= m.rp ? 0 : max(0, (m.cp - col0) / 64), m.x[(o.step() + 1) & 1] + col0 / 64 * m.rp + row0, m.rp,
+               m.two_planes >> (o.step() + 1) & 1, m.x_lo);
   }
   __device__ __forceinline__ bool put_square(const Ticket &o, const OrthMatrix &m, int cta, int row0, int col0, const Accumulator &acc,
                                              float (&v)[kN / 2]) {
     constexpr int kCols = kN / 2;
-    if (row0 >= m.mp || col0 >= m.mp) return true;
     const OrthStep &step = p.step[o.step()];
-    const int to = o.phase() == kOrthGram ? m.a : m.p;
+    const int panels = square_panels(m, row0, col0);
     float f = step.poly_c;
     if (o.phase() == kOrthGram) {
       const float s = o.step() == 0 ? p.ws.norm_factor[o.k] : 1.f;
@@ -404,7 +434,7 @@ struct OrthJob {
     }
 #pragma unroll
     for (int j = 0; j < kCols; ++j) v[j] *= f;
-    if (o.phase() == kOrthPoly) {
+    if (o.phase() == kOrthPoly && panels > 0) {
       for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) {
         if (plane) {
           __syncwarp();  // (the first plane has been read by all lanes)
@@ -415,7 +445,7 @@ struct OrthJob {
         staged_turn ^= 1;
 #pragma unroll
         for (int c = 0; c < kCols; c += 64) {
-          if (col0 + c >= m.mp) continue;
+          if (c / 64 >= panels) continue;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const uint4 w = lds_vector(acc.staging + (c / 64) * kStageBufBytes + acc.lane * 128 + ((j ^ (acc.lane & 7)) * 16));
@@ -436,13 +466,7 @@ struct OrthJob {
         for (int j = 0; j < kCols; ++j) v[j] += j == d ? step.poly_a : 0.f;
       }
     }
-#pragma unroll
-    for (int c = 0; c < kCols; c += 64) {
-      if (col0 + c >= m.mp) continue;
-      const int panel_row = (col0 + c) / 64 * m.mp + row0;
-      for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) put_rows(acc, v + c, to + plane * m.m_lo + panel_row, plane);
-    }
-    return true;
+    return put(o, acc, v, panels, (o.phase() == kOrthGram ? m.a : m.p) + col0 / 64 * m.mp + row0, m.mp, m.full, m.m_lo);
   }
 };
 

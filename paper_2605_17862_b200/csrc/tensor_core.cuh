@@ -209,9 +209,12 @@ struct ProductShape {
   static constexpr int kSmem = kStages * kStageBytes + kEpilogueWarps * kStageBufs * kStageBufBytes + 1024;
 };
 
+constexpr long long kLongWaitCycles = 2000000000;  // (~1 s: behind a claimed tile's wait for others)
 constexpr int kFeed = 4;  // tiles a CTA (pair) has claimed and some role has not yet taken note of
 struct ProductShared {
   unsigned long long full[8], empty[8], acc_full[4], acc_empty[4], drain, feed_full[kFeed], feed_empty[kFeed], staged[kEpilogueWarps];
+  unsigned long long order_full[kEpilogueWarps], order_empty[kEpilogueWarps];
+  int4 order[kEpilogueWarps];
   int4 feed[kFeed];
   uint32_t tmem;
   int failed;
@@ -222,6 +225,7 @@ struct Accumulator {
   int warp, lane, half;
   uint32_t staging;  // two staging buffers
   uint32_t staged;   // a barrier for copies into them
+  uint32_t order, order_full, order_empty;  // what the storing thread is to do with them (below)
 };
 // Takes a part of an accumulator: v += its columns, or v = them (or zero).
 template <bool kAdd, int kCols>
@@ -247,12 +251,37 @@ __device__ __forceinline__ void load_operand(const Operand &o, uint32_t at, uint
   }
 }
 
+// Where tiles wait for others, results are stored by a thread of their own, which waits until they are written and counts them, while
+// the epilogue warps go on.  Each of the eight puts one order to a round: the boxes in its two staging buffers go to rows y and z of the map
+// (negative: nothing), w counts are added to entry x of the counts; x negative: no more rounds.  The buffers are the warp's again
+// after order_empty.
+__device__ __forceinline__ bool store_orders(ProductShared &sh, uint32_t staging, const CUtensorMap *map, int *counts) {
+  for (uint32_t turn = 0;; turn ^= 1) {
+    int which = -1, units = 0;
+    for (int w = 0; w < kEpilogueWarps; ++w) {
+      if (!mbar_wait_bounded(smem_u32(&sh.order_full[w]), turn, kLongWaitCycles)) return false;
+      int4 o;
+      asm volatile("ld.shared.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(o.x), "=r"(o.y), "=r"(o.z), "=r"(o.w) : "r"(smem_u32(&sh.order[w])) : "memory");
+      if (o.x < 0) return true;  // (all of them say so)
+      which = o.x;
+      units += o.w;
+      const uint32_t from = staging + w * kStageBufs * kStageBufBytes;
+      if (o.y >= 0) tma_store(map, 0, o.y, from);
+      if (o.z >= 0) tma_store(map, 0, o.z, from + kStageBufBytes);
+    }
+    tma_store_commit();
+    tma_store_wait_read<0>();
+    for (int w = 0; w < kEpilogueWarps; ++w) mbar_arrive(smem_u32(&sh.order_empty[w]));
+    tma_store_wait_all();
+    if (units > 0) add_release(counts + which, units);
+  }
+}
+
 // Which tiles a CTA (pair) works on, as each role sees them.  Either every step-th one, or, where tiles wait for others (kClaimed),
 // the next that no one has: the thread that brings the first CTA's operands in takes it from a counter when it has nothing
 // left to ask for, and passes it on through shared memory.  Tiles are claimed in an order in which each comes behind those it waits for,
 // and a claimed tile is worked on: whatever part of the grid is resident, the lowest unfinished tile can always go on.
 // What the roles get is a ticket (16 bytes, `i` first: the tile, negative where there is no more).
-constexpr long long kLongWaitCycles = 2000000000;  // (~1 s: behind a claimed tile's wait for others)
 template <int kCtas, class Job>
 struct TileFeed {
   static constexpr long long kLimit = Job::kClaimed ? kLongWaitCycles : kWaitCycles;
@@ -327,8 +356,8 @@ struct TileFeed {
 // Job: Params (a kernel parameter); Job(params); Ticket; int64_t tiles(); void tile(ticket, int cta, Tile &);
 // void epilogue(ticket, int cta, const Accumulator &, float (&v)[kN / 2]); int32_t *status(); static constexpr bool kFp16, kTurns (it has
 // symmetric operands), kClaimed; and where that is true int *counter(), Ticket ticket(i), bool ready(ticket, limit), which returns
-// when what the tile reads is there, and bool prefetch(ticket, cta, acc, limit), what an epilogue warp asks for beforehand (epilogue is bool then;
-// false: a wait ran out).
+// when what the tile reads is there, bool prefetch(ticket, cta, acc, limit), what an epilogue warp asks for beforehand, bool finish(acc),
+// what it does at the end (epilogue is bool then; false: a wait ran out), and store_map() and done_counts() for the storing thread.
 struct TileNumber {
   int64_t i;
 };
@@ -355,7 +384,11 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       mbar_init(smem_u32(&sh.feed_full[i]), 1);
       mbar_init(smem_u32(&sh.feed_empty[i]), kCtas * (1 + kEpilogueWarps));
     }
-    for (int i = 0; i < kEpilogueWarps; ++i) mbar_init(smem_u32(&sh.staged[i]), 1);
+    for (int i = 0; i < kEpilogueWarps; ++i) {
+      mbar_init(smem_u32(&sh.staged[i]), 1);
+      mbar_init(smem_u32(&sh.order_full[i]), 1);
+      mbar_init(smem_u32(&sh.order_empty[i]), 1);
+    }
     mbar_init(smem_u32(&sh.drain), 1);
     sh.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -437,6 +470,13 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       }
       if (!ok || !feed.ok) sh.failed = 1;
     }
+    if constexpr (Job::kClaimed) {
+      if (warp == 2) {
+        // ---- stores, and the count of what is stored
+        if (elected && !store_orders(sh, staging, job.store_map(), job.done_counts())) sh.failed = 1;
+        __syncwarp();
+      }
+    }
     if (warp == 1 && cta == 0) {
       // ---- products
       const uint32_t acc_full = smem_u32(&sh.acc_full[0]), acc_empty = smem_u32(&sh.acc_empty[0]);
@@ -513,6 +553,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     acc.lane = lane;
     acc.staging = staging + (warp - kEpilogueWarp0) * kStageBufs * kStageBufBytes;
     acc.staged = smem_u32(&sh.staged[warp - kEpilogueWarp0]);
+    acc.order = smem_u32(&sh.order[warp - kEpilogueWarp0]);
+    acc.order_full = smem_u32(&sh.order_full[warp - kEpilogueWarp0]);
+    acc.order_empty = smem_u32(&sh.order_empty[warp - kEpilogueWarp0]);
     const uint32_t mine = tmem + ((uint32_t)(acc.warp * 32) << 16) + acc.half * (kN / 2);
     uint32_t buf = 0, turn = 0;
     bool ok = true;
@@ -561,6 +604,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       __syncwarp();
     }
     if (!ok || !feed.ok) sh.failed = 1;
+    if constexpr (Job::kClaimed) {
+      if (!job.finish(acc)) sh.failed = 1;
+    }
     if (lane == 0) tma_store_wait_all();
   }
 
