@@ -74,12 +74,12 @@ int prepare_rows(const fopd_head *h, const RowParts &at, char *base, const float
   if (h->mask) {
     int *index = reinterpret_cast<int *>(base + at.index), *active = reinterpret_cast<int *>(base + at.active);
     __nv_bfloat16 *copy = reinterpret_cast<__nv_bfloat16 *>(base + at.copy);
-    head_index_kernel<<<1, kHeadIndexThreads, 0, st>>>(h->mask, h->tokens, coef, (int)h->n_rows, h->vocab, index, active, logprob,
-                                                       lse, status);
+    const int64_t per = round_up((rows + kCompactBlocks - 1) / kCompactBlocks, 8);
+    const int rc = launch_early(head_compact_kernel, dim3((unsigned)((rows + per - 1) / per)), kCompactThreads, st, h->mask, h->tokens, coef,
+                                (int)rows, (int)per, h->vocab, static_cast<const __nv_bfloat16 *>(h->hidden), pitch, (int)h->dim,
+                                (int)round_up(h->dim, 8), copy, index, active, logprob, lse, status);
+    if (rc != FOPD_OK) return rc;
     rows = round_up(h->n_rows, 64);
-    head_gather_kernel<<<(unsigned)((rows + 7) / 8), 256, 0, st>>>(static_cast<const __nv_bfloat16 *>(h->hidden), pitch, index, active,
-                                                                    (int)h->dim, (int)round_up(h->dim, 8), copy);
-    if (launch_ok() != FOPD_OK) return FOPD_ERR_CUDA;
     out->rows.index = index;
     out->rows.active = active;
     hidden = copy;
@@ -116,11 +116,9 @@ int run_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *status,
     p.pitch = (int)pitch;
     p.status = status;
     rc = launch_product<kCtas, kN, LogprobJob<kCtas, kN>>(p, pitch / (kCtas * 128) * v_tiles, sms, st);
-    if (rc == FOPD_OK) {
-      head_join_kernel<<<(unsigned)((h->n_rows + 31) / 32), 1024, 0, st>>>(pre.rows, p.part, p.token_logit, 2 * (int)v_tiles, (int)pitch,
-                                                                           h->tokens, h->vocab, logprob, lse, status);
-      rc = launch_ok();
-    }
+    if (rc == FOPD_OK)
+      rc = launch_early(head_join_kernel, dim3((unsigned)((h->n_rows + 3) / 4)), kJoinThreads, st, pre.rows, (const float2 *)p.part,
+                        (const float *)p.token_logit, 2 * (int)v_tiles, (int)pitch, h->tokens, h->vocab, logprob, lse, status);
   }
   return tmp.give(rc);
 }
@@ -151,7 +149,7 @@ int run_grad(const fopd_head *h, const float *logprob, const float *lse, const f
   // splits of d_hidden's contraction: no tile longer than a quarter of a CTA's share of the piece's work, where the sums fit
   const int64_t d_tiles = (h->dim + kN - 1) / kN, h_tiles = pitch / kRows * d_tiles, w_tiles = piece / kRows * d_tiles;
   const int64_t share = ((o.d_hidden ? h_tiles * panels : 0) + (o.d_weight ? w_tiles * planes * ((h->n_rows + 63) / 64) : 0)) / (sms / kCtas);
-  int64_t split_panels = share / 4 > 8 ? share / 4 : 8;
+  int64_t split_panels = share / 4 > 16 ? share / 4 : 16;
   const int64_t sum_pitch = round_up(h->dim, 32), sum_each = pitch * sum_pitch * 4;
   int64_t splits = (panels + split_panels - 1) / split_panels;
   if (splits > kSumBytes / sum_each) splits = kSumBytes / sum_each;
@@ -174,6 +172,14 @@ int run_grad(const fopd_head *h, const float *logprob, const float *lse, const f
     rc = make_map(&g.panels_out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, 32, true);
   if (rc == FOPD_OK)
     rc = make_map(&q.panels, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, kBoxRows, true);
+  // (a box ends at a multiple of 16 bytes: rows that do not would be written beyond their end)
+  q.d_weight_boxes = o.d_weight && !o.add && h->dim * (o.d_weight_dtype == FOPD_F32 ? 4 : 2) % 16 == 0;
+  if (rc == FOPD_OK && q.d_weight_boxes) {
+    const bool f32 = o.d_weight_dtype == FOPD_F32;
+    const int64_t size = f32 ? 4 : 2, stride = h->vocab > 1 ? o.d_weight_stride : round_up(h->dim, 16 / size);
+    rc = make_map(&q.d_weight_out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, o.d_weight, h->dim, h->vocab,
+                  stride * size, 128 / (int)size, 32, true);
+  }
   if (rc == FOPD_OK)
     rc = make_map(&q.panels_along, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, 2 * kBoxRows, true);
   if (rc == FOPD_OK && o.d_hidden && h->mask &&
@@ -215,10 +221,12 @@ int run_grad(const fopd_head *h, const float *logprob, const float *lse, const f
     }
   }
   if (rc == FOPD_OK && o.d_hidden) {
-    head_hidden_kernel<<<row_grid(h->n_rows), 128, 0, st>>>(
-        pre.rows, q.sum, (int)splits, (int)pitch, (int)sum_pitch, h->tokens, logprob, coef, static_cast<const __nv_bfloat16 *>(h->weight),
-        h->weight_stride, h->vocab, (int)h->dim, o.d_hidden_stride, static_cast<__nv_bfloat16 *>(o.d_hidden));
-    rc = launch_ok();
+    const bool many = splits >= 8;
+    const int dims = many ? 128 : 1024;
+    rc = launch_early(many ? head_hidden_kernel<8> : head_hidden_kernel<1>,
+                      dim3(row_grid(h->n_rows), (unsigned)((h->dim + dims - 1) / dims)), 256, st, pre.rows, (const float *)q.sum, (int)splits,
+                      (int)pitch, (int)sum_pitch, h->tokens, logprob, coef, static_cast<const __nv_bfloat16 *>(h->weight), h->weight_stride,
+                      h->vocab, (int)h->dim, o.d_hidden_stride, static_cast<__nv_bfloat16 *>(o.d_hidden));
   }
   return tmp.give(rc);
 }

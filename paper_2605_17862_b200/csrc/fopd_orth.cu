@@ -154,9 +154,9 @@ int run_table(const std::vector<OrthMatrix> &g, const Group &o, const Scales &s,
   OrthTable<N> tab;
   tab.n = (int)g.size();
   std::copy(g.begin(), g.end(), tab.m);
-  orth_norm_kernel<N><<<(unsigned)o.norm_blocks, kOrthThreads, 0, st>>>(tab, o.ws);
-  orth_load_kernel<N><<<(unsigned)o.load_blocks, kOrthThreads, 0, st>>>(tab, o.ws, eps, status);
-  if (launch_ok() != FOPD_OK) return FOPD_ERR_CUDA;
+  int rc = launch_early(orth_norm_kernel<N>, dim3((unsigned)o.norm_blocks), kOrthThreads, st, tab, o.ws);
+  if (rc == FOPD_OK) rc = launch_early(orth_load_kernel<N>, dim3((unsigned)o.load_blocks), kOrthThreads, st, tab, o.ws, eps, status);
+  if (rc != FOPD_OK) return rc;
   const auto run = [&](auto p, auto launch) {
     p.boxes = o.boxes;
     p.boxes_along = o.boxes_along;

@@ -22,55 +22,66 @@ struct HeadRows {
 };
 
 // ------------------------------------------------------------------ rows that count, one after another
-// The kernel of one CTA that numbers them (and clears the others' results), then the copies of their hidden states.
-constexpr int kHeadIndexThreads = 1024;
-__global__ void __launch_bounds__(kHeadIndexThreads) head_index_kernel(const uint8_t *mask, const int32_t *tokens, const float *coef,
-                                                                       int n, int64_t vocab, int *index, int *active,
-                                                                       float *logprob, float *lse, int32_t *status) {
-  __shared__ int warp_sum[kHeadIndexThreads / 32];
-  __shared__ int base, bad;
+// Numbers the rows that count, copies their hidden states into place and clears the others' results, in one launch: a block takes
+// `per` rows and counts those before them itself (nine bytes to a row, from the L2; at most 512 blocks do so).
+constexpr int kCompactThreads = 256, kCompactBlocks = 512;
+__global__ void __launch_bounds__(kCompactThreads) head_compact_kernel(const uint8_t *mask, const int32_t *tokens, const float *coef,
+                                                                       int n, int per, int64_t vocab, const __nv_bfloat16 *hidden,
+                                                                       int64_t pitch, int dim, int copy_pitch, __nv_bfloat16 *copy,
+                                                                       int *index, int *active, float *logprob, float *lse,
+                                                                       int32_t *status) {
+  __shared__ int sums[kCompactThreads / 32], list[kCompactThreads];
+  grid_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (threadIdx.x == 0) base = bad = 0;
-  __syncthreads();
-  for (int at = 0; at < n; at += kHeadIndexThreads) {
-    const int i = at + threadIdx.x;
-    bool on = i < n && mask[i] != 0;
-    if (on && (uint32_t)tokens[i] >= (uint64_t)vocab) {
-      on = false;
-      bad = 1;
-    }
-    if (on && coef && coef[i] == 0.f) on = false;
-    const uint32_t vote = __ballot_sync(0xffffffffu, on);
-    if (lane == 0) warp_sum[warp] = __popc(vote);
+  const auto counts = [&](int i) {
+    return mask[i] != 0 && (uint32_t)tokens[i] < (uint64_t)vocab && (!coef || coef[i] != 0.f);
+  };
+  const auto sum_of = [&](int x) {  // over the block
+    x = __reduce_add_sync(0xffffffffu, x);
     __syncthreads();
-    int before = base;
-    for (int w = 0; w < warp; ++w) before += warp_sum[w];
-    if (on) index[before + __popc(vote & ((1u << lane) - 1))] = i;
-    if (i < n && !on) {
+    if (lane == 0) sums[warp] = x;
+    __syncthreads();
+    int s = 0;
+    for (int w = 0; w < kCompactThreads / 32; ++w) s += sums[w];
+    return s;
+  };
+  const int first = blockIdx.x * per, end = min(n, first + per);
+  int before = 0;
+  for (int i = threadIdx.x; i < first; i += kCompactThreads) before += counts(i);
+  before = sum_of(before);
+  const auto copy_row = [&](int from, int to) {  // a warp
+    const __nv_bfloat16 *src = from >= 0 ? hidden + (int64_t)from * pitch : nullptr;
+    __nv_bfloat16 *dst = copy + (int64_t)to * copy_pitch;
+#pragma unroll 4
+    for (int d = lane * 8; d < dim; d += 256) {
+      if (d + 8 <= dim) *reinterpret_cast<uint4 *>(dst + d) = src ? *reinterpret_cast<const uint4 *>(src + d) : make_uint4(0, 0, 0, 0);
+      else
+        for (int e = d; e < dim; ++e) dst[e] = src ? src[e] : __float2bfloat16_rn(0.f);
+    }
+  };
+  for (int at = first; at < end; at += kCompactThreads) {
+    const int i = at + threadIdx.x;
+    const bool on = i < end && counts(i);
+    const uint32_t vote = __ballot_sync(0xffffffffu, on);
+    const int all = sum_of(lane == 0 ? __popc(vote) : 0);
+    int place = before + __popc(vote & ((1u << lane) - 1));
+    for (int w = 0; w < warp; ++w) place += sums[w];
+    if (on) {
+      index[place] = i;
+      list[place - before] = i;
+    }
+    if (i < end && !on) {
       if (logprob) logprob[i] = 0.f;
       if (lse) lse[i] = 0.f;
+      if (status && mask[i] != 0 && (uint32_t)tokens[i] >= (uint64_t)vocab) atomicOr(status, FOPD_DEV_BAD_TOKEN);
     }
     __syncthreads();
-    if (threadIdx.x == kHeadIndexThreads - 1) base = before + __popc(vote);
-    __syncthreads();
+    for (int j = warp; j < all; j += kCompactThreads / 32) copy_row(list[j], before + j);
+    before += all;
   }
-  if (threadIdx.x == 0) {
-    *active = base;
-    if (bad && status) atomicOr(status, FOPD_DEV_BAD_TOKEN);
-  }
-}
-
-// A warp per row of the copy; rows up to the next multiple of 64 are cleared, for products along the rows.
-__global__ void __launch_bounds__(256) head_gather_kernel(const __nv_bfloat16 *hidden, int64_t pitch, const int *index,
-                                                          const int *active, int dim, int copy_pitch, __nv_bfloat16 *copy) {
-  const int r = blockIdx.x * 8 + (threadIdx.x >> 5), n = *active;
-  if (r >= (n + 63) / 64 * 64) return;
-  const __nv_bfloat16 *src = r < n ? hidden + (int64_t)index[r] * pitch : nullptr;
-  __nv_bfloat16 *dst = copy + (int64_t)r * copy_pitch;
-  for (int d = (threadIdx.x & 31) * 8; d < dim; d += 256) {
-    if (d + 8 <= dim) *reinterpret_cast<uint4 *>(dst + d) = src ? *reinterpret_cast<const uint4 *>(src + d) : make_uint4(0, 0, 0, 0);
-    else
-      for (int e = d; e < dim; ++e) dst[e] = src ? src[e] : __float2bfloat16_rn(0.f);
+  if (end == n && first < n) {  // the last block: the count, and zeros up to the next 64 rows, for products along the rows
+    if (threadIdx.x == 0) *active = before;
+    for (int r = before + warp; r < (before + 63) / 64 * 64; r += kCompactThreads / 32) copy_row(-1, r);
   }
 }
 
@@ -174,29 +185,42 @@ struct LogprobJob {
   }
 };
 
-// Joins the pieces of 32 rows: 32 threads to a row's pieces, then in a fixed order; exponentials fp32, sums and logs fp64.
-__global__ void __launch_bounds__(1024) head_join_kernel(HeadRows rows, const float2 *part, const float *token_logit, int pieces,
-                                                         int pitch, const int32_t *tokens, int64_t vocab, float *logprob,
-                                                         float *lse, int32_t *status) {
-  __shared__ float sm[32][33];
-  __shared__ double ss[32][33];
-  const int n = rows.count(), tx = threadIdx.x & 31, ty = threadIdx.x >> 5, r = blockIdx.x * 32 + tx;
-  if (blockIdx.x * 32 >= n) return;
-  float m = kNegBig;
-  double s = 0.0;
-  if (r < n)
-    for (int v = ty; v < pieces; v += 32) {
-      const float2 q = part[(int64_t)v * pitch + r];
-      if (q.x > m) {
-        s *= (double)ex2((m - q.x) * kLog2e);
-        m = q.x;
-      }
-      s += (double)(q.y * ex2((q.x - m) * kLog2e));
+// Joins the pieces of four rows: 64 threads to a row, merged in a fixed order; a row's last step in fp64.
+constexpr int kJoinThreads = 256;
+__global__ void __launch_bounds__(kJoinThreads) head_join_kernel(HeadRows rows, const float2 *part, const float *token_logit, int pieces,
+                                                                 int pitch, const int32_t *tokens, int64_t vocab, float *logprob,
+                                                                 float *lse, int32_t *status) {
+  __shared__ float2 shared[kJoinThreads / 32][4];
+  grid_wait();
+  const int n = rows.count(), k = threadIdx.x & 3, r = blockIdx.x * 4 + k, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (blockIdx.x * 4 >= n) return;
+  float m = kNegBig, s = 0.f;
+  const auto merge = [&](float om, float os) {
+    const float top = fmaxf(m, om);
+    s = __fmaf_rn(s, ex2((m - top) * kLog2e), __fmul_rn(os, ex2((om - top) * kLog2e)));
+    m = top;
+  };
+  constexpr int kAhead = 5;  // loads in flight
+  for (int v = threadIdx.x >> 2; v < pieces; v += kAhead * (kJoinThreads / 4)) {
+    float2 q[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int w = v + j * (kJoinThreads / 4);
+      q[j] = w < pieces && r < n ? part[(int64_t)w * pitch + r] : make_float2(kNegBig, 0.f);
     }
-  sm[ty][tx] = m;
-  ss[ty][tx] = s;
+    float top = m;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) top = fmaxf(top, q[j].x);
+    s *= ex2((m - top) * kLog2e);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) s = fmaf(q[j].y, ex2((q[j].x - top) * kLog2e), s);
+    m = top;
+  }
+#pragma unroll
+  for (int o = 4; o < 32; o <<= 1) merge(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, s, o));
+  if (lane < 4) shared[warp][lane] = make_float2(m, s);
   __syncthreads();
-  if (ty != 0 || r >= n) return;
+  if (threadIdx.x >= 4 || r >= n) return;
   const int row = rows.row(r), y = tokens[row];
   if (y < 0 || y >= vocab) {  // (without a mask rows are not sorted out beforehand)
     logprob[row] = 0.f;
@@ -204,14 +228,12 @@ __global__ void __launch_bounds__(1024) head_join_kernel(HeadRows rows, const fl
     if (status) atomicOr(status, FOPD_DEV_BAD_TOKEN);
     return;
   }
-  const float zy = token_logit[r];
-  m = zy;
-  for (int k = 0; k < 32; ++k) m = fmaxf(m, sm[k][tx]);
-  double rest = 0.0;
-  for (int k = 0; k < 32; ++k) rest += ss[k][tx] * exp((double)sm[k][tx] - (double)m);
-  const double d = (double)zy - (double)m, t = exp(d);
+  m = kNegBig, s = 0.f;
+  for (int w = 0; w < kJoinThreads / 32; ++w) merge(shared[w][k].x, shared[w][k].y);
+  const float zy = token_logit[r], top = fmaxf(m, zy);
+  const double d = (double)zy - (double)top, t = exp(d), rest = (double)s * exp((double)m - (double)top);
   logprob[row] = (float)(t > rest ? -log1p(rest / t) : d - log(rest + t));
-  if (lse) lse[row] = (float)((double)m + log(rest + t));
+  if (lse) lse[row] = (float)((double)top + log(rest + t));
 }
 
 // ------------------------------------------------------------------ gradient of the logits, a piece of the vocabulary
@@ -315,6 +337,8 @@ struct HeadGradsJob {
     int first;           // the first piece sets, the others add
     float *sum;          // [splits][pitch][sum_pitch]
     int sum_pitch;
+    CUtensorMap d_weight_out;  // boxes of 32 rows x 128 bytes
+    int d_weight_boxes;        // it is stored by way of those
     void *d_weight;      // or NULL
     int64_t d_weight_pitch;
     int d_weight_f32, add;
@@ -322,6 +346,7 @@ struct HeadGradsJob {
   };
   static constexpr int kRows = kCtas * 128;
   const Params &p;
+  Staging staging;
   int n, m_tiles, d_tiles, v_tiles;
   int64_t n_hidden;
   __device__ explicit HeadGradsJob(const Params &params) : p(params), n(params.rows.count()) {
@@ -369,7 +394,7 @@ struct HeadGradsJob {
     }
     t.b_lo = 0;
   }
-  __device__ __forceinline__ void epilogue(Ticket ticket, int cta, const Accumulator &acc, float (&g)[kN / 2]) const {
+  __device__ __forceinline__ void epilogue(Ticket ticket, int cta, const Accumulator &acc, float (&g)[kN / 2]) {
     int split, row0, d0;
     at(ticket.i, split, row0, d0);
     d0 += acc.half * (kN / 2);
@@ -390,6 +415,31 @@ struct HeadGradsJob {
       }
       return;
     }
+    if (p.d_weight_boxes) {  // (rows and columns that do not exist are left out by the copy)
+      const int64_t row_out = p.v0 + row - acc.lane;
+      if (row - acc.lane >= p.v_count) return;
+      const auto send = [&](const float *v, int d) {  // 128 bytes of each row
+        if (d >= p.dim) return;
+        const uint32_t at = staging.next(acc);
+        if (p.d_weight_f32) stage_box(at, acc.lane, [&](int j) { return __float_as_uint(v[j]); });
+        else
+          stage_box(at, acc.lane, [&](int j) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+            return *reinterpret_cast<const uint32_t *>(&h);
+          });
+        staging.send(acc, &p.d_weight_out, d, (int)row_out, at);
+      };
+      if (p.d_weight_f32) {
+        send(g, d0);
+        send(g + 32, d0 + 32);
+        if (kN > 128) send(g + kN / 2 - 64, d0 + kN / 2 - 64);
+        if (kN > 128) send(g + kN / 2 - 32, d0 + kN / 2 - 32);
+      } else {
+        send(g, d0);
+        if (kN > 128) send(g + kN / 2 - 64, d0 + kN / 2 - 64);
+      }
+      return;
+    }
     if (row >= p.v_count) return;
     const int64_t at = (p.v0 + row) * p.d_weight_pitch + d0;
     char *out = static_cast<char *>(p.d_weight);
@@ -398,41 +448,58 @@ struct HeadGradsJob {
   }
 };
 
-// d_hidden from the splits' sums, added in order, rows back in their places.  What the rounding to bf16 left of the token's own
-// entry of G, as a rule by far the largest of its row, is added here in fp32 (one row of the weights per row).
-__global__ void __launch_bounds__(128) head_hidden_kernel(HeadRows rows, const float *sum, int splits, int pitch, int sum_pitch,
+// d_hidden from the splits' sums, rows back in their places: a thread takes four dimensions of a row and the splits in order, or where
+// there are many, one of eight threads an eighth of them in order.  What the rounding to bf16 left of the token's own entry of G, as a
+// rule by far the largest of its row, is added here in fp32 (one row of the weights per row).
+template <int kGroups>
+__global__ void __launch_bounds__(256) head_hidden_kernel(HeadRows rows, const float *sum, int splits, int pitch, int sum_pitch,
                                                           const int32_t *tokens, const float *logprob, const float *coef,
                                                           const __nv_bfloat16 *weight, int64_t weight_pitch, int64_t vocab, int dim,
                                                           int64_t out_pitch, __nv_bfloat16 *out) {
-  const int n = rows.count();
+  constexpr int kLanes = 256 / kGroups;
+  __shared__ float4 part[kGroups][kLanes];
+  grid_wait();
+  const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes, n = rows.count(), d = (blockIdx.y * kLanes + lane) * 4;
+  const int per = (splits + kGroups - 1) / kGroups, first = group * per, end = min(splits, first + per);
   for (int r = blockIdx.x; r < n; r += gridDim.x) {
-    const int row = rows.row(r), y = tokens[row];
-    const bool known = y >= 0 && y < vocab;
-    const float c = known ? coef[row] : 0.f, g = c != 0.f ? c * expm1f(logprob[row]) : 0.f;
-    const float left = g - __bfloat162float(__float2bfloat16_rn(g));
-    const __nv_bfloat16 *w = weight + (known ? y : 0) * weight_pitch;
-    __nv_bfloat16 *o = out + (int64_t)row * out_pitch;
-    for (int d = threadIdx.x * 8; d < dim; d += 128 * 8) {
-      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      for (int s = 0; s < splits; ++s) {
-        const float4 *q = reinterpret_cast<const float4 *>(sum + ((int64_t)s * pitch + r) * sum_pitch + d);
-        const float4 a = q[0], b = q[1];
-        x[0] += a.x, x[1] += a.y, x[2] += a.z, x[3] += a.w, x[4] += b.x, x[5] += b.y, x[6] += b.z, x[7] += b.w;
-      }
-      if (d + 8 <= dim) {
-        if (left != 0.f) {
-          float v[8];
-          Elem<FOPD_BF16>::unpack(*reinterpret_cast<const uint4 *>(w + d), v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = fmaf(left, v[e], x[e]);
-        }
-        *reinterpret_cast<uint4 *>(o + d) = Elem<FOPD_BF16>::pack(x);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (d + e < dim) o[d + e] = __float2bfloat16_rn(left != 0.f ? fmaf(left, __bfloat162float(w[d + e]), x[e]) : x[e]);
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (d < dim) {
+      const float4 *q = reinterpret_cast<const float4 *>(sum + ((int64_t)first * pitch + r) * sum_pitch + d);
+#pragma unroll 4
+      for (int s = first; s < end; ++s, q += (int64_t)pitch * sum_pitch / 4) {
+        const float4 a = *q;
+        x.x += a.x, x.y += a.y, x.z += a.z, x.w += a.w;
       }
     }
+    if constexpr (kGroups > 1) {
+      part[group][lane] = x;
+      __syncthreads();
+      for (int g = 1; group == 0 && g < kGroups && g * per < splits; ++g) {
+        const float4 a = part[g][lane];
+        x.x += a.x, x.y += a.y, x.z += a.z, x.w += a.w;
+      }
+    }
+    if (group == 0 && d < dim) {
+      const int row = rows.row(r), y = tokens[row];
+      const bool known = y >= 0 && y < vocab;
+      const float c = known ? coef[row] : 0.f, g = c != 0.f ? c * expm1f(logprob[row]) : 0.f;
+      const float left = g - __bfloat162float(__float2bfloat16_rn(g));
+      const __nv_bfloat16 *w = weight + (known ? y : 0) * weight_pitch + d;
+      __nv_bfloat16 *o = out + (int64_t)row * out_pitch + d;
+      float v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (d + e < dim && left != 0.f) v[e] = fmaf(left, __bfloat162float(w[e]), v[e]);
+      if (d + 4 <= dim) {
+        const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
+        *reinterpret_cast<uint2 *>(o) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (d + e < dim) o[e] = __float2bfloat16_rn(v[e]);
+      }
+    }
+    if constexpr (kGroups > 1) __syncthreads();
   }
 }
 

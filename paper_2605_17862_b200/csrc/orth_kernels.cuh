@@ -37,7 +37,7 @@ struct OrthMatrix {
   uint8_t dtype, out_dtype, tall, full;
 };
 
-constexpr int kNormChunk = 32768;  // elements to a block
+constexpr int kNormChunk = 16384;  // elements to a block
 constexpr int kOrthThreads = 256;
 constexpr int kOrthChunk = 2;       // blocks of 64 that an accumulator adds up where the result is fp32
 constexpr int kLoadCols = 256;     // a block of the load takes 64 rows of these
@@ -84,10 +84,11 @@ __device__ __forceinline__ double block_sum(double s, double *scratch) {
   return t;
 }
 
-// Sums of squares in fp64, a block to 32,768 elements.
+// Sums of squares in fp64, a block to 16,384 elements.
 template <int N>
 __global__ void __launch_bounds__(kOrthThreads) orth_norm_kernel(const __grid_constant__ OrthTable<N> tab, OrthWorkspace ws) {
   __shared__ double scratch[kOrthThreads / 32];
+  grid_wait();
   const int k = find_entry(tab.n, (int)blockIdx.x, [&](int j) { return tab.m[j].norm_block; });
   const OrthMatrix &m = tab.m[k];
   const int64_t all = (int64_t)m.rows * m.cols, from = (int64_t)((int)blockIdx.x - m.norm_block) * kNormChunk;
@@ -97,6 +98,7 @@ __global__ void __launch_bounds__(kOrthThreads) orth_norm_kernel(const __grid_co
   const bool dense = m.rows == 1 || m.pitch == m.cols;
   if (dense && ((uintptr_t)m.data & 15) == 0) {  // (chunks start at whole vectors)
     const char *base = static_cast<const char *>(m.data);
+#pragma unroll 4
     for (int64_t i = from + threadIdx.x * per; i + per <= to; i += kOrthThreads * per) {
       const uint4 v = *reinterpret_cast<const uint4 *>(base + i * size);
       if (m.dtype == FOPD_BF16) {
@@ -138,34 +140,45 @@ template <int N>
 __global__ void __launch_bounds__(kOrthThreads) orth_load_kernel(const __grid_constant__ OrthTable<N> tab, OrthWorkspace ws, float eps,
                                                                  int32_t *status) {
   __shared__ double scratch[kOrthThreads / 32];
+  grid_wait();
   const int k = find_entry(tab.n, (int)blockIdx.x, [&](int j) { return tab.m[j].load_block; });
   const OrthMatrix &m = tab.m[k];
   const int block = (int)blockIdx.x - m.load_block;
   double s = 0.0;
   for (int i = threadIdx.x; i < m.norm_blocks; i += kOrthThreads) s += ws.partial[m.norm_block + i];
-  const double norm = sqrt(block_sum(s, scratch));
-  int e = 0;
-  double factor = 0.0, scale;
-  const bool finite = norm <= 1.7e308;
-  if (finite && norm > 0.0) {
-    frexp(norm, &e);  // norm in [2^(e-1), 2^e)
-    e = 15 - e;
-    factor = 1.0 / ((norm + (double)eps) * exp2((double)e));
+  __shared__ double scale_of_block;
+  __shared__ int exponent_of_block;
+  s = block_sum(s, scratch);
+  if (threadIdx.x == 0) {
+    const double norm = sqrt(s);
+    const bool finite = norm <= 1.7e308;
+    int e = 0;
+    double factor = 0.0;
+    if (finite && norm > 0.0) {
+      frexp(norm, &e);  // norm in [2^(e-1), 2^e)
+      e = 15 - e;
+      factor = 1.0 / ldexp(norm + (double)eps, e);
+    }
+    exponent_of_block = finite ? e : 0;
+    scale_of_block = finite ? ldexp(1.0, e) : __longlong_as_double(0x7ff8000000000000ll);
+    if (block == 0) {
+      ws.done[k] = 0;
+      if (k == 0) ws.done[tab.n] = 0;
+      ws.norm_factor[k] = finite ? (float)factor : __int_as_float(0x7fffffff);
+      if (!finite && status) atomicOr(status, FOPD_DEV_NONFINITE);
+    }
   }
-  scale = finite ? exp2((double)e) : __longlong_as_double(0x7ff8000000000000ll);
-  if (block == 0 && threadIdx.x == 0) {
-    ws.done[k] = 0;
-    if (k == 0) ws.done[tab.n] = 0;
-    ws.norm_factor[k] = finite ? (float)factor : __int_as_float(0x7fffffff);
-    if (!finite && status) atomicOr(status, FOPD_DEV_NONFINITE);
-  }
+  __syncthreads();
+  const double scale = scale_of_block;
+  const int e = exponent_of_block;
   const int col_blocks = (m.cp + kLoadCols - 1) / kLoadCols;
   const int row0 = block / col_blocks * 64, col0 = block % col_blocks * kLoadCols;
   const int size = m.dtype == FOPD_BF16 ? 2 : 4;
   const bool two = m.two_planes & 1;
   const bool aligned = (((uintptr_t)m.data | (uintptr_t)(m.rows > 1 ? m.pitch * size : 0)) & 15) == 0;
   const float f = (float)scale;  // (2^e may be beyond fp32 for the smallest matrices: then in fp64)
-  const bool in_range = !finite || (e > -126 && e < 126);
+  const bool in_range = e > -126 && e < 126;
+#pragma unroll 4
   for (int u = threadIdx.x; u < 64 * (kLoadCols / 8); u += kOrthThreads) {
     const int c = col0 + (u / 64 / 8) * 64 + (u & 7) * 8, r = row0 + ((u >> 3) & 63);
     if (c >= m.cp) continue;

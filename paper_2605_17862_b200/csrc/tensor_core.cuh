@@ -33,6 +33,13 @@ __device__ __forceinline__ bool elect_one() {  // the same lane each time
   return yes != 0;
 }
 
+// Kernels that follow one another in a call are launched early: each lets the next one's CTAs come up as soon as its own have started
+// and SMs come free, and waits here, before it reads or writes anything, until everything before it is done.
+__device__ __forceinline__ void grid_wait() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // ------------------------------------------------------------------ TMA
 template <int kCtas>
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
@@ -401,6 +408,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     cluster_wait();
   }
   tc_fence_after();
+  grid_wait();
   const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
 
   Job job(params);

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <atomic>
+#include <utility>
 
 #include "host_common.cuh"
 #include "tensor_core.cuh"
@@ -71,18 +72,39 @@ int launch_product(const typename Job::Params &params, int64_t most_tiles, int s
   }
   if (most_tiles <= 0) return FOPD_OK;
   const int64_t groups = most_tiles < sms / kCtas ? most_tiles : sms / kCtas;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = kCtas;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = kCtas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(groups * kCtas));
   cfg.blockDim = dim3(kProductThreads);
   cfg.dynamicSmemBytes = Shape::kSmem;
   cfg.stream = st;
   cfg.attrs = attr;
-  cfg.numAttrs = kCtas > 1 ? 1 : 0;
+  cfg.numAttrs = kCtas > 1 ? 2 : 1;
   if (cudaLaunchKernelEx(&cfg, kernel, params) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return FOPD_ERR_CUDA;
+  }
+  return FOPD_OK;
+}
+
+// Any other kernel of a call, launched early as well (it begins with grid_wait).
+template <class... Params, class... Args>
+int launch_early(void (*kernel)(Params...), dim3 grid, int threads, cudaStream_t st, Args &&...args) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...) != cudaSuccess) {
     (void)cudaGetLastError();
     return FOPD_ERR_CUDA;
   }
