@@ -195,10 +195,13 @@ struct Tile {
   Turn a_turn, b_turn;  // where the job has symmetric operands
   int k_blocks;  // 0: the product is zero
   int chunk;     // blocks (of all passes) to an accumulator, 0: all
-  int passes;
+  int passes;    // all but the last are small terms: where sums are taken out, one accumulator holds all of those
   uint32_t a_lo, b_lo;
 };
 
+__device__ __forceinline__ int first_chunk(const Tile &t) {
+  return t.chunk > 0 ? (t.passes > 1 ? (t.passes - 1) * t.k_blocks : min(t.chunk, t.k_blocks)) : t.passes * t.k_blocks;
+}
 __device__ __forceinline__ uint64_t smem_descriptor(uint32_t addr) {
   // 128-byte swizzle: groups of 8 rows of 128 bytes, 1,024 bytes apart; across: 64 rows further is the next box (along, this is not
   // looked at)
@@ -238,12 +241,17 @@ struct Accumulator {
 template <bool kAdd, int kCols>
 __device__ __forceinline__ void take_columns(float (&v)[kCols], uint32_t addr, bool zero) {
 #pragma unroll
-  for (int c = 0; c < kCols; c += 32) {
-    uint32_t r[32];
+  for (int c = 0; c < kCols; c += 64) {
+    uint32_t r[32], q[32];
     tmem_load(r, addr + c);
+    tmem_load(q, addr + c + 32);
     tmem_wait(r);
+    tmem_wait(q);
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[c + j] = kAdd ? v[c + j] + __uint_as_float(r[j]) : zero ? 0.f : __uint_as_float(r[j]);
+    for (int j = 0; j < 32; ++j) {
+      v[c + j] = kAdd ? v[c + j] + __uint_as_float(r[j]) : zero ? 0.f : __uint_as_float(r[j]);
+      v[c + 32 + j] = kAdd ? v[c + 32 + j] + __uint_as_float(q[j]) : zero ? 0.f : __uint_as_float(q[j]);
+    }
   }
 }
 
@@ -500,6 +508,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         uint32_t a_step = t.a.across ? kAcross : kAlong, b_step = t.b.across ? kAcross : kAlong;
         const uint64_t a0 = smem_descriptor(base), b0 = smem_descriptor(base + Shape::kABoxes * kBoxBytes);
         const int blocks = t.passes * t.k_blocks, chunk = t.chunk > 0 ? t.chunk : blocks;
+        int end = first_chunk(t);
         int in_pass = 0;
         int done = 0;
         do {
@@ -509,7 +518,6 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
           }
           tc_fence_after();
           const uint32_t d = tmem + buf * kN;
-          const int end = min(blocks, done + chunk);
           for (int k = done; k < end; ++k) {
             if (!mbar_wait_bounded(full + stage * 8, parity, kLimit)) {
               ok = false;
@@ -542,6 +550,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             turn ^= 1;
           }
           done = end;
+          end = min(blocks, end + chunk);
         } while (done < blocks);
         ok = __all_sync(0xffffffffu, ok);
       }
@@ -586,11 +595,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       }
     };
     for (typename Job::Ticket ticket; (ticket = feed.next()).i >= 0;) {
-      int blocks, chunk;
+      int blocks, chunk, done;
       {
         Tile t;
         job.tile(ticket, cta, t);
         blocks = t.passes * t.k_blocks;
+        done = first_chunk(t);
         chunk = t.chunk > 0 ? t.chunk : blocks;
       }
       if constexpr (Job::kClaimed) {
@@ -600,7 +610,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       float v[kN / 2];
       take_columns<false>(v, mine + buf * kN, blocks == 0);
       give_back();
-      for (int done = chunk; done < blocks; done += chunk) {
+      for (; done < blocks; done += chunk) {
         if (!wait()) break;
         take_columns<true>(v, mine + buf * kN, false);
         give_back();
