@@ -104,7 +104,7 @@ typedef enum {
   FOPD_ERR_NULL = -1,   /* a required pointer is NULL                          */
   FOPD_ERR_ALIGN = -2,  /* logits base or pitch, or workspace, not 16-byte aligned */
   FOPD_ERR_SIZE = -3,   /* negative size, row_stride < vocab or cols, too large */
-  FOPD_ERR_DTYPE = -4,  /* dtype is neither FOPD_BF16 nor FOPD_F32              */
+  FOPD_ERR_DTYPE = -4,  /* dtype is neither FOPD_BF16 nor FOPD_F32, or not one the call takes */
   FOPD_ERR_PARAM = -5,  /* a parameter out of its range or not finite           */
   FOPD_ERR_CUDA = -6,   /* a CUDA runtime call failed (launch, allocation)      */
   FOPD_ERR_ALIAS = -7,  /* dlogits overlaps student or teacher, an output an input
@@ -123,7 +123,7 @@ typedef enum {
                                    that call are not to be trusted               */
 #define FOPD_DEV_BAD_LOGITS 32  /* a row to draw from holds NaN or +inf, or no finite logit */
 #define FOPD_DEV_BAD_UNIFORM 64 /* a given random number outside [0, 1)         */
-#define FOPD_DEV_NONFINITE 128  /* a gradient is infinite or NaN (and so their norm) */
+#define FOPD_DEV_NONFINITE 128  /* a gradient or matrix holds an infinity or NaN (and so its norm) */
 
 /* alpha, beta >= 0 scale the two drift diagnostics (Eq. 11); xi is the gate
  * threshold (Eq. 13); lambda weights the rollout anchor (Eq. 16).  The paper
@@ -588,15 +588,15 @@ typedef struct {
                             both in bytes multiples of 16                                            */
   const int32_t *tokens; /* [n_rows]                                                                 */
   const uint8_t *mask;   /* [n_rows] 1 = counts, or NULL: all do                                     */
-  int64_t n_rows, vocab, dim; /* n_rows, vocab <= 2^30, dim <= 2^20                                  */
+  int64_t n_rows, vocab, dim; /* n_rows <= 2^27, vocab <= 2^30, dim <= 2^20                          */
   int64_t hidden_stride, weight_stride; /* >= dim where there is more than one row                   */
   int32_t dtype;         /* FOPD_BF16                                                                */
   int32_t reserved;      /* 0                                                                        */
 } fopd_head;
 
-/* logprob [n_rows] fp32, never above 0, and lse [n_rows] fp32 or NULL.  Products and sums in fp32 (a row's pieces are joined in
- * fp64); the log-prob of a nearly certain token comes from the sum of the others and keeps its relative accuracy.  The outputs must not lie on the inputs or on
- * one another. */
+/* logprob [n_rows] fp32, never above 0, and lse [n_rows] fp32 or NULL.  Logits are fp32 sums rounded to nearest every 512
+ * dimensions (a matrix instruction by itself cuts off what it drops), kept nowhere but on chip; the log-prob of a nearly certain token
+ * comes from the sum of the others and keeps its relative accuracy.  The outputs must not lie on the inputs or on one another. */
 int fopd_head_logprob(const fopd_head *h /* HOST */, float *logprob, float *lse, int32_t *status, void *stream);
 
 /*
@@ -609,8 +609,8 @@ int fopd_head_logprob(const fopd_head *h /* HOST */, float *logprob, float *lse,
  *   add_d_weight    not 0: d_weight += instead of = (the sum over chunks; in fp32 best)
  *
  * G is rounded to bf16 once for the products (2^-9 of each entry at most, of the size of a bf16 result's own rounding); for
- * a d_weight in fp32 what that leaves is kept and multiplied too (2^-17), which costs that product twice.  The temporary is up to
- * 1.3 GB and fp32 sums of d_hidden's size, and with a mask a copy of the hidden states.  Outputs must not lie on inputs or on one another.
+ * a d_weight in fp32 what that leaves is kept and multiplied too (2^-17), which costs that product twice.  The temporary is up to 1 GiB of G (more beyond 2^20 rows), fp32 sums of d_hidden's size or 256 MiB, and
+ * with a mask a copy of the hidden states.  Outputs must not lie on inputs or on one another.
  */
 int fopd_head_grad(const fopd_head *h /* HOST */, const float *logprob, const float *lse, const float *coef, void *d_hidden,
                    int64_t d_hidden_stride, void *d_weight, int64_t d_weight_stride, int32_t d_weight_dtype,
@@ -625,9 +625,8 @@ int fopd_head_grad(const fopd_head *h /* HOST */, const float *logprob, const fl
  * takes the orthogonal factor of its momentum for the update; customary are five steps of (3.4445, -4.7750, 2.0315), eps = 1e-7).
  * Wide, tall and square matrices, any sizes and pitches, all in one call.
  *
- * The norm is summed in fp64.  X, A and their polynomial are held in fp16 under powers of two, 11 bits and two planes where roundings would be
- * amplified by 32 or more; matrices whose result is fp32 in two planes throughout (22 bits; three products for each).  Products
- * and sums are fp32.  Results do not depend on the run.  A matrix of zeros gives zeros; one that holds an infinity or NaN
+ * The norm is summed in fp64.  X, A and their polynomial are held in fp16 under powers of two: 11 bits, and 22 where roundings of X would be
+ * amplified by 32 or more; for matrices whose result is fp32 22 throughout (three products for each).  Sums are fp32.  Results do not depend on the run.  A matrix of zeros gives zeros; one that holds an infinity or NaN
  * gives NaN and sets FOPD_DEV_NONFINITE, the others are not affected.  One whose norm is so far below eps that X's elements are
  * below 2^-39 loses them.
  */
@@ -646,7 +645,8 @@ typedef struct {
  *                  beyond 10^6.
  *   eps            >= 0, finite
  *
- * The temporary is up to eight bytes per element of the list (twelve for fp32 results), in groups of 1 GiB or one matrix.  No
+ * The temporary is up to eight bytes per element of the list and as many per element of the squares of the shorter sides, in groups
+ * of 1 GiB or one matrix.  No
  * result may overlap a matrix of the list or another result, as for fopd_grad_scale; in place it is allowed.
  */
 int fopd_orthogonalise(const fopd_matrix *matrices /* HOST */, int32_t n_matrices, const float *coefficients /* HOST */,

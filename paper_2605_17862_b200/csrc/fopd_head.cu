@@ -7,13 +7,13 @@ using namespace fopd;
 namespace {
 
 constexpr int64_t kPieceBytes = (int64_t)1 << 30;   // gradient of the logits kept at a time
+constexpr int64_t kLogprobRows = 32768;             // rows whose pieces (8 bytes to 128 tokens) are kept at a time
 constexpr int64_t kSumBytes = (int64_t)256 << 20;   // sums of d_hidden, where the vocabulary is cut into splits
 
 int check_head(const fopd_head *h) {
   if (!h) return FOPD_ERR_NULL;
   if (h->dtype != FOPD_BF16) return FOPD_ERR_DTYPE;
-  const int64_t most = (int64_t)1 << 30;
-  if (h->n_rows < 0 || h->vocab <= 0 || h->dim <= 0 || h->n_rows > most || h->vocab > most || h->dim > (1 << 20)) return FOPD_ERR_SIZE;
+  if (h->n_rows < 0 || h->vocab <= 0 || h->dim <= 0 || h->n_rows > 1 << 27 || h->vocab > 1 << 30 || h->dim > 1 << 20) return FOPD_ERR_SIZE;
   if ((h->n_rows > 1 && h->hidden_stride < h->dim) || (h->vocab > 1 && h->weight_stride < h->dim)) return FOPD_ERR_SIZE;
   if (h->hidden_stride > (int64_t)1 << 32 || h->weight_stride > (int64_t)1 << 32) return FOPD_ERR_SIZE;
   if (h->n_rows == 0) return FOPD_OK;
@@ -52,6 +52,8 @@ struct Temporary {
 // The rows of a call and where their hidden states are: the caller's, or with a mask a compacted copy.
 struct Prepared {
   HeadRows rows;
+  const void *hidden_at;   // and what they are from row `first` on: see rows_from
+  int64_t hidden_rows, hidden_pitch;
   CUtensorMap hidden, weight;                // boxes across
   CUtensorMap hidden_along, weight_along;
 };
@@ -68,7 +70,7 @@ RowParts row_parts(const fopd_head *h, Layout *lay) {
 }
 int prepare_rows(const fopd_head *h, const RowParts &at, char *base, const float *coef, float *logprob, float *lse, int32_t *status,
                  cudaStream_t st, Prepared *out) {
-  out->rows = {(int)h->n_rows, nullptr, nullptr};
+  out->rows = {(int)h->n_rows, 0, nullptr, nullptr};
   const void *hidden = h->hidden;
   int64_t rows = h->n_rows, pitch = h->n_rows > 1 ? h->hidden_stride : round_up(h->dim, 8);
   if (h->mask) {
@@ -90,13 +92,25 @@ int prepare_rows(const fopd_head *h, const RowParts &at, char *base, const float
     const int rc = make_map(across, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, at, h->dim, n, stride * 2, 64, kBoxRows, true);
     return rc != FOPD_OK ? rc : make_map(along, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, at, h->dim, n, stride * 2, 64, 2 * kBoxRows, true);
   };
+  out->hidden_at = hidden;
+  out->hidden_rows = rows;
+  out->hidden_pitch = pitch;
   const int rc = maps(&out->hidden, &out->hidden_along, hidden, rows, pitch);
   return rc != FOPD_OK ? rc : maps(&out->weight, &out->weight_along, h->weight, h->vocab, weight_pitch);
 }
 
+// The same from row `first` on, `n` rows at most.
+int rows_from(const fopd_head *h, int64_t first, int64_t n, Prepared *pre) {
+  if (first == 0 && n >= h->n_rows) return FOPD_OK;
+  pre->rows.first = (int)first;
+  pre->rows.n = (int)(h->n_rows - first < n ? h->n_rows - first : n);
+  return make_map(&pre->hidden_along, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, static_cast<const char *>(pre->hidden_at) + first * pre->hidden_pitch * 2,
+                  h->dim, pre->hidden_rows - first, pre->hidden_pitch * 2, 64, 2 * kBoxRows, true);
+}
+
 template <int kCtas, int kN>
 int run_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *status, int sms, cudaStream_t st) {
-  const int64_t v_tiles = (h->vocab + kN - 1) / kN, pitch = round_up(h->n_rows, kCtas * 128);
+  const int64_t v_tiles = (h->vocab + kN - 1) / kN, pitch = round_up(h->n_rows < kLogprobRows ? h->n_rows : kLogprobRows, kCtas * 128);
   Layout lay;
   const RowParts parts = row_parts(h, &lay);
   const int64_t part = lay.take(2 * v_tiles * pitch * 8), logit = lay.take(pitch * 4);
@@ -105,7 +119,9 @@ int run_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *status,
   if (rc != FOPD_OK) return rc;
   Prepared pre;
   rc = prepare_rows(h, parts, tmp.base, nullptr, logprob, lse, status, st, &pre);
-  if (rc == FOPD_OK) {
+  for (int64_t first = 0; rc == FOPD_OK && first < h->n_rows; first += kLogprobRows) {
+    rc = rows_from(h, first, kLogprobRows, &pre);
+    if (rc != FOPD_OK) break;
     typename LogprobJob<kCtas, kN>::Params p;
     p.hidden = pre.hidden_along;
     p.weight = pre.weight_along;
@@ -115,9 +131,9 @@ int run_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *status,
     p.token_logit = reinterpret_cast<float *>(tmp.base + logit);
     p.pitch = (int)pitch;
     p.status = status;
-    rc = launch_product<kCtas, kN, LogprobJob<kCtas, kN>>(p, pitch / (kCtas * 128) * v_tiles, sms, st);
+    rc = launch_product<kCtas, kN, LogprobJob<kCtas, kN>>(p, (pre.rows.n + kCtas * 128 - 1) / (kCtas * 128) * v_tiles, sms, st);
     if (rc == FOPD_OK)
-      rc = launch_early(head_join_kernel, dim3((unsigned)((h->n_rows + 3) / 4)), kJoinThreads, st, pre.rows, (const float2 *)p.part,
+      rc = launch_early(head_join_kernel, dim3((unsigned)((pre.rows.n + 3) / 4)), kJoinThreads, st, pre.rows, (const float2 *)p.part,
                         (const float *)p.token_logit, 2 * (int)v_tiles, (int)pitch, h->tokens, h->vocab, logprob, lse, status);
   }
   return tmp.give(rc);

@@ -12,13 +12,13 @@
 
 namespace fopd {
 
-// The rows a call works on: all n of them, or the *active first ones of a compacted copy.
+// The rows a launch works on: n from `first` on, or as many of those as there are among the *active first ones of a compacted copy.
 struct HeadRows {
-  int n;
-  const int *active;  // DEVICE count, or NULL: n
+  int n, first;
+  const int *active;  // DEVICE count, or NULL
   const int *index;   // compacted row -> row of the caller's, or NULL: the same
-  __device__ __forceinline__ int count() const { return active ? *active : n; }
-  __device__ __forceinline__ int row(int i) const { return index ? index[i] : i; }
+  __device__ __forceinline__ int count() const { return active ? max(0, min(n, *active - first)) : n; }
+  __device__ __forceinline__ int row(int i) const { return index ? index[first + i] : first + i; }
 };
 
 // ------------------------------------------------------------------ rows that count, one after another

@@ -117,6 +117,49 @@ class GradientClip:
         return self.norm
 
 
+class Orthogonalise:
+    """Newton-Schulz orthogonalisation of a set of matrices (momenta, or gradients behind a GradientClip), in place unless
+    ``outs`` is given; ``scales`` of the results, one per tensor.  Keep it as long as the tensors keep their memory."""
+
+    def __init__(self, tensors, outs=None, *, scales=None, coefficients=fb.NEWTON_SCHULZ_COEFFICIENTS, eps: float = 1e-7):
+        self.matrices = fb.MatrixList(tensors, outs, scales)
+        self.coefficients, self.eps = tuple(coefficients), float(eps)
+
+    def __call__(self, *, status=None, stream=None):
+        fb.fopd_orthogonalise(self.matrices, coefficients=self.coefficients, eps=self.eps, status=status, stream=stream)
+
+
+@dataclass
+class HeadChunk:
+    """Token rows of a supervised step before the head: hidden states, stored tokens, their weights in the loss."""
+    hidden: torch.Tensor  # [n, D] bf16
+    tokens: torch.Tensor  # [n] int32
+    coef: torch.Tensor  # [n] fp32
+    mask: torch.Tensor | None = None  # [n] uint8
+    d_hidden: torch.Tensor | None = None  # [n, D] bf16: where the gradient goes, or not wanted
+    logprob: torch.Tensor = None
+    lse: torch.Tensor = None
+
+    def __post_init__(self):
+        n = self.tokens.numel()
+        for name in ("logprob", "lse"):
+            if getattr(self, name) is None:
+                setattr(self, name, torch.zeros(n, dtype=torch.float32, device=self.hidden.device))
+
+
+def supervised_step(chunks, weight, d_weight, *, clip=None, update=None, status=None, stream=None):
+    """The gradient of -sum coef log p(token) through the vocabulary head without its logits: log-probs and gradients chunk by
+    chunk, the weights' gradient added up over the chunks (in fp32 best), then ``clip`` (a GradientClip) and ``update`` (an
+    Orthogonalise) where given, as a rule over d_weight and the model's other gradients."""
+    for j, ch in enumerate(chunks):
+        fb.fopd_head_logprob(ch.hidden, weight, ch.tokens, ch.logprob, lse=ch.lse, mask=ch.mask, status=status, stream=stream)
+        fb.fopd_head_grad(ch.hidden, weight, ch.tokens, ch.logprob, ch.lse, ch.coef, d_hidden=ch.d_hidden, d_weight=d_weight,
+                          add_d_weight=j > 0, mask=ch.mask, status=status, stream=stream)
+    for after in (clip, update):
+        if after is not None:
+            after(status=status, stream=stream)
+
+
 def step(chunks, dlogits, buf: BatchBuffers, tau, H, d_sup, p, rows=None, *, use_row_ws=True, clip=None, stream=None):
     """One pass of the whole hot path over one batch.  ``clip``: a GradientClip over the batch's
     dlogits (their columns in use), applied when all of them are written."""

@@ -252,6 +252,13 @@ def test_pieces_and_splits_of_the_vocabulary():
     assert float((dw.double() - want_w).norm()) <= 2.0 ** -14 * float(want_w.norm())
 
 
+@pytest.mark.parametrize("masked", [0.0, 0.1, 0.6, 1.0])
+def test_more_rows_than_are_kept_at_a_time(masked):
+    """Log-probs of more than 32,768 rows, the count of those that matter above it, below it or zero."""
+    h, w, y, mask, _ = inputs(70001, 300, 64, 22, masked=masked)
+    check_logprob(h, w, y, mask)
+
+
 def test_gradient_against_differences():
     """Central differences of the loss -sum coef logprob computed by the forward call itself along random directions."""
     n, V, D = 40, 500, 64
