@@ -33,8 +33,9 @@ __global__ void __launch_bounds__(kCompactThreads) head_compact_kernel(const uin
   __shared__ int sums[kCompactThreads / 32], list[kCompactThreads];
   grid_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const auto counts = [&](int i) {
-    return mask[i] != 0 && (uint32_t)tokens[i] < (uint64_t)vocab && (!coef || coef[i] != 0.f);
+  const auto counts = [&](int i) {  // (all three are asked for at once)
+    const bool on = mask[i] != 0, known = (uint32_t)tokens[i] < (uint64_t)vocab, weighs = coef ? coef[i] != 0.f : true;
+    return on & known & weighs;
   };
   const auto sum_of = [&](int x) {  // over the block
     x = __reduce_add_sync(0xffffffffu, x);
@@ -47,6 +48,7 @@ __global__ void __launch_bounds__(kCompactThreads) head_compact_kernel(const uin
   };
   const int first = blockIdx.x * per, end = min(n, first + per);
   int before = 0;
+#pragma unroll 4
   for (int i = threadIdx.x; i < first; i += kCompactThreads) before += counts(i);
   before = sum_of(before);
   const auto copy_row = [&](int from, int to) {  // a warp
@@ -399,20 +401,12 @@ struct HeadGradsJob {
     at(ticket.i, split, row0, d0);
     d0 += acc.half * (kN / 2);
     const int row = row0 + cta * 128 + acc.warp * 32 + acc.lane;
-    if (split >= 0) {
-      if (row >= n) return;
-      float *out = p.sum + ((int64_t)split * p.pitch + row) * p.sum_pitch + d0;
+    if (split >= 0) {  // (sum_pitch is a multiple of 32)
+      const uint32_t at = staging.idle(acc);
+      float *out = p.sum + ((int64_t)split * p.pitch + row - acc.lane) * p.sum_pitch + d0;
 #pragma unroll
-      for (int j = 0; j < kN / 2; j += 4) {
-        if (d0 + j >= p.dim) continue;  // (sum_pitch is a multiple of 32)
-        float4 *q = reinterpret_cast<float4 *>(out + j);
-        float4 v = make_float4(g[j], g[j + 1], g[j + 2], g[j + 3]);
-        if (!p.first) {
-          const float4 o = *q;
-          v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
-        }
-        *q = v;
-      }
+      for (int c = 0; c < kN / 2; c += 32)
+        put_rows_out<FOPD_F32>(at, acc.lane, g + c, out + c, p.sum_pitch, min(32, n - (row - acc.lane)), d0 + c < p.dim ? 32 : 0, !p.first);
       return;
     }
     if (p.d_weight_boxes) {  // (rows and columns that do not exist are left out by the copy)
@@ -440,11 +434,19 @@ struct HeadGradsJob {
       }
       return;
     }
-    if (row >= p.v_count) return;
-    const int64_t at = (p.v0 + row) * p.d_weight_pitch + d0;
-    char *out = static_cast<char *>(p.d_weight);
-    if (p.d_weight_f32) store_row<FOPD_F32, kN / 2>(out + at * 4, g, d0, p.dim, p.add);
-    else store_row<FOPD_BF16, kN / 2>(out + at * 2, g, d0, p.dim, p.add);
+    const uint32_t at = staging.idle(acc);
+    const int rows = min(32, p.v_count - (row - acc.lane));
+    const int64_t first = (p.v0 + row - acc.lane) * p.d_weight_pitch + d0;
+    if (p.d_weight_f32) {
+#pragma unroll
+      for (int c = 0; c < kN / 2; c += 32)
+        put_rows_out<FOPD_F32>(at, acc.lane, g + c, static_cast<float *>(p.d_weight) + first + c, p.d_weight_pitch, rows, min(32, p.dim - d0 - c), p.add);
+    } else {
+#pragma unroll
+      for (int c = 0; c < kN / 2; c += 64)
+        put_rows_out<FOPD_BF16>(at, acc.lane, g + c, static_cast<__nv_bfloat16 *>(p.d_weight) + first + c, p.d_weight_pitch, rows,
+                                min(64, p.dim - d0 - c), p.add);
+    }
   }
 };
 

@@ -394,41 +394,6 @@ struct OrthJob {
     return true;
   }
 
-  // 128 bytes of each of this warp's rows into the result, by way of a staging buffer so that lanes lie along the rows.
-  template <int DT>
-  __device__ __forceinline__ void put_out(const OrthMatrix &m, const Accumulator &acc, const float *v, int row0, int col0) const {
-    constexpr int kBytes = Elem<DT>::kBytes, kPer = Elem<DT>::kPerVec, kCols = 128 / kBytes;
-    if (row0 >= m.rows || col0 >= m.cols) return;
-    stage_box(acc.staging, acc.lane, [&](int j) {
-      if constexpr (DT == FOPD_F32) return __float_as_uint(v[j]);
-      const __nv_bfloat162 h = __floats2bfloat162_rn(v[(2 * j) % kCols], v[(2 * j + 1) % kCols]);
-      return *reinterpret_cast<const uint32_t *>(&h);
-    });
-    __syncwarp();
-    char *out = static_cast<char *>(m.out) + (row0 * m.out_pitch + col0) * kBytes;
-    const int rows = min(32, m.rows - row0), cols = min(kCols, m.cols - col0);
-    const bool aligned = (((uintptr_t)m.out | (uintptr_t)(m.out_pitch * kBytes)) & 15) == 0;
-    if (aligned && cols % kPer == 0) {
-      const int piece = acc.lane & 7;
-      for (int r = acc.lane >> 3; r < rows; r += 4)
-        if (piece * kPer < cols)
-          *reinterpret_cast<uint4 *>(out + r * m.out_pitch * kBytes + piece * 16) = lds_vector(acc.staging + r * 128 + ((piece ^ (r & 7)) * 16));
-    } else {
-      for (int r = 0; r < rows; ++r) {
-        uint32_t w;
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(acc.staging + r * 128 + (((acc.lane >> 2) ^ (r & 7)) * 16) + (acc.lane & 3) * 4) : "memory");
-        char *q = out + r * m.out_pitch * kBytes + acc.lane * 4;
-        if constexpr (DT == FOPD_F32) {
-          if (acc.lane < cols) *reinterpret_cast<uint32_t *>(q) = w;
-        } else {
-          if (2 * acc.lane < cols) *reinterpret_cast<uint16_t *>(q) = (uint16_t)w;
-          if (2 * acc.lane + 1 < cols) *reinterpret_cast<uint16_t *>(q + 2) = (uint16_t)(w >> 16);
-        }
-      }
-    }
-    __syncwarp();  // (before the buffer is written again)
-  }
-
   // A plane of A's values at a warp's part of a tile of P: up to two panels into the staging buffers.
   __device__ __forceinline__ int square_panels(const OrthMatrix &m, int row0, int col0) const {
     return row0 >= m.mp ? 0 : max(0, min(kN / 128, (m.mp - col0) / 64));
@@ -459,12 +424,16 @@ struct OrthJob {
     for (int j = 0; j < kCols; ++j) v[j] *= f;
     if (last(o)) {
       if (!buffers(acc)) return false;
+      const int rows = min(32, m.rows - row0);
+      const int64_t at = row0 * m.out_pitch + col0;
       if (m.out_dtype == FOPD_F32) {
 #pragma unroll
-        for (int c = 0; c < kCols; c += 32) put_out<FOPD_F32>(m, acc, v + c, row0, col0 + c);
+        for (int c = 0; c < kCols; c += 32)
+          put_rows_out<FOPD_F32>(acc.staging, acc.lane, v + c, static_cast<float *>(m.out) + at + c, m.out_pitch, rows, min(32, m.cols - col0 - c), false);
       } else {
 #pragma unroll
-        for (int c = 0; c < kCols; c += 64) put_out<FOPD_BF16>(m, acc, v + c, row0, col0 + c);
+        for (int c = 0; c < kCols; c += 64)
+          put_rows_out<FOPD_BF16>(acc.staging, acc.lane, v + c, static_cast<__nv_bfloat16 *>(m.out) + at + c, m.out_pitch, rows, min(64, m.cols - col0 - c), false);
       }
       return true;
     }

@@ -665,6 +665,12 @@ struct Staging {
     __syncwarp();
     return at;
   }
+  // One that no store by TMA is going to read, for other uses.
+  __device__ __forceinline__ uint32_t idle(const Accumulator &acc) {
+    if (acc.lane == 0) tma_store_wait_read<0>();
+    __syncwarp();
+    return acc.staging;
+  }
   __device__ __forceinline__ void send(const Accumulator &acc, const CUtensorMap *map, int x, int y, uint32_t at) {
     fence_async_shared();
     __syncwarp();
@@ -674,31 +680,72 @@ struct Staging {
     }
   }
 };
-// kCount results of a row from element `col` on, of which the row has `cols`; wide stores where they are aligned.
-template <int DT, int kCount>
-__device__ __forceinline__ void store_row(char *q, const float *g, int col, int cols, bool add) {
-  constexpr int kPer = Elem<DT>::kPerVec;
-  const bool aligned = ((uintptr_t)q & 15) == 0;
+// 128 bytes of each of a warp's rows to (or added to) rows at any pitch and alignment, by way of a staging buffer so that lanes lie along
+// the rows: v are the lane's 32 fp32 or 64 bf16 results; `rows` and `cols` of them exist.
+template <int DT>
+__device__ __forceinline__ void put_rows_out(uint32_t at, int lane, const float *v, void *to, int64_t pitch, int rows, int cols, bool add) {
+  constexpr int kBytes = Elem<DT>::kBytes, kPer = Elem<DT>::kPerVec, kCols = 128 / kBytes;
+  if (rows <= 0 || cols <= 0) return;
+  char *out = static_cast<char *>(to);
+  pitch *= kBytes;
+  const bool aligned = (((uintptr_t)out | (uintptr_t)pitch) & 15) == 0;
+  const int piece = lane & 7;
+  if (DT == FOPD_BF16 && add) {  // (sums are rounded once: the results stay fp32 up to the addition, half of the columns at a time)
 #pragma unroll
-  for (int j = 0; j < kCount; j += kPer) {
-    if (aligned && col + j + kPer <= cols) {
-      float x[kPer];
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) x[e] = g[j + e];
-      uint4 *w = reinterpret_cast<uint4 *>(q + j * Elem<DT>::kBytes);
-      if (add) {
-        float o[kPer];
-        Elem<DT>::unpack(*w, o);
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) x[e] += o[e];
+    for (int half = 0; half < 2; ++half) {
+      stage_box(at, lane, [&](int j) { return __float_as_uint(v[(half * 32 + j) % kCols]); });
+      __syncwarp();
+      for (int r = 0; r < rows; ++r) {
+        float x;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at + r * 128 + (((lane >> 2) ^ (r & 7)) * 16) + (lane & 3) * 4) : "memory");
+        if (half * 32 + lane < cols) {
+          char *q = out + r * pitch + (half * 32 + lane) * kBytes;
+          Elem<DT>::store1(q, 0, x + Elem<DT>::load1(q, 0));
+        }
       }
-      *w = Elem<DT>::pack(x);
-    } else {
+      __syncwarp();
+    }
+    return;
+  }
+  stage_box(at, lane, [&](int j) {
+    if constexpr (DT == FOPD_F32) return __float_as_uint(v[j]);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v[(2 * j) % kCols], v[(2 * j + 1) % kCols]);
+    return *reinterpret_cast<const uint32_t *>(&h);
+  });
+  __syncwarp();
+  if (aligned) {
+    for (int r = lane >> 3; r < rows; r += 4) {
+      uint4 w = lds_vector(at + r * 128 + ((piece ^ (r & 7)) * 16));
+      char *q = out + r * pitch + piece * 16;
+      if ((piece + 1) * kPer <= cols) {
+        if (DT == FOPD_F32 && add) {
+          const float4 o = *reinterpret_cast<const float4 *>(q);
+          w.x = __float_as_uint(__uint_as_float(w.x) + o.x), w.y = __float_as_uint(__uint_as_float(w.y) + o.y);
+          w.z = __float_as_uint(__uint_as_float(w.z) + o.z), w.w = __float_as_uint(__uint_as_float(w.w) + o.w);
+        }
+        *reinterpret_cast<uint4 *>(q) = w;
+      } else if (piece * kPer < cols) {  // the end of a row
+        float x[kPer];
+        Elem<DT>::unpack(w, x);
 #pragma unroll
-      for (int e = 0; e < kPer; ++e)
-        if (col + j + e < cols) Elem<DT>::store1(q, j + e, add ? g[j + e] + Elem<DT>::load1(q, j + e) : g[j + e]);
+        for (int e = 0; e < kPer; ++e)
+          if (piece * kPer + e < cols) Elem<DT>::store1(q, e, add ? x[e] + Elem<DT>::load1(q, e) : x[e]);
+      }
+    }
+  } else {
+    for (int r = 0; r < rows; ++r) {
+      uint32_t w;
+      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(at + r * 128 + (((lane >> 2) ^ (r & 7)) * 16) + (lane & 3) * 4) : "memory");
+      char *q = out + r * pitch + lane * 4;
+      if constexpr (DT == FOPD_F32) {
+        if (lane < cols) *reinterpret_cast<float *>(q) = add ? *reinterpret_cast<float *>(q) + __uint_as_float(w) : __uint_as_float(w);
+      } else {
+        if (2 * lane < cols) *reinterpret_cast<uint16_t *>(q) = (uint16_t)w;
+        if (2 * lane + 1 < cols) *reinterpret_cast<uint16_t *>(q + 2) = (uint16_t)(w >> 16);
+      }
     }
   }
+  __syncwarp();  // (before the buffer is written again)
 }
 
 }  // namespace fopd
