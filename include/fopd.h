@@ -609,7 +609,7 @@ int fopd_head_logprob(const fopd_head *h /* HOST */, float *logprob, float *lse,
  *   add_d_weight    not 0: d_weight += instead of = (the sum over chunks; in fp32 best)
  *
  * G is rounded to bf16 once for the products (2^-9 of each entry at most, of the size of a bf16 result's own rounding); for
- * a d_weight in fp32 what that leaves is kept and multiplied too (2^-17), which costs that product twice.  The temporary is up to 1 GiB of G (more beyond 2^20 rows), fp32 sums of d_hidden's size or 256 MiB, and
+ * a d_weight in fp32 what that leaves is kept and multiplied too (2^-17), which costs that product twice.  The temporary is up to 512 MiB of G (more beyond 2^19 rows), fp32 sums of d_hidden's size or 256 MiB, and
  * with a mask a copy of the hidden states.  Outputs must not lie on inputs or on one another.
  */
 int fopd_head_grad(const fopd_head *h /* HOST */, const float *logprob, const float *lse, const float *coef, void *d_hidden,

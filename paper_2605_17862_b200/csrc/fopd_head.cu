@@ -6,7 +6,7 @@ using namespace fopd;
 
 namespace {
 
-constexpr int64_t kPieceBytes = (int64_t)1 << 30;   // gradient of the logits kept at a time
+constexpr int64_t kPieceBytes = (int64_t)1 << 29;   // gradient of the logits kept at a time
 constexpr int64_t kLogprobRows = 32768;             // rows whose pieces (8 bytes to 128 tokens) are kept at a time
 constexpr int64_t kSumBytes = (int64_t)256 << 20;   // sums of d_hidden, where the vocabulary is cut into splits
 
@@ -52,11 +52,14 @@ struct Temporary {
 // The rows of a call and where their hidden states are: the caller's, or with a mask a compacted copy.
 struct Prepared {
   HeadRows rows;
-  const void *hidden_at;   // and what they are from row `first` on: see rows_from
+  const void *hidden_at;
   int64_t hidden_rows, hidden_pitch;
-  CUtensorMap hidden, weight;                // boxes across
-  CUtensorMap hidden_along, weight_along;
+  CUtensorMap hidden_along, weight_along;  // boxes for products along the dimensions
 };
+int operand_map(CUtensorMap *map, const void *at, int64_t dim, int64_t rows, int64_t pitch, int box_rows) {
+  return make_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, at, dim, rows, pitch * 2, 64, box_rows, true);
+}
+int64_t weight_pitch(const fopd_head *h) { return h->vocab > 1 ? h->weight_stride : round_up(h->dim, 8); }
 struct RowParts {
   int64_t index = 0, active = 0, copy = 0;
 };
@@ -87,16 +90,11 @@ int prepare_rows(const fopd_head *h, const RowParts &at, char *base, const float
     hidden = copy;
     pitch = round_up(h->dim, 8);
   }
-  const int64_t weight_pitch = h->vocab > 1 ? h->weight_stride : round_up(h->dim, 8);
-  const auto maps = [&](CUtensorMap *across, CUtensorMap *along, const void *at, int64_t n, int64_t stride) {
-    const int rc = make_map(across, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, at, h->dim, n, stride * 2, 64, kBoxRows, true);
-    return rc != FOPD_OK ? rc : make_map(along, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, at, h->dim, n, stride * 2, 64, 2 * kBoxRows, true);
-  };
   out->hidden_at = hidden;
   out->hidden_rows = rows;
   out->hidden_pitch = pitch;
-  const int rc = maps(&out->hidden, &out->hidden_along, hidden, rows, pitch);
-  return rc != FOPD_OK ? rc : maps(&out->weight, &out->weight_along, h->weight, h->vocab, weight_pitch);
+  const int rc = operand_map(&out->hidden_along, hidden, h->dim, rows, pitch, 2 * kBoxRows);
+  return rc != FOPD_OK ? rc : operand_map(&out->weight_along, h->weight, h->dim, h->vocab, weight_pitch(h), 2 * kBoxRows);
 }
 
 // The same from row `first` on, `n` rows at most.
@@ -104,8 +102,8 @@ int rows_from(const fopd_head *h, int64_t first, int64_t n, Prepared *pre) {
   if (first == 0 && n >= h->n_rows) return FOPD_OK;
   pre->rows.first = (int)first;
   pre->rows.n = (int)(h->n_rows - first < n ? h->n_rows - first : n);
-  return make_map(&pre->hidden_along, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, static_cast<const char *>(pre->hidden_at) + first * pre->hidden_pitch * 2,
-                  h->dim, pre->hidden_rows - first, pre->hidden_pitch * 2, 64, 2 * kBoxRows, true);
+  return operand_map(&pre->hidden_along, static_cast<const char *>(pre->hidden_at) + first * pre->hidden_pitch * 2, h->dim,
+                     pre->hidden_rows - first, pre->hidden_pitch, 2 * kBoxRows);
 }
 
 template <int kCtas, int kN>
@@ -184,6 +182,8 @@ int run_grad(const fopd_head *h, const float *logprob, const float *lse, const f
   rc = prepare_rows(h, parts, tmp.base, coef, nullptr, nullptr, status, st, &pre);
   typename GradLogitsJob<kCtas, kN>::Params g;
   typename HeadGradsJob<kCtas, kN>::Params q;
+  if (rc == FOPD_OK) rc = operand_map(&q.hidden, pre.hidden_at, h->dim, pre.hidden_rows, pre.hidden_pitch, kBoxRows);
+  if (rc == FOPD_OK) rc = operand_map(&q.weight, h->weight, h->dim, h->vocab, weight_pitch(h), kBoxRows);
   if (rc == FOPD_OK)
     rc = make_map(&g.panels_out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, 32, true);
   if (rc == FOPD_OK)
@@ -205,8 +205,6 @@ int run_grad(const fopd_head *h, const float *logprob, const float *lse, const f
   if (rc == FOPD_OK) {
     g.hidden = pre.hidden_along;
     g.weight = pre.weight_along;
-    q.hidden = pre.hidden;
-    q.weight = pre.weight;
     g.tokens = h->tokens;
     g.logprob = logprob;
     g.lse = lse;

@@ -72,6 +72,23 @@ def test_large_tiles(din):
         check(M, o, s)
 
 
+@pytest.mark.parametrize("shape", [(64, 2000), (2000, 70), (128, 8192), (300, 5000), (5000, 300), (130, 64 * 35 + 1), (520, 4100)])
+@pytest.mark.parametrize("din,dout", [(BF16, BF16), (F32, F32)])
+def test_few_tiles_with_long_products(shape, din, dout):
+    """One or a few tiles of X X^T, their contraction long; the same bits each time."""
+    M = matrix(*shape, seed=shape[0], dtype=din)
+    outs = [torch.empty(shape, device=DEV, dtype=dout) for _ in range(3)]
+    for o in outs:
+        run([M], [o])
+    check(M, outs[0])
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    other = matrix(90, 3000, 5, dtype=din)
+    more = [torch.empty(x.shape, device=DEV, dtype=dout) for x in (M, other)]
+    run([M, other], more)
+    check(M, more[0])
+    check(other, more[1])
+
+
 def test_results_are_near_orthogonal():
     """What it is for: singular values end up in [0.68, 1.21] (five steps reach 0.68 from 0.0035 up), directions stay."""
     M = matrix(300, 500, 3, F32, strong=False)
