@@ -88,13 +88,14 @@ __global__ void __launch_bounds__(kCompactThreads) head_compact_kernel(const uin
 }
 
 // ------------------------------------------------------------------ tiles of logits
-constexpr int kLogitChunk = 8;  // blocks of 64 dimensions that a matrix instruction's accumulator adds up
+constexpr int kLogitChunk = 8;  // for logits whose error is to stay that of fp32 sums: 512 dimensions
 struct LogitTiles {
   const CUtensorMap *hidden, *weight;
   HeadRows rows;
   int64_t vocab;
   int k_blocks;      // of 64 hidden dimensions
   int v_tile0, v_tiles;
+  int chunk;         // blocks that a matrix instruction's accumulator adds up, 0: all
 };
 // Tiles run over the rows first, in groups of 4,096 rows (a group's hidden states and the weights in flight stay in the L2).
 template <int kCtas, int kN>
@@ -119,7 +120,7 @@ __device__ __forceinline__ void logit_tile(const LogitTiles &l, int n_rows, int6
   t.a = {l.hidden, 0, row0 + cta * 128, 64, 0, 0, 128, 0, false};
   t.b = {l.weight, 0, (int)col0 + cta * (kN / kCtas), 64, 0, 0, 128, 0, false};
   t.k_blocks = l.k_blocks;
-  t.chunk = kLogitChunk;
+  t.chunk = l.chunk;
   t.passes = 1;
   t.a_lo = t.b_lo = 0;
 }
