@@ -608,9 +608,10 @@ int fopd_head_logprob(const fopd_head *h /* HOST */, float *logprob, float *lse,
  *   d_weight        [vocab, dim] in bf16 or fp32 (d_weight_dtype) at its pitch, or NULL (not both); layout rules of weight
  *   add_d_weight    not 0: d_weight += instead of = (the sum over chunks; in fp32 best)
  *
- * G is rounded to bf16 once for the products (2^-9 of each entry at most, of the size of a bf16 result's own rounding); for
- * a d_weight in fp32 what that leaves is kept and multiplied too (2^-17), which costs that product twice.  The temporary is up to 512 MiB of G (more beyond 2^19 rows), fp32 sums of d_hidden's size or 256 MiB, and
- * with a mask a copy of the hidden states.  Outputs must not lie on inputs or on one another.
+ * G is rounded to bf16 once for the products (2^-8 of each entry at most, of the size of a bf16 result's own rounding); for
+ * a d_weight in fp32 what that leaves is kept and multiplied too (2^-17), which costs that product twice.  The temporary is up to
+ * 512 MiB of G (more beyond 2^19 rows), fp32 sums of d_hidden's size or 256 MiB, and with a mask a copy of the hidden states.
+ * Outputs must not lie on inputs or on one another.
  */
 int fopd_head_grad(const fopd_head *h /* HOST */, const float *logprob, const float *lse, const float *coef, void *d_hidden,
                    int64_t d_hidden_stride, void *d_weight, int64_t d_weight_stride, int32_t d_weight_dtype,
@@ -626,7 +627,8 @@ int fopd_head_grad(const fopd_head *h /* HOST */, const float *logprob, const fl
  * Wide, tall and square matrices, any sizes and pitches, all in one call.
  *
  * The norm is summed in fp64.  X, A and their polynomial are held in fp16 under powers of two: 11 bits, and 22 where roundings of X would be
- * amplified by 32 or more; for matrices whose result is fp32 22 throughout (three products for each).  Sums are fp32.  Results do not depend on the run.  A matrix of zeros gives zeros; one that holds an infinity or NaN
+ * amplified by 32 or more; for matrices whose result is fp32 22 throughout (three products for each).  Sums are fp32.  Results do
+ * not depend on the run.  A matrix of zeros gives zeros; one that holds an infinity or NaN
  * gives NaN and sets FOPD_DEV_NONFINITE, the others are not affected.  One whose norm is so far below eps that X's elements are
  * below 2^-39 loses them.
  */
@@ -645,8 +647,8 @@ typedef struct {
  *                  beyond 10^6.
  *   eps            >= 0, finite
  *
- * The temporary is up to eight bytes per element of the list and as many per element of the squares of the shorter sides, in groups
- * of 1 GiB or one matrix.  No
+ * The temporary is up to eight bytes per element of the list and as many per element of the squares of the shorter sides, rows and
+ * columns rounded up to 64, in groups of 1 GiB or one matrix.  No
  * result may overlap a matrix of the list or another result, as for fopd_grad_scale; in place it is allowed.
  */
 int fopd_orthogonalise(const fopd_matrix *matrices /* HOST */, int32_t n_matrices, const float *coefficients /* HOST */,

@@ -86,18 +86,6 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity,
   } while (clock64() - t0 <= limit);
   return false;
 }
-// The same for a warp whose polls should not take issue slots from its neighbours.
-__device__ __forceinline__ bool mbar_wait_bounded_sleeping(uint32_t bar, uint32_t parity, long long limit) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const long long t0 = clock64();
-  do {
-    for (int i = 0; i < kPollsPerClock; ++i) {
-      __nanosleep(64);
-      if (mbar_try_wait(bar, parity)) return true;
-    }
-  } while (clock64() - t0 <= limit);
-  return false;
-}
 __device__ __forceinline__ bool mbar_wait_cluster_bounded(uint32_t bar, uint32_t parity, long long limit) {
   if (mbar_try_wait_cluster(bar, parity)) return true;
   const long long t0 = clock64();

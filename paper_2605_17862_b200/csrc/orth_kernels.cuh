@@ -216,6 +216,8 @@ __global__ void __launch_bounds__(kOrthThreads) orth_load_kernel(const __grid_co
 // All steps of all matrices in one launch.  Tiles are numbered step by step and in a step phase by phase over the whole list; one
 // that needs the results of the phase before waits for that phase of its own matrix only, so that the tail of one matrix's phase runs
 // beside the other matrices' tiles, and a phase of a single matrix costs a signal through the L2 instead of a launch.
+// Large lists are bound by the tensor pipe (14 matrices of two blocks of width 2,048: 83 % busy, 2.75 ms); small ones by the
+// chain of three phases a step, each 6 to 16 us from the first load to the last count (256 x 1,024 in fp32: 162 us for five steps).
 enum OrthPhase { kOrthGram = 0, kOrthPoly = 1, kOrthApply = 2 };
 constexpr int kOrthMostSteps = 16;
 
@@ -242,13 +244,14 @@ struct OrthJob {
   };
   struct Ticket {
     int i;
-    int k;              // matrix
-    int step_phase;     // 4 step + phase
-    uint32_t row_col;   // tile row << 16 | tile column (2^24 rows in tiles of 256)
-    __device__ __forceinline__ int step() const { return step_phase >> 2; }
-    __device__ __forceinline__ int phase() const { return step_phase & 3; }
-    __device__ __forceinline__ int row0() const { return (int)(row_col >> 16) * kRows; }
-    __device__ __forceinline__ int col0() const { return (int)(row_col & 0xffff) * kN; }
+    int of;        // matrix, step and phase
+    int row, col;  // of the tile
+    static __device__ __forceinline__ int pack(int k, int step, int phase) { return k << 8 | step << 2 | phase; }
+    __device__ __forceinline__ int k() const { return of >> 8; }
+    __device__ __forceinline__ int step() const { return of >> 2 & 63; }
+    __device__ __forceinline__ int phase() const { return of & 3; }
+    __device__ __forceinline__ int row0() const { return row * kRows; }
+    __device__ __forceinline__ int col0() const { return col * kN; }
   };
   const Params &p;
   uint32_t staged_turn = 0;  // parity of this warp's copies into its staging buffers
@@ -265,21 +268,24 @@ struct OrthJob {
     int t = i - step * per;
     const int phase = t < p.sym_tiles ? kOrthGram : t < 2 * p.sym_tiles ? kOrthPoly : kOrthApply;
     t -= phase * p.sym_tiles;
-    o.step_phase = 4 * step + phase;
+    int k;
     const OrthMatrix *tab = p.tab.m;
     if (phase == kOrthApply) {
-      o.k = find_entry(p.tab.n, t, [&](int j) { return tab[j].x_tile; });
-      t -= tab[o.k].x_tile;
-      const int across = (tab[o.k].cp + kN - 1) / kN;
-      o.row_col = (uint32_t)(t / across) << 16 | (uint32_t)(t % across);
+      k = find_entry(p.tab.n, t, [&](int j) { return tab[j].x_tile; });
+      t -= tab[k].x_tile;
+      const int across = (tab[k].cp + kN - 1) / kN;
+      o.row = t / across;
+      o.col = t % across;
     } else {
-      o.k = find_entry(p.tab.n, t, [&](int j) { return tab[j].sym_tile; });
-      t -= tab[o.k].sym_tile;
+      k = find_entry(p.tab.n, t, [&](int j) { return tab[j].sym_tile; });
+      t -= tab[k].sym_tile;
       int r = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
       while (r * (r + 1) / 2 > t) --r;
       while ((r + 1) * (r + 2) / 2 <= t) ++r;
-      o.row_col = (uint32_t)r << 16 | (uint32_t)(t - r * (r + 1) / 2);
+      o.row = r;
+      o.col = t - r * (r + 1) / 2;
     }
+    o.of = Ticket::pack(k, step, phase);
     return o;
   }
   // Units of a matrix's tiles before this phase.
@@ -288,8 +294,8 @@ struct OrthJob {
     return kCtas * kEpilogueWarps * (o.step() * (2 * sym + x) + o.phase() * sym);
   }
   __device__ __forceinline__ bool ready(const Ticket &o, long long limit) const {
-    const int want = units_before(o, p.tab.m[o.k]);
-    const int *done = p.ws.done + o.k;
+    const int want = units_before(o, p.tab.m[o.k()]);
+    const int *done = p.ws.done + o.k();
     if (load_acquire(done) < want) {
       const long long t0 = clock64();
       while (load_acquire(done) < want)
@@ -299,7 +305,7 @@ struct OrthJob {
     return true;
   }
   __device__ __forceinline__ void tile(const Ticket &o, int cta, Tile &t) const {
-    const OrthMatrix &m = p.tab.m[o.k];
+    const OrthMatrix &m = p.tab.m[o.k()];
     const int row0 = o.row0() + cta * 128, col0 = o.col0() + cta * (kN / kCtas);
     const bool x_two = m.two_planes >> o.step() & 1;
     const int x = m.x[o.step() & 1];
@@ -314,7 +320,7 @@ struct OrthJob {
     t.a_turn = t.b_turn = {1 << 30, &p.boxes, 0, 0};
     t.a_lo = t.b_lo = 0;
     t.passes = 1;
-    t.chunk = m.full ? kOrthChunk : 0;
+    t.chunk = m.full ? kOrthChunk : kLongChunk;
     if (o.phase() == kOrthGram) {
       t.a = m.tall ? across(x, m.rp, row0, m.x_lo) : along(x, m.rp, row0, m.x_lo);
       t.b = m.tall ? across(x, m.rp, col0, m.x_lo) : along(x, m.rp, col0, m.x_lo);
@@ -381,14 +387,14 @@ struct OrthJob {
         stage(acc, 0, v, false);
         if (two) stage(acc, 1, v, true);
       }
-      order(acc, o.k, have > 0 ? y : -1, have > 0 && two ? y + lo : -1, 1);
+      order(acc, o.k(), have > 0 ? y : -1, have > 0 && two ? y + lo : -1, 1);
     } else {
       for (int plane = 0; plane < (two ? 2 : 1); ++plane) {
         if (!buffers(acc)) return false;
         if (have > 0) stage(acc, 0, v, plane);
         if (have > 1) stage(acc, 1, v + 64, plane);
         const int at = y + plane * lo;
-        order(acc, o.k, have > 0 ? at : -1, have > 1 ? at + pitch : -1, plane == (two ? 1 : 0));
+        order(acc, o.k(), have > 0 ? at : -1, have > 1 ? at + pitch : -1, plane == (two ? 1 : 0));
       }
     }
     return true;
@@ -409,17 +415,17 @@ struct OrthJob {
   __device__ __forceinline__ bool prefetch(const Ticket &o, int cta, const Accumulator &acc, long long limit) {
     if (o.phase() != kOrthPoly) return true;
     const bool ok = __all_sync(0xffffffffu, ready(o, limit)) && buffers(acc);
-    if (ok) stage_square(o, p.tab.m[o.k], cta, acc, 0);
+    if (ok) stage_square(o, p.tab.m[o.k()], cta, acc, 0);
     return ok;
   }
   __device__ __forceinline__ bool epilogue(const Ticket &o, int cta, const Accumulator &acc, float (&v)[kN / 2]) {
-    const OrthMatrix &m = p.tab.m[o.k];
+    const OrthMatrix &m = p.tab.m[o.k()];
     const int row0 = o.row0() + cta * 128 + acc.warp * 32, col0 = o.col0() + acc.half * (kN / 2);
     return o.phase() == kOrthApply ? put_x(o, m, row0, col0, acc, v) : put_square(o, m, cta, row0, col0, acc, v);
   }
   __device__ __forceinline__ bool put_x(const Ticket &o, const OrthMatrix &m, int row0, int col0, const Accumulator &acc, float (&v)[kN / 2]) {
     constexpr int kCols = kN / 2;
-    const float f = (o.step() == 0 ? p.ws.norm_factor[o.k] : 1.f) * p.step[o.step()].apply * (last(o) ? m.scale : 1.f);
+    const float f = (o.step() == 0 ? p.ws.norm_factor[o.k()] : 1.f) * p.step[o.step()].apply * (last(o) ? m.scale : 1.f);
 #pragma unroll
     for (int j = 0; j < kCols; ++j) v[j] *= f;
     if (last(o)) {
@@ -429,11 +435,13 @@ struct OrthJob {
       if (m.out_dtype == FOPD_F32) {
 #pragma unroll
         for (int c = 0; c < kCols; c += 32)
-          put_rows_out<FOPD_F32>(acc.staging, acc.lane, v + c, static_cast<float *>(m.out) + at + c, m.out_pitch, rows, min(32, m.cols - col0 - c), false);
+          put_rows_out<FOPD_F32>(acc.staging, acc.lane, v + c, static_cast<float *>(m.out) + at + c, m.out_pitch, rows,
+                                 min(32, m.cols - col0 - c), false);
       } else {
 #pragma unroll
         for (int c = 0; c < kCols; c += 64)
-          put_rows_out<FOPD_BF16>(acc.staging, acc.lane, v + c, static_cast<__nv_bfloat16 *>(m.out) + at + c, m.out_pitch, rows, min(64, m.cols - col0 - c), false);
+          put_rows_out<FOPD_BF16>(acc.staging, acc.lane, v + c, static_cast<__nv_bfloat16 *>(m.out) + at + c, m.out_pitch, rows,
+                                  min(64, m.cols - col0 - c), false);
       }
       return true;
     }
@@ -447,7 +455,7 @@ struct OrthJob {
     const int panels = square_panels(m, row0, col0);
     float f = step.poly_c;
     if (o.phase() == kOrthGram) {
-      const float s = o.step() == 0 ? p.ws.norm_factor[o.k] : 1.f;
+      const float s = o.step() == 0 ? p.ws.norm_factor[o.k()] : 1.f;
       f = step.gram * s * s;
     }
 #pragma unroll

@@ -6,14 +6,16 @@
 // (four) accumulators in TMEM; warps 4 to 11 take a finished accumulator into registers, hand it back and work on from
 // there, beside the next products.  With kCtas = 2 a pair of CTAs works on one tile: each holds half of both operands and half the
 // accumulator's rows, and shared memory is read once for twice the products (cta_group::2; 64 instead of 96 bytes per SM and
-// cycle at 256 columns, which with the copies coming in is what 1-CTA tiles are short of).
+// cycle at 256 columns, which with the copies coming in is what 1-CTA tiles are short of: 14 matrices of width 2,048 take 3.3 ms in
+// tiles of 256 x 256 on pairs, 4.0 ms in tiles of 128 x 128).  Bound by the tensor pipe: 96 % busy at 4,096 x 151,936 x 2,048, at the
+// 1.38 GHz that the power cap leaves.
 //
 // Operands are 16-bit (both bf16 or both fp16), products and sums fp32.  Either operand may lie with the contraction along
-// its rows ("K-major") or across them; both come in boxes of 64 rows x 64 elements, so that one tensor map serves both.
+// its rows ("K-major") or across them; both come in boxes of 64 elements to a row, so that nothing is ever transposed.
 //
 // A matrix instruction does not round what it adds to the accumulator, it cuts it off: over K terms sums come out smaller by up to
 // K / 16 units of 2^-24.  A tile may therefore have its accumulator taken out every `chunk` blocks and added up in registers,
-// rounded to nearest; what that costs is hidden behind the products (at 8 blocks no difference in time was measured).
+// rounded to nearest: every eight blocks takes 1.5 % more time (the same case) and an error of 2.6e-7 instead of 1.2e-6.
 //
 // Every wait is bounded.  One that runs out raises a flag, the role leaves its loop, the others run out in turn, copies and
 // products in flight are waited for (again with a limit), TMEM is given back, FOPD_DEV_TIMEOUT goes to the status word.
@@ -66,9 +68,6 @@ __device__ __forceinline__ void tma_store_wait_read() {
 }
 __device__ __forceinline__ void tma_store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
-  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
-}
 
 // ------------------------------------------------------------------ TMEM and tcgen05
 template <int kCtas>
@@ -189,18 +188,20 @@ struct Turn {
   int y, cy;   // as in Operand, with x = kx = cx = 0 and ky = 64; y for block 0
 };
 
+constexpr int kLongChunk = 256;  // blocks to an accumulator also where results are bf16: what 16,384 terms lose is below 2^-14
+
 // The contraction may run over several pairs of planes: pass i takes a's second plane where bit i of a_lo is set, etc.
 struct Tile {
   Operand a, b;
   Turn a_turn, b_turn;  // where the job has symmetric operands
   int k_blocks;  // 0: the product is zero
-  int chunk;     // blocks (of all passes) to an accumulator, 0: all
+  int chunk;     // blocks (of all passes) to an accumulator
   int passes;    // all but the last are small terms: where sums are taken out, one accumulator holds all of those
   uint32_t a_lo, b_lo;
 };
 
 __device__ __forceinline__ int first_chunk(const Tile &t) {
-  return t.chunk > 0 ? (t.passes > 1 ? (t.passes - 1) * t.k_blocks : min(t.chunk, t.k_blocks)) : t.passes * t.k_blocks;
+  return t.passes > 1 ? (t.passes - 1) * t.k_blocks : min(t.chunk, t.k_blocks);
 }
 __device__ __forceinline__ uint64_t smem_descriptor(uint32_t addr) {
   // 128-byte swizzle: groups of 8 rows of 128 bytes, 1,024 bytes apart; across: 64 rows further is the next box (along, this is not
@@ -307,7 +308,8 @@ struct TileFeed {
   uint32_t n = 0;
   bool ok = true;
   using Ticket = typename Job::Ticket;
-  __device__ TileFeed(ProductShared &s, int c, int64_t tiles) : sh(s), cta(c), n_tiles(tiles), step(gridDim.x / kCtas), i((int64_t)(blockIdx.x / kCtas) - step) {}
+  __device__ TileFeed(ProductShared &s, int c, int64_t tiles)
+      : sh(s), cta(c), n_tiles(tiles), step(gridDim.x / kCtas), i((int64_t)(blockIdx.x / kCtas) - step) {}
   // (by all lanes of a warp) the next claimed tile; `asked` is what the elected lane got from the counter, -1 if it has yet to ask
   __device__ __forceinline__ Ticket next_claimed(const Job &job, bool elected, int asked) {
     const uint32_t slot = n % kFeed;
@@ -507,7 +509,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         uint32_t idesc = idesc0 | ((uint32_t)t.a.across << 15) | ((uint32_t)t.b.across << 16);
         uint32_t a_step = t.a.across ? kAcross : kAlong, b_step = t.b.across ? kAcross : kAlong;
         const uint64_t a0 = smem_descriptor(base), b0 = smem_descriptor(base + Shape::kABoxes * kBoxBytes);
-        const int blocks = t.passes * t.k_blocks, chunk = t.chunk > 0 ? t.chunk : blocks;
+        const int blocks = t.passes * t.k_blocks, chunk = t.chunk;
         int end = first_chunk(t);
         int in_pass = 0;
         int done = 0;
@@ -601,7 +603,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         job.tile(ticket, cta, t);
         blocks = t.passes * t.k_blocks;
         done = first_chunk(t);
-        chunk = t.chunk > 0 ? t.chunk : blocks;
+        chunk = t.chunk;
       }
       if constexpr (Job::kClaimed) {
         if (!(ok = job.prefetch(ticket, cta, acc, kLimit))) break;

@@ -148,9 +148,11 @@ class HeadChunk:
 
 
 def supervised_step(chunks, weight, d_weight, *, clip=None, update=None, status=None, stream=None):
-    """The gradient of -sum coef log p(token) through the vocabulary head without its logits: log-probs and gradients chunk by
+    """The gradient of -sum coef log p(token) through the vocabulary head without its logits (of one chunk or
+    more): log-probs and gradients chunk by
     chunk, the weights' gradient added up over the chunks (in fp32 best), then ``clip`` (a GradientClip) and ``update`` (an
     Orthogonalise) where given, as a rule over d_weight and the model's other gradients."""
+    assert len(chunks) > 0  # (the first sets d_weight)
     for j, ch in enumerate(chunks):
         fb.fopd_head_logprob(ch.hidden, weight, ch.tokens, ch.logprob, lse=ch.lse, mask=ch.mask, status=status, stream=stream)
         fb.fopd_head_grad(ch.hidden, weight, ch.tokens, ch.logprob, ch.lse, ch.coef, d_hidden=ch.d_hidden, d_weight=d_weight,

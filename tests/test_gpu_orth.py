@@ -89,6 +89,16 @@ def test_few_tiles_with_long_products(shape, din, dout):
     check(other, more[1])
 
 
+@pytest.mark.parametrize("shape", [(8_400_321, 2), (2, 8_400_321)])
+def test_more_tiles_along_a_side_than_sixteen_bits_count(shape):
+    M = matrix(*shape, seed=3, dtype=BF16, strong=False)
+    out = torch.full(shape, 7.0, device=DEV, dtype=BF16)
+    run([M], [out])
+    check(M, out)
+    want = oo.orthogonalise(M, FIVE)  # (sums over millions of rows lose no more than a bf16 rounding: they are taken out every 16,384)
+    assert float((out.double() - want).norm()) <= 2.0 ** -8 * float(want.norm())
+
+
 def test_results_are_near_orthogonal():
     """What it is for: singular values end up in [0.68, 1.21] (five steps reach 0.68 from 0.0035 up), directions stay."""
     M = matrix(300, 500, 3, F32, strong=False)
