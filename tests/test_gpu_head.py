@@ -259,6 +259,59 @@ def test_more_rows_than_are_kept_at_a_time(masked):
     check_logprob(h, w, y, mask)
 
 
+def test_weights_of_more_than_two_to_the_31_elements():
+    n, V, D = 3, 1_100_003, 2048
+    g = torch.Generator(device=DEV).manual_seed(9)
+    w = torch.empty((V, D), device=DEV, dtype=torch.bfloat16)
+    for at in range(0, V, 1 << 16):
+        w[at:at + (1 << 16)] = torch.randn(w[at:at + (1 << 16)].shape, generator=g, device=DEV) * (2 / math.sqrt(D))
+    h = torch.randn((n, D), generator=g, device=DEV).bfloat16()
+    y = torch.tensor([0, V - 1, V // 2], dtype=torch.int32, device=DEV)
+    c = torch.tensor([1.0, -0.5, 2.0], device=DEV)
+    lp, lse, status = logprob(h, w, y)
+    z = torch.cat([h.double() @ w[at:at + (1 << 16)].double().t() for at in range(0, V, 1 << 16)], 1)
+    lse64 = torch.logsumexp(z, 1)
+    lp64 = z.gather(1, y.long().unsqueeze(1)).squeeze(1) - lse64
+    assert status == 0 and float((lse.double() - lse64).abs().max()) < 1e-5 and float((lp.double() - lp64).abs().max()) < 1e-5
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    fb.fopd_head_grad(h, w, y, lp, lse, c, d_hidden=dh, d_weight=dw)
+    G = torch.softmax(z, 1)
+    G[torch.arange(n, device=DEV), y.long()] -= 1
+    G *= c.double().unsqueeze(1)
+    want = sum(G[:, at:at + (1 << 16)] @ w[at:at + (1 << 16)].double() for at in range(0, V, 1 << 16))
+    assert float((dh.double() - want).norm()) <= 2.0 ** -8 * float(want.norm())
+    for rows in (slice(0, 300), slice(V // 2 - 100, V // 2 + 100), slice(V - 300, V)):
+        want = G[:, rows].t() @ h.double()
+        assert float((dw[rows].double() - want).norm()) <= 2.0 ** -7 * float(want.norm())
+
+
+def test_hidden_states_of_more_than_two_to_the_31_elements():
+    n, V, D = 1_100_003, 200, 2048
+    g = torch.Generator(device=DEV).manual_seed(10)
+    h = torch.empty((n, D), device=DEV, dtype=torch.bfloat16)
+    for at in range(0, n, 1 << 16):
+        h[at:at + (1 << 16)] = torch.randn(h[at:at + (1 << 16)].shape, generator=g, device=DEV)
+    w = (torch.randn((V, D), generator=g, device=DEV) * (2 / math.sqrt(D))).bfloat16()
+    y = torch.randint(0, V, (n,), generator=g, device=DEV, dtype=torch.int32)
+    c = torch.rand(n, generator=g, device=DEV) / n
+    lp, lse, status = logprob(h, w, y)
+    dh, dw = torch.empty_like(h), torch.empty((V, D), device=DEV)
+    fb.fopd_head_grad(h, w, y, lp, lse, c, d_hidden=dh, d_weight=dw)
+    total = torch.zeros((V, D), dtype=torch.float64, device=DEV)
+    for at in range(0, n, 1 << 16):
+        rows = slice(at, at + (1 << 16))
+        hh, yy = h[rows].double(), y[rows].long().unsqueeze(1)
+        lp64 = torch.log_softmax(hh @ w.double().t(), 1)
+        assert float((lp[rows].double() - lp64.gather(1, yy).squeeze(1)).abs().max()) < 1e-5
+        G = lp64.exp()
+        G.scatter_add_(1, yy, torch.full_like(yy, -1.0, dtype=torch.float64))
+        G *= c[rows].double().unsqueeze(1)
+        want = G @ w.double()
+        assert float((dh[rows].double() - want).norm()) <= 2.0 ** -8 * float(want.norm())
+        total += G.t() @ hh
+    assert status == 0 and float((dw.double() - total).norm()) <= 2.0 ** -13 * float(total.norm())
+
+
 def test_gradient_against_differences():
     """Central differences of the loss -sum coef logprob computed by the forward call itself along random directions."""
     n, V, D = 40, 500, 64
