@@ -144,7 +144,7 @@ OrthMatrix describe(const fopd_matrix &m, const Scales &s, int32_t steps) {
 struct Group {
   OrthWorkspace ws;
   CUtensorMap boxes, boxes_along, rows_out;
-  int norm_blocks, load_blocks;
+  int norm_blocks, load_blocks, norm_chunk, load_cols;
   int64_t sym_tiles, x_tiles;
   bool pairs;  // tiles of 256 x 256 on pairs of CTAs
 };
@@ -153,6 +153,8 @@ int run_table(const std::vector<OrthMatrix> &g, const Group &o, const Scales &s,
               cudaStream_t st) {
   OrthTable<N> tab;
   tab.n = (int)g.size();
+  tab.norm_chunk = o.norm_chunk;
+  tab.load_cols = o.load_cols;
   std::copy(g.begin(), g.end(), tab.m);
   int rc = launch_early(orth_norm_kernel<N>, dim3((unsigned)o.norm_blocks), kOrthThreads, st, tab, o.ws);
   if (rc == FOPD_OK) rc = launch_early(orth_load_kernel<N>, dim3((unsigned)o.load_blocks), kOrthThreads, st, tab, o.ws, eps, status);
@@ -201,16 +203,21 @@ bool pairs_pay(const std::vector<OrthMatrix> &g, int sms) {
 int run_group(std::vector<OrthMatrix> &g, const Scales &s, int32_t steps, float eps, int32_t *status, int sms, cudaStream_t st) {
   // the largest first: their phases take longest, and the small ones' tiles fill what is left
   std::stable_sort(g.begin(), g.end(), [](const OrthMatrix &a, const OrthMatrix &b) { return (int64_t)a.rp * a.cp > (int64_t)b.rp * b.cp; });
+  // (short lists in small blocks: their norm and load are latencies)
+  int64_t elements = 0;
+  for (const OrthMatrix &m : g) elements += (int64_t)m.rows * m.cols;
+  const bool small = elements < (int64_t)1 << 22;
+  const int norm_chunk = small ? 4096 : 16384, load_cols = small ? 64 : 256;
   int64_t at = 0, norm_blocks = 0, load_blocks = 0;
   for (size_t i = 0; i < g.size(); ++i) {
     OrthMatrix &m = g[i];
     m.x[0] += (int)at, m.x[1] += (int)at, m.a += (int)at, m.p += (int)at;
     at += m.space;
     m.norm_block = (int)norm_blocks;
-    m.norm_blocks = (int)(((int64_t)m.rows * m.cols + kNormChunk - 1) / kNormChunk);
+    m.norm_blocks = (int)(((int64_t)m.rows * m.cols + norm_chunk - 1) / norm_chunk);
     norm_blocks += m.norm_blocks;
     m.load_block = (int)load_blocks;
-    load_blocks += (int64_t)(m.rp / 64) * ((m.cp + kLoadCols - 1) / kLoadCols);
+    load_blocks += (int64_t)(m.rp / 64) * ((m.cp + load_cols - 1) / load_cols);
   }
   const int tile = pairs_pay(g, sms) ? 256 : 128;
   int64_t sym_tiles = 0, x_tiles = 0;
@@ -232,6 +239,8 @@ int run_group(std::vector<OrthMatrix> &g, const Scales &s, int32_t steps, float 
           reinterpret_cast<__half *>(base + planes)};
   o.norm_blocks = (int)norm_blocks;
   o.load_blocks = (int)load_blocks;
+  o.norm_chunk = norm_chunk;
+  o.load_cols = load_cols;
   o.sym_tiles = sym_tiles;
   o.x_tiles = x_tiles;
   o.pairs = tile == 256;

@@ -37,10 +37,8 @@ struct OrthMatrix {
   uint8_t dtype, out_dtype, tall, full;
 };
 
-constexpr int kNormChunk = 16384;  // elements to a block
 constexpr int kOrthThreads = 256;
 constexpr int kOrthChunk = 2;       // blocks of 64 that an accumulator adds up where the result is fp32
-constexpr int kLoadCols = 256;     // a block of the load takes 64 rows of these
 
 struct OrthWorkspace {
   float *norm_factor;  // per matrix: 1 / ((|M| + eps) 2^e)
@@ -54,6 +52,8 @@ struct OrthWorkspace {
 template <int N>
 struct OrthTable {
   int n;
+  int norm_chunk;  // elements to a block of the norm
+  int load_cols;   // columns, by 64 rows, to a block of the load
   OrthMatrix m[N];
 };
 
@@ -84,15 +84,15 @@ __device__ __forceinline__ double block_sum(double s, double *scratch) {
   return t;
 }
 
-// Sums of squares in fp64, a block to 16,384 elements.
+// Sums of squares in fp64, a block to 16,384 elements (4,096 for short lists).
 template <int N>
 __global__ void __launch_bounds__(kOrthThreads) orth_norm_kernel(const __grid_constant__ OrthTable<N> tab, OrthWorkspace ws) {
   __shared__ double scratch[kOrthThreads / 32];
   grid_wait();
   const int k = find_entry(tab.n, (int)blockIdx.x, [&](int j) { return tab.m[j].norm_block; });
   const OrthMatrix &m = tab.m[k];
-  const int64_t all = (int64_t)m.rows * m.cols, from = (int64_t)((int)blockIdx.x - m.norm_block) * kNormChunk;
-  const int64_t to = from + kNormChunk < all ? from + kNormChunk : all;
+  const int64_t all = (int64_t)m.rows * m.cols, from = (int64_t)((int)blockIdx.x - m.norm_block) * tab.norm_chunk;
+  const int64_t to = from + tab.norm_chunk < all ? from + tab.norm_chunk : all;
   double s = 0.0;
   const int size = m.dtype == FOPD_BF16 ? 2 : 4, per = 16 / size;
   const bool dense = m.rows == 1 || m.pitch == m.cols;
@@ -135,7 +135,7 @@ __device__ __forceinline__ void split_half(float x, __half &hi, __half &lo) {
 }
 
 // Into the workspace times 2^e, with 2^e |M| in [2^14, 2^15): no element leaves fp16's range, and bf16 ones are exact down to 2^-24.
-// A block takes 64 rows x 256 columns and forms the norm from the partial sums itself (in order).
+// A block takes 64 rows x 256 columns (64 for short lists) and forms the norm from the partial sums itself (in order).
 template <int N>
 __global__ void __launch_bounds__(kOrthThreads) orth_load_kernel(const __grid_constant__ OrthTable<N> tab, OrthWorkspace ws, float eps,
                                                                  int32_t *status) {
@@ -171,15 +171,15 @@ __global__ void __launch_bounds__(kOrthThreads) orth_load_kernel(const __grid_co
   __syncthreads();
   const double scale = scale_of_block;
   const int e = exponent_of_block;
-  const int col_blocks = (m.cp + kLoadCols - 1) / kLoadCols;
-  const int row0 = block / col_blocks * 64, col0 = block % col_blocks * kLoadCols;
+  const int col_blocks = (m.cp + tab.load_cols - 1) / tab.load_cols;
+  const int row0 = block / col_blocks * 64, col0 = block % col_blocks * tab.load_cols;
   const int size = m.dtype == FOPD_BF16 ? 2 : 4;
   const bool two = m.two_planes & 1;
   const bool aligned = (((uintptr_t)m.data | (uintptr_t)(m.rows > 1 ? m.pitch * size : 0)) & 15) == 0;
   const float f = (float)scale;  // (2^e may be beyond fp32 for the smallest matrices: then in fp64)
   const bool in_range = e > -126 && e < 126;
 #pragma unroll 4
-  for (int u = threadIdx.x; u < 64 * (kLoadCols / 8); u += kOrthThreads) {
+  for (int u = threadIdx.x; u < 64 * (tab.load_cols / 8); u += kOrthThreads) {
     const int c = col0 + (u / 64 / 8) * 64 + (u & 7) * 8, r = row0 + ((u >> 3) & 63);
     if (c >= m.cp) continue;
     float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
