@@ -58,7 +58,9 @@
  *     its first call, with a lock that lets one host-buffer step run at a time
  *     per device; fopd_release_device_memory destroys them;
  *   - the fixed scratch array of fopd_token_stats_static and its cached device
- *     address per device.
+ *     address per device;
+ *   - for fopd_head_* and fopd_orthogonalise: the number of SMs per device, that a kernel's
+ *     shared memory has been set, and the address of the driver's call that makes tensor maps.
  * Calls with disjoint buffers may run concurrently from several host threads
  * and on several streams.
  *
