@@ -226,7 +226,7 @@ int run_grad(const fopd_head *h, const float *logprob, const float *lse, const f
     for (int64_t v0 = 0; rc == FOPD_OK && v0 < h->vocab; v0 += piece) {
       const int64_t count = h->vocab - v0 < piece ? h->vocab - v0 : piece;
       // (for bf16 gradients the logits' own last bits do not show: one accumulator)
-      g.l = {nullptr, nullptr, pre.rows, h->vocab, (int)((h->dim + 63) / 64), (int)(v0 / kN), (int)((count + kN - 1) / kN), lo ? kLogitChunk : kLongChunk};
+      g.l = {nullptr, nullptr, pre.rows, h->vocab, (int)((h->dim + 63) / 64), (int)(v0 / kN), (int)((count + kN - 1) / kN), lo ? kGradChunk : kLongChunk};
       q.v0 = v0;
       q.v_count = (int)count;
       q.first = v0 == 0;

@@ -88,7 +88,8 @@ __global__ void __launch_bounds__(kCompactThreads) head_compact_kernel(const uin
 }
 
 // ------------------------------------------------------------------ tiles of logits
-constexpr int kLogitChunk = 8;  // for logits whose error is to stay that of fp32 sums: 512 dimensions
+constexpr int kLogitChunk = 8;   // for logits whose error is to stay that of fp32 sums: 512 dimensions
+constexpr int kGradChunk = 16;   // for those behind a weights' gradient in fp32, next to the 2^-17 that two planes leave
 struct LogitTiles {
   const CUtensorMap *hidden, *weight;
   HeadRows rows;
@@ -145,7 +146,7 @@ struct LogprobJob {
   };
   const Params &p;
   LogitTiles l;
-  int n;
+  int n, y = -1;  // this thread's row's token
   __device__ explicit LogprobJob(const Params &params) : p(params), l(params.l), n(params.l.rows.count()) {
     l.hidden = &p.hidden;
     l.weight = &p.weight;
@@ -153,6 +154,13 @@ struct LogprobJob {
   __device__ int64_t tiles() const { return logit_tiles<kCtas, kN>(l, n); }
   __device__ int32_t *status() const { return p.status; }
   __device__ __forceinline__ void tile(Ticket ticket, int cta, Tile &t) const { logit_tile<kCtas, kN>(l, n, ticket.i, cta, t); }
+  __device__ __forceinline__ void prefetch(Ticket ticket, int cta, const Accumulator &acc) {
+    int row0;
+    int64_t v0;
+    logit_tile_at<kCtas, kN>(l, n, ticket.i, row0, v0);
+    const int row = row0 + cta * 128 + acc.warp * 32 + acc.lane;
+    y = row < n ? p.tokens[l.rows.row(row)] : -1;
+  }
   __device__ __forceinline__ void epilogue(Ticket ticket, int cta, const Accumulator &acc, float (&z)[kN / 2]) const {
     constexpr int kCols = kN / 2;
     int row0;
@@ -160,7 +168,6 @@ struct LogprobJob {
     logit_tile_at<kCtas, kN>(l, n, ticket.i, row0, v0);
     v0 += acc.half * kCols;
     const int row = row0 + cta * 128 + acc.warp * 32 + acc.lane;
-    const int y = row < n ? p.tokens[l.rows.row(row)] : -1;
     if (v0 + kCols > l.vocab) {
       const int have = (int)max((int64_t)0, l.vocab - v0);
 #pragma unroll
@@ -262,6 +269,8 @@ struct GradLogitsJob {
   LogitTiles l;
   int n;
   Staging staging;
+  int y = -1;  // this thread's row: token, lse, coefficient, entry of G at the token
+  float lse = 0.f, coef = 0.f, at_token = 0.f;
   __device__ explicit GradLogitsJob(const Params &params) : p(params), l(params.l), n(params.l.rows.count()) {
     l.hidden = &p.hidden;
     l.weight = &p.weight;
@@ -269,6 +278,25 @@ struct GradLogitsJob {
   __device__ int64_t tiles() const { return logit_tiles<kCtas, kN>(l, n); }
   __device__ int32_t *status() const { return p.status; }
   __device__ __forceinline__ void tile(Ticket ticket, int cta, Tile &t) const { logit_tile<kCtas, kN>(l, n, ticket.i, cta, t); }
+  __device__ __forceinline__ void prefetch(Ticket ticket, int cta, const Accumulator &acc) {
+    int row0;
+    int64_t v0;
+    logit_tile_at<kCtas, kN>(l, n, ticket.i, row0, v0);
+    const int row = row0 + cta * 128 + acc.warp * 32 + acc.lane;
+    lse = coef = at_token = 0.f;
+    y = -1;
+    if (row >= n) return;
+    const int r = l.rows.row(row), token = p.tokens[r];
+    const float c = p.coef[r], lp = p.logprob[r], z = p.lse[r];
+    if (token >= 0 && token < l.vocab) {
+      y = token;
+      lse = z;
+      coef = c;
+      at_token = c * expm1f(lp);  // p - 1 without the cancellation
+    } else if (p.status && v0 == 0 && acc.half == 0) {
+      atomicOr(p.status, FOPD_DEV_BAD_TOKEN);
+    }
+  }
   __device__ __forceinline__ void epilogue(Ticket ticket, int cta, const Accumulator &acc, float (&g)[kN / 2]) {
     constexpr int kCols = kN / 2;
     int row0;
@@ -276,24 +304,12 @@ struct GradLogitsJob {
     logit_tile_at<kCtas, kN>(l, n, ticket.i, row0, v0);
     v0 += acc.half * kCols;
     row0 += cta * 128 + acc.warp * 32;
-    const int row = row0 + acc.lane;
-    float lse = 0.f, coef = 0.f, at_token = 0.f;
-    int y = -1;
-    if (row < n) {
-      const int r = l.rows.row(row);
-      y = p.tokens[r];
-      if (y >= 0 && y < l.vocab) {
-        lse = p.lse[r];
-        coef = p.coef[r];
-        at_token = coef * expm1f(p.logprob[r]);  // p - 1 without the cancellation
-      } else {
-        y = -1;
-        if (p.status && v0 == 0) atomicOr(p.status, FOPD_DEV_BAD_TOKEN);
-      }
-    }
+    // coef e^{z - lse} with the exponent in one fused multiply-add; the rounding of lse log2(e), the same for the whole row, goes into the
+    // coefficient.  Rows without one: an exponential of zero.
     const bool live = coef != 0.f;
+    const float c = live ? lse * kLog2e : 1e30f, scale = live ? coef * (1.f - fmaf(lse, kLog2e, -c) * kLn2) : 0.f;
 #pragma unroll
-    for (int j = 0; j < kCols; ++j) g[j] = live ? coef * ex2((g[j] - lse) * kLog2e) : 0.f;
+    for (int j = 0; j < kCols; ++j) g[j] = scale * ex2(fmaf(g[j], kLog2e, -c));
     const int64_t mine = (int64_t)y - v0;
     if (live && mine >= 0 && mine < kCols) {
       const int at = (int)mine;
@@ -401,6 +417,7 @@ struct HeadGradsJob {
     }
     t.b_lo = 0;
   }
+  __device__ __forceinline__ void prefetch(Ticket, int, const Accumulator &) const {}
   __device__ __forceinline__ void epilogue(Ticket ticket, int cta, const Accumulator &acc, float (&g)[kN / 2]) {
     int split, row0, d0;
     at(ticket.i, split, row0, d0);

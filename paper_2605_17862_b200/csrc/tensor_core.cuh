@@ -371,10 +371,11 @@ struct TileFeed {
 };
 
 // Job: Params (a kernel parameter); Job(params); Ticket; int64_t tiles(); void tile(ticket, int cta, Tile &);
+// void prefetch(ticket, int cta, const Accumulator &), what an epilogue warp asks for while the products run;
 // void epilogue(ticket, int cta, const Accumulator &, float (&v)[kN / 2]); int32_t *status(); static constexpr bool kFp16, kTurns (it has
 // symmetric operands), kClaimed; and where that is true int *counter(), Ticket ticket(i), bool ready(ticket, limit), which returns
-// when what the tile reads is there, bool prefetch(ticket, cta, acc, limit), what an epilogue warp asks for beforehand, bool finish(acc),
-// what it does at the end (epilogue is bool then; false: a wait ran out), and store_map() and done_counts() for the storing thread.
+// when what the tile reads is there, bool finish(acc), what an epilogue warp does at the end
+// (prefetch, which gets the limit too, and epilogue are bool then; false: a wait ran out), and store_map() and done_counts() for the storing thread.
 struct TileNumber {
   int64_t i;
 };
@@ -607,6 +608,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       }
       if constexpr (Job::kClaimed) {
         if (!(ok = job.prefetch(ticket, cta, acc, kLimit))) break;
+      } else {
+        job.prefetch(ticket, cta, acc);
       }
       if (!wait()) break;
       float v[kN / 2];
