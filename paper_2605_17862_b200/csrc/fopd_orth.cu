@@ -118,7 +118,9 @@ OrthMatrix describe(const fopd_matrix &m, const Scales &s, int32_t steps) {
   o.scale = m.scale;
   o.dtype = (uint8_t)m.dtype;
   o.out_dtype = (uint8_t)m.out_dtype;
-  o.full = m.out_dtype == FOPD_F32;
+  // (also where a few numbers carry the whole result: the roundings of a 2 x 31 matrix do not average out, and a singular value that
+  // passes 1.15 on its way makes three times of them; 0.9 % of such a result, and one block more or less of the contraction)
+  o.full = m.out_dtype == FOPD_F32 || (std::min(m.rows, m.cols) <= 16 && std::max(m.rows, m.cols) <= 256);
   const uint32_t all = (1u << steps) - 1;
   o.two_planes = o.full ? all : s.loud & all;
   if (m.dtype == FOPD_BF16) o.two_planes &= ~1u;  // (bf16 values are whole in the first plane)

@@ -9,7 +9,8 @@
 // stand above the others, as 10 % and more.  So X, A and P are held in fp16 under powers of two that keep them just below its largest
 // number (11 bits, everything down to 2^-29 of the largest normal): an eighth of bf16's rounding at the same rate.  X has a second
 // plane of what the rounding left (together 22 bits) while the steps still ahead amplify by 32 or more, and P X then takes both; the
-// rounding of A and P is harmless, as it multiplies what is there.  Results in fp32 have two planes throughout, three products each.
+// rounding of A and P is harmless, as it multiplies what is there.  Results in fp32, and matrices of a few numbers, have two planes
+// throughout, three products each.
 // The scales follow from a bound on the largest singular value in each step, which the host takes from the coefficients.
 //
 // Everything lies in one workspace in panels of 64 columns ([panel][rows][64], rows and columns padded with zeros to 64), so that one
