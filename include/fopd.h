@@ -628,17 +628,18 @@ int fopd_head_grad(const fopd_head *h /* HOST */, const float *logprob, const fl
  * takes the orthogonal factor of its momentum for the update; customary are five steps of (3.4445, -4.7750, 2.0315), eps = 1e-7).
  * Wide, tall and square matrices, any sizes and pitches, all in one call.
  *
- * The norm is summed in fp64.  X, A and their polynomial are held in fp16 under powers of two: 11 bits, and 22 where roundings of X would be
- * amplified by 32 or more; for matrices whose result is fp32, and those of up to
- * 16 x 256, 22 throughout (three products for each).  Sums are fp32.  Results do
- * not depend on the run.  A matrix of zeros gives zeros; one that holds an infinity or NaN
- * gives NaN and sets FOPD_DEV_NONFINITE, the others are not affected.  One whose norm is so far below eps that X's elements are
- * below 2^-39 loses them.
+ * The norm is summed in fp64.  X, A and their polynomial are held in fp16 under powers of two: 11 bits, and 22 where
+ * roundings of X would be amplified by 32 or more; for matrices whose result is fp32, and those of up to 16 x 256, 22
+ * throughout (three products for each).  Sums are fp32.  Results do not depend on the run (their last bits may on what else is
+ * in the list: it decides the size of tiles).  A matrix of zeros gives zeros; one that holds an infinity or NaN gives NaN and
+ * sets FOPD_DEV_NONFINITE, the others are not affected.  One whose norm is so far below eps that X's elements are below 2^-39
+ * loses them.
  */
 typedef struct {
   const void *data;     /* [rows, cols] at a pitch of row_stride elements; aligned to its element          */
   void *out;            /* where the result goes, at out_stride; may be data with the same type and pitch   */
-  int64_t rows, cols;   /* <= 2^24 each; or 0: nothing is done                                               */
+  int64_t rows, cols;   /* <= 2^24 each, and together with the square of the smaller, rounded up to 64, <= 2^34;
+                           or 0: nothing is done                                                             */
   int64_t row_stride, out_stride; /* >= cols where rows > 1                                                  */
   float scale;          /* of the result, finite                                                             */
   int32_t dtype, out_dtype; /* fopd_dtype, matrix by matrix                                                  */
@@ -651,8 +652,8 @@ typedef struct {
  *   eps            >= 0, finite
  *
  * The temporary is up to eight bytes per element of the list and as many per element of the squares of the shorter sides, rows and
- * columns rounded up to 64, in groups of 1 GiB or one matrix.  No
- * result may overlap a matrix of the list or another result, as for fopd_grad_scale; in place it is allowed.
+ * columns rounded up to 64, in groups of 1 GiB or one matrix.  No result may overlap a matrix of the list or another result, as
+ * for fopd_grad_scale; in place it is allowed.
  */
 int fopd_orthogonalise(const fopd_matrix *matrices /* HOST */, int32_t n_matrices, const float *coefficients /* HOST */,
                        int32_t steps, float eps, int32_t *status, void *stream);
