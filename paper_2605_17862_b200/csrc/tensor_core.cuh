@@ -24,6 +24,7 @@
 #include <cuda.h>
 #include <cuda_fp16.h>
 
+#include "accumulators.cuh"
 #include "async.cuh"
 #include "common.cuh"
 
@@ -188,21 +189,17 @@ struct Turn {
   int y, cy;   // as in Operand, with x = kx = cx = 0 and ky = 64; y for block 0
 };
 
-constexpr int kLongChunk = 256;  // blocks to an accumulator also where results are bf16: what 16,384 terms lose is below 2^-14
-
 // The contraction may run over several pairs of planes: pass i takes a's second plane where bit i of a_lo is set, etc.
 struct Tile {
   Operand a, b;
   Turn a_turn, b_turn;  // where the job has symmetric operands
   int k_blocks;  // 0: the product is zero
-  int chunk;     // blocks (of all passes) to an accumulator
-  int passes;    // all but the last are small terms: where sums are taken out, one accumulator holds all of those
+  int chunk;     // blocks of the last pass to an accumulator, at most kLongChunk
+  int passes;    // all but the last are small terms, kLongChunk blocks to an accumulator
   uint32_t a_lo, b_lo;
 };
 
-__device__ __forceinline__ int first_chunk(const Tile &t) {
-  return t.passes > 1 ? (t.passes - 1) * t.k_blocks : min(t.chunk, t.k_blocks);
-}
+__device__ __forceinline__ int small_blocks(const Tile &t) { return (t.passes - 1) * t.k_blocks; }
 __device__ __forceinline__ uint64_t smem_descriptor(uint32_t addr) {
   // 128-byte swizzle: groups of 8 rows of 128 bytes, 1,024 bytes apart; across: 64 rows further is the next box (along, this is not
   // looked at)
@@ -510,8 +507,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         uint32_t idesc = idesc0 | ((uint32_t)t.a.across << 15) | ((uint32_t)t.b.across << 16);
         uint32_t a_step = t.a.across ? kAcross : kAlong, b_step = t.b.across ? kAcross : kAlong;
         const uint64_t a0 = smem_descriptor(base), b0 = smem_descriptor(base + Shape::kABoxes * kBoxBytes);
-        const int blocks = t.passes * t.k_blocks, chunk = t.chunk;
-        int end = first_chunk(t);
+        const int blocks = t.passes * t.k_blocks, small = small_blocks(t), chunk = t.chunk;
+        int end = accumulator_end(0, small, blocks, chunk);
         int in_pass = 0;
         int done = 0;
         do {
@@ -553,7 +550,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             turn ^= 1;
           }
           done = end;
-          end = min(blocks, end + chunk);
+          end = accumulator_end(done, small, blocks, chunk);
         } while (done < blocks);
         ok = __all_sync(0xffffffffu, ok);
       }
@@ -598,12 +595,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       }
     };
     for (typename Job::Ticket ticket; (ticket = feed.next()).i >= 0;) {
-      int blocks, chunk, done;
+      int blocks, small, chunk;
       {
         Tile t;
         job.tile(ticket, cta, t);
         blocks = t.passes * t.k_blocks;
-        done = first_chunk(t);
+        small = small_blocks(t);
         chunk = t.chunk;
       }
       if constexpr (Job::kClaimed) {
@@ -615,7 +612,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
       float v[kN / 2];
       take_columns<false>(v, mine + buf * kN, blocks == 0);
       give_back();
-      for (; done < blocks; done += chunk) {
+      for (int done = accumulator_end(0, small, blocks, chunk); done < blocks; done = accumulator_end(done, small, blocks, chunk)) {
         if (!wait()) break;
         take_columns<true>(v, mine + buf * kN, false);
         give_back();
