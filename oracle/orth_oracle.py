@@ -28,15 +28,15 @@ def _held(x, planes):
     return (hi + ((y - hi).half().double() if planes > 1 else 0.0)) / s
 
 
-def rounding_error(M, coefficients, eps=1e-7, full=False, loud=32.0, exact_input=True):
+def rounding_error(M, coefficients, eps=1e-7, full=False, loud=32.0, exact_input=True, square=False):
     """Frobenius norm of what the roundings of X, A and P leave in the result: X has two planes while the steps ahead amplify by
-    `loud` or more, A and P one; all have two with `full`.  The Gram matrix is that of X's first plane unless `full`."""
+    `loud` or more, A and P one (two with `square`); all have two with `full`.  The Gram matrix is that of X's first plane unless `full`."""
     want = orthogonalise(M, coefficients, eps)
     X = M.double()
     X = X / (X.square().sum().sqrt() + eps)
     X = X.mT if X.shape[0] > X.shape[1] else X
     one = torch.eye(X.shape[0], dtype=torch.float64, device=X.device)
-    two = 2 if full else 1
+    two, squares = 2 if full else 1, 2 if full or square else 1
     for k, (a, b, c) in enumerate(coefficients):
         ahead = 1.0
         for later in coefficients[k:]:
@@ -44,7 +44,7 @@ def rounding_error(M, coefficients, eps=1e-7, full=False, loud=32.0, exact_input
         first = X
         if k or not exact_input:
             X, first = _held(X, 2 if full or ahead >= loud else 1), _held(X, two)
-        A = _held(first @ first.mT, two)
-        X = _held(a * one + b * A + c * (A @ A), two) @ X
+        A = _held(first @ first.mT, squares)
+        X = _held(a * one + b * A + c * (A @ A), squares) @ X
     X = X.mT if M.shape[0] > M.shape[1] else X
     return float((X - want).norm()), want

@@ -13,6 +13,7 @@ namespace {
 constexpr int kMostSteps = kOrthMostSteps;
 constexpr int kGroup = 240;                               // matrices of one table
 constexpr int64_t kGroupBytes = (int64_t)1 << 30;         // workspace of one group, unless a single matrix takes more
+constexpr int64_t kFewAcross = 16, kFewAlong = 256;       // sides up to which roundings do not average out
 constexpr float kLoud = 32.f;                             // amplification ahead from which X keeps its second plane
 
 int check_matrices(const fopd_matrix *t, int32_t n) {
@@ -118,11 +119,12 @@ OrthMatrix describe(const fopd_matrix &m, const Scales &s, int32_t steps) {
   o.scale = m.scale;
   o.dtype = (uint8_t)m.dtype;
   o.out_dtype = (uint8_t)m.out_dtype;
-  // (also where a few numbers carry the whole result: the roundings of a 2 x 31 matrix do not average out, and a singular value that
-  // passes 1.15 on its way makes three times of them; 0.9 % of such a result, and one block more or less of the contraction)
-  o.full = m.out_dtype == FOPD_F32 || (std::min(m.rows, m.cols) <= 16 && std::max(m.rows, m.cols) <= 256);
+  // (the roundings of a few numbers do not average out, and a singular value that passes 1.15 on its way makes three times of them: A
+  // and P have as many as the shorter side says, X as both)
+  const bool thin = std::min(m.rows, m.cols) <= kFewAcross, few = thin && std::max(m.rows, m.cols) <= kFewAlong;
+  o.held = m.out_dtype == FOPD_F32 || few ? kOrthFull : thin ? kOrthSquare : kOrthPlain;
   const uint32_t all = (1u << steps) - 1;
-  o.two_planes = o.full ? all : s.loud & all;
+  o.two_planes = o.full() ? all : s.loud & all;
   if (m.dtype == FOPD_BF16) o.two_planes &= ~1u;  // (bf16 values are whole in the first plane)
   const int64_t x = (int64_t)o.rp * o.cp / 64, a = (int64_t)o.mp * o.mp / 64;
   uint32_t in_turn[2] = {0, 0};
@@ -135,9 +137,9 @@ OrthMatrix describe(const fopd_matrix &m, const Scales &s, int32_t steps) {
   }
   o.m_lo = (int)a;
   o.a = (int)at;
-  at += a * (1 + o.full);
+  at += a * (1 + o.square());
   o.p = (int)at;
-  at += a * (1 + o.full);
+  at += a * (1 + o.square());
   o.space = (int)at;
   return o;
 }
@@ -189,8 +191,9 @@ bool pairs_pay(const std::vector<OrthMatrix> &g, int sms) {
     double units[3] = {0, 0, 0}, longest[3] = {0, 0, 0};
     for (const OrthMatrix &m : g) {
       const double t = (m.mp + tile - 1) / tile, n_sym = t * (t + 1) / 2, n_x = (double)((m.rp + tile - 1) / tile) * ((m.cp + tile - 1) / tile);
-      const double unit = v ? 1.0 : m.full ? 0.43 : 0.6, passes = m.full ? 3 : 1, other = m.tall ? m.rp : m.cp;
-      const double each[3] = {other / 64 * passes * unit, m.mp / 64 * passes * unit, m.mp / 64 * passes * unit};
+      const double unit = v ? 1.0 : m.full() ? 0.43 : 0.6, other = m.tall ? m.rp : m.cp;
+      const double each[3] = {other / 64 * (m.full() ? 3 : 1) * unit, m.mp / 64 * (m.square() ? 3 : 1) * unit,
+                              m.mp / 64 * (m.full() ? 3 : m.square() ? 2 : 1) * unit};
       for (int k = 0; k < 3; ++k) {
         units[k] += (k < 2 ? n_sym : n_x) * each[k];
         longest[k] = std::max(longest[k], each[k]);

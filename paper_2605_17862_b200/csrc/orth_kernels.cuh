@@ -8,9 +8,12 @@
 // five steps of 3.4445).  In bf16 the rounding of X in the first steps comes out as 1 % of the result and, where a few strong directions
 // stand above the others, as 10 % and more.  So X, A and P are held in fp16 under powers of two that keep them just below its largest
 // number (11 bits, everything down to 2^-29 of the largest normal): an eighth of bf16's rounding at the same rate.  X has a second
-// plane of what the rounding left (together 22 bits) while the steps still ahead amplify by 32 or more, and P X then takes both; the
-// rounding of A and P is harmless, as it multiplies what is there.  Results in fp32, and matrices of a few numbers, have two planes
-// throughout, three products each.
+// plane of what the rounding left (together 22 bits) while the steps still ahead amplify by 32 or more, and P X then takes both.  The
+// rounding of A and P multiplies what is there and averages out over their elements, but for a shorter side of up to 16: one plane
+// takes 2 x 31, 2 x 600, 3 x 300 and 4 x 3,000 matrices 0.5 % off one time in a hundred and 0.9 % at most, 16 x 300 0.26 % and 17 x 40 0.30 %
+// (of which 0.17 % are a bf16 result's own rounding), whatever the longer side.  There A and P have two planes: 0.22 % at most from
+// 257 columns on.  Results in fp32, and matrices so short that X's roundings do not average out either (16 x 256: 2 x 17 0.43 % off
+// otherwise, 0.26 % as built), have two planes throughout, three products each.
 // The scales follow from a bound on the largest singular value in each step, which the host takes from the coefficients.
 //
 // Everything lies in one workspace in panels of 64 columns ([panel][rows][64], rows and columns padded with zeros to 64), so that one
@@ -21,6 +24,9 @@
 #include "tensor_core.cuh"
 
 namespace fopd {
+
+// What has two planes: nothing but X in some steps; A and P; X too, throughout.
+enum OrthHeld : uint8_t { kOrthPlain, kOrthSquare, kOrthFull };
 
 struct OrthMatrix {
   const void *data;
@@ -35,7 +41,10 @@ struct OrthMatrix {
   int sym_tile, x_tile;  // first tile of the matrix
   int norm_block, norm_blocks, load_block;
   float scale;
-  uint8_t dtype, out_dtype, tall, full;
+  uint8_t dtype, out_dtype, tall;
+  OrthHeld held;
+  __host__ __device__ __forceinline__ bool square() const { return held >= kOrthSquare; }
+  __host__ __device__ __forceinline__ bool full() const { return held == kOrthFull; }
 };
 
 constexpr int kOrthThreads = 256;
@@ -321,21 +330,21 @@ struct OrthJob {
     t.a_turn = t.b_turn = {1 << 30, &p.boxes, 0, 0};
     t.a_lo = t.b_lo = 0;
     t.passes = 1;
-    t.chunk = m.full ? kOrthChunk : kLongChunk;
+    t.chunk = m.full() ? kOrthChunk : kLongChunk;
     if (o.phase() == kOrthGram) {
       t.a = m.tall ? across(x, m.rp, row0, m.x_lo) : along(x, m.rp, row0, m.x_lo);
       t.b = m.tall ? across(x, m.rp, col0, m.x_lo) : along(x, m.rp, col0, m.x_lo);
       t.k_blocks = (m.tall ? m.rp : m.cp) / 64;
-      if (m.full && x_two) t.passes = 3, t.b_lo = 1, t.a_lo = 2;
+      if (m.full() && x_two) t.passes = 3, t.b_lo = 1, t.a_lo = 2;
     } else if (o.phase() == kOrthPoly) {
       symmetric(m.a, row0, o.row0(), t.a, t.a_turn);
       symmetric(m.a, col0, o.col0(), t.b, t.b_turn);
       t.k_blocks = m.mp / 64;
-      if (m.full) t.passes = 3, t.b_lo = 1, t.a_lo = 2;
+      if (m.square()) t.passes = 3, t.b_lo = 1, t.a_lo = 2;
     } else {
       t.k_blocks = m.mp / 64;
       uint32_t p_lo = 0, x_lo = 0;  // (the small terms first)
-      if (m.full) p_lo = 1u << (t.passes++ - 1);
+      if (m.square()) p_lo = 1u << (t.passes++ - 1);
       if (x_two) x_lo = 1u << (t.passes++ - 1);
       if (m.tall) {
         t.a = along(x, m.rp, row0, m.x_lo);
@@ -462,7 +471,7 @@ struct OrthJob {
 #pragma unroll
     for (int j = 0; j < kCols; ++j) v[j] *= f;
     if (o.phase() == kOrthPoly && panels > 0) {
-      for (int plane = 0; plane < (m.full ? 2 : 1); ++plane) {
+      for (int plane = 0; plane < (m.square() ? 2 : 1); ++plane) {
         if (plane) {
           __syncwarp();  // (the first plane has been read by all lanes)
           stage_square(o, m, cta, acc, 1);
@@ -493,7 +502,7 @@ struct OrthJob {
         for (int j = 0; j < kCols; ++j) v[j] += j == d ? step.poly_a : 0.f;
       }
     }
-    return put(o, acc, v, panels, (o.phase() == kOrthGram ? m.a : m.p) + col0 / 64 * m.mp + row0, m.mp, m.full, m.m_lo);
+    return put(o, acc, v, panels, (o.phase() == kOrthGram ? m.a : m.p) + col0 / 64 * m.mp + row0, m.mp, m.square(), m.m_lo);
   }
 };
 
