@@ -632,8 +632,8 @@ int fopd_head_grad(const fopd_head *h /* HOST */, const float *logprob, const fl
  * roundings of X would be amplified by 32 or more; A and its polynomial have 22 where the shorter side is at most 16, and all three
  * throughout for matrices whose result is fp32 and those of up to 16 x 256 (three products for each).  Sums are fp32.  Results do not depend on the run (their last bits may on what else is
  * in the list: it decides the size of tiles).  A matrix of zeros gives zeros; one that holds an infinity or NaN gives NaN and
- * sets FOPD_DEV_NONFINITE, the others are not affected.  One whose norm is so far below eps that X's elements are below 2^-39
- * loses them.
+ * sets FOPD_DEV_NONFINITE, the others are not affected.  The powers of two follow each matrix's norm and eps: where eps is far the
+ * larger, the result is as small as the definition says and as exact, down to 10^-30 of scale.
  */
 typedef struct {
   const void *data;     /* [rows, cols] at a pitch of row_stride elements; aligned to its element          */

@@ -63,7 +63,7 @@ int exponent_below(double bound) {  // bound * 2^e in (2^14, 2^15]
 }
 int make_scales(const float *coefficients, int32_t steps, Scales *s) {
   double most = 1.0;  // |M| / (|M| + eps) <= 1
-  int ex = 0;
+  int ex = 0, fall = 0;
   double ahead = 1.0;
   s->loud = 0;
   for (int k = steps - 1; k >= 0; --k) {
@@ -97,6 +97,9 @@ int make_scales(const float *coefficients, int32_t steps, Scales *s) {
     o.poly_b = (float)std::ldexp(b, ep - ea);
     o.poly_c = (float)std::ldexp(c, ep - 2 * ea);
     o.apply = (float)std::ldexp(1.0, (k == 0 ? 0 : -ex) - ep + ex_next);
+    // (singular values of at most 2^-lift most come out at most p times as large, and have room up to next)
+    o.fall = fall;
+    fall += std::max(0, (int)std::ceil(std::log2(most * p / next)));
     ex = ex_next;
     most = next;
   }
@@ -234,14 +237,14 @@ int run_group(std::vector<OrthMatrix> &g, const Scales &s, int32_t steps, float 
     x_tiles += ((int64_t)(m.rp + tile - 1) / tile) * ((m.cp + tile - 1) / tile);
   }
   Layout lay;
-  const int64_t planes = lay.take(at * 128), factor = lay.take((int64_t)g.size() * 4), done = lay.take(((int64_t)g.size() + 1) * 4),
-                partial = lay.take(norm_blocks * 8);
+  const int64_t planes = lay.take(at * 128), norm = lay.take((int64_t)(g.size() * sizeof(OrthNorm))), lifted = lay.take(4),
+                done = lay.take(((int64_t)g.size() + 1) * 4), partial = lay.take(norm_blocks * 8);
   char *base = nullptr;
   int rc = scratch_alloc(reinterpret_cast<void **>(&base), (size_t)lay.bytes, st);
   if (rc != FOPD_OK) return rc;
   Group o;
-  o.ws = {reinterpret_cast<float *>(base + factor), reinterpret_cast<int *>(base + done), reinterpret_cast<double *>(base + partial),
-          reinterpret_cast<__half *>(base + planes)};
+  o.ws = {reinterpret_cast<OrthNorm *>(base + norm), reinterpret_cast<int *>(base + lifted), reinterpret_cast<int *>(base + done),
+          reinterpret_cast<double *>(base + partial), reinterpret_cast<__half *>(base + planes)};
   o.norm_blocks = (int)norm_blocks;
   o.load_blocks = (int)load_blocks;
   o.norm_chunk = norm_chunk;

@@ -14,7 +14,9 @@
 // (of which 0.17 % are a bf16 result's own rounding), whatever the longer side.  There A and P have two planes: 0.22 % at most from
 // 257 columns on.  Results in fp32, and matrices so short that X's roundings do not average out either (16 x 256: 2 x 17 0.43 % off
 // otherwise, 0.26 % as built), have two planes throughout, three products each.
-// The scales follow from a bound on the largest singular value in each step, which the host takes from the coefficients.
+// The scales follow from a bound on the largest singular value in each step, which the host takes from the coefficients for a
+// largest one of 1.  Where eps makes it less, 2^-lift or below, X is held 2^lift higher (A 4^lift), and lift falls from step to step by as
+// much as the bound says that the step may amplify: a norm far below eps keeps its bits.
 //
 // Everything lies in one workspace in panels of 64 columns ([panel][rows][64], rows and columns padded with zeros to 64), so that one
 // tensor map serves every operand, along its rows or across them, and tiles need no edges.  A and A^2 are symmetric: only the
@@ -50,8 +52,13 @@ struct OrthMatrix {
 constexpr int kOrthThreads = 256;
 constexpr int kOrthChunk = 2;       // blocks of 64 that an accumulator adds up where the result is fp32
 
+struct OrthNorm {
+  float factor;  // 2^lift / ((|M| + eps) 2^e)
+  int lift;      // |M| / (|M| + eps) in [2^-(lift + 1), 2^-lift]
+};
 struct OrthWorkspace {
-  float *norm_factor;  // per matrix: 1 / ((|M| + eps) 2^e)
+  OrthNorm *norm;      // per matrix
+  int *lifted;         // whether any has a lift above 0
   int *done;           // per matrix: units of finished tiles (one for each epilogue warp); behind the last one the tiles claimed
   double *partial;     // per block of the norm
   __half *planes;
@@ -137,6 +144,7 @@ __global__ void __launch_bounds__(kOrthThreads) orth_norm_kernel(const __grid_co
   }
   s = block_sum(s, scratch);
   if (threadIdx.x == 0) ws.partial[blockIdx.x] = s;
+  if (threadIdx.x == 0 && blockIdx.x == 0) *ws.lifted = 0;
 }
 
 __device__ __forceinline__ void split_half(float x, __half &hi, __half &lo) {
@@ -159,28 +167,35 @@ __global__ void __launch_bounds__(kOrthThreads) orth_load_kernel(const __grid_co
   __shared__ double scale_of_block;
   __shared__ int exponent_of_block;
   s = block_sum(s, scratch);
+  const double norm = sqrt(s);
+  const bool finite = norm <= 1.7e308;
   if (threadIdx.x == 0) {
-    const double norm = sqrt(s);
-    const bool finite = norm <= 1.7e308;
     int e = 0;
-    double factor = 0.0;
     if (finite && norm > 0.0) {
       frexp(norm, &e);  // norm in [2^(e-1), 2^e)
       e = 15 - e;
-      factor = 1.0 / ldexp(norm + (double)eps, e);
     }
     exponent_of_block = finite ? e : 0;
     scale_of_block = finite ? ldexp(1.0, e) : __longlong_as_double(0x7ff8000000000000ll);
-    if (block == 0) {
-      ws.done[k] = 0;
-      if (k == 0) ws.done[tab.n] = 0;
-      ws.norm_factor[k] = finite ? (float)factor : __int_as_float(0x7fffffff);
-      if (!finite && status) atomicOr(status, FOPD_DEV_NONFINITE);
-    }
   }
   __syncthreads();
   const double scale = scale_of_block;
   const int e = exponent_of_block;
+  if (block == 0 && threadIdx.x == 0) {
+    OrthNorm of = {finite ? 0.f : __int_as_float(0x7fffffff), 0};
+    if (finite && norm > 0.0) {
+      const double with_eps = norm + (double)eps;
+      int a, b;
+      const double f = frexp(norm, &a), g = frexp(with_eps, &b);
+      of.lift = max(0, b - a - (f >= g ? 1 : 0));
+      of.factor = (float)(1.0 / ldexp(with_eps, e - of.lift));
+    }
+    ws.norm[k] = of;
+    if (of.lift > 0) *ws.lifted = 1;
+    ws.done[k] = 0;
+    if (k == 0) ws.done[tab.n] = 0;
+    if (!finite && status) atomicOr(status, FOPD_DEV_NONFINITE);
+  }
   const int col_blocks = (m.cp + tab.load_cols - 1) / tab.load_cols;
   const int row0 = block / col_blocks * 64, col0 = block % col_blocks * tab.load_cols;
   const int size = m.dtype == FOPD_BF16 ? 2 : 4;
@@ -231,11 +246,12 @@ __global__ void __launch_bounds__(kOrthThreads) orth_load_kernel(const __grid_co
 enum OrthPhase { kOrthGram = 0, kOrthPoly = 1, kOrthApply = 2 };
 constexpr int kOrthMostSteps = 16;
 
-// Factors of one step (powers of two but for the coefficients).  Values in the workspace are X 2^ex, A 2^ea, P 2^ep.
+// Factors of one step (powers of two but for the coefficients).  Values in the workspace are X 2^ex, A 2^ea, P 2^ep, but for the lift.
 struct OrthStep {
-  float gram;                   // from X's products to A's scale (first step: on top of norm_factor^2)
+  float gram;                   // from X's products to A's scale (first step: on top of the norm's factor squared)
   float poly_a, poly_b, poly_c; // P = a I + b A + c A^2, from A's values and A's products to P's scale
-  float apply;                  // from P X to the next X's scale; last step: to 1 (first step: on top of norm_factor)
+  float apply;                  // from P X to the next X's scale; last step: to 1 (first step: on top of the norm's factor)
+  int fall;                     // what is left of the lift in this step: its first value less this, at least 0
 };
 
 template <int kCtas, int kN, int N>
@@ -266,7 +282,9 @@ struct OrthJob {
   const Params &p;
   uint32_t staged_turn = 0;  // parity of this warp's copies into its staging buffers
   uint32_t order_turn = 1;   // and of the storing thread's handing them back
-  __device__ explicit OrthJob(const Params &params) : p(params) {}
+  int first_lift = 0;        // of the tile's matrix
+  const bool lifted;         // (as a rule none is, and tiles are spared the reading: with it and ldexpf it was 2 % of small lists' time)
+  __device__ explicit OrthJob(const Params &params) : p(params), lifted(*params.ws.lifted != 0) {}
   __device__ int64_t tiles() const { return (int64_t)p.steps * (2 * p.sym_tiles + p.x_tiles); }
   __device__ int32_t *status() const { return p.status; }
   __device__ int *counter() const { return p.ws.done + p.tab.n; }
@@ -423,11 +441,15 @@ struct OrthJob {
       tma_load<1>(acc.staging + c * kStageBufBytes, &p.rows_out, 0, m.a + plane * m.m_lo + (col0 / 64 + c) * m.mp + row0, acc.staged);
   }
   __device__ __forceinline__ bool prefetch(const Ticket &o, int cta, const Accumulator &acc, long long limit) {
+    if (lifted) first_lift = p.ws.norm[o.k()].lift;
     if (o.phase() != kOrthPoly) return true;
     const bool ok = __all_sync(0xffffffffu, ready(o, limit)) && buffers(acc);
     if (ok) stage_square(o, p.tab.m[o.k()], cta, acc, 0);
     return ok;
   }
+  __device__ __forceinline__ int lift(int step) const { return max(0, first_lift - p.step[step].fall); }
+  // (e <= 0; below 2^-126 taken for that)
+  static __device__ __forceinline__ float power_of_two(int e) { return __int_as_float((max(e, -126) + 127) << 23); }
   __device__ __forceinline__ bool epilogue(const Ticket &o, int cta, const Accumulator &acc, float (&v)[kN / 2]) {
     const OrthMatrix &m = p.tab.m[o.k()];
     const int row0 = o.row0() + cta * 128 + acc.warp * 32, col0 = o.col0() + acc.half * (kN / 2);
@@ -435,7 +457,9 @@ struct OrthJob {
   }
   __device__ __forceinline__ bool put_x(const Ticket &o, const OrthMatrix &m, int row0, int col0, const Accumulator &acc, float (&v)[kN / 2]) {
     constexpr int kCols = kN / 2;
-    const float f = (o.step() == 0 ? p.ws.norm_factor[o.k()] : 1.f) * p.step[o.step()].apply * (last(o) ? m.scale : 1.f);
+    float f = (o.step() == 0 ? p.ws.norm[o.k()].factor : 1.f) * p.step[o.step()].apply * (last(o) ? m.scale : 1.f);
+    const int down = lift(o.step()) - (last(o) ? 0 : lift(o.step() + 1));
+    f = f * power_of_two(-(down / 2)) * power_of_two(down / 2 - down);
 #pragma unroll
     for (int j = 0; j < kCols; ++j) v[j] *= f;
     if (last(o)) {
@@ -463,10 +487,13 @@ struct OrthJob {
     constexpr int kCols = kN / 2;
     const OrthStep &step = p.step[o.step()];
     const int panels = square_panels(m, row0, col0);
-    float f = step.poly_c;
+    float f = step.poly_c, poly_b = step.poly_b;
     if (o.phase() == kOrthGram) {
-      const float s = o.step() == 0 ? p.ws.norm_factor[o.k()] : 1.f;
+      const float s = o.step() == 0 ? p.ws.norm[o.k()].factor : 1.f;
       f = step.gram * s * s;
+    } else {
+      f *= power_of_two(-4 * lift(o.step()));
+      poly_b *= power_of_two(-2 * lift(o.step()));
     }
 #pragma unroll
     for (int j = 0; j < kCols; ++j) v[j] *= f;
@@ -489,8 +516,8 @@ struct OrthJob {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&u[e]));
-              v[c + 8 * j + 2 * e] = fmaf(step.poly_b, a.x, v[c + 8 * j + 2 * e]);
-              v[c + 8 * j + 2 * e + 1] = fmaf(step.poly_b, a.y, v[c + 8 * j + 2 * e + 1]);
+              v[c + 8 * j + 2 * e] = fmaf(poly_b, a.x, v[c + 8 * j + 2 * e]);
+              v[c + 8 * j + 2 * e + 1] = fmaf(poly_b, a.y, v[c + 8 * j + 2 * e + 1]);
             }
           }
         }
