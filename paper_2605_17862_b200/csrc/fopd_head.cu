@@ -38,14 +38,22 @@ bool meets_inputs(const fopd_head *h, const void *p, int64_t n) {
          meets(p, n, h->mask, h->n_rows);
 }
 
+// (an error is this call's alone: the next one's is not to find it)
+int clear_rows(void *p, int64_t pitch, int64_t width, int64_t rows, cudaStream_t st) {
+  if (cudaMemset2DAsync(p, (size_t)pitch, 0, (size_t)width, (size_t)rows, st) == cudaSuccess) return FOPD_OK;
+  (void)cudaGetLastError();
+  return FOPD_ERR_CUDA;
+}
+
 struct Temporary {
   char *base = nullptr;
   cudaStream_t st;
   explicit Temporary(cudaStream_t s) : st(s) {}
   int take(int64_t bytes) { return scratch_alloc(reinterpret_cast<void **>(&base), (size_t)bytes, st); }
   int give(int rc) {
-    if (base && cudaFreeAsync(base, st) != cudaSuccess && rc == FOPD_OK) rc = FOPD_ERR_CUDA;
-    return rc;
+    if (!base || cudaFreeAsync(base, st) == cudaSuccess) return rc;
+    (void)cudaGetLastError();
+    return rc == FOPD_OK ? FOPD_ERR_CUDA : rc;
   }
 };
 
@@ -198,10 +206,8 @@ int run_grad(const fopd_head *h, const float *logprob, const float *lse, const f
   }
   if (rc == FOPD_OK)
     rc = make_map(&q.panels_along, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, 2 * kBoxRows, true);
-  if (rc == FOPD_OK && o.d_hidden && h->mask &&
-      cudaMemset2DAsync(o.d_hidden, (size_t)(h->n_rows > 1 ? o.d_hidden_stride : round_up(h->dim, 8)) * 2, 0, (size_t)h->dim * 2,
-                        (size_t)h->n_rows, st) != cudaSuccess)
-    rc = FOPD_ERR_CUDA;
+  if (rc == FOPD_OK && o.d_hidden && h->mask)
+    rc = clear_rows(o.d_hidden, (h->n_rows > 1 ? o.d_hidden_stride : h->dim) * 2, h->dim * 2, h->n_rows, st);
   if (rc == FOPD_OK) {
     g.hidden = pre.hidden_along;
     g.weight = pre.weight_along;
@@ -279,13 +285,8 @@ int fopd_head_grad(const fopd_head *h, const float *logprob, const float *lse, c
     return FOPD_ERR_ALIGN;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (h->n_rows == 0) {  // no row: the weights' gradient is zero
-    if (d_weight && !add_d_weight &&
-        cudaMemset2DAsync(d_weight, (size_t)(h->vocab > 1 ? d_weight_stride : h->dim) * wsize, 0, (size_t)(h->dim * wsize), (size_t)h->vocab,
-                          st) != cudaSuccess) {
-      (void)cudaGetLastError();
-      return FOPD_ERR_CUDA;
-    }
-    return FOPD_OK;
+    return d_weight && !add_d_weight ? clear_rows(d_weight, (h->vocab > 1 ? d_weight_stride : h->dim) * wsize, h->dim * wsize, h->vocab, st)
+                                     : FOPD_OK;
   }
   if (!logprob || !lse || !coef) return FOPD_ERR_NULL;
   const int64_t nh = d_hidden ? matrix_bytes(h->n_rows, h->dim, d_hidden_stride, 2) : 0;

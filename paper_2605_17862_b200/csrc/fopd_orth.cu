@@ -261,8 +261,9 @@ int run_group(std::vector<OrthMatrix> &g, const Scales &s, int32_t steps, float 
          : n <= 64 ? run_table<64>(g, o, s, steps, eps, status, sms, st)
                    : run_table<kGroup>(g, o, s, steps, eps, status, sms, st);
   }
-  if (cudaFreeAsync(base, st) != cudaSuccess && rc == FOPD_OK) rc = FOPD_ERR_CUDA;
-  return rc;
+  if (cudaFreeAsync(base, st) == cudaSuccess) return rc;
+  (void)cudaGetLastError();
+  return rc == FOPD_OK ? FOPD_ERR_CUDA : rc;
 }
 
 }  // namespace
