@@ -7,7 +7,8 @@ using namespace fopd;
 namespace {
 
 constexpr int64_t kPieceBytes = (int64_t)1 << 29;   // gradient of the logits kept at a time
-constexpr int64_t kLogprobRows = 32768;             // rows whose pieces (8 bytes to 128 tokens) are kept at a time
+constexpr int64_t kPartBytes = (int64_t)1 << 29;    // rows' pieces (8 bytes to 128 tokens) kept at a time
+constexpr int64_t kLogprobRows = 32768;             // rows they are of at most
 constexpr int64_t kSumBytes = (int64_t)256 << 20;   // sums of d_hidden, where the vocabulary is cut into splits
 
 int check_head(const fopd_head *h) {
@@ -116,7 +117,10 @@ int rows_from(const fopd_head *h, int64_t first, int64_t n, Prepared *pre) {
 
 template <int kCtas, int kN>
 int run_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *status, int sms, cudaStream_t st) {
-  const int64_t v_tiles = (h->vocab + kN - 1) / kN, pitch = round_up(h->n_rows < kLogprobRows ? h->n_rows : kLogprobRows, kCtas * 128);
+  constexpr int64_t kRows = kCtas * 128;
+  const int64_t v_tiles = (h->vocab + kN - 1) / kN;
+  const int64_t fit = kPartBytes / (16 * v_tiles) / kRows * kRows, at_a_time = fit < kRows ? kRows : fit < kLogprobRows ? fit : kLogprobRows;
+  const int64_t pitch = round_up(h->n_rows < at_a_time ? h->n_rows : at_a_time, kRows);
   Layout lay;
   const RowParts parts = row_parts(h, &lay);
   const int64_t part = lay.take(2 * v_tiles * pitch * 8), logit = lay.take(pitch * 4);
@@ -125,8 +129,8 @@ int run_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *status,
   if (rc != FOPD_OK) return rc;
   Prepared pre;
   rc = prepare_rows(h, parts, tmp.base, nullptr, logprob, lse, status, st, &pre);
-  for (int64_t first = 0; rc == FOPD_OK && first < h->n_rows; first += kLogprobRows) {
-    rc = rows_from(h, first, kLogprobRows, &pre);
+  for (int64_t first = 0; rc == FOPD_OK && first < h->n_rows; first += at_a_time) {
+    rc = rows_from(h, first, at_a_time, &pre);
     if (rc != FOPD_OK) break;
     typename LogprobJob<kCtas, kN>::Params p;
     p.hidden = pre.hidden_along;
@@ -137,7 +141,7 @@ int run_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *status,
     p.token_logit = reinterpret_cast<float *>(tmp.base + logit);
     p.pitch = (int)pitch;
     p.status = status;
-    rc = launch_product<kCtas, kN, LogprobJob<kCtas, kN>>(p, (pre.rows.n + kCtas * 128 - 1) / (kCtas * 128) * v_tiles, sms, st);
+    rc = launch_product<kCtas, kN, LogprobJob<kCtas, kN>>(p, (pre.rows.n + kRows - 1) / kRows * v_tiles, sms, st);
     if (rc == FOPD_OK)
       rc = launch_early(head_join_kernel, dim3((unsigned)((pre.rows.n + 3) / 4)), kJoinThreads, st, pre.rows, (const float2 *)p.part,
                         (const float *)p.token_logit, 2 * (int)v_tiles, (int)pitch, h->tokens, h->vocab, logprob, lse, status);
