@@ -599,7 +599,7 @@ typedef struct {
 /* logprob [n_rows] fp32, never above 0, and lse [n_rows] fp32 or NULL.  Logits are fp32 sums rounded to nearest every 512
  * dimensions (a matrix instruction by itself cuts off what it drops), kept nowhere but on chip; the log-prob of a nearly certain token
  * comes from the sum of the others and keeps its relative accuracy.  The temporary is up to 512 MiB of maxima and sums (beyond 2^25
- * tokens 16 bytes for each) and with a mask a copy of the hidden states.  The outputs must not lie on the inputs or on one another. */
+ * tokens 16 bytes for each) and with a mask a copy of the hidden states.  The outputs must share no element with the inputs or one another. */
 int fopd_head_logprob(const fopd_head *h /* HOST */, float *logprob, float *lse, int32_t *status, void *stream);
 
 /*
@@ -614,7 +614,7 @@ int fopd_head_logprob(const fopd_head *h /* HOST */, float *logprob, float *lse,
  * G is rounded to bf16 once for the products (2^-8 of each entry at most, of the size of a bf16 result's own rounding); for
  * a d_weight in fp32 what that leaves is kept and multiplied too (2^-17), which costs that product twice.  The temporary is up to
  * 512 MiB of G (more beyond 2^19 rows), fp32 sums of d_hidden's size or 256 MiB, and with a mask a copy of the hidden states.
- * Outputs must not lie on inputs or on one another.
+ * Outputs must share no element with inputs or one another; columns of one wider matrix, beside each other, do not.
  */
 int fopd_head_grad(const fopd_head *h /* HOST */, const float *logprob, const float *lse, const float *coef, void *d_hidden,
                    int64_t d_hidden_stride, void *d_weight, int64_t d_weight_stride, int32_t d_weight_dtype,

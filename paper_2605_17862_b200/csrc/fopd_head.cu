@@ -1,5 +1,6 @@
 // Log-probs from hidden states and head weights, and their gradient: argument checks, workspaces, launches.
 #include "head_kernels.cuh"
+#include "host_ranges.cuh"
 #include "tensor_host.cuh"
 
 using namespace fopd;
@@ -25,18 +26,24 @@ int check_head(const fopd_head *h) {
   return FOPD_OK;
 }
 
-int64_t matrix_bytes(int64_t rows, int64_t cols, int64_t pitch, int64_t size) {
-  return rows > 0 ? ((rows - 1) * pitch + cols) * size : 0;
+// Where a tensor of the call lies.  Rows that share no element with those of another are apart, also in columns of one wider matrix.
+struct Place {
+  Range at;
+  bool there;
+};
+Place place(const void *p, int64_t rows, int64_t cols, int64_t stride, int64_t size) {
+  if (!p || rows <= 0) return {{}, false};
+  return {range_of(p, rows, cols, stride, (uintptr_t)size, 0, false), true};
 }
-bool meets(const void *a, int64_t na, const void *b, int64_t nb) {
-  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return a && b && na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
+Place vector_at(const void *p, int64_t n, int64_t size) { return place(p, 1, n, n, size); }
+bool meet(const Place &a, const Place &b) {
+  if (!a.there || !b.there || a.at.hi <= b.at.lo || b.at.hi <= a.at.lo) return false;
+  return a.at.lo <= b.at.lo ? !disjoint_columns(a.at, b.at) : !disjoint_columns(b.at, a.at);
 }
 // Whether an output meets one of the arrays that every call reads.
-bool meets_inputs(const fopd_head *h, const void *p, int64_t n) {
-  return meets(p, n, h->hidden, matrix_bytes(h->n_rows, h->dim, h->hidden_stride, 2)) ||
-         meets(p, n, h->weight, matrix_bytes(h->vocab, h->dim, h->weight_stride, 2)) || meets(p, n, h->tokens, h->n_rows * 4) ||
-         meets(p, n, h->mask, h->n_rows);
+bool meets_inputs(const fopd_head *h, const Place &p) {
+  return meet(p, place(h->hidden, h->n_rows, h->dim, h->hidden_stride, 2)) || meet(p, place(h->weight, h->vocab, h->dim, h->weight_stride, 2)) ||
+         meet(p, vector_at(h->tokens, h->n_rows, 4)) || meet(p, vector_at(h->mask, h->n_rows, 1));
 }
 
 // (an error is this call's alone: the next one's is not to find it)
@@ -264,8 +271,8 @@ int fopd_head_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *s
   int rc = check_head(h);
   if (rc != FOPD_OK || h->n_rows == 0) return rc;
   if (!logprob) return FOPD_ERR_NULL;
-  const int64_t n = h->n_rows * 4;
-  if (meets_inputs(h, logprob, n) || meets_inputs(h, lse, n) || meets(logprob, n, lse, n)) return FOPD_ERR_ALIAS;
+  const Place lp = vector_at(logprob, h->n_rows, 4), ls = vector_at(lse, h->n_rows, 4);
+  if (meets_inputs(h, lp) || meets_inputs(h, ls) || meet(lp, ls)) return FOPD_ERR_ALIAS;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int sms = 0;
   rc = current_sms(&sms);
@@ -293,11 +300,10 @@ int fopd_head_grad(const fopd_head *h, const float *logprob, const float *lse, c
                                      : FOPD_OK;
   }
   if (!logprob || !lse || !coef) return FOPD_ERR_NULL;
-  const int64_t nh = d_hidden ? matrix_bytes(h->n_rows, h->dim, d_hidden_stride, 2) : 0;
-  const int64_t nw = d_weight ? matrix_bytes(h->vocab, h->dim, d_weight_stride, wsize) : 0, n = h->n_rows * 4;
-  for (const void *in : {(const void *)logprob, (const void *)lse, (const void *)coef})
-    if (meets(d_hidden, nh, in, n) || meets(d_weight, nw, in, n)) return FOPD_ERR_ALIAS;
-  if (meets_inputs(h, d_hidden, nh) || meets_inputs(h, d_weight, nw) || meets(d_hidden, nh, d_weight, nw)) return FOPD_ERR_ALIAS;
+  const Place dh = place(d_hidden, h->n_rows, h->dim, d_hidden_stride, 2), dw = place(d_weight, h->vocab, h->dim, d_weight_stride, wsize);
+  for (const float *in : {logprob, lse, coef})
+    if (meet(dh, vector_at(in, h->n_rows, 4)) || meet(dw, vector_at(in, h->n_rows, 4))) return FOPD_ERR_ALIAS;
+  if (meets_inputs(h, dh) || meets_inputs(h, dw) || meet(dh, dw)) return FOPD_ERR_ALIAS;
   int sms = 0;
   rc = current_sms(&sms);
   if (rc != FOPD_OK) return rc;
