@@ -73,7 +73,7 @@ struct Prepared {
   CUtensorMap hidden_along, weight_along;  // boxes for products along the dimensions
 };
 int operand_map(CUtensorMap *map, const void *at, int64_t dim, int64_t rows, int64_t pitch, int box_rows) {
-  return make_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, at, dim, rows, pitch * 2, 64, box_rows, true);
+  return make_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, at, dim, rows, pitch * 2, 64, box_rows);
 }
 int64_t weight_pitch(const fopd_head *h) { return h->vocab > 1 ? h->weight_stride : round_up(h->dim, 8); }
 struct RowParts {
@@ -204,19 +204,19 @@ int run_grad(const fopd_head *h, const float *logprob, const float *lse, const f
   if (rc == FOPD_OK) rc = operand_map(&q.hidden, pre.hidden_at, h->dim, pre.hidden_rows, pre.hidden_pitch, kBoxRows);
   if (rc == FOPD_OK) rc = operand_map(&q.weight, h->weight, h->dim, h->vocab, weight_pitch(h), kBoxRows);
   if (rc == FOPD_OK)
-    rc = make_map(&g.panels_out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, 32, true);
+    rc = make_map(&g.panels_out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, 32);
   if (rc == FOPD_OK)
-    rc = make_map(&q.panels, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, kBoxRows, true);
+    rc = make_map(&q.panels, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, kBoxRows);
   // (a box ends at a multiple of 16 bytes: rows that do not would be written beyond their end)
   q.d_weight_boxes = o.d_weight && !o.add && h->dim * (o.d_weight_dtype == FOPD_F32 ? 4 : 2) % 16 == 0;
   if (rc == FOPD_OK && q.d_weight_boxes) {
     const bool f32 = o.d_weight_dtype == FOPD_F32;
     const int64_t size = f32 ? 4 : 2, stride = h->vocab > 1 ? o.d_weight_stride : round_up(h->dim, 16 / size);
     rc = make_map(&q.d_weight_out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, o.d_weight, h->dim, h->vocab,
-                  stride * size, 128 / (int)size, 32, true);
+                  stride * size, 128 / (int)size, 32);
   }
   if (rc == FOPD_OK)
-    rc = make_map(&q.panels_along, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, 2 * kBoxRows, true);
+    rc = make_map(&q.panels_along, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, tmp.base + g_at, 64, panels * pitch * planes, 128, 64, 2 * kBoxRows);
   if (rc == FOPD_OK && o.d_hidden && h->mask)
     rc = clear_rows(o.d_hidden, (h->n_rows > 1 ? o.d_hidden_stride : h->dim) * 2, h->dim * 2, h->n_rows, st);
   if (rc == FOPD_OK) {

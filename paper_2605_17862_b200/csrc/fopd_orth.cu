@@ -252,9 +252,9 @@ int run_group(std::vector<OrthMatrix> &g, const Scales &s, int32_t steps, float 
   o.sym_tiles = sym_tiles;
   o.x_tiles = x_tiles;
   o.pairs = tile == 256;
-  rc = make_map(&o.boxes, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, o.ws.planes, 64, at, 128, 64, kBoxRows, true);
-  if (rc == FOPD_OK) rc = make_map(&o.rows_out, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, o.ws.planes, 64, at, 128, 64, 32, true);
-  if (rc == FOPD_OK) rc = make_map(&o.boxes_along, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, o.ws.planes, 64, at, 128, 64, 2 * kBoxRows, true);
+  rc = make_map(&o.boxes, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, o.ws.planes, 64, at, 128, 64, kBoxRows);
+  if (rc == FOPD_OK) rc = make_map(&o.rows_out, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, o.ws.planes, 64, at, 128, 64, 32);
+  if (rc == FOPD_OK) rc = make_map(&o.boxes_along, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, o.ws.planes, 64, at, 128, 64, 2 * kBoxRows);
   if (rc == FOPD_OK) {
     const size_t n = g.size();
     rc = n <= 8    ? run_table<8>(g, o, s, steps, eps, status, sms, st)

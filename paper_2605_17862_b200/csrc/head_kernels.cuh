@@ -335,8 +335,9 @@ struct GradLogitsJob {
         staging.send(acc, &p.panels_out, 0, (panel0 + c / 64) * p.pitch + row0 + plane * p.lo, at);
       }
     };
+    static_assert(kCols == 128, "two panels");
     put(g, 0);
-    if (kCols > 64) put(g + 64, 64);
+    put(g + 64, 64);
   }
 };
 
@@ -445,14 +446,15 @@ struct HeadGradsJob {
           });
         staging.send(acc, &p.d_weight_out, d, (int)row_out, at);
       };
+      static_assert(kN == 256, "four boxes of 32 columns, two of 64");
       if (p.d_weight_f32) {
         send(g, d0);
         send(g + 32, d0 + 32);
-        if (kN > 128) send(g + kN / 2 - 64, d0 + kN / 2 - 64);
-        if (kN > 128) send(g + kN / 2 - 32, d0 + kN / 2 - 32);
+        send(g + 64, d0 + 64);
+        send(g + 96, d0 + 96);
       } else {
         send(g, d0);
-        if (kN > 128) send(g + kN / 2 - 64, d0 + kN / 2 - 64);
+        send(g + 64, d0 + 64);
       }
       return;
     }

@@ -29,16 +29,15 @@ inline TensorMapEncode tensor_map_encode() {
   return reinterpret_cast<TensorMapEncode>(fn);
 }
 
-// [rows, cols] 16-bit elements at a pitch in bytes (a multiple of 16, base 16-byte aligned); boxes of box_rows x box_cols.
+// [rows, cols] elements at a pitch in bytes (a multiple of 16, base 16-byte aligned); boxes of box_rows x 128 bytes, swizzled.
 inline int make_map(CUtensorMap *map, CUtensorMapDataType type, const void *base, int64_t cols, int64_t rows, int64_t pitch_bytes,
-                    int box_cols, int box_rows, bool swizzled) {
+                    int box_cols, int box_rows) {
   TensorMapEncode encode = tensor_map_encode();
   if (!encode) return FOPD_ERR_CUDA;
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch_bytes};
   const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, unit[2] = {1, 1};
   return encode(map, type, 2, const_cast<void *>(base), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
              ? FOPD_OK
              : FOPD_ERR_CUDA;
 }
