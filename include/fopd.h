@@ -597,7 +597,7 @@ typedef struct {
 } fopd_head;
 
 /* logprob [n_rows] fp32, never above 0, and lse [n_rows] fp32 or NULL.  Logits are fp32 sums rounded to nearest every 512
- * dimensions (a matrix instruction by itself cuts off what it drops), kept nowhere but on chip; the log-prob of a nearly certain token
+ * dimensions, every 128 for up to 128 rows (a matrix instruction by itself cuts off what it drops), kept nowhere but on chip; the log-prob of a nearly certain token
  * comes from the sum of the others and keeps its relative accuracy.  The temporary is up to 512 MiB of maxima and sums (beyond 2^25
  * tokens 16 bytes for each) and with a mask a copy of the hidden states.  The outputs must share no element with the inputs or one another. */
 int fopd_head_logprob(const fopd_head *h /* HOST */, float *logprob, float *lse, int32_t *status, void *stream);

@@ -142,7 +142,7 @@ int run_logprob(const fopd_head *h, float *logprob, float *lse, int32_t *status,
     typename LogprobJob<kCtas, kN>::Params p;
     p.hidden = pre.hidden_along;
     p.weight = pre.weight_along;
-    p.l = {nullptr, nullptr, pre.rows, h->vocab, (int)((h->dim + 63) / 64), 0, (int)v_tiles, kLogitChunk};
+    p.l = {nullptr, nullptr, pre.rows, h->vocab, (int)((h->dim + 63) / 64), 0, (int)v_tiles, kCtas == 1 ? kFewRowsChunk : kLogitChunk};
     p.tokens = h->tokens;
     p.part = reinterpret_cast<float2 *>(tmp.base + part);
     p.token_logit = reinterpret_cast<float *>(tmp.base + logit);
@@ -243,7 +243,8 @@ int run_grad(const fopd_head *h, const float *logprob, const float *lse, const f
     for (int64_t v0 = 0; rc == FOPD_OK && v0 < h->vocab; v0 += piece) {
       const int64_t count = h->vocab - v0 < piece ? h->vocab - v0 : piece;
       // (for bf16 gradients the logits' own last bits do not show: one accumulator)
-      g.l = {nullptr, nullptr, pre.rows, h->vocab, (int)((h->dim + 63) / 64), (int)(v0 / kN), (int)((count + kN - 1) / kN), lo ? kGradChunk : kLongChunk};
+      g.l = {nullptr, nullptr, pre.rows, h->vocab, (int)((h->dim + 63) / 64), (int)(v0 / kN), (int)((count + kN - 1) / kN),
+             !lo ? kLongChunk : kCtas == 1 ? kFewRowsChunk : kGradChunk};
       q.v0 = v0;
       q.v_count = (int)count;
       q.first = v0 == 0;

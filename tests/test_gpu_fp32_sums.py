@@ -44,3 +44,25 @@ def test_orthogonalised_matrices(shape):
         errors.append([float((x.double() - want).norm() / want.norm()) for x in (out, plain)])
     here, plain = (sum(e[k] for e in errors) / len(errors) for k in range(2))
     assert here <= 1.5 * plain, (here, plain)
+
+
+@pytest.mark.parametrize("n,at_once,V,D", [(96, 1, 32000, 1024), (64, 1, 8000, 2048), (128, 128, 32000, 1024), (96, 48, 8000, 2048)])
+def test_log_probs_of_few_rows(n, at_once, V, D):
+    """Logits ~ N(0, 3^2), every token a likely one: its logit is near the largest.  Few rows, one at a time or all at once (elementary products
+    are the more exact the fewer they are)."""
+    g = torch.Generator(device=DEV).manual_seed(n)
+    h = torch.randn((n, D), generator=g, device=DEV)
+    w = (torch.randn((V, D), generator=g, device=DEV) * (3 / math.sqrt(D))).bfloat16()
+    y = torch.randint(0, V, (n,), generator=g, device=DEV, dtype=torch.int32)
+    of = w[y.long()].float()
+    h = (h + of * (4.0 / of.square().sum(1, keepdim=True).sqrt())).bfloat16()
+    lp, plain, token = torch.empty(n, device=DEV), torch.empty(n, device=DEV), y.long().unsqueeze(1)
+    for k in range(0, n, at_once):
+        rows = slice(k, k + at_once)
+        fb.fopd_head_logprob(h[rows], w, y[rows], lp[rows])
+        z = h[rows].float() @ w.float().t()
+        m = z.amax(1, keepdim=True)
+        plain[rows] = (z.gather(1, token[rows]) - ((z - m).exp().sum(1, keepdim=True, dtype=torch.float64).log() + m)).squeeze(1).float()
+    want = torch.log_softmax(h.double() @ w.double().t(), 1).gather(1, token).squeeze(1)
+    here, plain = (float((x.double() - want).square().mean().sqrt()) for x in (lp, plain))
+    assert here <= 1.5 * plain, (here, plain)
