@@ -132,7 +132,7 @@ __device__ __forceinline__ void logit_tile(const LogitTiles &l, int n_rows, int6
 // ------------------------------------------------------------------ log-probs
 // A tile's epilogue: two threads per row, each the maximum and the sum of exponentials of 128 logits (exponents as in RowSweep), the
 // stored token's left out of the sum: the log-prob of a nearly certain token comes from the others' sum.
-// 4,096 x 151,936 x 2,048: 1.83 ms, the tensor pipe's rate; 48 rows: 105 us, reading the weights at 5.9 TB/s (128 rows a tile, three
+// 4,096 x 151,936 x 2,048: 1.83 to 1.89 ms, the tensor pipe's rate; 48 rows: 106 us, reading the weights at 5.9 TB/s (128 rows a tile, three
 // stages of 48 KB on each SM in flight).
 template <int kCtas, int kN>
 struct LogprobJob {
@@ -254,7 +254,8 @@ __global__ void __launch_bounds__(kJoinThreads) head_join_kernel(HeadRows rows, 
 // ------------------------------------------------------------------ gradient of the logits, a piece of the vocabulary
 // G goes to panels: [panel of 64 columns][pitch rows][64], bf16; a second plane of what the rounding left where the weights'
 // gradient is wanted in fp32.  One rounding to bf16 (2^-8 of an entry at most) is what a matrix instruction takes; it is of the size
-// of the bf16 results' own.  Each tile's boxes go out by TMA while the next one's products run: 4,096 x 151,936 x 2,048 in 1.76 ms.
+// of the bf16 results' own.  Each tile's boxes go out by TMA while the next one's products run: 4,096 x 151,936 x 2,048 in 1.6 ms, the tensor pipe
+// 91 to 92 % busy.
 template <int kCtas, int kN>
 struct GradLogitsJob {
   static constexpr bool kFp16 = false, kTurns = false, kClaimed = false;
@@ -347,7 +348,7 @@ struct GradLogitsJob {
 // ------------------------------------------------------------------ gradients of hidden states and weights
 // d_hidden's tiles run along the piece's columns, cut into `splits` where there are too few of them, and are added up in fp32
 // (in the workspace, in a fixed order); d_weight's run along the rows and are finished.  Both in one launch, the long tiles first:
-// 4,096 x 151,936 x 2,048 in 3.4 ms of products at 90 % of the tensor pipe; with 100 rows, where d_hidden alone would be four tiles,
+// 4,096 x 151,936 x 2,048 in 3.3 ms of products at 88 to 90 % of the tensor pipe; with 100 rows, where d_hidden alone would be four tiles,
 // 33 us for 32,000 x 1,024.
 template <int kCtas, int kN>
 struct HeadGradsJob {

@@ -244,8 +244,8 @@ __global__ void __launch_bounds__(kOrthThreads) orth_load_kernel(const __grid_co
 // All steps of all matrices in one launch.  Tiles are numbered step by step and in a step phase by phase over the whole list; one
 // that needs the results of the phase before waits for that phase of its own matrix only, so that the tail of one matrix's phase runs
 // beside the other matrices' tiles, and a phase of a single matrix costs a signal through the L2 instead of a launch.
-// Large lists are bound by the tensor pipe (14 matrices of two blocks of width 2,048: 83 % busy, 2.75 ms); small ones by the
-// chain of three phases a step, each 6 to 16 us from the first load to the last count (256 x 1,024 in fp32: 154 us for five steps, norm and load 15 of them).
+// Large lists are bound by the tensor pipe (14 matrices of two blocks of width 2,048: 81 to 83 % busy, 2.64 to 2.75 ms); small ones by the
+// chain of three phases a step, each 6 to 16 us from the first load to the last count (256 x 1,024 in fp32: 157 us for five steps, norm and load 15 of them).
 enum OrthPhase { kOrthGram = 0, kOrthPoly = 1, kOrthApply = 2 };
 constexpr int kOrthMostSteps = 16;
 

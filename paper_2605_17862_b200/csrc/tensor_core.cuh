@@ -7,14 +7,14 @@
 // there, beside the next products.  With kCtas = 2 a pair of CTAs works on one tile: each holds half of both operands and half the
 // accumulator's rows, and shared memory is read once for twice the products (cta_group::2; 64 instead of 96 bytes per SM and
 // cycle at 256 columns, which with the copies coming in is what 1-CTA tiles are short of: 14 matrices of width 2,048 take 3.3 ms in
-// tiles of 256 x 256 on pairs, 4.0 ms in tiles of 128 x 128).  Bound by the tensor pipe: 96 % busy at 4,096 x 151,936 x 2,048, at the
-// 1.38 GHz that the power cap leaves.
+// tiles of 256 x 256 on pairs, 4.0 ms in tiles of 128 x 128).  Bound by the tensor pipe: 93 to 96 % busy at 4,096 x 151,936 x 2,048, at the
+// 1.38 to 1.46 GHz that the power cap leaves.
 //
 // Operands are 16-bit (both bf16 or both fp16), products and sums fp32.  Either operand may lie with the contraction along
 // its rows ("K-major") or across them; both come in boxes of 64 elements to a row, so that nothing is ever transposed.
 //
 // A matrix instruction does not round what it adds to the accumulator, it cuts it off: over K terms sums come out smaller by up to
-// K / 16 units of 2^-24.  A tile may therefore have its accumulator taken out every `chunk` blocks and added up in registers,
+// K / 16 units of 2^-24.  A tile has its accumulator taken out every `chunk` blocks (accumulators.cuh) and added up in registers,
 // rounded to nearest: every eight blocks takes 1.5 % more time (the same case) and an error of 2.6e-7 instead of 1.2e-6.
 //
 // Every wait is bounded.  One that runs out raises a flag, the role leaves its loop, the others run out in turn, copies and
